@@ -344,6 +344,110 @@ curdkv_status curdkv_cache_step(const curdkv_cache* cache, const void* K_new, co
                                 int32_t budget, int32_t num_sink, int32_t window, void* workspace,
                                 size_t workspace_bytes, void* cuda_stream);
 
+/* ---- Serving the compressed cache (no counterpart in the paper): rows held in 4 bits, and
+ * attention for generation.
+ *
+ * curdkv_qcache holds, per (sequence, KV head), rows of K and V of 128 channels in 4 bits:
+ * 160 bytes for a row of both instead of 512.  Every row has four groups of 32 consecutive
+ * channels; a group with least value lo and greatest hi is held as
+ *   scale = bf16((hi - lo) / 15)   fp32 subtraction and division, rounded to bf16 (nearest even)
+ *   zero  = lo                      (a bf16 value: no rounding)
+ *   code  = rint((x - zero) / scale), ties to even, limited to 0 .. 15 (0 when scale is 0),
+ *           decided as in 64-bit arithmetic
+ * and stands for scale * code + zero.  A group that holds a NaN or an infinity, or whose range
+ * overflows fp32, comes back as NaN.  A row's codes are 64 bytes: channel 32g + 8t + u of K sits in
+ * nibble u (lowest first) of 32-bit word 4t + g, channel 32g + 4t + u of V in nibble u of 16-bit word
+ * 4t + g. */
+typedef struct curdkv_qcache {
+  void* K_codes;            /* uint8 [rows][64], 16-byte aligned, as are the next three     */
+  void* V_codes;
+  void* K_meta;             /* bf16 [rows][4][2]: scale and zero of each group              */
+  void* V_meta;
+  int32_t* count;           /* int32 [batch*kv_heads]: rows held; the caller zeroes it at start */
+  const int32_t* row_start; /* NULL: head p owns rows p*capacity .. (p+1)*capacity - 1.  Else int32
+                               [batch*kv_heads + 1], ascending: head p owns rows row_start[p] ..
+                               row_start[p+1] - 1 (heads of different sizes one behind the other) */
+  int64_t capacity;         /* rows per head (row_start NULL), else rows of the whole cache; at
+                               most 2^31 - 1                                                 */
+  int32_t batch, kv_heads;
+} curdkv_qcache;
+
+/* Quantises rows of K and V (bf16, as in curdkv_score; d = 128) into the cache, slot 0 upwards,
+ * and sets count.  What a cache held before is gone.
+ *   idx           NULL: the desc->seqlens / n_max rows of every head in order.  Else the rows to hold,
+ *                 as curdkv_select writes them: int32 [batch][kv_heads][idx_stride] with head_offsets
+ *                 NULL, or packed with head p's list starting at idx[head_offsets[p]]
+ *   head_counts   int32 [batch*kv_heads] entries of each list (required with idx)
+ *   workspace     NULL, or at least 256 bytes, 256-byte aligned, whose status word collects (it is
+ *                 not cleared): CURDKV_DEV_BAD_INDEX -- an index outside [0, n_b), whose slot becomes a
+ *                 row of zeros, a count beyond its list, row_start that does not ascend;
+ *                 CURDKV_DEV_CACHE_FULL -- a list longer than its head's room, cut to it
+ * One launch. */
+curdkv_status curdkv_qcache_store(const curdkv_qcache* cache, const void* K, const void* V,
+                                  const curdkv_desc* desc, const int32_t* idx, int64_t idx_stride,
+                                  const int32_t* head_counts, const int32_t* head_offsets,
+                                  void* workspace, void* cuda_stream);
+
+/* Holds K_new, V_new (desc: n_max = rows offered per head, seqlens = device int32 [batch] rows that
+ * are real, or NULL) behind the held rows and moves count.  Rows that do not fit are dropped and
+ * flagged (CURDKV_DEV_CACHE_FULL).  workspace as in curdkv_qcache_store.  One launch for up to 64 rows
+ * per head, two above. */
+curdkv_status curdkv_qcache_append(const curdkv_qcache* cache, const void* K_new, const void* V_new,
+                                   const curdkv_desc* desc, void* workspace, void* cuda_stream);
+
+/* Held rows back as bf16 (the value above, rounded once).
+ *   idx NULL, rows > 0    K_out, V_out bf16 [batch*kv_heads][rows][128]: slots 0 .. min(rows, count) - 1
+ *   idx NULL, rows = 0    outputs laid out as the cache's rows are
+ *   idx                   int32 [batch*kv_heads][rows]: output row t is slot idx[..][t]; a negative entry
+ *                         is passed over, one at or beyond count is flagged (CURDKV_DEV_BAD_INDEX)
+ * Output rows that have no slot are left untouched.  The outputs may not be the rows that the cache
+ * was stored from while another call still reads them.  workspace as in curdkv_qcache_store. */
+curdkv_status curdkv_qcache_read(const curdkv_qcache* cache, const int32_t* idx, int64_t rows,
+                                 void* K_out, void* V_out, void* workspace, void* cuda_stream);
+
+/* O = softmax(scale Q K^T) V over the held rows of every head, for generation: few query rows per
+ * KV head (the queries of a GQA group stacked along q_rows), every one sees every held row.
+ *   Q, O   bf16 [batch][kv_heads][q_rows][128] with element strides (multiples of 8, channels
+ *          contiguous, 16-byte aligned); O may not overlap Q
+ *   lse    NULL, or fp32 [batch][kv_heads][q_rows]: log of each row's sum of exponentials (natural,
+ *          of the scaled logits), for joining partial attentions
+ *   scale  finite, >= 0
+ * A head without rows gives O = 0 and lse = -inf.  Products of codes are exact, sums and the softmax
+ * are fp32; the weights are rounded to fp16 (11 bits) before they multiply the values, O is rounded
+ * once.  Keys are shared out over the SMs and the shares joined in a fixed order by a second launch
+ * (none where one share suffices).  Workspace (256-byte aligned): its status word collects (it is not
+ * cleared) CURDKV_DEV_BAD_INDEX, a count or row_start out of range; two calls that may overlap need
+ * a workspace each. */
+size_t curdkv_qcache_attention_workspace_bytes(const curdkv_qcache* cache, int32_t q_rows);
+curdkv_status curdkv_qcache_attention(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h,
+                                      int64_t q_stride_n, const curdkv_qcache* cache, float scale, void* O,
+                                      int64_t o_stride_b, int64_t o_stride_h, int64_t o_stride_n, float* lse,
+                                      void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Attention with a sliding window and sinks, causal: the rows that curdkv_select always keeps, as an
+ * attention of their own.  Sequence b has n_b = desc->seqlens[b] (or n_max) cached rows, its own new
+ * ones among them, and t_b = q_lens[b] (or q_rows) query tokens at the last t_b positions: query i
+ * stands at position n_b - t_b + i and sees the rows j <= its position with
+ *   j > position - window   or   j < num_sink.
+ *   Q, O      bf16 [batch][q_heads][q_rows][128] with element strides (multiples of 8, channels
+ *             contiguous, 16-byte aligned); query head q reads KV head q / (q_heads / kv_heads);
+ *             O may not overlap Q
+ *   q_lens    device int32 [batch] (clamped to [0, q_rows]), or NULL; output rows i >= t_b are left
+ *             untouched
+ *   window    >= 0; n_max or more is plain causal attention; num_sink >= 0
+ *   lse       NULL, or fp32 [batch][q_heads][q_rows], as above
+ *   scale     finite, >= 0
+ * A query that sees nothing (window = 0 without sinks, or a position below 0 because t_b > n_b)
+ * gives O = 0 and lse = -inf.  Rows at or beyond n_b are never used, whatever they hold; rows below it
+ * must be finite.  Softmax and sums in fp32, weights rounded to bf16 before they multiply the values,
+ * O rounded once.  d = 128.  workspace as in curdkv_qcache_attention. */
+size_t curdkv_attention_window_workspace_bytes(const curdkv_desc* desc, int32_t q_rows);
+curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h,
+                                      int64_t q_stride_n, const int32_t* q_lens, const void* K, const void* V,
+                                      const curdkv_desc* desc, int32_t num_sink, int32_t window, float scale,
+                                      void* O, int64_t o_stride_b, int64_t o_stride_h, int64_t o_stride_n,
+                                      float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* GQA (Sec. 3.2): query head q uses KV head q / (q_heads / kv_heads).  Writes
  * kv_head_of_q int32 [q_heads] (device) so that attention consumers can index
  * the shared selection without replicating the compacted cache. */

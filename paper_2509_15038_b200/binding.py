@@ -30,6 +30,9 @@ EXPORTS = (
     "curdkv_cache_compress", "curdkv_attention_workspace_bytes", "curdkv_attention_out",
     "curdkv_eviction_loss", "curdkv_gqa_expand", "curdkv_cache_compress_inplace",
     "curdkv_selftest_bounded_wait", "curdkv_selftest_gather_wait", "curdkv_compress", "curdkv_cache_step",
+    "curdkv_qcache_store", "curdkv_qcache_append", "curdkv_qcache_read",
+    "curdkv_qcache_attention_workspace_bytes", "curdkv_qcache_attention",
+    "curdkv_attention_window_workspace_bytes", "curdkv_attention_window",
 )
 
 
@@ -58,6 +61,16 @@ class Cache(ctypes.Structure):
         ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("raw", ctypes.c_void_p),
         ("pos", ctypes.c_void_p), ("count", ctypes.c_void_p), ("total", ctypes.c_void_p),
         ("capacity", ctypes.c_int32),
+    ]
+
+
+class QCache(ctypes.Structure):
+    """``curdkv_qcache``: device pointers of one 4-bit cache."""
+
+    _fields_ = [
+        ("K_codes", ctypes.c_void_p), ("V_codes", ctypes.c_void_p), ("K_meta", ctypes.c_void_p),
+        ("V_meta", ctypes.c_void_p), ("count", ctypes.c_void_p), ("row_start", ctypes.c_void_p),
+        ("capacity", ctypes.c_int64), ("batch", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
     ]
 
 
@@ -123,6 +136,23 @@ def load():
                                          ctypes.c_float, i32, vp, vp, ctypes.c_size_t, vp]
     lib.curdkv_eviction_loss.restype = ctypes.c_int
     lib.curdkv_eviction_loss.argtypes = [vp, vp, i32, i64, vp, vp, vp]
+    qp, f32 = ctypes.POINTER(QCache), ctypes.c_float
+    lib.curdkv_qcache_store.restype = ctypes.c_int
+    lib.curdkv_qcache_store.argtypes = [qp, vp, vp, dp, vp, i64, vp, vp, vp, vp]
+    lib.curdkv_qcache_append.restype = ctypes.c_int
+    lib.curdkv_qcache_append.argtypes = [qp, vp, vp, dp, vp, vp]
+    lib.curdkv_qcache_read.restype = ctypes.c_int
+    lib.curdkv_qcache_read.argtypes = [qp, vp, i64, vp, vp, vp, vp]
+    lib.curdkv_qcache_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.curdkv_qcache_attention_workspace_bytes.argtypes = [qp, i32]
+    lib.curdkv_qcache_attention.restype = ctypes.c_int
+    lib.curdkv_qcache_attention.argtypes = [vp, i32, i64, i64, i64, qp, f32, vp, i64, i64, i64, vp, vp,
+                                            ctypes.c_size_t, vp]
+    lib.curdkv_attention_window_workspace_bytes.restype = ctypes.c_size_t
+    lib.curdkv_attention_window_workspace_bytes.argtypes = [dp, i32]
+    lib.curdkv_attention_window.restype = ctypes.c_int
+    lib.curdkv_attention_window.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, dp, i32, i32, f32, vp, i64, i64,
+                                            i64, vp, vp, ctypes.c_size_t, vp]
     lib.curdkv_selftest_bounded_wait.restype = ctypes.c_int
     lib.curdkv_selftest_bounded_wait.argtypes = [ctypes.c_uint64, vp, vp]
     lib.curdkv_selftest_gather_wait.restype = ctypes.c_int
@@ -174,10 +204,12 @@ def make_desc(K: torch.Tensor, V: torch.Tensor, r: int, *, q_heads: Optional[int
                                 or not seqlens.is_contiguous()):
         raise ValueError("seqlens must be a contiguous int32 tensor of length B")
     B, H, n, d = K.shape
-    return Desc(B, H, q_heads or H, n, d, int(r),
+    desc = Desc(B, H, q_heads or H, n, d, int(r),
                 K.stride(0), K.stride(1), K.stride(2), V.stride(0), V.stride(1), V.stride(2),
                 seqlens.data_ptr() if seqlens is not None else None,
                 int(score_mode), int(use_projection), int(raw_scores), int(whiten), float(ridge))
+    desc.seqlens_tensor = seqlens        # the lengths live as long as the descriptor that points at them
+    return desc
 
 
 def workspace_bytes(desc: Desc, max_budget: int = 0, adaptive: bool = False) -> int:
@@ -447,6 +479,218 @@ def curdkv_eviction_loss(O_full, O_comp):
                                        _ptr(ref), _stream())
     _check(code, "curdkv_eviction_loss")
     return loss, ref
+
+
+# ---- serving: the 4-bit cache and the attention with a sliding window ---------------------------
+
+def _on_device(what: str, first: torch.Tensor, *rest: Optional[torch.Tensor]) -> int:
+    """Index of the device that every given tensor lies on, which has to be the current one (the
+    calls launch on its current stream)."""
+    dev = first.device
+    if dev.type != "cuda":
+        raise ValueError(f"{what}: tensors must be on a CUDA device")
+    for t in rest:
+        if t is not None and t.device != dev:
+            raise ValueError(f"{what}: tensors are on {dev} and {t.device}")
+    if dev.index != torch._C._cuda_getDevice():
+        raise ValueError(f"{what}: tensors are on {dev}, which is not the current device")
+    return dev.index
+
+
+def _int32(what: str, t: Optional[torch.Tensor], numel: Optional[int] = None) -> None:
+    if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or (numel is not None and t.numel() != numel)):
+        raise ValueError(f"{what} must be a contiguous int32 tensor" + (f" of {numel} entries" if numel is not None else ""))
+
+
+def _status_buffer(what: str, t: Optional[torch.Tensor]) -> None:
+    if t is not None and (not t.is_contiguous() or t.numel() * t.element_size() < 256):
+        raise ValueError(f"{what}: workspace must be contiguous and hold at least 256 bytes")
+
+
+def _raw_stream(index: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+class QuantCache:
+    """Torch-owned buffers of one 4-bit cache plus the ``curdkv_qcache`` view of them.
+
+    ``QuantCache(batch, kv_heads, capacity)`` gives every head ``capacity`` rows.  With ``row_start``
+    (int32 ``[batch * kv_heads + 1]``, ascending) the heads lie one behind the other, ``capacity`` rows in
+    all.  Rows are 128 channels: codes uint8 ``[..., 64]`` and meta bf16 ``[..., 4, 2]`` (scale, zero)."""
+
+    def __init__(self, batch: int, kv_heads: int, capacity: int, *, row_start: Optional[torch.Tensor] = None,
+                 device="cuda"):
+        rows = (capacity,) if row_start is not None else (batch, kv_heads, capacity)
+        codes = [torch.zeros(rows + (64,), dtype=torch.uint8, device=device) for _ in range(2)]
+        meta = [torch.zeros(rows + (4, 2), dtype=torch.bfloat16, device=device) for _ in range(2)]
+        count = torch.zeros((batch * kv_heads,), dtype=torch.int32, device=device)
+        self._set(*codes, *meta, count, batch, kv_heads, capacity, row_start)
+
+    @classmethod
+    def of(cls, K_codes, V_codes, K_meta, V_meta, count, batch: int, kv_heads: int, *,
+           row_start: Optional[torch.Tensor] = None) -> "QuantCache":
+        """A cache over buffers that exist already (contiguous, laid out as above)."""
+        self = cls.__new__(cls)
+        self._set(K_codes, V_codes, K_meta, V_meta, count, batch, kv_heads,
+                  K_codes.shape[0] if row_start is not None else K_codes.shape[2], row_start)
+        return self
+
+    def _set(self, K_codes, V_codes, K_meta, V_meta, count, batch, kv_heads, capacity, row_start):
+        rows = (capacity,) if row_start is not None else (batch, kv_heads, capacity)
+        for t, tail, dtype in ((K_codes, (64,), torch.uint8), (V_codes, (64,), torch.uint8),
+                               (K_meta, (4, 2), torch.bfloat16), (V_meta, (4, 2), torch.bfloat16)):
+            if tuple(t.shape) != rows + tail or t.dtype != dtype or not t.is_contiguous():
+                raise ValueError(f"a buffer of a QuantCache must be contiguous {dtype} {rows + tail}")
+        _int32("count", count, batch * kv_heads)
+        _int32("row_start", row_start, batch * kv_heads + 1)
+        self.K_codes, self.V_codes, self.K_meta, self.V_meta = K_codes, V_codes, K_meta, V_meta
+        self.count, self.row_start = count, row_start
+        self.batch, self.kv_heads, self.capacity, self.device = batch, kv_heads, capacity, K_codes.device
+        for t in (V_codes, K_meta, V_meta, count, row_start):
+            if t is not None and t.device != self.device:
+                raise ValueError("the buffers of a QuantCache must lie on one device")
+        self.c = QCache(K_codes.data_ptr(), V_codes.data_ptr(), K_meta.data_ptr(), V_meta.data_ptr(),
+                        count.data_ptr(), None if row_start is None else row_start.data_ptr(),
+                        capacity, batch, kv_heads)
+        self._ref = ctypes.byref(self.c)
+
+
+def curdkv_qcache_store(cache: QuantCache, K, V, desc: Desc, idx=None, head_counts=None, head_offsets=None, *,
+                        packed: bool = False, workspace: Optional[torch.Tensor] = None) -> None:
+    """Rows of K, V (all, or those a selection names, laid out as :func:`curdkv_select` returns them; ``packed``
+    for an adaptive one) quantised into ``cache`` from slot 0; sets ``cache.count``."""
+    dev = _on_device("curdkv_qcache_store", cache.K_codes, K, V, idx, head_counts, head_offsets, workspace)
+    P = cache.batch * cache.kv_heads
+    _int32("idx", idx)
+    _int32("head_counts", head_counts, P)
+    _status_buffer("curdkv_qcache_store", workspace)
+    stride = 0
+    if idx is not None and packed:
+        if head_offsets is None:
+            raise ValueError("a packed idx needs head_offsets")
+        _int32("head_offsets", head_offsets, P + 1)
+    elif idx is not None:
+        if P > 0 and idx.numel() % P != 0:
+            raise ValueError("idx must be [batch, kv_heads, budget]")
+        stride = idx.numel() // max(P, 1)
+    code = load().curdkv_qcache_store(cache._ref, _ptr(K), _ptr(V), ctypes.byref(desc), _ptr(idx), stride,
+                                      _ptr(head_counts) if idx is not None else None,
+                                      _ptr(head_offsets) if idx is not None and packed else None,
+                                      _ptr(workspace), _raw_stream(dev))
+    _check(code, "curdkv_qcache_store")
+
+
+def curdkv_qcache_append(cache: QuantCache, K_new, V_new, *, t_new: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None) -> None:
+    """K_new, V_new ``[B, Hkv, t, 128]`` quantised behind the held rows (``t_new`` int32 ``[B]``: real rows)."""
+    dev = _on_device("curdkv_qcache_append", cache.K_codes, K_new, V_new, t_new, workspace)
+    _status_buffer("curdkv_qcache_append", workspace)
+    desc = make_desc(K_new, V_new, 1, seqlens=t_new)
+    code = load().curdkv_qcache_append(cache._ref, _ptr(K_new), _ptr(V_new), ctypes.byref(desc), _ptr(workspace),
+                                       _raw_stream(dev))
+    _check(code, "curdkv_qcache_append")
+
+
+def curdkv_qcache_read(cache: QuantCache, idx: Optional[torch.Tensor] = None, *, K_out=None, V_out=None,
+                       workspace: Optional[torch.Tensor] = None):
+    """Held rows as bf16: laid out as the cache's rows are, or the slots ``idx`` (int32 ``[B, Hkv, rows]``, negative
+    entries passed over) names.  Rows without a slot keep what the outputs hold (zeros where this call makes them)."""
+    dev = _on_device("curdkv_qcache_read", cache.K_codes, idx, K_out, V_out, workspace)
+    _status_buffer("curdkv_qcache_read", workspace)
+    _int32("idx", idx)
+    P = cache.batch * cache.kv_heads
+    if idx is not None:
+        if P > 0 and idx.numel() % P != 0:
+            raise ValueError("idx must be [batch, kv_heads, rows]")
+        rows = idx.numel() // max(P, 1)
+        shape = (cache.batch, cache.kv_heads, rows, 128)
+    elif cache.row_start is not None:
+        rows, shape = 0, (cache.capacity, 128)
+    else:
+        rows, shape = cache.capacity, (cache.batch, cache.kv_heads, cache.capacity, 128)
+    out = []
+    for t in (K_out, V_out):
+        if t is None:
+            t = torch.zeros(shape, dtype=torch.bfloat16, device=cache.device)
+        elif t.dtype != torch.bfloat16 or not t.is_contiguous() or tuple(t.shape) != shape:
+            raise ValueError(f"outputs must be contiguous bf16 {shape}")
+        out.append(t)
+    if idx is not None and rows == 0:
+        return out[0], out[1]
+    code = load().curdkv_qcache_read(cache._ref, _ptr(idx), rows, _ptr(out[0]), _ptr(out[1]), _ptr(workspace),
+                                     _raw_stream(dev))
+    _check(code, "curdkv_qcache_read")
+    return out[0], out[1]
+
+
+def qcache_attention_workspace(cache: QuantCache, q_rows: int) -> torch.Tensor:
+    nbytes = int(load().curdkv_qcache_attention_workspace_bytes(cache._ref, int(q_rows)))
+    if nbytes == 0:
+        raise ValueError("invalid shape for curdkv_qcache_attention")
+    return torch.zeros((nbytes,), dtype=torch.uint8, device=cache.device)
+
+
+def attention_window_workspace(desc: Desc, q_rows: int, device="cuda") -> torch.Tensor:
+    nbytes = int(load().curdkv_attention_window_workspace_bytes(ctypes.byref(desc), int(q_rows)))
+    if nbytes == 0:
+        raise ValueError("invalid shape for curdkv_attention_window")
+    return torch.zeros((nbytes,), dtype=torch.uint8, device=device)
+
+
+def _queries(what, Q, O, lse):
+    if Q.dtype != torch.bfloat16 or Q.dim() != 4 or Q.stride(3) != 1 or Q.shape[3] != 128:
+        raise ValueError(f"{what}: Q must be bf16 [B, H, rows, 128] with a contiguous last axis")
+    if O is None:
+        O = torch.empty(Q.shape, dtype=torch.bfloat16, device=Q.device)
+    elif O.dtype != torch.bfloat16 or O.shape != Q.shape or O.stride(3) != 1:
+        raise ValueError(f"{what}: O must be bf16 of Q's shape with a contiguous last axis")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != Q.shape[:3] or not lse.is_contiguous()):
+        raise ValueError(f"{what}: lse must be contiguous fp32 [B, H, rows]")
+    return O
+
+
+def curdkv_qcache_attention(Q, cache: QuantCache, *, scale: float, O=None, lse=None,
+                            workspace: Optional[torch.Tensor] = None):
+    """O = softmax(scale Q K^T) V over the held rows.  Q bf16 ``[B, Hkv, q_rows, 128]``, the queries of a GQA group
+    stacked along q_rows; ``lse`` fp32 ``[B, Hkv, q_rows]`` receives the log sums where given.  Returns (O, workspace)."""
+    O = _queries("curdkv_qcache_attention", Q, O, lse)
+    if Q.shape[0] != cache.batch or Q.shape[1] != cache.kv_heads:
+        raise ValueError("curdkv_qcache_attention: Q and the cache differ in batch or heads")
+    m = Q.shape[2]
+    if workspace is None:
+        workspace = qcache_attention_workspace(cache, m)
+    dev = _on_device("curdkv_qcache_attention", cache.K_codes, Q, O, lse, workspace)
+    qb, qh, qn, _ = Q.stride()
+    ob, oh, on, _ = O.stride()
+    code = load().curdkv_qcache_attention(Q.data_ptr(), m, qb, qh, qn, cache._ref, scale, O.data_ptr(), ob, oh, on,
+                                          None if lse is None else lse.data_ptr(), workspace.data_ptr(),
+                                          workspace.numel(), _raw_stream(dev))
+    _check(code, "curdkv_qcache_attention")
+    return O, workspace
+
+
+def curdkv_attention_window(Q, K, V, desc: Desc, window: int, *, num_sink: int = 0, scale: float,
+                            q_lens: Optional[torch.Tensor] = None, O=None, lse=None,
+                            workspace: Optional[torch.Tensor] = None):
+    """Causal attention over the last ``window`` rows and the first ``num_sink``.  Q bf16 ``[B, Hq, t, 128]``: the last
+    ``q_lens`` (int32 ``[B]``, default t) positions of each sequence of ``desc``; query rows beyond leave O untouched.
+    Returns (O, workspace)."""
+    O = _queries("curdkv_attention_window", Q, O, lse)
+    if Q.shape[0] != desc.batch or Q.shape[1] != desc.q_heads:
+        raise ValueError("curdkv_attention_window: Q and the descriptor differ in batch or query heads")
+    _int32("q_lens", q_lens, desc.batch)
+    t = Q.shape[2]
+    if workspace is None:
+        workspace = attention_window_workspace(desc, t, device=Q.device)
+    dev = _on_device("curdkv_attention_window", Q, K, V, O, lse, q_lens, workspace)
+    qb, qh, qn, _ = Q.stride()
+    ob, oh, on, _ = O.stride()
+    code = load().curdkv_attention_window(Q.data_ptr(), t, qb, qh, qn, None if q_lens is None else q_lens.data_ptr(),
+                                          K.data_ptr(), V.data_ptr(), ctypes.byref(desc), num_sink, window, scale,
+                                          O.data_ptr(), ob, oh, on, None if lse is None else lse.data_ptr(),
+                                          workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
+    _check(code, "curdkv_attention_window")
+    return O, workspace
 
 
 def curdkv_profile_next_score(start: torch.cuda.Event, stop: torch.cuda.Event) -> None:

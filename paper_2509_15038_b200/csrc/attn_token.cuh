@@ -1,0 +1,688 @@
+// Attention of a few query rows per KV head over a long cache: the generation step.  Two caches,
+// one kernel: rows held in 4 bits (curdkv_qcache_attention) and bf16 rows of which a sliding window
+// and the first tokens are visible (curdkv_attention_window with few queries).
+//
+// What bounds it is the cache's bytes, each read once.  A CTA takes one (head, block of query rows,
+// share of the keys); its warps take tiles of the share's keys in turn, each warp with its own ring
+// of tiles in shared memory, filled by 16-byte asynchronous copies (rows that do not exist are
+// filled with zeros, so nothing behind a head's last row is ever read).  No barrier stands in the
+// key loop.  Per 16 keys a warp forms
+//   S^T [16 keys x 8 queries] = K Q^T        m16n8k16, keys as the M side: with the few queries of
+//   O^T [128 x 8 queries]    += V^T P^T      a KV head as N = 8 half the instructions that a layout
+//                                            with 16 padded queries as M would need
+// and between the two the online softmax: a warp's running maximum moves only when some logit
+// exceeds it by more than 2^kSlack (one vote per tile), and since S^T and O^T hold a query in the
+// same lanes the rescale needs no exchange.  P^T reaches the second product's operand layout by two
+// 8x8 transposes (movmatrix).  Sums, maxima and accumulators are fp32; the weights enter the second
+// product as fp16 (4-bit rows) or bf16 (bf16 rows), at most 2^-11 / 2^-8 of each weight off by
+// half a step; the row sum is taken over the unrounded weights.
+//
+// 4-bit rows cost five integer instructions per eight values and no conversion: a code left in the
+// low bits of a half is the fp16 subnormal code * 2^-24 (or code * 2^-20 one nibble up), which the
+// tensor cores multiply exactly.  The scales are applied outside: on the K side to the products of
+// each group of 32 channels (S = sum_g s_g (codes_g . q_g) + sum_g z_g sum(q_g), the second sum one
+// more matrix instruction whose A operand is the zeros), on the V side to the weights (one set per
+// group, P_g = p * s_g), with the zeros as a further instruction.  V's scales are brought to fp16
+// relative to a power of two per warp that follows the largest value seen, so any bf16 range works.
+#pragma once
+#include "qcache.cuh"
+
+namespace curdkv {
+namespace token {
+
+constexpr int kWarps = 8;
+constexpr int kThreads = kWarps * 32;
+constexpr int kStages = 3;
+constexpr float kSlack = 6.f;        // log2 units a logit may exceed the running maximum
+constexpr float kLift = 8.f;         // fp16 weights are 2^(x - m + kLift): at most 2^14, and exact
+                                     // to 11 bits down to 2^-22 of the largest
+
+struct Args {
+  const __nv_bfloat16* Q;            // [batch][q_heads][q_n][128], strides in elements
+  int64_t q_sb, q_sh, q_sn;
+  __nv_bfloat16* O;
+  int64_t o_sb, o_sh, o_sn;
+  float* lse;                        // [batch][q_heads][q_n] or nullptr
+  int heads, group, q_n;             // query heads per KV head; query tokens
+  int rows, blocks, splits;          // rows = group * q_n, row r = token r / group, head r % group
+  float scale_log2;                  // scale * log2(e)
+  // 4-bit rows
+  qcache::View cache;
+  // bf16 rows
+  KvView K, V;
+  const int32_t* seqlens;
+  const int32_t* q_lens;
+  int n_max, num_sink, window;
+  // partial results, one per (head, block, split): [8 NT] maxima and sums, [8 NT][128] sums of values
+  float* part_ml;
+  float* part_o;
+  uint32_t* status;
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) {
+  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+// 16 bytes global -> shared, zeros when `live` is false (nothing is read then).
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                        uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                         uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// 2^(e - 127) for 1 <= e <= 253, and 0 below
+__device__ __forceinline__ float pow2_biased(int e) { return __int_as_float(e > 0 ? e << 23 : 0); }
+
+template <bool Q4>
+struct Tile {                                              // one warp's stage
+  static constexpr int kKeys = Q4 ? 32 : 16;
+  static constexpr int kK = 0;
+  static constexpr int kV = kKeys * (Q4 ? qcache::kRowBytes : 256);
+  static constexpr int kKMeta = 2 * kV;
+  static constexpr int kVMeta = kKMeta + (Q4 ? kKeys * qcache::kMetaBytes : 0);
+  static constexpr int kBytes = kVMeta + (Q4 ? kKeys * qcache::kMetaBytes : 0);
+  // V's scales and zeros in fp16, pairs of keys side by side: [key pair][group] each
+  static constexpr int kScaled = Q4 ? kKeys * 8 * 2 : 0;
+  static constexpr int kWarpBytes = kStages * kBytes + kScaled;
+};
+template <bool Q4, int NT>
+constexpr int smem_bytes() {
+  constexpr int ring = kWarps * Tile<Q4>::kWarpBytes;
+  constexpr int merge = kWarps * 8 * NT * 132 * 4;         // the warps' sums meet in the ring's space
+  return ring > merge ? ring : merge;
+}
+
+// Keys a block of query rows sees, as a run of `total` positions u: row u for u < sinks, row
+// first + (u - sinks) above.
+struct Seen {
+  int sinks, first, total;
+  __device__ __forceinline__ int row(int u) const { return u < sinks ? u : first + (u - sinks); }
+};
+
+template <bool Q4, int NT>
+__global__ void __launch_bounds__(kThreads, 1) attend_kernel(const Args a) {
+  using T = Tile<Q4>;
+  constexpr int KB = T::kKeys / 16;
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ float s_m[kWarps][8 * NT], s_l[kWarps][8 * NT];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const int split = blockIdx.x % a.splits, pb = blockIdx.x / a.splits;
+  const int p = pb / a.blocks, blk = pb % a.blocks;
+  const int b = p / a.heads, h = p % a.heads;
+
+  // ------------------------------------------------------------ the keys of this block
+  const int r0 = blk * 8 * NT, r1 = min(a.rows, r0 + 8 * NT);   // query rows [r0, r1)
+  Seen seen;
+  int64_t first_row = 0;
+  int pos0 = 0, q_live = a.q_n;                            // position of query token 0; tokens that exist
+  if (Q4) {
+    int room;
+    const bool ok = qcache::rows_of(a.cache, p, first_row, room);
+    const int was = a.cache.count[p], held = was < 0 ? 0 : (was > room ? room : was);
+    if (blk == 0 && split == 0 && tid == 0 && (!ok || was != held)) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
+    seen.sinks = 0;
+    seen.first = 0;
+    seen.total = held;
+  } else {
+    const int n = seq_len_of(a.seqlens, b, a.n_max);
+    if (a.q_lens != nullptr) q_live = min(max(a.q_lens[b], 0), a.q_n);
+    pos0 = n - q_live;
+    const int i0 = r0 / a.group, i1 = min((r1 - 1) / a.group, q_live - 1);   // tokens of the block
+    const int hi = i1 >= i0 ? max(pos0 + i1 + 1, 0) : 0;   // keys [0, hi) may be seen
+    const int lo = (int)min((int64_t)hi, max((int64_t)0, (int64_t)pos0 + i0 + 1 - a.window));
+    seen.sinks = min(a.num_sink, lo);
+    seen.first = lo;
+    seen.total = seen.sinks + hi - lo;
+  }
+  // tiles of this split, and of this warp among them
+  const int tiles = (seen.total + T::kKeys - 1) / T::kKeys;
+  const int t_lo = (int)((int64_t)split * tiles / a.splits), t_hi = (int)((int64_t)(split + 1) * tiles / a.splits);
+
+  // ------------------------------------------------------------ the ring of this warp
+  unsigned char* ring = smem + warp * T::kWarpBytes;
+  const uint32_t ring_u = smem_addr(ring);
+  const __nv_bfloat16 *kb = nullptr, *vb = nullptr;
+  if (!Q4) {
+    kb = a.K.base + b * a.K.stride_b + h * a.K.stride_h;
+    vb = a.V.base + b * a.V.stride_b + h * a.V.stride_h;
+  }
+  auto fetch = [&](int tile, int stage) {
+    const uint32_t dst = ring_u + stage * T::kBytes;
+    const int u0 = tile * T::kKeys;
+    if (Q4) {
+      // two 64-byte rows share a 128-byte line of shared memory; the line's eight 16-byte places are
+      // permuted by the line number so that both products' reads are free of bank conflicts
+      const int64_t row0 = first_row + u0;
+      const uint8_t* ks = a.cache.K_codes + row0 * qcache::kRowBytes;
+      const uint8_t* vs = a.cache.V_codes + row0 * qcache::kRowBytes;
+      const int left = seen.total - u0;                    // rows of the tile that exist (or more)
+#pragma unroll
+      for (int i = 0; i < T::kKeys * 4 / 32; ++i) {
+        const int c = i * 32 + lane;                       // 16-byte chunk of the tile
+        const int line = c >> 3;
+        const uint32_t at = (uint32_t)(line * 128 + (((c & 7) ^ (2 * (line & 3))) * 16));
+        const bool live = (c >> 2) < left;
+        copy16(dst + T::kK + at, live ? ks + c * 16 : a.cache.K_codes, live);
+        copy16(dst + T::kV + at, live ? vs + c * 16 : a.cache.V_codes, live);
+      }
+      const bool live = lane < left;
+      const uint32_t* km = a.cache.K_meta + (row0 + lane) * 4;
+      const uint32_t* vm = a.cache.V_meta + (row0 + lane) * 4;
+      copy16(dst + T::kKMeta + lane * 16, live ? km : a.cache.K_meta, live);
+      copy16(dst + T::kVMeta + lane * 16, live ? vm : a.cache.V_meta, live);
+    } else {
+#pragma unroll
+      for (int i = 0; i < T::kKeys / 2; ++i) {
+        const int key = 2 * i + (lane >> 4), c = lane & 15;
+        const int u = u0 + key;
+        const bool live = u < seen.total;
+        const int64_t j = live ? seen.row(u) : 0;
+        const uint32_t at = (uint32_t)(key * 256 + ((c ^ (key & 7)) * 16));
+        copy16(dst + T::kK + at, live ? kb + j * a.K.stride_n + c * 8 : kb, live);
+        copy16(dst + T::kV + at, live ? vb + j * a.V.stride_n + c * 8 : vb, live);
+      }
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) {
+    if (t_lo + warp + s * kWarps < t_hi) fetch(t_lo + warp + s * kWarps, s);
+    copy_commit();
+  }
+
+  // ------------------------------------------------------------ the query rows of this block
+  // B operand of S^T: this lane holds query g of each set of 8, for 4-bit rows the channels
+  // 32 gr + 8 t + u of every group gr, for bf16 rows 16 s + 2 t + {0, 1, 8, 9} of every step s.
+  uint32_t q[NT][16], qz[NT][2];
+  float unit[NT][2];                                       // logit (log2 units) per unit of S, queries 2t, 2t + 1
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = r0 + 8 * nt + g;
+    const bool live = r < r1;
+    const __nv_bfloat16* src = a.Q + b * a.q_sb + (int64_t)(h * a.group + (live ? r % a.group : 0)) * a.q_sh +
+                               (int64_t)(live ? r / a.group : 0) * a.q_sn;
+    if (Q4) {
+      // the row times a power of two that brings its largest entry to 2^12 .. 2^13, as fp16: exact
+      // but for entries 2^26 times smaller than that
+      float x[4][8];
+#pragma unroll
+      for (int gr = 0; gr < 4; ++gr) {
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (live) v = *reinterpret_cast<const uint4*>(src + 32 * gr + 8 * t);
+        unpack_bf16x8(v, x[gr]);
+      }
+      float top = 0.f, sum[4];
+#pragma unroll
+      for (int gr = 0; gr < 4; ++gr) {
+        sum[gr] = 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          top = fmaxf(top, fabsf(x[gr][u]));
+          sum[gr] += x[gr][u];
+        }
+      }
+#pragma unroll
+      for (int o = 1; o <= 2; o <<= 1) {
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+#pragma unroll
+        for (int gr = 0; gr < 4; ++gr) sum[gr] += __shfl_xor_sync(0xffffffffu, sum[gr], o);
+      }
+      // biased exponent of the largest entry, kept where both powers below are normal numbers
+      const int e = min(max((__float_as_int(top) >> 23) & 255, 16), 240);
+      const float up = pow2_biased(127 + 12 - (e - 127)), down = pow2_biased(127 - 12 + (e - 127));
+#pragma unroll
+      for (int gr = 0; gr < 4; ++gr) {
+        // nibbles one place up stand for 16 times their code: their channels take q / 16
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float f = (u & 1) ? up * 0.0625f : up;
+          q[nt][gr * 4 + u] = pack_f16(x[gr][u] * f, x[gr][u + 4] * f);
+        }
+      }
+      // sum of the group t, in S's units (2^-24 up), as three bf16 pieces (24 bits)
+      const float z = (t == 0 ? sum[0] : t == 1 ? sum[1] : t == 2 ? sum[2] : sum[3]) * up * 0x1p-24f;
+      const float z0 = __bfloat162float(__float2bfloat16_rn(z));
+      const float z1 = __bfloat162float(__float2bfloat16_rn(z - z0));
+      qz[nt][0] = pack_bf16(z0, z1);
+      qz[nt][1] = pack_bf16(z - z0 - z1, 0.f);
+      // queries 2t and 2t + 1 live in lanes 8 t and 8 t + 4
+      unit[nt][0] = __shfl_sync(0xffffffffu, down, 8 * t) * 0x1p24f * a.scale_log2;
+      unit[nt][1] = __shfl_sync(0xffffffffu, down, 8 * t + 4) * 0x1p24f * a.scale_log2;
+    } else {
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          q[nt][2 * s + i] = live ? *reinterpret_cast<const uint32_t*>(src + 16 * s + 8 * i + 2 * t) : 0u;
+      unit[nt][0] = unit[nt][1] = a.scale_log2;
+    }
+  }
+  // positions of queries 2t, 2t + 1 of each set (bf16 rows with several query tokens)
+  int pos[NT][2];
+  if (!Q4) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) pos[nt][i] = pos0 + (r0 + 8 * nt + 2 * t + i) / a.group;
+  }
+  const int pos_lo = pos0 + r0 / a.group, pos_hi = pos0 + (r1 - 1) / a.group;
+
+  float acc[NT][8][4], accz[NT][4];                        // O^T: 128 channels x queries 2t, 2t + 1; zeros' part
+  float m[NT][2], l[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[nt][i][j] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) accz[nt][j] = 0.f;
+    m[nt][0] = m[nt][1] = -INFINITY;
+    l[nt][0] = l[nt][1] = 0.f;
+  }
+  int v_exp = 1;                                           // V's values are held relative to 2^(v_exp - 127)
+
+  // ------------------------------------------------------------ the key loop
+  int stage = 0;
+  for (int tile = t_lo + warp; tile < t_hi; tile += kWarps) {
+    {
+      const int ahead = tile + (kStages - 1) * kWarps;
+      const int into = stage == 0 ? kStages - 1 : stage - 1;
+      if (ahead < t_hi) fetch(ahead, into);
+      copy_commit();
+    }
+    copy_wait<kStages - 1>();
+    __syncwarp();
+    const unsigned char* st = ring + stage * T::kBytes;
+    const uint32_t st_u = ring_u + stage * T::kBytes;
+    const int u0 = tile * T::kKeys;
+    const int left = seen.total - u0;
+
+    // ---- S^T
+    float s[NT][KB][4];
+#pragma unroll
+    for (int kb16 = 0; kb16 < KB; ++kb16) {
+      if constexpr (Q4) {
+        uint32_t w[2][4];                                  // codes of rows g and g + 8: word = group
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int c = (kb16 * 16 + 8 * i + g) * 4 + t, line = c >> 3;
+          const uint4 v = *reinterpret_cast<const uint4*>(st + T::kK + line * 128 + (((c & 7) ^ (2 * (line & 3))) * 16));
+          w[i][0] = v.x; w[i][1] = v.y; w[i][2] = v.z; w[i][3] = v.w;
+        }
+        const uint32_t* meta = reinterpret_cast<const uint32_t*>(st + T::kKMeta) + (kb16 * 16 + g) * 4;
+        const uint32_t za = __byte_perm(meta[t], 0u, 0x3232), zb = __byte_perm(meta[32 + t], 0u, 0x3232);
+        const uint4 ma = *reinterpret_cast<const uint4*>(meta), mb = *reinterpret_cast<const uint4*>(meta + 32);
+        const uint32_t sa[4] = {ma.x, ma.y, ma.z, ma.w}, sb[4] = {mb.x, mb.y, mb.z, mb.w};
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[nt][kb16][j] = 0.f;
+          mma_bf16(s[nt][kb16], za, zb, za, zb, qz[nt][0], qz[nt][1]);
+        }
+#pragma unroll
+        for (int gr = 0; gr < 4; ++gr) {
+          uint32_t x[2][4];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t hi = w[i][gr] >> 8;
+            x[i][0] = w[i][gr] & 0x000f000fu;
+            x[i][1] = w[i][gr] & 0x00f000f0u;
+            x[i][2] = hi & 0x000f000fu;
+            x[i][3] = hi & 0x00f000f0u;
+          }
+          const float fa = __uint_as_float(sa[gr] << 16), fb = __uint_as_float(sb[gr] << 16);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            float d[4] = {0.f, 0.f, 0.f, 0.f};
+            mma_f16(d, x[0][0], x[1][0], x[0][1], x[1][1], q[nt][4 * gr], q[nt][4 * gr + 1]);
+            mma_f16(d, x[0][2], x[1][2], x[0][3], x[1][3], q[nt][4 * gr + 2], q[nt][4 * gr + 3]);
+            s[nt][kb16][0] = fmaf(d[0], fa, s[nt][kb16][0]);
+            s[nt][kb16][1] = fmaf(d[1], fa, s[nt][kb16][1]);
+            s[nt][kb16][2] = fmaf(d[2], fb, s[nt][kb16][2]);
+            s[nt][kb16][3] = fmaf(d[3], fb, s[nt][kb16][3]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[nt][kb16][j] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+          uint32_t x[4];
+          const int key = kb16 * 16 + (lane & 15), c = 2 * ks + (lane >> 4);
+          ldmatrix4(x, st_u + T::kK + key * 256 + ((c ^ (key & 7)) * 16));
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+            mma_bf16(s[nt][kb16], x[0], x[1], x[2], x[3], q[nt][2 * ks], q[nt][2 * ks + 1]);
+        }
+      }
+    }
+    // ---- logits in log2 units; what a query does not see becomes -inf
+    bool masked = left < T::kKeys;
+    if (!Q4) {
+      // a tile that every query of the block sees whole needs no comparison
+      const int j_lo = seen.row(u0), j_hi = seen.row(min(u0 + T::kKeys, seen.total) - 1);
+      masked = masked || j_hi > pos_lo || (j_hi >= a.num_sink && (int64_t)j_lo <= (int64_t)pos_hi - a.window &&
+                                           pos_hi != pos_lo);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int kb16 = 0; kb16 < KB; ++kb16)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[nt][kb16][j] *= unit[nt][j & 1];
+    if (masked) {
+#pragma unroll
+      for (int kb16 = 0; kb16 < KB; ++kb16)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int u = u0 + kb16 * 16 + 8 * i + g;
+          const int j = Q4 ? u : seen.row(u);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              bool see = u < seen.total;
+              if (!Q4) see = see && j <= pos[nt][c] && (j < a.num_sink || (int64_t)j > (int64_t)pos[nt][c] - a.window);
+              if (!see) s[nt][kb16][2 * i + c] = -INFINITY;
+            }
+        }
+    }
+    // ---- running maximum
+    bool move = false;
+    float top[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float x = fmaxf(s[nt][0][c], s[nt][0][2 + c]);
+#pragma unroll
+        for (int kb16 = 1; kb16 < KB; ++kb16) x = fmaxf(x, fmaxf(s[nt][kb16][c], s[nt][kb16][2 + c]));
+        top[nt][c] = x;
+        move = move || x > m[nt][c] + kSlack;
+      }
+    if (__any_sync(0xffffffffu, move)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float x = top[nt][c];
+#pragma unroll
+          for (int o = 4; o <= 16; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+          const float now = fmaxf(m[nt][c], x);
+          const float f = now == -INFINITY ? 1.f : exp2_approx(m[nt][c] - now);   // 0 on the first rows
+          m[nt][c] = now;
+          l[nt][c] *= f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            acc[nt][i][c] *= f;
+            acc[nt][i][2 + c] *= f;
+          }
+          accz[nt][c] *= f;
+        }
+    }
+    // ---- V's scales of this tile in fp16, relative to the power of two that covers its values
+    if constexpr (Q4) {
+      const uint4 v = *reinterpret_cast<const uint4*>(st + T::kVMeta + lane * 16);
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      uint32_t big = 0;
+#pragma unroll
+      for (int gr = 0; gr < 4; ++gr) {
+        const uint32_t z = w[gr] & 0x7fff0000u, sc = (w[gr] << 16) + (4u << 23);   // |zero|; 16 * scale
+        big = max(big, max(z, (w[gr] & 0x7fffu) != 0u ? sc : 0u));
+      }
+      const int e = min((int)(__reduce_max_sync(0xffffffffu, big) >> 23) + 1, 240);
+      if (e > v_exp) {
+        const float f = pow2_biased(127 + v_exp - e);
+        v_exp = e;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[nt][i][j] *= f;
+          accz[nt][0] *= f;
+          accz[nt][1] *= f;
+        }
+      }
+      const float inv = pow2_biased(254 - v_exp);
+      __half* scaled = reinterpret_cast<__half*>(ring + kStages * T::kBytes);
+#pragma unroll
+      for (int gr = 0; gr < 4; ++gr) {
+        const int at = (lane >> 1) * 8 + gr * 2 + (lane & 1);
+        scaled[at] = __float2half_rn(__uint_as_float(w[gr] << 16) * inv);
+        scaled[T::kKeys * 4 + at] = __float2half_rn(__uint_as_float(w[gr] & 0xffff0000u) * inv);
+      }
+      __syncwarp();
+    }
+    // ---- weights and O^T
+#pragma unroll
+    for (int kb16 = 0; kb16 < KB; ++kb16) {
+      uint32_t pt[NT][2];                                  // P^T as B operand: keys 2t, 2t + 1 / 2t + 8, 2t + 9 of query g
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float ref = m[nt][j & 1] == -INFINITY ? 0.f : m[nt][j & 1];
+          w[j] = exp2_approx(s[nt][kb16][j] - ref + (Q4 ? kLift : 0.f));
+        }
+        l[nt][0] += w[0] + w[2];
+        l[nt][1] += w[1] + w[3];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          pt[nt][i] = transpose8x8(Q4 ? pack_f16(w[2 * i], w[2 * i + 1]) : pack_bf16(w[2 * i], w[2 * i + 1]));
+      }
+      if constexpr (Q4) {
+        const __half* scaled = reinterpret_cast<const __half*>(ring + kStages * T::kBytes);
+        uint32_t x[2][4][4], sc[2][4], z[2];               // [keys 2t.. / 2t + 8..][group][nibble]
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int key = kb16 * 16 + 8 * i + 2 * t, pair = key >> 1;
+          uint2 v[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int c = (key + k) * 4 + (g >> 1), line = c >> 3;
+            v[k] = *reinterpret_cast<const uint2*>(st + T::kV + line * 128 + (((c & 7) ^ (2 * (line & 3))) * 16) + 8 * (g & 1));
+          }
+          // 16-bit words of the two keys side by side, one register a group
+          const uint32_t y[4] = {__byte_perm(v[0].x, v[1].x, 0x5410), __byte_perm(v[0].x, v[1].x, 0x7632),
+                                 __byte_perm(v[0].y, v[1].y, 0x5410), __byte_perm(v[0].y, v[1].y, 0x7632)};
+#pragma unroll
+          for (int gr = 0; gr < 4; ++gr) {
+            const uint32_t hi = y[gr] >> 8;
+            x[i][gr][0] = y[gr] & 0x000f000fu;
+            x[i][gr][1] = y[gr] & 0x00f000f0u;
+            x[i][gr][2] = hi & 0x000f000fu;
+            x[i][gr][3] = hi & 0x00f000f0u;
+          }
+          const uint4 f = *reinterpret_cast<const uint4*>(scaled + pair * 8);
+          sc[i][0] = f.x; sc[i][1] = f.y; sc[i][2] = f.z; sc[i][3] = f.w;
+          z[i] = g < 4 ? *reinterpret_cast<const uint32_t*>(scaled + T::kKeys * 4 + pair * 8 + 2 * g) : 0u;
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          mma_f16(accz[nt], z[0], 0u, z[1], 0u, pt[nt][0], pt[nt][1]);
+#pragma unroll
+          for (int gr = 0; gr < 4; ++gr) {
+            const uint32_t b0 = hmul2(pt[nt][0], sc[0][gr]), b1 = hmul2(pt[nt][1], sc[1][gr]);
+            mma_f16(acc[nt][2 * gr], x[0][gr][0], x[0][gr][1], x[1][gr][0], x[1][gr][1], b0, b1);
+            mma_f16(acc[nt][2 * gr + 1], x[0][gr][2], x[0][gr][3], x[1][gr][2], x[1][gr][3], b0, b1);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          uint32_t x[4];                                   // V^T: channels 16 i .. + 15 of the 16 keys
+          const int key = kb16 * 16 + (lane & 7) + ((lane >> 4) & 1) * 8, c = 2 * i + ((lane >> 3) & 1);
+          ldmatrix4_trans(x, st_u + T::kV + key * 256 + ((c ^ (key & 7)) * 16));
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) mma_bf16(acc[nt][i], x[0], x[1], x[2], x[3], pt[nt][0], pt[nt][1]);
+        }
+      }
+    }
+    __syncwarp();                                          // the stage may be filled again
+    stage = stage == kStages - 1 ? 0 : stage + 1;
+  }
+  copy_wait<0>();
+
+  // ------------------------------------------------------------ the warps' results meet
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+      for (int o = 4; o <= 16; o <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], o);
+      if (g == 0) {
+        s_m[warp][8 * nt + 2 * t + c] = m[nt][c];
+        s_l[warp][8 * nt + 2 * t + c] = l[nt][c];
+      }
+    }
+  __syncthreads();                                         // also: every warp is done with its ring
+  float* meet = reinterpret_cast<float*>(smem);            // [warp][8 NT][132]
+  const float back = Q4 ? pow2_biased(v_exp) : 1.f;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int qi = 8 * nt + 2 * t + c;
+      float all = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) all = fmaxf(all, s_m[w][qi]);
+      const float f = m[nt][c] == -INFINITY ? 0.f : exp2_approx(m[nt][c] - all) * back;
+      float* dst = meet + ((size_t)warp * 8 * NT + qi) * 132;
+      if (Q4) {
+#pragma unroll
+        for (int gr = 0; gr < 4; ++gr) {
+          const float z = __shfl_sync(0xffffffffu, accz[nt][c], gr * 4 + t);
+          float4 o;
+          o.x = (acc[nt][2 * gr][c] * 0x1p24f + z) * f;
+          o.y = (acc[nt][2 * gr][2 + c] * 0x1p20f + z) * f;
+          o.z = (acc[nt][2 * gr + 1][c] * 0x1p24f + z) * f;
+          o.w = (acc[nt][2 * gr + 1][2 + c] * 0x1p20f + z) * f;
+          *reinterpret_cast<float4*>(dst + 32 * gr + 4 * g) = o;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          dst[16 * i + g] = acc[nt][i][c] * f;
+          dst[16 * i + 8 + g] = acc[nt][i][2 + c] * f;
+        }
+      }
+    }
+  __syncthreads();
+  for (int e = tid; e < (r1 - r0) * 32; e += kThreads) {
+    const int qi = e >> 5, c4 = (e & 31) * 4;
+    float all = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) all = fmaxf(all, s_m[w][qi]);
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) sum += all == -INFINITY ? 0.f : s_l[w][qi] * exp2_approx(s_m[w][qi] - all);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float4 x = *reinterpret_cast<const float4*>(meet + ((size_t)w * 8 * NT + qi) * 132 + c4);
+      o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+    }
+    if (Q4) all -= kLift;
+    if (a.splits > 1) {
+      const size_t item = blockIdx.x;
+      *reinterpret_cast<float4*>(a.part_o + (item * 8 * NT + qi) * 128 + c4) = o;
+      if (c4 == 0) {
+        a.part_ml[(item * 8 * NT + qi) * 2] = all;
+        a.part_ml[(item * 8 * NT + qi) * 2 + 1] = sum;
+      }
+    } else {
+      const int r = r0 + qi, i = r / a.group, hq = h * a.group + r % a.group;
+      if (i >= q_live) continue;                           // rows behind the last query stay as they are
+      const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);   // a NaN sum stays one
+      uint2 v;
+      v.x = pack_bf16(o.x * inv, o.y * inv);
+      v.y = pack_bf16(o.z * inv, o.w * inv);
+      *reinterpret_cast<uint2*>(a.O + b * a.o_sb + (int64_t)hq * a.o_sh + (int64_t)i * a.o_sn + c4) = v;
+      if (c4 == 0 && a.lse != nullptr)
+        a.lse[((int64_t)b * a.heads * a.group + hq) * a.q_n + i] =
+            sum == 0.f ? -INFINITY : (all + log2f(sum)) * 0.6931471805599453f;
+    }
+  }
+}
+
+// Joins the splits: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s, in split order.
+// grid = batch * heads * rows, block = 32 (four channels a lane).
+__global__ void __launch_bounds__(32) join_kernel(const Args a, int block_rows) {
+  const int r = blockIdx.x % a.rows, p = blockIdx.x / a.rows;
+  const int b = p / a.heads, h = p % a.heads, i = r / a.group, hq = h * a.group + r % a.group;
+  const int lane = threadIdx.x;
+  if (a.q_lens != nullptr && i >= min(max(a.q_lens[b], 0), a.q_n)) return;
+  const size_t item0 = ((size_t)p * a.blocks + r / block_rows) * a.splits;
+  const int qi = r % block_rows;
+  float all = -INFINITY;
+  for (int s = lane; s < a.splits; s += 32) all = fmaxf(all, a.part_ml[((item0 + s) * block_rows + qi) * 2]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
+  float sum = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (all > -INFINITY) {
+    for (int s = 0; s < a.splits; ++s) {
+      const size_t at = (item0 + s) * block_rows + qi;
+      const float f = exp2_approx(a.part_ml[at * 2] - all);
+      const float4 x = *reinterpret_cast<const float4*>(a.part_o + at * 128 + lane * 4);
+      sum = fmaf(f, a.part_ml[at * 2 + 1], sum);
+      o.x = fmaf(f, x.x, o.x); o.y = fmaf(f, x.y, o.y); o.z = fmaf(f, x.z, o.z); o.w = fmaf(f, x.w, o.w);
+    }
+  }
+  const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
+  uint2 v;
+  v.x = pack_bf16(o.x * inv, o.y * inv);
+  v.y = pack_bf16(o.z * inv, o.w * inv);
+  *reinterpret_cast<uint2*>(a.O + b * a.o_sb + (int64_t)hq * a.o_sh + (int64_t)i * a.o_sn + lane * 4) = v;
+  if (lane == 0 && a.lse != nullptr)
+    a.lse[((int64_t)b * a.heads * a.group + hq) * a.q_n + i] =
+        sum == 0.f ? -INFINITY : (all + log2f(sum)) * 0.6931471805599453f;
+}
+
+}  // namespace token
+}  // namespace curdkv

@@ -25,6 +25,9 @@ curdkv_status score_unnormalised(const void* K, const void* V, const float* G, i
                                  const curdkv_desc* desc, float* scores, void* workspace,
                                  size_t workspace_bytes, void* cuda_stream);
 
+// The checks every call makes of a descriptor, and of K and V with it (defined beside the C ABI).
+curdkv_status check_call(const void* K, const void* V, const curdkv_desc* desc);
+
 struct KvView {          // one bf16 tensor [batch][heads][n_max][d], strides in elements
   const __nv_bfloat16* base;
   int64_t stride_b, stride_h, stride_n;

@@ -244,6 +244,11 @@ curdkv_status compact_impl(const void* K, const void* V, const curdkv_desc* desc
 namespace curdkv {
 void count_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
 
+curdkv_status check_call(const void* K, const void* V, const curdkv_desc* desc) {
+  const curdkv_status st = check_desc(desc);
+  return st != CURDKV_OK ? st : check_kv(K, V, desc);
+}
+
 curdkv_status score_unnormalised(const void* K, const void* V, const float* G, int32_t g_per_head,
                                  const curdkv_desc* desc, float* scores, void* workspace,
                                  size_t workspace_bytes, void* cuda_stream) {

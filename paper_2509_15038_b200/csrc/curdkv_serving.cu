@@ -1,0 +1,332 @@
+// Serving calls: the 4-bit cache (store, append, read, attention) and the attention with a sliding
+// window and sinks.  Argument checks and kernel launches.
+#include <atomic>
+#include <cmath>
+#include <cstdint>
+
+#include "attn_token.cuh"
+#include "common.cuh"
+#include "qcache.cuh"
+
+namespace {
+
+using namespace curdkv;
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline size_t round256(size_t x) { return (x + 255) & ~size_t(255); }
+
+bool launched() {
+  count_launch();
+  return cudaGetLastError() == cudaSuccess;
+}
+
+// SMs of the current device, or a B200's where none can be asked (workspace sizes).
+int sms() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) {
+    cudaGetLastError();
+    return 148;
+  }
+  return n;
+}
+
+curdkv_status check_cache(const curdkv_qcache* c) {
+  if (c == nullptr || c->K_codes == nullptr || c->V_codes == nullptr || c->K_meta == nullptr ||
+      c->V_meta == nullptr || c->count == nullptr)
+    return CURDKV_ERR_INVALID_ARG;
+  if (c->batch < 0 || c->kv_heads < 1 || c->capacity < 1) return CURDKV_ERR_INVALID_ARG;
+  if (!aligned16(c->K_codes) || !aligned16(c->V_codes) || !aligned16(c->K_meta) || !aligned16(c->V_meta))
+    return CURDKV_ERR_INVALID_ARG;
+  if ((int64_t)c->batch * c->kv_heads > (int64_t)1 << 24 || c->capacity > 0x7fffffffLL)
+    return CURDKV_ERR_UNSUPPORTED;
+  return CURDKV_OK;
+}
+
+qcache::View view_of(const curdkv_qcache* c) {
+  return qcache::View{static_cast<uint8_t*>(c->K_codes), static_cast<uint8_t*>(c->V_codes),
+                      static_cast<uint32_t*>(c->K_meta), static_cast<uint32_t*>(c->V_meta),
+                      c->count, c->row_start, c->capacity};
+}
+
+bool status_ok(const void* workspace) { return (reinterpret_cast<uintptr_t>(workspace) & 255u) == 0; }
+
+// CTAs per head so that `problems` heads of up to `rows` rows fill the device a few times over.
+int ctas_for(int64_t problems, int64_t rows, int rows_per_cta) {
+  int64_t want = (8LL * sms() + problems - 1) / (problems > 0 ? problems : 1);
+  const int64_t most = (rows + rows_per_cta - 1) / rows_per_cta;
+  if (want > most) want = most;
+  return (int)(want < 1 ? 1 : want);
+}
+
+curdkv_status check_rows(const curdkv_qcache* cache, const void* K, const void* V, const curdkv_desc* desc,
+                         const void* workspace) {
+  curdkv_status st = check_cache(cache);
+  if (st != CURDKV_OK) return st;
+  if ((st = check_call(K, V, desc)) != CURDKV_OK) return st;
+  if (desc->d != 128) return CURDKV_ERR_UNSUPPORTED;
+  if (desc->batch != cache->batch || desc->kv_heads != cache->kv_heads) return CURDKV_ERR_INVALID_ARG;
+  if (!status_ok(workspace)) return CURDKV_ERR_INVALID_ARG;
+  return CURDKV_OK;
+}
+
+// ---- attention of few query rows ---------------------------------------------------------------
+struct Plan {
+  int nt, blocks, splits;            // sets of 8 query rows a CTA takes, CTAs per head by rows, by keys
+  size_t ml_at, o_at, bytes;         // partial results inside the workspace, and its size
+};
+
+// Shares of the keys: the number that finishes first when `items` (head, block) pairs of `keys` keys
+// run one CTA per SM.  A share costs its keys and a fixed start (`start` keys' time); joining costs
+// a second launch (`join` keys' time).
+// Never more than kShareLimit CTAs per SM in all, and none below one round of the warps' tiles, which
+// bounds the workspace by `most_keys`, the longest a head can be, whatever `keys` this call sees.
+constexpr int kShareLimit = 8;
+Plan plan_token(int64_t problems, int64_t rows, int64_t keys, int64_t most_keys, int round_keys, int start, int join) {
+  Plan pl;
+  pl.nt = rows <= 8 ? 1 : 2;
+  pl.blocks = (int)((rows + 8 * pl.nt - 1) / (8 * pl.nt));
+  const int64_t items = problems * pl.blocks, slots = sms();
+  auto shares = [&](int64_t n) {
+    const int64_t by_rows = (n + round_keys - 1) / round_keys, by_sms = kShareLimit * slots / (items > 0 ? items : 1);
+    const int64_t most = by_rows < by_sms ? by_rows : by_sms;
+    return most < 1 ? 1 : (most > 128 ? 128 : most);
+  };
+  pl.splits = 1;
+  double best = 0.0;
+  for (int64_t s = 1; s <= shares(keys); ++s) {
+    const double waves = (double)((items * s + slots - 1) / slots);
+    const double cost = waves * ((double)((keys + s - 1) / s) + start) + (s > 1 ? join : 0);
+    if (s == 1 || cost < best) {
+      best = cost;
+      pl.splits = (int)s;
+    }
+  }
+  const int64_t room = shares(most_keys);
+  const size_t parts = room > 1 ? (size_t)items * room * 8 * pl.nt : 0;
+  pl.ml_at = 256;
+  pl.o_at = pl.ml_at + round256(parts * 2 * sizeof(float));
+  pl.bytes = pl.o_at + round256(parts * 128 * sizeof(float));
+  return pl;
+}
+
+Plan plan_qcache(const curdkv_qcache* c, int32_t q_rows) {
+  const int64_t P = (int64_t)c->batch * c->kv_heads;
+  int64_t keys = c->capacity;
+  // packed heads: the mean room, a few times over since the longest head decides
+  if (c->row_start != nullptr && P > 0) keys = (c->capacity + P - 1) / P * 2;
+  if (keys > c->capacity) keys = c->capacity;
+  return plan_token(P, q_rows, keys, c->capacity, token::kWarps * token::Tile<true>::kKeys, 800, 500);
+}
+
+Plan plan_window(const curdkv_desc* d, int32_t q_rows, int64_t seen) {
+  return plan_token((int64_t)d->batch * d->kv_heads, (int64_t)(d->q_heads / d->kv_heads) * q_rows, seen, d->n_max,
+                    token::kWarps * token::Tile<false>::kKeys, 260, 160);
+}
+
+template <bool Q4, int NT>
+bool launch_attend(const token::Args& a, int64_t problems, cudaStream_t stream) {
+  constexpr int smem = token::smem_bytes<Q4, NT>();
+  if (cudaFuncSetAttribute(token::attend_kernel<Q4, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) !=
+      cudaSuccess)
+    return false;
+  token::attend_kernel<Q4, NT><<<(unsigned)(problems * a.blocks * a.splits), token::kThreads, smem, stream>>>(a);
+  if (!launched()) return false;
+  if (a.splits > 1) {
+    token::join_kernel<<<(unsigned)(problems * a.rows), 32, 0, stream>>>(a, 8 * NT);
+    if (!launched()) return false;
+  }
+  return true;
+}
+
+bool query_strides_ok(const void* x, int64_t sb, int64_t sh, int64_t sn) {
+  return x != nullptr && aligned16(x) && sb >= 0 && sh >= 0 && sn >= 128 && sb % 8 == 0 && sh % 8 == 0 && sn % 8 == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+curdkv_status curdkv_qcache_store(const curdkv_qcache* cache, const void* K, const void* V,
+                                  const curdkv_desc* desc, const int32_t* idx, int64_t idx_stride,
+                                  const int32_t* head_counts, const int32_t* head_offsets,
+                                  void* workspace, void* cuda_stream) {
+  curdkv_status st = check_rows(cache, K, V, desc, workspace);
+  if (st != CURDKV_OK) return st;
+  if (idx != nullptr && (head_counts == nullptr || idx_stride < 0)) return CURDKV_ERR_INVALID_ARG;
+  if (idx == nullptr && (head_counts != nullptr || head_offsets != nullptr)) return CURDKV_ERR_INVALID_ARG;
+  const int64_t P = (int64_t)desc->batch * desc->kv_heads;
+  if (P == 0) return CURDKV_OK;
+  qcache::StoreArgs a;
+  a.cache = view_of(cache);
+  a.K = KvView{static_cast<const __nv_bfloat16*>(K), desc->k_stride_b, desc->k_stride_h, desc->k_stride_n};
+  a.V = KvView{static_cast<const __nv_bfloat16*>(V), desc->v_stride_b, desc->v_stride_h, desc->v_stride_n};
+  a.seqlens = desc->seqlens;
+  a.idx = idx;
+  a.head_counts = head_counts;
+  a.head_offsets = head_offsets;
+  a.idx_stride = idx_stride;
+  a.heads = desc->kv_heads;
+  a.n_max = desc->n_max;
+  a.status = static_cast<uint32_t*>(workspace);
+  int64_t rows = idx != nullptr && head_offsets == nullptr ? idx_stride : desc->n_max;
+  if (cache->row_start == nullptr && rows > cache->capacity) rows = cache->capacity;
+  a.ctas_per_head = ctas_for(P, rows, qcache::kStoreRowsPerCta);
+  if (P * a.ctas_per_head > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+  qcache::store_kernel<<<(unsigned)(P * a.ctas_per_head), qcache::kStoreWarps * 32, 0,
+                         static_cast<cudaStream_t>(cuda_stream)>>>(a);
+  return launched() ? CURDKV_OK : CURDKV_ERR_CUDA;
+}
+
+curdkv_status curdkv_qcache_append(const curdkv_qcache* cache, const void* K_new, const void* V_new,
+                                   const curdkv_desc* desc, void* workspace, void* cuda_stream) {
+  curdkv_status st = check_rows(cache, K_new, V_new, desc, workspace);
+  if (st != CURDKV_OK) return st;
+  const int64_t P = (int64_t)desc->batch * desc->kv_heads;
+  if (P == 0 || desc->n_max == 0) return CURDKV_OK;
+  qcache::AppendArgs a;
+  a.cache = view_of(cache);
+  a.K = KvView{static_cast<const __nv_bfloat16*>(K_new), desc->k_stride_b, desc->k_stride_h, desc->k_stride_n};
+  a.V = KvView{static_cast<const __nv_bfloat16*>(V_new), desc->v_stride_b, desc->v_stride_h, desc->v_stride_n};
+  a.t_new = desc->seqlens;
+  a.heads = desc->kv_heads;
+  a.t = desc->n_max;
+  a.chunks = (int)(((int64_t)desc->n_max + qcache::kAppendRows - 1) / qcache::kAppendRows);
+  a.status = static_cast<uint32_t*>(workspace);
+  if (P * a.chunks > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  qcache::append_kernel<<<(unsigned)(P * a.chunks), qcache::kStoreWarps * 32, 0, stream>>>(a);
+  if (!launched()) return CURDKV_ERR_CUDA;
+  if (a.chunks > 1) {
+    qcache::advance_kernel<<<(unsigned)((P + 255) / 256), 256, 0, stream>>>(a, (int)P);
+    if (!launched()) return CURDKV_ERR_CUDA;
+  }
+  return CURDKV_OK;
+}
+
+curdkv_status curdkv_qcache_read(const curdkv_qcache* cache, const int32_t* idx, int64_t rows, void* K_out,
+                                 void* V_out, void* workspace, void* cuda_stream) {
+  curdkv_status st = check_cache(cache);
+  if (st != CURDKV_OK) return st;
+  if (K_out == nullptr || V_out == nullptr || !aligned16(K_out) || !aligned16(V_out)) return CURDKV_ERR_INVALID_ARG;
+  if (rows < 0 || (idx != nullptr && rows < 1) || rows > 0x7fffffffLL || !status_ok(workspace))
+    return CURDKV_ERR_INVALID_ARG;
+  const int64_t P = (int64_t)cache->batch * cache->kv_heads;
+  if (P == 0) return CURDKV_OK;
+  qcache::ReadArgs a;
+  a.cache = view_of(cache);
+  a.idx = idx;
+  a.K_out = static_cast<__nv_bfloat16*>(K_out);
+  a.V_out = static_cast<__nv_bfloat16*>(V_out);
+  a.heads = cache->kv_heads;
+  a.rows = rows;
+  a.status = static_cast<uint32_t*>(workspace);
+  a.ctas_per_head = ctas_for(P, rows > 0 ? rows : cache->capacity, qcache::kStoreRowsPerCta);
+  if (P * a.ctas_per_head > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+  qcache::read_kernel<<<(unsigned)(P * a.ctas_per_head), qcache::kStoreWarps * 32, 0,
+                        static_cast<cudaStream_t>(cuda_stream)>>>(a);
+  return launched() ? CURDKV_OK : CURDKV_ERR_CUDA;
+}
+
+size_t curdkv_qcache_attention_workspace_bytes(const curdkv_qcache* cache, int32_t q_rows) {
+  if (cache == nullptr || cache->batch < 0 || cache->kv_heads < 1 || cache->capacity < 1 || q_rows < 1) return 0;
+  return plan_qcache(cache, q_rows).bytes;
+}
+
+curdkv_status curdkv_qcache_attention(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h,
+                                      int64_t q_stride_n, const curdkv_qcache* cache, float scale, void* O,
+                                      int64_t o_stride_b, int64_t o_stride_h, int64_t o_stride_n, float* lse,
+                                      void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  curdkv_status st = check_cache(cache);
+  if (st != CURDKV_OK) return st;
+  if (q_rows < 1 || !(scale >= 0.f) || std::isinf(scale)) return CURDKV_ERR_INVALID_ARG;
+  if (!query_strides_ok(Q, q_stride_b, q_stride_h, q_stride_n) ||
+      !query_strides_ok(O, o_stride_b, o_stride_h, o_stride_n) || Q == O)
+    return CURDKV_ERR_INVALID_ARG;
+  if (workspace == nullptr || !status_ok(workspace)) return CURDKV_ERR_INVALID_ARG;
+  const Plan pl = plan_qcache(cache, q_rows);
+  if (workspace_bytes < pl.bytes) return CURDKV_ERR_WORKSPACE;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const int64_t P = (int64_t)cache->batch * cache->kv_heads;
+  if (P == 0) return CURDKV_OK;
+  if (P * pl.blocks * pl.splits > 0x7fffffffLL || P * q_rows > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+  token::Args a = {};
+  a.Q = static_cast<const __nv_bfloat16*>(Q);
+  a.q_sb = q_stride_b; a.q_sh = q_stride_h; a.q_sn = q_stride_n;
+  a.O = static_cast<__nv_bfloat16*>(O);
+  a.o_sb = o_stride_b; a.o_sh = o_stride_h; a.o_sn = o_stride_n;
+  a.lse = lse;
+  a.heads = cache->kv_heads;
+  a.group = 1;
+  a.q_n = a.rows = q_rows;
+  a.blocks = pl.blocks;
+  a.splits = pl.splits;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.cache = view_of(cache);
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  a.part_ml = reinterpret_cast<float*>(ws + pl.ml_at);
+  a.part_o = reinterpret_cast<float*>(ws + pl.o_at);
+  a.status = reinterpret_cast<uint32_t*>(ws);
+  return (pl.nt == 1 ? launch_attend<true, 1>(a, P, stream) : launch_attend<true, 2>(a, P, stream)) ? CURDKV_OK
+                                                                                                  : CURDKV_ERR_CUDA;
+}
+
+size_t curdkv_attention_window_workspace_bytes(const curdkv_desc* desc, int32_t q_rows) {
+  if (desc == nullptr || desc->batch < 0 || desc->kv_heads < 1 || desc->q_heads < desc->kv_heads ||
+      desc->q_heads % desc->kv_heads != 0 || desc->n_max < 0 || q_rows < 1)
+    return 0;
+  return plan_window(desc, q_rows, desc->n_max).bytes;
+}
+
+curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h,
+                                      int64_t q_stride_n, const int32_t* q_lens, const void* K, const void* V,
+                                      const curdkv_desc* desc, int32_t num_sink, int32_t window, float scale,
+                                      void* O, int64_t o_stride_b, int64_t o_stride_h, int64_t o_stride_n,
+                                      float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  curdkv_status st = check_call(K, V, desc);
+  if (st != CURDKV_OK) return st;
+  if (desc->d != 128) return CURDKV_ERR_UNSUPPORTED;
+  if (q_rows < 1 || num_sink < 0 || window < 0 || !(scale >= 0.f) || std::isinf(scale)) return CURDKV_ERR_INVALID_ARG;
+  if (!query_strides_ok(Q, q_stride_b, q_stride_h, q_stride_n) ||
+      !query_strides_ok(O, o_stride_b, o_stride_h, o_stride_n) || Q == O)
+    return CURDKV_ERR_INVALID_ARG;
+  if (workspace == nullptr || !status_ok(workspace)) return CURDKV_ERR_INVALID_ARG;
+  // rows the block with the most visible ones sees: its window, the tokens between, the sinks
+  int64_t seen = (int64_t)window + num_sink + q_rows;
+  if (seen > desc->n_max) seen = desc->n_max;
+  Plan pl = plan_window(desc, q_rows, seen);
+  if (workspace_bytes < pl.bytes) return CURDKV_ERR_WORKSPACE;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  const int64_t P = (int64_t)desc->batch * desc->kv_heads;
+  if (P == 0) return CURDKV_OK;
+  token::Args a = {};
+  a.Q = static_cast<const __nv_bfloat16*>(Q);
+  a.q_sb = q_stride_b; a.q_sh = q_stride_h; a.q_sn = q_stride_n;
+  a.O = static_cast<__nv_bfloat16*>(O);
+  a.o_sb = o_stride_b; a.o_sh = o_stride_h; a.o_sn = o_stride_n;
+  a.lse = lse;
+  a.heads = desc->kv_heads;
+  a.group = desc->q_heads / desc->kv_heads;
+  a.q_n = q_rows;
+  if ((int64_t)a.group * q_rows > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+  a.rows = a.group * q_rows;
+  a.blocks = pl.blocks;
+  a.splits = pl.splits;
+  if (P * pl.blocks * pl.splits > 0x7fffffffLL || P * a.rows > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.K = KvView{static_cast<const __nv_bfloat16*>(K), desc->k_stride_b, desc->k_stride_h, desc->k_stride_n};
+  a.V = KvView{static_cast<const __nv_bfloat16*>(V), desc->v_stride_b, desc->v_stride_h, desc->v_stride_n};
+  a.seqlens = desc->seqlens;
+  a.q_lens = q_lens;
+  a.n_max = desc->n_max;
+  a.num_sink = num_sink;
+  a.window = window;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  a.part_ml = reinterpret_cast<float*>(ws + pl.ml_at);
+  a.part_o = reinterpret_cast<float*>(ws + pl.o_at);
+  a.status = reinterpret_cast<uint32_t*>(ws);
+  return (pl.nt == 1 ? launch_attend<false, 1>(a, P, stream) : launch_attend<false, 2>(a, P, stream)) ? CURDKV_OK
+                                                                                                    : CURDKV_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,409 @@
+"""The 4-bit cache on the GPU (store, append, read, attention) against the float64 oracle.  Needs a B200."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import curdkv_serving_oracle as orc
+from paper_2509_15038_b200 import binding as cur
+from paper_2509_15038_b200 import synth
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _rand(shape, seed, gain=1.0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = torch.randn(shape, generator=g, device=DEV) * gain
+    x[..., 3] *= 10.0
+    return x.to(torch.bfloat16)
+
+
+def _f64(t):
+    return synth.u16_to_f64(synth.to_u16(t))
+
+
+def _bits(t):
+    return t.view(torch.int16).cpu().numpy().view(np.uint16)
+
+
+def _check_rows(cache, p_rows, wants):
+    """Codes and metas of cache rows p_rows (flat indices) bit for bit those of the rows `wants` = (K, V) float64."""
+    for which, codes, meta, want in (("K", cache.K_codes, cache.K_meta, wants[0]), ("V", cache.V_codes, cache.V_meta, wants[1])):
+        c, _, _, m = orc.quantise(want)
+        got_c = codes.reshape(-1, 64).cpu().numpy()[p_rows]
+        got_m = _bits(meta.reshape(-1, 8)).reshape(-1, 4, 2)[p_rows]
+        # -0.0 and 0.0 are the same zero point
+        gm, wm = got_m.copy(), m.copy()
+        gm[gm == 0x8000] = 0
+        wm[wm == 0x8000] = 0
+        assert np.array_equal(gm, wm), which
+        assert np.array_equal(got_c, orc.pack(c, which)), which
+
+
+@pytest.mark.parametrize("B,H,n", [(1, 1, 1), (2, 3, 37), (1, 2, 1000), (3, 8, 130)])
+@pytest.mark.parametrize("layout", ["bhnd", "bnhd"])
+def test_store_all_rows_bit_exact(B, H, n, layout):
+    if layout == "bhnd":
+        K, V = _rand((B, H, n, 128), 1), _rand((B, H, n, 128), 2, 0.01)
+    else:                                            # heads inside the token axis: strided rows
+        K, V = (_rand((B, n, H, 128), s).transpose(1, 2) for s in (3, 4))
+    cache = cur.QuantCache(B, H, n + 5)
+    ws = torch.zeros(256, dtype=torch.uint8, device=DEV)
+    cur.curdkv_qcache_store(cache, K, V, cur.make_desc(K, V, 1), workspace=ws)
+    assert cur.curdkv_device_status(ws) == 0
+    assert cache.count.tolist() == [n] * (B * H)
+    rows = np.concatenate([np.arange(n) + p * (n + 5) for p in range(B * H)])
+    _check_rows(cache, rows, (_f64(K).reshape(-1, 128), _f64(V).reshape(-1, 128)))
+    # the rows behind are as they were
+    rest = np.setdiff1d(np.arange(B * H * (n + 5)), rows)
+    assert not cache.K_codes.view(-1, 64).cpu().numpy()[rest].any()
+    # and back: the value rounded to bf16 once (fma in fp32, then bf16: at most a half step of bf16 and 2^-24 of its parts)
+    Ko, Vo = cur.curdkv_qcache_read(cache)
+    for out, codes, meta, which in ((Ko, cache.K_codes, cache.K_meta, "K"), (Vo, cache.V_codes, cache.V_meta, "V")):
+        val, part = orc.unpack(codes.cpu().numpy().reshape(-1, 64)[rows], _bits(meta.reshape(-1, 8))[rows], which)
+        got = _f64(out).reshape(-1, 128)[rows]
+        assert np.all(np.abs(got - val) <= 2.0 ** -8 * np.abs(val) + 2.0 ** -23 * part)
+
+
+def test_store_hard_groups_bit_exact():
+    """Ties, constant groups, tiny and huge ranges, a tiny value beside a large zero point, signed zeros."""
+    rows = []
+    base = np.zeros(128)
+    rows.append(base.copy())                                             # all zero: scale 0
+    rows.append(np.full(128, -2.5))                                      # constant: scale 0, zero -2.5
+    r = base.copy(); r[0::32] = -1.40625; r[1::32] = 1.40625             # scale 0.1875 exactly; zeros fall on the tie 7.5
+    rows.append(r)
+    r = r.copy(); r[2::32] = 1e-10; r[3::32] = -1e-10                    # beside that tie on either side
+    rows.append(r)
+    r = np.tile(np.arange(32) * 0.5, 4); rows.append(r)                  # many ties: steps of half a code
+    r = np.tile(np.arange(32) * 2.0 ** -130, 4); rows.append(r)          # subnormal scale
+    r = np.tile(np.arange(32) * 2.0 ** 120, 4); rows.append(r)           # huge
+    r = base.copy(); r[5] = 2.0 ** -133; rows.append(r)                  # smallest subnormal bf16
+    r = base.copy(); r[7] = -0.0; r[40] = 1.0; rows.append(r)
+    x = np.stack(rows)
+    t = torch.tensor(x, dtype=torch.float64).to(torch.bfloat16)
+    t = torch.cat([t, (torch.randn(300, 128, generator=torch.Generator().manual_seed(0)) + 100).to(torch.bfloat16)])
+    K = t.view(1, 1, -1, 128).to(DEV)
+    V = -K
+    cache = cur.QuantCache(1, 1, K.shape[2])
+    cur.curdkv_qcache_store(cache, K, V, cur.make_desc(K, V, 1))
+    _check_rows(cache, np.arange(K.shape[2]), (_f64(K)[0, 0], _f64(V)[0, 0]))
+
+
+def test_store_nonfinite_group_stays_inside_its_group():
+    K = _rand((1, 1, 8, 128), 5)
+    K[0, 0, 1, 5] = float("nan")
+    K[0, 0, 2, 40] = float("inf")
+    K[0, 0, 3, 100] = -float("inf")
+    K[0, 0, 4, 70], K[0, 0, 4, 71] = 3e38, -3e38                         # a range beyond fp32
+    cache = cur.QuantCache(1, 1, 8)
+    cur.curdkv_qcache_store(cache, K, K, cur.make_desc(K, K, 1))
+    _check_rows(cache, np.arange(8), (_f64(K)[0, 0], _f64(K)[0, 0]))
+    for out in cur.curdkv_qcache_read(cache):
+        got = torch.isnan(out[0, 0]).view(8, 4, 32).cpu()
+        want = torch.zeros(8, 4, 32, dtype=torch.bool)
+        want[1, 0] = want[2, 1] = want[3, 3] = want[4, 2] = True
+        assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("adaptive", [False, True])
+def test_store_of_a_selection(adaptive):
+    """The rows curdkv_select names, fixed and packed, equal the gathered rows quantised."""
+    B, H, n, k = 2, 4, 700, 90
+    w = synth.shrink(synth.CONFIGS["cfg2"], layers=1, batch=B, n_max=n, kv_heads=H, q_heads=H)
+    K, V, _ = synth.make_kv(w, DEV)
+    lens = torch.tensor([700, 50], dtype=torch.int32, device=DEV)        # the second keeps all its 50 rows
+    desc = cur.make_desc(K, V, 32, seqlens=lens)
+    ws = cur.alloc_workspace(desc, k, adaptive)
+    G = torch.as_tensor(synth.make_G(128, 32, seed=0), device=DEV)
+    scores, _ = cur.curdkv_score(K, V, G, desc, ws)
+    idx, cnt, off = cur.curdkv_select(scores, desc, k, num_sink=4, window=16, adaptive=adaptive, workspace=ws)
+    if adaptive:
+        cache = cur.QuantCache(B, H, idx.numel(), row_start=off)
+    else:
+        cache = cur.QuantCache(B, H, k + 3)
+    cur.curdkv_qcache_store(cache, K, V, desc, idx, cnt, off, packed=adaptive, workspace=ws)
+    assert cur.curdkv_device_status(ws) == 0
+    assert torch.equal(cache.count, cnt.view(-1))
+    gi, gc, go = idx.cpu().numpy().reshape(-1) if adaptive else idx.cpu().numpy(), cnt.cpu().numpy(), off.cpu().numpy()
+    rows, wants = [], [[], []]
+    Kf, Vf = _f64(K), _f64(V)
+    for p in range(B * H):
+        b, h = divmod(p, H)
+        c = gc[b, h]
+        kept = gi[go[p]: go[p] + c] if adaptive else gi[b, h, :c]
+        rows.append((go[p] if adaptive else p * (k + 3)) + np.arange(c))
+        wants[0].append(Kf[b, h][kept])
+        wants[1].append(Vf[b, h][kept])
+    _check_rows(cache, np.concatenate(rows), [np.concatenate(x) for x in wants])
+
+
+def test_store_flags_bad_indices_and_overflow():
+    K, V = _rand((1, 2, 64, 128), 6), _rand((1, 2, 64, 128), 7)
+    desc = cur.make_desc(K, V, 1, seqlens=torch.tensor([40], dtype=torch.int32, device=DEV))
+    ws = torch.zeros(256, dtype=torch.uint8, device=DEV)
+    idx = torch.tensor([[0, 39, 40, -1], [1, 2, 1 << 30, 5]], dtype=torch.int32, device=DEV).view(1, 2, 4)
+    cnt = torch.tensor([4, 4], dtype=torch.int32, device=DEV)
+    cache = cur.QuantCache(1, 2, 4)
+    cache.K_codes.fill_(0xEE)
+    cur.curdkv_qcache_store(cache, K, V, desc, idx, cnt, workspace=ws)
+    assert cur.curdkv_device_status(ws) == cur.DEV_BAD_INDEX
+    Ko, _ = cur.curdkv_qcache_read(cache)
+    assert not Ko[0, 0, 2:].any() and not Ko[0, 1, 2].any()              # rows of zeros, not stale ones
+    assert cache.count.tolist() == [4, 4]
+    # a head with less room than its list: cut and flagged, the neighbour's rows untouched
+    ws.zero_()
+    small = cur.QuantCache(1, 2, 3)
+    cur.curdkv_qcache_store(small, K, V, desc, idx.clamp(0, 39), cnt, workspace=ws)
+    assert cur.curdkv_device_status(ws) == cur.DEV_CACHE_FULL
+    assert small.count.tolist() == [3, 3]
+    _check_rows(small, np.arange(6), (np.concatenate([_f64(K)[0, 0][[0, 39, 39]], _f64(K)[0, 1][[1, 2, 39]]]),
+                                      np.concatenate([_f64(V)[0, 0][[0, 39, 39]], _f64(V)[0, 1][[1, 2, 39]]])))
+    # a count beyond its list
+    ws.zero_()
+    cur.curdkv_qcache_store(cache, K, V, desc, idx.clamp(0, 39), cnt + 3, workspace=ws)
+    assert cur.curdkv_device_status(ws) & cur.DEV_BAD_INDEX and cache.count.tolist() == [4, 4]
+
+
+@pytest.mark.parametrize("steps", [[1] * 5, [64, 65, 1], [200]])
+@pytest.mark.parametrize("packed", [False, True])
+def test_append_equals_store(steps, packed):
+    B, H, total = 2, 3, sum(steps)
+    K, V = _rand((B, H, total, 128), 8), _rand((B, H, total, 128), 9)
+    start = torch.arange(B * H + 1, dtype=torch.int32, device=DEV) * total if packed else None
+    mk = lambda: cur.QuantCache(B, H, B * H * total if packed else total, row_start=start)  # noqa: E731
+    whole, grown = mk(), mk()
+    cur.curdkv_qcache_store(whole, K, V, cur.make_desc(K, V, 1))
+    at = 0
+    for t in steps:
+        cur.curdkv_qcache_append(grown, K[:, :, at:at + t], V[:, :, at:at + t])
+        at += t
+        assert grown.count.tolist() == [at] * (B * H)
+    for x in ("K_codes", "V_codes"):
+        assert torch.equal(getattr(whole, x), getattr(grown, x))
+    for x in ("K_meta", "V_meta"):
+        assert torch.equal(getattr(whole, x).view(torch.int16), getattr(grown, x).view(torch.int16))
+
+
+@pytest.mark.parametrize("t", [5, 70])
+def test_append_ragged_and_full(t):
+    B, H, cap = 3, 2, 80
+    K, V = _rand((B, H, t, 128), 10), _rand((B, H, t, 128), 11)
+    cache = cur.QuantCache(B, H, cap)
+    cache.count.copy_(torch.tensor([0, 0, 40, 40, 78, 78], dtype=torch.int32))
+    ws = torch.zeros(256, dtype=torch.uint8, device=DEV)
+    cur.curdkv_qcache_append(cache, K, V, t_new=torch.tensor([0, t - 1, t], dtype=torch.int32, device=DEV), workspace=ws)
+    fit = [0, min(t - 1, 40), 2]
+    full = cur.DEV_CACHE_FULL
+    assert cur.curdkv_device_status(ws) == full
+    assert cache.count.tolist() == [0, 0, 40 + fit[1], 40 + fit[1], 80, 80]
+    rows = [p * cap + h0 + np.arange(f) for p, (h0, f) in enumerate([(0, 0), (0, 0), (40, fit[1]), (40, fit[1]), (78, 2), (78, 2)])]
+    pick = lambda X: np.concatenate([_f64(X)[p // H, p % H][: len(r)] for p, r in enumerate(rows)])  # noqa: E731
+    _check_rows(cache, np.concatenate(rows), (pick(K), pick(V)))
+    live = np.zeros(B * H * cap, dtype=bool)
+    live[np.concatenate(rows)] = True
+    assert not cache.V_codes.view(-1, 64).cpu().numpy()[~live].any()
+
+
+def test_read_named_slots():
+    K, V = _rand((2, 2, 30, 128), 12), _rand((2, 2, 30, 128), 13)
+    cache = cur.QuantCache(2, 2, 32)
+    cur.curdkv_qcache_store(cache, K, V, cur.make_desc(K, V, 1))
+    idx = torch.tensor([[0, 29, -1], [5, 5, 30], [1, 2, 3], [-1, -1, 7]], dtype=torch.int32, device=DEV).view(2, 2, 3)
+    ws = torch.zeros(256, dtype=torch.uint8, device=DEV)
+    full_k, full_v = cur.curdkv_qcache_read(cache)
+    out = torch.full((2, 2, 3, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+    Ko, Vo = cur.curdkv_qcache_read(cache, idx, K_out=out.clone(), V_out=out.clone(), workspace=ws)
+    assert cur.curdkv_device_status(ws) == cur.DEV_BAD_INDEX             # slot 30 of a head that holds 30
+    for got, full in ((Ko, full_k), (Vo, full_v)):
+        for p, row in enumerate(idx.view(4, 3).tolist()):
+            for i, j in enumerate(row):
+                want = full.view(4, 32, 128)[p, j] if 0 <= j < 30 else out[0, 0, 0]
+                assert torch.equal(got.view(4, 3, 128)[p, i], want)
+
+
+def _check_attention(O, lse, Q, cache, counts, starts, scale, what=""):
+    """Against the oracle on the rows the codes stand for.  Error budget per output: the weights are rounded to fp16 twice
+    (half a step is 2^-11 each: once alone, once times the scale), the zero points meet only the first; logits carry fp32
+    sums of 128 products (and the zero points' part rounded to 24 bits), say 2^-20 of the sum of magnitudes, which enters
+    every weight twice (numerator and denominator); 2^-21 for the exponential and the fp32 sums over the keys per
+    addition chain; O is rounded to bf16 once (2^-8)."""
+    got, Qf = _f64(O), _f64(Q)
+    kc, vc = cache.K_codes.cpu().numpy().reshape(-1, 64), cache.V_codes.cpu().numpy().reshape(-1, 64)
+    km, vm = _bits(cache.K_meta.reshape(-1, 8)), _bits(cache.V_meta.reshape(-1, 8))
+    B, H = Q.shape[:2]
+    for p, c in enumerate(counts):
+        b, h = divmod(p, H)
+        rows = slice(starts[p], starts[p] + c)
+        k, kp = orc.unpack(kc[rows], km[rows], "K")
+        v, vp = orc.unpack(vc[rows], vm[rows], "V")
+        q = Qf[b, h]
+        want, want_lse, w = orc.attend(q, k, v, np.ones((q.shape[0], c), dtype=bool), scale)
+        if c == 0:
+            assert not got[b, h].any() and np.all(np.isneginf(lse[b, h].cpu().numpy()))
+            continue
+        d = 2.0 ** -20 * scale * (np.abs(q) @ kp.T).max(-1)              # logit error, natural units
+        rel = 2.0 ** -10 + 2 * d + 2.0 ** -18
+        tol = 2.0 ** -8 * np.abs(want) + rel[:, None] * (w @ vp) * (1 + 2.0 ** -7) + 1e-38
+        err = np.abs(got[b, h] - want)
+        assert np.all(err <= tol), f"{what} p={p} count={c}: {np.max(err / tol):.3g} of the tolerance"
+        assert np.all(np.abs(lse[b, h].cpu().numpy() - want_lse) <= d + 2.0 ** -20 * (1 + np.abs(want_lse)) + 2.0 ** -18)
+
+
+def _random_cache(B, H, cap, counts, seed, packed=False, k_gain=1.0, v_gain=1.0, v_shift=0.0):
+    n = max(max(counts), 1)
+    K = _rand((B, H, n, 128), seed, k_gain)
+    V = (_rand((B, H, n, 128), seed + 1, v_gain).float() + v_shift).to(torch.bfloat16)
+    if packed:
+        starts = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+        cache = cur.QuantCache(B, H, max(int(starts[-1]), 1), row_start=torch.as_tensor(starts, device=DEV))
+    else:
+        starts = np.arange(B * H) * cap
+        cache = cur.QuantCache(B, H, cap)
+    idx = torch.arange(n, dtype=torch.int32, device=DEV).expand(B, H, n).contiguous()
+    cur.curdkv_qcache_store(cache, K, V, cur.make_desc(K, V, 1), idx,
+                            torch.tensor(counts, dtype=torch.int32, device=DEV))
+    return cache, starts
+
+
+COUNTS = [0, 1, 15, 16, 17, 31, 32, 33, 255, 256, 257, 300, 700, 1000, 1023, 2049]
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("q_rows", [1, 4, 8, 9, 16, 37])
+def test_attention_matches_oracle(packed, q_rows):
+    B, H = 2, 8
+    cache, starts = _random_cache(B, H, 2100, COUNTS, 20, packed)
+    Q = _rand((B, H, q_rows, 128), 30)
+    lse = torch.zeros((B, H, q_rows), device=DEV)
+    scale = 128 ** -0.5
+    O, ws = cur.curdkv_qcache_attention(Q, cache, scale=scale, lse=lse)
+    assert cur.curdkv_device_status(ws) == 0
+    _check_attention(O, lse, Q, cache, COUNTS, starts, scale, f"packed={packed} q_rows={q_rows}")
+    again, _ = cur.curdkv_qcache_attention(Q, cache, scale=scale, workspace=ws)
+    assert torch.equal(O, again)                                         # no order of arrival decides anything
+
+
+@pytest.mark.parametrize("k_gain,v_gain,v_shift,q_gain", [
+    (1.0, 1e4, 0.0, 1.0), (1.0, 1e-6, 0.0, 1.0), (1e3, 1.0, 0.0, 1e-3), (1e-4, 1.0, 50.0, 1e4), (1.0, 1e30, 0.0, 1.0),
+    (1e-20, 1e-30, 0.0, 1e20), (5.0, 1.0, 0.0, 3.0)])
+def test_attention_over_the_range_of_bf16(k_gain, v_gain, v_shift, q_gain):
+    """Values far from 1 on every side, values that sit on an offset, and logits of hundreds."""
+    counts = [500, 3]
+    cache, starts = _random_cache(1, 2, 512, counts, 40, k_gain=k_gain, v_gain=v_gain, v_shift=v_shift)
+    Q = _rand((1, 2, 5, 128), 41, q_gain)
+    lse = torch.zeros((1, 2, 5), device=DEV)
+    O, _ = cur.curdkv_qcache_attention(Q, cache, scale=0.0884, lse=lse)
+    _check_attention(O, lse, Q, cache, counts, starts, float(np.float32(0.0884)), f"{k_gain} {v_gain} {v_shift} {q_gain}")
+
+
+def test_attention_values_that_grow_along_the_cache():
+    """Value rows whose scale grows by 2^40 along the sequence, and logits that grow with them: both running references move
+    many times."""
+    n = 900
+    ramp = torch.linspace(0, 1, n, device=DEV)[:, None]
+    K = _rand((1, 1, n, 128), 50, 0.2).float()
+    K[0, 0, :, 0] = 40 * ramp[:, 0]
+    V = _rand((1, 1, n, 128), 51).float() * torch.exp2(40 * (ramp - 0.5))
+    K, V = K.to(torch.bfloat16), V.to(torch.bfloat16)
+    cache = cur.QuantCache(1, 1, n)
+    cur.curdkv_qcache_store(cache, K, V, cur.make_desc(K, V, 1))
+    Q = _rand((1, 1, 4, 128), 52, 0.2)
+    Q[..., 0] = torch.tensor([1.0, -1.0, 0.0, 2.0], device=DEV)
+    lse = torch.zeros((1, 1, 4), device=DEV)
+    O, _ = cur.curdkv_qcache_attention(Q, cache, scale=1.0, lse=lse)
+    _check_attention(O, lse, Q, cache, [n], [0], 1.0)
+
+
+def test_attention_scale_zero_strides_and_stale_rows():
+    """Scale 0 averages the rows; strided Q and O; whatever lies behind the held rows (NaN metas) has no part."""
+    cache, starts = _random_cache(2, 2, 64, [40, 1, 64, 0], 60)
+    cache.K_meta.view(4, 64, 4, 2)[0, 40:] = float("nan")
+    cache.V_meta.view(4, 64, 4, 2)[0, 40:] = float("nan")
+    cache.V_meta.view(4, 64, 4, 2)[3] = float("inf")
+    wide = _rand((2, 6, 2, 192), 61)
+    Q = wide[..., :128].transpose(1, 2)                                  # [2, 2, 6, 128] with rows 384 apart
+    buf = torch.full((2, 6, 2, 136), 9.0, dtype=torch.bfloat16, device=DEV)
+    O = buf[..., 8:].transpose(1, 2)
+    lse = torch.zeros((2, 2, 6), device=DEV)
+    for scale in (0.0, 0.1):
+        cur.curdkv_qcache_attention(Q, cache, scale=scale, O=O, lse=lse)
+        _check_attention(O, lse, Q, cache, [40, 1, 64, 0], starts, float(np.float32(scale)))
+    assert torch.all(buf[..., :8] == 9.0)
+
+
+def test_attention_flags_a_count_out_of_range():
+    cache, starts = _random_cache(1, 2, 32, [32, 32], 70)
+    cache.count.copy_(torch.tensor([40, -3], dtype=torch.int32))
+    Q = _rand((1, 2, 1, 128), 71)
+    lse = torch.zeros((1, 2, 1), device=DEV)
+    O, ws = cur.curdkv_qcache_attention(Q, cache, scale=0.1, lse=lse)
+    assert cur.curdkv_device_status(ws) == cur.DEV_BAD_INDEX
+    _check_attention(O, lse, Q, cache, [32, 0], starts, float(np.float32(0.1)))
+
+
+def test_generation_together_in_a_graph():
+    """Prompt compressed into a packed 4-bit cache with slack, then generation steps (append, attend) captured once and
+    replayed with fresh rows; the cache and every output as the oracle has them."""
+    B, H, group, n, k, steps = 2, 4, 4, 600, 100, 5
+    w = synth.shrink(synth.CONFIGS["cfg2"], layers=1, batch=B, n_max=n, kv_heads=H, q_heads=H * group)
+    K, V, _ = synth.make_kv(w, DEV)
+    G = torch.as_tensor(synth.make_G(128, 32, seed=0), device=DEV)
+    desc = cur.make_desc(K, V, 32, q_heads=H * group)
+    ws = cur.alloc_workspace(desc, k, True)
+    _, _, idx, cnt, off, _, _ = cur.curdkv_compress(K, V, G, desc, k, ws, num_sink=4, window=16, adaptive=True)
+    start = off + 8 * torch.arange(B * H + 1, dtype=torch.int32, device=DEV)
+    cache = cur.QuantCache(B, H, int(start[-1].item()), row_start=start)
+    cur.curdkv_qcache_store(cache, K, V, desc, idx, cnt, off, packed=True, workspace=ws)
+    k1, v1 = (torch.zeros((B, H, 1, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    q1 = torch.zeros((B, H, group, 128), dtype=torch.bfloat16, device=DEV)
+    lse, O = torch.zeros((B, H, group), device=DEV), torch.zeros_like(q1)
+    aws = cur.qcache_attention_workspace(cache, group)
+    held = cache.count.clone()
+
+    def step():
+        cur.curdkv_qcache_append(cache, k1, v1, workspace=aws)
+        cur.curdkv_qcache_attention(q1, cache, scale=0.0884, O=O, lse=lse, workspace=aws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    cache.count.copy_(held)
+    for i in range(steps):
+        k1.copy_(_rand((B, H, 1, 128), 100 + i))
+        v1.copy_(_rand((B, H, 1, 128), 200 + i))
+        q1.copy_(_rand((B, H, group, 128), 300 + i))
+        graph.replay()
+        counts = (held + i + 1).tolist()
+        assert cache.count.tolist() == counts
+        rows = np.asarray([start[p].item() + counts[p] - 1 for p in range(B * H)])
+        _check_rows(cache, rows, (_f64(k1).reshape(-1, 128), _f64(v1).reshape(-1, 128)))
+        _check_attention(O, lse, q1, cache, counts, start.tolist(), float(np.float32(0.0884)), f"step {i}")
+    assert cur.curdkv_device_status(aws) == 0
+
+
+def test_long_cache_offsets_pass_32_bits():
+    """A cache whose codes lie beyond 4 GB: the last head's rows are its own."""
+    H, cap = 9, 1 << 23                                                  # 9 * 2^23 rows * 64 B = 4.8 GB a tensor
+    cache = cur.QuantCache(1, H, cap)
+    K, V = _rand((1, H, 50, 128), 80), _rand((1, H, 50, 128), 81)
+    cur.curdkv_qcache_store(cache, K, V, cur.make_desc(K, V, 1))
+    rows = np.arange(50) + 8 * cap
+    small = cur.QuantCache(1, 1, 50)
+    small.K_codes.copy_(cache.K_codes[:, 8:, :50])
+    small.V_codes.copy_(cache.V_codes[:, 8:, :50])
+    small.K_meta.copy_(cache.K_meta[:, 8:, :50])
+    small.V_meta.copy_(cache.V_meta[:, 8:, :50])
+    small.count.fill_(50)
+    _check_rows(small, np.arange(50), (_f64(K)[0, 8], _f64(V)[0, 8]))
+    assert rows[-1] * 64 > 1 << 32
+    Q = _rand((1, H, 2, 128), 82)
+    lse = torch.zeros((1, H, 2), device=DEV)
+    O, _ = cur.curdkv_qcache_attention(Q, cache, scale=0.1, lse=lse)
+    lse_s = torch.zeros((1, 1, 2), device=DEV)
+    cur.curdkv_qcache_attention(Q[:, 8:], small, scale=0.1, lse=lse_s)
+    _check_attention(O[:, 8:], lse[:, 8:], Q[:, 8:], small, [50], [0], float(np.float32(0.1)))
