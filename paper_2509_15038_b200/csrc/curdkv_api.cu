@@ -244,6 +244,16 @@ curdkv_status compact_impl(const void* K, const void* V, const curdkv_desc* desc
 namespace curdkv {
 void count_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
 
+bool rows_map(CUtensorMap* map, const void* base, int32_t batch, int32_t heads, int32_t rows, int64_t stride_b,
+              int64_t stride_h, int64_t stride_n) {
+  curdkv_desc d = {};
+  d.batch = batch;
+  d.kv_heads = heads;
+  d.n_max = rows;
+  d.d = 128;
+  return make_tile_map(map, base, &d, stride_b, stride_h, stride_n);
+}
+
 curdkv_status check_call(const void* K, const void* V, const curdkv_desc* desc) {
   const curdkv_status st = check_desc(desc);
   return st != CURDKV_OK ? st : check_kv(K, V, desc);

@@ -5,6 +5,7 @@
 #include <cstdint>
 
 #include "attn_token.cuh"
+#include "attn_window.cuh"
 #include "common.cuh"
 #include "qcache.cuh"
 
@@ -138,6 +139,16 @@ bool launch_attend(const token::Args& a, int64_t problems, cudaStream_t stream) 
   }
   return true;
 }
+
+// The prompt form reads its tensors through TMA maps, whose strides must be positive and below 2^40
+// bytes (where the axis is longer than one).
+bool map_strides_ok(int64_t batch, int64_t heads, int64_t rows, int64_t sb, int64_t sh, int64_t sn) {
+  const int64_t most = (int64_t)1 << 38;
+  return (batch <= 1 || (sb > 0 && sb < most)) && (heads <= 1 || (sh > 0 && sh < most)) && (rows <= 1 || sn < most);
+}
+
+// Query rows per KV head from which the prompt form is taken: see window_form.
+constexpr int kPromptRows = 64;
 
 bool query_strides_ok(const void* x, int64_t sb, int64_t sh, int64_t sn) {
   return x != nullptr && aligned16(x) && sb >= 0 && sh >= 0 && sn >= 128 && sb % 8 == 0 && sh % 8 == 0 && sn % 8 == 0;
@@ -299,6 +310,45 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const int64_t P = (int64_t)desc->batch * desc->kv_heads;
   if (P == 0) return CURDKV_OK;
+  const int group = desc->q_heads / desc->kv_heads;
+  const float scale_log2 = scale * 1.4426950408889634f;
+  if ((int64_t)group * q_rows >= kPromptRows && desc->n_max > 0 &&
+      map_strides_ok(desc->batch, desc->kv_heads, desc->n_max, desc->k_stride_b, desc->k_stride_h, desc->k_stride_n) &&
+      map_strides_ok(desc->batch, desc->kv_heads, desc->n_max, desc->v_stride_b, desc->v_stride_h, desc->v_stride_n) &&
+      map_strides_ok(desc->batch, desc->q_heads, q_rows, q_stride_b, q_stride_h, q_stride_n)) {
+    CUtensorMap mq, mk, mv;
+    if (!rows_map(&mq, Q, desc->batch, desc->q_heads, q_rows, q_stride_b, q_stride_h, q_stride_n) ||
+        !rows_map(&mk, K, desc->batch, desc->kv_heads, desc->n_max, desc->k_stride_b, desc->k_stride_h, desc->k_stride_n) ||
+        !rows_map(&mv, V, desc->batch, desc->kv_heads, desc->n_max, desc->v_stride_b, desc->v_stride_h, desc->v_stride_n))
+      return CURDKV_ERR_CUDA;
+    umma::WindowArgs wa = {};
+    wa.seqlens = desc->seqlens;
+    wa.q_lens = q_lens;
+    wa.batch = desc->batch;
+    wa.heads = desc->kv_heads;
+    wa.group = group;
+    wa.q_rows = q_rows;
+    wa.n_max = desc->n_max;
+    wa.num_sink = num_sink;
+    wa.window = window;
+    // a masked logit is -inf, and -inf times a scale of 0 would be NaN
+    wa.scale_log2 = scale_log2 > 1e-30f ? scale_log2 : 1e-30f;
+    wa.O = static_cast<__nv_bfloat16*>(O);
+    wa.o_sb = o_stride_b; wa.o_sh = o_stride_h; wa.o_sn = o_stride_n;
+    wa.lse = lse;
+    wa.status = static_cast<uint32_t*>(workspace);
+    wa.wait_ns = umma::kWaitLimitNs;
+    const int64_t pairs = (((int64_t)q_rows + kTileRows - 1) / kTileRows * group + 1) / 2;
+    if (P * pairs > 0x3fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+    wa.pairs = (int)pairs;
+    wa.items = (int)(P * pairs);
+    if (cudaFuncSetAttribute(umma::window_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, umma::kWinDynamic) !=
+        cudaSuccess)
+      return CURDKV_ERR_CUDA;
+    const int grid = wa.items < sms() ? wa.items : sms();
+    umma::window_umma_kernel<<<(unsigned)grid, umma::kWinThreads, umma::kWinDynamic, stream>>>(mq, mk, mv, wa);
+    return launched() ? CURDKV_OK : CURDKV_ERR_CUDA;
+  }
   token::Args a = {};
   a.Q = static_cast<const __nv_bfloat16*>(Q);
   a.q_sb = q_stride_b; a.q_sh = q_stride_h; a.q_sn = q_stride_n;
@@ -306,14 +356,14 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
   a.o_sb = o_stride_b; a.o_sh = o_stride_h; a.o_sn = o_stride_n;
   a.lse = lse;
   a.heads = desc->kv_heads;
-  a.group = desc->q_heads / desc->kv_heads;
+  a.group = group;
   a.q_n = q_rows;
   if ((int64_t)a.group * q_rows > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
   a.rows = a.group * q_rows;
   a.blocks = pl.blocks;
   a.splits = pl.splits;
   if (P * pl.blocks * pl.splits > 0x7fffffffLL || P * a.rows > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
-  a.scale_log2 = scale * 1.4426950408889634f;
+  a.scale_log2 = scale_log2;
   a.K = KvView{static_cast<const __nv_bfloat16*>(K), desc->k_stride_b, desc->k_stride_h, desc->k_stride_n};
   a.V = KvView{static_cast<const __nv_bfloat16*>(V), desc->v_stride_b, desc->v_stride_h, desc->v_stride_n};
   a.seqlens = desc->seqlens;

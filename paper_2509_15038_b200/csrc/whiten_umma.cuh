@@ -54,14 +54,6 @@ __device__ __forceinline__ Item item_of(const ItemArgs& a, uint32_t item) {
 __host__ __device__ constexpr uint32_t instr_desc_gram() {
   return instr_desc_bf16(128) | (1u << 15) | (1u << 16);
 }
-// Shared-memory descriptor of a 128-byte-swizzled tile read MN-major: the two
-// 64-channel spans are kHalfBytes apart (leading offset), groups of 8 rows
-// 1024 B apart (stride offset).
-__device__ __forceinline__ uint64_t smem_desc_mn_sw128(uint32_t addr) {
-  return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(kHalfBytes >> 4) << 16) | (64ull << 32) |
-         (1ull << 46) | (2ull << 61);
-}
-
 constexpr int kGramTmemCols = 512;                         // 2 stages x {K, V} x 128 columns
 constexpr int kGramBar = kSlots * kSlotBytes;
 constexpr int kGramDynamic = kGramBar + 256 + 1024;
