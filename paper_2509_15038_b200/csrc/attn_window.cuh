@@ -7,18 +7,24 @@
 // same rows for even groups, neighbouring row blocks for a group of one.  Only the key tiles that some
 // row of the pair sees are walked: those holding sinks, then those of the window.
 //
-// Ten warps.  Two groups of four softmax warps own one query tile each (a thread per row): S = Q K^T
-// arrives in TMEM, the thread keeps its row of 128 logits in registers, the weights go back over S as
-// bf16 and are the A operand of O += P V straight from TMEM.  One thread issues all products in the
-// order  P_A V, S_A', P_B V, S_B'  (S' the next key tile's), so that while one group turns logits
-// into weights the tensor pipe works for the other; P is handed over in halves, so that P V starts
-// on the first 64 keys.  One thread feeds Q and the ring of K and V tiles by TMA.  Items follow each
-// other without a gap: the next pair's first S is issued right behind the last product of this one,
-// and a group writes its O while that runs.
+// Eleven warps.  Four softmax warps own each query tile, a thread per row.  Keys come 64 at a time: S = Q K^T
+// arrives in one of two buffers in TMEM, the thread takes its 64 logits into registers, and the weights
+// go back over S as bf16, where they are the A operand of O += P V straight from TMEM.  Each query tile
+// has an issuing warp of its own: behind P V of a step it issues S two steps ahead into the buffer that
+// P has left, so that the softmax warps always find the next logits ready.  (With one buffer of 128 keys
+// softmax and products of a tile take turns: 4000 cycles per 128 keys and pair of tiles against 2900.)
+// The last warp walks the work: it feeds Q and the ring of K and V tiles by TMA and describes every step
+// (64 keys of one item) to the others in a small ring of its own.  Items follow each other without a gap.
 //
-// What bounds it: 128 x 128 keys cost the tensor pipe 1024 cycles (two products of 512) and the
-// exponentials of the tile 1024 cycles of the special function units, so every kPolyEvery-th pair of
-// weights is formed on the FMA pipe instead (a minimax polynomial of degree 4).
+// An issuing warp has to be quick between its batches of products, or the pipe runs dry: it works
+// converged with one elected lane issuing (inside `if (lane == 0)` the compiler cannot use uniform
+// registers, and a product beside busy softmax warps took 270 cycles to issue instead of 90).
+// Measured and dropped: two threads per row (a tile's softmax 2650 cycles against 1700, the warps crowding
+// each other out); one issuing warp for both tiles (it waits for one while the other is ready).
+//
+// What bounds it: 128 x 128 keys cost the tensor pipe 1280 cycles (S as N = 64 products of 48 cycles, P V
+// of 64) and the exponentials of the tile 1024 cycles of the special function units, so every
+// kPolyEvery-th pair of weights is formed on the FMA pipe instead (a minimax polynomial of degree 4).
 //
 // The running maximum moves only when a tile exceeds it by more than 2^8 (as in attn_umma.cuh); the
 // group then rescales its accumulator in TMEM, which after the first tiles is rare.  Value rows at or
@@ -32,9 +38,9 @@
 
 namespace curdkv {
 
-// Map of a bf16 tensor [batch][heads][rows][128] for tiles of 128 rows (defined beside the C ABI).
+// Map of a bf16 tensor [batch][heads][rows][128] for tiles of tile_rows rows (defined beside the C ABI).
 bool rows_map(CUtensorMap* map, const void* base, int32_t batch, int32_t heads, int32_t rows, int64_t stride_b,
-              int64_t stride_h, int64_t stride_n);
+              int64_t stride_h, int64_t stride_n, int32_t tile_rows);
 
 namespace umma {
 
@@ -50,76 +56,53 @@ struct WindowArgs {
   uint32_t* status;
   int pairs;                         // tile pairs per (sequence, KV head)
   int items;                         // batch * heads * pairs
+                                     // (num_sink and window: at most n_max, and n_max + q_rows below 2^30)
   unsigned long long wait_ns = kWaitLimitNs;
 };
 
-constexpr int kWinThreads = 320;
-constexpr int kWinRing = 5;
+constexpr int kWinThreads = 352;
+constexpr int kWinSoftmaxWarps = 8;
+constexpr int kWinKeys = 64;                               // keys of a step
+constexpr int kWinTileHalf = kWinKeys * 128;               // 64 keys x 64 channels
+constexpr int kWinTileBytes = 2 * kWinTileHalf;
+constexpr int kWinRing = 8;                                // tiles of K and V, in turn
 constexpr int kWinQ = 0;                                   // Q of the two tiles
 constexpr int kWinSlot0 = 2 * kSlotBytes;
-constexpr int kWinBar = kWinSlot0 + kWinRing * kSlotBytes;
-constexpr int kWinDynamic = kWinBar + 256 + 1024;
-constexpr int kWinTmemCols = 512;                          // S_A, S_B, O_A, O_B
+constexpr int kWinStage = kWinSlot0 + kWinRing * kWinTileBytes;         // 2 KB per softmax warp for its output
+constexpr int kWinBar = kWinStage + kWinSoftmaxWarps * 2048;
+constexpr int kWinInfoRing = 8;                            // steps described ahead
+constexpr int kWinDynamic = kWinBar + 1024 + 1024;
+constexpr int kWinTmemCols = 512;                          // S_A (two buffers of 64), S_B, O_A, O_B
 constexpr float kWinSlack = 8.f;
 
-// One query tile of an item: which rows, and which key tiles it needs.
+// A step: 64 keys of one item.  Flag bits of query tile g are shifted by 4 g.
+constexpr uint32_t kStepNeeds = 1u, kStepFirst = 2u, kStepLast = 4u;
+constexpr uint32_t kStepZero = 8u;                         // the query tile has rows that see no key at all: O = 0
+constexpr uint32_t kStepStop = 1u << 8;                    // no step: the work is done
+constexpr uint32_t kStepEmpty = 1u << 9;                   // no key tile: only zeros to write
+constexpr int kStepGroups = 12;                            // from this bit: groups of 16 keys that matter (1 .. 4)
+
+struct alignas(16) StepInfo {
+  uint32_t flags;
+  int j0, n, b;                      // first key; rows of the sequence; sequence
+  int head[2], row0[2];              // query heads; first query rows of the tiles
+  int pos0[2], rows[2];              // position of that row; rows that exist
+};
+static_assert(sizeof(StepInfo) == 48, "written and read as three 16-byte words");
+
+// One query tile of an item, and which tiles of 64 keys it needs: [0, sink_tiles) and [lo, hi).
 struct WinTile {
-  int rb, head;                      // row block, query head within the group
-  int rows;                          // query rows that exist (0: none)
-  int pos0;                          // position of its first row
-  int sink_tiles, lo, hi;            // key tiles [0, sink_tiles) and [lo, hi)
+  int rows, sink_tiles, lo, hi;
   __device__ __forceinline__ bool needs(int kt) const { return kt < sink_tiles || (kt >= lo && kt < hi); }
   __device__ __forceinline__ bool any() const { return sink_tiles > 0 || hi > lo; }
   __device__ __forceinline__ int first() const { return sink_tiles > 0 ? 0 : lo; }
   __device__ __forceinline__ int last() const { return max(sink_tiles, hi > lo ? hi : 0) - 1; }
 };
 
-struct WinItem {
-  int b, h, n, q;                    // sequence, KV head, cached rows, query tokens
-  WinTile t[2];
-  int sinks, lo, hi, tiles;          // key tiles of the pair: [0, sinks), then [lo, hi)
-  __device__ __forceinline__ int key_tile(int u) const { return u < sinks ? u : lo + (u - sinks); }
-};
-
-__device__ __forceinline__ WinItem win_item(const WindowArgs& a, int item) {
-  WinItem w;
-  // longest rows first: the row block falls from the last pair on, heads and sequences vary fastest
-  const int per = a.batch * a.heads;
-  const int pair = a.pairs - 1 - item / per, p = item % per;
-  w.b = p / a.heads;
-  w.h = p % a.heads;
-  w.n = seq_len_of(a.seqlens, w.b, a.n_max);
-  w.q = a.q_lens != nullptr ? min(max(a.q_lens[w.b], 0), a.q_rows) : a.q_rows;
-  w.sinks = 0;
-  w.lo = 0x7fffffff;
-  w.hi = 0;
-#pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    WinTile& t = w.t[g];
-    const int tau = 2 * pair + g;
-    t.rb = tau / a.group;
-    t.head = tau % a.group;
-    t.rows = min(max(w.q - t.rb * kTileRows, 0), kTileRows);
-    t.pos0 = w.n - w.q + t.rb * kTileRows;
-    t.sink_tiles = t.lo = t.hi = 0;
-    const int end = t.rows > 0 ? max(t.pos0 + t.rows, 0) : 0;          // keys [0, end) may be seen
-    if (end > 0) {
-      const int first = (int)max((int64_t)0, (int64_t)max(t.pos0, 0) + 1 - a.window);   // window's first key
-      t.sink_tiles = (min(a.num_sink, end) + kTileRows - 1) / kTileRows;
-      if (a.window > 0) {
-        t.lo = first / kTileRows;
-        t.hi = (end + kTileRows - 1) / kTileRows;
-        w.lo = min(w.lo, t.lo);
-        w.hi = max(w.hi, t.hi);
-      }
-      w.sinks = max(w.sinks, t.sink_tiles);
-    }
-  }
-  if (w.hi == 0) w.lo = 0;
-  w.lo = max(w.lo, w.sinks);                               // the runs do not overlap
-  w.hi = max(w.hi, w.lo);
-  w.tiles = w.sinks + w.hi - w.lo;
-  return w;
+// smem_desc_mn_sw128 for a tile of 64 keys: its two 64-channel spans are kWinTileHalf bytes apart.
+__device__ __forceinline__ uint64_t win_v_desc(uint32_t addr) {
+  return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(kWinTileHalf >> 4) << 16) | (64ull << 32) | (1ull << 46) |
+         (2ull << 61);
 }
 
 // 2^x for x <= 0 on the FMA pipe: x = i + f, |f| <= 1/2, 2^f by the polynomial of degree 4 with the
@@ -162,31 +145,35 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   const uint32_t gbar = bar0 + 8u * 2 * kWinRing;
   auto q_full = [&](int g) { return gbar + 8u * g; };
   auto q_empty = [&](int g) { return gbar + 16u + 8u * g; };
-  auto s_full = [&](int g) { return gbar + 32u + 8u * g; };
-  auto p_ready = [&](int g, int half) { return gbar + 48u + 16u * half + 8u * g; };
-  auto o_full = [&](int g) { return gbar + 80u + 8u * g; };
-  auto o_empty = [&](int g) { return gbar + 96u + 8u * g; };
-  const uint32_t drain_bar = gbar + 112u;
-  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(base_ptr + kWinBar + 8 * (2 * kWinRing + 15));
+  auto s_full = [&](int g, int buf) { return gbar + 32u + 16u * g + 8u * buf; };
+  auto p_ready = [&](int g, int buf) { return gbar + 64u + 16u * g + 8u * buf; };
+  auto o_full = [&](int g) { return gbar + 96u + 8u * g; };
+  auto o_empty = [&](int g) { return gbar + 112u + 8u * g; };
+  auto drain_bar = [&](int g) { return gbar + 128u + 8u * g; };
+  auto pv_done = [&](int g) { return gbar + 144u + 8u * g; };
+  auto info_full = [&](uint32_t e) { return gbar + 160u + 8u * e; };
+  auto info_empty = [&](uint32_t e) { return gbar + 160u + 8u * (kWinInfoRing + e); };
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(base_ptr + kWinBar + 480);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  uint4* info = reinterpret_cast<uint4*>(base_ptr + kWinBar + 512);           // [kWinInfoRing][3]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (tid == 0) {
-    for (int s = 0; s < kWinRing; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int s = 0; s < kWinRing; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 2); }
+    for (int e = 0; e < kWinInfoRing; ++e) { mbar_init(info_full(e), 1); mbar_init(info_empty(e), kWinSoftmaxWarps + 2); }
     for (int g = 0; g < 2; ++g) {
       mbar_init(q_full(g), 1);
       mbar_init(q_empty(g), 1);
-      mbar_init(s_full(g), 1);
-      mbar_init(p_ready(g, 0), 128);
-      mbar_init(p_ready(g, 1), 128);
+      for (int buf = 0; buf < 2; ++buf) { mbar_init(s_full(g, buf), 1); mbar_init(p_ready(g, buf), 128); }
       mbar_init(o_full(g), 1);
       mbar_init(o_empty(g), 128);
+      mbar_init(drain_bar(g), 1);
+      mbar_init(pv_done(g), 1);
     }
-    mbar_init(drain_bar, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 8) {
+  if (warp == kWinSoftmaxWarps) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)),
                  "r"((uint32_t)kWinTmemCols)
                  : "memory");
@@ -197,41 +184,109 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   tc_fence_after();
   const uint32_t tmem_base = *tmem_holder;
 
-  if (warp == 9) {
-    // ------------------------------------------------------------ TMA producer
+  if (warp == kWinSoftmaxWarps + 2) {
+    // ------------------------------------------------------------ the work, step by step, and its tiles
     // Ring order of an item: K_0, V_0, K_1, V_1, ...; its two Q tiles follow K_0.
     if (lane == 0) {
       uint64_t pol;
       asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(pol));
-      uint32_t it = 0, q_it[2] = {0, 0};
+      uint32_t it = 0, step = 0, q_it[2] = {0, 0};
       bool ok = true;
-      auto load = [&](const CUtensorMap* map, int kt, const WinItem& w) {
+      auto wait = [&](uint32_t bar, uint32_t parity) { return ok = ok && mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns); };
+      auto load = [&](const CUtensorMap* map, int j0, int h, int b) {
         const uint32_t slot = it % kWinRing;
-        if (!(ok = mbar_wait(empty_bar(slot), ((it / kWinRing) & 1u) ^ 1u, abort_flag, a.status, a.wait_ns))) return;
-        mbar_arrive_expect_tx(full_bar(slot), kSlotBytes);
-        const uint32_t dst = base + kWinSlot0 + slot * kSlotBytes;
-        tma_load_4d(dst, map, full_bar(slot), 0, kt * kTileRows, w.h, w.b, pol);
-        tma_load_4d(dst + kHalfBytes, map, full_bar(slot), 64, kt * kTileRows, w.h, w.b, pol);
+        if (!wait(empty_bar(slot), ((it / kWinRing) & 1u) ^ 1u)) return;
+        mbar_arrive_expect_tx(full_bar(slot), kWinTileBytes);
+        const uint32_t dst = base + kWinSlot0 + slot * kWinTileBytes;
+        tma_load_4d(dst, map, full_bar(slot), 0, j0, h, b, pol);
+        tma_load_4d(dst + kWinTileHalf, map, full_bar(slot), 64, j0, h, b, pol);
         ++it;
       };
-      for (int item = blockIdx.x; ok && item < a.items; item += gridDim.x) {
-        const WinItem w = win_item(a, item);
-        for (int u = 0; ok && u < w.tiles; ++u) {
-          load(&map_k, w.key_tile(u), w);
+      auto describe = [&](const StepInfo& i) {
+        const uint32_t e = step % kWinInfoRing;
+        if (!wait(info_empty(e), ((step / kWinInfoRing) & 1u) ^ 1u)) return;
+        info[3 * e] = make_uint4(i.flags, (uint32_t)i.j0, (uint32_t)i.n, (uint32_t)i.b);
+        info[3 * e + 1] = make_uint4((uint32_t)i.head[0], (uint32_t)i.head[1], (uint32_t)i.row0[0], (uint32_t)i.row0[1]);
+        info[3 * e + 2] = make_uint4((uint32_t)i.pos0[0], (uint32_t)i.pos0[1], (uint32_t)i.rows[0], (uint32_t)i.rows[1]);
+        mbar_arrive(info_full(e));
+        ++step;
+      };
+      // Items: the row blocks fall from the last pair on (longest rows first); heads and sequences
+      // vary fastest.
+      const int per = a.batch * a.heads;
+      const int skip_pairs = (int)gridDim.x / per, skip_p = (int)gridDim.x % per;
+      int pair = a.pairs - 1 - (int)blockIdx.x / per, p = (int)blockIdx.x % per;
+      while (ok && pair >= 0) {
+        const int b = p / a.heads, h = p % a.heads;
+        StepInfo i;
+        i.b = b;
+        i.n = seq_len_of(a.seqlens, b, a.n_max);
+        const int q = a.q_lens != nullptr ? min(max(a.q_lens[b], 0), a.q_rows) : a.q_rows;
+        WinTile t[2];
+        int sinks = 0, lo = 0x7fffffff, hi = 0, rb = 2 * pair / a.group, head = 2 * pair % a.group;
+        uint32_t zero = 0u;
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          i.head[g] = h * a.group + head;
+          i.row0[g] = rb * kTileRows;
+          i.rows[g] = t[g].rows = min(max(q - rb * kTileRows, 0), kTileRows);
+          i.pos0[g] = i.n - q + rb * kTileRows;
+          t[g].sink_tiles = t[g].lo = t[g].hi = 0;
+          const int end = t[g].rows > 0 ? max(i.pos0[g] + t[g].rows, 0) : 0;       // keys [0, end) may be seen
+          if (end > 0) {
+            t[g].sink_tiles = (min(a.num_sink, end) + kWinKeys - 1) / kWinKeys;
+            if (a.window > 0) {
+              t[g].lo = max(0, max(i.pos0[g], 0) + 1 - a.window) / kWinKeys;
+              t[g].hi = (end + kWinKeys - 1) / kWinKeys;
+              lo = min(lo, t[g].lo);
+              hi = max(hi, t[g].hi);
+            }
+            sinks = max(sinks, t[g].sink_tiles);
+          }
+          if (t[g].rows > 0 && !t[g].any()) zero |= kStepZero << (4 * g);
+          if (++head == a.group) { head = 0; ++rb; }
+        }
+        const int win_lo = lo;                             // first key tile that holds keys of a window
+        lo = max(hi > 0 ? lo : 0, sinks);                  // the pair's key tiles: [0, sinks), then [lo, hi)
+        const int tiles = sinks + max(hi - lo, 0);
+        if (tiles == 0 && zero != 0u) {
+          i.flags = kStepEmpty | zero;
+          i.j0 = 0;
+          describe(i);
+        }
+        for (int u = 0; ok && u < tiles; ++u) {
+          const int kt = u < sinks ? u : lo + (u - sinks);
+          i.j0 = kt * kWinKeys;
+          // a tile below the window holds sinks only: the rest of its keys need no products
+          const int keys = kt >= win_lo ? kWinKeys : min(a.num_sink - i.j0, kWinKeys);
+          i.flags = (uint32_t)((keys + 15) >> 4) << kStepGroups | (u == 0 ? zero : 0u);
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
+            if (t[g].needs(kt))
+              i.flags |= (kStepNeeds | (kt == t[g].first() ? kStepFirst : 0u) | (kt == t[g].last() ? kStepLast : 0u)) << (4 * g);
+          describe(i);
+          if (ok) load(&map_k, i.j0, h, b);
           if (u == 0) {
-            for (int g = 0; ok && g < 2; ++g) {
-              if (!w.t[g].any()) continue;           // nothing to multiply
-              if (!(ok = mbar_wait(q_empty(g), (q_it[g] & 1u) ^ 1u, abort_flag, a.status, a.wait_ns))) break;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+              if (!t[g].any() || !wait(q_empty(g), (q_it[g] & 1u) ^ 1u)) continue;
               mbar_arrive_expect_tx(q_full(g), kSlotBytes);
               const uint32_t dst = base + kWinQ + g * kSlotBytes;
-              const int hq = w.h * a.group + w.t[g].head;
-              tma_load_4d(dst, &map_q, q_full(g), 0, w.t[g].rb * kTileRows, hq, w.b, pol);
-              tma_load_4d(dst + kHalfBytes, &map_q, q_full(g), 64, w.t[g].rb * kTileRows, hq, w.b, pol);
+              tma_load_4d(dst, &map_q, q_full(g), 0, i.row0[g], i.head[g], b, pol);
+              tma_load_4d(dst + kHalfBytes, &map_q, q_full(g), 64, i.row0[g], i.head[g], b, pol);
               ++q_it[g];
             }
           }
-          if (ok) load(&map_v, w.key_tile(u), w);
+          if (ok) load(&map_v, i.j0, h, b);
         }
+        pair -= skip_pairs;
+        p += skip_p;
+        if (p >= per) { p -= per; --pair; }
+      }
+      if (ok) {
+        StepInfo i = {};
+        i.flags = kStepStop;
+        describe(i);
       }
       if (!ok) {                                           // let what was issued land before the CTA ends
         auto land = [&](uint32_t bar, uint32_t parity) {
@@ -239,105 +294,116 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           while (!mbar_try_wait(bar, parity) && global_ns() - t0 < a.wait_ns) {}
         };
         const uint32_t pending = it < (uint32_t)kWinRing ? it : (uint32_t)kWinRing;
-        for (uint32_t q = it - pending; q < it; ++q) land(full_bar(q % kWinRing), (q / kWinRing) & 1u);
+        for (uint32_t k = it - pending; k < it; ++k) land(full_bar(k % kWinRing), (k / kWinRing) & 1u);
+#pragma unroll
         for (int g = 0; g < 2; ++g)
           if (q_it[g] > 0) land(q_full(g), (q_it[g] - 1) & 1u);
       }
     }
-  } else if (warp == 8) {
-    // ------------------------------------------------------------ MMA issuer
-    if (lane == 0) {
-      constexpr uint32_t idesc_s = instr_desc_bf16(128);
-      constexpr uint32_t idesc_pv = instr_desc_pv();
-      uint32_t q_it[2] = {0, 0}, p_it[2] = {0, 0}, o_it[2] = {0, 0};
-      bool ok = true;
-      auto wait = [&](uint32_t bar, uint32_t parity) {
-        ok = ok && mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns);
-        return ok;
-      };
-      // One step is one key tile of one item; steps follow each other across items.
-      struct Step {
-        WinItem w;
-        int item, u;
-        uint32_t it;                                       // ring position of this step's K tile (V follows)
-      };
-      auto settle = [&](Step& s) {                         // the first item from s.item on that has key tiles
-        while (s.item < a.items) {
-          s.w = win_item(a, s.item);
-          if (s.w.tiles > 0) break;
-          s.item += gridDim.x;
+  } else if (warp >= kWinSoftmaxWarps) {
+    // ------------------------------------------------------------ products of query tile g
+    // The whole warp walks the steps and waits; one elected lane issues.
+    const int g = warp - kWinSoftmaxWarps;
+    constexpr uint32_t idesc_pv = instr_desc_pv();
+    constexpr uint32_t kSlotUnits = kWinTileBytes >> 4;
+    const uint64_t q_desc = smem_desc_sw128(base + kWinQ + g * kSlotBytes);
+    const uint64_t k_desc0 = smem_desc_sw128(base + kWinSlot0), v_desc0 = win_v_desc(base + kWinSlot0);
+    const uint32_t s_tmem = tmem_base + g * 128u, o_tmem = tmem_base + 256u + g * 128u;
+    uint32_t step = 0, it = 0;                             // steps described; ring entries described (two a step)
+    uint32_t q_phase = 0, p_phase = 0, o_phase = 1;        // (p_phase: a bit per buffer)
+    bool ok = true;                                        // the lanes agree on it at the end of each step
+    auto wait = [&](uint32_t bar, uint32_t parity) { ok = mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns) && ok; };
+    struct Pending { uint32_t f, it; };                    // flags and first ring entry of a step
+    auto next_step = [&](const Pending& before) {          // the step after the last one described
+      Pending s;
+      s.f = before.f;
+      s.it = it;
+      if (before.f & kStepStop) return s;
+      const uint32_t e = step % kWinInfoRing;
+      wait(info_full(e), (step / kWinInfoRing) & 1u);
+      const uint32_t f = info[3 * e].x;
+      __syncwarp();
+      if (elect_one()) mbar_arrive(info_empty(e));
+      ++step;
+      if (!(f & (kStepStop | kStepEmpty))) it += 2;
+      s.f = (f >> (4 * g) & 15u) | (f & ~255u);            // this tile's bits at the bottom
+      return s;
+    };
+    // S = Q K^T over the keys that matter, into buffer `buf`
+    auto issue_s = [&](const Pending& s, uint32_t buf) {
+      if (s.f & (kStepStop | kStepEmpty)) return;
+      const uint32_t slot = s.it % kWinRing;
+      wait(full_bar(slot), (s.it / kWinRing) & 1u);        // (a slot may only be given back once it was filled)
+      if (s.f & kStepNeeds) {
+        if (s.f & kStepFirst) {
+          wait(q_full(g), q_phase);
+          q_phase ^= 1u;
         }
-        s.u = 0;
-      };
-      // S_g = Q_g K^T of a step, if the step is one of tile g's
-      auto issue_s = [&](const Step& s, int g) {
-        const WinTile& t = s.w.t[g];
-        const int kt = s.w.key_tile(s.u);
-        const uint32_t slot = s.it % kWinRing;
-        if (!wait(full_bar(slot), (s.it / kWinRing) & 1u) || !t.needs(kt)) return;
-        if (kt == t.first() && !wait(q_full(g), q_it[g]++ & 1u)) return;
         tc_fence_after();
-        const uint64_t q_desc = smem_desc_sw128(base + kWinQ + g * kSlotBytes);
-        const uint64_t k_desc = smem_desc_sw128(base + kWinSlot0 + slot * kSlotBytes);
+        const uint64_t kd = k_desc0 + slot * kSlotUnits;
+        const uint32_t idesc = instr_desc_bf16(16 * (int)((s.f >> kStepGroups) & 15u));
+        if (elect_one()) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t off = (uint32_t)(k >> 2) * (kHalfBytes >> 4) + (uint32_t)(k & 3) * 2u;
-          tc_mma_bf16(tmem_base + g * 128u, q_desc + off, k_desc + off, idesc_s, k > 0);
+          for (int k = 0; k < 8; ++k)
+            tc_mma_bf16(s_tmem + 64u * buf, q_desc + (uint32_t)(k >> 2) * (kHalfBytes >> 4) + (uint32_t)(k & 3) * 2u,
+                        kd + (uint32_t)(k >> 2) * (kWinTileHalf >> 4) + (uint32_t)(k & 3) * 2u, idesc, k > 0);
+          tc_commit(s_full(g, buf));
+          tc_commit(empty_bar(slot));
+          if (s.f & kStepLast) tc_commit(q_empty(g));
         }
-        tc_commit(s_full(g));
-        if (kt == t.last()) tc_commit(q_empty(g));
-      };
-      // O_g (+)= P_g V of a step
-      auto issue_pv = [&](const Step& s, int g) {
-        const WinTile& t = s.w.t[g];
-        const int kt = s.w.key_tile(s.u);
-        const uint32_t at = s.it + 1, slot = at % kWinRing;
-        const bool first = kt == t.first();
-        if (!wait(full_bar(slot), (at / kWinRing) & 1u) || !t.needs(kt)) return;
-        if (first && !wait(o_empty(g), (o_it[g]++ & 1u) ^ 1u)) return;
-        const uint64_t v_desc = smem_desc_mn_sw128(base + kWinSlot0 + slot * kSlotBytes);
-        const uint32_t o_tmem = tmem_base + 256u + g * 128u, p_tmem = tmem_base + g * 128u;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          if (!wait(p_ready(g, half), p_it[g] & 1u)) return;
-          tc_fence_after();
-#pragma unroll
-          for (int k = 4 * half; k < 4 * half + 4; ++k)    // 16 keys: 8 columns of P, 2048 bytes of V
-            tc_mma_bf16_ts(o_tmem, p_tmem + 8u * k, v_desc + 128u * k, idesc_pv, (!first || k > 0) ? 1u : 0u);
-        }
-        ++p_it[g];
-        if (kt == t.last()) tc_commit(o_full(g));
-      };
-      Step now, next;
-      next.item = blockIdx.x;
-      next.it = 0;
-      settle(next);
-      if (next.item < a.items) {
-        issue_s(next, 0);
-        if (ok) issue_s(next, 1);
-        if (ok) tc_commit(empty_bar(next.it % kWinRing));
+      } else if (elect_one()) {
+        mbar_arrive(empty_bar(slot));
       }
-      while (ok && next.item < a.items) {
-        now = next;
-        next.it += 2;
-        if (++next.u == next.w.tiles) {
-          next.item += gridDim.x;
-          settle(next);
+      __syncwarp();
+    };
+    // O (+)= P V with the weights in buffer `buf`
+    auto issue_pv = [&](const Pending& s, uint32_t buf) {
+      if (s.f & (kStepStop | kStepEmpty)) return;
+      const uint32_t at = s.it + 1, slot = at % kWinRing;
+      wait(full_bar(slot), (at / kWinRing) & 1u);
+      if (s.f & kStepNeeds) {
+        const uint32_t first = s.f & kStepFirst;
+        if (first) {
+          wait(o_empty(g), o_phase);
+          o_phase ^= 1u;
         }
-        const bool more = next.item < a.items;
+        const uint64_t vd = v_desc0 + slot * kSlotUnits;
+        const int groups = (int)((s.f >> kStepGroups) & 15u);
+        wait(p_ready(g, buf), (p_phase >> buf) & 1u);
+        p_phase ^= 1u << buf;
+        tc_fence_after();
+        if (elect_one()) {
+          // 16 keys per product: 8 columns of P, 2048 bytes (128 units) of V
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          if (ok) issue_pv(now, g);
-          if (g == 1 && ok) tc_commit(empty_bar((now.it + 1) % kWinRing));       // V of this step
-          if (ok && more) issue_s(next, g);
+          for (int k = 0; k < 4; ++k)
+            if (k < groups)
+              tc_mma_bf16_ts(o_tmem, s_tmem + 64u * buf + 8u * k, vd + 128u * k, idesc_pv, (!first || k > 0) ? 1u : 0u);
+          tc_commit(empty_bar(slot));
+          tc_commit(pv_done(g));
+          if (s.f & kStepLast) tc_commit(o_full(g));
         }
-        if (ok && more) tc_commit(empty_bar(next.it % kWinRing));                // K of the next
+      } else if (elect_one()) {
+        mbar_arrive(empty_bar(slot));
       }
-      if (!ok) {
-        tc_commit(drain_bar);
-        const unsigned long long t0 = global_ns();
-        while (!mbar_try_wait(drain_bar, 0) && global_ns() - t0 < a.wait_ns) {}
-      }
+      __syncwarp();
+    };
+    Pending now = next_step(Pending{0u, 0u});
+    issue_s(now, 0);
+    Pending next = next_step(now);
+    issue_s(next, 1);
+    uint32_t buf = 0;
+    while ((ok = __all_sync(0xffffffffu, ok)) && !(now.f & kStepStop)) {
+      issue_pv(now, buf);
+      now = next;
+      next = next_step(now);
+      issue_s(next, buf);
+      buf ^= 1u;
+    }
+    if (!ok) {
+      if (elect_one()) tc_commit(drain_bar(g));
+      __syncwarp();
+      const unsigned long long t0 = global_ns();
+      while (!mbar_try_wait(drain_bar(g), 0) && global_ns() - t0 < a.wait_ns) {}
     }
   } else {
     // ------------------------------------------------------------ softmax and output
@@ -347,129 +413,169 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const uint32_t lane_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
     const uint32_t s_addr = lane_addr + g * 128u, o_addr = lane_addr + 256u + g * 128u;
     const float sc = a.scale_log2;
-    uint32_t it = 0, s_it = 0, o_it = 0;
-    bool ok = true;
-    for (int item = blockIdx.x; ok && item < a.items; item += gridDim.x) {
-      const WinItem w = win_item(a, item);
-      const WinTile t = g == 0 ? w.t[0] : w.t[1];
-      const int pos = t.pos0 + r;
-      float top = -INFINITY, sum = 0.f;
-      for (int u = 0; ok && u < w.tiles; ++u) {
-        const int kt = w.key_tile(u), j0 = kt * kTileRows;
-        if (!t.needs(kt)) continue;
-        if (j0 + kTileRows > w.n) {                        // value rows behind the sequence: cleared
-          const uint32_t at = it + 2 * u + 1, slot = at % kWinRing;
-          if (!(ok = warp_wait(full_bar(slot), (at / kWinRing) & 1u, abort_flag, a.status, a.wait_ns))) break;
-          unsigned char* v = base_ptr + kWinSlot0 + slot * kSlotBytes;
-          const int dead = kTileRows - max(w.n - j0, 0), from = kTileRows - dead;
-          for (int e = r; e < dead * 16; e += kTileRows) {
-            const int row = from + (e >> 4), c = e & 15;
-            *reinterpret_cast<uint4*>(v + (c >> 3) * kHalfBytes + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+    const uint64_t sc2 = pack2(sc, sc);
+    uint32_t step = 0, tiles = 0;                          // steps seen; key tiles passed
+    uint32_t s_phase = 0, o_phase = 0;                     // (s_phase: a bit per buffer)
+    uint32_t products = 0;                                 // P V products of this tile so far (over all items)
+    float top = -INFINITY, sum = 0.f;
+    for (;; ++step) {
+      const uint32_t e = step % kWinInfoRing;
+      if (!warp_wait(info_full(e), (step / kWinInfoRing) & 1u, abort_flag, a.status, a.wait_ns)) break;
+      const uint4 i0 = info[3 * e], i1 = info[3 * e + 1], i2 = info[3 * e + 2];
+      __syncwarp();
+      if (elect_one()) mbar_arrive(info_empty(e));
+      const uint32_t flags = i0.x >> (4 * g);
+      if (i0.x & kStepStop) break;
+      const uint32_t v_at = 2 * tiles + 1;                 // ring entry of this tile's V
+      if (!(i0.x & kStepEmpty)) ++tiles;
+      if (!(flags & (kStepNeeds | kStepZero))) continue;
+      const uint32_t buf = step & 1u, sb_addr = s_addr + 64u * buf;
+      const int j0 = (int)i0.y, n = (int)i0.z;
+      const int pos0 = (int)(g == 0 ? i2.x : i2.y), rows = (int)(g == 0 ? i2.z : i2.w);
+      const int pos = pos0 + r, pos_lo = pos0 + quarter * 32;              // this row; the warp's first
+      if (flags & (kStepFirst | kStepZero)) {
+        top = -INFINITY;
+        sum = 0.f;
+      }
+      if (flags & kStepNeeds) {
+        if (j0 + kWinKeys > n) {                           // value rows behind the sequence: cleared
+          const uint32_t slot = v_at % kWinRing;
+          if (!warp_wait(full_bar(slot), (v_at / kWinRing) & 1u, abort_flag, a.status, a.wait_ns)) break;
+          unsigned char* v = base_ptr + kWinSlot0 + slot * kWinTileBytes;
+          const int from = max(n - j0, 0);
+          for (int x = r; x < (kWinKeys - from) * 16; x += kTileRows) {
+            const int row = from + (x >> 4), c = x & 15;
+            *reinterpret_cast<uint4*>(v + (c >> 3) * kWinTileHalf + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
-        if (!(ok = warp_wait(s_full(g), s_it & 1u, abort_flag, a.status, a.wait_ns))) break;
-        ++s_it;
+        if (!warp_wait(s_full(g, buf), (s_phase >> buf) & 1u, abort_flag, a.status, a.wait_ns)) break;
+        s_phase ^= 1u << buf;
         tc_fence_after();
-        float v[128];
-#pragma unroll
-        for (int c0 = 0; c0 < 128; c0 += 32) tmem_ld32(s_addr + c0, *reinterpret_cast<float(*)[32]>(v + c0));
-        tmem_ld_wait();
-        // a tile that every row of the query tile sees whole needs no mask
-        const bool whole = j0 + kTileRows - 1 <= t.pos0 &&
-                           ((int64_t)j0 > (int64_t)t.pos0 + kTileRows - 1 - a.window || j0 + kTileRows <= a.num_sink);
-        if (!whole) {
-          // columns [lo, hi) are in the window, those below sk are sinks
-          const int hi = min(max(pos + 1 - j0, 0), 128);
-          const int lo = (int)min(max((int64_t)pos + 1 - a.window - j0, (int64_t)0), (int64_t)128);
-          const int sk = min(max(a.num_sink - j0, 0), 128);
-#pragma unroll
-          for (int c0 = 0; c0 < 128; c0 += 32) {
-            auto below = [&](int x) { return x >= c0 + 32 ? 0xffffffffu : (x <= c0 ? 0u : (1u << (x - c0)) - 1u); };
-            const uint32_t see = below(hi) & (~below(lo) | below(sk));
-#pragma unroll
-            for (int c = 0; c < 32; ++c)
-              if (!((see >> c) & 1u)) v[c0 + c] = -INFINITY;
-          }
-        }
-        float ext[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-        for (int c = 4; c < 124; c += 8)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) ext[j] = max3(ext[j], v[c + 2 * j], v[c + 2 * j + 1]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) ext[j] = fmaxf(ext[j], v[124 + j]);
-        const float tile_top = fmaxf(fmaxf(ext[0], ext[1]), fmaxf(ext[2], ext[3])) * sc;
-        const bool move = tile_top > top + kWinSlack || top == -INFINITY;
-        const float new_top = move ? fmaxf(top, tile_top) : top;
-        if (kt != t.first() && __any_sync(0xffffffffu, move)) {      // (the previous product has retired)
-          const float alpha = !move || new_top == -INFINITY ? 1.f : fast_exp2(top - new_top);
-          sum *= alpha;
-#pragma unroll 1
-          for (int c0 = 0; c0 < 128; c0 += 32) {
-            float o[32];
-            tmem_ld32(o_addr + c0, o);
-            tmem_ld_wait();
-#pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] *= alpha;
-            tmem_st32(o_addr + c0, o);
-          }
-          tmem_st_wait();
-        }
-        top = new_top;
-        const float ref = top == -INFINITY ? 0.f : top;
-        const uint64_t sc2 = pack2(sc, sc), nref2 = pack2(-ref, -ref);
-        uint64_t part[4] = {0ull, 0ull, 0ull, 0ull};
-        // (a masked logit has to give exactly 0, which the polynomial does not: special function units
-        // alone for the few tiles with a mask)
-        auto weights = [&](auto poly) {
-#pragma unroll
-          for (int c0 = 0; c0 < 128; c0 += 32) {
-            uint32_t h[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const uint64_t x2 = fma2(pack2(v[c0 + 2 * e], v[c0 + 2 * e + 1]), sc2, nref2);
-              uint64_t w2;
-              if (poly.value && e % kPolyEvery == kPolyEvery - 1) {
-                w2 = exp2_poly2(x2);
-              } else {
-                float x0, x1;
-                unpack2(x2, x0, x1);
-                w2 = pack2(fast_exp2(x0), fast_exp2(x1));
-              }
-              part[e & 3] = add2(part[e & 3], w2);
-              float w0, w1;
-              unpack2(w2, w0, w1);
-              const __nv_bfloat162 b2 = __floats2bfloat162_rn(w0, w1);
-              h[e] = *reinterpret_cast<const uint32_t*>(&b2);
-            }
-            tmem_st16(s_addr + (uint32_t)c0 / 2, h);
-            if (c0 == 32 || c0 == 96) {                    // 64 keys' weights are in place
-              tmem_st_wait();
-              tc_fence_before();
-              mbar_arrive(p_ready(g, c0 == 96));
-            }
-          }
+        // What the warp's 32 rows see of each 32 keys: all, none, or some.  Tiles seen whole (most) run
+        // without a branch.
+        auto all_seen = [&](int k, int keys) {
+          return k + keys - 1 <= pos_lo && (k > pos_lo + 31 - a.window || k + keys <= a.num_sink);
         };
-        if (whole) weights(std::true_type{});
-        else weights(std::false_type{});
+        auto none_seen = [&](int k) {
+          return k > pos_lo + 31 || (k >= a.num_sink && k + 31 <= pos_lo - a.window);
+        };
+        const bool whole = all_seen(j0, kWinKeys);
+        float v[64];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) tmem_ld32(sb_addr + 32 * c, *reinterpret_cast<float(*)[32]>(v + 32 * c));
+        tmem_ld_wait();
+        float mx;
+        if (whole) {
+          float ext[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+          for (int e = 4; e < 60; e += 8)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ext[j] = max3(ext[j], v[e + 2 * j], v[e + 2 * j + 1]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) ext[j] = fmaxf(ext[j], v[60 + j]);
+          mx = fmaxf(fmaxf(ext[0], ext[1]), fmaxf(ext[2], ext[3]));
+        } else {
+          mx = -INFINITY;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const int k = j0 + 32 * c;
+            if (none_seen(k)) continue;
+            if (!all_seen(k, 32)) {
+              // columns [lo, hi) are in the window, those below sk are sinks
+              auto below = [](int x) { return x >= 32 ? 0xffffffffu : (x <= 0 ? 0u : (1u << x) - 1u); };
+              const uint32_t see = below(pos + 1 - k) & (~below(pos + 1 - a.window - k) | below(a.num_sink - k));
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (!(see & (1u << e))) v[32 * c + e] = -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) mx = max3(mx, v[32 * c + e], v[32 * c + e + 1]);
+          }
+        }
+        const float tile_top = mx * sc;
+        const bool move = tile_top > top + kWinSlack || top == -INFINITY;
+        if (__any_sync(0xffffffffu, move)) {
+          const float new_top = move ? fmaxf(top, tile_top) : top;
+          if (!(flags & kStepFirst)) {                     // rescale, once the previous product has retired
+            if (!warp_wait(pv_done(g), (products - 1u) & 1u, abort_flag, a.status, a.wait_ns)) break;
+            tc_fence_after();
+            const float alpha = !move || new_top == -INFINITY ? 1.f : fast_exp2(top - new_top);
+            sum *= alpha;
+#pragma unroll 1
+            for (int c0 = 0; c0 < 128; c0 += 16) {
+              uint32_t o[16];
+              tmem_ld16(o_addr + c0, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int c = 0; c < 16; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * alpha);
+              tmem_st16(o_addr + c0, o);
+            }
+            tmem_st_wait();
+          }
+          top = new_top;
+        }
+        const float ref = top == -INFINITY ? 0.f : top;
+        const uint64_t nref2 = pack2(-ref, -ref);
+        uint64_t part[2] = {0ull, 0ull};
+        // (a masked logit has to give exactly 0, which the polynomial does not)
+        auto weights = [&](int c, auto poly) {
+          uint32_t h[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const uint64_t x2 = fma2(pack2(v[32 * c + 2 * e], v[32 * c + 2 * e + 1]), sc2, nref2);
+            uint64_t w2;
+            if (poly.value && e % kPolyEvery == kPolyEvery - 1) {
+              w2 = exp2_poly2(x2);
+            } else {
+              float x0, x1;
+              unpack2(x2, x0, x1);
+              w2 = pack2(fast_exp2(x0), fast_exp2(x1));
+            }
+            part[e & 1] = add2(part[e & 1], w2);
+            float w0, w1;
+            unpack2(w2, w0, w1);
+            const __nv_bfloat162 b2 = __floats2bfloat162_rn(w0, w1);
+            h[e] = *reinterpret_cast<const uint32_t*>(&b2);
+          }
+          tmem_st16(sb_addr + 16 * c, h);
+        };
+        if (whole) {
+          weights(0, std::true_type{});
+          weights(1, std::true_type{});
+        } else {
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            if (none_seen(j0 + 32 * c)) {
+              uint32_t h[16];
+#pragma unroll
+              for (int e = 0; e < 16; ++e) h[e] = 0u;
+              tmem_st16(sb_addr + 16 * c, h);
+            } else {
+              weights(c, std::false_type{});
+            }
+          }
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(p_ready(g, buf));
+        ++products;
         float p0, p1;
-        unpack2(add2(add2(part[0], part[1]), add2(part[2], part[3])), p0, p1);
+        unpack2(add2(part[0], part[1]), p0, p1);
         sum += p0 + p1;
-      }
-      it += 2 * w.tiles;
-      // ---- output of this tile
-      const bool any = t.any();
-      if (any && ok) {
-        ok = warp_wait(o_full(g), o_it & 1u, abort_flag, a.status, a.wait_ns);
-        ++o_it;
+        if (!(flags & kStepLast)) continue;
+        if (!warp_wait(o_full(g), o_phase, abort_flag, a.status, a.wait_ns)) break;
+        o_phase ^= 1u;
         tc_fence_after();
       }
-      if (ok) {
+      // ---- output of this tile
+      {
+        const bool any = flags & kStepNeeds;
         const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);    // a NaN sum stays one
-        const int hq = w.h * a.group + t.head;
-        const int64_t row = (int64_t)t.rb * kTileRows + r;
-        __nv_bfloat16* out = a.O + w.b * a.o_sb + hq * a.o_sh + row * a.o_sn;
+        const int b = (int)i0.w, hq = (int)(g == 0 ? i1.x : i1.y), row0 = (int)(g == 0 ? i1.z : i1.w);
+        __nv_bfloat16* out = a.O + b * a.o_sb + hq * a.o_sh + (int64_t)(row0 + quarter * 32) * a.o_sn;
+        unsigned char* stage = base_ptr + kWinStage + warp * 2048;           // 32 rows of 64 bytes
+        const int live = rows - quarter * 32;
 #pragma unroll 1
         for (int c0 = 0; c0 < 128; c0 += 32) {
           float o[32];
@@ -480,24 +586,34 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
             for (int c = 0; c < 32; ++c) o[c] = 0.f;
           }
-          if (r < t.rows) {
+          // Rows go through shared memory, so that four lanes write 64 bytes of one row side by side
+          // (16-byte stores to 32 different rows took 8000 cycles a tile).  Two rows share 128 bytes, whose
+          // eight places are permuted against bank conflicts.
 #pragma unroll
-            for (int c = 0; c < 32; c += 8) {
-              uint4 x;
-              x.x = token::pack_bf16(o[c] * inv, o[c + 1] * inv);
-              x.y = token::pack_bf16(o[c + 2] * inv, o[c + 3] * inv);
-              x.z = token::pack_bf16(o[c + 4] * inv, o[c + 5] * inv);
-              x.w = token::pack_bf16(o[c + 6] * inv, o[c + 7] * inv);
-              *reinterpret_cast<uint4*>(out + c0 + c) = x;
-            }
+          for (int c = 0; c < 4; ++c) {
+            uint4 x;
+            x.x = token::pack_bf16(o[8 * c] * inv, o[8 * c + 1] * inv);
+            x.y = token::pack_bf16(o[8 * c + 2] * inv, o[8 * c + 3] * inv);
+            x.z = token::pack_bf16(o[8 * c + 4] * inv, o[8 * c + 5] * inv);
+            x.w = token::pack_bf16(o[8 * c + 6] * inv, o[8 * c + 7] * inv);
+            const int place = ((lane & 1) * 4 + c) ^ ((lane >> 1) & 7);
+            *reinterpret_cast<uint4*>(stage + (lane >> 1) * 128 + place * 16) = x;
           }
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int row = 8 * k + (lane >> 2), c = lane & 3, place = ((row & 1) * 4 + c) ^ ((row >> 1) & 7);
+            const uint4 x = *reinterpret_cast<const uint4*>(stage + (row >> 1) * 128 + place * 16);
+            if (row < live) *reinterpret_cast<uint4*>(out + (int64_t)row * a.o_sn + c0 + 8 * c) = x;
+          }
+          __syncwarp();
         }
         if (any) {
           tc_fence_before();
           mbar_arrive(o_empty(g));
         }
-        if (r < t.rows && a.lse != nullptr)
-          a.lse[((int64_t)w.b * a.heads * a.group + hq) * a.q_rows + row] =
+        if (r < rows && a.lse != nullptr)
+          a.lse[((int64_t)b * a.heads * a.group + hq) * a.q_rows + row0 + r] =
               sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
       }
     }
@@ -505,7 +621,7 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
   tc_fence_before();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == kWinSoftmaxWarps) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)kWinTmemCols)
                  : "memory");

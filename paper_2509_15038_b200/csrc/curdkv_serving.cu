@@ -312,14 +312,16 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
   if (P == 0) return CURDKV_OK;
   const int group = desc->q_heads / desc->kv_heads;
   const float scale_log2 = scale * 1.4426950408889634f;
-  if ((int64_t)group * q_rows >= kPromptRows && desc->n_max > 0 &&
+  if ((int64_t)group * q_rows >= kPromptRows && desc->n_max > 0 && (int64_t)desc->n_max + q_rows < (1 << 30) &&
       map_strides_ok(desc->batch, desc->kv_heads, desc->n_max, desc->k_stride_b, desc->k_stride_h, desc->k_stride_n) &&
       map_strides_ok(desc->batch, desc->kv_heads, desc->n_max, desc->v_stride_b, desc->v_stride_h, desc->v_stride_n) &&
       map_strides_ok(desc->batch, desc->q_heads, q_rows, q_stride_b, q_stride_h, q_stride_n)) {
     CUtensorMap mq, mk, mv;
-    if (!rows_map(&mq, Q, desc->batch, desc->q_heads, q_rows, q_stride_b, q_stride_h, q_stride_n) ||
-        !rows_map(&mk, K, desc->batch, desc->kv_heads, desc->n_max, desc->k_stride_b, desc->k_stride_h, desc->k_stride_n) ||
-        !rows_map(&mv, V, desc->batch, desc->kv_heads, desc->n_max, desc->v_stride_b, desc->v_stride_h, desc->v_stride_n))
+    if (!rows_map(&mq, Q, desc->batch, desc->q_heads, q_rows, q_stride_b, q_stride_h, q_stride_n, kTileRows) ||
+        !rows_map(&mk, K, desc->batch, desc->kv_heads, desc->n_max, desc->k_stride_b, desc->k_stride_h, desc->k_stride_n,
+                  umma::kWinKeys) ||
+        !rows_map(&mv, V, desc->batch, desc->kv_heads, desc->n_max, desc->v_stride_b, desc->v_stride_h, desc->v_stride_n,
+                  umma::kWinKeys))
       return CURDKV_ERR_CUDA;
     umma::WindowArgs wa = {};
     wa.seqlens = desc->seqlens;
@@ -329,8 +331,8 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
     wa.group = group;
     wa.q_rows = q_rows;
     wa.n_max = desc->n_max;
-    wa.num_sink = num_sink;
-    wa.window = window;
+    wa.num_sink = num_sink < desc->n_max ? num_sink : desc->n_max;
+    wa.window = window < desc->n_max ? window : desc->n_max;
     // a masked logit is -inf, and -inf times a scale of 0 would be NaN
     wa.scale_log2 = scale_log2 > 1e-30f ? scale_log2 : 1e-30f;
     wa.O = static_cast<__nv_bfloat16*>(O);
