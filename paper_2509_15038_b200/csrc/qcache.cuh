@@ -45,16 +45,65 @@ __device__ __forceinline__ bool rows_of(const View& c, int64_t p, int64_t& first
   return ok;
 }
 
-// rint((x - z) / s) in 64 bits: the definition, for values that the 32-bit path finds next to a
-// border between two codes (about one in 10^5).
-__device__ __noinline__ float code_exact(float x, float z, float s) {
-  const double q = rint(((double)x - (double)z) / (double)s);
-  return (float)fmin(fmax(q, 0.0), 15.0);
+// The exact code of each of eight values, given one that is off by at most one.  With r that code,
+// e = (x - z) - r s is formed without error (the difference by TwoSum, r s by the fused multiply-add)
+// and compared with s / 2; ties go to the even code.
+__device__ __noinline__ void codes_exact(const float (&x)[8], float z, float s, float (&r)[8]) {
+  const float h = 0.5f * s;
+#pragma unroll 1
+  for (int u = 0; u < 8; ++u) {
+    if (s < 0x1p-100f || s > 0x1p100f) {                   // products below may leave fp32's range
+      r[u] = (float)fmin(fmax(rint(((double)x[u] - (double)z) / (double)s), 0.0), 15.0);
+      continue;
+    }
+    const float d = __fsub_rn(x[u], z), back = __fsub_rn(d, x[u]);
+    float low = __fadd_rn(__fsub_rn(x[u], __fsub_rn(d, back)), __fsub_rn(-z, back));   // x - z = d + low
+    if (fabsf(low) < 0x1p-50f * s) low = 0.f;              // beyond 64-bit arithmetic's sight
+    const float e = __fmaf_rn(-r[u], s, d), over = (fabsf(e) - h) + copysignf(1.f, e) * low;
+    const bool odd = (int)r[u] & 1;
+    if (over > 0.f || (over == 0.f && odd)) r[u] += copysignf(1.f, e);
+    r[u] = fminf(fmaxf(r[u], 0.f), 15.f);
+  }
 }
 
-// The eight channels 8 * l16 .. 8 * l16 + 7 of one row: their codes, four bits each from the
-// lowest, and the (scale, zero) word of their group, which four neighbouring lanes share.  All 32
-// lanes of the warp call this together.
+// Pairs of fp32 values in one instruction.
+__device__ __forceinline__ uint64_t f2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void unf2(uint64_t r, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ uint64_t add_f2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t mul_f2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t fma_f2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t sub_f2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// d / 15 correctly rounded: one correction by the exact residual after multiplying with the correctly
+// rounded reciprocal (Markstein); ranges where the residual could underflow divide.
+__device__ __forceinline__ float fifteenth(float d) {
+  if (!(d > 0x1p-80f && d < 0x1p120f)) return __fdiv_rn(d, 15.f);
+  const float y = 1.f / 15.f, q = __fmul_rn(d, y);
+  return __fmaf_rn(__fmaf_rn(-15.f, q, d), y, q);
+}
+
+// Eight channels of one group: their codes, four bits each from the lowest, and the (scale, zero)
+// word of the group, which four neighbouring lanes share.  All 32 lanes of the warp call this together.
 __device__ __forceinline__ uint32_t quantise8(const uint4& v, uint32_t& meta) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   // greatest x and greatest -x side by side; a NaN anywhere in the group wins both
@@ -65,65 +114,112 @@ __device__ __forceinline__ uint32_t quantise8(const uint4& v, uint32_t& meta) {
     top = __hmax2_nan(top, x);
     low = __hmin2_nan(low, x);
   }
-  __nv_bfloat162 ext = __halves2bfloat162(__hmax_nan(__low2bfloat16(top), __high2bfloat16(top)),
-                                          __hneg(__hmin_nan(__low2bfloat16(low), __high2bfloat16(low))));
+  const uint32_t tu = *reinterpret_cast<const uint32_t*>(&top), lu = *reinterpret_cast<const uint32_t*>(&low) ^ 0x80008000u;
+  const uint32_t one = __byte_perm(tu, lu, 0x5410), two = __byte_perm(tu, lu, 0x7632);
+  __nv_bfloat162 ext = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&one), *reinterpret_cast<const __nv_bfloat162*>(&two));
 #pragma unroll
   for (int o = 1; o <= 2; o <<= 1) {
-    uint32_t mine = *reinterpret_cast<const uint32_t*>(&ext);
-    const uint32_t other = __shfl_xor_sync(0xffffffffu, mine, o);
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t*>(&ext), o);
     ext = __hmax2_nan(ext, *reinterpret_cast<const __nv_bfloat162*>(&other));
   }
-  const float hi = __low2float(ext), lo = -__high2float(ext);
-  const __nv_bfloat16 sb = __float2bfloat16_rn(__fdiv_rn(__fsub_rn(hi, lo), 15.f));
+  const uint32_t eu = *reinterpret_cast<const uint32_t*>(&ext);
+  const float hi = __uint_as_float(eu << 16), lo = -__uint_as_float(eu & 0xffff0000u);
+  const __nv_bfloat16 sb = __float2bfloat16_rn(fifteenth(__fsub_rn(hi, lo)));
   const float s = __bfloat162float(sb);
   if (!(s < INFINITY)) {             // a NaN, an infinity or a range beyond fp32: the group is NaN
     meta = 0x7fc0u;
     return 0u;
   }
   meta = (uint32_t)__bfloat16_as_ushort(sb) | (__float_as_uint(lo) & 0xffff0000u);
-  const float inv = s > 0.f ? __frcp_rn(s) : 0.f;
-  float x[8], r[8];
-  unpack_bf16x8(v, x);
-  // t carries at most ~3e-6 of absolute error (two roundings of a value below 15.1 and that of
-  // 1/s), so a t farther than 2e-5 from every border rounds as the exact ratio does -- where 1/s is a
-  // normal number
-  bool near = s < 0x1p-120f || s > 0x1p120f;
+  // The ratio (x - lo) / s by the approximate reciprocal and one correction with the exact residual
+  // (Markstein): where the ratio is a representable number, as every tie between two codes is, that
+  // number exactly.  Ties are common (x - lo and s are both short numbers: one value in 300 of cached rows).
+  // A ratio that is no tie can only round to one, or x - lo to fewer bits than it has, where |x| or |lo| is
+  // below 2^-12 s; such rows, and scales whose reciprocal is no normal number, are decided exactly.
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+  uint32_t least = w[0] & 0x7fff7fffu;
 #pragma unroll
-  for (int u = 0; u < 8; ++u) {
-    const float t = fminf((x[u] - lo) * inv, 15.f);
-    r[u] = rintf(t);
-    const float e = fabsf(t - r[u]);
-    near = near || e > 0.49998f;
+  for (int i = 1; i < 4; ++i) {
+    const uint32_t x = w[i] & 0x7fff7fffu;
+    const __nv_bfloat162 m = __hmin2(*reinterpret_cast<const __nv_bfloat162*>(&least), *reinterpret_cast<const __nv_bfloat162*>(&x));
+    least = *reinterpret_cast<const uint32_t*>(&m);
   }
-  if (near && s > 0.f) {
-#pragma unroll 1
-    for (int u = 0; u < 8; ++u) r[u] = code_exact(x[u], lo, s);
+  const float tiny = fminf(fminf(__uint_as_float(least << 16), __uint_as_float(least & 0xffff0000u)), fabsf(lo));
+  const bool hard = s < 0x1p-100f || s > 0x1p100f;
+  if (hard) inv = 0.f;
+  const uint64_t lo2 = f2(lo, lo), inv2 = f2(inv, inv), ns2 = f2(-s, -s), magic = f2(12582912.f, 12582912.f);   // 1.5 * 2^23
+  uint64_t r2[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint64_t d2 = sub_f2(f2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)), lo2);
+    const uint64_t q2 = mul_f2(d2, inv2), t2 = fma_f2(fma_f2(ns2, q2, d2), inv2, q2);
+    r2[i] = sub_f2(add_f2(t2, magic), magic);              // rounded to an integer, ties to even
   }
-  // codes are small integers: gather them as digits of two base-16 numbers below 2^16
-  const float a = fmaf(r[3], 4096.f, fmaf(r[2], 256.f, fmaf(r[1], 16.f, r[0])));
-  const float b = fmaf(r[7], 4096.f, fmaf(r[6], 256.f, fmaf(r[5], 16.f, r[4])));
-  return (uint32_t)a | ((uint32_t)b << 16);
+  if ((hard || tiny < 0x1p-12f * s) && s > 0.f) {
+    float x[8], r[8];
+    unpack_bf16x8(v, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unf2(r2[i], r[2 * i], r[2 * i + 1]);
+    codes_exact(x, lo, s, r);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r2[i] = f2(r[2 * i], r[2 * i + 1]);
+  }
+  // codes are small integers: gather them as digits (even and odd ones apart, then together), and
+  // take the sums' bits from above 2^23
+  const uint64_t by256 = f2(256.f, 256.f);
+  float e01, o01, e23, o23;
+  unf2(fma_f2(r2[1], by256, r2[0]), e01, o01);
+  unf2(fma_f2(r2[3], by256, r2[2]), e23, o23);
+  return __byte_perm(__float_as_uint(fmaf(o01, 16.f, e01) + 8388608.f), __float_as_uint(fmaf(o23, 16.f, e23) + 8388608.f), 0x5410);
 }
 
-// Writes one row's codes and metas from the 16 lanes that quantised it (l16 = lane & 15, K rows in
-// lanes 0-15, V rows in lanes 16-31).  Called by all 32 lanes; `put` = this lane's row exists.
-__device__ __forceinline__ void put_row(const View& c, int64_t row, int half, int l16, uint32_t codes,
-                                        uint32_t meta, bool put) {
-  const int g = l16 >> 2, t = l16 & 3;
-  // V: the two 16-bit words 4 (2t) + g and 4 (2t + 1) + g; lanes of groups g and g ^ 1 exchange
-  // one each, and every lane then holds a whole 32-bit word
-  const uint32_t give = (g & 1) ? (codes & 0xffffu) : (codes >> 16);
-  const uint32_t got = __shfl_xor_sync(0xffffffffu, give, 4);
-  const uint32_t v_word = (g & 1) ? (got | (codes & 0xffff0000u)) : ((codes & 0xffffu) | (got << 16));
-  const int v_at = 4 * t + 2 * (g & 1) + (g >> 1);
+// How a warp takes rows: lanes 0-15 four rows of K, lanes 16-31 the same four rows of V; the four lanes
+// t of a row take channels 32 g + 8 t .. + 7 of every group g.  That is a 64-byte run of the row for each
+// g, and the codes of a lane are 16 bytes of the cache's row, whichever tensor.
+struct RowLane {
+  int half, row, t;
+  __device__ __forceinline__ RowLane() {
+    const int lane = threadIdx.x & 31;
+    half = lane >> 4;
+    row = (lane >> 2) & 3;
+    t = lane & 3;
+  }
+};
+// 16-bit words g of two 8-channel runs <-> the 16-bit words of a V row's 16 bytes (runs 2 t and
+// 2 t + 1 of four channels, groups ascending in each)
+__device__ __forceinline__ uint4 to_v_order(const uint32_t (&w)[4]) {
+  return make_uint4(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410),
+                    __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632));
+}
+__device__ __forceinline__ void from_v_order(const uint4& v, uint32_t (&w)[4]) {
+  w[0] = __byte_perm(v.x, v.z, 0x5410);
+  w[1] = __byte_perm(v.x, v.z, 0x7632);
+  w[2] = __byte_perm(v.y, v.w, 0x5410);
+  w[3] = __byte_perm(v.y, v.w, 0x7632);
+}
+// Quantises this lane's 32 channels and writes them to cache row `row` when `put`.  Called by all 32
+// lanes.
+__device__ __forceinline__ void put_row(const View& c, int64_t row, const RowLane& l, const uint4 (&v)[4], bool put) {
+  uint32_t w[4], m[4];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) w[g] = quantise8(v[g], m[g]);
   if (!put) return;
-  uint8_t* base = half ? c.V_codes : c.K_codes;
-  reinterpret_cast<uint32_t*>(base + row * kRowBytes)[half ? v_at : 4 * t + g] = half ? v_word : codes;
-  if (t == 0) (half ? c.V_meta : c.K_meta)[row * 4 + g] = meta;
+  const uint4 codes = l.half ? to_v_order(w) : make_uint4(w[0], w[1], w[2], w[3]);
+  reinterpret_cast<uint4*>(l.half ? c.V_codes : c.K_codes)[row * 4 + l.t] = codes;
+  if (l.t == 0) reinterpret_cast<uint4*>(l.half ? c.V_meta : c.K_meta)[row] = make_uint4(m[0], m[1], m[2], m[3]);
+}
+__device__ __forceinline__ void get_row(const __nv_bfloat16* src, const RowLane& l, bool live, uint4 (&v)[4]) {
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    v[g] = make_uint4(0u, 0u, 0u, 0u);
+    if (live) v[g] = __ldg(reinterpret_cast<const uint4*>(src) + 4 * g + l.t);
+  }
 }
 
 constexpr int kStoreWarps = 8;
-constexpr int kStoreRowsPerWarp = 4;                       // rows of K and of V a warp has in flight
+constexpr int kStoreTurns = 2;                             // runs of four rows a warp has in flight
+constexpr int kStoreRowsPerWarp = 4 * kStoreTurns;
 constexpr int kStoreRowsPerCta = kStoreWarps * kStoreRowsPerWarp;
 
 struct StoreArgs {
@@ -143,7 +239,8 @@ struct StoreArgs {
 __global__ void __launch_bounds__(kStoreWarps * 32) store_kernel(const StoreArgs a) {
   const int p = blockIdx.x / a.ctas_per_head, part = blockIdx.x % a.ctas_per_head;
   const int b = p / a.heads, h = p % a.heads;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
+  const int warp = threadIdx.x >> 5;
+  const RowLane l;
   const int n = seq_len_of(a.seqlens, b, a.n_max);
   int64_t first;
   int room;
@@ -168,31 +265,29 @@ __global__ void __launch_bounds__(kStoreWarps * 32) store_kernel(const StoreArgs
   if (lead && offered > room) flag_status(a.status, CURDKV_DEV_CACHE_FULL);
   const int count = (int)(offered < room ? offered : room);
   if (lead) a.cache.count[p] = count;
-  const KvView& T = half ? a.V : a.K;
+  const KvView& T = l.half ? a.V : a.K;
   const __nv_bfloat16* src = T.base + b * T.stride_b + h * T.stride_h;
 
   for (int t0 = (part * kStoreWarps + warp) * kStoreRowsPerWarp; t0 < count;
        t0 += a.ctas_per_head * kStoreRowsPerCta) {
-    int mine = -1;
-    if (lane < kStoreRowsPerWarp && t0 + lane < count) {
-      mine = ix != nullptr ? __ldg(ix + t0 + lane) : t0 + lane;
-      if (mine < 0 || mine >= n) {
-        flag_status(a.status, CURDKV_DEV_BAD_INDEX);
-        mine = -1;
+    uint4 v[kStoreTurns][4];
+#pragma unroll
+    for (int i = 0; i < kStoreTurns; ++i) {
+      const int slot = t0 + 4 * i + l.row;
+      int j = -1;
+      if (slot < count) {
+        j = ix != nullptr ? __ldg(ix + slot) : slot;
+        if (j < 0 || j >= n) {                             // an index outside the sequence: a row of zeros
+          flag_status(a.status, CURDKV_DEV_BAD_INDEX);
+          j = -1;
+        }
       }
-    }
-    uint4 v[kStoreRowsPerWarp];
-#pragma unroll
-    for (int i = 0; i < kStoreRowsPerWarp; ++i) {
-      const int j = __shfl_sync(0xffffffffu, mine, i);
-      v[i] = make_uint4(0u, 0u, 0u, 0u);                   // an index outside the sequence: a row of zeros
-      if (j >= 0) v[i] = __ldg(reinterpret_cast<const uint4*>(src + (int64_t)j * T.stride_n) + l16);
+      get_row(src + (int64_t)j * T.stride_n, l, j >= 0, v[i]);
     }
 #pragma unroll
-    for (int i = 0; i < kStoreRowsPerWarp; ++i) {
-      uint32_t meta;
-      const uint32_t codes = quantise8(v[i], meta);
-      put_row(a.cache, first + t0 + i, half, l16, codes, meta, t0 + i < count);
+    for (int i = 0; i < kStoreTurns; ++i) {
+      const int slot = t0 + 4 * i + l.row;
+      put_row(a.cache, first + slot, l, v[i], slot < count);
     }
   }
 }
@@ -220,7 +315,8 @@ __device__ __forceinline__ int rows_to_append(const AppendArgs& a, int p, int he
 __global__ void __launch_bounds__(kStoreWarps * 32) append_kernel(const AppendArgs a) {
   const int p = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
   const int b = p / a.heads, h = p % a.heads;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
+  const int warp = threadIdx.x >> 5;
+  const RowLane l;
   int64_t first;
   int room;
   const bool ok = rows_of(a.cache, p, first, room);
@@ -232,24 +328,14 @@ __global__ void __launch_bounds__(kStoreWarps * 32) append_kernel(const AppendAr
     if (!ok || was != held) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
     if (full) flag_status(a.status, CURDKV_DEV_CACHE_FULL);
   }
-  const KvView& T = half ? a.V : a.K;
+  const KvView& T = l.half ? a.V : a.K;
   const __nv_bfloat16* src = T.base + b * T.stride_b + h * T.stride_h;
   const int end = min(tb, (chunk + 1) * kAppendRows);
-  for (int t0 = chunk * kAppendRows + warp; t0 < end; t0 += 2 * kStoreWarps) {
-    uint4 v[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int j = t0 + i * kStoreWarps;
-      v[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (j < end) v[i] = __ldg(reinterpret_cast<const uint4*>(src + (int64_t)j * T.stride_n) + l16);
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int j = t0 + i * kStoreWarps;
-      uint32_t meta;
-      const uint32_t codes = quantise8(v[i], meta);
-      put_row(a.cache, first + held + j, half, l16, codes, meta, j < end);
-    }
+  for (int t0 = chunk * kAppendRows + 4 * warp; t0 < end; t0 += 4 * kStoreWarps) {
+    const int j = t0 + l.row;
+    uint4 v[4];
+    get_row(src + (int64_t)j * T.stride_n, l, j < end, v);
+    put_row(a.cache, first + held + j, l, v, j < end);
   }
   if (a.chunks == 1) {
     __syncthreads();                                       // every thread has read the counter
@@ -279,13 +365,18 @@ struct ReadArgs {
   uint32_t* status;
 };
 
-// Eight channels of a row from their codes: bf16(s * code + z), one rounding (fma).
+// Eight channels of a row from their codes: bf16(s * code + z), fp32 inside.
 __device__ __forceinline__ uint4 dequantise8(uint32_t codes, uint32_t meta) {
   const float s = __uint_as_float(meta << 16), z = __uint_as_float(meta & 0xffff0000u);
+  const uint64_t s2 = f2(s, s), z2 = f2(z, z), base = f2(8388608.f, 8388608.f);
   uint32_t o[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float x0 = fmaf(s, (float)((codes >> (8 * i)) & 15u), z), x1 = fmaf(s, (float)((codes >> (8 * i + 4)) & 15u), z);
+    // the code as a float: its bits under the exponent of 2^23, minus 2^23
+    const uint64_t c2 = sub_f2(f2(__uint_as_float(((codes >> (8 * i)) & 15u) | 0x4b000000u),
+                                  __uint_as_float(((codes >> (8 * i + 4)) & 15u) | 0x4b000000u)), base);
+    float x0, x1;
+    unf2(fma_f2(s2, c2, z2), x0, x1);
     const __nv_bfloat162 x = __floats2bfloat162_rn(x0, x1);
     o[i] = *reinterpret_cast<const uint32_t*>(&x);
   }
@@ -296,8 +387,8 @@ __device__ __forceinline__ uint4 dequantise8(uint32_t codes, uint32_t meta) {
 // it is.  grid = batch * heads * ctas_per_head, block = 256.
 __global__ void __launch_bounds__(kStoreWarps * 32) read_kernel(const ReadArgs a) {
   const int p = blockIdx.x / a.ctas_per_head, part = blockIdx.x % a.ctas_per_head;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, half = lane >> 4, l16 = lane & 15;
-  const int g = l16 >> 2, t = l16 & 3;
+  const int warp = threadIdx.x >> 5;
+  const RowLane l;
   int64_t first;
   int room;
   const bool ok = rows_of(a.cache, p, first, room);
@@ -305,36 +396,40 @@ __global__ void __launch_bounds__(kStoreWarps * 32) read_kernel(const ReadArgs a
   if (part == 0 && threadIdx.x == 0 && (!ok || was != held)) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
   const int64_t want = a.idx != nullptr ? a.rows : (a.rows > 0 && a.rows < held ? a.rows : held);
   const int64_t out0 = a.rows > 0 ? (int64_t)p * a.rows : first;
-  const uint8_t* codes = half ? a.cache.V_codes : a.cache.K_codes;
-  const uint32_t* metas = half ? a.cache.V_meta : a.cache.K_meta;
-  __nv_bfloat16* out = half ? a.V_out : a.K_out;
+  const uint4* codes = reinterpret_cast<const uint4*>(l.half ? a.cache.V_codes : a.cache.K_codes);
+  const uint4* metas = reinterpret_cast<const uint4*>(l.half ? a.cache.V_meta : a.cache.K_meta);
+  __nv_bfloat16* out = l.half ? a.V_out : a.K_out;
   for (int64_t t0 = (int64_t)(part * kStoreWarps + warp) * kStoreRowsPerWarp; t0 < want;
        t0 += (int64_t)a.ctas_per_head * kStoreRowsPerCta) {
-    uint32_t c[kStoreRowsPerWarp], m[kStoreRowsPerWarp];
-    int64_t row[kStoreRowsPerWarp];
+    uint4 c[kStoreTurns], m[kStoreTurns];
+    bool live[kStoreTurns];
 #pragma unroll
-    for (int i = 0; i < kStoreRowsPerWarp; ++i) {
-      row[i] = -1;
-      if (t0 + i < want) {
-        const int64_t j = a.idx != nullptr ? (int64_t)__ldg(a.idx + (int64_t)p * a.rows + t0 + i) : t0 + i;
-        if (j >= held && l16 == 0) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
-        if (j >= 0 && j < held) row[i] = first + j;
-      }
-      if (row[i] >= 0) {
-        const uint8_t* r = codes + row[i] * kRowBytes;
-        if (half) {
-          const uint16_t* hw = reinterpret_cast<const uint16_t*>(r);
-          c[i] = (uint32_t)hw[8 * t + g] | ((uint32_t)hw[8 * t + 4 + g] << 16);
-        } else {
-          c[i] = reinterpret_cast<const uint32_t*>(r)[4 * t + g];
+    for (int i = 0; i < kStoreTurns; ++i) {
+      const int64_t slot = t0 + 4 * i + l.row;
+      int64_t j = -1;
+      if (slot < want) {
+        j = a.idx != nullptr ? (int64_t)__ldg(a.idx + (int64_t)p * a.rows + slot) : slot;
+        if (j >= held) {
+          flag_status(a.status, CURDKV_DEV_BAD_INDEX);
+          j = -1;
         }
-        m[i] = metas[row[i] * 4 + g];
+      }
+      live[i] = j >= 0;
+      if (live[i]) {
+        c[i] = __ldg(codes + (first + j) * 4 + l.t);
+        m[i] = __ldg(metas + first + j);
       }
     }
 #pragma unroll
-    for (int i = 0; i < kStoreRowsPerWarp; ++i)
-      if (row[i] >= 0)
-        __stcs(reinterpret_cast<uint4*>(out + (out0 + t0 + i) * 128) + l16, dequantise8(c[i], m[i]));
+    for (int i = 0; i < kStoreTurns; ++i) {
+      if (!live[i]) continue;
+      uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+      if (l.half) from_v_order(c[i], w);
+      const uint32_t mw[4] = {m[i].x, m[i].y, m[i].z, m[i].w};
+      uint4* dst = reinterpret_cast<uint4*>(out + (out0 + t0 + 4 * i + l.row) * 128) + l.t;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) __stcs(dst + 4 * g, dequantise8(w[g], mw[g]));
+    }
   }
 }
 
