@@ -268,27 +268,28 @@ __global__ void __launch_bounds__(kStoreWarps * 32) store_kernel(const StoreArgs
   const KvView& T = l.half ? a.V : a.K;
   const __nv_bfloat16* src = T.base + b * T.stride_b + h * T.stride_h;
 
-  for (int t0 = (part * kStoreWarps + warp) * kStoreRowsPerWarp; t0 < count;
-       t0 += a.ctas_per_head * kStoreRowsPerCta) {
-    uint4 v[kStoreTurns][4];
+  // Rows of the turn after this one are in flight while this one's are quantised, and the index of the
+  // turn after that: a turn's chain of two loads (index, row) would otherwise be waited for in full.
+  const int stride = a.ctas_per_head * kStoreWarps * 4;
+  auto index_of = [&](int slot) {
+    if (slot >= count) return -1;
+    const int j = ix != nullptr ? __ldg(ix + slot) : slot;
+    return j >= 0 && j < n ? j : -2;                       // outside the sequence: a row of zeros
+  };
+  int slot = (part * kStoreWarps + warp) * 4 + l.row;
+  int now = index_of(slot), next = index_of(slot + stride);
+  uint4 v[4];
+  get_row(src + (int64_t)now * T.stride_n, l, now >= 0, v);
+  for (; slot - l.row < count; slot += stride) {
+    uint4 ahead[4];
+    get_row(src + (int64_t)next * T.stride_n, l, next >= 0, ahead);
+    const int after = index_of(slot + 2 * stride);
+    if (now == -2) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
+    put_row(a.cache, first + slot, l, v, slot < count);
+    now = next;
+    next = after;
 #pragma unroll
-    for (int i = 0; i < kStoreTurns; ++i) {
-      const int slot = t0 + 4 * i + l.row;
-      int j = -1;
-      if (slot < count) {
-        j = ix != nullptr ? __ldg(ix + slot) : slot;
-        if (j < 0 || j >= n) {                             // an index outside the sequence: a row of zeros
-          flag_status(a.status, CURDKV_DEV_BAD_INDEX);
-          j = -1;
-        }
-      }
-      get_row(src + (int64_t)j * T.stride_n, l, j >= 0, v[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < kStoreTurns; ++i) {
-      const int slot = t0 + 4 * i + l.row;
-      put_row(a.cache, first + slot, l, v[i], slot < count);
-    }
+    for (int g = 0; g < 4; ++g) v[g] = ahead[g];
   }
 }
 
