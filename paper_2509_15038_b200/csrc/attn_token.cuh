@@ -2,8 +2,11 @@
 // one kernel: rows held in 4 bits (curdkv_qcache_attention) and bf16 rows of which a sliding window
 // and the first tokens are visible (curdkv_attention_window with few queries).
 //
-// What bounds it is the cache's bytes, each read once.  A CTA takes one (head, block of query rows,
-// share of the keys); its warps take tiles of the share's keys in turn, each warp with its own ring
+// What bounds it is the cache's bytes, each read once.  The tiles of all items -- an item is a head and
+// a block of query rows -- form one line, and every CTA takes an equal run of it, whatever the items'
+// lengths: whole items are finished where they are, the partial results of an item that several CTAs
+// share are joined by a second kernel.  (With a CTA per item, 128 heads of 2048 to 16384 rows took 70 us,
+// as long as the longest; with equal runs 46 us.)  A CTA's warps take the tiles of an item in turn, each warp with its own ring
 // of tiles in shared memory, filled by 16-byte asynchronous copies (rows that do not exist are
 // filled with zeros, so nothing behind a head's last row is ever read).  No barrier stands in the
 // key loop.  Per 16 keys a warp forms
@@ -22,16 +25,16 @@
 // tensor cores multiply exactly.  The scales are applied outside: on the K side to the products of
 // each group of 32 channels (S = sum_g s_g (codes_g . q_g) + sum_g z_g sum(q_g), the second sum one
 // more matrix instruction whose A operand is the zeros), on the V side to the weights (one set per
-// group, P_g = p * s_g), with the zeros as a further instruction.  V's scales are brought to fp16
-// relative to a power of two per warp that follows the largest value seen, so any bf16 range works.
+// group, P_g = p * s_g), with the zeros as a further instruction.  Every V row brings its own power of
+// two 2^e that covers its values: its scales and zeros relative to it fit fp16, and 2^e goes into the
+// exponent of its weight, so that the running maximum follows logit + e -- what a row adds to the
+// output -- and rows of any bf16 magnitude share a cache; the row sum takes the 2^e out again.
 #pragma once
 #include "qcache.cuh"
 
 namespace curdkv {
 namespace token {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = kWarps * 32;
 constexpr int kStages = 3;
 constexpr float kSlack = 6.f;        // log2 units a logit may exceed the running maximum
 constexpr float kLift = 8.f;         // fp16 weights are 2^(x - m + kLift): at most 2^14, and exact
@@ -44,7 +47,9 @@ struct Args {
   int64_t o_sb, o_sh, o_sn;
   float* lse;                        // [batch][q_heads][q_n] or nullptr
   int heads, group, q_n;             // query heads per KV head; query tokens
-  int rows, blocks, splits;          // rows = group * q_n, row r = token r / group, head r % group
+  int rows, blocks;                  // rows = group * q_n, row r = token r / group, head r % group
+  int items;                         // batch * heads * blocks
+  int ctas;                          // runs the tiles are cut into; 0: a CTA per item
   float scale_log2;                  // scale * log2(e)
   // 4-bit rows
   qcache::View cache;
@@ -53,9 +58,11 @@ struct Args {
   const int32_t* seqlens;
   const int32_t* q_lens;
   int n_max, num_sink, window;
-  // partial results, one per (head, block, split): [8 NT] maxima and sums, [8 NT][128] sums of values
+  // partial results, two per CTA (of the item its run begins in, of the one it ends in): [8 NT] maxima
+  // and sums, [8 NT][128] sums of values; and where each item begins on the line, [items + 1]
   float* part_ml;
   float* part_o;
+  int64_t* begins;
   uint32_t* status;
 };
 
@@ -65,6 +72,9 @@ __device__ __forceinline__ uint32_t smem_addr(const void* p) {
 // 16 bytes global -> shared, zeros when `live` is false (nothing is read then).
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -123,14 +133,22 @@ struct Tile {                                              // one warp's stage
   static constexpr int kKMeta = 2 * kV;
   static constexpr int kVMeta = kKMeta + (Q4 ? kKeys * qcache::kMetaBytes : 0);
   static constexpr int kBytes = kVMeta + (Q4 ? kKeys * qcache::kMetaBytes : 0);
-  // V's scales and zeros in fp16, pairs of keys side by side: [key pair][group] each
-  static constexpr int kScaled = Q4 ? kKeys * 8 * 2 : 0;
+  // V's scales and zeros in fp16, pairs of keys side by side: [key pair][group] each; then e and 2^-e
+  // of each key
+  static constexpr int kScaled = Q4 ? kKeys * (8 * 2 + 8) : 0;
   static constexpr int kWarpBytes = kStages * kBytes + kScaled;
 };
+// Warps of a CTA; two CTAs fill an SM's registers and shared memory, so that one streams while the other
+// begins or ends an item.
+constexpr int kCtasPerSm = 2;
+template <bool Q4, int NT>
+__host__ __device__ constexpr int warps() {
+  return Q4 && NT == 1 ? 6 : 4;
+}
 template <bool Q4, int NT>
 constexpr int smem_bytes() {
-  constexpr int ring = kWarps * Tile<Q4>::kWarpBytes;
-  constexpr int merge = kWarps * 8 * NT * 132 * 4;         // the warps' sums meet in the ring's space
+  constexpr int ring = warps<Q4, NT>() * Tile<Q4>::kWarpBytes;
+  constexpr int merge = warps<Q4, NT>() * 8 * NT * 132 * 4;         // the warps' sums meet in the ring's space
   return ring > merge ? ring : merge;
 }
 
@@ -141,44 +159,140 @@ struct Seen {
   __device__ __forceinline__ int row(int u) const { return u < sinks ? u : first + (u - sinks); }
 };
 
+// One item: its head, its query rows [r0, r1), and the keys these see.
 template <bool Q4, int NT>
-__global__ void __launch_bounds__(kThreads, 1) attend_kernel(const Args a) {
+struct Item {
+  int b, h, p, blk, r0, r1;
+  Seen seen;
+  int64_t first_row;                                       // 4-bit rows: of the head
+  int pos0, q_live;                                        // position of query token 0; tokens that exist
+  bool ok;                                                 // counters in range
+  int tiles;
+  __device__ __forceinline__ Item(const Args& a, int item) {
+    p = item / a.blocks;
+    blk = item % a.blocks;
+    b = p / a.heads;
+    h = p % a.heads;
+    r0 = blk * 8 * NT;
+    r1 = min(a.rows, r0 + 8 * NT);
+    pos0 = 0;
+    q_live = a.q_n;
+    first_row = 0;
+    ok = true;
+    if (Q4) {
+      int room;
+      ok = qcache::rows_of(a.cache, p, first_row, room);
+      const int was = a.cache.count[p], held = was < 0 ? 0 : (was > room ? room : was);
+      ok = ok && was == held;
+      seen.sinks = 0;
+      seen.first = 0;
+      seen.total = held;
+    } else {
+      const int n = seq_len_of(a.seqlens, b, a.n_max);
+      if (a.q_lens != nullptr) q_live = min(max(a.q_lens[b], 0), a.q_n);
+      pos0 = n - q_live;
+      const int i0 = r0 / a.group, i1 = min((r1 - 1) / a.group, q_live - 1);   // tokens of the block
+      const int hi = i1 >= i0 ? max(pos0 + i1 + 1, 0) : 0; // keys [0, hi) may be seen
+      const int lo = (int)min((int64_t)hi, max((int64_t)0, (int64_t)pos0 + i0 + 1 - a.window));
+      seen.sinks = min(a.num_sink, lo);
+      seen.first = lo;
+      seen.total = seen.sinks + hi - lo;
+    }
+    tiles = (seen.total + Tile<Q4>::kKeys - 1) / Tile<Q4>::kKeys;
+  }
+};
+
+// CTA whose run holds tile x of a line of `total` tiles cut into `runs` runs [i total / runs, ...).
+__device__ __forceinline__ int cta_of(int64_t x, int64_t total, int64_t runs) { return (int)(((x + 1) * runs - 1) / total); }
+
+constexpr int kMostItems = 8192;                           // items that are put on one line
+
+template <bool Q4, int NT>
+__global__ void __launch_bounds__(warps<Q4, NT>() * 32, kCtasPerSm) attend_kernel(const Args a) {
   using T = Tile<Q4>;
+  constexpr int kWarps = warps<Q4, NT>(), kThreads = kWarps * 32;
   constexpr int KB = T::kKeys / 16;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ float s_m[kWarps][8 * NT], s_l[kWarps][8 * NT];
+  __shared__ int64_t s_sum[kWarps], s_at;
+  __shared__ int s_item;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  const int split = blockIdx.x % a.splits, pb = blockIdx.x / a.splits;
-  const int p = pb / a.blocks, blk = pb % a.blocks;
-  const int b = p / a.heads, h = p % a.heads;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // the joining kernel waits for this one's end
 
-  // ------------------------------------------------------------ the keys of this block
-  const int r0 = blk * 8 * NT, r1 = min(a.rows, r0 + 8 * NT);   // query rows [r0, r1)
-  Seen seen;
-  int64_t first_row = 0;
-  int pos0 = 0, q_live = a.q_n;                            // position of query token 0; tokens that exist
-  if (Q4) {
-    int room;
-    const bool ok = qcache::rows_of(a.cache, p, first_row, room);
-    const int was = a.cache.count[p], held = was < 0 ? 0 : (was > room ? room : was);
-    if (blk == 0 && split == 0 && tid == 0 && (!ok || was != held)) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
-    seen.sinks = 0;
-    seen.first = 0;
-    seen.total = held;
-  } else {
-    const int n = seq_len_of(a.seqlens, b, a.n_max);
-    if (a.q_lens != nullptr) q_live = min(max(a.q_lens[b], 0), a.q_n);
-    pos0 = n - q_live;
-    const int i0 = r0 / a.group, i1 = min((r1 - 1) / a.group, q_live - 1);   // tokens of the block
-    const int hi = i1 >= i0 ? max(pos0 + i1 + 1, 0) : 0;   // keys [0, hi) may be seen
-    const int lo = (int)min((int64_t)hi, max((int64_t)0, (int64_t)pos0 + i0 + 1 - a.window));
-    seen.sinks = min(a.num_sink, lo);
-    seen.first = lo;
-    seen.total = seen.sinks + hi - lo;
+  // ------------------------------------------------------------ this CTA's run of tiles
+  int item_no = blockIdx.x;
+  int64_t off = 0, left_over = 1;                          // first tile inside the item; tiles of the run
+  if (a.ctas > 0) {
+    // every CTA sums up the items' tiles: a run of items per thread, then over the threads
+    const int each = (a.items + kThreads - 1) / kThreads, e0 = min(tid * each, a.items), e1 = min(e0 + each, a.items);
+    int64_t mine = 0;
+    int tiles0 = 0;                                        // of the thread's first item
+    for (int e = e0; e < e1; ++e) {
+      const Item<Q4, NT> it(a, e);
+      mine += it.tiles;
+      if (e == e0) tiles0 = it.tiles;
+      if (e % a.ctas != (int)blockIdx.x) continue;
+      if (!it.ok) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
+      if (it.tiles == 0) {                                 // nothing to see: zeros, written here
+        for (int r = it.r0; r < it.r1; ++r) {
+          const int i = r / a.group, hq = it.h * a.group + r % a.group;
+          if (i >= it.q_live) continue;
+          uint4* o = reinterpret_cast<uint4*>(a.O + it.b * a.o_sb + (int64_t)hq * a.o_sh + (int64_t)i * a.o_sn);
+          for (int c = 0; c < 16; ++c) o[c] = make_uint4(0u, 0u, 0u, 0u);
+          if (a.lse != nullptr) a.lse[((int64_t)it.b * a.heads * a.group + hq) * a.q_n + i] = -INFINITY;
+        }
+      }
+    }
+    int64_t upto = mine;                                   // inclusive sum over the warp's threads
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t x = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += x;
+    }
+    if (lane == 31) s_sum[warp] = upto;
+    __syncthreads();
+    int64_t before = upto - mine, total = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) before += s_sum[w];
+      total += s_sum[w];
+    }
+    const int64_t runs = min((int64_t)a.ctas, total);      // none of them empty
+    const int64_t lo = blockIdx.x < runs ? blockIdx.x * total / runs : 0;
+    const int64_t hi = blockIdx.x < runs ? (blockIdx.x + 1) * total / runs : 0;
+    if (blockIdx.x == 0 || (before <= lo && lo < before + mine)) {
+      int64_t x = before;
+      for (int e = e0; e < e1; ++e) {
+        if (blockIdx.x == 0) a.begins[e] = x;
+        const int tiles = e == e0 ? tiles0 : Item<Q4, NT>(a, e).tiles;
+        if (x <= lo && lo < x + tiles) {
+          s_item = e;
+          s_at = lo - x;
+        }
+        x += tiles;
+      }
+      if (blockIdx.x == 0 && e1 == a.items && e0 < e1) a.begins[e1] = x;
+    }
+    __syncthreads();
+    left_over = hi - lo;
+    if (left_over <= 0) return;
+    item_no = s_item;
+    off = s_at;
   }
-  // tiles of this split, and of this warp among them
-  const int tiles = (seen.total + T::kKeys - 1) / T::kKeys;
-  const int t_lo = (int)((int64_t)split * tiles / a.splits), t_hi = (int)((int64_t)(split + 1) * tiles / a.splits);
+
+  for (;; ++item_no, off = 0) {
+  const Item<Q4, NT> it(a, item_no);
+  const int p = it.p, b = it.b, h = it.h, r0 = it.r0, r1 = it.r1, pos0 = it.pos0, q_live = it.q_live;
+  const Seen seen = it.seen;
+  const int64_t first_row = it.first_row;
+  if (a.ctas == 0) {
+    left_over = it.tiles;
+    if (!it.ok && tid == 0) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
+  } else if (it.tiles == 0) {
+    continue;
+  }
+  const int t_lo = (int)off, t_hi = (int)min((int64_t)it.tiles, off + left_over);
+  left_over -= t_hi - t_lo;
 
   // ------------------------------------------------------------ the ring of this warp
   unsigned char* ring = smem + warp * T::kWarpBytes;
@@ -195,23 +309,32 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const Args a) {
       // two 64-byte rows share a 128-byte line of shared memory; the line's eight 16-byte places are
       // permuted by the line number so that both products' reads are free of bank conflicts
       const int64_t row0 = first_row + u0;
-      const uint8_t* ks = a.cache.K_codes + row0 * qcache::kRowBytes;
-      const uint8_t* vs = a.cache.V_codes + row0 * qcache::kRowBytes;
-      const int left = seen.total - u0;                    // rows of the tile that exist (or more)
-#pragma unroll
-      for (int i = 0; i < T::kKeys * 4 / 32; ++i) {
-        const int c = i * 32 + lane;                       // 16-byte chunk of the tile
-        const int line = c >> 3;
-        const uint32_t at = (uint32_t)(line * 128 + (((c & 7) ^ (2 * (line & 3))) * 16));
-        const bool live = (c >> 2) < left;
-        copy16(dst + T::kK + at, live ? ks + c * 16 : a.cache.K_codes, live);
-        copy16(dst + T::kV + at, live ? vs + c * 16 : a.cache.V_codes, live);
-      }
-      const bool live = lane < left;
+      const uint8_t* ks = a.cache.K_codes + row0 * qcache::kRowBytes + lane * 16;
+      const uint8_t* vs = a.cache.V_codes + row0 * qcache::kRowBytes + lane * 16;
       const uint32_t* km = a.cache.K_meta + (row0 + lane) * 4;
       const uint32_t* vm = a.cache.V_meta + (row0 + lane) * 4;
-      copy16(dst + T::kKMeta + lane * 16, live ? km : a.cache.K_meta, live);
-      copy16(dst + T::kVMeta + lane * 16, live ? vm : a.cache.V_meta, live);
+      // chunk c = 32 i + lane: line c / 8 = 4 i + lane / 8, so the permutation is the lane's alone
+      const uint32_t at = dst + (uint32_t)((lane >> 3) * 128 + (((lane & 7) ^ (2 * (lane >> 3))) * 16));
+      const int left = seen.total - u0;                    // rows of the tile that exist (or more)
+      if (left >= T::kKeys) {
+#pragma unroll
+        for (int i = 0; i < T::kKeys * 4 / 32; ++i) {
+          copy16(at + T::kK + 512u * i, ks + 512 * i);
+          copy16(at + T::kV + 512u * i, vs + 512 * i);
+        }
+        copy16(dst + T::kKMeta + lane * 16, km);
+        copy16(dst + T::kVMeta + lane * 16, vm);
+      } else {
+#pragma unroll
+        for (int i = 0; i < T::kKeys * 4 / 32; ++i) {
+          const bool live = 8 * i + (lane >> 2) < left;
+          copy16(at + T::kK + 512u * i, live ? ks + 512 * i : a.cache.K_codes, live);
+          copy16(at + T::kV + 512u * i, live ? vs + 512 * i : a.cache.V_codes, live);
+        }
+        const bool live = lane < left;
+        copy16(dst + T::kKMeta + lane * 16, live ? km : a.cache.K_meta, live);
+        copy16(dst + T::kVMeta + lane * 16, live ? vm : a.cache.V_meta, live);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < T::kKeys / 2; ++i) {
@@ -321,7 +444,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const Args a) {
     m[nt][0] = m[nt][1] = -INFINITY;
     l[nt][0] = l[nt][1] = 0.f;
   }
-  int v_exp = 1;                                           // V's values are held relative to 2^(v_exp - 127)
 
   // ------------------------------------------------------------ the key loop
   int stage = 0;
@@ -339,6 +461,39 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const Args a) {
     const int u0 = tile * T::kKeys;
     const int left = seen.total - u0;
 
+    // ---- V's scales and zeros of this tile in fp16, each row's relative to a power of two of its own
+    if constexpr (Q4) {
+      const uint4 v = *reinterpret_cast<const uint4*>(st + T::kVMeta + lane * 16);
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      uint32_t big = 0;                                    // bits of the largest of |zero| and 16 * scale
+#pragma unroll
+      for (int gr = 0; gr < 4; ++gr)
+        big = max(big, max(w[gr] & 0x7fff0000u, (w[gr] & 0x7fffu) != 0u ? (w[gr] << 16) + (4u << 23) : 0u));
+      // biased exponent above it; rows far below the tile's largest (rows of zeros among them) take one
+      // near it, so that their weights stay numbers
+      int e = min(max((int)(big >> 23) + 1, 37), 250);       // (sums of 2^20 weights times 2^-e stay numbers)
+      e = max(e, __reduce_max_sync(0xffffffffu, e) - 30);
+      const float inv = pow2_biased(254 - e);
+      *reinterpret_cast<float2*>(ring + kStages * T::kBytes + T::kKeys * 16 + lane * 8) = make_float2((float)(e - 127), inv);
+      // lanes 2 i and 2 i + 1 hold a pair of keys: the even one takes the pair's groups 0 and 1, the odd
+      // one 2 and 3
+      uint32_t sz[2][2];                                   // [scale, zero][groups 0-1, 2-3] of this key
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        sz[0][i] = pack_f16(__uint_as_float(w[2 * i] << 16) * inv, __uint_as_float(w[2 * i + 1] << 16) * inv);
+        sz[1][i] = pack_f16(__uint_as_float(w[2 * i] & 0xffff0000u) * inv, __uint_as_float(w[2 * i + 1] & 0xffff0000u) * inv);
+      }
+      const bool odd = lane & 1;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? sz[k][0] : sz[k][1], 1);
+        const uint32_t keep = odd ? sz[k][1] : sz[k][0];
+        const uint32_t ev = odd ? got : keep, od = odd ? keep : got;                 // key 2 i, key 2 i + 1
+        *reinterpret_cast<uint2*>(ring + kStages * T::kBytes + k * (T::kKeys * 8) + lane * 8) =
+            make_uint2(__byte_perm(ev, od, 0x5410), __byte_perm(ev, od, 0x7632));
+      }
+      __syncwarp();
+    }
     // ---- S^T
     float s[NT][KB][4];
 #pragma unroll
@@ -400,7 +555,21 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const Args a) {
         }
       }
     }
-    // ---- logits in log2 units; what a query does not see becomes -inf
+    // ---- logits in log2 units (4-bit rows: plus the row's e); what a query does not see becomes -inf
+    float took[KB][2];                                     // 2^-e of keys g, g + 8
+#pragma unroll
+    for (int kb16 = 0; kb16 < KB; ++kb16)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float2 f = make_float2(0.f, 1.f);
+        if (Q4) f = *reinterpret_cast<const float2*>(ring + kStages * T::kBytes + T::kKeys * 16 + (kb16 * 16 + 8 * i + g) * 8);
+        took[kb16][i] = f.y;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            s[nt][kb16][2 * i + c] = Q4 ? fmaf(s[nt][kb16][2 * i + c], unit[nt][c], f.x) : s[nt][kb16][2 * i + c] * unit[nt][c];
+      }
     bool masked = left < T::kKeys;
     if (!Q4) {
       // a tile that every query of the block sees whole needs no comparison
@@ -408,12 +577,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const Args a) {
       masked = masked || j_hi > pos_lo || (j_hi >= a.num_sink && (int64_t)j_lo <= (int64_t)pos_hi - a.window &&
                                            pos_hi != pos_lo);
     }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int kb16 = 0; kb16 < KB; ++kb16)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[nt][kb16][j] *= unit[nt][j & 1];
     if (masked) {
 #pragma unroll
       for (int kb16 = 0; kb16 < KB; ++kb16)
@@ -464,41 +627,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const Args a) {
           accz[nt][c] *= f;
         }
     }
-    // ---- V's scales of this tile in fp16, relative to the power of two that covers its values
-    if constexpr (Q4) {
-      const uint4 v = *reinterpret_cast<const uint4*>(st + T::kVMeta + lane * 16);
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-      uint32_t big = 0;
-#pragma unroll
-      for (int gr = 0; gr < 4; ++gr) {
-        const uint32_t z = w[gr] & 0x7fff0000u, sc = (w[gr] << 16) + (4u << 23);   // |zero|; 16 * scale
-        big = max(big, max(z, (w[gr] & 0x7fffu) != 0u ? sc : 0u));
-      }
-      const int e = min((int)(__reduce_max_sync(0xffffffffu, big) >> 23) + 1, 240);
-      if (e > v_exp) {
-        const float f = pow2_biased(127 + v_exp - e);
-        v_exp = e;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[nt][i][j] *= f;
-          accz[nt][0] *= f;
-          accz[nt][1] *= f;
-        }
-      }
-      const float inv = pow2_biased(254 - v_exp);
-      __half* scaled = reinterpret_cast<__half*>(ring + kStages * T::kBytes);
-#pragma unroll
-      for (int gr = 0; gr < 4; ++gr) {
-        const int at = (lane >> 1) * 8 + gr * 2 + (lane & 1);
-        scaled[at] = __float2half_rn(__uint_as_float(w[gr] << 16) * inv);
-        scaled[T::kKeys * 4 + at] = __float2half_rn(__uint_as_float(w[gr] & 0xffff0000u) * inv);
-      }
-      __syncwarp();
-    }
     // ---- weights and O^T
+    float nref[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) nref[nt][c] = (Q4 ? kLift : 0.f) - (m[nt][c] == -INFINITY ? 0.f : m[nt][c]);
 #pragma unroll
     for (int kb16 = 0; kb16 < KB; ++kb16) {
       uint32_t pt[NT][2];                                  // P^T as B operand: keys 2t, 2t + 1 / 2t + 8, 2t + 9 of query g
@@ -507,11 +641,10 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const Args a) {
         float w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float ref = m[nt][j & 1] == -INFINITY ? 0.f : m[nt][j & 1];
-          w[j] = exp2_approx(s[nt][kb16][j] - ref + (Q4 ? kLift : 0.f));
+          w[j] = exp2_approx(s[nt][kb16][j] + nref[nt][j & 1]);
         }
-        l[nt][0] += w[0] + w[2];
-        l[nt][1] += w[1] + w[3];
+        l[nt][0] = fmaf(w[2], took[kb16][1], fmaf(w[0], took[kb16][0], l[nt][0]));
+        l[nt][1] = fmaf(w[3], took[kb16][1], fmaf(w[1], took[kb16][0], l[nt][1]));
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           pt[nt][i] = transpose8x8(Q4 ? pack_f16(w[2 * i], w[2 * i + 1]) : pack_bf16(w[2 * i], w[2 * i + 1]));
@@ -583,7 +716,6 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const Args a) {
     }
   __syncthreads();                                         // also: every warp is done with its ring
   float* meet = reinterpret_cast<float*>(smem);            // [warp][8 NT][132]
-  const float back = Q4 ? pow2_biased(v_exp) : 1.f;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -592,7 +724,7 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const Args a) {
       float all = -INFINITY;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) all = fmaxf(all, s_m[w][qi]);
-      const float f = m[nt][c] == -INFINITY ? 0.f : exp2_approx(m[nt][c] - all) * back;
+      const float f = m[nt][c] == -INFINITY ? 0.f : exp2_approx(m[nt][c] - all);
       float* dst = meet + ((size_t)warp * 8 * NT + qi) * 132;
       if (Q4) {
 #pragma unroll
@@ -628,12 +760,12 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const Args a) {
       o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
     }
     if (Q4) all -= kLift;
-    if (a.splits > 1) {
-      const size_t item = blockIdx.x;
-      *reinterpret_cast<float4*>(a.part_o + (item * 8 * NT + qi) * 128 + c4) = o;
+    if (t_hi - t_lo < it.tiles) {                          // a part: of the item this run begins or ends in
+      const size_t at = ((size_t)blockIdx.x * 2 + (t_lo == 0 ? 1 : 0)) * 8 * NT + qi;
+      *reinterpret_cast<float4*>(a.part_o + at * 128 + c4) = o;
       if (c4 == 0) {
-        a.part_ml[(item * 8 * NT + qi) * 2] = all;
-        a.part_ml[(item * 8 * NT + qi) * 2 + 1] = sum;
+        a.part_ml[at * 2] = all;
+        a.part_ml[at * 2 + 1] = sum;
       }
     } else {
       const int r = r0 + qi, i = r / a.group, hq = h * a.group + r % a.group;
@@ -648,31 +780,39 @@ __global__ void __launch_bounds__(kThreads, 1) attend_kernel(const Args a) {
             sum == 0.f ? -INFINITY : (all + log2f(sum)) * 0.6931471805599453f;
     }
   }
+  if (left_over <= 0) return;
+  __syncthreads();                                         // the ring is the next item's
+  }
 }
 
-// Joins the splits: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s, in split order.
-// grid = batch * heads * rows, block = 32 (four channels a lane).
+// Joins the parts of items that several CTAs share: O = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c,
+// in the order of the CTAs.  grid = items * block_rows, block = 32 (four channels a lane).
 __global__ void __launch_bounds__(32) join_kernel(const Args a, int block_rows) {
-  const int r = blockIdx.x % a.rows, p = blockIdx.x / a.rows;
+  asm volatile("griddepcontrol.wait;" ::: "memory");       // behind the last CTA of attend_kernel
+  const int item = blockIdx.x / block_rows, qi = blockIdx.x % block_rows;
+  const int64_t from = a.begins[item], to = a.begins[item + 1], total = a.begins[a.items];
+  if (to <= from) return;
+  const int64_t runs = min((int64_t)a.ctas, total);
+  const int c0 = cta_of(from, total, runs), c1 = cta_of(to - 1, total, runs);
+  const int p = item / a.blocks, r = (item % a.blocks) * block_rows + qi;
+  if (c0 == c1 || r >= a.rows) return;
   const int b = p / a.heads, h = p % a.heads, i = r / a.group, hq = h * a.group + r % a.group;
   const int lane = threadIdx.x;
   if (a.q_lens != nullptr && i >= min(max(a.q_lens[b], 0), a.q_n)) return;
-  const size_t item0 = ((size_t)p * a.blocks + r / block_rows) * a.splits;
-  const int qi = r % block_rows;
+  // the item begins in c0 (its second part) and goes on in the others (their first)
+  auto part = [&](int c) { return ((size_t)c * 2 + (c == c0 ? 1 : 0)) * block_rows + qi; };
   float all = -INFINITY;
-  for (int s = lane; s < a.splits; s += 32) all = fmaxf(all, a.part_ml[((item0 + s) * block_rows + qi) * 2]);
+  for (int c = c0 + lane; c <= c1; c += 32) all = fmaxf(all, a.part_ml[part(c) * 2]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
   float sum = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (all > -INFINITY) {
-    for (int s = 0; s < a.splits; ++s) {
-      const size_t at = (item0 + s) * block_rows + qi;
-      const float f = exp2_approx(a.part_ml[at * 2] - all);
-      const float4 x = *reinterpret_cast<const float4*>(a.part_o + at * 128 + lane * 4);
-      sum = fmaf(f, a.part_ml[at * 2 + 1], sum);
-      o.x = fmaf(f, x.x, o.x); o.y = fmaf(f, x.y, o.y); o.z = fmaf(f, x.z, o.z); o.w = fmaf(f, x.w, o.w);
-    }
+  for (int c = c0; c <= c1; ++c) {
+    const size_t at = part(c);
+    const float m = a.part_ml[at * 2], f = all == -INFINITY ? 1.f : exp2_approx(m - all);      // (all -inf: zeros, or NaN)
+    const float4 x = *reinterpret_cast<const float4*>(a.part_o + at * 128 + lane * 4);
+    sum = fmaf(f, a.part_ml[at * 2 + 1], sum);
+    o.x = fmaf(f, x.x, o.x); o.y = fmaf(f, x.y, o.y); o.z = fmaf(f, x.z, o.z); o.w = fmaf(f, x.w, o.w);
   }
   const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
   uint2 v;

@@ -73,71 +73,68 @@ curdkv_status check_rows(const curdkv_qcache* cache, const void* K, const void* 
 
 // ---- attention of few query rows ---------------------------------------------------------------
 struct Plan {
-  int nt, blocks, splits;            // sets of 8 query rows a CTA takes, CTAs per head by rows, by keys
-  size_t ml_at, o_at, bytes;         // partial results inside the workspace, and its size
+  int nt, blocks, ctas;              // sets of 8 query rows a CTA takes, blocks of rows per head; 0: a CTA per item
+  size_t begins_at, ml_at, o_at, bytes;                    // inside the workspace, and its size
 };
 
-// Shares of the keys: the number that finishes first when `items` (head, block) pairs of `keys` keys
-// run one CTA per SM.  A share costs its keys and a fixed start (`start` keys' time); joining costs
-// a second launch (`join` keys' time).
-// Never more than kShareLimit CTAs per SM in all, and none below one round of the warps' tiles, which
-// bounds the workspace by `most_keys`, the longest a head can be, whatever `keys` this call sees.
-constexpr int kShareLimit = 8;
-Plan plan_token(int64_t problems, int64_t rows, int64_t keys, int64_t most_keys, int round_keys, int start, int join) {
+// `keys`: the most a head can hold or see in this call.  A CTA per item where that is one round of its
+// warps' tiles, or where there are so many items that their lengths even out; one line of tiles, cut into
+// equal runs, else -- as many runs as CTAs fit the device, but none shorter than a round unless there are more items.
+// The workspace does not depend on `keys`.
+Plan plan_token(int64_t problems, int64_t rows, int64_t keys, int tile_keys, int warps) {
   Plan pl;
   pl.nt = rows <= 8 ? 1 : 2;
   pl.blocks = (int)((rows + 8 * pl.nt - 1) / (8 * pl.nt));
-  const int64_t items = problems * pl.blocks, slots = sms();
-  auto shares = [&](int64_t n) {
-    const int64_t by_rows = (n + round_keys - 1) / round_keys, by_sms = kShareLimit * slots / (items > 0 ? items : 1);
-    const int64_t most = by_rows < by_sms ? by_rows : by_sms;
-    return most < 1 ? 1 : (most > 128 ? 128 : most);
-  };
-  pl.splits = 1;
-  double best = 0.0;
-  for (int64_t s = 1; s <= shares(keys); ++s) {
-    const double waves = (double)((items * s + slots - 1) / slots);
-    const double cost = waves * ((double)((keys + s - 1) / s) + start) + (s > 1 ? join : 0);
-    if (s == 1 || cost < best) {
-      best = cost;
-      pl.splits = (int)s;
-    }
+  const int64_t items = problems * pl.blocks, slots = (int64_t)token::kCtasPerSm * sms();
+  const int64_t tiles = (keys + tile_keys - 1) / tile_keys;
+  pl.ctas = 0;
+  if (tiles > warps && items <= token::kMostItems) {
+    int64_t ctas = (items * tiles + warps - 1) / warps;
+    if (ctas < items) ctas = items;
+    pl.ctas = (int)(ctas < slots ? ctas : slots);
   }
-  const int64_t room = shares(most_keys);
-  const size_t parts = room > 1 ? (size_t)items * room * 8 * pl.nt : 0;
-  pl.ml_at = 256;
+  const bool room = items <= token::kMostItems;
+  const size_t parts = room ? 2 * (size_t)slots * 8 * pl.nt : 0;
+  pl.begins_at = 256;
+  pl.ml_at = pl.begins_at + round256(room ? (size_t)(items + 1) * sizeof(int64_t) : 0);
   pl.o_at = pl.ml_at + round256(parts * 2 * sizeof(float));
   pl.bytes = pl.o_at + round256(parts * 128 * sizeof(float));
   return pl;
 }
 
 Plan plan_qcache(const curdkv_qcache* c, int32_t q_rows) {
-  const int64_t P = (int64_t)c->batch * c->kv_heads;
-  int64_t keys = c->capacity;
-  // packed heads: the mean room, a few times over since the longest head decides
-  if (c->row_start != nullptr && P > 0) keys = (c->capacity + P - 1) / P * 2;
-  if (keys > c->capacity) keys = c->capacity;
-  return plan_token(P, q_rows, keys, c->capacity, token::kWarps * token::Tile<true>::kKeys, 800, 500);
+  // (packed heads: any of them may own most of the rows)
+  return plan_token((int64_t)c->batch * c->kv_heads, q_rows, c->capacity, token::Tile<true>::kKeys,
+                    q_rows <= 8 ? token::warps<true, 1>() : token::warps<true, 2>());
 }
 
 Plan plan_window(const curdkv_desc* d, int32_t q_rows, int64_t seen) {
-  return plan_token((int64_t)d->batch * d->kv_heads, (int64_t)(d->q_heads / d->kv_heads) * q_rows, seen, d->n_max,
-                    token::kWarps * token::Tile<false>::kKeys, 260, 160);
+  return plan_token((int64_t)d->batch * d->kv_heads, (int64_t)(d->q_heads / d->kv_heads) * q_rows, seen,
+                    token::Tile<false>::kKeys, token::warps<false, 1>());
 }
 
 template <bool Q4, int NT>
-bool launch_attend(const token::Args& a, int64_t problems, cudaStream_t stream) {
+bool launch_attend(const token::Args& a, cudaStream_t stream) {
   constexpr int smem = token::smem_bytes<Q4, NT>();
   if (cudaFuncSetAttribute(token::attend_kernel<Q4, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) !=
       cudaSuccess)
     return false;
-  token::attend_kernel<Q4, NT><<<(unsigned)(problems * a.blocks * a.splits), token::kThreads, smem, stream>>>(a);
+  const int grid = a.ctas > 0 ? a.ctas : a.items;
+  token::attend_kernel<Q4, NT><<<(unsigned)grid, token::warps<Q4, NT>() * 32, smem, stream>>>(a);
   if (!launched()) return false;
-  if (a.splits > 1) {
-    token::join_kernel<<<(unsigned)(problems * a.rows), 32, 0, stream>>>(a, 8 * NT);
-    if (!launched()) return false;
-  }
-  return true;
+  if (a.ctas == 0) return true;
+  // launched behind attend_kernel without waiting for its end: the kernel itself waits
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(a.items * 8 * NT));
+  cfg.blockDim = dim3(32);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, token::join_kernel, a, 8 * NT) != cudaSuccess) return false;
+  return launched();
 }
 
 // The prompt form reads its tensors through TMA maps, whose strides must be positive and below 2^40
@@ -260,7 +257,7 @@ curdkv_status curdkv_qcache_attention(const void* Q, int32_t q_rows, int64_t q_s
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   const int64_t P = (int64_t)cache->batch * cache->kv_heads;
   if (P == 0) return CURDKV_OK;
-  if (P * pl.blocks * pl.splits > 0x7fffffffLL || P * q_rows > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+  if (P * pl.blocks > 0x7fffffffLL || P * q_rows > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
   token::Args a = {};
   a.Q = static_cast<const __nv_bfloat16*>(Q);
   a.q_sb = q_stride_b; a.q_sh = q_stride_h; a.q_sn = q_stride_n;
@@ -271,14 +268,18 @@ curdkv_status curdkv_qcache_attention(const void* Q, int32_t q_rows, int64_t q_s
   a.group = 1;
   a.q_n = a.rows = q_rows;
   a.blocks = pl.blocks;
-  a.splits = pl.splits;
+  a.items = (int)(P * pl.blocks);
+  a.ctas = pl.ctas;
+  // (a masked product is -inf, and -inf times a scale of 0 would be NaN)
   a.scale_log2 = scale * 1.4426950408889634f;
+  if (a.scale_log2 < 1e-30f) a.scale_log2 = 1e-30f;
   a.cache = view_of(cache);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
+  a.begins = reinterpret_cast<int64_t*>(ws + pl.begins_at);
   a.part_ml = reinterpret_cast<float*>(ws + pl.ml_at);
   a.part_o = reinterpret_cast<float*>(ws + pl.o_at);
   a.status = reinterpret_cast<uint32_t*>(ws);
-  return (pl.nt == 1 ? launch_attend<true, 1>(a, P, stream) : launch_attend<true, 2>(a, P, stream)) ? CURDKV_OK
+  return (pl.nt == 1 ? launch_attend<true, 1>(a, stream) : launch_attend<true, 2>(a, stream)) ? CURDKV_OK
                                                                                                   : CURDKV_ERR_CUDA;
 }
 
@@ -302,7 +303,7 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
       !query_strides_ok(O, o_stride_b, o_stride_h, o_stride_n) || Q == O)
     return CURDKV_ERR_INVALID_ARG;
   if (workspace == nullptr || !status_ok(workspace)) return CURDKV_ERR_INVALID_ARG;
-  // rows the block with the most visible ones sees: its window, the tokens between, the sinks
+  // the most rows a block of queries sees: its window, the tokens between, the sinks
   int64_t seen = (int64_t)window + num_sink + q_rows;
   if (seen > desc->n_max) seen = desc->n_max;
   Plan pl = plan_window(desc, q_rows, seen);
@@ -311,7 +312,8 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
   const int64_t P = (int64_t)desc->batch * desc->kv_heads;
   if (P == 0) return CURDKV_OK;
   const int group = desc->q_heads / desc->kv_heads;
-  const float scale_log2 = scale * 1.4426950408889634f;
+  // a masked product is -inf, and -inf times a scale of 0 would be NaN
+  const float scale_log2 = scale * 1.4426950408889634f > 1e-30f ? scale * 1.4426950408889634f : 1e-30f;
   if ((int64_t)group * q_rows >= kPromptRows && desc->n_max > 0 && (int64_t)desc->n_max + q_rows < (1 << 30) &&
       map_strides_ok(desc->batch, desc->kv_heads, desc->n_max, desc->k_stride_b, desc->k_stride_h, desc->k_stride_n) &&
       map_strides_ok(desc->batch, desc->kv_heads, desc->n_max, desc->v_stride_b, desc->v_stride_h, desc->v_stride_n) &&
@@ -333,8 +335,7 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
     wa.n_max = desc->n_max;
     wa.num_sink = num_sink < desc->n_max ? num_sink : desc->n_max;
     wa.window = window < desc->n_max ? window : desc->n_max;
-    // a masked logit is -inf, and -inf times a scale of 0 would be NaN
-    wa.scale_log2 = scale_log2 > 1e-30f ? scale_log2 : 1e-30f;
+    wa.scale_log2 = scale_log2;
     wa.O = static_cast<__nv_bfloat16*>(O);
     wa.o_sb = o_stride_b; wa.o_sh = o_stride_h; wa.o_sn = o_stride_n;
     wa.lse = lse;
@@ -363,8 +364,9 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
   if ((int64_t)a.group * q_rows > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
   a.rows = a.group * q_rows;
   a.blocks = pl.blocks;
-  a.splits = pl.splits;
-  if (P * pl.blocks * pl.splits > 0x7fffffffLL || P * a.rows > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+  a.items = (int)(P * pl.blocks);
+  a.ctas = pl.ctas;
+  if (P * pl.blocks > 0x7fffffffLL || P * a.rows > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
   a.scale_log2 = scale_log2;
   a.K = KvView{static_cast<const __nv_bfloat16*>(K), desc->k_stride_b, desc->k_stride_h, desc->k_stride_n};
   a.V = KvView{static_cast<const __nv_bfloat16*>(V), desc->v_stride_b, desc->v_stride_h, desc->v_stride_n};
@@ -374,10 +376,11 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
   a.num_sink = num_sink;
   a.window = window;
   unsigned char* ws = static_cast<unsigned char*>(workspace);
+  a.begins = reinterpret_cast<int64_t*>(ws + pl.begins_at);
   a.part_ml = reinterpret_cast<float*>(ws + pl.ml_at);
   a.part_o = reinterpret_cast<float*>(ws + pl.o_at);
   a.status = reinterpret_cast<uint32_t*>(ws);
-  return (pl.nt == 1 ? launch_attend<false, 1>(a, P, stream) : launch_attend<false, 2>(a, P, stream)) ? CURDKV_OK
+  return (pl.nt == 1 ? launch_attend<false, 1>(a, stream) : launch_attend<false, 2>(a, stream)) ? CURDKV_OK
                                                                                                     : CURDKV_ERR_CUDA;
 }
 
