@@ -138,17 +138,18 @@ struct Tile {                                              // one warp's stage
   static constexpr int kScaled = Q4 ? kKeys * (8 * 2 + 8) : 0;
   static constexpr int kWarpBytes = kStages * kBytes + kScaled;
 };
-// Warps of a CTA; two CTAs fill an SM's registers and shared memory, so that one streams while the other
-// begins or ends an item.
-constexpr int kCtasPerSm = 2;
+// Four warps a CTA, one on each of the SM's schedulers (six a CTA, two CTAs, left two schedulers with
+// twice the warps of the others), and as many CTAs as registers and shared memory hold: one streams
+// while another begins or ends an item.
+constexpr int kWarps = 4, kThreads = kWarps * 32;
 template <bool Q4, int NT>
-__host__ __device__ constexpr int warps() {
-  return Q4 && NT == 1 ? 6 : 4;
+__host__ __device__ constexpr int ctas_per_sm() {
+  return Q4 && NT == 1 ? 3 : 2;
 }
 template <bool Q4, int NT>
 constexpr int smem_bytes() {
-  constexpr int ring = warps<Q4, NT>() * Tile<Q4>::kWarpBytes;
-  constexpr int merge = warps<Q4, NT>() * 8 * NT * 132 * 4;         // the warps' sums meet in the ring's space
+  constexpr int ring = kWarps * Tile<Q4>::kWarpBytes;
+  constexpr int merge = kWarps * 8 * NT * 132 * 4;         // the warps' sums meet in the ring's space
   return ring > merge ? ring : merge;
 }
 
@@ -208,9 +209,8 @@ __device__ __forceinline__ int cta_of(int64_t x, int64_t total, int64_t runs) { 
 constexpr int kMostItems = 8192;                           // items that are put on one line
 
 template <bool Q4, int NT>
-__global__ void __launch_bounds__(warps<Q4, NT>() * 32, kCtasPerSm) attend_kernel(const Args a) {
+__global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kernel(const Args a) {
   using T = Tile<Q4>;
-  constexpr int kWarps = warps<Q4, NT>(), kThreads = kWarps * 32;
   constexpr int KB = T::kKeys / 16;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ float s_m[kWarps][8 * NT], s_l[kWarps][8 * NT];

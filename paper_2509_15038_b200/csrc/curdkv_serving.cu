@@ -77,21 +77,25 @@ struct Plan {
   size_t begins_at, ml_at, o_at, bytes;                    // inside the workspace, and its size
 };
 
-// `keys`: the most a head can hold or see in this call.  A CTA per item where that is one round of its
-// warps' tiles, or where there are so many items that their lengths even out; one line of tiles, cut into
-// equal runs, else -- as many runs as CTAs fit the device, but none shorter than a round unless there are more items.
-// The workspace does not depend on `keys`.
-Plan plan_token(int64_t problems, int64_t rows, int64_t keys, int tile_keys, int warps) {
+// `keys`: the most a head can hold or see in this call.  A CTA per item where that is a few rounds of its
+// warps' tiles (joining parts costs a second launch, as long as about eight rounds), or where there are so
+// many items that their lengths even out; one line of tiles, cut into equal runs, else -- as many runs as
+// CTAs fit the device, but none shorter than two rounds unless there are more items.  (Four times as many
+// runs, to even out SMs of different speed, was slower: 282 against 276 us for 64 heads of 131072 rows, 66
+// against 51 for 128 heads of 2048 to 16384.)  The workspace does not depend on `keys`.
+Plan plan_token(int64_t problems, int64_t rows, int64_t keys, int tile_keys, int ctas_per_sm) {
   Plan pl;
   pl.nt = rows <= 8 ? 1 : 2;
   pl.blocks = (int)((rows + 8 * pl.nt - 1) / (8 * pl.nt));
-  const int64_t items = problems * pl.blocks, slots = (int64_t)token::kCtasPerSm * sms();
+  const int64_t items = problems * pl.blocks, slots = (int64_t)ctas_per_sm * sms();
   const int64_t tiles = (keys + tile_keys - 1) / tile_keys;
   pl.ctas = 0;
-  if (tiles > warps && items <= token::kMostItems) {
-    int64_t ctas = (items * tiles + warps - 1) / warps;
+  if (tiles > 8 * token::kWarps && items <= token::kMostItems) {
+    const int64_t rounds = (items * tiles + token::kWarps - 1) / token::kWarps;
+    int64_t ctas = rounds / 2;
     if (ctas < items) ctas = items;
-    pl.ctas = (int)(ctas < slots ? ctas : slots);
+    if (ctas > slots) ctas = slots;
+    pl.ctas = (int)ctas;
   }
   const bool room = items <= token::kMostItems;
   const size_t parts = room ? 2 * (size_t)slots * 8 * pl.nt : 0;
@@ -105,12 +109,12 @@ Plan plan_token(int64_t problems, int64_t rows, int64_t keys, int tile_keys, int
 Plan plan_qcache(const curdkv_qcache* c, int32_t q_rows) {
   // (packed heads: any of them may own most of the rows)
   return plan_token((int64_t)c->batch * c->kv_heads, q_rows, c->capacity, token::Tile<true>::kKeys,
-                    q_rows <= 8 ? token::warps<true, 1>() : token::warps<true, 2>());
+                    q_rows <= 8 ? token::ctas_per_sm<true, 1>() : token::ctas_per_sm<true, 2>());
 }
 
 Plan plan_window(const curdkv_desc* d, int32_t q_rows, int64_t seen) {
   return plan_token((int64_t)d->batch * d->kv_heads, (int64_t)(d->q_heads / d->kv_heads) * q_rows, seen,
-                    token::Tile<false>::kKeys, token::warps<false, 1>());
+                    token::Tile<false>::kKeys, token::ctas_per_sm<false, 1>());
 }
 
 template <bool Q4, int NT>
@@ -120,7 +124,7 @@ bool launch_attend(const token::Args& a, cudaStream_t stream) {
       cudaSuccess)
     return false;
   const int grid = a.ctas > 0 ? a.ctas : a.items;
-  token::attend_kernel<Q4, NT><<<(unsigned)grid, token::warps<Q4, NT>() * 32, smem, stream>>>(a);
+  token::attend_kernel<Q4, NT><<<(unsigned)grid, token::kThreads, smem, stream>>>(a);
   if (!launched()) return false;
   if (a.ctas == 0) return true;
   // launched behind attend_kernel without waiting for its end: the kernel itself waits
