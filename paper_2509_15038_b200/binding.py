@@ -196,17 +196,19 @@ def make_desc(K: torch.Tensor, V: torch.Tensor, r: int, *, q_heads: Optional[int
               use_projection: int = 1, raw_scores: int = 0, whiten: int = 0,
               ridge: float = 0.0) -> Desc:
     """Descriptor of bf16 K, V ``[B, Hkv, n_max, d]`` (any strides with d contiguous)."""
-    if K.dtype != torch.bfloat16 or V.dtype != torch.bfloat16:
+    if K.dtype is not torch.bfloat16 or V.dtype is not torch.bfloat16:
         raise TypeError("K and V must be bf16")
-    if K.dim() != 4 or K.shape != V.shape or K.stride(3) != 1 or V.stride(3) != 1:
+    shape, k, v = K.shape, K.stride(), V.stride()
+    if len(shape) != 4 or shape != V.shape or k[3] != 1 or v[3] != 1:
         raise ValueError("K and V must be [B, Hkv, n, d] with a contiguous last axis")
-    if seqlens is not None and (seqlens.dtype != torch.int32 or seqlens.numel() != K.shape[0]
-                                or not seqlens.is_contiguous()):
+    B, H, n, d = shape
+    if seqlens is None:
+        lens = None
+    elif seqlens.dtype is not torch.int32 or seqlens.numel() != B or not seqlens.is_contiguous():
         raise ValueError("seqlens must be a contiguous int32 tensor of length B")
-    B, H, n, d = K.shape
-    desc = Desc(B, H, q_heads or H, n, d, int(r),
-                K.stride(0), K.stride(1), K.stride(2), V.stride(0), V.stride(1), V.stride(2),
-                seqlens.data_ptr() if seqlens is not None else None,
+    else:
+        lens = seqlens.data_ptr()
+    desc = Desc(B, H, q_heads or H, n, d, int(r), k[0], k[1], k[2], v[0], v[1], v[2], lens,
                 int(score_mode), int(use_projection), int(raw_scores), int(whiten), float(ridge))
     desc.seqlens_tensor = seqlens        # the lengths live as long as the descriptor that points at them
     return desc
@@ -486,19 +488,19 @@ def curdkv_eviction_loss(O_full, O_comp):
 def _on_device(what: str, first: torch.Tensor, *rest: Optional[torch.Tensor]) -> int:
     """Index of the device that every given tensor lies on, which has to be the current one (the
     calls launch on its current stream)."""
-    dev = first.device
-    if dev.type != "cuda":
+    dev = first.get_device()
+    if dev < 0:
         raise ValueError(f"{what}: tensors must be on a CUDA device")
     for t in rest:
-        if t is not None and t.device != dev:
-            raise ValueError(f"{what}: tensors are on {dev} and {t.device}")
-    if dev.index != torch._C._cuda_getDevice():
-        raise ValueError(f"{what}: tensors are on {dev}, which is not the current device")
-    return dev.index
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"{what}: tensors are on {first.device} and {t.device}")
+    if dev != torch._C._cuda_getDevice():
+        raise ValueError(f"{what}: tensors are on {first.device}, which is not the current device")
+    return dev
 
 
 def _int32(what: str, t: Optional[torch.Tensor], numel: Optional[int] = None) -> None:
-    if t is not None and (t.dtype != torch.int32 or not t.is_contiguous() or (numel is not None and t.numel() != numel)):
+    if t is not None and (t.dtype is not torch.int32 or not t.is_contiguous() or (numel is not None and t.numel() != numel)):
         raise ValueError(f"{what} must be a contiguous int32 tensor" + (f" of {numel} entries" if numel is not None else ""))
 
 
@@ -509,6 +511,10 @@ def _status_buffer(what: str, t: Optional[torch.Tensor]) -> None:
 
 def _raw_stream(index: int) -> int:
     return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _addr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
 
 
 class QuantCache:
@@ -573,10 +579,12 @@ def curdkv_qcache_store(cache: QuantCache, K, V, desc: Desc, idx=None, head_coun
         if P > 0 and idx.numel() % P != 0:
             raise ValueError("idx must be [batch, kv_heads, budget]")
         stride = idx.numel() // max(P, 1)
+    if P == 0:
+        return
     code = load().curdkv_qcache_store(cache._ref, _ptr(K), _ptr(V), ctypes.byref(desc), _ptr(idx), stride,
-                                      _ptr(head_counts) if idx is not None else None,
-                                      _ptr(head_offsets) if idx is not None and packed else None,
-                                      _ptr(workspace), _raw_stream(dev))
+                                      _addr(head_counts) if idx is not None else None,
+                                      _addr(head_offsets) if idx is not None and packed else None,
+                                      _addr(workspace), _raw_stream(dev))
     _check(code, "curdkv_qcache_store")
 
 
@@ -586,8 +594,10 @@ def curdkv_qcache_append(cache: QuantCache, K_new, V_new, *, t_new: Optional[tor
     dev = _on_device("curdkv_qcache_append", cache.K_codes, K_new, V_new, t_new, workspace)
     _status_buffer("curdkv_qcache_append", workspace)
     desc = make_desc(K_new, V_new, 1, seqlens=t_new)
-    code = load().curdkv_qcache_append(cache._ref, _ptr(K_new), _ptr(V_new), ctypes.byref(desc), _ptr(workspace),
-                                       _raw_stream(dev))
+    if K_new.numel() == 0:
+        return
+    code = load().curdkv_qcache_append(cache._ref, K_new.data_ptr(), V_new.data_ptr(), ctypes.byref(desc),
+                                       _addr(workspace), _raw_stream(dev))
     _check(code, "curdkv_qcache_append")
 
 
@@ -612,12 +622,12 @@ def curdkv_qcache_read(cache: QuantCache, idx: Optional[torch.Tensor] = None, *,
     for t in (K_out, V_out):
         if t is None:
             t = torch.zeros(shape, dtype=torch.bfloat16, device=cache.device)
-        elif t.dtype != torch.bfloat16 or not t.is_contiguous() or tuple(t.shape) != shape:
+        elif t.dtype is not torch.bfloat16 or not t.is_contiguous() or t.shape != shape:
             raise ValueError(f"outputs must be contiguous bf16 {shape}")
         out.append(t)
-    if idx is not None and rows == 0:
+    if out[0].numel() == 0:
         return out[0], out[1]
-    code = load().curdkv_qcache_read(cache._ref, _ptr(idx), rows, _ptr(out[0]), _ptr(out[1]), _ptr(workspace),
+    code = load().curdkv_qcache_read(cache._ref, _addr(idx), rows, out[0].data_ptr(), out[1].data_ptr(), _addr(workspace),
                                      _raw_stream(dev))
     _check(code, "curdkv_qcache_read")
     return out[0], out[1]
@@ -638,34 +648,36 @@ def attention_window_workspace(desc: Desc, q_rows: int, device="cuda") -> torch.
 
 
 def _queries(what, Q, O, lse):
-    if Q.dtype != torch.bfloat16 or Q.dim() != 4 or Q.stride(3) != 1 or Q.shape[3] != 128:
+    """Checks Q, O and lse; returns O (made where not given), Q's shape, and both tensors' strides."""
+    shape, q = Q.shape, Q.stride()
+    if Q.dtype is not torch.bfloat16 or len(shape) != 4 or q[3] != 1 or shape[3] != 128:
         raise ValueError(f"{what}: Q must be bf16 [B, H, rows, 128] with a contiguous last axis")
     if O is None:
-        O = torch.empty(Q.shape, dtype=torch.bfloat16, device=Q.device)
-    elif O.dtype != torch.bfloat16 or O.shape != Q.shape or O.stride(3) != 1:
+        O = torch.empty(shape, dtype=torch.bfloat16, device=Q.device)
+    o = O.stride()
+    if O.dtype is not torch.bfloat16 or O.shape != shape or o[3] != 1:
         raise ValueError(f"{what}: O must be bf16 of Q's shape with a contiguous last axis")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != Q.shape[:3] or not lse.is_contiguous()):
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != shape[:3] or not lse.is_contiguous()):
         raise ValueError(f"{what}: lse must be contiguous fp32 [B, H, rows]")
-    return O
+    return O, shape, q, o
 
 
 def curdkv_qcache_attention(Q, cache: QuantCache, *, scale: float, O=None, lse=None,
                             workspace: Optional[torch.Tensor] = None):
     """O = softmax(scale Q K^T) V over the held rows.  Q bf16 ``[B, Hkv, q_rows, 128]``, the queries of a GQA group
     stacked along q_rows; ``lse`` fp32 ``[B, Hkv, q_rows]`` receives the log sums where given.  Returns (O, workspace)."""
-    O = _queries("curdkv_qcache_attention", Q, O, lse)
-    if Q.shape[0] != cache.batch or Q.shape[1] != cache.kv_heads:
+    O, (B, H, m, _), q, o = _queries("curdkv_qcache_attention", Q, O, lse)
+    if B != cache.batch or H != cache.kv_heads:
         raise ValueError("curdkv_qcache_attention: Q and the cache differ in batch or heads")
-    m = Q.shape[2]
     if workspace is None:
         workspace = qcache_attention_workspace(cache, m)
     dev = _on_device("curdkv_qcache_attention", cache.K_codes, Q, O, lse, workspace)
-    qb, qh, qn, _ = Q.stride()
-    ob, oh, on, _ = O.stride()
-    code = load().curdkv_qcache_attention(Q.data_ptr(), m, qb, qh, qn, cache._ref, scale, O.data_ptr(), ob, oh, on,
-                                          None if lse is None else lse.data_ptr(), workspace.data_ptr(),
-                                          workspace.numel(), _raw_stream(dev))
-    _check(code, "curdkv_qcache_attention")
+    if B == 0:
+        return O, workspace
+    code = load().curdkv_qcache_attention(Q.data_ptr(), m, q[0], q[1], q[2], cache._ref, scale, O.data_ptr(), o[0], o[1],
+                                          o[2], _addr(lse), workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
+    if code:
+        _check(code, "curdkv_qcache_attention")
     return O, workspace
 
 
@@ -675,21 +687,20 @@ def curdkv_attention_window(Q, K, V, desc: Desc, window: int, *, num_sink: int =
     """Causal attention over the last ``window`` rows and the first ``num_sink``.  Q bf16 ``[B, Hq, t, 128]``: the last
     ``q_lens`` (int32 ``[B]``, default t) positions of each sequence of ``desc``; query rows beyond leave O untouched.
     Returns (O, workspace)."""
-    O = _queries("curdkv_attention_window", Q, O, lse)
-    if Q.shape[0] != desc.batch or Q.shape[1] != desc.q_heads:
+    O, (B, H, t, _), q, o = _queries("curdkv_attention_window", Q, O, lse)
+    if B != desc.batch or H != desc.q_heads:
         raise ValueError("curdkv_attention_window: Q and the descriptor differ in batch or query heads")
-    _int32("q_lens", q_lens, desc.batch)
-    t = Q.shape[2]
+    _int32("q_lens", q_lens, B)
     if workspace is None:
         workspace = attention_window_workspace(desc, t, device=Q.device)
     dev = _on_device("curdkv_attention_window", Q, K, V, O, lse, q_lens, workspace)
-    qb, qh, qn, _ = Q.stride()
-    ob, oh, on, _ = O.stride()
-    code = load().curdkv_attention_window(Q.data_ptr(), t, qb, qh, qn, None if q_lens is None else q_lens.data_ptr(),
-                                          K.data_ptr(), V.data_ptr(), ctypes.byref(desc), num_sink, window, scale,
-                                          O.data_ptr(), ob, oh, on, None if lse is None else lse.data_ptr(),
-                                          workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
-    _check(code, "curdkv_attention_window")
+    if B == 0:
+        return O, workspace
+    code = load().curdkv_attention_window(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), _ptr(K), _ptr(V),
+                                          ctypes.byref(desc), num_sink, window, scale, O.data_ptr(), o[0], o[1], o[2],
+                                          _addr(lse), workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
+    if code:
+        _check(code, "curdkv_attention_window")
     return O, workspace
 
 

@@ -117,12 +117,23 @@ Plan plan_window(const curdkv_desc* d, int32_t q_rows, int64_t seen) {
                     token::Tile<false>::kKeys, token::ctas_per_sm<false, 1>());
 }
 
+// Lets `kernel` use `bytes` of shared memory on the current device; asked of the driver once per device.
+template <typename Kernel>
+bool allow_smem(Kernel kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return true;
+}
+
 template <bool Q4, int NT>
 bool launch_attend(const token::Args& a, cudaStream_t stream) {
   constexpr int smem = token::smem_bytes<Q4, NT>();
-  if (cudaFuncSetAttribute(token::attend_kernel<Q4, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) !=
-      cudaSuccess)
-    return false;
+  static std::atomic<uint64_t> done{0};
+  if (!allow_smem(token::attend_kernel<Q4, NT>, smem, done)) return false;
   const int grid = a.ctas > 0 ? a.ctas : a.items;
   token::attend_kernel<Q4, NT><<<(unsigned)grid, token::kThreads, smem, stream>>>(a);
   if (!launched()) return false;
@@ -349,9 +360,8 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
     if (P * pairs > 0x3fffffffLL) return CURDKV_ERR_UNSUPPORTED;
     wa.pairs = (int)pairs;
     wa.items = (int)(P * pairs);
-    if (cudaFuncSetAttribute(umma::window_umma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, umma::kWinDynamic) !=
-        cudaSuccess)
-      return CURDKV_ERR_CUDA;
+    static std::atomic<uint64_t> done{0};
+    if (!allow_smem(umma::window_umma_kernel, umma::kWinDynamic, done)) return CURDKV_ERR_CUDA;
     const int grid = wa.items < sms() ? wa.items : sms();
     umma::window_umma_kernel<<<(unsigned)grid, umma::kWinThreads, umma::kWinDynamic, stream>>>(mq, mk, mv, wa);
     return launched() ? CURDKV_OK : CURDKV_ERR_CUDA;
