@@ -350,7 +350,8 @@ curdkv_status curdkv_cache_step(const curdkv_cache* cache, const void* K_new, co
  * curdkv_qcache holds, per (sequence, KV head), rows of K and V of 128 channels in 4 bits:
  * 160 bytes for a row of both instead of 512.  Every row has four groups of 32 consecutive
  * channels; a group with least value lo and greatest hi is held as
- *   scale = bf16((hi - lo) / 15)   fp32 subtraction and division, rounded to bf16 (nearest even)
+ *   scale = bf16((hi - lo) * (1/15))   fp32 subtraction and product with the fp32 number next to 1/15,
+ *                                      rounded to bf16 (nearest even)
  *   zero  = lo                      (a bf16 value: no rounding)
  *   code  = rint((x - zero) / scale), ties to even, limited to 0 .. 15 (0 when scale is 0),
  *           decided as in 64-bit arithmetic

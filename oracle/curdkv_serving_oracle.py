@@ -1,7 +1,7 @@
 """Oracle of the serving calls: 4-bit rows and attention over them, and the attention with a sliding window and sinks, in
 numpy float64 on the host, shared with nothing on the GPU side.
 
-A group of 32 channels with least value lo and greatest hi is held as scale = bf16(fp32(hi - lo) / 15), zero = lo and
+A group of 32 channels with least value lo and greatest hi is held as scale = bf16(fp32(hi - lo) * fp32(1/15)), zero = lo and
 codes rint((x - zero) / scale) in 0 .. 15; channel 32 g + 8 t + u of K sits in nibble u of 32-bit word 4 t + g of its
 row's 64 bytes, channel 32 g + 4 t + u of V in nibble u of 16-bit word 4 t + g.
 """
@@ -25,7 +25,7 @@ def quantise(x):
     x = np.asarray(x, dtype=np.float64).reshape(-1, 4, 32)
     with np.errstate(all="ignore"):
         lo, hi = x.min(-1), x.max(-1)
-        s32 = ((hi.astype(np.float32) - lo.astype(np.float32)) / np.float32(15)).astype(np.float32)
+        s32 = ((hi.astype(np.float32) - lo.astype(np.float32)) * np.float32(1 / 15)).astype(np.float32)
         bits = bf16_bits(s32)
         s = bf16_value(bits).astype(np.float64)
         bad = ~np.isfinite(s) | ~np.isfinite(x).all(-1)

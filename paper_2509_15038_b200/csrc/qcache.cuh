@@ -2,7 +2,7 @@
 // pairs.  Quantising store (with or without a selection), append, and the way back to bf16.
 //
 // A group of 32 channels with least value lo and greatest hi is held as
-//   s = bf16((hi - lo) / 15),  z = lo,  code = rint((x - z) / s)  (ties to even, 0 .. 15)
+//   s = bf16((hi - lo) * fp32(1/15)),  z = lo,  code = rint((x - z) / s)  (ties to even, 0 .. 15)
 // and stands for s * code + z.  The zero needs no rounding (lo is a bf16 value), and the
 // rounding of the scale costs nothing either: the codes are formed with the rounded scale, and
 // at the top of the range (hi - lo) / s <= 15 (1 + 2^-8) still rounds to 15.
@@ -94,14 +94,6 @@ __device__ __forceinline__ uint64_t sub_f2(uint64_t a, uint64_t b) {
   return d;
 }
 
-// d / 15 correctly rounded: one correction by the exact residual after multiplying with the correctly
-// rounded reciprocal (Markstein); ranges where the residual could underflow divide.
-__device__ __forceinline__ float fifteenth(float d) {
-  if (!(d > 0x1p-80f && d < 0x1p120f)) return __fdiv_rn(d, 15.f);
-  const float y = 1.f / 15.f, q = __fmul_rn(d, y);
-  return __fmaf_rn(__fmaf_rn(-15.f, q, d), y, q);
-}
-
 // Eight channels of one group: their codes, four bits each from the lowest, and the (scale, zero)
 // word of the group, which four neighbouring lanes share.  All 32 lanes of the warp call this together.
 __device__ __forceinline__ uint32_t quantise8(const uint4& v, uint32_t& meta) {
@@ -124,7 +116,7 @@ __device__ __forceinline__ uint32_t quantise8(const uint4& v, uint32_t& meta) {
   }
   const uint32_t eu = *reinterpret_cast<const uint32_t*>(&ext);
   const float hi = __uint_as_float(eu << 16), lo = -__uint_as_float(eu & 0xffff0000u);
-  const __nv_bfloat16 sb = __float2bfloat16_rn(fifteenth(__fsub_rn(hi, lo)));
+  const __nv_bfloat16 sb = __float2bfloat16_rn(__fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f));
   const float s = __bfloat162float(sb);
   if (!(s < INFINITY)) {             // a NaN, an infinity or a range beyond fp32: the group is NaN
     meta = 0x7fc0u;
