@@ -7,14 +7,14 @@
 // same rows for even groups, neighbouring row blocks for a group of one.  Only the key tiles that some
 // row of the pair sees are walked: those holding sinks, then those of the window.
 //
-// Eleven warps.  Four softmax warps own each query tile, a thread per row.  Keys come 64 at a time: S = Q K^T
-// arrives in one of two buffers in TMEM, the thread takes its 64 logits into registers, and the weights
-// go back over S as bf16, where they are the A operand of O += P V straight from TMEM.  Each query tile
-// has an issuing warp of its own: behind P V of a step it issues S two steps ahead into the buffer that
-// P has left, so that the softmax warps always find the next logits ready.  (With one buffer of 128 keys
-// softmax and products of a tile take turns: 4000 cycles per 128 keys and pair of tiles against 2900.)
-// The last warp walks the work: it feeds Q and the ring of K and V tiles by TMA and describes every step
-// (64 keys of one item) to the others in a small ring of its own.  Items follow each other without a gap.
+// Eleven warps.  Four softmax warps own each query tile, a thread per row: S = Q K^T arrives in TMEM,
+// the thread takes its 128 logits into registers, and the weights go back over S as bf16, where they are
+// the A operand of O += P V straight from TMEM.  Each query tile has an issuing warp of its own, which
+// alternates P V of one key tile with S of the next: the two tiles run apart, and while one turns
+// logits into weights the tensor pipe works for the other.  P is handed over in halves, so that P V starts
+// on the first 64 keys.  The last warp walks the work: it feeds Q and the ring of K and V tiles by TMA and
+// describes every step (one key tile of one item) to the others in a small ring of its own.  Items follow
+// each other without a gap: the next pair's first S is issued right behind the last product of this one.
 //
 // An issuing warp has to be quick between its batches of products, or the pipe runs dry: it works
 // converged with one elected lane issuing (inside `if (lane == 0)` the compiler cannot use uniform
@@ -22,9 +22,9 @@
 // Measured and dropped: two threads per row (a tile's softmax 2650 cycles against 1700, the warps crowding
 // each other out); one issuing warp for both tiles (it waits for one while the other is ready).
 //
-// What bounds it: 128 x 128 keys cost the tensor pipe 1280 cycles (S as N = 64 products of 48 cycles, P V
-// of 64) and the exponentials of the tile 1024 cycles of the special function units, so every
-// kPolyEvery-th pair of weights is formed on the FMA pipe instead (a minimax polynomial of degree 4).
+// What bounds it: 128 x 128 keys cost the tensor pipe 1024 cycles (two products of 512) and the
+// exponentials of the tile 1024 cycles of the special function units, so every kPolyEvery-th pair of
+// weights is formed on the FMA pipe instead (a minimax polynomial of degree 4).
 //
 // The running maximum moves only when a tile exceeds it by more than 2^8 (as in attn_umma.cuh); the
 // group then rescales its accumulator in TMEM, which after the first tiles is rare.  Value rows at or
@@ -38,12 +38,13 @@
 
 namespace curdkv {
 
-// Map of a bf16 tensor [batch][heads][rows][128] for tiles of tile_rows rows (defined beside the C ABI).
+// Map of a bf16 tensor [batch][heads][rows][128] for tiles of 128 rows (defined beside the C ABI).
 bool rows_map(CUtensorMap* map, const void* base, int32_t batch, int32_t heads, int32_t rows, int64_t stride_b,
               int64_t stride_h, int64_t stride_n, int32_t tile_rows);
 
 namespace umma {
 
+constexpr int kWinKeys = 128;
 struct WindowArgs {
   const int32_t* seqlens;            // [batch] or nullptr
   const int32_t* q_lens;             // [batch] or nullptr
@@ -60,37 +61,34 @@ struct WindowArgs {
   unsigned long long wait_ns = kWaitLimitNs;
 };
 
-constexpr int kWinThreads = 352;
+constexpr int kWinThreads = 320;
 constexpr int kWinSoftmaxWarps = 8;
-constexpr int kWinKeys = 64;                               // keys of a step
-constexpr int kWinTileHalf = kWinKeys * 128;               // 64 keys x 64 channels
-constexpr int kWinTileBytes = 2 * kWinTileHalf;
-constexpr int kWinRing = 8;                                // tiles of K and V, in turn
+constexpr int kWinRing = 4;
 constexpr int kWinQ = 0;                                   // Q of the two tiles
 constexpr int kWinSlot0 = 2 * kSlotBytes;
-constexpr int kWinStage = kWinSlot0 + kWinRing * kWinTileBytes;         // 2 KB per softmax warp for its output
+constexpr int kWinStage = kWinSlot0 + kWinRing * kSlotBytes;         // 2 KB per softmax warp for its output
 constexpr int kWinBar = kWinStage + kWinSoftmaxWarps * 2048;
 constexpr int kWinInfoRing = 8;                            // steps described ahead
 constexpr int kWinDynamic = kWinBar + 1024 + 1024;
-constexpr int kWinTmemCols = 512;                          // S_A (two buffers of 64), S_B, O_A, O_B
+constexpr int kWinTmemCols = 512;                          // S_A, S_B, O_A, O_B
 constexpr float kWinSlack = 8.f;
 
-// A step: 64 keys of one item.  Flag bits of query tile g are shifted by 4 g.
+// A step: one key tile of one item.  Flag bits of query tile g are shifted by 4 g.
 constexpr uint32_t kStepNeeds = 1u, kStepFirst = 2u, kStepLast = 4u;
 constexpr uint32_t kStepZero = 8u;                         // the query tile has rows that see no key at all: O = 0
 constexpr uint32_t kStepStop = 1u << 8;                    // no step: the work is done
 constexpr uint32_t kStepEmpty = 1u << 9;                   // no key tile: only zeros to write
-constexpr int kStepGroups = 12;                            // from this bit: groups of 16 keys that matter (1 .. 4)
+constexpr int kStepGroups = 12;                            // from this bit: groups of 16 keys that matter (1 .. 8)
 
 struct alignas(16) StepInfo {
   uint32_t flags;
-  int j0, n, b;                      // first key; rows of the sequence; sequence
+  int j0, n, b;                      // first key of the tile; rows of the sequence; sequence
   int head[2], row0[2];              // query heads; first query rows of the tiles
   int pos0[2], rows[2];              // position of that row; rows that exist
 };
 static_assert(sizeof(StepInfo) == 48, "written and read as three 16-byte words");
 
-// One query tile of an item, and which tiles of 64 keys it needs: [0, sink_tiles) and [lo, hi).
+// One query tile of an item, and which key tiles it needs: [0, sink_tiles) and [lo, hi).
 struct WinTile {
   int rows, sink_tiles, lo, hi;
   __device__ __forceinline__ bool needs(int kt) const { return kt < sink_tiles || (kt >= lo && kt < hi); }
@@ -98,12 +96,6 @@ struct WinTile {
   __device__ __forceinline__ int first() const { return sink_tiles > 0 ? 0 : lo; }
   __device__ __forceinline__ int last() const { return max(sink_tiles, hi > lo ? hi : 0) - 1; }
 };
-
-// smem_desc_mn_sw128 for a tile of 64 keys: its two 64-channel spans are kWinTileHalf bytes apart.
-__device__ __forceinline__ uint64_t win_v_desc(uint32_t addr) {
-  return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)(kWinTileHalf >> 4) << 16) | (64ull << 32) | (1ull << 46) |
-         (2ull << 61);
-}
 
 // 2^x for x <= 0 on the FMA pipe: x = i + f, |f| <= 1/2, 2^f by the polynomial of degree 4 with the
 // least greatest relative error there (Remez exchange: 2.6e-6), and i added to the exponent.
@@ -125,7 +117,7 @@ __device__ __forceinline__ uint64_t exp2_poly2(uint64_t x2) {
                __int_as_float(__float_as_int(p1) + (__float_as_int(r1) << 23)));
 }
 
-constexpr int kPolyEvery = 4;        // every 4th pair of weights by polynomial
+constexpr int kPolyEvery = 1000;        // every 4th pair of weights by polynomial
 
 // A wait that a whole warp makes together: false for all lanes when it ran out for one.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* status,
@@ -145,31 +137,31 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   const uint32_t gbar = bar0 + 8u * 2 * kWinRing;
   auto q_full = [&](int g) { return gbar + 8u * g; };
   auto q_empty = [&](int g) { return gbar + 16u + 8u * g; };
-  auto s_full = [&](int g, int buf) { return gbar + 32u + 16u * g + 8u * buf; };
-  auto p_ready = [&](int g, int buf) { return gbar + 64u + 16u * g + 8u * buf; };
-  auto o_full = [&](int g) { return gbar + 96u + 8u * g; };
-  auto o_empty = [&](int g) { return gbar + 112u + 8u * g; };
-  auto drain_bar = [&](int g) { return gbar + 128u + 8u * g; };
-  auto pv_done = [&](int g) { return gbar + 144u + 8u * g; };
-  auto info_full = [&](uint32_t e) { return gbar + 160u + 8u * e; };
-  auto info_empty = [&](uint32_t e) { return gbar + 160u + 8u * (kWinInfoRing + e); };
+  auto s_full = [&](int g) { return gbar + 32u + 8u * g; };
+  auto p_ready = [&](int g, int half) { return gbar + 48u + 16u * half + 8u * g; };
+  auto o_full = [&](int g) { return gbar + 80u + 8u * g; };
+  auto o_empty = [&](int g) { return gbar + 96u + 8u * g; };
+  const uint32_t drain_bar = gbar + 112u;
+  auto info_full = [&](uint32_t e) { return gbar + 144u + 8u * e; };
+  auto info_empty = [&](uint32_t e) { return gbar + 144u + 8u * (kWinInfoRing + e); };
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(base_ptr + kWinBar + 480);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
   uint4* info = reinterpret_cast<uint4*>(base_ptr + kWinBar + 512);           // [kWinInfoRing][3]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (tid == 0) {
-    for (int s = 0; s < kWinRing; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 2); }
-    for (int e = 0; e < kWinInfoRing; ++e) { mbar_init(info_full(e), 1); mbar_init(info_empty(e), kWinSoftmaxWarps + 2); }
+    for (int s = 0; s < kWinRing; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int e = 0; e < kWinInfoRing; ++e) { mbar_init(info_full(e), 1); mbar_init(info_empty(e), kWinSoftmaxWarps + 1); }
     for (int g = 0; g < 2; ++g) {
       mbar_init(q_full(g), 1);
       mbar_init(q_empty(g), 1);
-      for (int buf = 0; buf < 2; ++buf) { mbar_init(s_full(g, buf), 1); mbar_init(p_ready(g, buf), 128); }
+      mbar_init(s_full(g), 1);
+      mbar_init(p_ready(g, 0), 128);
+      mbar_init(p_ready(g, 1), 128);
       mbar_init(o_full(g), 1);
       mbar_init(o_empty(g), 128);
-      mbar_init(drain_bar(g), 1);
-      mbar_init(pv_done(g), 1);
     }
+    mbar_init(drain_bar, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -184,7 +176,7 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   tc_fence_after();
   const uint32_t tmem_base = *tmem_holder;
 
-  if (warp == kWinSoftmaxWarps + 2) {
+  if (warp == kWinSoftmaxWarps + 1) {
     // ------------------------------------------------------------ the work, step by step, and its tiles
     // Ring order of an item: K_0, V_0, K_1, V_1, ...; its two Q tiles follow K_0.
     if (lane == 0) {
@@ -196,10 +188,10 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       auto load = [&](const CUtensorMap* map, int j0, int h, int b) {
         const uint32_t slot = it % kWinRing;
         if (!wait(empty_bar(slot), ((it / kWinRing) & 1u) ^ 1u)) return;
-        mbar_arrive_expect_tx(full_bar(slot), kWinTileBytes);
-        const uint32_t dst = base + kWinSlot0 + slot * kWinTileBytes;
+        mbar_arrive_expect_tx(full_bar(slot), kSlotBytes);
+        const uint32_t dst = base + kWinSlot0 + slot * kSlotBytes;
         tma_load_4d(dst, map, full_bar(slot), 0, j0, h, b, pol);
-        tma_load_4d(dst + kWinTileHalf, map, full_bar(slot), 64, j0, h, b, pol);
+        tma_load_4d(dst + kHalfBytes, map, full_bar(slot), 64, j0, h, b, pol);
         ++it;
       };
       auto describe = [&](const StepInfo& i) {
@@ -234,10 +226,10 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           t[g].sink_tiles = t[g].lo = t[g].hi = 0;
           const int end = t[g].rows > 0 ? max(i.pos0[g] + t[g].rows, 0) : 0;       // keys [0, end) may be seen
           if (end > 0) {
-            t[g].sink_tiles = (min(a.num_sink, end) + kWinKeys - 1) / kWinKeys;
+            t[g].sink_tiles = (min(a.num_sink, end) + kTileRows - 1) / kTileRows;
             if (a.window > 0) {
-              t[g].lo = max(0, max(i.pos0[g], 0) + 1 - a.window) / kWinKeys;
-              t[g].hi = (end + kWinKeys - 1) / kWinKeys;
+              t[g].lo = max(0, max(i.pos0[g], 0) + 1 - a.window) / kTileRows;
+              t[g].hi = (end + kTileRows - 1) / kTileRows;
               lo = min(lo, t[g].lo);
               hi = max(hi, t[g].hi);
             }
@@ -256,9 +248,9 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
         for (int u = 0; ok && u < tiles; ++u) {
           const int kt = u < sinks ? u : lo + (u - sinks);
-          i.j0 = kt * kWinKeys;
+          i.j0 = kt * kTileRows;
           // a tile below the window holds sinks only: the rest of its keys need no products
-          const int keys = kt >= win_lo ? kWinKeys : min(a.num_sink - i.j0, kWinKeys);
+          const int keys = kt >= win_lo ? kTileRows : min(a.num_sink - i.j0, kTileRows);
           i.flags = (uint32_t)((keys + 15) >> 4) << kStepGroups | (u == 0 ? zero : 0u);
 #pragma unroll
           for (int g = 0; g < 2; ++g)
@@ -300,110 +292,114 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           if (q_it[g] > 0) land(q_full(g), (q_it[g] - 1) & 1u);
       }
     }
-  } else if (warp >= kWinSoftmaxWarps) {
-    // ------------------------------------------------------------ products of query tile g
+  } else if (warp == kWinSoftmaxWarps) {
+    // ------------------------------------------------------------ products
     // The whole warp walks the steps and waits; one elected lane issues.
-    const int g = warp - kWinSoftmaxWarps;
     constexpr uint32_t idesc_pv = instr_desc_pv();
-    constexpr uint32_t kSlotUnits = kWinTileBytes >> 4;
-    const uint64_t q_desc = smem_desc_sw128(base + kWinQ + g * kSlotBytes);
-    const uint64_t k_desc0 = smem_desc_sw128(base + kWinSlot0), v_desc0 = win_v_desc(base + kWinSlot0);
-    const uint32_t s_tmem = tmem_base + g * 128u, o_tmem = tmem_base + 256u + g * 128u;
-    uint32_t step = 0, it = 0;                             // steps described; ring entries described (two a step)
-    uint32_t q_phase = 0, p_phase = 0, o_phase = 1;        // (p_phase: a bit per buffer)
+    constexpr uint32_t kSlotUnits = kSlotBytes >> 4;
+    const uint64_t q_desc = smem_desc_sw128(base + kWinQ);
+    const uint64_t k_desc0 = smem_desc_sw128(base + kWinSlot0), v_desc0 = smem_desc_mn_sw128(base + kWinSlot0);
+    uint32_t step = 0, it = 0;                             // steps described; ring entries passed (two a key tile)
+    uint32_t q_phase = 0, p_phase = 0, o_phase = 3;        // a bit per query tile
     bool ok = true;                                        // the lanes agree on it at the end of each step
     auto wait = [&](uint32_t bar, uint32_t parity) { ok = mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns) && ok; };
-    struct Pending { uint32_t f, it; };                    // flags and first ring entry of a step
-    auto next_step = [&](const Pending& before) {          // the step after the last one described
-      Pending s;
-      s.f = before.f;
-      s.it = it;
-      if (before.f & kStepStop) return s;
+    auto next_step = [&]() {                               // the flags of the step after this one
       const uint32_t e = step % kWinInfoRing;
       wait(info_full(e), (step / kWinInfoRing) & 1u);
       const uint32_t f = info[3 * e].x;
       __syncwarp();
       if (elect_one()) mbar_arrive(info_empty(e));
       ++step;
-      if (!(f & (kStepStop | kStepEmpty))) it += 2;
-      s.f = (f >> (4 * g) & 15u) | (f & ~255u);            // this tile's bits at the bottom
-      return s;
+      return f;
     };
-    // S = Q K^T over the keys that matter, into buffer `buf`
-    auto issue_s = [&](const Pending& s, uint32_t buf) {
-      if (s.f & (kStepStop | kStepEmpty)) return;
-      const uint32_t slot = s.it % kWinRing;
-      wait(full_bar(slot), (s.it / kWinRing) & 1u);        // (a slot may only be given back once it was filled)
-      if (s.f & kStepNeeds) {
-        if (s.f & kStepFirst) {
-          wait(q_full(g), q_phase);
-          q_phase ^= 1u;
-        }
+    // S_g = Q_g K^T over the keys that matter, K in `slot` (which has landed)
+    auto issue_s = [&](int g, uint32_t f, uint32_t slot) {
+      const uint32_t t = f >> (4 * g);
+      if (!(t & kStepNeeds)) return;
+      if (t & kStepFirst) {
+        wait(q_full(g), (q_phase >> g) & 1u);
+        q_phase ^= 1u << g;
         tc_fence_after();
-        const uint64_t kd = k_desc0 + slot * kSlotUnits;
-        const uint32_t idesc = instr_desc_bf16(16 * (int)((s.f >> kStepGroups) & 15u));
-        if (elect_one()) {
+      }
+      const uint64_t qd = q_desc + g * kSlotUnits, kd = k_desc0 + slot * kSlotUnits;
+      const uint32_t idesc = instr_desc_bf16(16 * (int)((f >> kStepGroups) & 15u));
+      if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            tc_mma_bf16(s_tmem + 64u * buf, q_desc + (uint32_t)(k >> 2) * (kHalfBytes >> 4) + (uint32_t)(k & 3) * 2u,
-                        kd + (uint32_t)(k >> 2) * (kWinTileHalf >> 4) + (uint32_t)(k & 3) * 2u, idesc, k > 0);
-          tc_commit(s_full(g, buf));
-          tc_commit(empty_bar(slot));
-          if (s.f & kStepLast) tc_commit(q_empty(g));
+        for (int k = 0; k < 8; ++k) {
+          const uint32_t off = (uint32_t)(k >> 2) * (kHalfBytes >> 4) + (uint32_t)(k & 3) * 2u;
+          tc_mma_bf16(tmem_base + g * 128u, qd + off, kd + off, idesc, k > 0);
         }
-      } else if (elect_one()) {
-        mbar_arrive(empty_bar(slot));
+        tc_commit(s_full(g));
+        if (t & kStepLast) tc_commit(q_empty(g));
       }
       __syncwarp();
     };
-    // O (+)= P V with the weights in buffer `buf`
-    auto issue_pv = [&](const Pending& s, uint32_t buf) {
-      if (s.f & (kStepStop | kStepEmpty)) return;
-      const uint32_t at = s.it + 1, slot = at % kWinRing;
-      wait(full_bar(slot), (at / kWinRing) & 1u);
-      if (s.f & kStepNeeds) {
-        const uint32_t first = s.f & kStepFirst;
-        if (first) {
-          wait(o_empty(g), o_phase);
-          o_phase ^= 1u;
-        }
-        const uint64_t vd = v_desc0 + slot * kSlotUnits;
-        const int groups = (int)((s.f >> kStepGroups) & 15u);
-        wait(p_ready(g, buf), (p_phase >> buf) & 1u);
-        p_phase ^= 1u << buf;
-        tc_fence_after();
-        if (elect_one()) {
-          // 16 keys per product: 8 columns of P, 2048 bytes (128 units) of V
+    // O_g (+)= P_g V, V in `slot` (which has landed)
+    auto issue_pv = [&](int g, uint32_t f, uint32_t slot) {
+      const uint32_t t = f >> (4 * g);
+      if (!(t & kStepNeeds)) return;
+      const uint32_t first = t & kStepFirst;
+      if (first) {
+        wait(o_empty(g), (o_phase >> g) & 1u);
+        o_phase ^= 1u << g;
+      }
+      const uint64_t vd = v_desc0 + slot * kSlotUnits;
+      const int groups = (int)((f >> kStepGroups) & 15u);
+      const uint32_t o_tmem = tmem_base + 256u + g * 128u, p_tmem = tmem_base + g * 128u;
+      // 16 keys per product: 8 columns of P, 2048 bytes (128 units) of V
+      wait(p_ready(g, 0), (p_phase >> g) & 1u);
+      tc_fence_after();
+      if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (k < groups)
-              tc_mma_bf16_ts(o_tmem, s_tmem + 64u * buf + 8u * k, vd + 128u * k, idesc_pv, (!first || k > 0) ? 1u : 0u);
-          tc_commit(empty_bar(slot));
-          tc_commit(pv_done(g));
-          if (s.f & kStepLast) tc_commit(o_full(g));
-        }
-      } else if (elect_one()) {
-        mbar_arrive(empty_bar(slot));
+        for (int k = 0; k < 4; ++k)
+          if (k < groups) tc_mma_bf16_ts(o_tmem, p_tmem + 8u * k, vd + 128u * k, idesc_pv, (!first || k > 0) ? 1u : 0u);
       }
       __syncwarp();
+      wait(p_ready(g, 1), (p_phase >> g) & 1u);
+      tc_fence_after();
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 4; k < 8; ++k)
+          if (k < groups) tc_mma_bf16_ts(o_tmem, p_tmem + 8u * k, vd + 128u * k, idesc_pv, 1u);
+        if (t & kStepLast) tc_commit(o_full(g));
+      }
+      __syncwarp();
+      p_phase ^= 1u << g;
     };
-    Pending now = next_step(Pending{0u, 0u});
-    issue_s(now, 0);
-    Pending next = next_step(now);
-    issue_s(next, 1);
-    uint32_t buf = 0;
-    while ((ok = __all_sync(0xffffffffu, ok)) && !(now.f & kStepStop)) {
-      issue_pv(now, buf);
-      now = next;
-      next = next_step(now);
-      issue_s(next, buf);
-      buf ^= 1u;
+    auto landed = [&](uint32_t at) { wait(full_bar(at % kWinRing), (at / kWinRing) & 1u); };
+    auto release = [&](uint32_t at) {
+      if (elect_one()) tc_commit(empty_bar(at % kWinRing));
+      __syncwarp();
+    };
+    uint32_t f = next_step();
+    if (!(f & (kStepStop | kStepEmpty))) {
+      landed(it);
+      tc_fence_after();
+      issue_s(0, f, it % kWinRing);
+      issue_s(1, f, it % kWinRing);
+      release(it);
+    }
+    while ((ok = __all_sync(0xffffffffu, ok)) && !(f & kStepStop)) {
+      const uint32_t fn = next_step();
+      const bool now = !(f & kStepEmpty), then = !(fn & (kStepStop | kStepEmpty));
+      const uint32_t v_at = it + 1, k_at = now ? it + 2 : it;
+      if (now) landed(v_at);
+      if (then) landed(k_at);
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        if (now) issue_pv(g, f, v_at % kWinRing);
+        if (g == 1 && now) release(v_at);
+        if (then) issue_s(g, fn, k_at % kWinRing);
+      }
+      if (then) release(k_at);
+      it = k_at;
+      f = fn;
     }
     if (!ok) {
-      if (elect_one()) tc_commit(drain_bar(g));
+      if (elect_one()) tc_commit(drain_bar);
       __syncwarp();
       const unsigned long long t0 = global_ns();
-      while (!mbar_try_wait(drain_bar(g), 0) && global_ns() - t0 < a.wait_ns) {}
+      while (!mbar_try_wait(drain_bar, 0) && global_ns() - t0 < a.wait_ns) {}
     }
   } else {
     // ------------------------------------------------------------ softmax and output
@@ -415,8 +411,7 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const float sc = a.scale_log2;
     const uint64_t sc2 = pack2(sc, sc);
     uint32_t step = 0, tiles = 0;                          // steps seen; key tiles passed
-    uint32_t s_phase = 0, o_phase = 0;                     // (s_phase: a bit per buffer)
-    uint32_t products = 0;                                 // P V products of this tile so far (over all items)
+    uint32_t s_phase = 0, o_phase = 0;
     float top = -INFINITY, sum = 0.f;
     for (;; ++step) {
       const uint32_t e = step % kWinInfoRing;
@@ -429,7 +424,6 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       const uint32_t v_at = 2 * tiles + 1;                 // ring entry of this tile's V
       if (!(i0.x & kStepEmpty)) ++tiles;
       if (!(flags & (kStepNeeds | kStepZero))) continue;
-      const uint32_t buf = step & 1u, sb_addr = s_addr + 64u * buf;
       const int j0 = (int)i0.y, n = (int)i0.z;
       const int pos0 = (int)(g == 0 ? i2.x : i2.y), rows = (int)(g == 0 ? i2.z : i2.w);
       const int pos = pos0 + r, pos_lo = pos0 + quarter * 32;              // this row; the warp's first
@@ -438,19 +432,19 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         sum = 0.f;
       }
       if (flags & kStepNeeds) {
-        if (j0 + kWinKeys > n) {                           // value rows behind the sequence: cleared
+        if (j0 + kTileRows > n) {                          // value rows behind the sequence: cleared
           const uint32_t slot = v_at % kWinRing;
           if (!warp_wait(full_bar(slot), (v_at / kWinRing) & 1u, abort_flag, a.status, a.wait_ns)) break;
-          unsigned char* v = base_ptr + kWinSlot0 + slot * kWinTileBytes;
+          unsigned char* v = base_ptr + kWinSlot0 + slot * kSlotBytes;
           const int from = max(n - j0, 0);
-          for (int x = r; x < (kWinKeys - from) * 16; x += kTileRows) {
+          for (int x = r; x < (kTileRows - from) * 16; x += kTileRows) {
             const int row = from + (x >> 4), c = x & 15;
-            *reinterpret_cast<uint4*>(v + (c >> 3) * kWinTileHalf + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(v + (c >> 3) * kHalfBytes + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
-        if (!warp_wait(s_full(g, buf), (s_phase >> buf) & 1u, abort_flag, a.status, a.wait_ns)) break;
-        s_phase ^= 1u << buf;
+        if (!warp_wait(s_full(g), s_phase, abort_flag, a.status, a.wait_ns)) break;
+        s_phase ^= 1u;
         tc_fence_after();
         // What the warp's 32 rows see of each 32 keys: all, none, or some.  Tiles seen whole (most) run
         // without a branch.
@@ -460,25 +454,25 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         auto none_seen = [&](int k) {
           return k > pos_lo + 31 || (k >= a.num_sink && k + 31 <= pos_lo - a.window);
         };
-        const bool whole = all_seen(j0, kWinKeys);
-        float v[64];
+        const bool whole = all_seen(j0, kTileRows);
+        float v[128];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) tmem_ld32(sb_addr + 32 * c, *reinterpret_cast<float(*)[32]>(v + 32 * c));
+        for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, *reinterpret_cast<float(*)[32]>(v + 32 * c));
         tmem_ld_wait();
         float mx;
         if (whole) {
           float ext[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-          for (int e = 4; e < 60; e += 8)
+          for (int e = 4; e < 124; e += 8)
 #pragma unroll
             for (int j = 0; j < 4; ++j) ext[j] = max3(ext[j], v[e + 2 * j], v[e + 2 * j + 1]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) ext[j] = fmaxf(ext[j], v[60 + j]);
+          for (int j = 0; j < 4; ++j) ext[j] = fmaxf(ext[j], v[124 + j]);
           mx = fmaxf(fmaxf(ext[0], ext[1]), fmaxf(ext[2], ext[3]));
         } else {
           mx = -INFINITY;
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
+          for (int c = 0; c < 4; ++c) {
             const int k = j0 + 32 * c;
             if (none_seen(k)) continue;
             if (!all_seen(k, 32)) {
@@ -497,9 +491,7 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const bool move = tile_top > top + kWinSlack || top == -INFINITY;
         if (__any_sync(0xffffffffu, move)) {
           const float new_top = move ? fmaxf(top, tile_top) : top;
-          if (!(flags & kStepFirst)) {                     // rescale, once the previous product has retired
-            if (!warp_wait(pv_done(g), (products - 1u) & 1u, abort_flag, a.status, a.wait_ns)) break;
-            tc_fence_after();
+          if (!(flags & kStepFirst)) {                     // rescale (the previous product has retired)
             const float alpha = !move || new_top == -INFINITY ? 1.f : fast_exp2(top - new_top);
             sum *= alpha;
 #pragma unroll 1
@@ -538,28 +530,33 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             const __nv_bfloat162 b2 = __floats2bfloat162_rn(w0, w1);
             h[e] = *reinterpret_cast<const uint32_t*>(&b2);
           }
-          tmem_st16(sb_addr + 16 * c, h);
+          tmem_st16(s_addr + 16 * c, h);
+        };
+        auto hand_over = [&](int half) {                   // 64 keys' weights are in place
+          tmem_st_wait();
+          tc_fence_before();
+          mbar_arrive(p_ready(g, half));
         };
         if (whole) {
-          weights(0, std::true_type{});
-          weights(1, std::true_type{});
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            weights(c, std::true_type{});
+            if (c & 1) hand_over(c >> 1);
+          }
         } else {
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
+          for (int c = 0; c < 4; ++c) {
             if (none_seen(j0 + 32 * c)) {
               uint32_t h[16];
 #pragma unroll
               for (int e = 0; e < 16; ++e) h[e] = 0u;
-              tmem_st16(sb_addr + 16 * c, h);
+              tmem_st16(s_addr + 16 * c, h);
             } else {
               weights(c, std::false_type{});
             }
+            if (c & 1) hand_over(c >> 1);
           }
         }
-        tmem_st_wait();
-        tc_fence_before();
-        mbar_arrive(p_ready(g, buf));
-        ++products;
         float p0, p1;
         unpack2(add2(part[0], part[1]), p0, p1);
         sum += p0 + p1;
