@@ -31,8 +31,6 @@
 // beyond the sequence's end are cleared in shared memory by the softmax threads (a zero weight would
 // not stop a NaN).  All waits are bounded.
 #pragma once
-#include <type_traits>
-
 #include "attn_token.cuh"
 #include "umma_ptx.cuh"
 
@@ -44,7 +42,8 @@ bool rows_map(CUtensorMap* map, const void* base, int32_t batch, int32_t heads, 
 
 namespace umma {
 
-constexpr int kWinKeys = 128;
+constexpr int kWinKeys = 128;                              // keys of a step
+
 struct WindowArgs {
   const int32_t* seqlens;            // [batch] or nullptr
   const int32_t* q_lens;             // [batch] or nullptr
@@ -66,8 +65,8 @@ constexpr int kWinSoftmaxWarps = 8;
 constexpr int kWinRing = 4;
 constexpr int kWinQ = 0;                                   // Q of the two tiles
 constexpr int kWinSlot0 = 2 * kSlotBytes;
-constexpr int kWinStage = kWinSlot0 + kWinRing * kSlotBytes;         // 2 KB per softmax warp for its output
-constexpr int kWinBar = kWinStage + kWinSoftmaxWarps * 2048;
+constexpr int kWinStage = kWinSlot0 + kWinRing * kSlotBytes;         // 4 KB per softmax warp for its output
+constexpr int kWinBar = kWinStage + kWinSoftmaxWarps * 4096;
 constexpr int kWinInfoRing = 8;                            // steps described ahead
 constexpr int kWinDynamic = kWinBar + 1024 + 1024;
 constexpr int kWinTmemCols = 512;                          // S_A, S_B, O_A, O_B
@@ -96,28 +95,6 @@ struct WinTile {
   __device__ __forceinline__ int first() const { return sink_tiles > 0 ? 0 : lo; }
   __device__ __forceinline__ int last() const { return max(sink_tiles, hi > lo ? hi : 0) - 1; }
 };
-
-// 2^x for x <= 0 on the FMA pipe: x = i + f, |f| <= 1/2, 2^f by the polynomial of degree 4 with the
-// least greatest relative error there (Remez exchange: 2.6e-6), and i added to the exponent.
-__device__ __forceinline__ uint64_t exp2_poly2(uint64_t x2) {
-  float x0, x1;
-  unpack2(x2, x0, x1);
-  const uint64_t x = pack2(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
-  const uint64_t magic = pack2(12582912.f, 12582912.f);   // 1.5 * 2^23: adding it rounds to an integer
-  const uint64_t r = add2(x, magic);
-  const uint64_t f = sub2(x, sub2(r, magic));
-  uint64_t p = fma2(pack2(0x1.3997d6p-7f, 0x1.3997d6p-7f), f, pack2(0x1.ca1440p-5f, 0x1.ca1440p-5f));
-  p = fma2(p, f, pack2(0x1.ec06dap-3f, 0x1.ec06dap-3f));
-  p = fma2(p, f, pack2(0x1.62e0dcp-1f, 0x1.62e0dcp-1f));
-  p = fma2(p, f, pack2(0x1.ffffe8p-1f, 0x1.ffffe8p-1f));
-  float p0, p1, r0, r1;
-  unpack2(p, p0, p1);
-  unpack2(r, r0, r1);
-  return pack2(__int_as_float(__float_as_int(p0) + (__float_as_int(r0) << 23)),
-               __int_as_float(__float_as_int(p1) + (__float_as_int(r1) << 23)));
-}
-
-constexpr int kPolyEvery = 1000;        // every 4th pair of weights by polynomial
 
 // A wait that a whole warp makes together: false for all lanes when it ran out for one.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* status,
@@ -174,7 +151,7 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem_base = *tmem_holder;
+  constexpr uint32_t tmem_base = 0u;                       // all 512 columns are this CTA's: they begin at 0
 
   if (warp == kWinSoftmaxWarps + 1) {
     // ------------------------------------------------------------ the work, step by step, and its tiles
@@ -299,8 +276,9 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     constexpr uint32_t kSlotUnits = kSlotBytes >> 4;
     const uint64_t q_desc = smem_desc_sw128(base + kWinQ);
     const uint64_t k_desc0 = smem_desc_sw128(base + kWinSlot0), v_desc0 = smem_desc_mn_sw128(base + kWinSlot0);
-    uint32_t step = 0, it = 0;                             // steps described; ring entries passed (two a key tile)
+    uint32_t step = 0;                                     // steps described
     uint32_t q_phase = 0, p_phase = 0, o_phase = 3;        // a bit per query tile
+    uint32_t ring_phase = 0;                               // a bit per ring slot
     bool ok = true;                                        // the lanes agree on it at the end of each step
     auto wait = [&](uint32_t bar, uint32_t parity) { ok = mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns) && ok; };
     auto next_step = [&]() {                               // the flags of the step after this one
@@ -312,88 +290,86 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       ++step;
       return f;
     };
-    // S_g = Q_g K^T over the keys that matter, K in `slot` (which has landed)
-    auto issue_s = [&](int g, uint32_t f, uint32_t slot) {
-      const uint32_t t = f >> (4 * g);
-      if (!(t & kStepNeeds)) return;
-      if (t & kStepFirst) {
-        wait(q_full(g), (q_phase >> g) & 1u);
-        q_phase ^= 1u << g;
-        tc_fence_after();
-      }
-      const uint64_t qd = q_desc + g * kSlotUnits, kd = k_desc0 + slot * kSlotUnits;
-      const uint32_t idesc = instr_desc_bf16(16 * (int)((f >> kStepGroups) & 15u));
-      if (elect_one()) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t off = (uint32_t)(k >> 2) * (kHalfBytes >> 4) + (uint32_t)(k & 3) * 2u;
-          tc_mma_bf16(tmem_base + g * 128u, qd + off, kd + off, idesc, k > 0);
-        }
-        tc_commit(s_full(g));
-        if (t & kStepLast) tc_commit(q_empty(g));
-      }
+    auto landed = [&](uint32_t slot) { wait(full_bar(slot), (ring_phase >> slot) & 1u); ring_phase ^= 1u << slot; };
+    auto release = [&](uint32_t slot) {
+      if (elect_one()) tc_commit(empty_bar(slot));
       __syncwarp();
     };
-    // O_g (+)= P_g V, V in `slot` (which has landed)
-    auto issue_pv = [&](int g, uint32_t f, uint32_t slot) {
-      const uint32_t t = f >> (4 * g);
-      if (!(t & kStepNeeds)) return;
-      const uint32_t first = t & kStepFirst;
-      if (first) {
-        wait(o_empty(g), (o_phase >> g) & 1u);
-        o_phase ^= 1u << g;
-      }
-      const uint64_t vd = v_desc0 + slot * kSlotUnits;
-      const int groups = (int)((f >> kStepGroups) & 15u);
-      const uint32_t o_tmem = tmem_base + 256u + g * 128u, p_tmem = tmem_base + g * 128u;
-      // 16 keys per product: 8 columns of P, 2048 bytes (128 units) of V
-      wait(p_ready(g, 0), (p_phase >> g) & 1u);
-      tc_fence_after();
-      if (elect_one()) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (k < groups) tc_mma_bf16_ts(o_tmem, p_tmem + 8u * k, vd + 128u * k, idesc_pv, (!first || k > 0) ? 1u : 0u);
-      }
-      __syncwarp();
-      wait(p_ready(g, 1), (p_phase >> g) & 1u);
-      tc_fence_after();
-      if (elect_one()) {
-#pragma unroll
-        for (int k = 4; k < 8; ++k)
-          if (k < groups) tc_mma_bf16_ts(o_tmem, p_tmem + 8u * k, vd + 128u * k, idesc_pv, 1u);
-        if (t & kStepLast) tc_commit(o_full(g));
-      }
-      __syncwarp();
-      p_phase ^= 1u << g;
-    };
-    auto landed = [&](uint32_t at) { wait(full_bar(at % kWinRing), (at / kWinRing) & 1u); };
-    auto release = [&](uint32_t at) {
-      if (elect_one()) tc_commit(empty_bar(at % kWinRing));
-      __syncwarp();
-    };
-    uint32_t f = next_step();
-    if (!(f & (kStepStop | kStepEmpty))) {
-      landed(it);
-      tc_fence_after();
-      issue_s(0, f, it % kWinRing);
-      issue_s(1, f, it % kWinRing);
-      release(it);
-    }
+    auto real = [](uint32_t flags) { return !(flags & (kStepStop | kStepEmpty)); };
+    // One copy of the code of either product, in a rolled loop: unrolled over tiles and slots it fell out of
+    // the instruction cache, and a product took 100 cycles to issue instead of 64.
+    // What the loop needs besides products -- the flags of the step after the next, tiles that have to have
+    // landed -- is asked for between the batches of products, a little at a time: the pipe has work for
+    // the next two or three hundred cycles then.
+    uint32_t f = kStepEmpty, fn = next_step();             // this step's flags, the next one's
+    uint32_t parity = 0;                                   // K and V of this step are in slots 2 parity, 2 parity + 1
+#pragma unroll 1
     while ((ok = __all_sync(0xffffffffu, ok)) && !(f & kStepStop)) {
-      const uint32_t fn = next_step();
-      const bool now = !(f & kStepEmpty), then = !(fn & (kStepStop | kStepEmpty));
-      const uint32_t v_at = it + 1, k_at = now ? it + 2 : it;
-      if (now) landed(v_at);
-      if (then) landed(k_at);
-#pragma unroll
+      const bool now = real(f), then = real(fn);
+      const uint32_t v_slot = 2 * parity + 1, k_slot = now ? 2 - 2 * parity : 2 * parity;
+      const uint64_t vd = v_desc0 + v_slot * kSlotUnits, kd = k_desc0 + k_slot * kSlotUnits;
+      uint32_t f2 = fn;
+#pragma unroll 1
       for (int g = 0; g < 2; ++g) {
-        if (now) issue_pv(g, f, v_at % kWinRing);
-        if (g == 1 && now) release(v_at);
-        if (then) issue_s(g, fn, k_at % kWinRing);
+        const uint32_t t = f >> (4 * g), tn = fn >> (4 * g);
+        // O_g (+)= P_g V: 16 keys per product, 8 columns of P, 2048 bytes (128 units) of V
+        if (now && (t & kStepNeeds)) {
+          const int groups = (int)((f >> kStepGroups) & 15u);
+          const uint32_t o_tmem = tmem_base + 256u + g * 128u, p_tmem = tmem_base + g * 128u;
+          if (t & kStepFirst) {
+            wait(o_empty(g), (o_phase >> g) & 1u);
+            o_phase ^= 1u << g;
+          }
+          wait(p_ready(g, 0), (p_phase >> g) & 1u);
+          tc_fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (k < groups) tc_mma_bf16_ts(o_tmem, p_tmem + 8u * k, vd + 128u * k, idesc_pv, (k > 0 || !(t & kStepFirst)) ? 1u : 0u);
+          }
+          __syncwarp();
+          wait(p_ready(g, 1), (p_phase >> g) & 1u);
+          tc_fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 4; k < 8; ++k)
+              if (k < groups) tc_mma_bf16_ts(o_tmem, p_tmem + 8u * k, vd + 128u * k, idesc_pv, 1u);
+            if (t & kStepLast) tc_commit(o_full(g));
+          }
+          __syncwarp();
+          p_phase ^= 1u << g;
+        }
+        if (now && g == 1) release(v_slot);
+        if (then && g == 0) landed(k_slot);
+        // S_g = Q_g K^T of the next step, over the keys that matter
+        if (then && (tn & kStepNeeds)) {
+          if (tn & kStepFirst) {
+            wait(q_full(g), (q_phase >> g) & 1u);
+            q_phase ^= 1u << g;
+          }
+          tc_fence_after();
+          const uint64_t qd = q_desc + g * kSlotUnits;
+          const uint32_t idesc = instr_desc_bf16(16 * (int)((fn >> kStepGroups) & 15u));
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              const uint32_t off = (uint32_t)(k >> 2) * (kHalfBytes >> 4) + (uint32_t)(k & 3) * 2u;
+              tc_mma_bf16(tmem_base + g * 128u, qd + off, kd + off, idesc, k > 0);
+            }
+            tc_commit(s_full(g));
+            if (tn & kStepLast) tc_commit(q_empty(g));
+          }
+          __syncwarp();
+        }
+        if (g == 0 && !(fn & kStepStop)) f2 = next_step();
       }
-      if (then) release(k_at);
-      it = k_at;
+      if (then) {
+        release(k_slot);
+        landed(k_slot + 1);
+      }
+      if (now) parity ^= 1u;
       f = fn;
+      fn = f2;
     }
     if (!ok) {
       if (elect_one()) tc_commit(drain_bar);
@@ -459,34 +435,27 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, *reinterpret_cast<float(*)[32]>(v + 32 * c));
         tmem_ld_wait();
-        float mx;
-        if (whole) {
-          float ext[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-          for (int e = 4; e < 124; e += 8)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) ext[j] = max3(ext[j], v[e + 2 * j], v[e + 2 * j + 1]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) ext[j] = fmaxf(ext[j], v[124 + j]);
-          mx = fmaxf(fmaxf(ext[0], ext[1]), fmaxf(ext[2], ext[3]));
-        } else {
-          mx = -INFINITY;
+        if (!whole) {
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const int k = j0 + 32 * c;
-            if (none_seen(k)) continue;
-            if (!all_seen(k, 32)) {
-              // columns [lo, hi) are in the window, those below sk are sinks
-              auto below = [](int x) { return x >= 32 ? 0xffffffffu : (x <= 0 ? 0u : (1u << x) - 1u); };
-              const uint32_t see = below(pos + 1 - k) & (~below(pos + 1 - a.window - k) | below(a.num_sink - k));
+            if (all_seen(k, 32)) continue;
+            // columns [lo, hi) are in the window, those below sk are sinks
+            auto below = [](int x) { return x >= 32 ? 0xffffffffu : (x <= 0 ? 0u : (1u << x) - 1u); };
+            const uint32_t see = below(pos + 1 - k) & (~below(pos + 1 - a.window - k) | below(a.num_sink - k));
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (!(see & (1u << e))) v[32 * c + e] = -INFINITY;
-            }
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) mx = max3(mx, v[32 * c + e], v[32 * c + e + 1]);
+            for (int e = 0; e < 32; ++e)
+              if (!(see & (1u << e))) v[32 * c + e] = -INFINITY;
           }
         }
+        float ext[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+        for (int e = 4; e < 124; e += 8)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) ext[j] = max3(ext[j], v[e + 2 * j], v[e + 2 * j + 1]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ext[j] = fmaxf(ext[j], v[124 + j]);
+        const float mx = fmaxf(fmaxf(ext[0], ext[1]), fmaxf(ext[2], ext[3]));
         const float tile_top = mx * sc;
         const bool move = tile_top > top + kWinSlack || top == -INFINITY;
         if (__any_sync(0xffffffffu, move)) {
@@ -510,25 +479,15 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const float ref = top == -INFINITY ? 0.f : top;
         const uint64_t nref2 = pack2(-ref, -ref);
         uint64_t part[2] = {0ull, 0ull};
-        // (a masked logit has to give exactly 0, which the polynomial does not)
-        auto weights = [&](int c, auto poly) {
+        auto weights = [&](int c) {
           uint32_t h[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const uint64_t x2 = fma2(pack2(v[32 * c + 2 * e], v[32 * c + 2 * e + 1]), sc2, nref2);
-            uint64_t w2;
-            if (poly.value && e % kPolyEvery == kPolyEvery - 1) {
-              w2 = exp2_poly2(x2);
-            } else {
-              float x0, x1;
-              unpack2(x2, x0, x1);
-              w2 = pack2(fast_exp2(x0), fast_exp2(x1));
-            }
-            part[e & 1] = add2(part[e & 1], w2);
-            float w0, w1;
-            unpack2(w2, w0, w1);
-            const __nv_bfloat162 b2 = __floats2bfloat162_rn(w0, w1);
-            h[e] = *reinterpret_cast<const uint32_t*>(&b2);
+            float x0, x1;
+            unpack2(fma2(pack2(v[32 * c + 2 * e], v[32 * c + 2 * e + 1]), sc2, nref2), x0, x1);
+            const float w0 = fast_exp2(x0), w1 = fast_exp2(x1);
+            part[e & 1] = add2(part[e & 1], pack2(w0, w1));
+            h[e] = token::pack_bf16(w0, w1);
           }
           tmem_st16(s_addr + 16 * c, h);
         };
@@ -537,25 +496,17 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           tc_fence_before();
           mbar_arrive(p_ready(g, half));
         };
-        if (whole) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            weights(c, std::true_type{});
-            if (c & 1) hand_over(c >> 1);
+        for (int c = 0; c < 4; ++c) {
+          if (!whole && none_seen(j0 + 32 * c)) {
+            uint32_t h[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) h[e] = 0u;
+            tmem_st16(s_addr + 16 * c, h);
+          } else {
+            weights(c);
           }
-        } else {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (none_seen(j0 + 32 * c)) {
-              uint32_t h[16];
-#pragma unroll
-              for (int e = 0; e < 16; ++e) h[e] = 0u;
-              tmem_st16(s_addr + 16 * c, h);
-            } else {
-              weights(c, std::false_type{});
-            }
-            if (c & 1) hand_over(c >> 1);
-          }
+          if (c & 1) hand_over(c >> 1);
         }
         float p0, p1;
         unpack2(add2(part[0], part[1]), p0, p1);
@@ -571,43 +522,40 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);    // a NaN sum stays one
         const int b = (int)i0.w, hq = (int)(g == 0 ? i1.x : i1.y), row0 = (int)(g == 0 ? i1.z : i1.w);
         __nv_bfloat16* out = a.O + b * a.o_sb + hq * a.o_sh + (int64_t)(row0 + quarter * 32) * a.o_sn;
-        unsigned char* stage = base_ptr + kWinStage + warp * 2048;           // 32 rows of 64 bytes
+        unsigned char* stage = base_ptr + kWinStage + warp * 4096;           // 32 rows of 128 bytes
         const int live = rows - quarter * 32;
-#pragma unroll 1
-        for (int c0 = 0; c0 < 128; c0 += 32) {
-          float o[32];
-          if (any) {
-            tmem_ld32(o_addr + c0, o);
-            tmem_ld_wait();
-          } else {
+        float o[128];
+        if (any) {
 #pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] = 0.f;
-          }
-          // Rows go through shared memory, so that four lanes write 64 bytes of one row side by side
-          // (16-byte stores to 32 different rows took 8000 cycles a tile).  Two rows share 128 bytes, whose
-          // eight places are permuted against bank conflicts.
+          for (int c = 0; c < 4; ++c) tmem_ld32(o_addr + 32 * c, *reinterpret_cast<float(*)[32]>(o + 32 * c));
+          tmem_ld_wait();
+          tc_fence_before();
+          mbar_arrive(o_empty(g));                         // the next item's products may begin
+        } else {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint4 x;
-            x.x = token::pack_bf16(o[8 * c] * inv, o[8 * c + 1] * inv);
-            x.y = token::pack_bf16(o[8 * c + 2] * inv, o[8 * c + 3] * inv);
-            x.z = token::pack_bf16(o[8 * c + 4] * inv, o[8 * c + 5] * inv);
-            x.w = token::pack_bf16(o[8 * c + 6] * inv, o[8 * c + 7] * inv);
-            const int place = ((lane & 1) * 4 + c) ^ ((lane >> 1) & 7);
-            *reinterpret_cast<uint4*>(stage + (lane >> 1) * 128 + place * 16) = x;
+          for (int c = 0; c < 128; ++c) o[c] = 0.f;
+        }
+        // Rows go through shared memory, so that eight lanes write 128 bytes of one row side by side
+        // (16-byte stores to 32 different rows took 8000 cycles a tile); a row's eight places are permuted
+        // against bank conflicts.
+#pragma unroll
+        for (int c0 = 0; c0 < 128; c0 += 64) {
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            const float* x = o + c0 + 8 * c;
+            *reinterpret_cast<uint4*>(stage + lane * 128 + (c ^ (lane & 7)) * 16) =
+                make_uint4(token::pack_bf16(x[0] * inv, x[1] * inv), token::pack_bf16(x[2] * inv, x[3] * inv),
+                           token::pack_bf16(x[4] * inv, x[5] * inv), token::pack_bf16(x[6] * inv, x[7] * inv));
           }
           __syncwarp();
+          const int c = lane & 7;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int row = 8 * k + (lane >> 2), c = lane & 3, place = ((row & 1) * 4 + c) ^ ((row >> 1) & 7);
-            const uint4 x = *reinterpret_cast<const uint4*>(stage + (row >> 1) * 128 + place * 16);
+          for (int k = 0; k < 8; ++k) {
+            const int row = 4 * k + (lane >> 3);
+            const uint4 x = *reinterpret_cast<const uint4*>(stage + row * 128 + (c ^ (row & 7)) * 16);
             if (row < live) *reinterpret_cast<uint4*>(out + (int64_t)row * a.o_sn + c0 + 8 * c) = x;
           }
           __syncwarp();
-        }
-        if (any) {
-          tc_fence_before();
-          mbar_arrive(o_empty(g));
         }
         if (r < rows && a.lse != nullptr)
           a.lse[((int64_t)b * a.heads * a.group + hq) * a.q_rows + row0 + r] =
