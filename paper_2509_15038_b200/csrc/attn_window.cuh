@@ -7,24 +7,30 @@
 // same rows for even groups, neighbouring row blocks for a group of one.  Only the key tiles that some
 // row of the pair sees are walked: those holding sinks, then those of the window.
 //
-// Eleven warps.  Four softmax warps own each query tile, a thread per row: S = Q K^T arrives in TMEM,
+// Ten warps.  Four softmax warps own each query tile, a thread per row: S = Q K^T arrives in TMEM,
 // the thread takes its 128 logits into registers, and the weights go back over S as bf16, where they are
-// the A operand of O += P V straight from TMEM.  Each query tile has an issuing warp of its own, which
-// alternates P V of one key tile with S of the next: the two tiles run apart, and while one turns
-// logits into weights the tensor pipe works for the other.  P is handed over in halves, so that P V starts
-// on the first 64 keys.  The last warp walks the work: it feeds Q and the ring of K and V tiles by TMA and
-// describes every step (one key tile of one item) to the others in a small ring of its own.  Items follow
-// each other without a gap: the next pair's first S is issued right behind the last product of this one.
+// the A operand of O += P V straight from TMEM.  One issuing warp alternates P V of a key tile with S of
+// the next, tile by tile: while one query tile turns logits into weights the tensor pipe works for the
+// other.  P is handed over in halves, so that P V starts on the first 64 keys.  The last warp walks
+// the work: it feeds Q and the ring of K and V tiles by TMA and describes every step (one key tile of one
+// item) to the others in a small ring of its own.  Items follow each other without a gap: the next pair's
+// first S is issued right behind the last product of this one, and O is free again as soon as it is in
+// registers.
 //
-// An issuing warp has to be quick between its batches of products, or the pipe runs dry: it works
+// The issuing warp has to be quick between its batches of products, or the pipe runs dry: it works
 // converged with one elected lane issuing (inside `if (lane == 0)` the compiler cannot use uniform
-// registers, and a product beside busy softmax warps took 270 cycles to issue instead of 90).
-// Measured and dropped: two threads per row (a tile's softmax 2650 cycles against 1700, the warps crowding
-// each other out); one issuing warp for both tiles (it waits for one while the other is ready).
+// registers, and a product beside busy softmax warps took 270 cycles to issue instead of 90), in one rolled
+// loop with little code.  Measured and dropped: two threads per row (a tile's softmax 2650 cycles against
+// 1700, the warps crowding each other out); an issuing warp per query tile (194 us where this takes 180);
+// 64-key steps; every other pair of exponentials as a polynomial on the FMA pipe (no change: the
+// special function units are not what is waited for).
 //
-// What bounds it: 128 x 128 keys cost the tensor pipe 1024 cycles (two products of 512) and the
-// exponentials of the tile 1024 cycles of the special function units, so every kPolyEvery-th pair of
-// weights is formed on the FMA pipe instead (a minimax polynomial of degree 4).
+// What bounds it: the tensor pipe's issue.  A step of 128 keys is 32 products of 64 cycles for the two tiles,
+// 2048 cycles, and 1024 cycles of the special function units; it takes 3500 to 3900, with or without the softmax
+// between, since a product is issued every 95 cycles here and the waits between the batches come on top.  A
+// change of items costs 4000 cycles (the last product, O through registers, the first S of the next) every
+// nine steps at window 1024.  8192 tokens, 32 / 8 heads, window 1024: 180 us, 718 TFLOP/s over the visible
+// keys; 4 prompts of up to 2000 tokens, window 512: 74 us.
 //
 // The running maximum moves only when a tile exceeds it by more than 2^8 (as in attn_umma.cuh); the
 // group then rescales its accumulator in TMEM, which after the first tiles is rare.  Value rows at or
@@ -38,11 +44,9 @@ namespace curdkv {
 
 // Map of a bf16 tensor [batch][heads][rows][128] for tiles of 128 rows (defined beside the C ABI).
 bool rows_map(CUtensorMap* map, const void* base, int32_t batch, int32_t heads, int32_t rows, int64_t stride_b,
-              int64_t stride_h, int64_t stride_n, int32_t tile_rows);
+              int64_t stride_h, int64_t stride_n);
 
 namespace umma {
-
-constexpr int kWinKeys = 128;                              // keys of a step
 
 struct WindowArgs {
   const int32_t* seqlens;            // [batch] or nullptr

@@ -86,9 +86,9 @@ EncodeTiledFn encode_tiled_fn() {
 }
 
 // bf16 tensor [batch][heads][n_max][128] -> 4-D map (channel, row, head, batch) with a
-// box of 64 channels x tile_rows rows and the 128-byte swizzle the MMA descriptors expect.
+// box of 64 channels x 128 rows and the 128-byte swizzle the MMA descriptors expect.
 bool make_tile_map(CUtensorMap* map, const void* base, const curdkv_desc* d, int64_t sb, int64_t sh,
-                   int64_t sn, int32_t tile_rows = kTileRows) {
+                   int64_t sn) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (fn == nullptr) return false;
   const cuuint64_t dims[4] = {(cuuint64_t)d->d, (cuuint64_t)d->n_max, (cuuint64_t)d->kv_heads,
@@ -97,7 +97,7 @@ bool make_tile_map(CUtensorMap* map, const void* base, const curdkv_desc* d, int
   const cuuint64_t row = (cuuint64_t)sn * 2;
   const cuuint64_t strides[3] = {row, d->kv_heads > 1 ? (cuuint64_t)sh * 2 : row,
                                  d->batch > 1 ? (cuuint64_t)sb * 2 : row};
-  const cuuint32_t box[4] = {64, (cuuint32_t)tile_rows, 1, 1};
+  const cuuint32_t box[4] = {64, (cuuint32_t)kTileRows, 1, 1};
   const cuuint32_t estr[4] = {1, 1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box,
             estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
@@ -245,13 +245,13 @@ namespace curdkv {
 void count_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
 
 bool rows_map(CUtensorMap* map, const void* base, int32_t batch, int32_t heads, int32_t rows, int64_t stride_b,
-              int64_t stride_h, int64_t stride_n, int32_t tile_rows) {
+              int64_t stride_h, int64_t stride_n) {
   curdkv_desc d = {};
   d.batch = batch;
   d.kv_heads = heads;
   d.n_max = rows;
   d.d = 128;
-  return make_tile_map(map, base, &d, stride_b, stride_h, stride_n, tile_rows);
+  return make_tile_map(map, base, &d, stride_b, stride_h, stride_n);
 }
 
 curdkv_status check_call(const void* K, const void* V, const curdkv_desc* desc) {

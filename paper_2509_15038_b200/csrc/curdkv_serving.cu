@@ -153,14 +153,30 @@ bool launch_attend(const token::Args& a, cudaStream_t stream) {
 }
 
 // The prompt form reads its tensors through TMA maps, whose strides must be positive and below 2^40
-// bytes (where the axis is longer than one).
+// bytes (where the axis is longer than one); the token form takes the others.
 bool map_strides_ok(int64_t batch, int64_t heads, int64_t rows, int64_t sb, int64_t sh, int64_t sn) {
   const int64_t most = (int64_t)1 << 38;
   return (batch <= 1 || (sb > 0 && sb < most)) && (heads <= 1 || (sh > 0 && sh < most)) && (rows <= 1 || sn < most);
 }
 
-// Query rows per KV head from which the prompt form is taken: see window_form.
-constexpr int kPromptRows = 64;
+// Which form of the window attention a call takes: the one whose slowest SM is estimated to end first.
+// Measured: the token form needs 12.3 ns per key for 16 query rows of a KV head on one SM, plus the time of 64
+// keys, and spreads its work evenly; the prompt form 15.6 ns per key for a pair of 128-row tiles, full or not,
+// plus the time of some 320 keys (tiles partly outside the window, the start of an item), and takes whole
+// rounds of a pair per SM.  In us, token | prompt, rows = query rows per KV head, at the sizes around the
+// change from one to the other:
+//   16 x 8 heads, 8192 keys, window 8192, 32 / 64 / 128 rows         177 | 315    347 | 318    601 | 320
+//   16 x 8 heads, window 1024, 32 / 64 / 128 rows                     35 | 56      57 | 56     101 | 56
+//   16 x 8 heads, 512 keys, window 256, 64 / 128 rows                 21 | 29      39 | 29
+//    4 x 8 heads, 8192 keys, window 8192, 64 / 128 / 256 rows         76 | 121    135 | 121    267 | 147
+//    1 x 8 heads, 8192 keys, window 8192, 256 rows                    75 | 143    (the pairs fill few SMs)
+//   64 x 8 heads, 512 keys, window 256, 128 / 256 rows               133 | 160    258 | 160
+bool prompt_form(int64_t problems, int64_t rows, int64_t pairs, int64_t window_keys, int64_t n_max) {
+  const int64_t keys = window_keys < n_max ? window_keys : n_max;
+  const double token = 12.3 * (double)(problems * ((rows + 15) / 16)) / sms() * (double)(keys + 64);
+  const double prompt = 15.6 * (double)((problems * pairs + sms() - 1) / sms()) * (double)(keys + 320);
+  return prompt < token;
+}
 
 bool query_strides_ok(const void* x, int64_t sb, int64_t sh, int64_t sn) {
   return x != nullptr && aligned16(x) && sb >= 0 && sh >= 0 && sn >= 128 && sb % 8 == 0 && sh % 8 == 0 && sn % 8 == 0;
@@ -329,16 +345,16 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
   const int group = desc->q_heads / desc->kv_heads;
   // a masked product is -inf, and -inf times a scale of 0 would be NaN
   const float scale_log2 = scale * 1.4426950408889634f > 1e-30f ? scale * 1.4426950408889634f : 1e-30f;
-  if ((int64_t)group * q_rows >= kPromptRows && desc->n_max > 0 && (int64_t)desc->n_max + q_rows < (1 << 30) &&
+  const int64_t pairs = (((int64_t)q_rows + kTileRows - 1) / kTileRows * group + 1) / 2;
+  if (desc->n_max > 0 && (int64_t)desc->n_max + q_rows < (1 << 30) && P * pairs <= 0x3fffffffLL &&
+      prompt_form(P, (int64_t)group * q_rows, pairs, (int64_t)window + num_sink, desc->n_max) &&
       map_strides_ok(desc->batch, desc->kv_heads, desc->n_max, desc->k_stride_b, desc->k_stride_h, desc->k_stride_n) &&
       map_strides_ok(desc->batch, desc->kv_heads, desc->n_max, desc->v_stride_b, desc->v_stride_h, desc->v_stride_n) &&
       map_strides_ok(desc->batch, desc->q_heads, q_rows, q_stride_b, q_stride_h, q_stride_n)) {
     CUtensorMap mq, mk, mv;
-    if (!rows_map(&mq, Q, desc->batch, desc->q_heads, q_rows, q_stride_b, q_stride_h, q_stride_n, kTileRows) ||
-        !rows_map(&mk, K, desc->batch, desc->kv_heads, desc->n_max, desc->k_stride_b, desc->k_stride_h, desc->k_stride_n,
-                  umma::kWinKeys) ||
-        !rows_map(&mv, V, desc->batch, desc->kv_heads, desc->n_max, desc->v_stride_b, desc->v_stride_h, desc->v_stride_n,
-                  umma::kWinKeys))
+    if (!rows_map(&mq, Q, desc->batch, desc->q_heads, q_rows, q_stride_b, q_stride_h, q_stride_n) ||
+        !rows_map(&mk, K, desc->batch, desc->kv_heads, desc->n_max, desc->k_stride_b, desc->k_stride_h, desc->k_stride_n) ||
+        !rows_map(&mv, V, desc->batch, desc->kv_heads, desc->n_max, desc->v_stride_b, desc->v_stride_h, desc->v_stride_n))
       return CURDKV_ERR_CUDA;
     umma::WindowArgs wa = {};
     wa.seqlens = desc->seqlens;
@@ -356,8 +372,6 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
     wa.lse = lse;
     wa.status = static_cast<uint32_t*>(workspace);
     wa.wait_ns = umma::kWaitLimitNs;
-    const int64_t pairs = (((int64_t)q_rows + kTileRows - 1) / kTileRows * group + 1) / 2;
-    if (P * pairs > 0x3fffffffLL) return CURDKV_ERR_UNSUPPORTED;
     wa.pairs = (int)pairs;
     wa.items = (int)(P * pairs);
     static std::atomic<uint64_t> done{0};

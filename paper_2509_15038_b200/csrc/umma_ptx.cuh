@@ -57,31 +57,6 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
   }
 }
-// The same wait for kernels in which many warps wait beside others that work: the hardware parks the
-// thread for up to a millisecond a try, so that waiting takes no issue slots from the working warps.
-__device__ __forceinline__ bool mbar_park(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* status,
-                                          unsigned long long limit_ns) {
-  unsigned long long t0 = 0;
-  for (;;) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity), "r"(1000000u)
-        : "memory");
-    if (ok != 0) return true;
-    if (*abort_flag) return false;
-    const unsigned long long now = global_ns();
-    if (t0 == 0) t0 = now;
-    if (now - t0 > limit_ns) {
-      *abort_flag = 1;
-      flag_status(status, CURDKV_DEV_TIMEOUT);
-      return false;
-    }
-  }
-}
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar,
                                             int c0, int c1, int c2, int c3, uint64_t policy) {
   asm volatile(

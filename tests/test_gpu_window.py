@@ -200,3 +200,111 @@ def test_parts_join_by_their_log_sums():
         vp = np.concatenate([vp, np.abs(_f64(V)[0, h, n_old:])])
         want, _, wt = orc.attend(_f64(Q)[0, h], k, v, np.ones((1, k.shape[0]), bool), float(np.float32(0.1)))
         assert np.all(np.abs(joined[0, h] - want) <= (2.0 ** -8 + 2.0 ** -8 + 2.0 ** -12) * (wt @ vp) * (1 + 2.0 ** -7))
+
+
+# Prompts over enough heads that the tensor-core form for prompts is taken (few heads and short windows
+# take the form for few query rows, which the tests above cover).
+HEADS = [0, 13, 31]                                        # query heads that are compared
+
+
+@pytest.mark.parametrize("t", [129, 300, 700])
+@pytest.mark.parametrize("window,sink", [(64, 4), (128, 0), (129, 130), (333, 1), (5000, 0), (0, 300)])
+def test_prompts_over_many_heads(t, window, sink):
+    _run(3, 8, 4, 700, t, window, sink, lens=[700, 650, 90], q_lens=[t, t - 37, 90], seed=130, heads=HEADS)
+
+
+@pytest.mark.parametrize("window,sink", [(1, 0), (2, 1), (0, 3), (0, 0)])
+def test_long_prompts_that_see_little(window, sink):
+    _run(3, 16, 4, 1200, 1200, window, sink, lens=[1200, 0, 1], q_lens=[1200, 1200, 1200], seed=135, heads=[0, 63])
+
+
+@pytest.mark.parametrize("B,H,group,n,t", [(30, 9, 1, 300, 300), (12, 8, 3, 260, 260), (3, 8, 8, 129, 129), (64, 8, 1, 200, 200),
+                                          (8, 8, 4, 64, 64), (8, 8, 4, 127, 90), (3, 16, 4, 1500, 200), (40, 8, 16, 40, 20)])
+def test_prompt_shapes_over_many_heads(B, H, group, n, t):
+    lens = [max(1, n - 41) if b % 2 else n for b in range(B)]
+    _run(B, H, group, n, t, 100, 4, lens=lens, q_lens=[max(1, min(t, x)) for x in lens], seed=140, heads=[0, H * group - 1])
+
+
+def test_prompts_with_rows_behind_the_sequence_that_hold_anything():
+    K, V = _rand((3, 8, 512, 128), 150), _rand((3, 8, 512, 128), 151)
+    lens = [300, 257, 512]
+    for b, n in enumerate(lens):
+        K[b, :, n:] = float("nan")
+        V[b, :, n:] = float("inf")
+    _run(3, 8, 4, 512, 250, 100, 4, lens=lens, K=K, V=V, seed=152, heads=HEADS)
+
+
+def test_prompts_with_strides_and_views():
+    B, H, group, n, t = 3, 8, 4, 400, 300
+    K, V = (_rand((B, n, H, 128), 160 + i).transpose(1, 2) for i in range(2))
+    Q = _rand((B, t, H * group, 128), 162).transpose(1, 2)
+    desc = cur.make_desc(K, V, 1, q_heads=H * group)
+    buf = torch.full((B, t, H * group, 136), 5.0, dtype=torch.bfloat16, device=DEV)
+    O = buf[..., :128].transpose(1, 2)
+    lse = torch.zeros((B, H * group, t), device=DEV)
+    cur.curdkv_attention_window(Q, K, V, desc, 90, num_sink=4, scale=0.1, O=O, lse=lse)
+    _check(O, lse, Q, K, V, [n] * B, [t] * B, 90, 4, float(np.float32(0.1)), heads=HEADS)
+    assert torch.all(buf[..., 128:] == 5.0)
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+def test_prompts_with_logits_that_grow_or_shrink(sign):
+    H, n, t = 8, 1200, 700
+    ramp = torch.linspace(0, 1, n, device=DEV)
+    K = _rand((2, H, n, 128), 170, 0.2).float()
+    K[..., 0] = 40 * (ramp if sign > 0 else 1 - ramp)
+    K = K.to(torch.bfloat16)
+    V = _rand((2, H, n, 128), 171)
+    Q = _rand((2, 4 * H, t, 128), 172, 0.2).float()
+    Q[..., 0] += 3
+    Q = Q.to(torch.bfloat16)
+    desc = cur.make_desc(K, V, 1, q_heads=4 * H)
+    lse = torch.zeros((2, 4 * H, t), device=DEV)
+    for scale, window in ((1.0, 5000), (1.0, 700), (0.0, 700)):
+        O, ws = cur.curdkv_attention_window(Q, K, V, desc, window, num_sink=3, scale=scale, lse=lse)
+        assert cur.curdkv_device_status(ws) == 0
+        _check(O, lse, Q, K, V, [n, n], [t, t], window, 3, scale, heads=[0, 31], what=f"{sign} {scale} {window}")
+
+
+@pytest.mark.parametrize("t", [1, 300])
+def test_heads_and_sequences_that_share_their_rows(t):
+    """K and V broadcast over sequences and KV heads (strides of zero), as beams over one prompt have them."""
+    B, H, group, n = 3, 8, 4, 400
+    K, V = (_rand((1, 1, n, 128), 180 + i).expand(B, H, n, 128) for i in range(2))
+    _run(B, H, group, n, t, 150, 4, K=K, V=V, seed=182, heads=HEADS)
+
+
+def test_prompts_replayed_and_beside_another_call():
+    """A captured call replayed with other rows and lengths, while another prompt runs on a second stream with a workspace of
+    its own."""
+    B, H, group, n, t, window, sink = 3, 8, 4, 1500, 300, 300, 4
+    K, V = _rand((B, H, n, 128), 190), _rand((B, H, n, 128), 191)
+    lens = torch.tensor([1400, 900, 10], dtype=torch.int32, device=DEV)
+    desc = cur.make_desc(K, V, 1, q_heads=H * group, seqlens=lens)
+    Q = _rand((B, H * group, t, 128), 192)
+    O, lse = torch.zeros_like(Q), torch.zeros(Q.shape[:3], device=DEV)
+    ws = cur.attention_window_workspace(desc, t)
+    call = lambda: cur.curdkv_attention_window(Q, K, V, desc, window, num_sink=sink, scale=0.1, O=O, lse=lse, workspace=ws)  # noqa: E731
+    call()
+    other = (_rand((2, H, 800, 128), 193), _rand((2, H, 800, 128), 194))
+    od = cur.make_desc(*other, 1, q_heads=H * group)
+    oq = _rand((2, H * group, 700, 128), 195)
+    oo, ows = torch.zeros_like(oq), cur.attention_window_workspace(od, 700)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    side = torch.cuda.Stream()
+    for i in range(3):
+        K.copy_(_rand(K.shape, 200 + i))
+        Q.copy_(_rand(Q.shape, 210 + i))
+        now = [1400 + i, 900 - 300 * i, 10 + i]
+        lens.copy_(torch.tensor(now, dtype=torch.int32))
+        oo.zero_()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            cur.curdkv_attention_window(oq, *other, od, 100, scale=0.1, O=oo, workspace=ows)
+        graph.replay()
+        torch.cuda.current_stream().wait_stream(side)
+        _check(O, lse, Q, K, V, now, [t] * B, window, sink, float(np.float32(0.1)), heads=[0, 31])
+        _check(oo, None, oq, *other, [800, 800], [700, 700], 100, 0, float(np.float32(0.1)), heads=[5])
+    assert cur.curdkv_device_status(ws) == 0 and cur.curdkv_device_status(ows) == 0
