@@ -439,8 +439,9 @@ curdkv_status curdkv_qcache_attention(const void* Q, int32_t q_rows, int64_t q_s
  *   lse       NULL, or fp32 [batch][q_heads][q_rows], as above
  *   scale     finite, >= 0
  * A query that sees nothing (window = 0 without sinks, or a position below 0 because t_b > n_b)
- * gives O = 0 and lse = -inf.  Rows at or beyond n_b are never used, whatever they hold; rows below it
- * must be finite.  Softmax and sums in fp32, weights rounded to bf16 before they multiply the values,
+ * gives O = 0 and lse = -inf.  Rows that no query of the sequence sees (at or beyond n_b, or older than
+ * the first query's window and no sinks) are never used, whatever they hold; the others must be finite.
+ * Softmax and sums in fp32, weights rounded to bf16 before they multiply the values,
  * O rounded once.  d = 128.  workspace as in curdkv_qcache_attention. */
 size_t curdkv_attention_window_workspace_bytes(const curdkv_desc* desc, int32_t q_rows);
 curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h,

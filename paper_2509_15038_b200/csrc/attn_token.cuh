@@ -194,7 +194,7 @@ struct Item {
       pos0 = n - q_live;
       const int i0 = r0 / a.group, i1 = min((r1 - 1) / a.group, q_live - 1);   // tokens of the block
       const int hi = i1 >= i0 ? max(pos0 + i1 + 1, 0) : 0; // keys [0, hi) may be seen
-      const int lo = (int)min((int64_t)hi, max((int64_t)0, (int64_t)pos0 + i0 + 1 - a.window));
+      const int lo = a.window > 0 ? (int)min((int64_t)hi, max((int64_t)0, (int64_t)pos0 + i0 + 1 - a.window)) : hi;
       seen.sinks = min(a.num_sink, lo);
       seen.first = lo;
       seen.total = seen.sinks + hi - lo;

@@ -33,9 +33,7 @@
 // keys; 4 prompts of up to 2000 tokens, window 512: 74 us.
 //
 // The running maximum moves only when a tile exceeds it by more than 2^8 (as in attn_umma.cuh); the
-// group then rescales its accumulator in TMEM, which after the first tiles is rare.  Value rows at or
-// beyond the sequence's end are cleared in shared memory by the softmax threads (a zero weight would
-// not stop a NaN).  All waits are bounded.
+// group then rescales its accumulator in TMEM, which after the first tiles is rare.  All waits are bounded.
 #pragma once
 #include "attn_token.cuh"
 #include "umma_ptx.cuh"
@@ -412,14 +410,19 @@ window_umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         sum = 0.f;
       }
       if (flags & kStepNeeds) {
-        if (j0 + kTileRows > n) {                          // value rows behind the sequence: cleared
+        // Value rows that no query of the sequence sees -- behind its end, or older than its first query's
+        // window and no sinks -- are cleared: a weight of zero would not stop a NaN.
+        const int first_pos = pos0 - (int)(g == 0 ? i1.z : i1.w);
+        const int old = a.window > 0 ? min(n, max(first_pos + 1 - a.window, 0)) : n;       // keys [num_sink, old)
+        const int used = 16 * (int)((i0.x >> kStepGroups) & 15u);            // rows of the tile that are multiplied
+        if (j0 + used > n || (j0 < old && j0 + used > a.num_sink)) {
           const uint32_t slot = v_at % kWinRing;
           if (!warp_wait(full_bar(slot), (v_at / kWinRing) & 1u, abort_flag, a.status, a.wait_ns)) break;
           unsigned char* v = base_ptr + kWinSlot0 + slot * kSlotBytes;
-          const int from = max(n - j0, 0);
-          for (int x = r; x < (kTileRows - from) * 16; x += kTileRows) {
-            const int row = from + (x >> 4), c = x & 15;
-            *reinterpret_cast<uint4*>(v + (c >> 3) * kHalfBytes + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          for (int x = r; x < used * 16; x += kTileRows) {
+            const int row = x >> 4, c = x & 15, key = j0 + row;
+            if (key >= n || (key >= a.num_sink && key < old))
+              *reinterpret_cast<uint4*>(v + (c >> 3) * kHalfBytes + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }

@@ -153,10 +153,10 @@ bool launch_attend(const token::Args& a, cudaStream_t stream) {
 }
 
 // The prompt form reads its tensors through TMA maps, whose strides must be positive and below 2^40
-// bytes (where the axis is longer than one); the token form takes the others.
-bool map_strides_ok(int64_t batch, int64_t heads, int64_t rows, int64_t sb, int64_t sh, int64_t sn) {
+// bytes (for sequences and heads: where there are several); the token form takes the others.
+bool map_strides_ok(int64_t batch, int64_t heads, int64_t sb, int64_t sh, int64_t sn) {
   const int64_t most = (int64_t)1 << 38;
-  return (batch <= 1 || (sb > 0 && sb < most)) && (heads <= 1 || (sh > 0 && sh < most)) && (rows <= 1 || sn < most);
+  return (batch <= 1 || (sb > 0 && sb < most)) && (heads <= 1 || (sh > 0 && sh < most)) && sn < most;
 }
 
 // Which form of the window attention a call takes: the one whose slowest SM is estimated to end first.
@@ -348,9 +348,9 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
   const int64_t pairs = (((int64_t)q_rows + kTileRows - 1) / kTileRows * group + 1) / 2;
   if (desc->n_max > 0 && (int64_t)desc->n_max + q_rows < (1 << 30) && P * pairs <= 0x3fffffffLL &&
       prompt_form(P, (int64_t)group * q_rows, pairs, (int64_t)window + num_sink, desc->n_max) &&
-      map_strides_ok(desc->batch, desc->kv_heads, desc->n_max, desc->k_stride_b, desc->k_stride_h, desc->k_stride_n) &&
-      map_strides_ok(desc->batch, desc->kv_heads, desc->n_max, desc->v_stride_b, desc->v_stride_h, desc->v_stride_n) &&
-      map_strides_ok(desc->batch, desc->q_heads, q_rows, q_stride_b, q_stride_h, q_stride_n)) {
+      map_strides_ok(desc->batch, desc->kv_heads, desc->k_stride_b, desc->k_stride_h, desc->k_stride_n) &&
+      map_strides_ok(desc->batch, desc->kv_heads, desc->v_stride_b, desc->v_stride_h, desc->v_stride_n) &&
+      map_strides_ok(desc->batch, desc->q_heads, q_stride_b, q_stride_h, q_stride_n)) {
     CUtensorMap mq, mk, mv;
     if (!rows_map(&mq, Q, desc->batch, desc->q_heads, q_rows, q_stride_b, q_stride_h, q_stride_n) ||
         !rows_map(&mk, K, desc->batch, desc->kv_heads, desc->n_max, desc->k_stride_b, desc->k_stride_h, desc->k_stride_n) ||

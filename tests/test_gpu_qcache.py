@@ -407,3 +407,59 @@ def test_long_cache_offsets_pass_32_bits():
     lse_s = torch.zeros((1, 1, 2), device=DEV)
     cur.curdkv_qcache_attention(Q[:, 8:], small, scale=0.1, lse=lse_s)
     _check_attention(O[:, 8:], lse[:, 8:], Q[:, 8:], small, [50], [0], float(np.float32(0.1)))
+
+
+def test_store_and_read_the_same_index_more_than_once():
+    B, H, n = 2, 2, 90
+    K, V = _rand((B, H, n, 128), 400), _rand((B, H, n, 128), 401)
+    rng = np.random.default_rng(5)
+    idx = torch.from_numpy(np.concatenate([rng.integers(0, n, (B, H, 50)), np.full((B, H, 20), 7)], -1).astype(np.int32)).to(DEV)
+    cache = cur.QuantCache(B, H, 80)
+    ws = torch.zeros(256, dtype=torch.uint8, device=DEV)
+    counts = torch.full((B * H,), 70, dtype=torch.int32, device=DEV)
+    cur.curdkv_qcache_store(cache, K, V, cur.make_desc(K, V, 1), idx, counts, workspace=ws)
+    take = lambda x: np.take_along_axis(_f64(x), idx.cpu().numpy()[..., None].astype(np.int64), 2).reshape(-1, 128)  # noqa: E731
+    _check_rows(cache, np.concatenate([np.arange(70) + 80 * p for p in range(B * H)]), (take(K), take(V)))
+    again = torch.tensor([69, 0, 69, -1, 69], dtype=torch.int32, device=DEV).expand(B, H, 5).contiguous()
+    k, v = cur.curdkv_qcache_read(cache, again, workspace=ws)
+    assert cur.curdkv_device_status(ws) == 0
+    assert torch.equal(k[:, :, 0], k[:, :, 2]) and torch.equal(v[:, :, 0], v[:, :, 4]) and not k[:, :, 3].any()
+
+
+def test_attention_calls_side_by_side():
+    """Two streams, two caches, a workspace each: the same results as one after the other; and a call that follows an
+    append on its own stream sees the new row."""
+    sets = []
+    for i in range(2):
+        B, H, n = 3, 8, 3000 + 500 * i
+        K, V = _rand((B, H, n, 128), 410 + 2 * i), _rand((B, H, n, 128), 411 + 2 * i)
+        cache = cur.QuantCache(B, H, n + 40)
+        cur.curdkv_qcache_store(cache, K, V, cur.make_desc(K, V, 1))
+        Q = _rand((B, H, 4, 128), 420 + i, 0.3)
+        sets.append((cache, Q, torch.empty_like(Q), cur.qcache_attention_workspace(cache, 4), torch.cuda.Stream()))
+    run = lambda s: cur.curdkv_qcache_attention(s[1], s[0], scale=0.1, O=s[2], workspace=s[3])  # noqa: E731
+    alone = []
+    for s in sets:
+        run(s)
+        alone.append(s[2].clone())
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for s in sets:
+            with torch.cuda.stream(s[4]):
+                run(s)
+    torch.cuda.synchronize()
+    for s, want in zip(sets, alone):
+        assert torch.equal(s[2], want)
+        assert cur.curdkv_device_status(s[3]) == 0
+    cache, Q, O, ws, stream = sets[0]
+    with torch.cuda.stream(stream):
+        big = torch.zeros((3, 8, 1, 128), device=DEV)
+        big += 20 * torch.sign(Q[:, :, :1].float())
+        big[..., 3] = 0
+        new = big.to(torch.bfloat16)
+        cur.curdkv_qcache_append(cache, new, torch.full_like(new, 5.0))
+        run(sets[0])
+    torch.cuda.synchronize()
+    # a key of 20 sign(q) has logits of 2 sum |q|, some 60 above every other: its value, 5, is the answer of query 0 to
+    # within the weight of the others (exp(-20) each at most) and the roundings to fp16 and bf16
+    assert torch.all((O[:, :, 0].float() - 5.0).abs() <= 5.0 * (2.0 ** -8 + 2.0 ** -10))

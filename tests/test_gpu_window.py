@@ -308,3 +308,30 @@ def test_prompts_replayed_and_beside_another_call():
         _check(O, lse, Q, K, V, now, [t] * B, window, sink, float(np.float32(0.1)), heads=[0, 31])
         _check(oo, None, oq, *other, [800, 800], [700, 700], 100, 0, float(np.float32(0.1)), heads=[5])
     assert cur.curdkv_device_status(ws) == 0 and cur.curdkv_device_status(ows) == 0
+
+
+@pytest.mark.parametrize("B,H,group,t", [(2, 2, 2, 1), (2, 2, 2, 7), (3, 8, 4, 250)])
+@pytest.mark.parametrize("window,sink", [(100, 4), (0, 5), (0, 0), (33, 130), (300, 0)])
+def test_rows_that_no_query_sees_hold_anything(B, H, group, t, window, sink):
+    """Old rows that have left the first query's window, as a cache that drops them leaves them."""
+    n = 700
+    K, V = _rand((B, H, n, 128), 220), _rand((B, H, n, 128), 221)
+    lens = [700, 555, 600][:B]
+    for b, m in enumerate(lens):
+        unseen = torch.from_numpy(~orc.window_mask(m, t, window, sink).any(0)).to(DEV)
+        K[b, :, :m][:, unseen] = float("nan")
+        V[b, :, :m][:, unseen] = float("inf")
+        K[b, :, m:] = float("inf")
+        V[b, :, m:] = float("nan")
+    Q = _rand((B, H * group, t, 128), 222)
+    desc = cur.make_desc(K, V, 1, q_heads=H * group, seqlens=torch.tensor(lens, dtype=torch.int32, device=DEV))
+    lse = torch.zeros(Q.shape[:3], device=DEV)
+    O, ws = cur.curdkv_attention_window(Q, K, V, desc, window, num_sink=sink, scale=0.1, lse=lse)
+    assert cur.curdkv_device_status(ws) == 0
+    K, V = (torch.nan_to_num(x, 0.0, 0.0, 0.0) for x in (K, V))          # (rows the oracle gives no weight)
+    _check(O, lse, Q, K, V, lens, [t] * B, window, sink, float(np.float32(0.1)), heads=[0, H * group - 1])
+
+
+def test_prompts_without_queries_in_some_sequences():
+    _run(4, 8, 4, 400, 300, 90, 4, lens=[400, 400, 0, 1], q_lens=[0, 300, 300, 0], seed=230, heads=HEADS)
+    _run(3, 8, 4, 400, 300, 90, 4, lens=[400, 400, 300], q_lens=[0, -5, 0], seed=231, heads=HEADS)
