@@ -801,18 +801,41 @@ __global__ void __launch_bounds__(32) join_kernel(const Args a, int block_rows) 
   if (a.q_lens != nullptr && i >= min(max(a.q_lens[b], 0), a.q_n)) return;
   // the item begins in c0 (its second part) and goes on in the others (their first)
   auto part = [&](int c) { return ((size_t)c * 2 + (c == c0 ? 1 : 0)) * block_rows + qi; };
-  float all = -INFINITY;
-  for (int c = c0 + lane; c <= c1; c += 32) all = fmaxf(all, a.part_ml[part(c) * 2]);
+  // maxima and sums: a lane per part; sums of values: four parts in flight
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
+  auto at = [&](int c) { return part(min(c, c1)); };
+  auto values = [&](int c) { return *reinterpret_cast<const float4*>(a.part_o + at(c) * 128 + lane * 4); };
+  const float2 first = ml[at(c0 + lane)];
+  float4 x[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = values(c0 + k);
+  float all = first.x;
+  for (int c = c0 + 32 + lane; c <= c1; c += 32) all = fmaxf(all, ml[part(c)].x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
   float sum = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int c = c0; c <= c1; ++c) {
-    const size_t at = part(c);
-    const float m = a.part_ml[at * 2], f = all == -INFINITY ? 1.f : exp2_approx(m - all);      // (all -inf: zeros, or NaN)
-    const float4 x = *reinterpret_cast<const float4*>(a.part_o + at * 128 + lane * 4);
-    sum = fmaf(f, a.part_ml[at * 2 + 1], sum);
-    o.x = fmaf(f, x.x, o.x); o.y = fmaf(f, x.y, o.y); o.z = fmaf(f, x.z, o.z); o.w = fmaf(f, x.w, o.w);
+  for (int cb = c0; cb <= c1; cb += 32) {
+    const float2 e = cb == c0 ? first : ml[at(cb + lane)];
+    const float f = cb + lane > c1 ? 0.f : (all == -INFINITY ? 1.f : exp2_approx(e.x - all));      // (all -inf: zeros, or NaN)
+    float l = f * e.y;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+    sum += l;
+    for (int c = cb; c < cb + 32 && c <= c1; c += 4) {
+      float4 now[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        now[k] = x[k];
+        if (c + 4 <= c1) x[k] = values(c + 4 + k);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float fk = __shfl_sync(0xffffffffu, f, c - cb + k);
+        if (c + k > c1) continue;
+        o.x = fmaf(fk, now[k].x, o.x); o.y = fmaf(fk, now[k].y, o.y); o.z = fmaf(fk, now[k].z, o.z); o.w = fmaf(fk, now[k].w, o.w);
+      }
+    }
   }
   const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
   uint2 v;
