@@ -54,7 +54,7 @@ bool status_ok(const void* workspace) { return (reinterpret_cast<uintptr_t>(work
 
 // CTAs per head so that `problems` heads of up to `rows` rows fill the device a few times over.
 int ctas_for(int64_t problems, int64_t rows, int rows_per_cta) {
-  int64_t want = (8LL * sms() + problems - 1) / (problems > 0 ? problems : 1);
+  int64_t want = (16LL * sms() + problems - 1) / (problems > 0 ? problems : 1);
   const int64_t most = (rows + rows_per_cta - 1) / rows_per_cta;
   if (want > most) want = most;
   return (int)(want < 1 ? 1 : want);
