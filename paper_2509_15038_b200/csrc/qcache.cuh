@@ -243,7 +243,7 @@ struct StoreArgs {
 };
 
 // Gathers the selected rows and holds them in 4 bits, slot 0 upwards; sets count.
-// 436224 rows of 64 heads (223 MB read, 70 MB written): 81 us, 3.6 TB/s.  What bounds it is the quantiser's
+// 435712 rows of 256 heads (223 MB read, 70 MB written): 81 us, 3.6 TB/s.  What bounds it is the quantiser's
 // instructions, some 125 per 8 x 32 channels (72 % of the issue slots, 55 % of the integer pipe).  With the next
 // turn's rows in registers instead of shared memory 94 us (80 registers: three CTAs an SM where this runs
 // four, and one turn ahead); with half as many CTAs 5 us more, since the last ones run alone.
@@ -408,7 +408,7 @@ __device__ __forceinline__ uint4 dequantise8(uint32_t codes, uint32_t meta) {
 }
 
 // Held rows as bf16.  Rows beyond count, and entries of idx that are negative, leave the output as
-// it is.  What bounds it are the bytes: 436224 rows, 70 MB read and 223 MB written, 50 us, 5.9 TB/s.
+// it is.  What bounds it are the bytes: 435712 rows, 70 MB read and 223 MB written, 50 us, 5.9 TB/s.
 // grid = batch * heads * ctas_per_head, block = 256.
 __global__ void __launch_bounds__(kStoreWarps * 32) read_kernel(const ReadArgs a) {
   const int p = blockIdx.x / a.ctas_per_head, part = blockIdx.x % a.ctas_per_head;
