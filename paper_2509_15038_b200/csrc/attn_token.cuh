@@ -2,14 +2,19 @@
 // one kernel: rows held in 4 bits (curdkv_qcache_attention) and bf16 rows of which a sliding window
 // and the first tokens are visible (curdkv_attention_window with few queries).
 //
-// What bounds it is the cache's bytes, each read once.  The tiles of all items -- an item is a head and
-// a block of query rows -- form one line, and every CTA takes an equal run of it, whatever the items'
-// lengths: whole items are finished where they are, the partial results of an item that several CTAs
-// share are joined by a second kernel.  (With a CTA per item, 128 heads of 2048 to 16384 rows took 70 us,
-// as long as the longest; with equal runs 46 us.)  A CTA's warps take the tiles of an item in turn, each warp with its own ring
-// of tiles in shared memory, filled by 16-byte asynchronous copies (rows that do not exist are
-// filled with zeros, so nothing behind a head's last row is ever read).  No barrier stands in the
-// key loop.  Per 16 keys a warp forms
+// What has to be moved are the cache's bytes, each once.  4-bit rows are bound by the instructions that
+// unpack and weigh them instead (some 285 per 16 keys of a warp, integer pipe 57 % busy): 64 heads of 131072
+// rows and 4 queries 236 us, 5.7 TB/s (280 when the device's power limit holds its clock down); a copy that
+// only loads takes 196.  bf16 rows are bound by their loads: 128 heads with a window of 4096 52 us,
+// 5.0 TB/s, some 10 us of it start, scan and join.
+// The tiles of all items -- an item is a head and a block of query rows -- form one line, and every CTA takes
+// an equal run of it, whatever the items' lengths: whole items are finished where they are, the partial
+// results of an item that several CTAs share are joined by a second kernel.  (128 heads of 2048 to 16384 rows:
+// 70 us with a CTA per item, as long as the longest, 49 with equal runs.  Even heads pay for it: the 128
+// windows of 4096 took 44 us with a CTA of eight warps each.)  A CTA's warps take the tiles of an item in
+// turn, each warp with its own ring of tiles in shared memory, filled by 16-byte asynchronous copies (rows
+// that do not exist are filled with zeros, so nothing behind a head's last row is ever read).  No barrier
+// stands in the key loop.  Per 16 keys a warp forms
 //   S^T [16 keys x 8 queries] = K Q^T        m16n8k16, keys as the M side: with the few queries of
 //   O^T [128 x 8 queries]    += V^T P^T      a KV head as N = 8 half the instructions that a layout
 //                                            with 16 padded queries as M would need
@@ -451,10 +456,11 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
     if constexpr (Q4) {
       const uint4 v = *reinterpret_cast<const uint4*>(st + T::kVMeta + lane * 16);
       const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-      uint32_t big = 0;                                    // bits of the largest of |zero| and 16 * scale
+      uint32_t top = w[0] & 0x7fff7fffu;                   // largest |zero| and largest scale, bf16 side by side
 #pragma unroll
-      for (int gr = 0; gr < 4; ++gr)
-        big = max(big, max(w[gr] & 0x7fff0000u, (w[gr] & 0x7fffu) != 0u ? (w[gr] << 16) + (4u << 23) : 0u));
+      for (int gr = 1; gr < 4; ++gr) top = __vmaxu2(top, w[gr] & 0x7fff7fffu);
+      // bits of the larger of |zero| and 16 * scale (a scale of 0 gives 2^-123, which the limit below covers)
+      const uint32_t big = max(top & 0x7fff0000u, (top << 16) + (4u << 23));
       // biased exponent above it; rows far below the tile's largest (rows of zeros among them) take one
       // near it, so that their weights stay numbers
       int e = min(max((int)(big >> 23) + 1, 37), 250);       // (sums of 2^20 weights times 2^-e stay numbers)
