@@ -21,16 +21,18 @@
 // converged with one elected lane issuing (inside `if (lane == 0)` the compiler cannot use uniform
 // registers, and a product beside busy softmax warps took 270 cycles to issue instead of 90), in one rolled
 // loop with little code.  Measured and dropped: two threads per row (a tile's softmax 2650 cycles against
-// 1700, the warps crowding each other out); an issuing warp per query tile (194 us where this takes 180);
-// 64-key steps; every other pair of exponentials as a polynomial on the FMA pipe (no change: the
-// special function units are not what is waited for).
+// 1700, the warps crowding each other out); an issuing warp per query tile (205 us where this takes 180: the
+// tiles fall into step, and their exponentials with them; with turns for the exponentials 199); 64-key
+// steps; every other pair of exponentials as a polynomial on the FMA pipe (no change).
 //
-// What bounds it: the tensor pipe's issue.  A step of 128 keys is 32 products of 64 cycles for the two tiles,
-// 2048 cycles, and 1024 cycles of the special function units; it takes 3500 to 3900, with or without the softmax
-// between, since a product is issued every 95 cycles here and the waits between the batches come on top.  A
-// change of items costs 4000 cycles (the last product, O through registers, the first S of the next) every
-// nine steps at window 1024.  8192 tokens, 32 / 8 heads, window 1024: 180 us, 718 TFLOP/s over the visible
-// keys; 4 prompts of up to 2000 tokens, window 512: 74 us.
+// What bounds it: the chain of one query tile.  A step of 128 keys takes 3900 cycles: 2300 from logits to weights
+// (500 for reading them and the maximum, 850 for each half of the exponentials and its hand-over), 256 for the
+// second half of P V, 512 for the next S, and some 800 of waits and wake-ups between them.  S cannot be issued
+// earlier, because the weights lie over it and two S and two O fill TMEM.  Of the 3900 cycles the two tiles keep
+// the tensor pipe busy for 2048, and the special function units for as many.  A change of items costs
+// 4000 cycles (the last product, O through registers, the first S of the next) every nine steps at window
+// 1024.  8192 tokens, 32 / 8 heads, window 1024: 180 us, 718 TFLOP/s over the visible keys; 4 prompts of up
+// to 2000 tokens, window 512: 72 us.
 //
 // The running maximum moves only when a tile exceeds it by more than 2^8 (as in attn_umma.cuh); the
 // group then rescales its accumulator in TMEM, which after the first tiles is rare.  All waits are bounded.
