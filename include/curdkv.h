@@ -415,8 +415,8 @@ curdkv_status curdkv_qcache_read(const curdkv_qcache* cache, const int32_t* idx,
  *   scale  finite, >= 0
  * A head without rows gives O = 0 and lse = -inf.  Products of codes are exact, sums and the softmax
  * are fp32; the weights are rounded to fp16 (11 bits) before they multiply the values, O is rounded
- * once.  Keys are shared out over the SMs and the shares joined in a fixed order by a second launch
- * (none where one share suffices).  Workspace (256-byte aligned): its status word collects (it is not
+ * once.  Keys are shared out over the SMs and the shares joined in a fixed order, in the same launch or, for
+ * long caches, by a second one.  Workspace (256-byte aligned): its status word collects (it is not
  * cleared) CURDKV_DEV_BAD_INDEX, a count or row_start out of range; two calls that may overlap need
  * a workspace each. */
 size_t curdkv_qcache_attention_workspace_bytes(const curdkv_qcache* cache, int32_t q_rows);

@@ -5,16 +5,17 @@
 // What has to be moved are the cache's bytes, each once.  4-bit rows are bound by the instructions that
 // unpack and weigh them instead (some 285 per 16 keys of a warp, integer pipe 57 % busy): 64 heads of 131072
 // rows and 4 queries 236 us, 5.7 TB/s (280 when the device's power limit holds its clock down); a copy that
-// only loads takes 196.  bf16 rows are bound by their loads: 128 heads with a window of 4096 52 us,
-// 5.0 TB/s, some 10 us of it start, scan and join.
+// only loads takes 196.  bf16 rows are bound by their loads: 128 heads with a window of 4096 46 us, 5.7 TB/s.
 // The tiles of all items -- an item is a head and a block of query rows -- form one line, and every CTA takes
 // an equal run of it, whatever the items' lengths: whole items are finished where they are, the partial
 // results of an item that several CTAs share are joined by a second kernel.  (128 heads of 2048 to 16384 rows:
-// 70 us with a CTA per item, as long as the longest, 49 with equal runs.  Even heads pay for it: the 128
-// windows of 4096 took 44 us with a CTA of eight warps each.)  A CTA's warps take the tiles of an item in
-// turn, each warp with its own ring of tiles in shared memory, filled by 16-byte asynchronous copies (rows
-// that do not exist are filled with zeros, so nothing behind a head's last row is ever read).  No barrier
-// stands in the key loop.  Per 16 keys a warp forms
+// 70 us with a CTA per item, as long as the longest, 49 with equal runs.)  Where that gains little an item has
+// a CTA or a cluster of two, four or eight to itself, whose parts are joined through distributed shared
+// memory in the same launch: 8 heads of 1702 rows 6.4 us, 10.7 with equal runs and the second kernel; 128
+// windows of 4096 46 us against 53.  A CTA's warps take its tiles in turn, each warp with its own ring of
+// tiles in shared memory, filled by 16-byte asynchronous copies (rows that do not exist are filled with
+// zeros, so nothing behind a head's last row is ever read).  No barrier stands in the key loop.  Per 16
+// keys a warp forms
 //   S^T [16 keys x 8 queries] = K Q^T        m16n8k16, keys as the M side: with the few queries of
 //   O^T [128 x 8 queries]    += V^T P^T      a KV head as N = 8 half the instructions that a layout
 //                                            with 16 padded queries as M would need
@@ -54,7 +55,8 @@ struct Args {
   int heads, group, q_n;             // query heads per KV head; query tokens
   int rows, blocks;                  // rows = group * q_n, row r = token r / group, head r % group
   int items;                         // batch * heads * blocks
-  int ctas;                          // runs the tiles are cut into; 0: a CTA per item
+  int ctas;                          // runs the tiles are cut into; 0: a cluster of 2^split CTAs per item
+  int split;
   float scale_log2;                  // scale * log2(e)
   // 4-bit rows
   qcache::View cache;
@@ -112,6 +114,26 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
   const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&r);
+}
+// A cluster's barrier, and shared memory of its CTA `rank`.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float2 peer_float2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 peer_float4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
 }
 // 2^(e - 127) for 1 <= e <= 253, and 0 below
 __device__ __forceinline__ float pow2_biased(int e) { return __int_as_float(e > 0 ? e << 23 : 0); }
@@ -197,6 +219,7 @@ struct Item {
 // CTA whose run holds tile x of a line of `total` tiles cut into `runs` runs [i total / runs, ...).
 __device__ __forceinline__ int cta_of(int64_t x, int64_t total, int64_t runs) { return (int)(((x + 1) * runs - 1) / total); }
 
+constexpr int kMostSplit = 3;                              // log2 of the CTAs of a cluster
 constexpr int kMostItems = 8192;                           // items that are put on one line
 
 template <bool Q4, int NT>
@@ -205,13 +228,15 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
   constexpr int KB = T::kKeys / 16;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ float s_m[kWarps][8 * NT], s_l[kWarps][8 * NT];
+  __shared__ float2 s_ml[8 * NT];                          // the CTA's maxima and sums (clusters)
   __shared__ int64_t s_sum[kWarps], s_at;
   __shared__ int s_item;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // the joining kernel waits for this one's end
 
   // ------------------------------------------------------------ this CTA's run of tiles
-  int item_no = blockIdx.x;
+  const int rank = blockIdx.x & ((1 << a.split) - 1);     // (split is 0 where the line is cut)
+  int item_no = blockIdx.x >> a.split;
   int64_t off = 0, left_over = 1;                          // first tile inside the item; tiles of the run
   if (a.ctas > 0) {
     // every CTA sums up the items' tiles: a run of items per thread, then over the threads
@@ -277,8 +302,8 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
   const Seen seen = it.seen;
   const int64_t first_row = it.first_row;
   if (a.ctas == 0) {
-    left_over = it.tiles;
-    if (!it.ok && tid == 0) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
+    off = (it.tiles * rank) >> a.split;                    // (at most 2^27 tiles)
+    left_over = ((it.tiles * (rank + 1)) >> a.split) - off;
   } else if (it.tiles == 0) {
     continue;
   }
@@ -738,6 +763,19 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
       }
     }
   __syncthreads();
+  // one row's four channels: O = sums / sum, and its log sum
+  auto finish = [&](int qi, int c4, const float4& o, float top, float sum) {
+    const int r = r0 + qi, i = r / a.group, hq = h * a.group + r % a.group;
+    if (i >= q_live) return;                               // rows behind the last query stay as they are
+    const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);     // a NaN sum stays one
+    uint2 v;
+    v.x = pack_bf16(o.x * inv, o.y * inv);
+    v.y = pack_bf16(o.z * inv, o.w * inv);
+    *reinterpret_cast<uint2*>(a.O + b * a.o_sb + (int64_t)hq * a.o_sh + (int64_t)i * a.o_sn + c4) = v;
+    if (c4 == 0 && a.lse != nullptr)
+      a.lse[((int64_t)b * a.heads * a.group + hq) * a.q_n + i] =
+          sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
+  };
   for (int e = tid; e < (r1 - r0) * 32; e += kThreads) {
     const int qi = e >> 5, c4 = (e & 31) * 4;
     float all = -INFINITY, sum = 0.f;
@@ -752,7 +790,10 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
       o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
     }
     if (Q4) all -= kLift;
-    if (t_hi - t_lo < it.tiles) {                          // a part: of the item this run begins or ends in
+    if (a.split > 0) {                                     // (only this thread reads these four places)
+      *reinterpret_cast<float4*>(meet + (size_t)qi * 132 + c4) = o;
+      if (c4 == 0) s_ml[qi] = make_float2(all, sum);
+    } else if (t_hi - t_lo < it.tiles) {                   // a part: of the item this run begins or ends in
       const size_t at = ((size_t)blockIdx.x * 2 + (t_lo == 0 ? 1 : 0)) * 8 * NT + qi;
       *reinterpret_cast<float4*>(a.part_o + at * 128 + c4) = o;
       if (c4 == 0) {
@@ -760,17 +801,40 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
         a.part_ml[at * 2 + 1] = sum;
       }
     } else {
-      const int r = r0 + qi, i = r / a.group, hq = h * a.group + r % a.group;
-      if (i >= q_live) continue;                           // rows behind the last query stay as they are
-      const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);   // a NaN sum stays one
-      uint2 v;
-      v.x = pack_bf16(o.x * inv, o.y * inv);
-      v.y = pack_bf16(o.z * inv, o.w * inv);
-      *reinterpret_cast<uint2*>(a.O + b * a.o_sb + (int64_t)hq * a.o_sh + (int64_t)i * a.o_sn + c4) = v;
-      if (c4 == 0 && a.lse != nullptr)
-        a.lse[((int64_t)b * a.heads * a.group + hq) * a.q_n + i] =
-            sum == 0.f ? -INFINITY : (all + log2f(sum)) * 0.6931471805599453f;
+      finish(qi, c4, o, all, sum);
     }
+  }
+  if (a.ctas == 0) {
+    // (flagged behind the matrix instructions, which a warp has to reach together)
+    if (!it.ok && rank == 0 && tid == 0) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
+    if (a.split == 0) return;
+    // the CTAs of a cluster join their parts, in the order of their ranks, a share of the rows each
+    cluster_sync();
+    for (int e = rank * kThreads + tid; e < (r1 - r0) * 32; e += kThreads << a.split) {
+      const int qi = e >> 5, c4 = (e & 31) * 4;
+      const uint32_t ml = smem_addr(&s_ml[qi]), at = smem_addr(meet + (size_t)qi * 132 + c4);
+      float2 part[1 << kMostSplit];
+      float4 x[1 << kMostSplit];
+      float all = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int c = 0; c < (1 << kMostSplit); ++c) {
+        if (c >> a.split) break;
+        part[c] = peer_float2(peer_addr(ml, c));
+        x[c] = peer_float4(peer_addr(at, c));
+        all = fmaxf(all, part[c].x);
+      }
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int c = 0; c < (1 << kMostSplit); ++c) {
+        if (c >> a.split) break;
+        const float f = all == -INFINITY ? 1.f : exp2_approx(part[c].x - all);                 // (all -inf: zeros, or NaN)
+        sum = fmaf(f, part[c].y, sum);
+        o.x = fmaf(f, x[c].x, o.x); o.y = fmaf(f, x[c].y, o.y); o.z = fmaf(f, x[c].z, o.z); o.w = fmaf(f, x[c].w, o.w);
+      }
+      finish(qi, c4, o, all, sum);
+    }
+    cluster_sync();                                        // nobody leaves while its parts are read
+    return;
   }
   if (left_over <= 0) return;
   __syncthreads();                                         // the ring is the next item's

@@ -73,26 +73,45 @@ curdkv_status check_rows(const curdkv_qcache* cache, const void* K, const void* 
 
 // ---- attention of few query rows ---------------------------------------------------------------
 struct Plan {
-  int nt, blocks, ctas;              // sets of 8 query rows a CTA takes, blocks of rows per head; 0: a CTA per item
+  int nt, blocks;                    // sets of 8 query rows a CTA takes, blocks of rows per head
+  int ctas, split;                   // runs of the line; 0: a cluster of 2^split CTAs per item
   size_t begins_at, ml_at, o_at, bytes;                    // inside the workspace, and its size
 };
 
-// `keys`: the most a head can hold or see in this call.  A CTA per item where that is a few rounds of its
-// warps' tiles (joining parts costs a second launch, as long as about eight rounds), or where there are so
-// many items that their lengths even out; one line of tiles, cut into equal runs, else -- as many runs as
-// CTAs fit the device, but none shorter than two rounds unless there are more items.  (Four times as many
-// runs, to even out SMs of different speed, was slower: 282 against 276 us for 64 heads of 131072 rows, 66
-// against 51 for 128 heads of 2048 to 16384.)  The workspace does not depend on `keys`.
-Plan plan_token(int64_t problems, int64_t rows, int64_t keys, int tile_keys, int ctas_per_sm) {
+// `keys`: what the longest head may hold or see in this call, `total`: all heads together.  An item has a cluster to itself -- the most CTAs, up to
+// eight, that find room on the device at once with two rounds of tiles each -- unless one line of all tiles, cut
+// into equal runs, needs so many rounds less that joining its parts pays.  Runs: as many as CTAs fit the
+// device, but none shorter than two rounds unless there are more items.  In us, clusters | line:
+//    8 heads of 4 bits:    1702 rows 6.4 | 10.7     3340 rows 8.0 | 11.7     8192 rows 11.5 | 11.4
+//   32 heads:              1702 rows 7.6 | 12.0     8192 rows 15.8 | 21.1    16384 rows 24.4 | 28.0
+//  128 heads:              1702 rows 13.7 | 18.8    3340 rows 21.0 | 25.4    one head of 8192 rows 12 | 10.4
+//  128 heads, bf16:        window 1024 14.6 | 20.3  window 4096 44.3 | 52.2
+//  456 heads:              1702 rows 36.3 | 38.3    8192 rows 139 | 115      bf16, window 2048 76.5 | 83.2
+// 1024 heads:              1702 rows 58.0 | 71.6    8192 rows 230 | 244      bf16, window 2048 160 | 178
+// (Four times as many runs, to even out SMs of different speed, was slower: 282 against 276 us for 64 heads of
+// 131072 rows, 66 against 51 for 128 heads of 2048 to 16384.)  The workspace depends on neither.
+Plan plan_token(int64_t problems, int64_t rows, int64_t keys, int64_t total, int tile_keys, int ctas_per_sm) {
   Plan pl;
   pl.nt = rows <= 8 ? 1 : 2;
   pl.blocks = (int)((rows + 8 * pl.nt - 1) / (8 * pl.nt));
   const int64_t items = problems * pl.blocks, slots = (int64_t)ctas_per_sm * sms();
-  const int64_t tiles = (keys + tile_keys - 1) / tile_keys;
+  const int64_t tiles = (keys + tile_keys - 1) / tile_keys, all = (total / tile_keys + problems) * pl.blocks;
   pl.ctas = 0;
-  if (tiles > 8 * token::kWarps && items <= token::kMostItems) {
-    const int64_t rounds = (items * tiles + token::kWarps - 1) / token::kWarps;
-    int64_t ctas = rounds / 2;
+  pl.split = 0;
+  while (pl.split < token::kMostSplit && (items << (pl.split + 1)) <= slots && tiles > (2 * token::kWarps) << pl.split)
+    ++pl.split;
+  const int64_t cluster = (int64_t)token::kWarps << pl.split;
+  // Rounds of tiles when every item has its cluster: those of one item where all run at once; else as many
+  // as the SMs need for all, the last, partly filled wave counted as a quarter at least (few CTAs on an SM are faster).
+  const int64_t per = (tiles + cluster - 1) / cluster, n = items << pl.split, rest = n % slots;
+  const int64_t last = rest == 0 ? 0 : (rest > slots / 4 ? rest : slots / 4);
+  const int64_t alone = n <= slots ? per : (n - rest + last) * per / slots;
+  const int64_t even = (all + token::kWarps * slots - 1) / (token::kWarps * slots);             // of equal runs
+  // the line's own cost: the join, and the scan of its items
+  const int64_t line = n <= slots ? 7 : 3 + items / 256;
+  if (alone > even + line && items <= token::kMostItems) {
+    pl.split = 0;
+    int64_t ctas = all / (2 * token::kWarps);
     if (ctas < items) ctas = items;
     if (ctas > slots) ctas = slots;
     pl.ctas = (int)ctas;
@@ -107,14 +126,19 @@ Plan plan_token(int64_t problems, int64_t rows, int64_t keys, int tile_keys, int
 }
 
 Plan plan_qcache(const curdkv_qcache* c, int32_t q_rows) {
-  // (packed heads: any of them may own most of the rows)
-  return plan_token((int64_t)c->batch * c->kv_heads, q_rows, c->capacity, token::Tile<true>::kKeys,
+  // Packed heads share `capacity` rows unevenly: the longest is taken to hold four times its share.  (8 heads of
+  // 1702 rows take 6.5 us so and 14.5 with equal runs, one of 12916 and seven of 100 15 and 48.)
+  const int64_t P = (int64_t)c->batch * c->kv_heads, share = P > 0 ? 4 * ((c->capacity + P - 1) / P) : 0;
+  const bool packed = c->row_start != nullptr;
+  const int64_t longest = packed && share < c->capacity ? share : c->capacity;
+  return plan_token(P, q_rows, longest, packed ? c->capacity : P * c->capacity, token::Tile<true>::kKeys,
                     q_rows <= 8 ? token::ctas_per_sm<true, 1>() : token::ctas_per_sm<true, 2>());
 }
 
 Plan plan_window(const curdkv_desc* d, int32_t q_rows, int64_t seen) {
-  return plan_token((int64_t)d->batch * d->kv_heads, (int64_t)(d->q_heads / d->kv_heads) * q_rows, seen,
-                    token::Tile<false>::kKeys, token::ctas_per_sm<false, 1>());
+  const int64_t P = (int64_t)d->batch * d->kv_heads;
+  return plan_token(P, (int64_t)(d->q_heads / d->kv_heads) * q_rows, seen, P * seen, token::Tile<false>::kKeys,
+                    token::ctas_per_sm<false, 1>());
 }
 
 // Lets `kernel` use `bytes` of shared memory on the current device; asked of the driver once per device.
@@ -134,6 +158,21 @@ bool launch_attend(const token::Args& a, cudaStream_t stream) {
   constexpr int smem = token::smem_bytes<Q4, NT>();
   static std::atomic<uint64_t> done{0};
   if (!allow_smem(token::attend_kernel<Q4, NT>, smem, done)) return false;
+  if (a.split > 0) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)a.items << a.split);
+    cfg.blockDim = dim3(token::kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 1u << a.split;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, token::attend_kernel<Q4, NT>, a) != cudaSuccess) return false;
+    return launched();
+  }
   const int grid = a.ctas > 0 ? a.ctas : a.items;
   token::attend_kernel<Q4, NT><<<(unsigned)grid, token::kThreads, smem, stream>>>(a);
   if (!launched()) return false;
@@ -301,6 +340,7 @@ curdkv_status curdkv_qcache_attention(const void* Q, int32_t q_rows, int64_t q_s
   a.blocks = pl.blocks;
   a.items = (int)(P * pl.blocks);
   a.ctas = pl.ctas;
+  a.split = pl.split;
   // (a masked product is -inf, and -inf times a scale of 0 would be NaN)
   a.scale_log2 = scale * 1.4426950408889634f;
   if (a.scale_log2 < 1e-30f) a.scale_log2 = 1e-30f;
@@ -394,6 +434,7 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
   a.blocks = pl.blocks;
   a.items = (int)(P * pl.blocks);
   a.ctas = pl.ctas;
+  a.split = pl.split;
   if (P * pl.blocks > 0x7fffffffLL || P * a.rows > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
   a.scale_log2 = scale_log2;
   a.K = KvView{static_cast<const __nv_bfloat16*>(K), desc->k_stride_b, desc->k_stride_h, desc->k_stride_n};

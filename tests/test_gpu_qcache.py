@@ -463,3 +463,35 @@ def test_attention_calls_side_by_side():
     # a key of 20 sign(q) has logits of 2 sum |q|, some 60 above every other: its value, 5, is the answer of query 0 to
     # within the weight of the others (exp(-20) each at most) and the roundings to fp16 and bf16
     assert torch.all((O[:, :, 0].float() - 5.0).abs() <= 5.0 * (2.0 ** -8 + 2.0 ** -10))
+
+
+@pytest.mark.parametrize("q_rows", [1, 5, 16])
+@pytest.mark.parametrize("B,H,cap", [(1, 1, 20000), (3, 2, 12000), (1, 2, 3001), (10, 8, 1500), (25, 8, 600), (60, 8, 100)])
+def test_attention_however_the_keys_are_shared_out(B, H, cap, q_rows):
+    """Equal runs over all heads, clusters of eight, four and two CTAs per head, one CTA per head; heads without rows, with one,
+    with one more than a tile."""
+    rng = np.random.default_rng(B)
+    counts = rng.integers(0, cap + 1, B * H).tolist()
+    for p, c in enumerate([cap, 0, 1, 33, cap - 1]):
+        if p < B * H:
+            counts[p] = c
+    cache, starts = _random_cache(B, H, cap, counts, 430)
+    Q = _rand((B, H, q_rows, 128), 431)
+    lse = torch.zeros((B, H, q_rows), device=DEV)
+    O, ws = cur.curdkv_qcache_attention(Q, cache, scale=0.0884, lse=lse)
+    assert cur.curdkv_device_status(ws) == 0
+    _check_attention(O, lse, Q, cache, counts, starts, float(np.float32(0.0884)), f"{(B, H, cap, q_rows)}")
+    for _ in range(3):
+        again, _ = cur.curdkv_qcache_attention(Q, cache, scale=0.0884, workspace=ws)
+        assert torch.equal(O, again)
+
+
+@pytest.mark.parametrize("cap", [32, 500, 3000])
+def test_attention_flags_counts_and_attends_to_the_rest(cap):
+    cache, starts = _random_cache(2, 2, cap, [cap] * 4, 440)
+    cache.count.copy_(torch.tensor([cap + 1, -3, cap, 5], dtype=torch.int32))
+    Q = _rand((2, 2, 3, 128), 441)
+    lse = torch.zeros((2, 2, 3), device=DEV)
+    O, ws = cur.curdkv_qcache_attention(Q, cache, scale=0.1, lse=lse)
+    assert cur.curdkv_device_status(ws) == cur.DEV_BAD_INDEX
+    _check_attention(O, lse, Q, cache, [cap, 0, cap, 5], starts, float(np.float32(0.1)))

@@ -335,3 +335,12 @@ def test_rows_that_no_query_sees_hold_anything(B, H, group, t, window, sink):
 def test_prompts_without_queries_in_some_sequences():
     _run(4, 8, 4, 400, 300, 90, 4, lens=[400, 400, 0, 1], q_lens=[0, 300, 300, 0], seed=230, heads=HEADS)
     _run(3, 8, 4, 400, 300, 90, 4, lens=[400, 400, 300], q_lens=[0, -5, 0], seed=231, heads=HEADS)
+
+
+@pytest.mark.parametrize("t", [1, 3])
+@pytest.mark.parametrize("B,H,n,window", [(1, 1, 9000, 8900), (1, 2, 3001, 2900), (9, 8, 1200, 1000), (18, 8, 700, 500), (40, 8, 300, 90)])
+def test_few_tokens_however_the_keys_are_shared_out(B, H, n, window, t):
+    """Equal runs over all heads, clusters of eight, four and two CTAs per head, one CTA per head."""
+    lens = [n - 7 * b if b % 5 else n for b in range(B)]
+    lens[-1] = n if B == 1 else 1
+    _run(B, H, 4, n, t, window, 4, lens=lens, q_lens=[min(t, x) for x in lens], seed=240, heads=[0, 4 * H - 1])
