@@ -696,7 +696,8 @@ def curdkv_attention_window(Q, K, V, desc: Desc, window: int, *, num_sink: int =
     dev = _on_device("curdkv_attention_window", Q, K, V, O, lse, q_lens, workspace)
     if B == 0:
         return O, workspace
-    code = load().curdkv_attention_window(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), _ptr(K), _ptr(V),
+    code = load().curdkv_attention_window(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), K.data_ptr() or _ptr(K),
+                                          V.data_ptr() or _ptr(V),
                                           ctypes.byref(desc), num_sink, window, scale, O.data_ptr(), o[0], o[1], o[2],
                                           _addr(lse), workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
     if code:

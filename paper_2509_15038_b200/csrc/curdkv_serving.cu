@@ -21,15 +21,20 @@ bool launched() {
   return cudaGetLastError() == cudaSuccess;
 }
 
-// SMs of the current device, or a B200's where none can be asked (workspace sizes).
+// SMs of the current device (asked of the driver once per device), or a B200's where none can be asked
+// (workspace sizes).
 int sms() {
+  static std::atomic<int> known[64];
   int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) {
-    cudaGetLastError();
-    return 148;
+  if (cudaGetDevice(&dev) == cudaSuccess) {
+    if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0) {
+      if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
+      return n;
+    }
   }
-  return n;
+  cudaGetLastError();
+  return 148;
 }
 
 curdkv_status check_cache(const curdkv_qcache* c) {
@@ -212,8 +217,9 @@ bool map_strides_ok(int64_t batch, int64_t heads, int64_t sb, int64_t sh, int64_
 //   64 x 8 heads, 512 keys, window 256, 128 / 256 rows               133 | 160    258 | 160
 bool prompt_form(int64_t problems, int64_t rows, int64_t pairs, int64_t window_keys, int64_t n_max) {
   const int64_t keys = window_keys < n_max ? window_keys : n_max;
-  const double token = 12.3 * (double)(problems * ((rows + 15) / 16)) / sms() * (double)(keys + 64);
-  const double prompt = 15.6 * (double)((problems * pairs + sms() - 1) / sms()) * (double)(keys + 320);
+  const int64_t places = sms();
+  const double token = 12.3 * (double)(problems * ((rows + 15) / 16)) / (double)places * (double)(keys + 64);
+  const double prompt = 15.6 * (double)((problems * pairs + places - 1) / places) * (double)(keys + 320);
   return prompt < token;
 }
 
