@@ -204,22 +204,22 @@ bool map_strides_ok(int64_t batch, int64_t heads, int64_t sb, int64_t sh, int64_
 }
 
 // Which form of the window attention a call takes: the one whose slowest SM is estimated to end first.
-// Measured: the token form needs 12.3 ns per key for 16 query rows of a KV head on one SM, plus the time of 64
-// keys, and spreads its work evenly; the prompt form 15.6 ns per key for a pair of 128-row tiles, full or not,
-// plus the time of some 320 keys (tiles partly outside the window, the start of an item), and takes whole
-// rounds of a pair per SM.  In us, token | prompt, rows = query rows per KV head, at the sizes around the
-// change from one to the other:
-//   16 x 8 heads, 8192 keys, window 8192, 32 / 64 / 128 rows         177 | 315    347 | 318    601 | 320
-//   16 x 8 heads, window 1024, 32 / 64 / 128 rows                     35 | 56      57 | 56     101 | 56
-//   16 x 8 heads, 512 keys, window 256, 64 / 128 rows                 21 | 29      39 | 29
-//    4 x 8 heads, 8192 keys, window 8192, 64 / 128 / 256 rows         76 | 121    135 | 121    267 | 147
+// Measured: the token form needs 9.8 ns per key for 16 query rows of a KV head on one SM, plus the time of 64
+// keys, and spreads its work evenly; the prompt form 18 ns per key for a pair of 128-row tiles (14.7 for a
+// single one), full or not, plus the time of some 320 keys (tiles partly outside the window, the start of an
+// item), and takes whole rounds of a pair per SM.  In us, token | prompt, rows = query rows per KV head, at the
+// sizes around the change from one to the other:
+//   16 x 8 heads, 8192 keys, window 8192, 32 / 64 / 128 rows         177 | 309    271 | 324    536 | 324
+//   16 x 8 heads, window 1024, 32 / 64 / 128 rows                     25 | 58      47 | 58      89 | 58
+//   16 x 8 heads, 512 keys, window 256, 64 / 128 rows                 21 | 31      39 | 31
+//    4 x 8 heads, 8192 keys, window 8192, 64 / 128 / 256 rows         76 | 121    135 | 121    271 | 147
 //    1 x 8 heads, 8192 keys, window 8192, 256 rows                    75 | 143    (the pairs fill few SMs)
-//   64 x 8 heads, 512 keys, window 256, 128 / 256 rows               133 | 160    258 | 160
-bool prompt_form(int64_t problems, int64_t rows, int64_t pairs, int64_t window_keys, int64_t n_max) {
-  const int64_t keys = window_keys < n_max ? window_keys : n_max;
-  const int64_t places = sms();
-  const double token = 12.3 * (double)(problems * ((rows + 15) / 16)) / (double)places * (double)(keys + 64);
-  const double prompt = 15.6 * (double)((problems * pairs + places - 1) / places) * (double)(keys + 320);
+//   64 x 8 heads, 512 keys, window 256, 128 / 256 rows               133 | 165    259 | 166
+bool prompt_form(int64_t problems, int64_t rows, int64_t tiles, int64_t window_keys, int64_t n_max) {
+  const int64_t keys = window_keys < n_max ? window_keys : n_max, places = sms(), pairs = (tiles + 1) / 2;
+  const double token = 9.8 * (double)(problems * ((rows + 15) / 16)) / (double)places * (double)(keys + 64);
+  const double prompt =
+      (tiles > 1 ? 18.0 : 14.7) * (double)((problems * pairs + places - 1) / places) * (double)(keys + 320);
   return prompt < token;
 }
 
@@ -391,9 +391,9 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
   const int group = desc->q_heads / desc->kv_heads;
   // a masked product is -inf, and -inf times a scale of 0 would be NaN
   const float scale_log2 = scale * 1.4426950408889634f > 1e-30f ? scale * 1.4426950408889634f : 1e-30f;
-  const int64_t pairs = (((int64_t)q_rows + kTileRows - 1) / kTileRows * group + 1) / 2;
+  const int64_t tiles = ((int64_t)q_rows + kTileRows - 1) / kTileRows * group, pairs = (tiles + 1) / 2;
   if (desc->n_max > 0 && (int64_t)desc->n_max + q_rows < (1 << 30) && P * pairs <= 0x3fffffffLL &&
-      prompt_form(P, (int64_t)group * q_rows, pairs, (int64_t)window + num_sink, desc->n_max) &&
+      prompt_form(P, (int64_t)group * q_rows, tiles, (int64_t)window + num_sink, desc->n_max) &&
       map_strides_ok(desc->batch, desc->kv_heads, desc->k_stride_b, desc->k_stride_h, desc->k_stride_n) &&
       map_strides_ok(desc->batch, desc->kv_heads, desc->v_stride_b, desc->v_stride_h, desc->v_stride_n) &&
       map_strides_ok(desc->batch, desc->q_heads, q_stride_b, q_stride_h, q_stride_n)) {
