@@ -115,8 +115,10 @@ __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
   const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
-// A cluster's barrier, and shared memory of its CTA `rank`.
+// A cluster's barrier, and shared memory of its CTA `rank`.  The barrier, like the matrix instructions, is of the
+// aligned kind: a warp has to come to it with all its lanes together, whatever one of them did alone before.
 __device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
@@ -290,6 +292,7 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
       if (blockIdx.x == 0 && e1 == a.items && e0 < e1) a.begins[e1] = x;
     }
     __syncthreads();
+    __syncwarp();                                          // lanes above went different ways; matrix instructions follow
     left_over = hi - lo;
     if (left_over <= 0) return;
     item_no = s_item;
@@ -805,9 +808,14 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
     }
   }
   if (a.ctas == 0) {
-    // (flagged behind the matrix instructions, which a warp has to reach together)
-    if (!it.ok && rank == 0 && tid == 0) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
-    if (a.split == 0) return;
+    // (one lane's work: behind all matrix instructions and barriers, to which a warp has to come together)
+    auto flag = [&]() {
+      if (!it.ok && rank == 0 && tid == 0) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
+    };
+    if (a.split == 0) {
+      flag();
+      return;
+    }
     // the CTAs of a cluster join their parts, in the order of their ranks, a share of the rows each
     cluster_sync();
     for (int e = rank * kThreads + tid; e < (r1 - r0) * 32; e += kThreads << a.split) {
@@ -834,10 +842,12 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
       finish(qi, c4, o, all, sum);
     }
     cluster_sync();                                        // nobody leaves while its parts are read
+    flag();
     return;
   }
   if (left_over <= 0) return;
   __syncthreads();                                         // the ring is the next item's
+  __syncwarp();
   }
 }
 

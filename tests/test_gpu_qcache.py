@@ -495,3 +495,38 @@ def test_attention_flags_counts_and_attends_to_the_rest(cap):
     O, ws = cur.curdkv_qcache_attention(Q, cache, scale=0.1, lse=lse)
     assert cur.curdkv_device_status(ws) == cur.DEV_BAD_INDEX
     _check_attention(O, lse, Q, cache, [cap, 0, cap, 5], starts, float(np.float32(0.1)))
+
+
+def _launches(call):
+    before = cur.launch_count()
+    call()
+    return cur.launch_count() - before
+
+
+@pytest.mark.parametrize("B,H,cap,launches", [(1, 2, 20000, 2), (3, 2, 12000, 2), (1, 8, 1700, 1), (2, 2, 300, 1), (4, 8, 60, 1)])
+@pytest.mark.parametrize("bad", ["counts", "row_start"])
+def test_attention_flags_bad_heads_in_every_form(B, H, cap, launches, bad):
+    """Counts out of range, and row_start that runs backwards or beyond the cache, over equal runs (two launches), clusters
+    and single CTAs: flagged, the head bounded or empty, every other head as the oracle has it."""
+    P = B * H
+    counts = [max(cap - 3 * p, 0) for p in range(P)]
+    cache, starts = _random_cache(B, H, cap, counts, 450, packed=bad == "row_start")
+    held = list(counts)
+    if bad == "counts":
+        held[0], held[P - 1] = cap, 0
+        cache.count.copy_(torch.tensor([cap + 7] + counts[1:-1] + [-1], dtype=torch.int32))
+    else:                                            # the first head ends before it begins, the last one behind the cache
+        held[0], held[P - 1] = 0, 0
+        cache.row_start[0] = cache.row_start[1] + 1
+        cache.row_start[P] = cache.capacity + 1
+    Q = _rand((B, H, 4, 128), 451)
+    lse = torch.zeros((B, H, 4), device=DEV)
+    ws = cur.qcache_attention_workspace(cache, 4)
+    call = lambda: cur.curdkv_qcache_attention(Q, cache, scale=0.0884, O=O, lse=lse, workspace=ws)  # noqa: E731
+    for _ in range(3):
+        O = torch.full_like(Q, 3.0)
+        ws[:256].zero_()
+        n = _launches(call)
+        assert n == launches or bad == "row_start"
+        assert cur.curdkv_device_status(ws) == cur.DEV_BAD_INDEX
+        _check_attention(O, lse, Q, cache, held, starts, float(np.float32(0.0884)), f"{(B, H, cap, bad)}")
