@@ -8,6 +8,7 @@ is raised.
 from __future__ import annotations
 
 import ctypes
+import struct
 from pathlib import Path
 from typing import Optional
 
@@ -499,6 +500,26 @@ def _on_device(what: str, first: torch.Tensor, *rest: Optional[torch.Tensor]) ->
     return dev
 
 
+# batch, kv_heads, q_heads, n_max, d, r and the strides of K and V
+_DESC_ROWS = struct.Struct("=6i6q").unpack_from
+
+
+def _described(what: str, K: torch.Tensor, V: torch.Tensor, desc: Desc, dev: int) -> None:
+    """K and V have to be what the descriptor says, whose shape and strides the kernels go by, and its lengths have to
+    lie where they run."""
+    shape = K.shape
+    B, H, _, n, d, _, kb, kh, kn, vb, vh, vn = _DESC_ROWS(desc)          # (its fields at once: half a microsecond less)
+    if K.dtype is not torch.bfloat16 or V.dtype is not torch.bfloat16:
+        raise TypeError(f"{what}: K and V must be bf16")
+    if shape != (B, H, n, d) or shape != V.shape:
+        raise ValueError(f"{what}: K is {tuple(shape)}, V {tuple(V.shape)}, the descriptor says {(B, H, n, d)}")
+    if K.stride() != (kb, kh, kn, 1) or V.stride() != (vb, vh, vn, 1):
+        raise ValueError(f"{what}: K or V has other strides than the descriptor")
+    lens = getattr(desc, "seqlens_tensor", None)
+    if lens is not None and lens.get_device() != dev:
+        raise ValueError(f"{what}: the descriptor's seqlens are on {lens.device}")
+
+
 def _int32(what: str, t: Optional[torch.Tensor], numel: Optional[int] = None) -> None:
     if t is not None and (t.dtype is not torch.int32 or not t.is_contiguous() or (numel is not None and t.numel() != numel)):
         raise ValueError(f"{what} must be a contiguous int32 tensor" + (f" of {numel} entries" if numel is not None else ""))
@@ -566,6 +587,7 @@ def curdkv_qcache_store(cache: QuantCache, K, V, desc: Desc, idx=None, head_coun
     """Rows of K, V (all, or those a selection names, laid out as :func:`curdkv_select` returns them; ``packed``
     for an adaptive one) quantised into ``cache`` from slot 0; sets ``cache.count``."""
     dev = _on_device("curdkv_qcache_store", cache.K_codes, K, V, idx, head_counts, head_offsets, workspace)
+    _described("curdkv_qcache_store", K, V, desc, dev)
     P = cache.batch * cache.kv_heads
     _int32("idx", idx)
     _int32("head_counts", head_counts, P)
@@ -694,6 +716,7 @@ def curdkv_attention_window(Q, K, V, desc: Desc, window: int, *, num_sink: int =
     if workspace is None:
         workspace = attention_window_workspace(desc, t, device=Q.device)
     dev = _on_device("curdkv_attention_window", Q, K, V, O, lse, q_lens, workspace)
+    _described("curdkv_attention_window", K, V, desc, dev)
     if B == 0:
         return O, workspace
     code = load().curdkv_attention_window(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), K.data_ptr() or _ptr(K),

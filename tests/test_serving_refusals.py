@@ -130,3 +130,42 @@ def test_oracle_of_the_format():
     assert orc.PLACES["V"][32 * 1 + 4 * 6 + 3] == 4 * (4 * 6 + 1) + 3
     m = orc.window_mask(6, 2, 2, 1)
     assert m.tolist() == [[True, False, False, True, True, False], [True, False, False, False, True, True]]
+
+
+def _elsewhere(monkeypatch):
+    """Has the binding take CPU tensors for tensors of device 0, and fail where a call would reach the library."""
+    monkeypatch.setattr(cur, "_on_device", lambda what, first, *rest: 0)
+
+    def reached():
+        raise AssertionError("the call was not refused")
+    monkeypatch.setattr(cur, "load", reached)
+
+
+def test_rows_that_the_descriptor_does_not_describe(monkeypatch):
+    """K and V shorter, of another type or laid out otherwise than their descriptor says, and lengths on another device, are
+    refused: the kernels go by the descriptor and would read beyond the tensors."""
+    K = torch.zeros((1, 2, 16, 128), dtype=torch.bfloat16)
+    desc = cur.make_desc(K, K, 1)
+    cache = cur.QuantCache(1, 2, 16, device="cpu")
+    Q = torch.zeros((1, 2, 1, 128), dtype=torch.bfloat16)
+    ws = torch.zeros(1 << 20, dtype=torch.uint8)
+    assert (cur.Desc.n_max.offset, cur.Desc.k_stride_b.offset, cur.Desc.v_stride_n.offset) == (12, 24, 64)   # as they are read
+    _elsewhere(monkeypatch)
+    calls = (lambda k, v, d: cur.curdkv_qcache_store(cache, k, v, d),
+             lambda k, v, d: cur.curdkv_attention_window(Q, k, v, d, 4, scale=0.1, workspace=ws))
+    turned = torch.zeros((1, 16, 2, 128), dtype=torch.bfloat16).transpose(1, 2)
+    for call in calls:
+        for k, v in ((K[:, :, :8], K), (K, K[:, :, :8]), (K[:, :1], K[:, :1]), (K[:, :, :8], K[:, :, :8])):
+            with pytest.raises(ValueError, match="descriptor"):
+                call(k, v, desc)
+        for k, v in ((turned, K), (K, turned)):
+            with pytest.raises(ValueError, match="strides"):
+                call(k, v, desc)
+        for k, v in ((K.half(), K), (K, K.float())):
+            with pytest.raises(TypeError, match="bf16"):
+                call(k, v, desc)
+        away = cur.make_desc(K, K, 1, seqlens=torch.full((1,), 16, dtype=torch.int32))       # on the host
+        with pytest.raises(ValueError, match="seqlens"):
+            call(K, K, away)
+        with pytest.raises(AssertionError, match="not refused"):     # and what is described passes
+            call(K, K, desc)
