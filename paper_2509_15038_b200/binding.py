@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import struct
+from operator import index
 from pathlib import Path
 from typing import Optional
 
@@ -525,6 +526,12 @@ def _int32(what: str, t: Optional[torch.Tensor], numel: Optional[int] = None) ->
         raise ValueError(f"{what} must be a contiguous int32 tensor" + (f" of {numel} entries" if numel is not None else ""))
 
 
+def _count(x: int) -> int:
+    """A number of rows for an int32 argument: what no cache holds is as good as the largest (ctypes would drop the upper
+    bits), what is negative is left to the call to refuse."""
+    return min(max(index(x), -1), 0x7FFFFFFF)
+
+
 def _status_buffer(what: str, t: Optional[torch.Tensor]) -> None:
     if t is not None and (not t.is_contiguous() or t.numel() * t.element_size() < 256):
         raise ValueError(f"{what}: workspace must be contiguous and hold at least 256 bytes")
@@ -721,8 +728,8 @@ def curdkv_attention_window(Q, K, V, desc: Desc, window: int, *, num_sink: int =
         return O, workspace
     code = load().curdkv_attention_window(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), K.data_ptr() or _ptr(K),
                                           V.data_ptr() or _ptr(V),
-                                          ctypes.byref(desc), num_sink, window, scale, O.data_ptr(), o[0], o[1], o[2],
-                                          _addr(lse), workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
+                                          ctypes.byref(desc), _count(num_sink), _count(window), scale, O.data_ptr(), o[0],
+                                          o[1], o[2], _addr(lse), workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
     if code:
         _check(code, "curdkv_attention_window")
     return O, workspace

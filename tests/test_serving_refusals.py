@@ -169,3 +169,30 @@ def test_rows_that_the_descriptor_does_not_describe(monkeypatch):
             call(K, K, away)
         with pytest.raises(AssertionError, match="not refused"):     # and what is described passes
             call(K, K, desc)
+
+
+@pytest.mark.parametrize("big", [2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63, 10 ** 30])
+def test_numbers_beyond_int32_are_not_cut(monkeypatch, big):
+    """A window, or sinks, of more rows than int32 counts reach the library as the largest number, negative ones as one that
+    it refuses."""
+    K = torch.zeros((1, 2, 16, 128), dtype=torch.bfloat16)
+    Q, ws = torch.zeros((1, 2, 1, 128), dtype=torch.bfloat16), torch.zeros(1 << 20, dtype=torch.uint8)
+    got = []
+
+    class Library:
+        @staticmethod
+        def curdkv_attention_window(*args):
+            got.append(args[9:11])
+            return 0
+    monkeypatch.setattr(cur, "_on_device", lambda what, first, *rest: 0)
+    monkeypatch.setattr(cur, "_raw_stream", lambda device: 0)
+    monkeypatch.setattr(cur, "load", lambda: Library)
+    call = lambda window, sink: cur.curdkv_attention_window(Q, K, K, cur.make_desc(K, K, 1), window, num_sink=sink, scale=0.1, workspace=ws)  # noqa: E731
+    call(big, 4)
+    call(4, big)
+    call(-big, 0)
+    call(0, -big)
+    call(np.int64(7), 0)
+    assert got == [(4, 2 ** 31 - 1), (2 ** 31 - 1, 4), (0, -1), (-1, 0), (0, 7)]
+    with pytest.raises(TypeError):
+        call(1.5, 0)
