@@ -413,8 +413,13 @@ curdkv_status curdkv_qcache_read(const curdkv_qcache* cache, const int32_t* idx,
  *   lse    NULL, or fp32 [batch][kv_heads][q_rows]: log of each row's sum of exponentials (natural,
  *          of the scaled logits), for joining partial attentions
  *   scale  finite, >= 0
- * A head without rows gives O = 0 and lse = -inf.  Products of codes are exact, sums and the softmax
- * are fp32; the weights are rounded to fp16 (11 bits) before they multiply the values, O is rounded
+ * A head without rows gives O = 0 and lse = -inf.  Products of codes, scales and zeros are exact (entries of
+ * a query row 2^26 times smaller than its largest are rounded), sums and the softmax are fp32.  A weight is
+ * rounded to fp16 (11 bits) before it multiplies V's zeros, and its product with a scale once more; bits lost
+ * below fp16's range come to no more than 2^-10 of the sum of |scale code| + |zero| times weight of a channel.
+ * That holds for finite V rows and groups of any size side by side, but for what contributes less than 2^-90 of
+ * the head's largest value (rows and groups more than some 2^8 apart take longer).  A NaN or an infinity in a
+ * group of V makes the group's 32 channels NaN and no others; one in a group of K the head.  O is rounded
  * once.  Keys are shared out over the SMs and the shares joined in a fixed order, in the same launch or, for
  * long caches, by a second one.  Workspace (256-byte aligned): its status word collects (it is not
  * cleared) CURDKV_DEV_BAD_INDEX, a count or row_start out of range; two calls that may overlap need

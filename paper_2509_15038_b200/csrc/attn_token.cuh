@@ -19,22 +19,29 @@
 //   S^T [16 keys x 8 queries] = K Q^T        m16n8k16, keys as the M side: with the few queries of
 //   O^T [128 x 8 queries]    += V^T P^T      a KV head as N = 8 half the instructions that a layout
 //                                            with 16 padded queries as M would need
-// and between the two the online softmax: a warp's running maximum moves only when some logit
-// exceeds it by more than 2^kSlack (one vote per tile), and since S^T and O^T hold a query in the
-// same lanes the rescale needs no exchange.  P^T reaches the second product's operand layout by two
-// 8x8 transposes (movmatrix).  Sums, maxima and accumulators are fp32; the weights enter the second
-// product as fp16 (4-bit rows) or bf16 (bf16 rows), at most 2^-11 / 2^-8 of each weight off by
-// half a step; the row sum is taken over the unrounded weights.
+// and between the two the online softmax: a warp's reference moves only when some logit exceeds it by more
+// than 2^slack (one vote per tile), and since S^T and O^T hold a query in the same lanes the rescale needs
+// no exchange.  P^T reaches the second product's operand layout by two 8x8 transposes (movmatrix).  Sums,
+// references and accumulators are fp32; the weights enter the second product as fp16 (4-bit rows) or bf16
+// (bf16 rows), at most 2^-11 / 2^-8 of each weight off; the row sum is taken over the unrounded weights.
 //
 // 4-bit rows cost five integer instructions per eight values and no conversion: a code left in the
 // low bits of a half is the fp16 subnormal code * 2^-24 (or code * 2^-20 one nibble up), which the
 // tensor cores multiply exactly.  The scales are applied outside: on the K side to the products of
 // each group of 32 channels (S = sum_g s_g (codes_g . q_g) + sum_g z_g sum(q_g), the second sum one
 // more matrix instruction whose A operand is the zeros), on the V side to the weights (one set per
-// group, P_g = p * s_g), with the zeros as a further instruction.  Every V row brings its own power of
-// two 2^e that covers its values: its scales and zeros relative to it fit fp16, and 2^e goes into the
-// exponent of its weight, so that the running maximum follows logit + e -- what a row adds to the
-// output -- and rows of any bf16 magnitude share a cache; the row sum takes the 2^e out again.
+// group, P_g = p * s_g), with the zeros as a further instruction.
+//
+// The values' magnitude is kept out of the weights' 16 bits.  A warp holds one power of two 2^E for V: scales
+// and zeros relative to it are exact in fp16 as long as every scale of a tile lies some 2^8 to 2^14 below
+// 2^E at most and every zero in [2^(E-17), 2^(E+14)), or is 0 (a vote per tile).  E follows the tiles: one that lies elsewhere but fits
+// by itself brings its own.  A tile that fits nowhere -- groups or rows further apart than that, or a NaN or an
+// infinity, which may meet its own group's channels only -- takes its products in bf16 instead, weights times
+// scale split into two pieces: 16 bits, at fp32's range.  So does a tile whose weights the reference of the
+// accumulators would push towards fp16's lower end (values far larger than its own have gone before).
+// O^T is held in units of 2^(T + E - lift) and the row sum in units of 2^(R - lift), R the reference of the
+// logits alone: what a row's values are like has no part in the sum.  T, E and R are whole numbers, so that
+// every rescale is a power of two.  What contributes less than 2^-90 of the largest value held may be lost.
 #pragma once
 #include "qcache.cuh"
 
@@ -42,9 +49,20 @@ namespace curdkv {
 namespace token {
 
 constexpr int kStages = 3;
-constexpr float kSlack = 6.f;        // log2 units a logit may exceed the running maximum
-constexpr float kLift = 8.f;         // fp16 weights are 2^(x - m + kLift): at most 2^14, and exact
-                                     // to 11 bits down to 2^-22 of the largest
+// Log2 units a logit may exceed the running maximum; fp16 weights are 2^(x - m + kLift): at most 2^15.
+template <bool Q4>
+__host__ __device__ constexpr float slack() { return Q4 ? 4.f : 6.f; }
+constexpr float kLift = 11.f;
+// A tile's products are taken in fp16 when its scales lie in [2^(E - span), 2^E) and its zeros in
+// [2^(E - kZeroDown), 2^(E + kZeroUp)), where both are exact.  Weight times scale then loses bits below 2^-14, by at
+// most 2^-25 a key, of 2^(kLift - 1 - span - far) that the key of the largest logit has: 2^-10 of the sum of magnitudes
+// for 2^n keys, were all errors alike, with a span of 24 - n; far adds one more step (below).
+constexpr int kZeroUp = 14, kZeroDown = 17;
+constexpr int kLeastSpan = 8, kMostSpan = 14;
+__device__ __forceinline__ int span_of(int keys) { return min(max(__clz(max(keys - 1, 1)) - 8, kLeastSpan), kMostSpan); }
+constexpr int kLeastE = -126, kMostE = 112;                // 2^-E is a normal number, and an infinite zero is outside
+constexpr int kMostAbove = 60;       // how far values may lie above 2^E
+constexpr int kFar = 1;              // T - R above which fp16 weights have too few bits
 
 struct Args {
   const __nv_bfloat16* Q;            // [batch][q_heads][q_n][128], strides in elements
@@ -65,8 +83,8 @@ struct Args {
   const int32_t* seqlens;
   const int32_t* q_lens;
   int n_max, num_sink, window;
-  // partial results, two per CTA (of the item its run begins in, of the one it ends in): [8 NT] maxima
-  // and sums, [8 NT][128] sums of values; and where each item begins on the line, [items + 1]
+  // partial results, two per CTA (of the item its run begins in, of the one it ends in): [8 NT] references,
+  // sums and units (Part), [8 NT][128] sums of values; and where each item begins on the line, [items + 1]
   float* part_ml;
   float* part_o;
   int64_t* begins;
@@ -126,11 +144,6 @@ __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t rank) {
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
-__device__ __forceinline__ float2 peer_float2(uint32_t addr) {
-  float2 v;
-  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
-  return v;
-}
 __device__ __forceinline__ float4 peer_float4(uint32_t addr) {
   float4 v;
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
@@ -139,6 +152,25 @@ __device__ __forceinline__ float4 peer_float4(uint32_t addr) {
 }
 // 2^(e - 127) for 1 <= e <= 253, and 0 below
 __device__ __forceinline__ float pow2_biased(int e) { return __int_as_float(e > 0 ? e << 23 : 0); }
+// 2^d for whole d < 127, 0 below 2^-126, and back: whole numbers pass through the low bits of 1.5 * 2^23 + d
+// (the conversion instructions take several times as long)
+__device__ __forceinline__ float pow2_whole(float d) {
+  return __int_as_float(__float_as_int(fmaxf(d, -127.f) + (12582912.f + 127.f)) << 23);
+}
+__device__ __forceinline__ int exponent_of(float pow2) { return (__float_as_int(pow2) >> 23) - 127; }
+__device__ __forceinline__ float whole_of(float pow2) {
+  return __int_as_float((__float_as_int(pow2) >> 23) + 0x4b400000) - (12582912.f + 127.f);
+}
+
+// What a warp, or several, have of one query: sum = sum of 2^(x - ref), and sums of values in units of
+// 2^(ref + unit), where the unit says how large the values are (0 for bf16 rows).
+struct Part {
+  float ref, sum, unit;
+};
+// Joining parts: `all` is the largest reference, `unit` the largest of unit + (ref - all).  A part's sum
+// counts 2^(ref - all), its values 2^(unit + (ref - all) - that unit).
+__device__ __forceinline__ float above(const Part& p, float all) { return p.unit + (p.ref - all); }
+__device__ __forceinline__ float share(float d, float all) { return all == -INFINITY ? 1.f : exp2_approx(d); }   // (all -inf: zeros, or NaN)
 
 template <bool Q4>
 struct Tile {                                              // one warp's stage
@@ -148,9 +180,8 @@ struct Tile {                                              // one warp's stage
   static constexpr int kKMeta = 2 * kV;
   static constexpr int kVMeta = kKMeta + (Q4 ? kKeys * qcache::kMetaBytes : 0);
   static constexpr int kBytes = kVMeta + (Q4 ? kKeys * qcache::kMetaBytes : 0);
-  // V's scales and zeros in fp16, pairs of keys side by side: [key pair][group] each; then e and 2^-e
-  // of each key
-  static constexpr int kScaled = Q4 ? kKeys * (8 * 2 + 8) : 0;
+  // V's scales and zeros in fp16, pairs of keys side by side: [key pair][group] each
+  static constexpr int kScaled = Q4 ? kKeys * 8 * 2 : 0;
   static constexpr int kWarpBytes = kStages * kBytes + kScaled;
 };
 // Four warps a CTA, one on each of the SM's schedulers (six a CTA, two CTAs, left two schedulers with
@@ -221,6 +252,91 @@ struct Item {
 // CTA whose run holds tile x of a line of `total` tiles cut into `runs` runs [i total / runs, ...).
 __device__ __forceinline__ int cta_of(int64_t x, int64_t total, int64_t runs) { return (int)(((x + 1) * runs - 1) / total); }
 
+// V's 16-bit words number g of four-bit rows `key` and `key` + 1 of a stage side by side, one register a group.
+__device__ __forceinline__ void v_words(const unsigned char* st, int key, int g, uint32_t (&y)[4]) {
+  uint2 v[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int c = (key + k) * 4 + (g >> 1), line = c >> 3;
+    v[k] = *reinterpret_cast<const uint2*>(st + Tile<true>::kV + line * 128 + (((c & 7) ^ (2 * (line & 3))) * 16) + 8 * (g & 1));
+  }
+  y[0] = __byte_perm(v[0].x, v[1].x, 0x5410);
+  y[1] = __byte_perm(v[0].x, v[1].x, 0x7632);
+  y[2] = __byte_perm(v[0].y, v[1].y, 0x5410);
+  y[3] = __byte_perm(v[0].y, v[1].y, 0x7632);
+}
+
+// O^T += V^T P^T of a tile whose scales and zeros fp16 does not hold: in bf16, weights (times scale) in two pieces; codes as
+// numbers, those one nibble up times 16 as in the other form, and 2^-24 with the scales, so that the units are the same.
+// (Some 1.8 times the other form's time: 64 heads of 131072 rows, every tile so, 425 us against 235.  As a
+// function called with copies of the accumulators four times.)
+template <int NT>
+__device__ __forceinline__ void wide_products(float (&acc)[NT][8][4], float (&accz)[NT][4], const float (&weights)[NT][2][4],
+                                              const unsigned char* st, float inv) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  auto pieces = [&](float a, float b, uint32_t& most, uint32_t& rest) {
+    const uint32_t top2 = pack_bf16(a, b);
+    most = transpose8x8(top2);
+    rest = transpose8x8(pack_bf16(a - __uint_as_float(top2 << 16), b - __uint_as_float(top2 & 0xffff0000u)));
+  };
+  auto number = [](uint32_t code) {                        // 0 .. 15 in each half -> bf16
+    const uint32_t up = code | 0x43004300u, base = 0x43004300u;                // 128 + code, 128
+    const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&up), *reinterpret_cast<const __nv_bfloat162*>(&base));
+    return *reinterpret_cast<const uint32_t*>(&d);
+  };
+  auto times16 = [](uint32_t v) {
+    const __nv_bfloat162 d = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v), __float2bfloat162_rn(16.f));
+    return *reinterpret_cast<const uint32_t*>(&d);
+  };
+#pragma unroll
+  for (int kb16 = 0; kb16 < 2; ++kb16) {
+    const uint32_t* meta = reinterpret_cast<const uint32_t*>(st + Tile<true>::kVMeta) + kb16 * 64;
+    uint32_t y[2][4], z[2] = {0u, 0u};
+    v_words(st, kb16 * 16 + 2 * t, g, y[0]);
+    v_words(st, kb16 * 16 + 8 + 2 * t, g, y[1]);
+    if (g < 4) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        z[i] = pack_bf16(__uint_as_float(meta[(8 * i + 2 * t) * 4 + g] & 0xffff0000u) * inv,
+                         __uint_as_float(meta[(8 * i + 2 * t + 1) * 4 + g] & 0xffff0000u) * inv);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float(&w)[4] = weights[nt][kb16];
+      uint32_t most[2], rest[2];
+      pieces(w[0], w[1], most[0], rest[0]);
+      pieces(w[2], w[3], most[1], rest[1]);
+      mma_bf16(accz[nt], z[0], 0u, z[1], 0u, most[0], most[1]);
+      mma_bf16(accz[nt], z[0], 0u, z[1], 0u, rest[0], rest[1]);
+    }
+#pragma unroll
+    for (int gr = 0; gr < 4; ++gr) {
+      uint32_t v[2][4];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          v[i][k] = number((y[i][gr] >> (4 * k)) & 0x000f000fu);
+          if (k & 1) v[i][k] = times16(v[i][k]);
+        }
+      const float sa = __uint_as_float(meta[g * 4 + gr] << 16) * inv * 0x1p-24f;
+      const float sb = __uint_as_float(meta[(8 + g) * 4 + gr] << 16) * inv * 0x1p-24f;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float(&w)[4] = weights[nt][kb16];
+        uint32_t most[2], rest[2];
+        pieces(w[0] * sa, w[1] * sa, most[0], rest[0]);
+        pieces(w[2] * sb, w[3] * sb, most[1], rest[1]);
+        mma_bf16(acc[nt][2 * gr], v[0][0], v[0][1], v[1][0], v[1][1], most[0], most[1]);
+        mma_bf16(acc[nt][2 * gr], v[0][0], v[0][1], v[1][0], v[1][1], rest[0], rest[1]);
+        mma_bf16(acc[nt][2 * gr + 1], v[0][2], v[0][3], v[1][2], v[1][3], most[0], most[1]);
+        mma_bf16(acc[nt][2 * gr + 1], v[0][2], v[0][3], v[1][2], v[1][3], rest[0], rest[1]);
+      }
+    }
+  }
+}
+
 constexpr int kMostSplit = 3;                              // log2 of the CTAs of a cluster
 constexpr int kMostItems = 8192;                           // items that are put on one line
 
@@ -229,8 +345,8 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
   using T = Tile<Q4>;
   constexpr int KB = T::kKeys / 16;
   extern __shared__ __align__(128) unsigned char smem[];
-  __shared__ float s_m[kWarps][8 * NT], s_l[kWarps][8 * NT];
-  __shared__ float2 s_ml[8 * NT];                          // the CTA's maxima and sums (clusters)
+  __shared__ Part s_part[kWarps][8 * NT];
+  __shared__ float4 s_ml[8 * NT];                          // the CTA's references, sums and units
   __shared__ int64_t s_sum[kWarps], s_at;
   __shared__ int s_item;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -451,7 +567,20 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
   const int pos_lo = pos0 + r0 / a.group, pos_hi = pos0 + (r1 - 1) / a.group;
 
   float acc[NT][8][4], accz[NT][4];                        // O^T: 128 channels x queries 2t, 2t + 1; zeros' part
-  float m[NT][2], l[NT][2];
+  // m: reference of the weights (T for 4-bit rows); l: row sum; rise: 2^(T - R)
+  float m[NT][2], l[NT][2], rise[NT][2];
+  // (this warp's share of the run's keys)
+  const int span = span_of(((t_hi - t_lo + kWarps - 1) / kWarps) * T::kKeys);
+  int vexp;                                                // E
+  uint32_t below_hi, from_lo;                              // what brings what lies too high, or high enough, to bit 15
+  auto set_unit = [&](int e) {
+    vexp = e;
+    const int hi = 128 * (e + 127), lo = hi - 128 * span - 1, zero_lo = hi - 128 * kZeroDown - 1;
+    below_hi = (uint32_t)(0x8000 - hi) | (uint32_t)(0x8000 - hi - 128 * kZeroUp) << 16;
+    from_lo = (uint32_t)(0x8000 - max(lo, 0)) | (uint32_t)(0x8000 - max(zero_lo, 0)) << 16;
+  };
+  set_unit(kLeastE);
+  bool far = false;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -462,6 +591,7 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
     for (int j = 0; j < 4; ++j) accz[nt][j] = 0.f;
     m[nt][0] = m[nt][1] = -INFINITY;
     l[nt][0] = l[nt][1] = 0.f;
+    rise[nt][0] = rise[nt][1] = 1.f;
   }
 
   // ------------------------------------------------------------ the key loop
@@ -480,39 +610,28 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
     const int u0 = tile * T::kKeys;
     const int left = seen.total - u0;
 
-    // ---- V's scales and zeros of this tile in fp16, each row's relative to a power of two of its own
-    if constexpr (Q4) {
+    // ---- do V's scales and zeros lie where E has them?  (largest and least of the row's, bf16 bits side by side, 0 apart)
+    auto v_meta = [&](uint32_t (&w)[4]) {
       const uint4 v = *reinterpret_cast<const uint4*>(st + T::kVMeta + lane * 16);
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-      uint32_t top = w[0] & 0x7fff7fffu;                   // largest |zero| and largest scale, bf16 side by side
+      w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    };
+    auto extremes = [](const uint32_t (&w)[4], uint32_t& top, uint32_t& low) {
+      top = w[0] & 0x7fff7fffu;
+      low = top - 0x00010001u;                             // (0 becomes the largest)
 #pragma unroll
-      for (int gr = 1; gr < 4; ++gr) top = __vmaxu2(top, w[gr] & 0x7fff7fffu);
-      // bits of the larger of |zero| and 16 * scale (a scale of 0 gives 2^-123, which the limit below covers)
-      const uint32_t big = max(top & 0x7fff0000u, (top << 16) + (4u << 23));
-      // biased exponent above it; rows far below the tile's largest (rows of zeros among them) take one
-      // near it, so that their weights stay numbers
-      int e = min(max((int)(big >> 23) + 1, 37), 250);       // (sums of 2^20 weights times 2^-e stay numbers)
-      e = max(e, __reduce_max_sync(0xffffffffu, e) - 30);
-      const float inv = pow2_biased(254 - e);
-      *reinterpret_cast<float2*>(ring + kStages * T::kBytes + T::kKeys * 16 + lane * 8) = make_float2((float)(e - 127), inv);
-      // lanes 2 i and 2 i + 1 hold a pair of keys: the even one takes the pair's groups 0 and 1, the odd
-      // one 2 and 3
-      uint32_t sz[2][2];                                   // [scale, zero][groups 0-1, 2-3] of this key
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        sz[0][i] = pack_f16(__uint_as_float(w[2 * i] << 16) * inv, __uint_as_float(w[2 * i + 1] << 16) * inv);
-        sz[1][i] = pack_f16(__uint_as_float(w[2 * i] & 0xffff0000u) * inv, __uint_as_float(w[2 * i + 1] & 0xffff0000u) * inv);
+      for (int gr = 1; gr < 4; ++gr) {
+        const uint32_t x = w[gr] & 0x7fff7fffu;
+        top = __vmaxu2(top, x);
+        low = __vminu2(low, x - 0x00010001u);
       }
-      const bool odd = lane & 1;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? sz[k][0] : sz[k][1], 1);
-        const uint32_t keep = odd ? sz[k][1] : sz[k][0];
-        const uint32_t ev = odd ? got : keep, od = odd ? keep : got;                 // key 2 i, key 2 i + 1
-        *reinterpret_cast<uint2*>(ring + kStages * T::kBytes + k * (T::kKeys * 8) + lane * 8) =
-            make_uint2(__byte_perm(ev, od, 0x5410), __byte_perm(ev, od, 0x7632));
-      }
-      __syncwarp();
+      low = __vminu2(low, 0x7fff7fffu);
+    };
+    bool elsewhere = false;
+    if constexpr (Q4) {
+      uint32_t w[4], top, low;
+      v_meta(w);
+      extremes(w, top, low);
+      elsewhere = (((top + below_hi) | ~(low + from_lo)) & 0x80008000u) != 0u;
     }
     // ---- S^T
     float s[NT][KB][4];
@@ -575,21 +694,13 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
         }
       }
     }
-    // ---- logits in log2 units (4-bit rows: plus the row's e); what a query does not see becomes -inf
-    float took[KB][2];                                     // 2^-e of keys g, g + 8
+    // ---- logits in log2 units; what a query does not see becomes -inf
 #pragma unroll
     for (int kb16 = 0; kb16 < KB; ++kb16)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        float2 f = make_float2(0.f, 1.f);
-        if (Q4) f = *reinterpret_cast<const float2*>(ring + kStages * T::kBytes + T::kKeys * 16 + (kb16 * 16 + 8 * i + g) * 8);
-        took[kb16][i] = f.y;
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int c = 0; c < 2; ++c)
-            s[nt][kb16][2 * i + c] = Q4 ? fmaf(s[nt][kb16][2 * i + c], unit[nt][c], f.x) : s[nt][kb16][2 * i + c] * unit[nt][c];
-      }
+        for (int j = 0; j < 4; ++j) s[nt][kb16][j] *= unit[nt][j & 1];
     bool masked = left < T::kKeys;
     if (!Q4) {
       // a tile that every query of the block sees whole needs no comparison
@@ -615,7 +726,7 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
         }
     }
     // ---- running maximum
-    bool move = false;
+    bool move = elsewhere;
     float top[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -625,9 +736,51 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
 #pragma unroll
         for (int kb16 = 1; kb16 < KB; ++kb16) x = fmaxf(x, fmaxf(s[nt][kb16][c], s[nt][kb16][2 + c]));
         top[nt][c] = x;
-        move = move || x > m[nt][c] + kSlack;
+        move = move || x > m[nt][c] + slack<Q4>();
       }
+    bool wide = false;                                     // fp16 does not hold this tile's scales and zeros
     if (__any_sync(0xffffffffu, move)) {
+      int shift = 0;                                       // by how much this tile moves E
+      if (Q4 && __any_sync(0xffffffffu, elsewhere)) {
+        uint32_t w[4], top, low;
+        v_meta(w);
+        extremes(w, top, low);
+        const int hi = max((int)(top & 0xffffu), (int)(top >> 16) - 128 * kZeroUp);
+        const int lo = min((int)(low & 0xffffu), (int)(low >> 16) + 128 * (kZeroDown - span));
+        auto outside = [&](int h, int l, int e) { return h >= 128 * (e + 127) || l < 128 * (e + 127 - span) - 1; };
+        int th = (int)__reduce_max_sync(0xffffffffu, (unsigned)max(hi, 0));
+        const int tl = (int)__reduce_min_sync(0xffffffffu, (unsigned)lo);
+        const bool huge = th >= 128 * (kMostE + 127);      // a NaN or an infinity among them, perhaps
+        if (huge) {
+          int h = 0;                                       // the largest of the others
+#pragma unroll
+          for (int gr = 0; gr < 4; ++gr) {
+            const int sc = (int)(w[gr] & 0x7fffu), ze = (int)((w[gr] >> 16) & 0x7fffu);
+            h = max(h, max(sc >= 0x7f80 ? 0 : sc, ze >= 0x7f80 ? 0 : ze - 128 * kZeroUp));
+          }
+          th = (int)__reduce_max_sync(0xffffffffu, (unsigned)h);
+        }
+        const int own = (th >> 7) - 126;                   // every scale is below 2^own
+        // A tile that fits by itself brings its E, but not one so low that fp16 weights would lose their bits against
+        // the accumulators' unit: later tiles would then all pay for this one.  One that does not keeps E, unless its
+        // values lie too far above (then E is such that rows like its smaller ones fit next).
+        int to = vexp;
+        wide = huge || outside(th, tl, own);
+        if (!wide) {
+          to = own;
+          if (own < vexp) {
+            int up = 0;                                    // of the accumulators' unit over 2^E
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) up = max(up, max(exponent_of(rise[nt][0]), exponent_of(rise[nt][1])));
+            wide = __any_sync(0xffffffffu, vexp - own + up > kFar);
+            if (wide) to = vexp;
+          }
+        } else if (own > vexp + kMostAbove) {
+          to = min(kMostE, max(own - kMostAbove, min(own, (tl >> 7) - 127 + span / 2)));
+        }
+        shift = to - vexp;
+        set_unit(to);
+      }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -635,10 +788,22 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
           float x = top[nt][c];
 #pragma unroll
           for (int o = 4; o <= 16; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-          const float now = fmaxf(m[nt][c], x);
-          const float f = now == -INFINITY ? 1.f : exp2_approx(m[nt][c] - now);   // 0 on the first rows
-          m[nt][c] = now;
-          l[nt][c] *= f;
+          float f;                                         // 0 on the first rows
+          if (Q4) {
+            // T + E of the accumulators stays where it is or rises; R rises with the logits alone
+            const float r = m[nt][c] - whole_of(rise[nt][c]), was = m[nt][c] - (float)shift;
+            x = ceilf(x);
+            const float r_now = fmaxf(r, x), now = fmaxf(fmaxf(was, x), r_now - 100.f);
+            f = now == -INFINITY ? 1.f : pow2_whole(was - now);
+            l[nt][c] *= now == -INFINITY ? 1.f : pow2_whole(r - r_now);
+            rise[nt][c] = now == -INFINITY ? 1.f : pow2_whole(now - r_now);
+            m[nt][c] = now;
+          } else {
+            const float now = fmaxf(m[nt][c], x);
+            f = now == -INFINITY ? 1.f : exp2_approx(m[nt][c] - now);
+            m[nt][c] = now;
+            l[nt][c] *= f;
+          }
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             acc[nt][i][c] *= f;
@@ -646,6 +811,12 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
           }
           accz[nt][c] *= f;
         }
+      if (Q4) {
+        bool above_r = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) above_r = above_r || fmaxf(rise[nt][0], rise[nt][1]) > (float)(1 << kFar);
+        far = __any_sync(0xffffffffu, above_r);
+      }
     }
     // ---- weights and O^T
     float nref[NT][2];
@@ -653,18 +824,48 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int c = 0; c < 2; ++c) nref[nt][c] = (Q4 ? kLift : 0.f) - (m[nt][c] == -INFINITY ? 0.f : m[nt][c]);
+    // the weights take the logits' place
+    auto weigh = [&](float (&w)[4], int nt) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = exp2_approx(w[j] + nref[nt][j & 1]);
+      if (Q4) {
+        l[nt][0] = fmaf(w[2], rise[nt][0], fmaf(w[0], rise[nt][0], l[nt][0]));
+        l[nt][1] = fmaf(w[3], rise[nt][1], fmaf(w[1], rise[nt][1], l[nt][1]));
+      } else {
+        l[nt][0] = w[2] + (w[0] + l[nt][0]);
+        l[nt][1] = w[3] + (w[1] + l[nt][1]);
+      }
+    };
+    if (!Q4 || __builtin_expect(!(wide || far), 1)) {
+    if constexpr (Q4) {
+      // V's scales and zeros in fp16: lanes 2 i and 2 i + 1 hold a pair of keys; the even one takes the pair's groups 0 and
+      // 1, the odd one 2 and 3
+      const float inv = pow2_biased(127 - vexp);
+      uint32_t w[4], sz[2][2];                             // [scale, zero][groups 0-1, 2-3] of this key
+      v_meta(w);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        sz[0][i] = pack_f16(__uint_as_float(w[2 * i] << 16) * inv, __uint_as_float(w[2 * i + 1] << 16) * inv);
+        sz[1][i] = pack_f16(__uint_as_float(w[2 * i] & 0xffff0000u) * inv, __uint_as_float(w[2 * i + 1] & 0xffff0000u) * inv);
+      }
+      const bool odd = lane & 1;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? sz[k][0] : sz[k][1], 1);
+        const uint32_t keep = odd ? sz[k][1] : sz[k][0];
+        const uint32_t ev = odd ? got : keep, od = odd ? keep : got;                 // key 2 i, key 2 i + 1
+        *reinterpret_cast<uint2*>(ring + kStages * T::kBytes + k * (T::kKeys * 8) + lane * 8) =
+            make_uint2(__byte_perm(ev, od, 0x5410), __byte_perm(ev, od, 0x7632));
+      }
+      __syncwarp();
+    }
 #pragma unroll
     for (int kb16 = 0; kb16 < KB; ++kb16) {
       uint32_t pt[NT][2];                                  // P^T as B operand: keys 2t, 2t + 1 / 2t + 8, 2t + 9 of query g
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        float w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          w[j] = exp2_approx(s[nt][kb16][j] + nref[nt][j & 1]);
-        }
-        l[nt][0] = fmaf(w[2], took[kb16][1], fmaf(w[0], took[kb16][0], l[nt][0]));
-        l[nt][1] = fmaf(w[3], took[kb16][1], fmaf(w[1], took[kb16][0], l[nt][1]));
+        float(&w)[4] = s[nt][kb16];
+        weigh(w, nt);
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           pt[nt][i] = transpose8x8(Q4 ? pack_f16(w[2 * i], w[2 * i + 1]) : pack_bf16(w[2 * i], w[2 * i + 1]));
@@ -674,16 +875,9 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
         uint32_t x[2][4][4], sc[2][4], z[2];               // [keys 2t.. / 2t + 8..][group][nibble]
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int key = kb16 * 16 + 8 * i + 2 * t, pair = key >> 1;
-          uint2 v[2];
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int c = (key + k) * 4 + (g >> 1), line = c >> 3;
-            v[k] = *reinterpret_cast<const uint2*>(st + T::kV + line * 128 + (((c & 7) ^ (2 * (line & 3))) * 16) + 8 * (g & 1));
-          }
-          // 16-bit words of the two keys side by side, one register a group
-          const uint32_t y[4] = {__byte_perm(v[0].x, v[1].x, 0x5410), __byte_perm(v[0].x, v[1].x, 0x7632),
-                                 __byte_perm(v[0].y, v[1].y, 0x5410), __byte_perm(v[0].y, v[1].y, 0x7632)};
+          const int pair = (kb16 * 16 + 8 * i + 2 * t) >> 1;
+          uint32_t y[4];
+          v_words(st, kb16 * 16 + 8 * i + 2 * t, g, y);
 #pragma unroll
           for (int gr = 0; gr < 4; ++gr) {
             const uint32_t hi = y[gr] >> 8;
@@ -717,6 +911,13 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
         }
       }
     }
+    } else if constexpr (Q4) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int kb16 = 0; kb16 < KB; ++kb16) weigh(s[nt][kb16], nt);
+      wide_products<NT>(acc, accz, s, st, pow2_biased(127 - vexp));
+    }
     __syncwarp();                                          // the stage may be filled again
     stage = stage == kStages - 1 ? 0 : stage + 1;
   }
@@ -730,8 +931,13 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
 #pragma unroll
       for (int o = 4; o <= 16; o <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], o);
       if (g == 0) {
-        s_m[warp][8 * nt + 2 * t + c] = m[nt][c];
-        s_l[warp][8 * nt + 2 * t + c] = l[nt][c];
+        Part own = {m[nt][c], l[nt][c], 0.f};
+        if (Q4) {
+          const int up = exponent_of(rise[nt][c]);
+          own.ref -= (float)up;
+          own.unit = (float)(vexp + up);
+        }
+        s_part[warp][8 * nt + 2 * t + c] = own;
       }
     }
   __syncthreads();                                         // also: every warp is done with its ring
@@ -741,10 +947,21 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
       const int qi = 8 * nt + 2 * t + c;
-      float all = -INFINITY;
+      float all = -INFINITY, unit = Q4 ? -INFINITY : 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) all = fmaxf(all, s_m[w][qi]);
-      const float f = m[nt][c] == -INFINITY ? 0.f : exp2_approx(m[nt][c] - all);
+      for (int w = 0; w < kWarps; ++w) all = fmaxf(all, s_part[w][qi].ref);
+      if (Q4) {
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) unit = fmaxf(unit, above(s_part[w][qi], all));
+      }
+      if (warp == 0) {
+        float sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) sum = fmaf(s_part[w][qi].sum, share(s_part[w][qi].ref - all, all), sum);
+        if (g == 0) s_ml[qi] = make_float4(Q4 ? all - kLift : all, sum, unit, 0.f);
+        __syncwarp();
+      }
+      const float f = share(Q4 ? above(s_part[warp][qi], all) - unit : m[nt][c] - all, all);
       float* dst = meet + ((size_t)warp * 8 * NT + qi) * 132;
       if (Q4) {
 #pragma unroll
@@ -766,14 +983,15 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
       }
     }
   __syncthreads();
-  // one row's four channels: O = sums / sum, and its log sum
-  auto finish = [&](int qi, int c4, const float4& o, float top, float sum) {
+  // one row's four channels: O = sums / sum in units of 2^unit, and its log sum
+  auto finish = [&](int qi, int c4, const float4& o, float top, float sum, float unit) {
     const int r = r0 + qi, i = r / a.group, hq = h * a.group + r % a.group;
     if (i >= q_live) return;                               // rows behind the last query stay as they are
     const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);     // a NaN sum stays one
+    const float up = Q4 ? exp2_approx(unit) : 1.f;         // (apart from the sum's: either may be far from 1)
     uint2 v;
-    v.x = pack_bf16(o.x * inv, o.y * inv);
-    v.y = pack_bf16(o.z * inv, o.w * inv);
+    v.x = pack_bf16(o.x * inv * up, o.y * inv * up);
+    v.y = pack_bf16(o.z * inv * up, o.w * inv * up);
     *reinterpret_cast<uint2*>(a.O + b * a.o_sb + (int64_t)hq * a.o_sh + (int64_t)i * a.o_sn + c4) = v;
     if (c4 == 0 && a.lse != nullptr)
       a.lse[((int64_t)b * a.heads * a.group + hq) * a.q_n + i] =
@@ -781,30 +999,21 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
   };
   for (int e = tid; e < (r1 - r0) * 32; e += kThreads) {
     const int qi = e >> 5, c4 = (e & 31) * 4;
-    float all = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) all = fmaxf(all, s_m[w][qi]);
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) sum += all == -INFINITY ? 0.f : s_l[w][qi] * exp2_approx(s_m[w][qi] - all);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
       const float4 x = *reinterpret_cast<const float4*>(meet + ((size_t)w * 8 * NT + qi) * 132 + c4);
       o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
     }
-    if (Q4) all -= kLift;
     if (a.split > 0) {                                     // (only this thread reads these four places)
       *reinterpret_cast<float4*>(meet + (size_t)qi * 132 + c4) = o;
-      if (c4 == 0) s_ml[qi] = make_float2(all, sum);
     } else if (t_hi - t_lo < it.tiles) {                   // a part: of the item this run begins or ends in
       const size_t at = ((size_t)blockIdx.x * 2 + (t_lo == 0 ? 1 : 0)) * 8 * NT + qi;
       *reinterpret_cast<float4*>(a.part_o + at * 128 + c4) = o;
-      if (c4 == 0) {
-        a.part_ml[at * 2] = all;
-        a.part_ml[at * 2 + 1] = sum;
-      }
+      if (c4 == 0) reinterpret_cast<float4*>(a.part_ml)[at] = s_ml[qi];
     } else {
-      finish(qi, c4, o, all, sum);
+      const float4 ml = s_ml[qi];
+      finish(qi, c4, o, ml.x, ml.y, ml.z);
     }
   }
   if (a.ctas == 0) {
@@ -821,25 +1030,31 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
     for (int e = rank * kThreads + tid; e < (r1 - r0) * 32; e += kThreads << a.split) {
       const int qi = e >> 5, c4 = (e & 31) * 4;
       const uint32_t ml = smem_addr(&s_ml[qi]), at = smem_addr(meet + (size_t)qi * 132 + c4);
-      float2 part[1 << kMostSplit];
+      Part part[1 << kMostSplit];
       float4 x[1 << kMostSplit];
-      float all = -INFINITY, sum = 0.f;
+      float all = -INFINITY, sum = 0.f, unit = -INFINITY;
 #pragma unroll
       for (int c = 0; c < (1 << kMostSplit); ++c) {
         if (c >> a.split) break;
-        part[c] = peer_float2(peer_addr(ml, c));
+        const float4 y = peer_float4(peer_addr(ml, c));
+        part[c] = Part{y.x, y.y, y.z};
         x[c] = peer_float4(peer_addr(at, c));
-        all = fmaxf(all, part[c].x);
+        all = fmaxf(all, part[c].ref);
+      }
+#pragma unroll
+      for (int c = 0; c < (1 << kMostSplit); ++c) {
+        if (c >> a.split) break;
+        unit = fmaxf(unit, above(part[c], all));
       }
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int c = 0; c < (1 << kMostSplit); ++c) {
         if (c >> a.split) break;
-        const float f = all == -INFINITY ? 1.f : exp2_approx(part[c].x - all);                 // (all -inf: zeros, or NaN)
-        sum = fmaf(f, part[c].y, sum);
+        const float f = share(above(part[c], all) - unit, all);
+        sum = fmaf(share(part[c].ref - all, all), part[c].sum, sum);
         o.x = fmaf(f, x[c].x, o.x); o.y = fmaf(f, x[c].y, o.y); o.z = fmaf(f, x[c].z, o.z); o.w = fmaf(f, x[c].w, o.w);
       }
-      finish(qi, c4, o, all, sum);
+      finish(qi, c4, o, all, sum, unit);
     }
     cluster_sync();                                        // nobody leaves while its parts are read
     flag();
@@ -851,8 +1066,7 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
   }
 }
 
-// Joins the parts of items that several CTAs share: O = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) l_c,
-// in the order of the CTAs.  grid = items * block_rows, block = 32 (four channels a lane).
+// Joins the parts of items that several CTAs share (Part), in the order of the CTAs.  grid = items * block_rows, block = 32 (four channels a lane).
 __global__ void __launch_bounds__(32) join_kernel(const Args a, int block_rows) {
   asm volatile("griddepcontrol.wait;" ::: "memory");       // behind the last CTA of attend_kernel
   const int item = blockIdx.x / block_rows, qi = blockIdx.x % block_rows;
@@ -868,23 +1082,34 @@ __global__ void __launch_bounds__(32) join_kernel(const Args a, int block_rows) 
   // the item begins in c0 (its second part) and goes on in the others (their first)
   auto part = [&](int c) { return ((size_t)c * 2 + (c == c0 ? 1 : 0)) * block_rows + qi; };
   // maxima and sums: a lane per part; sums of values: four parts in flight
-  const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
   auto at = [&](int c) { return part(min(c, c1)); };
+  auto head = [&](int c) {
+    const float4 y = reinterpret_cast<const float4*>(a.part_ml)[at(c)];
+    return Part{y.x, y.y, y.z};
+  };
   auto values = [&](int c) { return *reinterpret_cast<const float4*>(a.part_o + at(c) * 128 + lane * 4); };
-  const float2 first = ml[at(c0 + lane)];
+  const Part first = head(c0 + lane);
   float4 x[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) x[k] = values(c0 + k);
-  float all = first.x;
-  for (int c = c0 + 32 + lane; c <= c1; c += 32) all = fmaxf(all, ml[part(c)].x);
+  auto most = [](float v) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+  };
+  float all = first.ref;
+  for (int c = c0 + 32 + lane; c <= c1; c += 32) all = fmaxf(all, head(c).ref);
+  all = most(all);
+  float unit = above(first, all);
+  for (int c = c0 + 32 + lane; c <= c1; c += 32) unit = fmaxf(unit, above(head(c), all));
+  unit = most(fmaxf(unit, -INFINITY));                     // (not a NaN, where all is -inf)
   float sum = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int cb = c0; cb <= c1; cb += 32) {
-    const float2 e = cb == c0 ? first : ml[at(cb + lane)];
-    const float f = cb + lane > c1 ? 0.f : (all == -INFINITY ? 1.f : exp2_approx(e.x - all));      // (all -inf: zeros, or NaN)
-    float l = f * e.y;
+    const Part e = cb == c0 ? first : head(cb + lane);
+    const bool live = cb + lane <= c1;
+    const float f = live ? share(above(e, all) - unit, all) : 0.f;
+    float l = live ? share(e.ref - all, all) * e.sum : 0.f;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
     sum += l;
@@ -904,9 +1129,10 @@ __global__ void __launch_bounds__(32) join_kernel(const Args a, int block_rows) 
     }
   }
   const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
+  const float up = exp2_approx(unit);                      // 1 for bf16 rows
   uint2 v;
-  v.x = pack_bf16(o.x * inv, o.y * inv);
-  v.y = pack_bf16(o.z * inv, o.w * inv);
+  v.x = pack_bf16(o.x * inv * up, o.y * inv * up);
+  v.y = pack_bf16(o.z * inv * up, o.w * inv * up);
   *reinterpret_cast<uint2*>(a.O + b * a.o_sb + (int64_t)hq * a.o_sh + (int64_t)i * a.o_sn + lane * 4) = v;
   if (lane == 0 && a.lse != nullptr)
     a.lse[((int64_t)b * a.heads * a.group + hq) * a.q_n + i] =

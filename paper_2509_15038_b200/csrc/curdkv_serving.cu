@@ -125,7 +125,7 @@ Plan plan_token(int64_t problems, int64_t rows, int64_t keys, int64_t total, int
   const size_t parts = room ? 2 * (size_t)slots * 8 * pl.nt : 0;
   pl.begins_at = 256;
   pl.ml_at = pl.begins_at + round256(room ? (size_t)(items + 1) * sizeof(int64_t) : 0);
-  pl.o_at = pl.ml_at + round256(parts * 2 * sizeof(float));
+  pl.o_at = pl.ml_at + round256(parts * 4 * sizeof(float));
   pl.bytes = pl.o_at + round256(parts * 128 * sizeof(float));
   return pl;
 }

@@ -530,3 +530,123 @@ def test_attention_flags_bad_heads_in_every_form(B, H, cap, launches, bad):
         assert n == launches or bad == "row_start"
         assert cur.curdkv_device_status(ws) == cur.DEV_BAD_INDEX
         _check_attention(O, lse, Q, cache, held, starts, float(np.float32(0.0884)), f"{(B, H, cap, bad)}")
+
+
+def _check_wild(O, lse, Q, cache, counts, starts, scale, what=""):
+    """_check_attention's budget for values of any size, NaN among them: a channel is NaN where the oracle's is and nowhere
+    else, and every other channel is held to the budget by its own channel's values.  Below it, what is less than 2^-90 of
+    the head's largest value counts as nothing."""
+    got, Qf = _f64(O), _f64(Q)
+    kc, vc = cache.K_codes.cpu().numpy().reshape(-1, 64), cache.V_codes.cpu().numpy().reshape(-1, 64)
+    km, vm = _bits(cache.K_meta.reshape(-1, 8)), _bits(cache.V_meta.reshape(-1, 8))
+    H = Q.shape[1]
+    for p, c in enumerate(counts):
+        b, h = divmod(p, H)
+        rows = slice(starts[p], starts[p] + c)
+        k, kp = orc.unpack(kc[rows], km[rows], "K")
+        v, vp = orc.unpack(vc[rows], vm[rows], "V")
+        q = Qf[b, h]
+        want, want_lse, w = orc.attend(q, k, v, np.ones((q.shape[0], c), dtype=bool), scale)
+        d = 2.0 ** -20 * scale * (np.abs(q) @ kp.T).max(-1)
+        rel = 2.0 ** -10 + 2 * d + 2.0 ** -18
+        least = 2.0 ** -90 * np.abs(v[np.isfinite(v)]).max(initial=0.0)
+        tol = 2.0 ** -8 * np.abs(want) + rel[:, None] * (w @ vp) * (1 + 2.0 ** -7) + least + 1e-38
+        nan = np.isnan(want)
+        assert np.array_equal(np.isnan(got[b, h]), nan), f"{what} p={p}: NaN in other channels"
+        err = np.abs(got[b, h] - want)
+        assert np.all((err <= tol)[~nan]), f"{what} p={p} count={c}: {np.max((err / tol)[~nan]):.3g} of the tolerance"
+        assert np.all(np.abs(lse[b, h].cpu().numpy() - want_lse) <= d + 2.0 ** -20 * (1 + np.abs(want_lse)) + 2.0 ** -18), what
+
+
+def _attend_wild(V, seed, q_rows=4, K=None, scale=0.0884, Q=None, what=""):
+    H, n = V.shape[1:3]
+    K = _rand((1, H, n, 128), seed) if K is None else K
+    cache = cur.QuantCache(1, H, n)
+    cur.curdkv_qcache_store(cache, K, V, cur.make_desc(K, V, 1))
+    Q = _rand((1, H, q_rows, 128), seed + 1) if Q is None else Q
+    lse = torch.zeros((1, H, Q.shape[2]), device=DEV)
+    O, ws = cur.curdkv_qcache_attention(Q, cache, scale=scale, lse=lse)
+    assert cur.curdkv_device_status(ws) == 0
+    _check_wild(O, lse, Q, cache, [n] * H, [h * n for h in range(H)], float(np.float32(scale)), what)
+
+
+@pytest.mark.parametrize("n", [20, 128, 700, 20000])
+@pytest.mark.parametrize("power", [10, 13, 16, 20, 40, 90, -10, -20, -40, -90])
+def test_attention_one_group_of_one_row_far_from_the_rest(n, power):
+    """One group of one V row 2^power times as large as everything else: the other 96 channels, and the other rows, keep
+    their precision.  The row stands at the start, in the middle and at the end of a head."""
+    V = _rand((1, 3, n, 128), 500).float()
+    for h, row in enumerate((0, n // 2, n - 1)):
+        V[0, h, row, 32 * h + 32: 32 * h + 64] *= 2.0 ** power
+    _attend_wild(V.to(torch.bfloat16), 501, q_rows=4 if n > 700 else 16, what=f"{n} 2^{power}")
+
+
+@pytest.mark.parametrize("n", [20, 128, 700, 20000])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_attention_non_finite_values_stay_in_their_group(n, value):
+    V = _rand((1, 3, n, 128), 510)
+    for h, row in enumerate((0, n // 2, n - 1)):
+        V[0, h, row, 32 * h + 5] = value
+    _attend_wild(V, 511, what=f"{n} {value}")
+    V[0, 0, :, 127] = value                                  # and a whole group of a head
+    _attend_wild(V, 512, q_rows=9, what=f"{n} {value}")
+
+
+@pytest.mark.parametrize("n", [33, 700, 20000])
+@pytest.mark.parametrize("kind", ["rows", "groups", "channels", "tiles", "single", "offsets", "sparse"])
+def test_attention_values_of_every_size_side_by_side(n, kind):
+    """Magnitudes between 2^-40 and 2^40 that differ from row to row, from group to group, from channel to channel, from tile to
+    tile; rows of a single channel; groups on a large offset; rows that are mostly zero."""
+    g = torch.Generator(device=DEV).manual_seed(520)
+    V = torch.randn((1, 2, n, 128), generator=g, device=DEV)
+    rand = lambda *shape: 80 * torch.rand(shape, generator=g, device=DEV) - 40  # noqa: E731
+    if kind == "rows":
+        V = V * torch.exp2(rand(1, 2, n, 1))
+    elif kind == "groups":
+        V = V * torch.exp2(rand(1, 2, n, 4)).repeat_interleave(32, -1)
+    elif kind == "channels":
+        V = V * torch.exp2(rand(1, 2, n, 128))
+    elif kind == "tiles":
+        V = V * torch.exp2(rand(1, 2, (n + 31) // 32, 1)).repeat_interleave(32, 2)[:, :, :n]
+    elif kind == "single":
+        V = V * 2.0 ** 30 * (torch.rand(V.shape, generator=g, device=DEV) < 0.01)
+        V[:, :, 1::2] = torch.randn((1, 2, n // 2, 128), generator=g, device=DEV).abs()
+    elif kind == "offsets":
+        V = V + torch.exp2(rand(1, 2, n, 4) / 3).repeat_interleave(32, -1)
+    else:
+        V = torch.where(torch.rand((1, 2, n, 4), generator=g, device=DEV) < 0.2, torch.exp2(rand(1, 2, n, 4)), 0.0).repeat_interleave(32, -1) * V
+    _attend_wild(V.to(torch.bfloat16), 521, q_rows=4 if n > 700 else 11, what=f"{n} {kind}")
+
+
+@pytest.mark.parametrize("n", [96, 700, 20000])
+@pytest.mark.parametrize("slope", [30.0, -30.0, 90.0, -90.0])
+def test_attention_values_against_the_logits(n, slope):
+    """Values that grow or fall by 2^slope along the head while the logits fall or grow by some 2^40: what matters for the
+    output is not what matters for the row sum."""
+    ramp = torch.linspace(0, 1, n, device=DEV)
+    V = _rand((1, 2, n, 128), 530).float() * torch.exp2(slope * (ramp - 0.5))[:, None]
+    K = _rand((1, 2, n, 128), 531, 0.2).float()
+    K[..., 0] = 28 * ramp
+    Q = _rand((1, 2, 4, 128), 532, 0.2)
+    Q[..., 0] = torch.tensor([-1.0, 1.0, -0.3, 0.0], device=DEV)
+    _attend_wild(V.to(torch.bfloat16), 533, K=K.to(torch.bfloat16), Q=Q, scale=1.0, what=f"{n} {slope}")
+
+
+@pytest.mark.parametrize("big", [1e6, 1e12, 1e20, 1e30])
+@pytest.mark.parametrize("n", [64, 128, 2048, 24000])
+def test_attention_rows_of_zeros_beside_large_ones(n, big):
+    """Equal weights: the mean of the rows, and log n, whatever half of them is zero or 2^-100 of the others."""
+    for small in (0.0, 1e-6):
+        V = torch.full((1, 2, n, 128), small, device=DEV)
+        V[0, 0, n // 2:] = big
+        V[0, 1, : n // 2] = big
+        V = V.to(torch.bfloat16)
+        cache = cur.QuantCache(1, 2, n)
+        K = _rand((1, 2, n, 128), 540)
+        cur.curdkv_qcache_store(cache, K, V, cur.make_desc(K, V, 1))
+        lse = torch.zeros((1, 2, 3), device=DEV)
+        O, _ = cur.curdkv_qcache_attention(_rand((1, 2, 3, 128), 541), cache, scale=0.0, lse=lse)
+        want = 0.5 * V[0, 0, -1, 0].double() + 0.5 * V[0, 0, 0, 0].double()
+        # weights, and their products with a scale of 0: exact; the fp32 sums of n equal terms and O's rounding remain
+        assert torch.all((O.double() - want).abs() <= want * (2.0 ** -8 + 2.0 ** -18)), (big, small)
+        assert torch.all((lse.double() - np.log(n)).abs() <= 2.0 ** -18 + 2.0 ** -20 * np.log(n))
