@@ -352,6 +352,8 @@ curdkv_status curdkv_cache_step(const curdkv_cache* cache, const void* K_new, co
  * channels; a group with least value lo and greatest hi is held as
  *   scale = bf16((hi - lo) * (1/15))   fp32 subtraction and product with the fp32 number next to 1/15,
  *                                      rounded to bf16 (nearest even)
+ *                                      (as PyTorch divides a CUDA tensor by 15; a bf16 number nearest to
+ *                                      the quotient, the upper one of two as near in some cases)
  *   zero  = lo                      (a bf16 value: no rounding)
  *   code  = rint((x - zero) / scale), ties to even, limited to 0 .. 15 (0 when scale is 0),
  *           decided as in 64-bit arithmetic

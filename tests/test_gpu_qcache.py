@@ -650,3 +650,35 @@ def test_attention_rows_of_zeros_beside_large_ones(n, big):
         # weights, and their products with a scale of 0: exact; the fp32 sums of n equal terms and O's rounding remain
         assert torch.all((O.double() - want).abs() <= want * (2.0 ** -8 + 2.0 ** -18)), (big, small)
         assert torch.all((lse.double() - np.log(n)).abs() <= 2.0 ** -18 + 2.0 ** -20 * np.log(n))
+
+
+def test_store_scales_whose_quotient_lies_between_two_numbers():
+    """Groups with hi - lo = 15 m, m midway between two bf16 numbers: the scale is the written rule's, bf16 of the fp32 product
+    with fp32(1/15), which is one of the two numbers nearest to the quotient: half a step off, and the product's own 2^-24."""
+    los = -(128 + np.arange(128)) * 2.0 ** -13                           # 8-bit numbers of [2^-6, 2^-5)
+    rows = [(8.5625, -0.021484375)]
+    for lo in los:                                                       # 12-bit differences: hi has to be a bf16 number too
+        for odd in range(257, 512, 2):                                   # m = odd / 2^9 ... times a power of two
+            for e in range(-8, 8):
+                hi = 15 * odd * 2.0 ** (e - 9) + lo
+                if hi > 0 and hi == float(orc.bf16_value(orc.bf16_bits(hi))):
+                    rows.append((hi, lo))
+    rows = rows[: 4 * (len(rows) // 4)]
+    assert len(rows) >= 4
+    x = np.zeros((len(rows), 32))
+    x[:, 0], x[:, 1] = np.asarray(rows).T
+    x = x.reshape(-1, 128)
+    K = torch.tensor(x, dtype=torch.float64).to(torch.bfloat16).view(1, 1, -1, 128).to(DEV)
+    assert np.array_equal(_f64(K)[0, 0], x)
+    cache = cur.QuantCache(1, 1, x.shape[0])
+    cur.curdkv_qcache_store(cache, K, K, cur.make_desc(K, K, 1))
+    d = np.asarray(rows)[:, 0] - np.asarray(rows)[:, 1]
+    for meta in (cache.K_meta, cache.V_meta):
+        s = _f64(meta)[0, 0, :, :, 0].reshape(-1)
+        assert np.array_equal(s, orc.bf16_value(orc.bf16_bits(d.astype(np.float32) * np.float32(1 / 15))))
+        step = 2.0 ** (np.floor(np.log2(s)) - 7)
+        assert np.all(np.abs(s - d / 15) <= 0.5 * step + 2.0 ** -23 * s)
+        assert s[0] == 0.57421875
+    # and as PyTorch has it
+    t = ((K.float().unflatten(-1, (4, 32)).amax(-1) - K.float().unflatten(-1, (4, 32)).amin(-1)) / 15).to(torch.bfloat16)
+    assert torch.equal(t[0, 0], cache.K_meta[0, 0, :, :, 0])
