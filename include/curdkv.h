@@ -403,7 +403,7 @@ curdkv_status curdkv_qcache_append(const curdkv_qcache* cache, const void* K_new
  *   idx NULL, rows = 0    outputs laid out as the cache's rows are
  *   idx                   int32 [batch*kv_heads][rows]: output row t is slot idx[..][t]; a negative entry
  *                         is passed over, one at or beyond count is flagged (CURDKV_DEV_BAD_INDEX)
- * Output rows that have no slot are left untouched.  The outputs may not be the rows that the cache
+ * Output rows that have no slot are left untouched.  K_out and V_out may not overlap, nor be the rows that the cache
  * was stored from while another call still reads them.  workspace as in curdkv_qcache_store. */
 curdkv_status curdkv_qcache_read(const curdkv_qcache* cache, const int32_t* idx, int64_t rows,
                                  void* K_out, void* V_out, void* workspace, void* cuda_stream);
@@ -411,7 +411,8 @@ curdkv_status curdkv_qcache_read(const curdkv_qcache* cache, const int32_t* idx,
 /* O = softmax(scale Q K^T) V over the held rows of every head, for generation: few query rows per
  * KV head (the queries of a GQA group stacked along q_rows), every one sees every held row.
  *   Q, O   bf16 [batch][kv_heads][q_rows][128] with element strides (multiples of 8, channels
- *          contiguous, 16-byte aligned); O may not overlap Q
+ *          contiguous, 16-byte aligned); O may not overlap Q, nor a row of O another (by ascending
+ *          stride, each axis steps over all that the ones before it reach)
  *   lse    NULL, or fp32 [batch][kv_heads][q_rows]: log of each row's sum of exponentials (natural,
  *          of the scaled logits), for joining partial attentions
  *   scale  finite, >= 0
@@ -439,7 +440,7 @@ curdkv_status curdkv_qcache_attention(const void* Q, int32_t q_rows, int64_t q_s
  *   j > position - window   or   j < num_sink.
  *   Q, O      bf16 [batch][q_heads][q_rows][128] with element strides (multiples of 8, channels
  *             contiguous, 16-byte aligned); query head q reads KV head q / (q_heads / kv_heads);
- *             O may not overlap Q
+ *             O may not overlap Q, nor a row of O another (as above)
  *   q_lens    device int32 [batch] (clamped to [0, q_rows]), or NULL; output rows i >= t_b are left
  *             untouched
  *   window    >= 0; n_max or more is plain causal attention; num_sink >= 0

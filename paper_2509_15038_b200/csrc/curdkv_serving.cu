@@ -227,6 +227,28 @@ bool query_strides_ok(const void* x, int64_t sb, int64_t sh, int64_t sn) {
   return x != nullptr && aligned16(x) && sb >= 0 && sh >= 0 && sn >= 128 && sb % 8 == 0 && sh % 8 == 0 && sn % 8 == 0;
 }
 
+// Rows that are written may not share memory with one another: by ascending stride, each axis has to step over all
+// that the ones before it reach.  (An axis of one never steps.)
+bool rows_apart(int64_t batch, int64_t heads, int64_t rows, int64_t sb, int64_t sh, int64_t sn) {
+  int64_t size[3] = {batch, heads, rows}, step[3] = {sb, sh, sn};
+  __int128 reach = 128;
+  for (int done = 0; done < 3; ++done) {
+    int least = -1;
+    for (int i = 0; i < 3; ++i)
+      if (size[i] > 1 && (least < 0 || step[i] < step[least])) least = i;
+    if (least < 0) break;
+    if (step[least] < reach) return false;
+    reach += (__int128)(size[least] - 1) * step[least];
+    size[least] = 1;
+  }
+  return true;
+}
+
+bool overlap(const void* a, const void* b, __int128 bytes) {
+  const __int128 x = (__int128)reinterpret_cast<uintptr_t>(a), y = (__int128)reinterpret_cast<uintptr_t>(b);
+  return x < y + bytes && y < x + bytes;
+}
+
 }  // namespace
 
 extern "C" {
@@ -296,6 +318,9 @@ curdkv_status curdkv_qcache_read(const curdkv_qcache* cache, const int32_t* idx,
   if (rows < 0 || (idx != nullptr && rows < 1) || rows > 0x7fffffffLL || !status_ok(workspace))
     return CURDKV_ERR_INVALID_ARG;
   const int64_t P = (int64_t)cache->batch * cache->kv_heads;
+  const int64_t out_rows = rows > 0 ? rows : cache->capacity;                // of a head, or of all of a packed cache
+  if (overlap(K_out, V_out, (__int128)(rows > 0 || cache->row_start == nullptr ? P : 1) * out_rows * 256))
+    return CURDKV_ERR_INVALID_ARG;
   if (P == 0) return CURDKV_OK;
   qcache::ReadArgs a;
   a.cache = view_of(cache);
@@ -325,7 +350,8 @@ curdkv_status curdkv_qcache_attention(const void* Q, int32_t q_rows, int64_t q_s
   if (st != CURDKV_OK) return st;
   if (q_rows < 1 || !(scale >= 0.f) || std::isinf(scale)) return CURDKV_ERR_INVALID_ARG;
   if (!query_strides_ok(Q, q_stride_b, q_stride_h, q_stride_n) ||
-      !query_strides_ok(O, o_stride_b, o_stride_h, o_stride_n) || Q == O)
+      !query_strides_ok(O, o_stride_b, o_stride_h, o_stride_n) || Q == O ||
+      !rows_apart(cache->batch, cache->kv_heads, q_rows, o_stride_b, o_stride_h, o_stride_n))
     return CURDKV_ERR_INVALID_ARG;
   if (workspace == nullptr || !status_ok(workspace)) return CURDKV_ERR_INVALID_ARG;
   const Plan pl = plan_qcache(cache, q_rows);
@@ -377,7 +403,8 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
   if (desc->d != 128) return CURDKV_ERR_UNSUPPORTED;
   if (q_rows < 1 || num_sink < 0 || window < 0 || !(scale >= 0.f) || std::isinf(scale)) return CURDKV_ERR_INVALID_ARG;
   if (!query_strides_ok(Q, q_stride_b, q_stride_h, q_stride_n) ||
-      !query_strides_ok(O, o_stride_b, o_stride_h, o_stride_n) || Q == O)
+      !query_strides_ok(O, o_stride_b, o_stride_h, o_stride_n) || Q == O ||
+      !rows_apart(desc->batch, desc->q_heads, q_rows, o_stride_b, o_stride_h, o_stride_n))
     return CURDKV_ERR_INVALID_ARG;
   if (workspace == nullptr || !status_ok(workspace)) return CURDKV_ERR_INVALID_ARG;
   // the most rows a block of queries sees: its window, the tokens between, the sinks

@@ -196,3 +196,27 @@ def test_numbers_beyond_int32_are_not_cut(monkeypatch, big):
     assert got == [(4, 2 ** 31 - 1), (2 ** 31 - 1, 4), (0, -1), (-1, 0), (0, 7)]
     with pytest.raises(TypeError):
         call(1.5, 0)
+
+
+@pytest.mark.parametrize("call,os,kw", [
+    (_attend, (1024, 0, 128), {}), (_attend, (1024, 384, 128), {}), (_attend, (1024, 128, 128), {}), (_attend, (1024, 128, 136), {}),
+    (_attend, (0, 512, 128), dict(c=_cache(batch=2))), (_attend, (1016, 512, 128), dict(c=_cache(batch=2))),
+    (_window, (4096, 0, 128), {}), (_window, (4096, 504, 128), {}), (_window, (4096, 128, 1016), {}),
+    (_window, (128, 512, 128), dict(d=_desc(batch=2))), (_window, (0, 512, 128), dict(d=_desc(batch=2))),
+])
+def test_output_rows_that_share_memory(call, os, kw):
+    """Rows of O that lie over one another, as those of an expanded tensor, would be written by several at once."""
+    before = cur.launch_count()
+    assert call(os=os, **kw) == 1
+    assert cur.launch_count() == before
+
+
+def test_read_into_one_buffer_twice():
+    lib, before = cur.load(), cur.launch_count()
+    rows = 2 * 4 * 256                                       # bytes of 2 heads of 4 rows
+    for k, v in ((ANY, ANY), (ANY, ANY + rows - 16), (ANY + rows - 16, ANY)):
+        assert lib.curdkv_qcache_read(ctypes.byref(_cache()), None, 4, k, v, None, None) == 1
+        assert lib.curdkv_qcache_read(ctypes.byref(_cache()), ANY, 4, k, v, None, None) == 1
+        assert lib.curdkv_qcache_read(ctypes.byref(_cache(capacity=4)), None, 0, k, v, None, None) == 1
+        assert lib.curdkv_qcache_read(ctypes.byref(_cache(capacity=8, row_start=ANY)), None, 0, k, v, None, None) == 1
+    assert cur.launch_count() == before
