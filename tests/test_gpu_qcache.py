@@ -682,3 +682,100 @@ def test_store_scales_whose_quotient_lies_between_two_numbers():
     # and as PyTorch has it
     t = ((K.float().unflatten(-1, (4, 32)).amax(-1) - K.float().unflatten(-1, (4, 32)).amin(-1)) / 15).to(torch.bfloat16)
     assert torch.equal(t[0, 0], cache.K_meta[0, 0, :, :, 0])
+
+
+def _line_case(seed, packed):
+    """Few long heads, which equal runs over all of them and a joining launch take."""
+    counts = [20000, 0, 1, 7777, 33, 12000]
+    cache, starts = _random_cache(3, 2, 20000, counts, seed, packed)
+    return cache, starts, counts
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_attention_over_equal_runs_captured_and_replayed(packed):
+    """Replayed with other rows, counts and queries, and after another call on the same workspace."""
+    cache, starts, counts = _line_case(600, packed)
+    Q, lse = _rand((3, 2, 4, 128), 601), torch.zeros((3, 2, 4), device=DEV)
+    O, ws = torch.zeros_like(Q), cur.qcache_attention_workspace(cache, 4)
+    call = lambda: cur.curdkv_qcache_attention(Q, cache, scale=0.0884, O=O, lse=lse, workspace=ws)  # noqa: E731
+    assert _launches(call) == 2
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(4):
+        Q.copy_(_rand(Q.shape, 610 + i))
+        cache.V_codes.bitwise_xor_(0x5A)
+        now = [counts[0] - 100 * i, 0, 1, counts[3] - 5000 * (i % 2), 33 - i, 4000 * i]
+        cache.count.copy_(torch.tensor(now, dtype=torch.int32))
+        if i == 2:
+            cache.count.zero_()                              # nothing at all: one replay of zeros
+            now = [0] * 6
+        graph.replay()
+        _check_attention(O, lse, Q, cache, now, starts, float(np.float32(0.0884)), f"{packed} {i}")
+        first = O.clone()
+        graph.replay()
+        assert torch.equal(first, O)
+    assert cur.curdkv_device_status(ws) == 0
+
+
+def test_attention_over_equal_runs_side_by_side():
+    """Two streams, a workspace each, both with their joining launch; one of them packed."""
+    sets = []
+    for i in range(2):
+        cache, starts, counts = _line_case(620 + 10 * i, bool(i))
+        Q = _rand((3, 2, 3, 128), 640 + i)
+        sets.append((cache, starts, counts, Q, torch.zeros_like(Q), torch.zeros((3, 2, 3), device=DEV),
+                     cur.qcache_attention_workspace(cache, 3), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    before = cur.launch_count()
+    for _ in range(20):
+        for s in sets:
+            with torch.cuda.stream(s[7]):
+                cur.curdkv_qcache_attention(s[3], s[0], scale=0.1, O=s[4], lse=s[5], workspace=s[6])
+    torch.cuda.synchronize()
+    assert cur.launch_count() - before == 80
+    for s in sets:
+        _check_attention(s[4], s[5], s[3], s[0], s[2], s[1], float(np.float32(0.1)))
+        assert cur.curdkv_device_status(s[6]) == 0
+
+
+@pytest.mark.parametrize("q_rows", [1, 8, 9, 40])
+def test_attention_over_equal_runs_stale_rows_and_untouched_memory(q_rows):
+    """NaN behind the held rows, and a workspace of exactly the stated size: nothing behind it is written."""
+    cache, starts, counts = _line_case(650, False)
+    for p, c in enumerate(counts):
+        cache.K_meta.view(6, 20000, 4, 2)[p, c:] = float("nan")
+        cache.V_meta.view(6, 20000, 4, 2)[p, c:] = float("nan")
+    Q, lse = _rand((3, 2, q_rows, 128), 651), torch.zeros((3, 2, q_rows), device=DEV)
+    size = cur.qcache_attention_workspace(cache, q_rows).numel()
+    buf = torch.full((size + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+    buf[:256] = 0
+    call = lambda: cur.curdkv_qcache_attention(Q, cache, scale=0.1, lse=lse, workspace=buf[:size])  # noqa: E731
+    O, _ = call()
+    assert _launches(call) == 2
+    assert torch.all(buf[size:] == 0xA5) and cur.curdkv_device_status(buf) == 0
+    _check_attention(O, lse, Q, cache, counts, starts, float(np.float32(0.1)))
+    with pytest.raises(cur.CurdkvError, match="status 3"):
+        cur.curdkv_qcache_attention(Q, cache, scale=0.1, workspace=buf[: size - 1])
+
+
+@pytest.mark.parametrize("q_rows", [1, 20])
+def test_attention_over_more_heads_than_a_line_holds(q_rows):
+    """More than 8192 heads (or blocks of rows): one CTA each, a workspace without parts."""
+    B, H, cap = 1100, 8, 40
+    rng = np.random.default_rng(3)
+    counts = rng.integers(0, cap + 1, B * H)
+    cache, starts = _random_cache(B, H, cap, counts.tolist(), 660)
+    Q, lse = _rand((B, H, q_rows, 128), 661), torch.zeros((B, H, q_rows), device=DEV)
+    ws = cur.qcache_attention_workspace(cache, q_rows)
+    assert ws.numel() == 256
+    assert _launches(lambda: cur.curdkv_qcache_attention(Q, cache, scale=0.1, lse=lse, workspace=ws)) == 1
+    O, _ = cur.curdkv_qcache_attention(Q, cache, scale=0.1, lse=lse, workspace=ws)
+    assert cur.curdkv_device_status(ws) == 0
+    kc, vc = (x.view(B * H, cap, 64) for x in (cache.K_codes, cache.V_codes))
+    km, vm = (x.view(B * H, cap, 4, 2) for x in (cache.K_meta, cache.V_meta))
+    for p in [0, 1, 8191, 8192, B * H - 1] + rng.integers(0, B * H, 20).tolist():
+        one = cur.QuantCache.of(*(x[p][None, None].contiguous() for x in (kc, vc, km, vm)), cache.count[p:p + 1].clone(), 1, 1)
+        b, h = divmod(p, H)
+        _check_attention(O[b:b + 1, h:h + 1], lse[b:b + 1, h:h + 1], Q[b:b + 1, h:h + 1], one, [int(counts[p])], [0],
+                         float(np.float32(0.1)), f"head {p}")

@@ -344,3 +344,69 @@ def test_few_tokens_however_the_keys_are_shared_out(B, H, n, window, t):
     lens = [n - 7 * b if b % 5 else n for b in range(B)]
     lens[-1] = n if B == 1 else 1
     _run(B, H, 4, n, t, window, 4, lens=lens, q_lens=[min(t, x) for x in lens], seed=240, heads=[0, 4 * H - 1])
+
+
+@pytest.mark.parametrize("t", [1, 6])
+def test_few_tokens_over_equal_runs_replayed_and_beside_another_call(t):
+    """One long head, which equal runs and a joining launch take: captured, replayed with other rows and lengths, while another
+    such call runs on a second stream with a workspace of its own."""
+    n, window, sink = 12000, 11000, 4
+    K, V = _rand((1, 1, n, 128), 300), _rand((1, 1, n, 128), 301)
+    lens = torch.tensor([n], dtype=torch.int32, device=DEV)
+    desc = cur.make_desc(K, V, 1, q_heads=2, seqlens=lens)
+    Q = _rand((1, 2, t, 128), 302)
+    O, lse = torch.zeros_like(Q), torch.zeros(Q.shape[:3], device=DEV)
+    size = cur.attention_window_workspace(desc, t).numel()
+    buf = torch.full((size + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+    buf[:256] = 0
+    call = lambda: cur.curdkv_attention_window(Q, K, V, desc, window, num_sink=sink, scale=0.1, O=O, lse=lse, workspace=buf[:size])  # noqa: E731
+    before = cur.launch_count()
+    call()
+    assert cur.launch_count() - before == 2
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    side, oq, oo = torch.cuda.Stream(), _rand(Q.shape, 303), torch.zeros_like(Q)
+    ows = cur.attention_window_workspace(desc, t)
+    for now in (n, 9001, 17, n - 1):
+        K.copy_(_rand(K.shape, 310 + now))
+        Q.copy_(_rand(Q.shape, 320 + now))
+        lens.fill_(now)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            cur.curdkv_attention_window(oq, K, V, desc, n, scale=0.1, O=oo, workspace=ows)
+        graph.replay()
+        torch.cuda.current_stream().wait_stream(side)
+        _check(O, lse, Q, K, V, [now], [t], window, sink, float(np.float32(0.1)), what=f"{now}")
+        _check(oo, None, oq, K, V, [now], [t], n, 0, float(np.float32(0.1)), what=f"{now} beside")
+    assert torch.all(buf[size:] == 0xA5) and cur.curdkv_device_status(buf) == 0 and cur.curdkv_device_status(ows) == 0
+
+
+@pytest.mark.parametrize("n", [1, 100, 5000, 40000])
+@pytest.mark.parametrize("q_rows", [1, 5, 64, 200])
+def test_the_stated_workspace_is_enough_for_every_window(n, q_rows):
+    """The size call knows no window: what it says serves any, plans for the window's keys included."""
+    K = _rand((2, 2, n, 128), 330)
+    desc = cur.make_desc(K, K, 1, q_heads=4)
+    size = cur.attention_window_workspace(desc, q_rows).numel()
+    Q = _rand((2, 4, q_rows, 128), 331)
+    buf = torch.full((size + 4096,), 0xA5, dtype=torch.uint8, device=DEV)
+    buf[:256] = 0
+    for window, sink in ((0, 0), (1, 0), (0, 4), (17, 4), (1000, 4), (4096, 0), (n, 0), (2 ** 31 - 1, 2 ** 31 - 1)):
+        lse = torch.zeros(Q.shape[:3], device=DEV)
+        O, _ = cur.curdkv_attention_window(Q, K, K, desc, window, num_sink=sink, scale=0.1, lse=lse, workspace=buf[:size])
+        assert torch.all(buf[size:] == 0xA5) and cur.curdkv_device_status(buf) == 0
+        t = min(q_rows, n)                                   # queries before the first row see nothing
+        assert not O[:, :, :q_rows - t].any()
+        _check(O[:, :, q_rows - t:], lse[:, :, q_rows - t:], Q[:, :, q_rows - t:], K, K, [n, n], [t, t], window, sink,
+               float(np.float32(0.1)), heads=[0, 3], what=f"{window} {sink}")
+        with pytest.raises(cur.CurdkvError, match="status 3"):
+            cur.curdkv_attention_window(Q, K, K, desc, window, num_sink=sink, scale=0.1, workspace=buf[: size - 1])
+
+
+@pytest.mark.parametrize("t", [1, 3])
+def test_few_tokens_over_more_heads_than_a_line_holds(t):
+    B = 1100
+    lens = [(37 * b) % 61 for b in range(B)]
+    Q, K, V, desc, O = _run(B, 8, 1, 60, t, 20, 4, lens=lens, q_lens=[min(t, x) for x in lens], seed=340, heads=[0, 7])
+    assert cur.attention_window_workspace(desc, t).numel() == 256
