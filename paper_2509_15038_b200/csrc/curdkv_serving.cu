@@ -1,6 +1,7 @@
 // Serving calls: the 4-bit cache (store, append, read, attention) and the attention with a sliding
 // window and sinks.  Argument checks and kernel launches.
 #include <atomic>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 
@@ -373,9 +374,7 @@ curdkv_status curdkv_qcache_attention(const void* Q, int32_t q_rows, int64_t q_s
   a.items = (int)(P * pl.blocks);
   a.ctas = pl.ctas;
   a.split = pl.split;
-  // (a masked product is -inf, and -inf times a scale of 0 would be NaN)
   a.scale_log2 = scale * 1.4426950408889634f;
-  if (a.scale_log2 < 1e-30f) a.scale_log2 = 1e-30f;
   a.cache = view_of(cache);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   a.begins = reinterpret_cast<int64_t*>(ws + pl.begins_at);
@@ -416,8 +415,7 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
   const int64_t P = (int64_t)desc->batch * desc->kv_heads;
   if (P == 0) return CURDKV_OK;
   const int group = desc->q_heads / desc->kv_heads;
-  // a masked product is -inf, and -inf times a scale of 0 would be NaN
-  const float scale_log2 = scale * 1.4426950408889634f > 1e-30f ? scale * 1.4426950408889634f : 1e-30f;
+  const float scale_log2 = scale * 1.4426950408889634f;
   const int64_t tiles = ((int64_t)q_rows + kTileRows - 1) / kTileRows * group, pairs = (tiles + 1) / 2;
   if (desc->n_max > 0 && (int64_t)desc->n_max + q_rows < (1 << 30) && P * pairs <= 0x3fffffffLL &&
       prompt_form(P, (int64_t)group * q_rows, tiles, (int64_t)window + num_sink, desc->n_max) &&
@@ -439,7 +437,8 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
     wa.n_max = desc->n_max;
     wa.num_sink = num_sink < desc->n_max ? num_sink : desc->n_max;
     wa.window = window < desc->n_max ? window : desc->n_max;
-    wa.scale_log2 = scale_log2;
+    // (this form masks products before it scales them, and -inf times 0 would be NaN)
+    wa.scale_log2 = scale_log2 > FLT_MIN ? scale_log2 : FLT_MIN;
     wa.O = static_cast<__nv_bfloat16*>(O);
     wa.o_sb = o_stride_b; wa.o_sh = o_stride_h; wa.o_sn = o_stride_n;
     wa.lse = lse;

@@ -779,3 +779,12 @@ def test_attention_over_more_heads_than_a_line_holds(q_rows):
         b, h = divmod(p, H)
         _check_attention(O[b:b + 1, h:h + 1], lse[b:b + 1, h:h + 1], Q[b:b + 1, h:h + 1], one, [int(counts[p])], [0],
                          float(np.float32(0.1)), f"head {p}")
+
+
+@pytest.mark.parametrize("scale", [0.0, 1e-32, 1e-36])
+def test_attention_tiny_scales_with_large_products(scale):
+    counts = [500, 3]
+    cache, starts = _random_cache(1, 2, 512, counts, 670, k_gain=1e16)
+    Q, lse = _rand((1, 2, 4, 128), 671, 1e15), torch.zeros((1, 2, 4), device=DEV)
+    O, _ = cur.curdkv_qcache_attention(Q, cache, scale=scale, lse=lse)
+    _check_attention(O, lse, Q, cache, counts, starts, float(np.float32(scale)))

@@ -410,3 +410,16 @@ def test_few_tokens_over_more_heads_than_a_line_holds(t):
     lens = [(37 * b) % 61 for b in range(B)]
     Q, K, V, desc, O = _run(B, 8, 1, 60, t, 20, 4, lens=lens, q_lens=[min(t, x) for x in lens], seed=340, heads=[0, 7])
     assert cur.attention_window_workspace(desc, t).numel() == 256
+
+
+@pytest.mark.parametrize("B,H,t", [(1, 2, 1), (1, 2, 5), (3, 8, 250)])
+@pytest.mark.parametrize("scale", [0.0, 1e-32, 1e-36])
+def test_tiny_scales_with_large_products(B, H, t, scale):
+    """A scale of 0 averages whatever the products are (1e32 here), and tiny ones are not taken for larger ones."""
+    K, Q = _rand((B, H, 400, 128), 350, 1e16), _rand((B, 2 * H, t, 128), 351, 1e15)
+    V = _rand((B, H, 400, 128), 352)
+    desc = cur.make_desc(K, V, 1, q_heads=2 * H)
+    lse = torch.zeros(Q.shape[:3], device=DEV)
+    O, ws = cur.curdkv_attention_window(Q, K, V, desc, 300, num_sink=4, scale=scale, lse=lse)
+    assert cur.curdkv_device_status(ws) == 0
+    _check(O, lse, Q, K, V, [400] * B, [t] * B, 300, 4, float(np.float32(scale)), heads=[0, 2 * H - 1])
