@@ -379,7 +379,8 @@ typedef struct curdkv_qcache {
  * and sets count.  What a cache held before is gone.
  *   idx           NULL: the desc->seqlens / n_max rows of every head in order.  Else the rows to hold,
  *                 as curdkv_select writes them: int32 [batch][kv_heads][idx_stride] with head_offsets
- *                 NULL, or packed with head p's list starting at idx[head_offsets[p]]
+ *                 NULL, or packed with head p's list starting at idx[head_offsets[p]] (idx_stride then the
+ *                 number of entries idx has, behind which no list is followed, or 0)
  *   head_counts   int32 [batch*kv_heads] entries of each list (required with idx)
  *   workspace     NULL, or at least 256 bytes, 256-byte aligned, whose status word collects (it is
  *                 not cleared): CURDKV_DEV_BAD_INDEX -- an index outside [0, n_b), whose slot becomes a

@@ -604,6 +604,7 @@ def curdkv_qcache_store(cache: QuantCache, K, V, desc: Desc, idx=None, head_coun
         if head_offsets is None:
             raise ValueError("a packed idx needs head_offsets")
         _int32("head_offsets", head_offsets, P + 1)
+        stride = idx.numel()
     elif idx is not None:
         if P > 0 and idx.numel() % P != 0:
             raise ValueError("idx must be [batch, kv_heads, budget]")

@@ -237,7 +237,7 @@ struct StoreArgs {
   const int32_t* idx;                // or nullptr: every row
   const int32_t* head_counts;        // with idx
   const int32_t* head_offsets;       // packed idx, or nullptr
-  int64_t idx_stride;                // fixed idx
+  int64_t idx_stride;                // fixed idx; packed: entries of idx, or 0
   int heads, n_max, ctas_per_head;
   uint32_t* status;                  // or nullptr
 };
@@ -266,6 +266,7 @@ __global__ void __launch_bounds__(kStoreWarps * 32, 4) store_kernel(const StoreA
     if (a.head_offsets != nullptr) {
       at = a.head_offsets[p];
       listed = (int64_t)a.head_offsets[p + 1] - at;
+      if (a.idx_stride > 0) listed = min(listed, a.idx_stride - at);       // nothing behind idx is read
     }
     if (at < 0 || offered < 0 || offered > listed) {       // a count beyond the index row: corrupted
       ok = false;

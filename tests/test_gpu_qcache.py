@@ -788,3 +788,27 @@ def test_attention_tiny_scales_with_large_products(scale):
     Q, lse = _rand((1, 2, 4, 128), 671, 1e15), torch.zeros((1, 2, 4), device=DEV)
     O, _ = cur.curdkv_qcache_attention(Q, cache, scale=scale, lse=lse)
     _check_attention(O, lse, Q, cache, counts, starts, float(np.float32(scale)))
+
+
+def test_store_lists_that_run_beyond_their_index():
+    """A packed index shorter than its offsets say (those of another selection): lists are cut at its end and flagged, nothing
+    behind it is read."""
+    K, V = _rand((1, 3, 64, 128), 680), _rand((1, 3, 64, 128), 681)
+    desc = cur.make_desc(K, V, 1)
+    store = torch.full((64,), 1 << 20, dtype=torch.int32, device=DEV)    # what lies behind the index would be out of range
+    store[:24] = torch.arange(24, dtype=torch.int32, device=DEV)
+    counts = torch.tensor([10, 10, 10], dtype=torch.int32, device=DEV)
+    for entries, off, held in ((24, [0, 10, 20, 30], [10, 10, 4]), (10, [0, 10, 20, 30], [10, 0, 0]), (24, [0, 10, 40, 50], [10, 10, 0])):
+        cache, ws = cur.QuantCache(1, 3, 12), torch.zeros(256, dtype=torch.uint8, device=DEV)
+        cur.curdkv_qcache_store(cache, K, V, desc, store[:entries], counts, torch.tensor(off, dtype=torch.int32, device=DEV), packed=True,
+                                workspace=ws)
+        assert cur.curdkv_device_status(ws) == cur.DEV_BAD_INDEX
+        assert cache.count.tolist() == held
+        rows = np.concatenate([np.arange(c) + 12 * p for p, c in enumerate(held)])
+        pick = lambda x: np.concatenate([_f64(x)[0, p][off[p]: off[p] + c] for p, c in enumerate(held)])  # noqa: E731
+        _check_rows(cache, rows, (pick(K), pick(V)))
+    # offsets that fit: as ever
+    cache, ws = cur.QuantCache(1, 3, 12), torch.zeros(256, dtype=torch.uint8, device=DEV)
+    cur.curdkv_qcache_store(cache, K, V, desc, store[:24], torch.tensor([10, 10, 4], dtype=torch.int32, device=DEV),
+                            torch.tensor([0, 10, 20, 24], dtype=torch.int32, device=DEV), packed=True, workspace=ws)
+    assert cur.curdkv_device_status(ws) == 0 and cache.count.tolist() == [10, 10, 4]
