@@ -449,8 +449,10 @@ curdkv_status curdkv_qcache_attention(const void* Q, int32_t q_rows, int64_t q_s
  *   scale     finite, >= 0
  * A query that sees nothing (window = 0 without sinks, or a position below 0 because t_b > n_b)
  * gives O = 0 and lse = -inf.  Rows that no query of the sequence sees (at or beyond n_b, or older than
- * the first query's window and no sinks) are never used, whatever they hold; the others must be finite.
- * Softmax and sums in fp32, weights rounded to bf16 before they multiply the values,
+ * the first query's window and no sinks) are never used, whatever they hold; the others must be finite
+ * (a row that one query sees and another does not reaches both with a weight, 0 for the latter).
+ * Softmax and sums in fp32 (weights up to 2^8 before they are divided by their sum: values times 2^8 times
+ * the rows seen have to stay within fp32), weights rounded to bf16 before they multiply the values,
  * O rounded once.  d = 128.  workspace as in curdkv_qcache_attention. */
 size_t curdkv_attention_window_workspace_bytes(const curdkv_desc* desc, int32_t q_rows);
 curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h,

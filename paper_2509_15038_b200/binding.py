@@ -514,8 +514,10 @@ def _described(what: str, K: torch.Tensor, V: torch.Tensor, desc: Desc, dev: int
         raise TypeError(f"{what}: K and V must be bf16")
     if shape != (B, H, n, d) or shape != V.shape:
         raise ValueError(f"{what}: K is {tuple(shape)}, V {tuple(V.shape)}, the descriptor says {(B, H, n, d)}")
-    if K.stride() != (kb, kh, kn, 1) or V.stride() != (vb, vh, vn, 1):
-        raise ValueError(f"{what}: K or V has other strides than the descriptor")
+    k, v = K.stride(), V.stride()
+    if k != (kb, kh, kn, 1) or v != (vb, vh, vn, 1):       # (an axis of one is never stepped along)
+        if any(n > 1 and (a, b) != (c, d) for n, a, b, c, d in zip(shape, k, v, (kb, kh, kn, 1), (vb, vh, vn, 1))):
+            raise ValueError(f"{what}: K or V has other strides than the descriptor")
     lens = getattr(desc, "seqlens_tensor", None)
     if lens is not None and lens.get_device() != dev:
         raise ValueError(f"{what}: the descriptor's seqlens are on {lens.device}")
@@ -529,6 +531,8 @@ def _int32(what: str, t: Optional[torch.Tensor], numel: Optional[int] = None) ->
 def _count(x: int) -> int:
     """A number of rows for an int32 argument: what no cache holds is as good as the largest (ctypes would drop the upper
     bits), what is negative is left to the call to refuse."""
+    if x.__class__ is int and -1 <= x <= 0x7FFFFFFF:
+        return x
     return min(max(index(x), -1), 0x7FFFFFFF)
 
 

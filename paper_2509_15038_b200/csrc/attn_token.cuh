@@ -3,16 +3,16 @@
 // and the first tokens are visible (curdkv_attention_window with few queries).
 //
 // What has to be moved are the cache's bytes, each once.  4-bit rows are bound by the instructions that
-// unpack and weigh them instead (some 285 per 16 keys of a warp, integer pipe 57 % busy): 64 heads of 131072
-// rows and 4 queries 236 us, 5.7 TB/s (280 when the device's power limit holds its clock down); a copy that
-// only loads takes 196.  bf16 rows are bound by their loads: 128 heads with a window of 4096 46 us, 5.7 TB/s.
+// unpack and weigh them instead (some 281 per 16 keys of a warp, integer pipe 59 % busy): 64 heads of 131072
+// rows and 4 queries 235 us, 5.7 TB/s (273 when the device's power limit holds its clock down); a copy that
+// only loads takes 196.  bf16 rows are bound by their loads: 128 heads with a window of 4096 46 us, 5.8 TB/s.
 // The tiles of all items -- an item is a head and a block of query rows -- form one line, and every CTA takes
 // an equal run of it, whatever the items' lengths: whole items are finished where they are, the partial
 // results of an item that several CTAs share are joined by a second kernel.  (128 heads of 2048 to 16384 rows:
-// 70 us with a CTA per item, as long as the longest, 49 with equal runs.)  Where that gains little an item has
-// a CTA or a cluster of two, four or eight to itself, whose parts are joined through distributed shared
-// memory in the same launch: 8 heads of 1702 rows 6.4 us, 10.7 with equal runs and the second kernel; 128
-// windows of 4096 46 us against 53.  A CTA's warps take its tiles in turn, each warp with its own ring of
+// 51 us; with a CTA per item, as long as the longest, it was 70 where equal runs took 49.)  Where that gains
+// little an item has a CTA or a cluster of two, four or eight to itself, whose parts are joined through
+// distributed shared memory in the same launch: 8 heads of 1702 rows 7.4 us, 12.7 with equal runs and the second
+// kernel; 128 windows of 4096 46 us against 53.  A CTA's warps take its tiles in turn, each warp with its own ring of
 // tiles in shared memory, filled by 16-byte asynchronous copies (rows that do not exist are filled with
 // zeros, so nothing behind a head's last row is ever read).  No barrier stands in the key loop.  Per 16
 // keys a warp forms
@@ -33,9 +33,9 @@
 // group, P_g = p * s_g), with the zeros as a further instruction.
 //
 // The values' magnitude is kept out of the weights' 16 bits.  A warp holds one power of two 2^E for V: scales
-// and zeros relative to it are exact in fp16 as long as every scale of a tile lies some 2^8 to 2^14 below
-// 2^E at most and every zero in [2^(E-17), 2^(E+14)), or is 0 (a vote per tile).  E follows the tiles: one that lies elsewhere but fits
-// by itself brings its own.  A tile that fits nowhere -- groups or rows further apart than that, or a NaN or an
+// and zeros relative to it are exact in fp16, and have bits enough, as long as every scale of a tile lies below
+// 2^E but not more than 2^8 to 2^14 below (the fewer keys, the more), and every zero in [2^(E-17), 2^(E+14)), or
+// is 0 (a vote per tile).  E follows the tiles: one that lies elsewhere but fits by itself brings its own.  A tile that fits nowhere -- groups or rows further apart than that, or a NaN or an
 // infinity, which may meet its own group's channels only -- takes its products in bf16 instead, weights times
 // scale split into two pieces: 16 bits, at fp32's range.  So does a tile whose weights the reference of the
 // accumulators would push towards fp16's lower end (values far larger than its own have gone before).

@@ -87,13 +87,18 @@ struct Plan {
 // `keys`: what the longest head may hold or see in this call, `total`: all heads together.  An item has a cluster to itself -- the most CTAs, up to
 // eight, that find room on the device at once with two rounds of tiles each -- unless one line of all tiles, cut
 // into equal runs, needs so many rounds less that joining its parts pays.  Runs: as many as CTAs fit the
-// device, but none shorter than two rounds unless there are more items.  In us, clusters | line:
-//    8 heads of 4 bits:    1702 rows 6.4 | 10.7     3340 rows 8.0 | 11.7     8192 rows 11.5 | 11.4
-//   32 heads:              1702 rows 7.6 | 12.0     8192 rows 15.8 | 21.1    16384 rows 24.4 | 28.0
-//  128 heads:              1702 rows 13.7 | 18.8    3340 rows 21.0 | 25.4    one head of 8192 rows 12 | 10.4
-//  128 heads, bf16:        window 1024 14.6 | 20.3  window 4096 44.3 | 52.2
-//  456 heads:              1702 rows 36.3 | 38.3    8192 rows 139 | 115      bf16, window 2048 76.5 | 83.2
-// 1024 heads:              1702 rows 58.0 | 71.6    8192 rows 230 | 244      bf16, window 2048 160 | 178
+// device, but none shorter than two rounds unless there are more items.  In us, clusters | line, 4 query rows,
+// heads full, calls in a graph over rows that are not in L2; the rule takes the faster one of each pair:
+//    8 heads of 4 bits:    1702 rows 7.4 | 12.7     3340 rows 9.0 | 14.0     8192 rows 12.1 | 18.0
+//   32 heads:              1702 rows 9.4 | 14.5     8192 rows 16.7 | 22.6    16384 rows 25.9 | 30.1
+//  128 heads:              1702 rows 14.9 | 20.8    3340 rows 22.3 | 27.0    one head of 8192 rows 11.6 | 11.6
+//  128 heads, bf16:        window 1024 15.8 | 20.7  window 4096 46.1 | 52.9
+//  456 heads:              1702 rows 38.2 | 40.5    8192 rows 140 | 118      bf16, window 2048 78.7 | 84.9
+// 1024 heads:              1702 rows 61.4 | 76.7    8192 rows 228 | 245      bf16, window 2048 160 | 179
+//   16 query rows:         128 heads of 1702 rows 20.1 | 28.2    8 of 16384 24.2 | 23.6    64 of 131072 367 | 329
+// What the host knows is the capacity, not what is held: a cache much larger than that may take the line where
+// clusters are faster (8 heads of 1702 rows in a cache of 17020 7.2 | 15.2, of 131072 8.9 | 16.4; 128 heads of
+// 1702 in one of 17020 15.0 | 20.3).
 // (Four times as many runs, to even out SMs of different speed, was slower: 282 against 276 us for 64 heads of
 // 131072 rows, 66 against 51 for 128 heads of 2048 to 16384.)  The workspace depends on neither.
 Plan plan_token(int64_t problems, int64_t rows, int64_t keys, int64_t total, int tile_keys, int ctas_per_sm) {
@@ -133,7 +138,7 @@ Plan plan_token(int64_t problems, int64_t rows, int64_t keys, int64_t total, int
 
 Plan plan_qcache(const curdkv_qcache* c, int32_t q_rows) {
   // Packed heads share `capacity` rows unevenly: the longest is taken to hold four times its share.  (8 heads of
-  // 1702 rows take 6.5 us so and 14.5 with equal runs, one of 12916 and seven of 100 15 and 48.)
+  // 1702 rows take 8.0 us so and 13.1 with equal runs, one of 12916 and seven of 100 15.8 and 17.3.)
   const int64_t P = (int64_t)c->batch * c->kv_heads, share = P > 0 ? 4 * ((c->capacity + P - 1) / P) : 0;
   const bool packed = c->row_start != nullptr;
   const int64_t longest = packed && share < c->capacity ? share : c->capacity;
@@ -208,14 +213,19 @@ bool map_strides_ok(int64_t batch, int64_t heads, int64_t sb, int64_t sh, int64_
 // Measured: the token form needs 9.8 ns per key for 16 query rows of a KV head on one SM, plus the time of 64
 // keys, and spreads its work evenly; the prompt form 18 ns per key for a pair of 128-row tiles (14.7 for a
 // single one), full or not, plus the time of some 320 keys (tiles partly outside the window, the start of an
-// item), and takes whole rounds of a pair per SM.  In us, token | prompt, rows = query rows per KV head, at the
-// sizes around the change from one to the other:
-//   16 x 8 heads, 8192 keys, window 8192, 32 / 64 / 128 rows         177 | 309    271 | 324    536 | 324
-//   16 x 8 heads, window 1024, 32 / 64 / 128 rows                     25 | 58      47 | 58      89 | 58
-//   16 x 8 heads, 512 keys, window 256, 64 / 128 rows                 21 | 31      39 | 31
-//    4 x 8 heads, 8192 keys, window 8192, 64 / 128 / 256 rows         76 | 121    135 | 121    271 | 147
-//    1 x 8 heads, 8192 keys, window 8192, 256 rows                    75 | 143    (the pairs fill few SMs)
-//   64 x 8 heads, 512 keys, window 256, 128 / 256 rows               133 | 165    259 | 166
+// item), and takes whole rounds of a pair per SM.  In us, token | prompt, rows = query rows per KV head (group x
+// tokens), at the sizes around the change from one to the other.  The token form's time goes by the rows alone, the
+// prompt form's by group * ceil(tokens / 128) tiles: it stands for groups of 1 / 4 / 8.  The rule takes the faster
+// one of each pair.
+//   16 x 8 heads, 8192 keys, window 8192    32 rows  175 | 124 / 293 / 579      64 rows  272 | 126 / 293 / 576
+//                                          128 rows  535 | 127 / 295 / 577
+//   16 x 8 heads, 8192 keys, window 1024    32 rows   25 | 28 / 57 / 104        64 rows   46 | 28 / 57 / 105
+//                                          128 rows   88 | 28 / 57 / 105
+//   16 x 8 heads, 512 keys, window 256      64 rows   21 | 16 / 30 / 51        128 rows   39 | 17 / 30 / 52
+//    4 x 8 heads, 8192 keys, window 8192    64 rows   76 | 121 / 148 / 148     128 rows  134 | 121 / 147 / 150
+//                                          256 rows  270 | 148 / 149 / 152
+//    1 x 8 heads, 8192 keys, window 8192   256 rows   72 | 143 / 143 / 145     (the pairs fill few SMs)
+//   64 x 8 heads, 512 keys, window 256     128 rows  132 | 49 / 87 / 164       256 rows  258 | 60 / 88 / 164
 bool prompt_form(int64_t problems, int64_t rows, int64_t tiles, int64_t window_keys, int64_t n_max) {
   const int64_t keys = window_keys < n_max ? window_keys : n_max, places = sms(), pairs = (tiles + 1) / 2;
   const double token = 9.8 * (double)(problems * ((rows + 15) / 16)) / (double)places * (double)(keys + 64);

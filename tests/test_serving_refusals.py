@@ -169,6 +169,9 @@ def test_rows_that_the_descriptor_does_not_describe(monkeypatch):
             call(K, K, away)
         with pytest.raises(AssertionError, match="not refused"):     # and what is described passes
             call(K, K, desc)
+        odd = torch.zeros(5000, dtype=torch.bfloat16).as_strided((1, 2, 16, 128), (8, 2048, 128, 1))   # an axis of one
+        with pytest.raises(AssertionError, match="not refused"):
+            call(odd, K, desc)
 
 
 @pytest.mark.parametrize("big", [2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63, 10 ** 30])
