@@ -812,3 +812,23 @@ def test_store_lists_that_run_beyond_their_index():
     cur.curdkv_qcache_store(cache, K, V, desc, store[:24], torch.tensor([10, 10, 4], dtype=torch.int32, device=DEV),
                             torch.tensor([0, 10, 20, 24], dtype=torch.int32, device=DEV), packed=True, workspace=ws)
     assert cur.curdkv_device_status(ws) == 0 and cache.count.tolist() == [10, 10, 4]
+
+
+@pytest.mark.parametrize("n", [40, 700, 20000])
+@pytest.mark.parametrize("q_rows", [4, 16])
+def test_attention_non_finite_queries_stay_in_their_row(n, q_rows):
+    cache, starts = _random_cache(1, 2, n, [n, n // 2], 690)
+    Q = _rand((1, 2, q_rows, 128), 691)
+    lse = torch.zeros((1, 2, q_rows), device=DEV)
+    want, _ = cur.curdkv_qcache_attention(Q, cache, scale=0.0884, lse=lse)
+    _check_attention(want, lse, Q, cache, [n, n // 2], starts, float(np.float32(0.0884)))
+    bad = Q.clone()
+    bad[0, 0, 1, 5], bad[0, 1, 2, 77] = float("nan"), float("inf")
+    got, _ = cur.curdkv_qcache_attention(bad, cache, scale=0.0884)
+    rest = torch.ones(Q.shape[:3], dtype=torch.bool, device=DEV)
+    rest[0, 0, 1] = rest[0, 1, 2] = False
+    assert torch.isnan(got[~rest]).all()
+    # another row's weights do not enter, but where its logits move the shared vote a weight may be rounded elsewhere
+    lse2 = torch.where(rest, lse, 0.0)
+    O = torch.where(rest[..., None], got, want)
+    _check_attention(O, torch.where(rest, lse2, lse), Q, cache, [n, n // 2], starts, float(np.float32(0.0884)))

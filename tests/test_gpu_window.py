@@ -423,3 +423,17 @@ def test_tiny_scales_with_large_products(B, H, t, scale):
     O, ws = cur.curdkv_attention_window(Q, K, V, desc, 300, num_sink=4, scale=scale, lse=lse)
     assert cur.curdkv_device_status(ws) == 0
     _check(O, lse, Q, K, V, [400] * B, [t] * B, 300, 4, float(np.float32(scale)), heads=[0, 2 * H - 1])
+
+
+@pytest.mark.parametrize("B,H,group,t", [(1, 2, 4, 1), (2, 2, 4, 5), (3, 8, 4, 250)])
+def test_non_finite_queries_stay_in_their_row(B, H, group, t):
+    Q, K, V, desc, O = _run(B, H, group, 700, t, 300, 4, seed=360, heads=[0, H * group - 1])
+    bad = Q.clone()
+    bad[0, 0, t // 2, 5], bad[B - 1, H * group - 1, 0, 77] = float("nan"), float("nan")
+    got, ws = cur.curdkv_attention_window(bad, K, V, desc, 300, num_sink=4, scale=128 ** -0.5)
+    assert cur.curdkv_device_status(ws) == 0
+    rest = torch.ones(Q.shape[:3], dtype=torch.bool, device=DEV)
+    rest[0, 0, t // 2] = rest[B - 1, H * group - 1, 0] = False
+    assert torch.isnan(got[~rest]).all()
+    _check(torch.where(rest[..., None], got, O), None, Q, K, V, [700] * B, [t] * B, 300, 4, float(np.float32(128 ** -0.5)),
+           heads=[0, 1, H * group - 1])
