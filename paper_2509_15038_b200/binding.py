@@ -549,6 +549,11 @@ def _addr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+def _base(t: torch.Tensor, other: torch.Tensor) -> int:
+    """Address of `t`; of `other` where an empty tensor has none (its rows are none: it is not followed)."""
+    return t.data_ptr() or other.data_ptr()
+
+
 class QuantCache:
     """Torch-owned buffers of one 4-bit cache plus the ``curdkv_qcache`` view of them.
 
@@ -609,13 +614,15 @@ def curdkv_qcache_store(cache: QuantCache, K, V, desc: Desc, idx=None, head_coun
             raise ValueError("a packed idx needs head_offsets")
         _int32("head_offsets", head_offsets, P + 1)
         stride = idx.numel()
+        packed = stride > 0                  # (an empty index holds lists of nothing, whatever the offsets say)
     elif idx is not None:
         if P > 0 and idx.numel() % P != 0:
             raise ValueError("idx must be [batch, kv_heads, budget]")
         stride = idx.numel() // max(P, 1)
     if P == 0:
         return
-    code = load().curdkv_qcache_store(cache._ref, _ptr(K), _ptr(V), ctypes.byref(desc), _ptr(idx), stride,
+    code = load().curdkv_qcache_store(cache._ref, _base(K, cache.K_codes), _base(V, cache.K_codes), ctypes.byref(desc),
+                                      None if idx is None else _base(idx, cache.K_codes), stride,
                                       _addr(head_counts) if idx is not None else None,
                                       _addr(head_offsets) if idx is not None and packed else None,
                                       _addr(workspace), _raw_stream(dev))
@@ -731,9 +738,8 @@ def curdkv_attention_window(Q, K, V, desc: Desc, window: int, *, num_sink: int =
     _described("curdkv_attention_window", K, V, desc, dev)
     if B == 0:
         return O, workspace
-    code = load().curdkv_attention_window(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), K.data_ptr() or _ptr(K),
-                                          V.data_ptr() or _ptr(V),
-                                          ctypes.byref(desc), _count(num_sink), _count(window), scale, O.data_ptr(), o[0],
+    code = load().curdkv_attention_window(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), K.data_ptr() or Q.data_ptr(),
+                                          V.data_ptr() or Q.data_ptr(), ctypes.byref(desc), _count(num_sink), _count(window), scale, O.data_ptr(), o[0],
                                           o[1], o[2], _addr(lse), workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
     if code:
         _check(code, "curdkv_attention_window")

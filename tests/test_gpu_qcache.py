@@ -832,3 +832,33 @@ def test_attention_non_finite_queries_stay_in_their_row(n, q_rows):
     lse2 = torch.where(rest, lse, 0.0)
     O = torch.where(rest[..., None], got, want)
     _check_attention(O, torch.where(rest, lse2, lse), Q, cache, [n, n // 2], starts, float(np.float32(0.0884)))
+
+
+def test_store_append_and_read_of_nothing():
+    """No rows, an empty selection (fixed and packed), no new tokens, no slots asked for: counts say so, nothing else moves."""
+    K, none = _rand((1, 2, 8, 128), 700), torch.zeros((1, 2, 0, 128), dtype=torch.bfloat16, device=DEV)
+    zeros = torch.zeros(3, dtype=torch.int32, device=DEV)
+    ws = torch.zeros(256, dtype=torch.uint8, device=DEV)
+    for case in ("rows", "fixed", "packed"):
+        cache = cur.QuantCache(1, 2, 4)
+        cache.K_codes.fill_(0xEE)
+        cache.count.fill_(3)
+        if case == "rows":
+            cur.curdkv_qcache_store(cache, none, none, cur.make_desc(none, none, 1), workspace=ws)
+        else:
+            idx = torch.zeros((1, 2, 0) if case == "fixed" else (0,), dtype=torch.int32, device=DEV)
+            cur.curdkv_qcache_store(cache, K, K, cur.make_desc(K, K, 1), idx, zeros[:2], zeros if case == "packed" else None,
+                                    packed=case == "packed", workspace=ws)
+        assert cache.count.tolist() == [0, 0] and torch.all(cache.K_codes == 0xEE), case
+    bad = torch.zeros(256, dtype=torch.uint8, device=DEV)                # offsets and counts that an empty index does not have
+    cur.curdkv_qcache_store(cache, K, K, cur.make_desc(K, K, 1), idx, zeros[:2] + 4, 4 * torch.arange(3, dtype=torch.int32, device=DEV),
+                            packed=True, workspace=bad)
+    assert cur.curdkv_device_status(bad) == cur.DEV_BAD_INDEX
+    assert cache.count.tolist() == [0, 0] and torch.all(cache.K_codes == 0xEE)
+    cur.curdkv_qcache_append(cache, none, none, workspace=ws)
+    cur.curdkv_qcache_append(cache, K[:, :, :3], K[:, :, :3], t_new=torch.zeros(1, dtype=torch.int32, device=DEV), workspace=ws)
+    assert cache.count.tolist() == [0, 0] and torch.all(cache.K_codes == 0xEE)
+    out = cur.curdkv_qcache_read(cache, torch.zeros((1, 2, 0), dtype=torch.int32, device=DEV), workspace=ws)
+    assert [tuple(x.shape) for x in out] == [(1, 2, 0, 128)] * 2
+    assert not cur.curdkv_qcache_read(cache, workspace=ws)[0].any()
+    assert cur.curdkv_device_status(ws) == 0

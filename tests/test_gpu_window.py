@@ -437,3 +437,12 @@ def test_non_finite_queries_stay_in_their_row(B, H, group, t):
     assert torch.isnan(got[~rest]).all()
     _check(torch.where(rest[..., None], got, O), None, Q, K, V, [700] * B, [t] * B, 300, 4, float(np.float32(128 ** -0.5)),
            heads=[0, 1, H * group - 1])
+
+
+@pytest.mark.parametrize("B,H,t", [(1, 2, 1), (1, 2, 5), (3, 8, 250)])
+def test_a_cache_without_rows(B, H, t):
+    K, Q = torch.zeros((B, H, 0, 128), dtype=torch.bfloat16, device=DEV), _rand((B, 2 * H, t, 128), 370)
+    lse = torch.zeros(Q.shape[:3], device=DEV)
+    O, ws = cur.curdkv_attention_window(Q, K, K, cur.make_desc(K, K, 1, q_heads=2 * H), 100, num_sink=4, scale=0.1, lse=lse)
+    assert cur.curdkv_device_status(ws) == 0
+    assert not O.any() and torch.all(lse == -float("inf"))
