@@ -35,10 +35,11 @@
 // The values' magnitude is kept out of the weights' 16 bits.  A warp holds one power of two 2^E for V: scales
 // and zeros relative to it are exact in fp16, and have bits enough, as long as every scale of a tile lies below
 // 2^E but not more than 2^8 to 2^14 below (the fewer keys, the more), and every zero in [2^(E-17), 2^(E+14)), or
-// is 0 (a vote per tile).  E follows the tiles: one that lies elsewhere but fits by itself brings its own.  A tile that fits nowhere -- groups or rows further apart than that, or a NaN or an
-// infinity, which may meet its own group's channels only -- takes its products in bf16 instead, weights times
-// scale split into two pieces: 16 bits, at fp32's range.  So does a tile whose weights the reference of the
-// accumulators would push towards fp16's lower end (values far larger than its own have gone before).
+// is 0 (a vote per tile).  E follows the tiles: one that lies elsewhere but fits by itself brings its own.  A tile
+// that fits nowhere -- groups or rows further apart than that, or a NaN or an infinity, which may meet its own
+// group's channels only -- takes its products in bf16 instead, weights times scale split into two pieces: 16 bits,
+// at fp32's range.  So does one that lies far below what went before: fp16 weights in the accumulators' unit
+// would lose their bits.
 // O^T is held in units of 2^(T + E - lift) and the row sum in units of 2^(R - lift), R the reference of the
 // logits alone: what a row's values are like has no part in the sum.  T, E and R are whole numbers, so that
 // every rescale is a power of two.  What contributes less than 2^-90 of the largest value held may be lost.
@@ -55,14 +56,14 @@ __host__ __device__ constexpr float slack() { return Q4 ? 4.f : 6.f; }
 constexpr float kLift = 11.f;
 // A tile's products are taken in fp16 when its scales lie in [2^(E - span), 2^E) and its zeros in
 // [2^(E - kZeroDown), 2^(E + kZeroUp)), where both are exact.  Weight times scale then loses bits below 2^-14, by at
-// most 2^-25 a key, of 2^(kLift - 1 - span - far) that the key of the largest logit has: 2^-10 of the sum of magnitudes
-// for 2^n keys, were all errors alike, with a span of 24 - n; far adds one more step (below).
+// most 2^-25 a key, of 2^(kLift - 1 - span - kFall) that the key of the largest logit has: 2^-10 of the sum of magnitudes
+// for 2^n keys, were all errors alike, with a span of 24 - n.
 constexpr int kZeroUp = 14, kZeroDown = 17;
 constexpr int kLeastSpan = 8, kMostSpan = 14;
 __device__ __forceinline__ int span_of(int keys) { return min(max(__clz(max(keys - 1, 1)) - 8, kLeastSpan), kMostSpan); }
 constexpr int kLeastE = -126, kMostE = 112;                // 2^-E is a normal number, and an infinite zero is outside
 constexpr int kMostAbove = 60;       // how far values may lie above 2^E
-constexpr int kFar = 1;              // T - R above which fp16 weights have too few bits
+constexpr int kFall = 1;             // how far E may fall while the accumulators' unit stays: T - R at most
 
 struct Args {
   const __nv_bfloat16* Q;            // [batch][q_heads][q_n][128], strides in elements
@@ -580,7 +581,6 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
     from_lo = (uint32_t)(0x8000 - max(lo, 0)) | (uint32_t)(0x8000 - max(zero_lo, 0)) << 16;
   };
   set_unit(kLeastE);
-  bool far = false;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -738,7 +738,7 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
         top[nt][c] = x;
         move = move || x > m[nt][c] + slack<Q4>();
       }
-    bool wide = false;                                     // fp16 does not hold this tile's scales and zeros
+    bool wide = false;                                     // fp16 is not enough for this tile
     if (__any_sync(0xffffffffu, move)) {
       int shift = 0;                                       // by how much this tile moves E
       if (Q4 && __any_sync(0xffffffffu, elsewhere)) {
@@ -772,7 +772,7 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
             int up = 0;                                    // of the accumulators' unit over 2^E
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) up = max(up, max(exponent_of(rise[nt][0]), exponent_of(rise[nt][1])));
-            wide = __any_sync(0xffffffffu, vexp - own + up > kFar);
+            wide = __any_sync(0xffffffffu, vexp - own + up > kFall);
             if (wide) to = vexp;
           }
         } else if (own > vexp + kMostAbove) {
@@ -811,12 +811,6 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
           }
           accz[nt][c] *= f;
         }
-      if (Q4) {
-        bool above_r = false;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) above_r = above_r || fmaxf(rise[nt][0], rise[nt][1]) > (float)(1 << kFar);
-        far = __any_sync(0xffffffffu, above_r);
-      }
     }
     // ---- weights and O^T
     float nref[NT][2];
@@ -836,7 +830,7 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<Q4, NT>())) attend_kern
         l[nt][1] = w[3] + (w[1] + l[nt][1]);
       }
     };
-    if (!Q4 || __builtin_expect(!(wide || far), 1)) {
+    if (!Q4 || __builtin_expect(!wide, 1)) {
     if constexpr (Q4) {
       // V's scales and zeros in fp16: lanes 2 i and 2 i + 1 hold a pair of keys; the even one takes the pair's groups 0 and
       // 1, the odd one 2 and 3
