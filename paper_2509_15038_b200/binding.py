@@ -712,6 +712,8 @@ def curdkv_qcache_attention(Q, cache: QuantCache, *, scale: float, O=None, lse=N
         raise ValueError("curdkv_qcache_attention: Q and the cache differ in batch or heads")
     if workspace is None:
         workspace = qcache_attention_workspace(cache, m)
+    elif not workspace.is_contiguous():
+        raise ValueError("curdkv_qcache_attention: workspace must be contiguous")
     dev = _on_device("curdkv_qcache_attention", cache.K_codes, Q, O, lse, workspace)
     if B == 0:
         return O, workspace
@@ -734,6 +736,8 @@ def curdkv_attention_window(Q, K, V, desc: Desc, window: int, *, num_sink: int =
     _int32("q_lens", q_lens, B)
     if workspace is None:
         workspace = attention_window_workspace(desc, t, device=Q.device)
+    elif not workspace.is_contiguous():
+        raise ValueError("curdkv_attention_window: workspace must be contiguous")
     dev = _on_device("curdkv_attention_window", Q, K, V, O, lse, q_lens, workspace)
     _described("curdkv_attention_window", K, V, desc, dev)
     if B == 0:

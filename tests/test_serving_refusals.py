@@ -223,3 +223,19 @@ def test_read_into_one_buffer_twice():
         assert lib.curdkv_qcache_read(ctypes.byref(_cache(capacity=4)), None, 0, k, v, None, None) == 1
         assert lib.curdkv_qcache_read(ctypes.byref(_cache(capacity=8, row_start=ANY)), None, 0, k, v, None, None) == 1
     assert cur.launch_count() == before
+
+
+def test_workspaces_that_are_smaller_than_they_look(monkeypatch):
+    """A workspace is counted by its elements: one that is expanded, or strided, does not hold as many bytes side by side."""
+    K, Q = torch.zeros((1, 2, 16, 128), dtype=torch.bfloat16), torch.zeros((1, 2, 1, 128), dtype=torch.bfloat16)
+    cache, desc = cur.QuantCache(1, 2, 16, device="cpu"), cur.make_desc(K, K, 1)
+    _elsewhere(monkeypatch)
+    for ws in (torch.zeros(1, dtype=torch.uint8).expand(1 << 20), torch.zeros(1 << 20, dtype=torch.uint8)[::2],
+               torch.zeros((256, 64), dtype=torch.uint8).t()):
+        for call in (lambda: cur.curdkv_qcache_attention(Q, cache, scale=0.1, workspace=ws),
+                     lambda: cur.curdkv_attention_window(Q, K, K, desc, 4, scale=0.1, workspace=ws),
+                     lambda: cur.curdkv_qcache_store(cache, K, K, desc, workspace=ws),
+                     lambda: cur.curdkv_qcache_append(cache, K, K, workspace=ws),
+                     lambda: cur.curdkv_qcache_read(cache, workspace=ws)):
+            with pytest.raises(ValueError, match="workspace must be contiguous"):
+                call()
