@@ -461,6 +461,45 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
                                       void* O, int64_t o_stride_b, int64_t o_stride_h, int64_t o_stride_n,
                                       float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* ---- Eviction by accumulated attention weight (no counterpart in the paper): the rows of a generation-phase cache are ranked
+ * by the softmax weight they have received, in place of their l^KV.  cache->raw then holds those weights:
+ * curdkv_attention_scores gives a prompt's, curdkv_cache_push brings new rows in and takes the least looked-at ones out,
+ * curdkv_cache_attention adds what each step's queries give.
+ *
+ * One step's bookkeeping: what curdkv_cache_append and curdkv_cache_compress_inplace do one after the other (same arguments,
+ * kept rows, order of slots and status flags), with the new rows' scores given instead of formed with G.
+ *   scores_new  fp32 [batch][kv_heads][n_max], or NULL: 0 each (rows to be kept on arrival belong in the window)
+ *   desc_new    as in curdkv_cache_append; r, score_mode, raw_scores and whiten are not used
+ *   workspace   curdkv_cache_workspace_bytes(batch, kv_heads, n_max, capacity, budget)
+ * Requires budget >= 1 and num_sink + window <= budget.  A cache of at most 8 rows above its budget, as generation needs,
+ * takes one launch (two with more than 8 heads), whose CTAs look for the rows that leave instead of sorting, and
+ * leaves slots at or beyond the new count as they were; others (capacity <= 204800) run as the calls it stands for, whose
+ * evicted rows may stay behind in those slots. */
+curdkv_status curdkv_cache_push(const curdkv_cache* cache, const void* K_new, const void* V_new, const float* scores_new,
+                                const curdkv_desc* desc_new, int32_t budget, int32_t num_sink, int32_t window,
+                                void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* O = softmax(scale Q K^T) V over the rows that a generation-phase cache holds, and the weights they get:
+ *   weights[b][h][j] += sum over the query heads of KV head h and the live query tokens of softmax(scale Q K^T)_j .
+ * Sequence b has t_b = q_lens[b] (or q_rows) query tokens, the last t_b of total[b]: with q_rows > 1, token i stands at
+ * position total[b] - t_b + i and sees the held rows whose `pos` is at most that; with q_rows = 1 it sees all of them.
+ *   Q, O      bf16 [batch][q_heads][q_rows][128] with element strides (multiples of 8, channels contiguous, 16-byte
+ *             aligned); query head q reads KV head q / (q_heads / kv_heads); O may not overlap Q, nor a row of O another
+ *   q_lens    device int32 [batch] (clamped to [0, q_rows]), or NULL; output rows i >= t_b are left untouched
+ *   desc      supplies batch, kv_heads, q_heads and d (128)
+ *   lse       NULL, or fp32 [batch][q_heads][q_rows]: log of each row's sum of exponentials
+ *   weights   NULL, or fp32 [batch][kv_heads][capacity], cache->raw for instance; only held slots are changed
+ *   scale     finite, >= 0
+ * q_rows * (q_heads / kv_heads) <= 1024.  A query that sees nothing gives O = 0, lse = -inf and no weight.  Held rows must be
+ * finite.  Softmax and sums in fp32, weights added in a fixed order; a weight is rounded to bf16 before it multiplies the
+ * values, O is rounded once.  Two launches.  Workspace (256-byte aligned): its status word collects (it is not cleared)
+ * CURDKV_DEV_BAD_INDEX, a count out of range; two calls that may overlap need a workspace each. */
+size_t curdkv_cache_attention_workspace_bytes(const curdkv_cache* cache, const curdkv_desc* desc, int32_t q_rows);
+curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_n,
+                                     const int32_t* q_lens, const curdkv_cache* cache, const curdkv_desc* desc, float scale,
+                                     void* O, int64_t o_stride_b, int64_t o_stride_h, int64_t o_stride_n, float* lse,
+                                     float* weights, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* GQA (Sec. 3.2): query head q uses KV head q / (q_heads / kv_heads).  Writes
  * kv_head_of_q int32 [q_heads] (device) so that attention consumers can index
  * the shared selection without replicating the compacted cache. */

@@ -35,6 +35,7 @@ EXPORTS = (
     "curdkv_qcache_store", "curdkv_qcache_append", "curdkv_qcache_read",
     "curdkv_qcache_attention_workspace_bytes", "curdkv_qcache_attention",
     "curdkv_attention_window_workspace_bytes", "curdkv_attention_window",
+    "curdkv_cache_push", "curdkv_cache_attention_workspace_bytes", "curdkv_cache_attention",
 )
 
 
@@ -155,6 +156,13 @@ def load():
     lib.curdkv_attention_window.restype = ctypes.c_int
     lib.curdkv_attention_window.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, dp, i32, i32, f32, vp, i64, i64,
                                             i64, vp, vp, ctypes.c_size_t, vp]
+    lib.curdkv_cache_push.restype = ctypes.c_int
+    lib.curdkv_cache_push.argtypes = [cp, vp, vp, vp, dp, i32, i32, i32, vp, ctypes.c_size_t, vp]
+    lib.curdkv_cache_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.curdkv_cache_attention_workspace_bytes.argtypes = [cp, dp, i32]
+    lib.curdkv_cache_attention.restype = ctypes.c_int
+    lib.curdkv_cache_attention.argtypes = [vp, i32, i64, i64, i64, vp, cp, dp, f32, vp, i64, i64, i64, vp, vp, vp,
+                                           ctypes.c_size_t, vp]
     lib.curdkv_selftest_bounded_wait.restype = ctypes.c_int
     lib.curdkv_selftest_bounded_wait.argtypes = [ctypes.c_uint64, vp, vp]
     lib.curdkv_selftest_gather_wait.restype = ctypes.c_int
@@ -391,15 +399,35 @@ class DeviceCache:
     """Torch-owned buffers of one generation-phase cache plus the ``curdkv_cache`` view of them."""
 
     def __init__(self, batch: int, kv_heads: int, capacity: int, d: int, device="cuda"):
-        self.batch, self.kv_heads, self.capacity, self.d = batch, kv_heads, capacity, d
-        self.K = torch.zeros((batch, kv_heads, capacity, d), dtype=torch.bfloat16, device=device)
-        self.V = torch.zeros_like(self.K)
-        self.raw = torch.zeros((batch, kv_heads, capacity), dtype=torch.float32, device=device)
-        self.pos = torch.full((batch, kv_heads, capacity), -1, dtype=torch.int32, device=device)
-        self.count = torch.zeros((batch,), dtype=torch.int32, device=device)
-        self.total = torch.zeros((batch,), dtype=torch.int32, device=device)
-        self.c = Cache(self.K.data_ptr(), self.V.data_ptr(), self.raw.data_ptr(), self.pos.data_ptr(),
-                       self.count.data_ptr(), self.total.data_ptr(), capacity)
+        K = torch.zeros((batch, kv_heads, capacity, d), dtype=torch.bfloat16, device=device)
+        raw = torch.zeros((batch, kv_heads, capacity), dtype=torch.float32, device=device)
+        pos = torch.full((batch, kv_heads, capacity), -1, dtype=torch.int32, device=device)
+        count = torch.zeros((batch,), dtype=torch.int32, device=device)
+        self._set(K, torch.zeros_like(K), raw, pos, count, torch.zeros_like(count))
+
+    @classmethod
+    def of(cls, K, V, raw, pos, count, total) -> "DeviceCache":
+        """A cache over buffers that exist already: K, V bf16 ``[B, Hkv, capacity, d]``, raw fp32 and pos int32 of
+        ``[B, Hkv, capacity]``, count and total int32 ``[B]``, contiguous, on one device."""
+        self = cls.__new__(cls)
+        if K.dim() != 4:
+            raise ValueError("K of a DeviceCache must be [batch, kv_heads, capacity, d]")
+        for t, shape, dtype in ((K, K.shape, torch.bfloat16), (V, K.shape, torch.bfloat16), (raw, K.shape[:3], torch.float32),
+                                (pos, K.shape[:3], torch.int32), (count, K.shape[:1], torch.int32),
+                                (total, K.shape[:1], torch.int32)):
+            if t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+                raise ValueError(f"a buffer of a DeviceCache must be contiguous {dtype} {tuple(shape)}")
+            if t.device != K.device:
+                raise ValueError("the buffers of a DeviceCache must lie on one device")
+        self._set(K, V, raw, pos, count, total)
+        return self
+
+    def _set(self, K, V, raw, pos, count, total):
+        self.batch, self.kv_heads, self.capacity, self.d = K.shape
+        self.K, self.V, self.raw, self.pos, self.count, self.total = K, V, raw, pos, count, total
+        self.c = Cache(K.data_ptr(), V.data_ptr(), raw.data_ptr(), pos.data_ptr(), count.data_ptr(), total.data_ptr(),
+                       self.capacity)
+        self._ref = ctypes.byref(self.c)
 
 
 def cache_workspace(batch: int, kv_heads: int, t_max: int, capacity: int, budget: int,
@@ -747,6 +775,73 @@ def curdkv_attention_window(Q, K, V, desc: Desc, window: int, *, num_sink: int =
                                           o[1], o[2], _addr(lse), workspace.data_ptr(), workspace.numel(), _raw_stream(dev))
     if code:
         _check(code, "curdkv_attention_window")
+    return O, workspace
+
+
+# ---- generation over a cache whose rows are ranked by the attention weights they receive --------
+
+def curdkv_cache_push(cache: DeviceCache, K_new, V_new, budget: int, workspace: torch.Tensor, *, num_sink: int = 0,
+                      window: int = 0, scores_new: Optional[torch.Tensor] = None,
+                      t_new: Optional[torch.Tensor] = None) -> None:
+    """K_new, V_new ``[B, Hkv, t, d]`` join ``cache`` with the scores ``scores_new`` (fp32 ``[B, Hkv, t]``; 0 each where not
+    given), then rows beyond ``budget`` leave: the least of ``cache.raw`` but for sinks and the ``window`` most recent.
+    The workspace is :func:`cache_workspace`'s."""
+    what = "curdkv_cache_push"
+    dev = _on_device(what, cache.K, K_new, V_new, scores_new, t_new, workspace)
+    _status_buffer(what, workspace)
+    desc = make_desc(K_new, V_new, 1, seqlens=t_new)
+    shape = K_new.shape
+    if shape[0] != cache.batch or shape[1] != cache.kv_heads or shape[3] != cache.d:
+        raise ValueError(f"{what}: new rows are {tuple(shape)}, the cache {(cache.batch, cache.kv_heads, cache.capacity, cache.d)}")
+    if scores_new is not None and (scores_new.dtype is not torch.float32 or scores_new.shape != shape[:3]
+                                   or not scores_new.is_contiguous()):
+        raise ValueError(f"{what}: scores_new must be contiguous fp32 {tuple(shape[:3])}")
+    code = load().curdkv_cache_push(cache._ref, _base(K_new, cache.K), _base(V_new, cache.K), _addr(scores_new),
+                                    ctypes.byref(desc), index(budget), _count(num_sink), _count(window), workspace.data_ptr(),
+                                    workspace.numel() * workspace.element_size(), _raw_stream(dev))
+    if code:
+        _check(code, what)
+
+
+def _cache_desc(cache: DeviceCache, q_heads: int) -> Desc:
+    return Desc(cache.batch, cache.kv_heads, q_heads, cache.capacity, cache.d, 1)
+
+
+def cache_attention_workspace(cache: DeviceCache, q_heads: int, q_rows: int) -> torch.Tensor:
+    desc = _cache_desc(cache, int(q_heads))
+    nbytes = int(load().curdkv_cache_attention_workspace_bytes(cache._ref, ctypes.byref(desc), int(q_rows)))
+    if nbytes == 0:
+        raise ValueError("invalid shape for curdkv_cache_attention")
+    return torch.zeros((nbytes,), dtype=torch.uint8, device=cache.K.device)
+
+
+def curdkv_cache_attention(Q, cache: DeviceCache, *, scale: float, weights: Optional[torch.Tensor] = None,
+                           q_lens: Optional[torch.Tensor] = None, O=None, lse=None,
+                           workspace: Optional[torch.Tensor] = None):
+    """O = softmax(scale Q K^T) V over the held rows, Q bf16 ``[B, Hq, t, 128]`` the last ``q_lens`` (default t) tokens of each
+    sequence; ``weights`` (fp32 ``[B, Hkv, capacity]``, ``cache.raw`` for instance) grows by the softmax weights of each
+    row, summed over its query heads and tokens.  Returns (O, workspace)."""
+    what = "curdkv_cache_attention"
+    O, (B, H, t, _), q, o = _queries(what, Q, O, lse)
+    if B != cache.batch or H % cache.kv_heads or H == 0:
+        raise ValueError(f"{what}: Q and the cache differ in batch or heads")
+    _int32("q_lens", q_lens, B)
+    if weights is not None and (weights.dtype is not torch.float32 or weights.shape != cache.raw.shape
+                                or not weights.is_contiguous()):
+        raise ValueError(f"{what}: weights must be contiguous fp32 {tuple(cache.raw.shape)}")
+    if workspace is None:
+        workspace = cache_attention_workspace(cache, H, t)
+    elif not workspace.is_contiguous():
+        raise ValueError(f"{what}: workspace must be contiguous")
+    dev = _on_device(what, cache.K, Q, O, lse, q_lens, weights, workspace)
+    if B == 0:
+        return O, workspace
+    desc = _cache_desc(cache, H)
+    code = load().curdkv_cache_attention(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), cache._ref, ctypes.byref(desc), scale,
+                                         O.data_ptr(), o[0], o[1], o[2], _addr(lse), _addr(weights), workspace.data_ptr(),
+                                         workspace.numel() * workspace.element_size(), _raw_stream(dev))
+    if code:
+        _check(code, what)
     return O, workspace
 
 

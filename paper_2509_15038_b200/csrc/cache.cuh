@@ -21,11 +21,14 @@ struct CacheView {
 struct AppendArgs {
   CacheView cache;
   KvView K_new, V_new;     // [batch][heads][t][d]
-  const float* raw_new;    // [batch][heads][t]
+  const float* raw_new;    // [batch][heads][t] (nullptr: 0)
   const int32_t* t_new;    // [batch] or nullptr (every sequence brings t rows)
   int heads, t, d;
   uint32_t* status;
 };
+
+// Appends rows and moves the counters (defined beside the C ABI); the launch has to fit a grid.
+curdkv_status append_rows(const AppendArgs& a, int32_t batch, cudaStream_t stream);
 
 constexpr int kAppendWarps = 8;
 constexpr int kAppendRowsPerCta = 32;
@@ -75,7 +78,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32) cache_append_kernel(const A
     for (int j = 0; j < kAppendRowsPerCta / kAppendWarps; ++j) {
       const int i = row0 + j * kAppendWarps;
       if (i < tb) {
-        a.cache.raw[(size_t)p * a.cache.capacity + held + i] = a.raw_new[(size_t)p * a.t + i];
+        a.cache.raw[(size_t)p * a.cache.capacity + held + i] = a.raw_new != nullptr ? a.raw_new[(size_t)p * a.t + i] : 0.f;
         a.cache.pos[(size_t)p * a.cache.capacity + held + i] = first_pos + i;
       }
     }

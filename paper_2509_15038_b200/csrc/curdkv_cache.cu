@@ -4,7 +4,9 @@
 #include <cstdint>
 
 #include "cache.cuh"
+#include "cache_push.cuh"
 #include "common.cuh"
+#include "host.cuh"
 
 namespace {
 
@@ -55,6 +57,19 @@ CacheView view_of(const curdkv_cache* c) {
 
 }  // namespace
 
+namespace curdkv {
+curdkv_status append_rows(const AppendArgs& a, int32_t batch, cudaStream_t stream) {
+  const int64_t P = (int64_t)batch * a.heads, chunks = (a.t + kAppendRowsPerCta - 1) / kAppendRowsPerCta;
+  cache_append_kernel<<<(unsigned)(P * chunks), kAppendWarps * 32, 0, stream>>>(a);
+  count_launch();
+  if (cudaGetLastError() != cudaSuccess) return CURDKV_ERR_CUDA;
+  cache_advance_kernel<<<(unsigned)((batch + 255) / 256), 256, 0, stream>>>(a.cache, a.t_new, a.t, batch);
+  count_launch();
+  if (cudaGetLastError() != cudaSuccess) return CURDKV_ERR_CUDA;
+  return CURDKV_OK;
+}
+}  // namespace curdkv
+
 extern "C" {
 
 size_t curdkv_cache_workspace_bytes(int32_t batch, int32_t kv_heads, int32_t t_max, int32_t capacity,
@@ -99,14 +114,7 @@ curdkv_status curdkv_cache_append(const curdkv_cache* cache, const void* K_new, 
   a.status = reinterpret_cast<uint32_t*>(ws + L.score_ws);
   const int64_t chunks = (d.n_max + kAppendRowsPerCta - 1) / kAppendRowsPerCta;
   if (P * chunks > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
-  cache_append_kernel<<<(unsigned)(P * chunks), kAppendWarps * 32, 0, stream>>>(a);
-  count_launch();
-  if (cudaGetLastError() != cudaSuccess) return CURDKV_ERR_CUDA;
-  cache_advance_kernel<<<(unsigned)((d.batch + 255) / 256), 256, 0, stream>>>(a.cache, d.seqlens, d.n_max,
-                                                                             d.batch);
-  count_launch();
-  if (cudaGetLastError() != cudaSuccess) return CURDKV_ERR_CUDA;
-  return CURDKV_OK;
+  return append_rows(a, d.batch, stream);
 }
 
 curdkv_status curdkv_cache_compress(const curdkv_cache* in, const curdkv_cache* out,
@@ -278,6 +286,64 @@ curdkv_status curdkv_cache_step(const curdkv_cache* cache, const void* K_new, co
   count_launch();
   if (cudaGetLastError() != cudaSuccess) return CURDKV_ERR_CUDA;
   return CURDKV_OK;
+}
+
+curdkv_status curdkv_cache_push(const curdkv_cache* cache, const void* K_new, const void* V_new, const float* scores_new,
+                                const curdkv_desc* desc_new, int32_t budget, int32_t num_sink, int32_t window,
+                                void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (!cache_ok(cache) || workspace == nullptr || !host::status_ok(workspace)) return CURDKV_ERR_INVALID_ARG;
+  if (budget < 1 || num_sink < 0 || window < 0 || (int64_t)num_sink + window > budget) return CURDKV_ERR_INVALID_ARG;
+  curdkv_status st = check_call(K_new, V_new, desc_new);
+  if (st != CURDKV_OK) return st;
+  if (desc_new->d % 8 != 0 || !host::aligned16(cache->K) || !host::aligned16(cache->V)) return CURDKV_ERR_INVALID_ARG;
+  CacheWorkspace L;
+  if (!layout(desc_new->batch, desc_new->kv_heads, desc_new->n_max, cache->capacity, budget, &L)) return CURDKV_ERR_INVALID_ARG;
+  if (workspace_bytes < L.total) return CURDKV_ERR_WORKSPACE;
+  const int64_t P = (int64_t)desc_new->batch * desc_new->kv_heads;
+  if (P == 0) return CURDKV_OK;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  PushArgs s = {};
+  AppendArgs& a = s.append;
+  a.cache = view_of(cache);
+  a.K_new = KvView{static_cast<const __nv_bfloat16*>(K_new), desc_new->k_stride_b, desc_new->k_stride_h, desc_new->k_stride_n};
+  a.V_new = KvView{static_cast<const __nv_bfloat16*>(V_new), desc_new->v_stride_b, desc_new->v_stride_h, desc_new->v_stride_n};
+  a.raw_new = scores_new;
+  a.t_new = desc_new->seqlens;
+  a.heads = desc_new->kv_heads;
+  a.t = desc_new->n_max;
+  a.d = desc_new->d;
+  a.status = static_cast<uint32_t*>(workspace);
+  if (cache->capacity - (int64_t)budget > kPushMost || P > 0x7fffffffLL) {
+    // more rows than a handful may have to go: append, then select
+    const int64_t chunks = (desc_new->n_max + kAppendRowsPerCta - 1) / kAppendRowsPerCta;
+    if (cache->capacity > 200 * 1024 || P * chunks > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+    if (chunks > 0) {
+      if ((st = append_rows(a, desc_new->batch, stream)) != CURDKV_OK) return st;
+    }
+    curdkv_desc d = *desc_new;
+    d.r = 1;
+    return curdkv_cache_compress_inplace(cache, &d, budget, num_sink, window, workspace, workspace_bytes, cuda_stream);
+  }
+  s.budget = budget;
+  s.num_sink = num_sink;
+  s.window = window;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)P);
+  cfg.blockDim = dim3(cache->capacity <= 4096 ? 256 : 1024);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr = {};
+  if (a.heads <= 8) {                                      // a cluster per sequence
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)a.heads;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+  } else {
+    s.tickets = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(workspace) + L.tickets);
+    if (cudaMemsetAsync(s.tickets, 0, (size_t)desc_new->batch * sizeof(int32_t), stream) != cudaSuccess) return CURDKV_ERR_CUDA;
+  }
+  if (cudaLaunchKernelEx(&cfg, cache_push_kernel, s) != cudaSuccess) return CURDKV_ERR_CUDA;
+  return host::launched() ? CURDKV_OK : CURDKV_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -8,35 +8,13 @@
 #include "attn_token.cuh"
 #include "attn_window.cuh"
 #include "common.cuh"
+#include "host.cuh"
 #include "qcache.cuh"
 
 namespace {
 
 using namespace curdkv;
-
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline size_t round256(size_t x) { return (x + 255) & ~size_t(255); }
-
-bool launched() {
-  count_launch();
-  return cudaGetLastError() == cudaSuccess;
-}
-
-// SMs of the current device (asked of the driver once per device), or a B200's where none can be asked
-// (workspace sizes).
-int sms() {
-  static std::atomic<int> known[64];
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) == cudaSuccess) {
-    if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0) {
-      if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
-      return n;
-    }
-  }
-  cudaGetLastError();
-  return 148;
-}
+using namespace curdkv::host;
 
 curdkv_status check_cache(const curdkv_qcache* c) {
   if (c == nullptr || c->K_codes == nullptr || c->V_codes == nullptr || c->K_meta == nullptr ||
@@ -55,8 +33,6 @@ qcache::View view_of(const curdkv_qcache* c) {
                       static_cast<uint32_t*>(c->K_meta), static_cast<uint32_t*>(c->V_meta),
                       c->count, c->row_start, c->capacity};
 }
-
-bool status_ok(const void* workspace) { return (reinterpret_cast<uintptr_t>(workspace) & 255u) == 0; }
 
 // CTAs per head so that `problems` heads of up to `rows` rows fill the device a few times over.
 int ctas_for(int64_t problems, int64_t rows, int rows_per_cta) {
@@ -152,18 +128,6 @@ Plan plan_window(const curdkv_desc* d, int32_t q_rows, int64_t seen) {
                     token::ctas_per_sm<false, 1>());
 }
 
-// Lets `kernel` use `bytes` of shared memory on the current device; asked of the driver once per device.
-template <typename Kernel>
-bool allow_smem(Kernel kernel, int bytes, std::atomic<uint64_t>& done) {
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess) return false;
-  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
-  if (done.load(std::memory_order_relaxed) & bit) return true;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
-  done.fetch_or(bit, std::memory_order_relaxed);
-  return true;
-}
-
 template <bool Q4, int NT>
 bool launch_attend(const token::Args& a, cudaStream_t stream) {
   constexpr int smem = token::smem_bytes<Q4, NT>();
@@ -202,13 +166,6 @@ bool launch_attend(const token::Args& a, cudaStream_t stream) {
   return launched();
 }
 
-// The prompt form reads its tensors through TMA maps, whose strides must be positive and below 2^40
-// bytes (for sequences and heads: where there are several); the token form takes the others.
-bool map_strides_ok(int64_t batch, int64_t heads, int64_t sb, int64_t sh, int64_t sn) {
-  const int64_t most = (int64_t)1 << 38;
-  return (batch <= 1 || (sb > 0 && sb < most)) && (heads <= 1 || (sh > 0 && sh < most)) && sn < most;
-}
-
 // Which form of the window attention a call takes: the one whose slowest SM is estimated to end first.
 // Measured: the token form needs 9.8 ns per key for 16 query rows of a KV head on one SM, plus the time of 64
 // keys, and spreads its work evenly; the prompt form 18 ns per key for a pair of 128-row tiles (14.7 for a
@@ -232,32 +189,6 @@ bool prompt_form(int64_t problems, int64_t rows, int64_t tiles, int64_t window_k
   const double prompt =
       (tiles > 1 ? 18.0 : 14.7) * (double)((problems * pairs + places - 1) / places) * (double)(keys + 320);
   return prompt < token;
-}
-
-bool query_strides_ok(const void* x, int64_t sb, int64_t sh, int64_t sn) {
-  return x != nullptr && aligned16(x) && sb >= 0 && sh >= 0 && sn >= 128 && sb % 8 == 0 && sh % 8 == 0 && sn % 8 == 0;
-}
-
-// Rows that are written may not share memory with one another: by ascending stride, each axis has to step over all
-// that the ones before it reach.  (An axis of one never steps.)
-bool rows_apart(int64_t batch, int64_t heads, int64_t rows, int64_t sb, int64_t sh, int64_t sn) {
-  int64_t size[3] = {batch, heads, rows}, step[3] = {sb, sh, sn};
-  __int128 reach = 128;
-  for (int done = 0; done < 3; ++done) {
-    int least = -1;
-    for (int i = 0; i < 3; ++i)
-      if (size[i] > 1 && (least < 0 || step[i] < step[least])) least = i;
-    if (least < 0) break;
-    if (step[least] < reach) return false;
-    reach += (__int128)(size[least] - 1) * step[least];
-    size[least] = 1;
-  }
-  return true;
-}
-
-bool overlap(const void* a, const void* b, __int128 bytes) {
-  const __int128 x = (__int128)reinterpret_cast<uintptr_t>(a), y = (__int128)reinterpret_cast<uintptr_t>(b);
-  return x < y + bytes && y < x + bytes;
 }
 
 }  // namespace

@@ -1,0 +1,191 @@
+// Generation over a cache whose rows collect the attention weights they receive, and the attention of a
+// batch that shares a prefix.  Argument checks and kernel launches.
+#include <cmath>
+#include <cstdint>
+
+#include "attn_rows.cuh"
+#include "host.cuh"
+
+namespace {
+
+using namespace curdkv;
+using namespace curdkv::host;
+
+// How the keys of `problems` KV heads with `query_rows` query rows each are cut into parts.
+struct RowsPlan {
+  int nt, blocks, chunk, chunks;
+  size_t entries;                    // query rows of all parts
+};
+
+// As many parts as fill the device (two CTAs an SM) when heads are few, so that a head's keys are read by many SMs; several
+// rounds of parts when they are many, so that the last round costs little and ragged heads even out.  A part has at least
+// two steps of its four warps (128 keys).
+RowsPlan plan_rows(int64_t problems, int64_t query_rows, int64_t keys) {
+  RowsPlan pl;
+  pl.nt = query_rows <= 8 ? 1 : 2;
+  pl.blocks = (int)((query_rows + 8 * pl.nt - 1) / (8 * pl.nt));
+  const int64_t items = problems * pl.blocks > 0 ? problems * pl.blocks : 1, slots = 2 * (int64_t)sms();
+  int64_t chunks = items <= slots ? slots / items : (6 * slots + items - 1) / items;
+  int64_t chunk = chunks > 0 ? (keys + chunks - 1) / chunks : keys;
+  const int64_t least = items <= slots ? 128 : 512;
+  if (chunk < least) chunk = least;
+  chunk = (chunk + 63) / 64 * 64;
+  chunks = keys > 0 ? (keys + chunk - 1) / chunk : 1;
+  pl.chunk = (int)chunk;
+  pl.chunks = (int)chunks;
+  pl.entries = (size_t)items * chunks * 8 * pl.nt;
+  return pl;
+}
+
+size_t parts_bytes(size_t entries) { return round256(entries * sizeof(float2)) + round256(entries * 128 * sizeof(float)); }
+
+template <int NT, bool LOGITS>
+bool launch_parts(const rows::Args& a, int64_t ctas, cudaStream_t stream) {
+  constexpr int smem = rows::smem_bytes<NT>();
+  static std::atomic<uint64_t> done{0};
+  if (!allow_smem(rows::part_kernel<NT, LOGITS>, smem, done)) return false;
+  rows::part_kernel<NT, LOGITS><<<(unsigned)ctas, rows::kThreads, smem, stream>>>(a);
+  return launched();
+}
+
+template <bool PREFIX, bool LOGITS>
+bool launch_join(const rows::JoinArgs& a, int64_t ctas, cudaStream_t stream) {
+  // launched behind the kernel before it without waiting for its end: the kernel itself waits
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3(rows::kJoinWarps * 32);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, rows::join_parts_kernel<PREFIX, LOGITS>, a) != cudaSuccess) return false;
+  return launched();
+}
+
+rows::Parts parts_of(const RowsPlan& pl, unsigned char* at, const int32_t* lens, int n_max) {
+  rows::Parts x = {};
+  x.ml = reinterpret_cast<const float2*>(at);
+  x.o = reinterpret_cast<const float*>(at + round256(pl.entries * sizeof(float2)));
+  x.lens = lens;
+  x.n_max = n_max;
+  x.chunk = pl.chunk;
+  x.chunks = pl.chunks;
+  x.tile_rows = 8 * pl.nt;
+  x.tiles = pl.blocks;
+  return x;
+}
+
+bool cache_ok(const curdkv_cache* c) {
+  return c != nullptr && c->K != nullptr && c->V != nullptr && c->raw != nullptr && c->pos != nullptr &&
+         c->count != nullptr && c->total != nullptr && c->capacity >= 1;
+}
+
+// ---- attention over a generation-phase cache ---------------------------------------------------
+struct CachePlan {
+  RowsPlan rows;
+  int pitch, slices;
+  size_t parts_at, logits_at, bytes;
+};
+
+bool heads_ok(const curdkv_desc* d) {
+  return d != nullptr && d->batch >= 0 && d->kv_heads >= 1 && d->q_heads >= d->kv_heads && d->q_heads % d->kv_heads == 0;
+}
+
+bool plan_cache(const curdkv_cache* c, const curdkv_desc* d, int32_t q_rows, CachePlan* pl) {
+  if (c == nullptr || c->capacity < 1 || c->capacity > (1 << 30) || !heads_ok(d) || q_rows < 1) return false;
+  const int64_t P = (int64_t)d->batch * d->kv_heads, rows = (int64_t)(d->q_heads / d->kv_heads) * q_rows;
+  if (rows > rows::kMostRows || P > (1 << 24)) return false;
+  pl->rows = plan_rows(P, rows, c->capacity);
+  pl->pitch = (int)(rows < 8 * pl->rows.nt ? (rows + 1) / 2 * 2 : 8 * pl->rows.nt);
+  // joining: about four CTAs an SM, but 512 keys each at least
+  int64_t slices = (4 * (int64_t)sms() + (P > 0 ? P : 1) - 1) / (P > 0 ? P : 1);
+  const int64_t most = (c->capacity + 511) / 512;
+  if (slices > most) slices = most;
+  pl->slices = (int)slices;
+  pl->parts_at = 256;
+  pl->logits_at = pl->parts_at + parts_bytes(pl->rows.entries);
+  pl->bytes = pl->logits_at + round256((size_t)P * pl->rows.blocks * c->capacity * pl->pitch * sizeof(float));
+  return true;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t curdkv_cache_attention_workspace_bytes(const curdkv_cache* cache, const curdkv_desc* desc, int32_t q_rows) {
+  CachePlan pl;
+  return plan_cache(cache, desc, q_rows, &pl) ? pl.bytes : 0;
+}
+
+curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_n,
+                                     const int32_t* q_lens, const curdkv_cache* cache, const curdkv_desc* desc, float scale,
+                                     void* O, int64_t o_stride_b, int64_t o_stride_h, int64_t o_stride_n, float* lse,
+                                     float* weights, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  if (!cache_ok(cache) || !heads_ok(desc) || q_rows < 1 || !(scale >= 0.f) || std::isinf(scale)) return CURDKV_ERR_INVALID_ARG;
+  if (desc->d != 128) return CURDKV_ERR_UNSUPPORTED;
+  if (!aligned16(cache->K) || !aligned16(cache->V)) return CURDKV_ERR_INVALID_ARG;
+  if (!query_strides_ok(Q, q_stride_b, q_stride_h, q_stride_n) || !query_strides_ok(O, o_stride_b, o_stride_h, o_stride_n) ||
+      Q == O || !rows_apart(desc->batch, desc->q_heads, q_rows, o_stride_b, o_stride_h, o_stride_n))
+    return CURDKV_ERR_INVALID_ARG;
+  if (workspace == nullptr || !status_ok(workspace)) return CURDKV_ERR_INVALID_ARG;
+  CachePlan pl;
+  if (!plan_cache(cache, desc, q_rows, &pl)) return CURDKV_ERR_UNSUPPORTED;
+  if (workspace_bytes < pl.bytes) return CURDKV_ERR_WORKSPACE;
+  const int64_t P = (int64_t)desc->batch * desc->kv_heads;
+  if (P == 0) return CURDKV_OK;
+  const int64_t ctas = P * pl.rows.blocks * pl.rows.chunks;
+  if (ctas > 0x7fffffffLL || P * pl.slices > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  const int64_t row = 128, head = row * cache->capacity, seq = head * desc->kv_heads;
+  rows::Args a = {};
+  a.q = rows::Queries{static_cast<const __nv_bfloat16*>(Q), q_stride_b, q_stride_h, q_stride_n, desc->kv_heads,
+                      desc->q_heads / desc->kv_heads, q_rows, 1, desc->q_heads / desc->kv_heads * q_rows};
+  a.q_lens = q_lens;
+  a.K = KvView{static_cast<const __nv_bfloat16*>(cache->K), seq, head, row};
+  a.V = KvView{static_cast<const __nv_bfloat16*>(cache->V), seq, head, row};
+  a.lens = cache->count;
+  a.n_max = cache->capacity;
+  if (q_rows > 1) {                                        // (one token sees every held row)
+    a.pos = cache->pos;
+    a.total = cache->total;
+    a.causal = 1;
+  }
+  a.blocks = pl.rows.blocks;
+  a.chunk = pl.rows.chunk;
+  a.chunks = pl.rows.chunks;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  const rows::Parts own = parts_of(pl.rows, ws + pl.parts_at, cache->count, cache->capacity);
+  a.part_ml = const_cast<float2*>(own.ml);
+  a.part_o = const_cast<float*>(own.o);
+  a.status = reinterpret_cast<uint32_t*>(ws);
+  rows::JoinArgs j = {};
+  j.own = own;
+  j.heads = desc->kv_heads;
+  j.group = a.q.group;
+  j.t = q_rows;
+  j.share = 1;
+  j.q_lens = q_lens;
+  j.O = static_cast<__nv_bfloat16*>(O);
+  j.o_sb = o_stride_b; j.o_sh = o_stride_h; j.o_sn = o_stride_n;
+  j.lse = lse;
+  j.slices = 1;
+  if (weights == nullptr) {
+    if (!(pl.rows.nt == 1 ? launch_parts<1, false>(a, ctas, stream) : launch_parts<2, false>(a, ctas, stream))) return CURDKV_ERR_CUDA;
+    return launch_join<false, false>(j, P, stream) ? CURDKV_OK : CURDKV_ERR_CUDA;
+  }
+  a.logits = reinterpret_cast<float*>(ws + pl.logits_at);
+  a.pitch = pl.pitch;
+  j.slices = pl.slices;
+  j.logits = a.logits;
+  j.n_max = cache->capacity;
+  j.pitch = pl.pitch;
+  j.block_rows = 8 * pl.rows.nt;
+  j.weights = weights;
+  if (!(pl.rows.nt == 1 ? launch_parts<1, true>(a, ctas, stream) : launch_parts<2, true>(a, ctas, stream))) return CURDKV_ERR_CUDA;
+  return launch_join<false, true>(j, P * pl.slices, stream) ? CURDKV_OK : CURDKV_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -13,23 +13,9 @@
 //   V row: channel 32 g + 4 t + u in nibble u of 16-bit word 4 t + g  (t < 8, g, u < 4)
 #pragma once
 #include "common.cuh"
+#include "warp_ptx.cuh"
 
 namespace curdkv {
-
-// ---- asynchronous copies, 16 bytes a thread
-__device__ __forceinline__ uint32_t smem_addr(const void* p) {
-  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
-}
-// 16 bytes global -> shared, zeros when `live` is false (nothing is read then).
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 namespace qcache {
 
