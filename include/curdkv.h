@@ -500,6 +500,32 @@ curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_st
                                      void* O, int64_t o_stride_b, int64_t o_stride_h, int64_t o_stride_n, float* lse,
                                      float* weights, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
+/* Attention of a decoding batch whose sequences share a prefix, computed once for all of them (no counterpart in the paper):
+ * desc->batch sequences, desc_prefix->batch prefixes, of which each serves desc->batch / desc_prefix->batch sequences, one
+ * behind the other (layers folded into the batch have a prefix each).  Sequence b has n_b = desc->seqlens[b] (or n_max)
+ * rows of its own behind the prefix, its new ones among them, and t_b = q_lens[b] (or q_rows) query tokens at the last t_b
+ * positions: token i sees every row of the prefix (desc_prefix->seqlens, one length a prefix, or n_max) and the own rows
+ * j <= n_b - t_b + i.
+ *   O = softmax(scale Q [K_prefix; K]^T) [V_prefix; V]
+ *   K_prefix, V_prefix, K, V   bf16, described by the two descriptors as in curdkv_score (d = 128, the same kv_heads; q_heads
+ *             of `desc`); either may have no rows (n_max = 0), and is not followed then
+ *   Q, O      bf16 [batch][q_heads][q_rows][128] with element strides, as in curdkv_cache_attention
+ *   q_lens    device int32 [batch] (clamped to [0, q_rows]), or NULL; output rows i >= t_b are left untouched
+ *   lse       NULL, or fp32 [batch][q_heads][q_rows], as in curdkv_cache_attention
+ *   scale     finite, >= 0
+ * Meant for generation, few tokens a sequence: own rows are read once for every 16 of its query rows.  A query that sees
+ * nothing gives O = 0 and lse = -inf.  Rows at or beyond a length may hold anything, the others must be finite.  Softmax and
+ * sums in fp32, weights rounded to bf16 before they multiply the values, O rounded once; parts are joined in a fixed
+ * order.  Up to three launches.  Workspace (256-byte aligned): its status word collects (it is not cleared)
+ * CURDKV_DEV_BAD_INDEX, a length out of range (it is cut), and CURDKV_DEV_TIMEOUT; two calls that may overlap need a
+ * workspace each. */
+size_t curdkv_attention_prefix_workspace_bytes(const curdkv_desc* desc_prefix, const curdkv_desc* desc, int32_t q_rows);
+curdkv_status curdkv_attention_prefix(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_n,
+                                      const int32_t* q_lens, const void* K_prefix, const void* V_prefix,
+                                      const curdkv_desc* desc_prefix, const void* K, const void* V, const curdkv_desc* desc,
+                                      float scale, void* O, int64_t o_stride_b, int64_t o_stride_h, int64_t o_stride_n, float* lse,
+                                      void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* GQA (Sec. 3.2): query head q uses KV head q / (q_heads / kv_heads).  Writes
  * kv_head_of_q int32 [q_heads] (device) so that attention consumers can index
  * the shared selection without replicating the compacted cache. */

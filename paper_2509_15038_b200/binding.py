@@ -36,6 +36,7 @@ EXPORTS = (
     "curdkv_qcache_attention_workspace_bytes", "curdkv_qcache_attention",
     "curdkv_attention_window_workspace_bytes", "curdkv_attention_window",
     "curdkv_cache_push", "curdkv_cache_attention_workspace_bytes", "curdkv_cache_attention",
+    "curdkv_attention_prefix_workspace_bytes", "curdkv_attention_prefix",
 )
 
 
@@ -163,6 +164,11 @@ def load():
     lib.curdkv_cache_attention.restype = ctypes.c_int
     lib.curdkv_cache_attention.argtypes = [vp, i32, i64, i64, i64, vp, cp, dp, f32, vp, i64, i64, i64, vp, vp, vp,
                                            ctypes.c_size_t, vp]
+    lib.curdkv_attention_prefix_workspace_bytes.restype = ctypes.c_size_t
+    lib.curdkv_attention_prefix_workspace_bytes.argtypes = [dp, dp, i32]
+    lib.curdkv_attention_prefix.restype = ctypes.c_int
+    lib.curdkv_attention_prefix.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, dp, vp, vp, dp, f32, vp, i64, i64, i64, vp, vp,
+                                            ctypes.c_size_t, vp]
     lib.curdkv_selftest_bounded_wait.restype = ctypes.c_int
     lib.curdkv_selftest_bounded_wait.argtypes = [ctypes.c_uint64, vp, vp]
     lib.curdkv_selftest_gather_wait.restype = ctypes.c_int
@@ -840,6 +846,44 @@ def curdkv_cache_attention(Q, cache: DeviceCache, *, scale: float, weights: Opti
     code = load().curdkv_cache_attention(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), cache._ref, ctypes.byref(desc), scale,
                                          O.data_ptr(), o[0], o[1], o[2], _addr(lse), _addr(weights), workspace.data_ptr(),
                                          workspace.numel() * workspace.element_size(), _raw_stream(dev))
+    if code:
+        _check(code, what)
+    return O, workspace
+
+
+# ---- attention of a batch that shares a prefix -----------------------------------------------
+
+def attention_prefix_workspace(desc_prefix: Desc, desc: Desc, q_rows: int, device="cuda") -> torch.Tensor:
+    nbytes = int(load().curdkv_attention_prefix_workspace_bytes(ctypes.byref(desc_prefix), ctypes.byref(desc), int(q_rows)))
+    if nbytes == 0:
+        raise ValueError("invalid shape for curdkv_attention_prefix")
+    return torch.zeros((nbytes,), dtype=torch.uint8, device=device)
+
+
+def curdkv_attention_prefix(Q, K_prefix, V_prefix, desc_prefix: Desc, K, V, desc: Desc, *, scale: float,
+                            q_lens: Optional[torch.Tensor] = None, O=None, lse=None,
+                            workspace: Optional[torch.Tensor] = None):
+    """Attention over shared rows ``[Bp, Hkv, n0, 128]`` and each sequence's own ``[B, Hkv, n, 128]`` behind them; sequences
+    ``i * B / Bp`` onwards share prefix i.  Q bf16 ``[B, Hq, t, 128]``: the last ``q_lens`` (int32 ``[B]``, default t)
+    positions of each sequence, which see the whole prefix; query rows beyond leave O untouched.  Returns (O, workspace)."""
+    what = "curdkv_attention_prefix"
+    O, (B, H, t, _), q, o = _queries(what, Q, O, lse)
+    if B != desc.batch or H != desc.q_heads:
+        raise ValueError(f"{what}: Q and the descriptor differ in batch or query heads")
+    _int32("q_lens", q_lens, B)
+    if workspace is None:
+        workspace = attention_prefix_workspace(desc_prefix, desc, t, device=Q.device)
+    elif not workspace.is_contiguous():
+        raise ValueError(f"{what}: workspace must be contiguous")
+    dev = _on_device(what, Q, K_prefix, V_prefix, K, V, O, lse, q_lens, workspace)
+    _described(what, K_prefix, V_prefix, desc_prefix, dev)
+    _described(what, K, V, desc, dev)
+    if B == 0:
+        return O, workspace
+    code = load().curdkv_attention_prefix(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), _base(K_prefix, Q), _base(V_prefix, Q),
+                                          ctypes.byref(desc_prefix), _base(K, Q), _base(V, Q), ctypes.byref(desc), scale,
+                                          O.data_ptr(), o[0], o[1], o[2], _addr(lse), workspace.data_ptr(),
+                                          workspace.numel() * workspace.element_size(), _raw_stream(dev))
     if code:
         _check(code, what)
     return O, workspace

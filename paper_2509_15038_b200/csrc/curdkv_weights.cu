@@ -110,6 +110,27 @@ bool plan_cache(const curdkv_cache* c, const curdkv_desc* d, int32_t q_rows, Cac
   return true;
 }
 
+// ---- attention behind a shared prefix ----------------------------------------------------------
+struct PrefixPlan {
+  RowsPlan pre, own;
+  size_t pre_at, own_at, bytes;
+};
+
+bool plan_prefix(const curdkv_desc* dp, const curdkv_desc* d, int32_t q_rows, PrefixPlan* pl) {
+  if (!heads_ok(dp) || !heads_ok(d) || q_rows < 1 || dp->n_max < 0 || d->n_max < 0 || dp->n_max > (1 << 30) || d->n_max > (1 << 30))
+    return false;
+  if (dp->kv_heads != d->kv_heads || (d->batch > 0 && (dp->batch < 1 || d->batch % dp->batch != 0))) return false;
+  const int64_t P = (int64_t)d->batch * d->kv_heads, P0 = (int64_t)dp->batch * dp->kv_heads;
+  const int64_t rows = (int64_t)(d->q_heads / d->kv_heads) * q_rows, share = d->batch > 0 ? d->batch / dp->batch : 1;
+  if (P > (1 << 24) || rows > (1 << 24) || rows * share > (1 << 28)) return false;
+  pl->pre = plan_rows(P0, rows * share, dp->n_max);
+  pl->own = plan_rows(P, rows, d->n_max);
+  pl->pre_at = 256;
+  pl->own_at = pl->pre_at + parts_bytes(pl->pre.entries);
+  pl->bytes = pl->own_at + parts_bytes(pl->own.entries);
+  return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -186,6 +207,84 @@ curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_st
   j.weights = weights;
   if (!(pl.rows.nt == 1 ? launch_parts<1, true>(a, ctas, stream) : launch_parts<2, true>(a, ctas, stream))) return CURDKV_ERR_CUDA;
   return launch_join<false, true>(j, P * pl.slices, stream) ? CURDKV_OK : CURDKV_ERR_CUDA;
+}
+
+size_t curdkv_attention_prefix_workspace_bytes(const curdkv_desc* desc_prefix, const curdkv_desc* desc, int32_t q_rows) {
+  PrefixPlan pl;
+  return plan_prefix(desc_prefix, desc, q_rows, &pl) ? pl.bytes : 0;
+}
+
+curdkv_status curdkv_attention_prefix(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_n,
+                                      const int32_t* q_lens, const void* K_prefix, const void* V_prefix,
+                                      const curdkv_desc* desc_prefix, const void* K, const void* V, const curdkv_desc* desc,
+                                      float scale, void* O, int64_t o_stride_b, int64_t o_stride_h, int64_t o_stride_n, float* lse,
+                                      void* workspace, size_t workspace_bytes, void* cuda_stream) {
+  curdkv_status st = check_call(K_prefix, V_prefix, desc_prefix);
+  if (st != CURDKV_OK) return st;
+  if ((st = check_call(K, V, desc)) != CURDKV_OK) return st;
+  if (desc->d != 128 || desc_prefix->d != 128) return CURDKV_ERR_UNSUPPORTED;
+  if (q_rows < 1 || !(scale >= 0.f) || std::isinf(scale)) return CURDKV_ERR_INVALID_ARG;
+  if (desc_prefix->kv_heads != desc->kv_heads) return CURDKV_ERR_INVALID_ARG;
+  if (desc->batch > 0 && (desc_prefix->batch < 1 || desc->batch % desc_prefix->batch != 0)) return CURDKV_ERR_INVALID_ARG;
+  if (!query_strides_ok(Q, q_stride_b, q_stride_h, q_stride_n) || !query_strides_ok(O, o_stride_b, o_stride_h, o_stride_n) ||
+      Q == O || !rows_apart(desc->batch, desc->q_heads, q_rows, o_stride_b, o_stride_h, o_stride_n))
+    return CURDKV_ERR_INVALID_ARG;
+  if (workspace == nullptr || !status_ok(workspace)) return CURDKV_ERR_INVALID_ARG;
+  PrefixPlan pl;
+  if (!plan_prefix(desc_prefix, desc, q_rows, &pl)) return CURDKV_ERR_UNSUPPORTED;
+  if (workspace_bytes < pl.bytes) return CURDKV_ERR_WORKSPACE;
+  const int64_t P = (int64_t)desc->batch * desc->kv_heads, P0 = (int64_t)desc_prefix->batch * desc->kv_heads;
+  if (P == 0) return CURDKV_OK;
+  const int64_t pre_ctas = P0 * pl.pre.blocks * pl.pre.chunks, own_ctas = P * pl.own.blocks * pl.own.chunks;
+  if (pre_ctas > 0x7fffffffLL || own_ctas > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+  cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  const int group = desc->q_heads / desc->kv_heads, share = desc->batch / desc_prefix->batch;
+  rows::JoinArgs j = {};
+  j.prefix = parts_of(pl.pre, ws + pl.pre_at, desc_prefix->seqlens, desc_prefix->n_max);
+  j.own = parts_of(pl.own, ws + pl.own_at, desc->seqlens, desc->n_max);
+  rows::Args a = {};
+  a.scale_log2 = scale * 1.4426950408889634f;
+  a.q_lens = q_lens;
+  a.status = reinterpret_cast<uint32_t*>(ws);
+  auto run = [&](const RowsPlan& r, const rows::Parts& parts, int64_t ctas) {
+    a.blocks = r.blocks;
+    a.chunk = r.chunk;
+    a.chunks = r.chunks;
+    a.part_ml = const_cast<float2*>(parts.ml);
+    a.part_o = const_cast<float*>(parts.o);
+    return r.nt == 1 ? launch_parts<1, false>(a, ctas, stream) : launch_parts<2, false>(a, ctas, stream);
+  };
+  if (desc_prefix->n_max > 0) {
+    a.q = rows::Queries{static_cast<const __nv_bfloat16*>(Q), q_stride_b, q_stride_h, q_stride_n, desc->kv_heads, group, q_rows,
+                        share, share * q_rows * group};
+    a.K = KvView{static_cast<const __nv_bfloat16*>(K_prefix), desc_prefix->k_stride_b, desc_prefix->k_stride_h, desc_prefix->k_stride_n};
+    a.V = KvView{static_cast<const __nv_bfloat16*>(V_prefix), desc_prefix->v_stride_b, desc_prefix->v_stride_h, desc_prefix->v_stride_n};
+    a.lens = desc_prefix->seqlens;
+    a.n_max = desc_prefix->n_max;
+    if (!run(pl.pre, j.prefix, pre_ctas)) return CURDKV_ERR_CUDA;
+  }
+  if (desc->n_max > 0) {
+    a.q = rows::Queries{static_cast<const __nv_bfloat16*>(Q), q_stride_b, q_stride_h, q_stride_n, desc->kv_heads, group, q_rows,
+                        1, q_rows * group};
+    a.K = KvView{static_cast<const __nv_bfloat16*>(K), desc->k_stride_b, desc->k_stride_h, desc->k_stride_n};
+    a.V = KvView{static_cast<const __nv_bfloat16*>(V), desc->v_stride_b, desc->v_stride_h, desc->v_stride_n};
+    a.lens = desc->seqlens;
+    a.n_max = desc->n_max;
+    a.causal = 1;
+    if (!run(pl.own, j.own, own_ctas)) return CURDKV_ERR_CUDA;
+  }
+  j.heads = desc->kv_heads;
+  j.group = group;
+  j.t = q_rows;
+  j.share = share;
+  j.q_lens = q_lens;
+  j.O = static_cast<__nv_bfloat16*>(O);
+  j.o_sb = o_stride_b; j.o_sh = o_stride_h; j.o_sn = o_stride_n;
+  j.lse = lse;
+  j.slices = (group * q_rows + 4 * rows::kJoinWarps - 1) / (4 * rows::kJoinWarps);
+  if (P * j.slices > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+  return launch_join<true, false>(j, P * j.slices, stream) ? CURDKV_OK : CURDKV_ERR_CUDA;
 }
 
 }  // extern "C"
