@@ -464,9 +464,34 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
 /* ---- Eviction by accumulated attention weight (no counterpart in the paper): the rows of a generation-phase cache are ranked
  * by the softmax weight they have received, in place of their l^KV.  cache->raw then holds those weights:
  * curdkv_attention_scores gives a prompt's, curdkv_cache_push brings new rows in and takes the least looked-at ones out,
- * curdkv_cache_attention adds what each step's queries give.
- *
- * One step's bookkeeping: what curdkv_cache_append and curdkv_cache_compress_inplace do one after the other (same arguments,
+ * curdkv_cache_attention adds what each step's queries give. */
+/* Scores of a prompt's rows by the attention weights they receive, in place of their l^KV (what curdkv_score gives):
+ *   scores[b][h][j] = sum over the query heads of KV head h and the live query tokens i of
+ *                     exp(scale q_i . k_j - lse_i), j <= n_b - t_b + i,
+ * causal: sequence b has n_b = desc->seqlens[b] (or n_max) rows and t_b = q_lens[b] (or q_rows) query tokens at the last t_b
+ * positions -- all of the prompt, or its last few, whose view of the rows stands for what comes.  lse_i is the log of
+ * the row's sum of exponentials.  desc->raw_scores = 0 divides by the number of query rows that see something, so that a
+ * head's scores sum to 1; 1 leaves the sums.  curdkv_select, curdkv_compact and curdkv_qcache_store take them as any scores.
+ *   Q          bf16 [batch][q_heads][q_rows][128] with element strides (multiples of 8, channels contiguous, 16-byte
+ *              aligned, positive); query head q reads KV head q / (q_heads / kv_heads)
+ *   K, desc    as in curdkv_score (d = 128; positive strides); values, r, score_mode and whiten are not used
+ *   q_lens     device int32 [batch] (clamped to [0, q_rows]), or NULL
+ *   lse        fp32 [batch][q_heads][q_rows].  lse_given = 1: read, as curdkv_attention_window with a window of n_max leaves
+ *              it, which halves the work (-inf: the row sees nothing).  lse_given = 0: NULL, or written for the
+ *              live tokens (-inf for one that sees nothing)
+ *   scores     fp32 [batch][kv_heads][n_max]; entries j >= n_b are set to 0
+ *   scale      finite, >= 0
+ * Rows of K at or beyond n_b and query rows at or beyond t_b may hold anything, the others must be finite.  Products are
+ * those of bf16 numbers summed in fp32, exponentials and sums fp32, added in a fixed order.  q_heads / kv_heads <= 128;
+ * strides below 2^39 bytes.  Up to four launches.  Workspace (256-byte aligned): its status word collects (it is not
+ * cleared) CURDKV_DEV_TIMEOUT; two calls that may overlap need a workspace each. */
+size_t curdkv_attention_scores_workspace_bytes(const curdkv_desc* desc, int32_t q_rows);
+curdkv_status curdkv_attention_scores(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_n,
+                                      const int32_t* q_lens, const void* K, const curdkv_desc* desc, float scale, float* lse,
+                                      int32_t lse_given, float* scores, void* workspace, size_t workspace_bytes,
+                                      void* cuda_stream);
+
+/* One step's bookkeeping: what curdkv_cache_append and curdkv_cache_compress_inplace do one after the other (same arguments,
  * kept rows, order of slots and status flags), with the new rows' scores given instead of formed with G.
  *   scores_new  fp32 [batch][kv_heads][n_max], or NULL: 0 each (rows to be kept on arrival belong in the window)
  *   desc_new    as in curdkv_cache_append; r, score_mode, raw_scores and whiten are not used

@@ -37,6 +37,7 @@ EXPORTS = (
     "curdkv_attention_window_workspace_bytes", "curdkv_attention_window",
     "curdkv_cache_push", "curdkv_cache_attention_workspace_bytes", "curdkv_cache_attention",
     "curdkv_attention_prefix_workspace_bytes", "curdkv_attention_prefix",
+    "curdkv_attention_scores_workspace_bytes", "curdkv_attention_scores",
 )
 
 
@@ -169,6 +170,10 @@ def load():
     lib.curdkv_attention_prefix.restype = ctypes.c_int
     lib.curdkv_attention_prefix.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp, dp, vp, vp, dp, f32, vp, i64, i64, i64, vp, vp,
                                             ctypes.c_size_t, vp]
+    lib.curdkv_attention_scores_workspace_bytes.restype = ctypes.c_size_t
+    lib.curdkv_attention_scores_workspace_bytes.argtypes = [dp, i32]
+    lib.curdkv_attention_scores.restype = ctypes.c_int
+    lib.curdkv_attention_scores.argtypes = [vp, i32, i64, i64, i64, vp, vp, dp, f32, vp, i32, vp, vp, ctypes.c_size_t, vp]
     lib.curdkv_selftest_bounded_wait.restype = ctypes.c_int
     lib.curdkv_selftest_bounded_wait.argtypes = [ctypes.c_uint64, vp, vp]
     lib.curdkv_selftest_gather_wait.restype = ctypes.c_int
@@ -557,6 +562,21 @@ def _described(what: str, K: torch.Tensor, V: torch.Tensor, desc: Desc, dev: int
         raise ValueError(f"{what}: the descriptor's seqlens are on {lens.device}")
 
 
+def _described_keys(what: str, K: torch.Tensor, desc: Desc, dev: int) -> None:
+    """The same where only K is read."""
+    B, H, _, n, d, _, kb, kh, kn, _, _, _ = _DESC_ROWS(desc)
+    shape, k = K.shape, K.stride()
+    if K.dtype is not torch.bfloat16:
+        raise TypeError(f"{what}: K must be bf16")
+    if shape != (B, H, n, d):
+        raise ValueError(f"{what}: K is {tuple(shape)}, the descriptor says {(B, H, n, d)}")
+    if k != (kb, kh, kn, 1) and any(n > 1 and a != c for n, a, c in zip(shape, k, (kb, kh, kn, 1))):
+        raise ValueError(f"{what}: K has other strides than the descriptor")
+    lens = getattr(desc, "seqlens_tensor", None)
+    if lens is not None and lens.get_device() != dev:
+        raise ValueError(f"{what}: the descriptor's seqlens are on {lens.device}")
+
+
 def _int32(what: str, t: Optional[torch.Tensor], numel: Optional[int] = None) -> None:
     if t is not None and (t.dtype is not torch.int32 or not t.is_contiguous() or (numel is not None and t.numel() != numel)):
         raise ValueError(f"{what} must be a contiguous int32 tensor" + (f" of {numel} entries" if numel is not None else ""))
@@ -785,6 +805,53 @@ def curdkv_attention_window(Q, K, V, desc: Desc, window: int, *, num_sink: int =
 
 
 # ---- generation over a cache whose rows are ranked by the attention weights they receive --------
+
+def attention_scores_workspace(desc: Desc, q_rows: int, device="cuda") -> torch.Tensor:
+    nbytes = int(load().curdkv_attention_scores_workspace_bytes(ctypes.byref(desc), int(q_rows)))
+    if nbytes == 0:
+        raise ValueError("invalid shape for curdkv_attention_scores")
+    return torch.zeros((nbytes,), dtype=torch.uint8, device=device)
+
+
+def curdkv_attention_scores(Q, K, desc: Desc, *, scale: float, q_lens: Optional[torch.Tensor] = None,
+                            lse: Optional[torch.Tensor] = None, lse_given: bool = False,
+                            scores: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Scores fp32 ``[B, Hkv, n_max]`` of the rows of K: the causal softmax weights they receive from Q bf16 ``[B, Hq, t, 128]``,
+    the last ``q_lens`` (default t) tokens of each sequence of ``desc``, summed over query heads and tokens (normalised
+    unless ``desc.raw_scores``).  ``lse`` fp32 ``[B, Hq, t]`` receives the log sums, or with ``lse_given`` brings them.
+    Returns (scores, workspace)."""
+    what = "curdkv_attention_scores"
+    shape, q = Q.shape, Q.stride()
+    if Q.dtype is not torch.bfloat16 or len(shape) != 4 or q[3] != 1 or shape[3] != 128:
+        raise ValueError(f"{what}: Q must be bf16 [B, H, rows, 128] with a contiguous last axis")
+    B, H, t, _ = shape
+    if B != desc.batch or H != desc.q_heads:
+        raise ValueError(f"{what}: Q and the descriptor differ in batch or query heads")
+    _int32("q_lens", q_lens, B)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != shape[:3] or not lse.is_contiguous()):
+        raise ValueError(f"{what}: lse must be contiguous fp32 [B, H, rows]")
+    if lse_given and lse is None:
+        raise ValueError(f"{what}: lse_given without lse")
+    out = (B, desc.kv_heads, desc.n_max)
+    if scores is None:
+        scores = torch.empty(out, dtype=torch.float32, device=Q.device)
+    elif scores.dtype is not torch.float32 or scores.shape != out or not scores.is_contiguous():
+        raise ValueError(f"{what}: scores must be contiguous fp32 {out}")
+    if workspace is None:
+        workspace = attention_scores_workspace(desc, t, device=Q.device)
+    elif not workspace.is_contiguous():
+        raise ValueError(f"{what}: workspace must be contiguous")
+    dev = _on_device(what, Q, K, q_lens, lse, scores, workspace)
+    _described_keys(what, K, desc, dev)
+    if B == 0:
+        return scores, workspace
+    code = load().curdkv_attention_scores(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), _base(K, Q), ctypes.byref(desc), scale,
+                                          _addr(lse), int(bool(lse_given)), _base(scores, Q), workspace.data_ptr(),
+                                          workspace.numel() * workspace.element_size(), _raw_stream(dev))
+    if code:
+        _check(code, what)
+    return scores, workspace
+
 
 def curdkv_cache_push(cache: DeviceCache, K_new, V_new, budget: int, workspace: torch.Tensor, *, num_sink: int = 0,
                       window: int = 0, scores_new: Optional[torch.Tensor] = None,

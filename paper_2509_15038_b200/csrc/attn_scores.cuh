@@ -1,0 +1,432 @@
+// Attention weights of a prompt summed per key: w_j = sum over query rows r of 2^(x_rj - L_r), x = scale log2(e) q_r . k_j over
+// the keys that row sees, L_r = log2 of its sum of exponentials.  No values, no output rows: two streams of logits that
+// stay on the SM.
+//
+//   rows     S = Q K^T, a thread per query row: running maximum and sum, L_r                    (skipped when L is given)
+//   columns  S^T = K Q^T, a thread per key: w_j is a sum along the thread's own row of the accumulator
+//
+// Transposing the second product puts each sum into one thread: no exchange between lanes, no atomics, a fixed order.
+// Both are one kernel: "fixed" operand tiles A (M side: a thread a row of them) against a stream of tiles B.  A CTA works on
+// a pair of A tiles, four epilogue warps each, so that every B tile is used twice; the accumulators (128 x 128 fp32) are
+// double-buffered per A tile and fill TMEM.  What a pair sees -- the key tiles up to its last position, the row tiles from
+// its first one on -- is cut into units of at most `seg` B tiles, dealt to the persistent CTAs longest first, in
+// alternating direction.
+//
+// Query rows of a KV head are tiled as tokens x heads of the group (a 5-D map), so a tile of 128 rows is 128 / group tokens:
+// few tokens of many heads fill a tile, and little of a tile lies beyond the diagonal.
+#pragma once
+#include "umma_ptx.cuh"
+
+namespace curdkv {
+namespace umma {
+
+struct ScoreArgs {
+  const int32_t* seqlens;            // [batch] or nullptr
+  const int32_t* q_lens;             // [batch] or nullptr
+  int batch, heads, group, q_rows, n_max;
+  int tokens;                        // of a row tile: 128 / group; tokens * group rows
+  int row_tiles, key_tiles;          // per (sequence, KV head)
+  int segs, seg;                     // units per pair, B tiles of a unit at most
+  int units;                         // pairs * batch * heads * segs
+  float scale_log2;
+  float2* stats;                     // rows: [segs][batch * heads][row_tiles][128] maximum (log2 units), sum
+  const float* logsum;               // columns: [batch * heads][row_tiles][128] L, +inf for rows that do not count
+  float* out;                        // columns: [segs][batch * heads][n_max]
+  int normalise;                     // columns: out is final (segs = 1) and divided by the rows that count
+  uint32_t* status;
+  unsigned long long wait_ns = kWaitLimitNs;
+};
+
+constexpr int kScoreThreads = 320;                         // TMA, MMA, 2 x 4 epilogue warps
+constexpr int kScoreRing = 3;
+constexpr int kScoreA = 0;                                 // two pairs of A tiles
+constexpr int kScoreB = 4 * kSlotBytes;
+constexpr int kScoreLog = kScoreB + kScoreRing * kSlotBytes;          // L of the row tile in each B slot
+constexpr int kScoreBar = kScoreLog + kScoreRing * 512;
+constexpr int kScoreDynamic = kScoreBar + 256 + 1024;
+constexpr int kScoreTmemCols = 512;                        // S of A tile g, buffer u at 128 (2 g + u)
+constexpr float kScoreSlack = 8.f;
+
+// The live query tokens of a sequence and where they stand.
+struct ScoreSeq {
+  int n, q, pos0;                                          // rows, tokens, position of token 0
+  __device__ __forceinline__ ScoreSeq(const ScoreArgs& a, int b) {
+    n = seq_len_of(a.seqlens, b, a.n_max);
+    q = a.q_lens != nullptr ? min(max(a.q_lens[b], 0), a.q_rows) : a.q_rows;
+    pos0 = n - q;
+  }
+};
+
+// A unit: a pair of A tiles of one (sequence, KV head) and a run of B tiles.
+template <bool COLS>
+struct ScoreUnit {
+  int p, b, h, seg, a0, count, first, steps;               // A tiles a0 .. a0 + count - 1; B tiles first .. first + steps - 1
+  __device__ __forceinline__ ScoreUnit(const ScoreArgs& a, int unit) {
+    const int tiles = COLS ? a.key_tiles : a.row_tiles, P = a.batch * a.heads, pairs = (tiles + 1) / 2;
+    seg = unit % a.segs;
+    p = unit / a.segs % P;
+    const int at = unit / a.segs / P;
+    a0 = 2 * (COLS ? at : pairs - 1 - at);                 // longest first
+    count = min(2, tiles - a0);
+    b = p / a.heads;
+    h = p % a.heads;
+    const ScoreSeq s(a, b);
+    int end;
+    if (COLS) {                                            // row tiles whose last token stands at or behind the first key
+      end = (s.q + a.tokens - 1) / a.tokens;
+      first = max(0, a0 * kTileRows - s.pos0) / a.tokens;
+      if (a0 * kTileRows >= s.n) end = 0;
+    } else {                                               // key tiles up to the pair's last position
+      const int tok = min((a0 + count) * a.tokens, s.q);   // tokens below this
+      end = tok > a0 * a.tokens ? (max(s.pos0 + tok, 0) + kTileRows - 1) / kTileRows : 0;
+      first = 0;
+    }
+    first += seg * a.seg;
+    steps = min(max(end - first, 0), a.seg);
+  }
+};
+
+// map_q: 5-D (channel, head of the group, token, KV head, sequence), boxes of 64 x group x tokens; map_k: tiles of 128 rows.
+template <bool COLS>
+__global__ void __launch_bounds__(kScoreThreads, 1)
+score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const ScoreArgs a) {
+  extern __shared__ unsigned char smem_dyn[];
+  const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+  unsigned char* base_ptr = smem_dyn + (base - smem_u32(smem_dyn));
+  const uint32_t bar0 = base + kScoreBar;
+  auto a_full = [&](uint32_t s) { return bar0 + 8u * s; };
+  auto a_empty = [&](uint32_t s) { return bar0 + 16u + 8u * s; };
+  auto b_full = [&](uint32_t s) { return bar0 + 32u + 8u * s; };
+  auto b_empty = [&](uint32_t s) { return bar0 + 32u + 8u * (kScoreRing + s); };
+  const uint32_t gbar = bar0 + 32u + 16u * kScoreRing;
+  auto s_full = [&](uint32_t g, uint32_t u) { return gbar + 16u * g + 8u * u; };
+  auto s_empty = [&](uint32_t g, uint32_t u) { return gbar + 32u + 16u * g + 8u * u; };
+  const uint32_t drain_bar = gbar + 64u;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(base_ptr + kScoreBar + 32 + 16 * kScoreRing + 72);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int rows_used = a.tokens * a.group;                // of a row tile
+
+  if (tid == 0) {
+    for (int s = 0; s < 2; ++s) { mbar_init(a_full(s), 1); mbar_init(a_empty(s), 1); }
+    // (columns: the eight epilogue warps read the row tile's L beside the product)
+    for (int s = 0; s < kScoreRing; ++s) { mbar_init(b_full(s), 1); mbar_init(b_empty(s), COLS ? 9 : 1); }
+    for (int g = 0; g < 2; ++g)
+      for (int u = 0; u < 2; ++u) { mbar_init(s_full(g, u), 1); mbar_init(s_empty(g, u), 4); }
+    mbar_init(drain_bar, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  // rows of a query tile that no copy ever fills: zeros
+  if (rows_used < kTileRows) {
+    const int slots = COLS ? kScoreRing : 4, from = COLS ? kScoreB : kScoreA, dead = (kTileRows - rows_used) * 8;
+    for (int x = tid; x < slots * 2 * dead; x += kScoreThreads) {
+      const int half = x / dead, y = x % dead;             // half tiles lie kHalfBytes apart
+      *reinterpret_cast<uint4*>(base_ptr + from + half * kHalfBytes + rows_used * 128 + y * 16) = make_uint4(0u, 0u, 0u, 0u);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)),
+                 "r"((uint32_t)kScoreTmemCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  constexpr uint32_t tmem_base = 0u;                       // all 512 columns are this CTA's: they begin at 0
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");       // L comes from the kernel before
+
+  // unit number k of this CTA: the deal changes direction every round
+  auto unit_at = [&](int k) {
+    const int G = (int)gridDim.x, c = (int)blockIdx.x;
+    return (int64_t)k * G + ((k & 1) ? G - 1 - c : c);
+  };
+  if (warp == 0) {
+    // ------------------------------------------------------------ TMA producer
+    if (lane == 0) {
+      uint64_t keep;
+      asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep));
+      const uint32_t q_bytes = (uint32_t)rows_used * 256u;
+      bool ok = true;
+      uint32_t it = 0, pairs = 0;
+      auto wait = [&](uint32_t bar, uint32_t parity) { return ok = ok && mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns); };
+      auto load_q = [&](uint32_t dst, uint32_t bar, int tile, const ScoreUnit<COLS>& u) {
+        tma_load_5d(dst, &map_q, bar, 0, 0, tile * a.tokens, u.h, u.b);
+        tma_load_5d(dst + kHalfBytes, &map_q, bar, 64, 0, tile * a.tokens, u.h, u.b);
+      };
+      auto load_k = [&](uint32_t dst, uint32_t bar, int tile, const ScoreUnit<COLS>& u) {
+        tma_load_4d(dst, &map_k, bar, 0, tile * kTileRows, u.h, u.b, keep);
+        tma_load_4d(dst + kHalfBytes, &map_k, bar, 64, tile * kTileRows, u.h, u.b, keep);
+      };
+      for (int k = 0; ok && unit_at(k) < a.units; ++k) {
+        const ScoreUnit<COLS> u(a, (int)unit_at(k));
+        if (u.steps == 0) continue;
+        const uint32_t s = pairs & 1u;
+        if (!wait(a_empty(s), ((pairs >> 1) & 1u) ^ 1u)) break;
+        ++pairs;
+        mbar_arrive_expect_tx(a_full(s), (uint32_t)u.count * (COLS ? (uint32_t)kSlotBytes : q_bytes));
+        for (int g = 0; g < u.count; ++g) {
+          const uint32_t dst = base + kScoreA + (2 * s + g) * kSlotBytes;
+          if (COLS) load_k(dst, a_full(s), u.a0 + g, u); else load_q(dst, a_full(s), u.a0 + g, u);
+        }
+        for (int x = 0; x < u.steps; ++x, ++it) {
+          const uint32_t slot = it % kScoreRing;
+          if (!wait(b_empty(slot), ((it / kScoreRing) & 1u) ^ 1u)) break;
+          const uint32_t dst = base + kScoreB + slot * kSlotBytes;
+          const int tile = u.first + x;
+          mbar_arrive_expect_tx(b_full(slot), COLS ? q_bytes + 512u : (uint32_t)kSlotBytes);
+          if (COLS) {
+            load_q(dst, b_full(slot), tile, u);
+            bulk_load(base + kScoreLog + slot * 512, a.logsum + ((int64_t)u.p * a.row_tiles + tile) * kTileRows, 512u, b_full(slot));
+          } else {
+            load_k(dst, b_full(slot), tile, u);
+          }
+        }
+      }
+      if (!ok) {                                           // let what was issued land before the CTA ends
+        auto land = [&](uint32_t bar, uint32_t parity) {
+          const unsigned long long t0 = global_ns();
+          while (!mbar_try_wait(bar, parity) && global_ns() - t0 < a.wait_ns) {}
+        };
+        for (uint32_t x = it - min(it, (uint32_t)kScoreRing); x < it; ++x) land(b_full(x % kScoreRing), (x / kScoreRing) & 1u);
+        for (uint32_t x = pairs - min(pairs, 2u); x < pairs; ++x) land(a_full(x & 1u), (x >> 1) & 1u);
+      }
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------ products: the whole warp waits, one lane issues
+    constexpr uint32_t kSlotUnits = kSlotBytes >> 4;
+    const uint64_t a_desc0 = smem_desc_sw128(base + kScoreA), b_desc0 = smem_desc_sw128(base + kScoreB);
+    constexpr uint32_t idesc = instr_desc_bf16(kTileRows);
+    bool ok = true;
+    uint32_t it = 0, pairs = 0, done[2] = {0, 0};          // B tiles, pairs, products of each A tile
+    auto wait = [&](uint32_t bar, uint32_t parity) { ok = mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns) && ok; };
+    for (int k = 0; ok && unit_at(k) < a.units; ++k) {
+      const ScoreUnit<COLS> u(a, (int)unit_at(k));
+      if (u.steps == 0) continue;
+      const uint32_t s = pairs & 1u;
+      wait(a_full(s), (pairs >> 1) & 1u);
+      ++pairs;
+      for (int x = 0; x < u.steps; ++x, ++it) {
+        const uint32_t slot = it % kScoreRing;
+        wait(b_full(slot), (it / kScoreRing) & 1u);
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          if (g >= u.count) continue;
+          const uint32_t buf = done[g] & 1u;
+          wait(s_empty(g, buf), ((done[g] >> 1) & 1u) ^ 1u);
+          ++done[g];
+          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+          tc_fence_after();
+          const uint64_t ad = a_desc0 + (2 * s + g) * kSlotUnits, bd = b_desc0 + slot * kSlotUnits;
+          if (elect_one()) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const uint32_t off = (uint32_t)(e >> 2) * (kHalfBytes >> 4) + (uint32_t)(e & 3) * 2u;
+              tc_mma_bf16(tmem_base + 128u * (2 * g + buf), ad + off, bd + off, idesc, e > 0);
+            }
+            tc_commit(s_full(g, buf));
+          }
+          __syncwarp();
+        }
+        if (!ok) break;
+        if (elect_one()) tc_commit(b_empty(slot));
+        __syncwarp();
+      }
+      if (!ok) break;
+      if (elect_one()) tc_commit(a_empty(s));
+      __syncwarp();
+    }
+    if (!ok) {
+      if (elect_one()) tc_commit(drain_bar);
+      __syncwarp();
+      const unsigned long long t0 = global_ns();
+      while (!mbar_try_wait(drain_bar, 0) && global_ns() - t0 < a.wait_ns) {}
+    }
+  } else {
+    // ------------------------------------------------------------ epilogue: thread r of A tile g
+    const int g = (warp - 2) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    const uint32_t lane_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
+    const float sc = a.scale_log2;
+    const uint64_t sc2 = pack2(sc, sc);
+    bool ok = true;
+    uint32_t it = 0, done = 0;
+    for (int k = 0; ok && unit_at(k) < a.units; ++k) {
+      const ScoreUnit<COLS> u(a, (int)unit_at(k));
+      const ScoreSeq seq(a, u.b);
+      const bool mine = g < u.count;
+      const int P = a.batch * a.heads;
+      if (COLS) {
+        const int key = (u.a0 + g) * kTileRows + r;
+        uint64_t part[2] = {0ull, 0ull};
+        for (int x = 0; x < u.steps; ++x, ++it) {
+          const uint32_t slot = it % kScoreRing;
+          // (L of the row tile lands with it; a group without a tile keeps pace, its arrivals count)
+          ok = mbar_wait(b_full(slot), (it / kScoreRing) & 1u, abort_flag, a.status, a.wait_ns);
+          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+          if (mine) {
+            const uint32_t buf = done & 1u;
+            ok = mbar_wait(s_full(g, buf), (done >> 1) & 1u, abort_flag, a.status, a.wait_ns);
+            if (!(ok = __all_sync(0xffffffffu, ok))) break;
+            ++done;
+            tc_fence_after();
+            const uint32_t s_addr = lane_addr + 128u * (2 * g + buf);
+            const float4* L = reinterpret_cast<const float4*>(base_ptr + kScoreLog + slot * 512);
+            const int tile = u.first + x, tok0 = tile * a.tokens;
+            // columns [c_lo, c_hi) count: tokens at or behind this key, and those that exist
+            const int c_hi = min(seq.q - tok0, a.tokens) * a.group;
+            const int ahead = key - (seq.pos0 + tok0), c_lo = ahead > 0 ? min(ahead, a.tokens) * a.group : 0;
+            const bool whole = __all_sync(0xffffffffu, c_lo == 0) && c_hi >= rows_used;
+#pragma unroll
+            for (int c0 = 0; c0 < 128; c0 += 32) {
+              float v[32];
+              tmem_ld32(s_addr + c0, v);
+              tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) {
+                const float4 l4 = L[(c0 + e) >> 2];
+                float x0, x1, x2, x3;
+                unpack2(fma2(pack2(v[e], v[e + 1]), sc2, pack2(-l4.x, -l4.y)), x0, x1);
+                unpack2(fma2(pack2(v[e + 2], v[e + 3]), sc2, pack2(-l4.z, -l4.w)), x2, x3);
+                if (!whole) {
+                  const int c = c0 + e;
+                  if (c < c_lo || c >= c_hi) x0 = -INFINITY;
+                  if (c + 1 < c_lo || c + 1 >= c_hi) x1 = -INFINITY;
+                  if (c + 2 < c_lo || c + 2 >= c_hi) x2 = -INFINITY;
+                  if (c + 3 < c_lo || c + 3 >= c_hi) x3 = -INFINITY;
+                }
+                part[0] = add2(part[0], pack2(fast_exp2(x0), fast_exp2(x1)));
+                part[1] = add2(part[1], pack2(fast_exp2(x2), fast_exp2(x3)));
+              }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (elect_one()) mbar_arrive(s_empty(g, buf));
+          }
+          __syncwarp();
+          if (elect_one()) mbar_arrive(b_empty(slot));
+        }
+        if (ok && mine && key < a.n_max) {
+          float p0, p1;
+          unpack2(add2(part[0], part[1]), p0, p1);
+          float w = p0 + p1;
+          if (a.normalise) w *= 1.f / (float)max(min(seq.q, seq.n) * a.group, 1);
+          a.out[((int64_t)u.seg * P + u.p) * a.n_max + key] = key < seq.n ? w : 0.f;
+        }
+      } else if (mine) {
+        const int tile = u.a0 + g, tok = tile * a.tokens + r / a.group;
+        const int pos = r < rows_used && tok < seq.q ? seq.pos0 + tok : -1;        // keys up to here
+        float top = -INFINITY, sum = 0.f;
+        for (int x = 0; x < u.steps; ++x) {
+          const uint32_t buf = done & 1u;
+          ok = mbar_wait(s_full(g, buf), (done >> 1) & 1u, abort_flag, a.status, a.wait_ns);
+          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+          ++done;
+          tc_fence_after();
+          const uint32_t s_addr = lane_addr + 128u * (2 * g + buf);
+          float v[128];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, *reinterpret_cast<float(*)[32]>(v + 32 * c));
+          tmem_ld_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (elect_one()) mbar_arrive(s_empty(g, buf));   // S is in registers
+          const int see = pos + 1 - (u.first + x) * kTileRows;                     // columns below this
+          if (__any_sync(0xffffffffu, see < kTileRows)) {
+#pragma unroll
+            for (int e = 0; e < 128; ++e)
+              if (e >= see) v[e] = -INFINITY;
+          }
+          float ext[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+          for (int e = 4; e < 124; e += 8)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ext[j] = max3(ext[j], v[e + 2 * j], v[e + 2 * j + 1]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) ext[j] = fmaxf(ext[j], v[124 + j]);
+          const float tile_top = fmaxf(fmaxf(ext[0], ext[1]), fmaxf(ext[2], ext[3])) * sc;
+          if (tile_top > top + kScoreSlack || top == -INFINITY) {
+            const float now = fmaxf(top, tile_top);
+            sum *= now == -INFINITY ? 1.f : fast_exp2(top - now);
+            top = now;
+          }
+          const float ref = top == -INFINITY ? 0.f : top;
+          const uint64_t nref2 = pack2(-ref, -ref);
+          uint64_t part[2] = {0ull, 0ull};
+#pragma unroll
+          for (int e = 0; e < 128; e += 2) {
+            float x0, x1;
+            unpack2(fma2(pack2(v[e], v[e + 1]), sc2, nref2), x0, x1);
+            part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], pack2(fast_exp2(x0), fast_exp2(x1)));
+          }
+          float p0, p1;
+          unpack2(add2(part[0], part[1]), p0, p1);
+          sum += p0 + p1;
+        }
+        if (ok && u.steps > 0)
+          a.stats[(((int64_t)u.seg * P + u.p) * a.row_tiles + tile) * kTileRows + r] = make_float2(top, sum);
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)kScoreTmemCols)
+                 : "memory");
+  }
+}
+
+// L of every query row, from the parts of the rows pass or from log sums that the caller has; +inf where a row does not count.
+// grid = batch * heads * row tiles, block = 128.
+__global__ void __launch_bounds__(128) score_logsum_kernel(const ScoreArgs a, const float* given, float* logsum, float* lse_out) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int tile = blockIdx.x % a.row_tiles, p = blockIdx.x / a.row_tiles, b = p / a.heads, h = p % a.heads, r = threadIdx.x;
+  const ScoreSeq s(a, b);
+  const int tok = tile * a.tokens + r / a.group;
+  const bool live = r < a.tokens * a.group && tok < s.q;
+  const int64_t at = ((int64_t)b * a.heads * a.group + h * a.group + r % a.group) * a.q_rows + tok;
+  float L = INFINITY;
+  if (live && s.pos0 + tok >= 0) {
+    if (given != nullptr) {
+      L = given[at] * 1.4426950408889634f;
+      if (L == -INFINITY) L = INFINITY;                    // (a row that saw nothing)
+    } else {
+      // the pair of tiles this one belongs to walked these key tiles
+      const int end_tok = min((tile / 2 * 2 + min(2, a.row_tiles - tile / 2 * 2)) * a.tokens, s.q);
+      const int used = (((s.pos0 + end_tok) + kTileRows - 1) / kTileRows + a.seg - 1) / a.seg;
+      float top = -INFINITY, sum = 0.f;
+      for (int g = 0; g < used; ++g)
+        top = fmaxf(top, a.stats[(((int64_t)g * a.batch * a.heads + p) * a.row_tiles + tile) * kTileRows + r].x);
+      for (int g = 0; g < used; ++g) {
+        const float2 e = a.stats[(((int64_t)g * a.batch * a.heads + p) * a.row_tiles + tile) * kTileRows + r];
+        sum += e.y * (top == -INFINITY ? 1.f : fast_exp2(e.x - top));
+      }
+      L = sum == 0.f ? INFINITY : top + log2f(sum);
+    }
+  }
+  logsum[((int64_t)p * a.row_tiles + tile) * kTileRows + r] = L;
+  if (live && lse_out != nullptr) lse_out[at] = L == INFINITY ? -INFINITY : L * 0.6931471805599453f;
+}
+
+// Sums the units' parts of each key in order.  grid = batch * heads * ceil(n_max / 256), block = 256.
+__global__ void __launch_bounds__(256) score_sum_kernel(const ScoreArgs a, const float* parts, float* scores, int normalise) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int each = (a.n_max + 255) / 256, p = blockIdx.x / each, key = blockIdx.x % each * 256 + threadIdx.x;
+  if (key >= a.n_max) return;
+  const ScoreSeq s(a, p / a.heads);
+  float w = 0.f;
+  if (key < s.n) {
+    for (int g = 0; g < a.segs; ++g) w += parts[((int64_t)g * a.batch * a.heads + p) * a.n_max + key];
+    if (normalise) w *= 1.f / (float)max(min(s.q, s.n) * a.group, 1);
+  }
+  scores[(int64_t)p * a.n_max + key] = w;
+}
+
+}  // namespace umma
+}  // namespace curdkv

@@ -42,10 +42,6 @@
 
 namespace curdkv {
 
-// Map of a bf16 tensor [batch][heads][rows][128] for tiles of 128 rows (defined beside the C ABI).
-bool rows_map(CUtensorMap* map, const void* base, int32_t batch, int32_t heads, int32_t rows, int64_t stride_b,
-              int64_t stride_h, int64_t stride_n);
-
 namespace umma {
 
 struct WindowArgs {

@@ -254,6 +254,22 @@ bool rows_map(CUtensorMap* map, const void* base, int32_t batch, int32_t heads, 
   return make_tile_map(map, base, &d, stride_b, stride_h, stride_n);
 }
 
+bool bf16_map(CUtensorMap* map, const void* base, int rank, const uint64_t* sizes, const int64_t* strides, const uint32_t* box) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (fn == nullptr || rank < 2 || rank > 5) return false;
+  cuuint64_t dims[5], bytes[4];
+  cuuint32_t boxes[5], estr[5];
+  for (int i = 0; i < rank; ++i) {
+    dims[i] = sizes[i];
+    boxes[i] = box[i];
+    estr[i] = 1;
+    if (i > 0) bytes[i - 1] = sizes[i] > 1 ? (cuuint64_t)strides[i] * 2 : 256;   // a size-1 axis never moves: any legal stride
+  }
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), dims, bytes, boxes, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 curdkv_status check_call(const void* K, const void* V, const curdkv_desc* desc) {
   const curdkv_status st = check_desc(desc);
   return st != CURDKV_OK ? st : check_kv(K, V, desc);
