@@ -7,10 +7,14 @@
 //
 // Transposing the second product puts each sum into one thread: no exchange between lanes, no atomics, a fixed order.
 // Both are one kernel: "fixed" operand tiles A (M side: a thread a row of them) against a stream of tiles B.  A CTA works on
-// a pair of A tiles, four epilogue warps each, so that every B tile is used twice; the accumulators (128 x 128 fp32) are
-// double-buffered per A tile and fill TMEM.  What a pair sees -- the key tiles up to its last position, the row tiles from
+// a pair of A tiles, eight epilogue warps each (two threads a row, 64 columns each), so that every B tile is used twice; three accumulators
+// (128 x 128 fp32) go round.  What a pair sees -- the key tiles up to its last position, the row tiles from
 // its first one on -- is cut into units of at most `seg` B tiles, dealt to the persistent CTAs longest first, in
 // alternating direction.
+//
+// A's operand comes from TMEM: a product of 128 x 128 x 16 reads 4 KB of shared memory then instead of 8, and takes 67 cycles
+// instead of 130.  The epilogue warps bring the next unit's A tiles there, each its row, as soon as the last product with the
+// one before has retired, and only then turn to that product's sums: the tensor pipe does not wait for the change.
 //
 // Query rows of a KV head are tiled as tokens x heads of the group (a 5-D map), so a tile of 128 rows is 128 / group tokens:
 // few tokens of many heads fill a tile, and little of a tile lies beyond the diagonal.
@@ -28,24 +32,27 @@ struct ScoreArgs {
   int row_tiles, key_tiles;          // per (sequence, KV head)
   int segs, seg;                     // units per pair, B tiles of a unit at most
   int units;                         // pairs * batch * heads * segs
-  float scale_log2;
-  float2* stats;                     // rows: [segs][batch * heads][row_tiles][128] maximum (log2 units), sum
-  const float* logsum;               // columns: [batch * heads][row_tiles][128] L, +inf for rows that do not count
-  float* out;                        // columns: [segs][batch * heads][n_max]
-  int normalise;                     // columns: out is final (segs = 1) and divided by the rows that count
+  float scale_log2;                  // scale log2(e)
+  float log2_of_ln, ln_of_log2;      // from natural log sums to L and back: log2(e) times what rounding made of scale_log2
+  float2* stats;                     // rows: [segs][2][batch * heads][row_tiles][128] maximum (log2 units), sum
+  const float* logsum;               // columns: [batch * heads][row_tiles][128] -L, -inf for rows that do not count
+  float* out;                        // columns: [segs][2][batch * heads][n_max]; [batch * heads][n_max], 0 before, where segs = 1
+  int normalise;                     // columns: divide by the rows that count (segs = 1)
   uint32_t* status;
   unsigned long long wait_ns = kWaitLimitNs;
 };
 
-constexpr int kScoreThreads = 320;                         // TMA, MMA, 2 x 4 epilogue warps
-constexpr int kScoreRing = 3;
-constexpr int kScoreA = 0;                                 // two pairs of A tiles
-constexpr int kScoreB = 4 * kSlotBytes;
-constexpr int kScoreLog = kScoreB + kScoreRing * kSlotBytes;          // L of the row tile in each B slot
+constexpr int kScoreThreads = 576;                         // TMA, MMA, 2 x 8 epilogue warps
+constexpr int kScoreRing = 4;
+constexpr int kScoreA = 0;                                 // a pair of A tiles on its way to TMEM
+constexpr int kScoreB = 2 * kSlotBytes;
+constexpr int kScoreLog = kScoreB + kScoreRing * kSlotBytes;          // -L of the row tile in each B slot
 constexpr int kScoreBar = kScoreLog + kScoreRing * 512;
 constexpr int kScoreDynamic = kScoreBar + 256 + 1024;
-constexpr int kScoreTmemCols = 512;                        // S of A tile g, buffer u at 128 (2 g + u)
+constexpr int kScoreTmemCols = 512;                        // three accumulators of 128 columns, then A tile g at 384 + 64 g
+constexpr uint32_t kScoreTmemA = 384, kScoreBufs = 3;
 constexpr float kScoreSlack = 8.f;
+constexpr int kScorePoly = 2;                              // of 8 pairs of exponentials, how many the FMA pipe takes
 
 // The live query tokens of a sequence and where they stand.
 struct ScoreSeq {
@@ -86,6 +93,24 @@ struct ScoreUnit {
   }
 };
 
+// The units of a CTA in turn, those without steps passed over: the deal changes direction every round.
+template <bool COLS>
+struct ScoreDeal {
+  int64_t at;                                              // unit, or beyond the last
+  int k;
+  __device__ __forceinline__ void next(const ScoreArgs& a, ScoreUnit<COLS>& u) {
+    for (;; ++k) {
+      const int G = (int)gridDim.x, c = (int)blockIdx.x;
+      at = (int64_t)k * G + ((k & 1) ? G - 1 - c : c);
+      if (at >= a.units) return;
+      u = ScoreUnit<COLS>(a, (int)at);
+      if (u.steps > 0) break;
+    }
+    ++k;
+  }
+  __device__ __forceinline__ bool more(const ScoreArgs& a) const { return at < a.units; }
+};
+
 // map_q: 5-D (channel, head of the group, token, KV head, sequence), boxes of 64 x group x tokens; map_k: tiles of 128 rows.
 template <bool COLS>
 __global__ void __launch_bounds__(kScoreThreads, 1)
@@ -94,32 +119,34 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
   const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
   unsigned char* base_ptr = smem_dyn + (base - smem_u32(smem_dyn));
   const uint32_t bar0 = base + kScoreBar;
-  auto a_full = [&](uint32_t s) { return bar0 + 8u * s; };
-  auto a_empty = [&](uint32_t s) { return bar0 + 16u + 8u * s; };
-  auto b_full = [&](uint32_t s) { return bar0 + 32u + 8u * s; };
-  auto b_empty = [&](uint32_t s) { return bar0 + 32u + 8u * (kScoreRing + s); };
-  const uint32_t gbar = bar0 + 32u + 16u * kScoreRing;
-  auto s_full = [&](uint32_t g, uint32_t u) { return gbar + 16u * g + 8u * u; };
-  auto s_empty = [&](uint32_t g, uint32_t u) { return gbar + 32u + 16u * g + 8u * u; };
-  const uint32_t drain_bar = gbar + 64u;
-  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(base_ptr + kScoreBar + 32 + 16 * kScoreRing + 72);
+  auto a_full = [&](uint32_t g) { return bar0 + 8u * g; };             // in shared memory
+  auto a_empty = [&](uint32_t g) { return bar0 + 16u + 8u * g; };
+  auto a_ready = [&](uint32_t g) { return bar0 + 32u + 8u * g; };      // in TMEM
+  auto s_full = [&](uint32_t u) { return bar0 + 48u + 8u * u; };
+  auto s_empty = [&](uint32_t u) { return bar0 + 48u + 8u * (kScoreBufs + u); };
+  const uint32_t bbar = bar0 + 48u + 16u * kScoreBufs;
+  auto b_full = [&](uint32_t s) { return bbar + 8u * s; };
+  auto b_empty = [&](uint32_t s) { return bbar + 8u * (kScoreRing + s); };
+  constexpr int kBars = 48 + 16 * (int)kScoreBufs + 16 * kScoreRing;
+  const uint32_t drain_bar = bar0 + kBars;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(base_ptr + kScoreBar + kBars + 8);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  static_assert(kBars + 16 <= 256, "barriers fit");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rows_used = a.tokens * a.group;                // of a row tile
 
   if (tid == 0) {
-    for (int s = 0; s < 2; ++s) { mbar_init(a_full(s), 1); mbar_init(a_empty(s), 1); }
-    // (columns: the eight epilogue warps read the row tile's L beside the product)
-    for (int s = 0; s < kScoreRing; ++s) { mbar_init(b_full(s), 1); mbar_init(b_empty(s), COLS ? 9 : 1); }
-    for (int g = 0; g < 2; ++g)
-      for (int u = 0; u < 2; ++u) { mbar_init(s_full(g, u), 1); mbar_init(s_empty(g, u), 4); }
+    for (int g = 0; g < 2; ++g) { mbar_init(a_full(g), 1); mbar_init(a_empty(g), 8); mbar_init(a_ready(g), 8); }
+    // (columns: the sixteen epilogue warps read the row tile's L beside the product)
+    for (int s = 0; s < kScoreRing; ++s) { mbar_init(b_full(s), 1); mbar_init(b_empty(s), COLS ? 17 : 1); }
+    for (uint32_t u = 0; u < kScoreBufs; ++u) { mbar_init(s_full(u), 1); mbar_init(s_empty(u), 8); }
     mbar_init(drain_bar, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   // rows of a query tile that no copy ever fills: zeros
   if (rows_used < kTileRows) {
-    const int slots = COLS ? kScoreRing : 4, from = COLS ? kScoreB : kScoreA, dead = (kTileRows - rows_used) * 8;
+    const int slots = COLS ? kScoreRing : 2, from = COLS ? kScoreB : kScoreA, dead = (kTileRows - rows_used) * 8;
     for (int x = tid; x < slots * 2 * dead; x += kScoreThreads) {
       const int half = x / dead, y = x % dead;             // half tiles lie kHalfBytes apart
       *reinterpret_cast<uint4*>(base_ptr + from + half * kHalfBytes + rows_used * 128 + y * 16) = make_uint4(0u, 0u, 0u, 0u);
@@ -139,11 +166,9 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");       // L comes from the kernel before
 
-  // unit number k of this CTA: the deal changes direction every round
-  auto unit_at = [&](int k) {
-    const int G = (int)gridDim.x, c = (int)blockIdx.x;
-    return (int64_t)k * G + ((k & 1) ? G - 1 - c : c);
-  };
+  ScoreUnit<COLS> u(a, 0);
+  ScoreDeal<COLS> deal{0, 0};
+  deal.next(a, u);
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
     if (lane == 0) {
@@ -151,39 +176,33 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep));
       const uint32_t q_bytes = (uint32_t)rows_used * 256u;
       bool ok = true;
-      uint32_t it = 0, pairs = 0;
+      uint32_t it = 0, tiles[2] = {0, 0};
       auto wait = [&](uint32_t bar, uint32_t parity) { return ok = ok && mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns); };
-      auto load_q = [&](uint32_t dst, uint32_t bar, int tile, const ScoreUnit<COLS>& u) {
-        tma_load_5d(dst, &map_q, bar, 0, 0, tile * a.tokens, u.h, u.b);
-        tma_load_5d(dst + kHalfBytes, &map_q, bar, 64, 0, tile * a.tokens, u.h, u.b);
-      };
-      auto load_k = [&](uint32_t dst, uint32_t bar, int tile, const ScoreUnit<COLS>& u) {
-        tma_load_4d(dst, &map_k, bar, 0, tile * kTileRows, u.h, u.b, keep);
-        tma_load_4d(dst + kHalfBytes, &map_k, bar, 64, tile * kTileRows, u.h, u.b, keep);
-      };
-      for (int k = 0; ok && unit_at(k) < a.units; ++k) {
-        const ScoreUnit<COLS> u(a, (int)unit_at(k));
-        if (u.steps == 0) continue;
-        const uint32_t s = pairs & 1u;
-        if (!wait(a_empty(s), ((pairs >> 1) & 1u) ^ 1u)) break;
-        ++pairs;
-        mbar_arrive_expect_tx(a_full(s), (uint32_t)u.count * (COLS ? (uint32_t)kSlotBytes : q_bytes));
-        for (int g = 0; g < u.count; ++g) {
-          const uint32_t dst = base + kScoreA + (2 * s + g) * kSlotBytes;
-          if (COLS) load_k(dst, a_full(s), u.a0 + g, u); else load_q(dst, a_full(s), u.a0 + g, u);
+      auto load = [&](bool queries, uint32_t dst, uint32_t bar, int tile) {
+        if (queries) {
+          tma_load_5d(dst, &map_q, bar, 0, 0, tile * a.tokens, u.h, u.b);
+          tma_load_5d(dst + kHalfBytes, &map_q, bar, 64, 0, tile * a.tokens, u.h, u.b);
+        } else {
+          tma_load_4d(dst, &map_k, bar, 0, tile * kTileRows, u.h, u.b, keep);
+          tma_load_4d(dst + kHalfBytes, &map_k, bar, 64, tile * kTileRows, u.h, u.b, keep);
         }
-        for (int x = 0; x < u.steps; ++x, ++it) {
+      };
+      for (; ok && deal.more(a); deal.next(a, u)) {
+        for (int g = 0; g < u.count; ++g) {
+          if (!wait(a_empty(g), (tiles[g] & 1u) ^ 1u)) break;
+          ++tiles[g];
+          mbar_arrive_expect_tx(a_full(g), COLS ? (uint32_t)kSlotBytes : q_bytes);
+          load(!COLS, base + kScoreA + g * kSlotBytes, a_full(g), u.a0 + g);
+        }
+        for (int x = 0; ok && x < u.steps; ++x) {
           const uint32_t slot = it % kScoreRing;
           if (!wait(b_empty(slot), ((it / kScoreRing) & 1u) ^ 1u)) break;
-          const uint32_t dst = base + kScoreB + slot * kSlotBytes;
+          ++it;
           const int tile = u.first + x;
           mbar_arrive_expect_tx(b_full(slot), COLS ? q_bytes + 512u : (uint32_t)kSlotBytes);
-          if (COLS) {
-            load_q(dst, b_full(slot), tile, u);
+          load(COLS, base + kScoreB + slot * kSlotBytes, b_full(slot), tile);
+          if (COLS)
             bulk_load(base + kScoreLog + slot * 512, a.logsum + ((int64_t)u.p * a.row_tiles + tile) * kTileRows, 512u, b_full(slot));
-          } else {
-            load_k(dst, b_full(slot), tile, u);
-          }
         }
       }
       if (!ok) {                                           // let what was issued land before the CTA ends
@@ -192,52 +211,47 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
           while (!mbar_try_wait(bar, parity) && global_ns() - t0 < a.wait_ns) {}
         };
         for (uint32_t x = it - min(it, (uint32_t)kScoreRing); x < it; ++x) land(b_full(x % kScoreRing), (x / kScoreRing) & 1u);
-        for (uint32_t x = pairs - min(pairs, 2u); x < pairs; ++x) land(a_full(x & 1u), (x >> 1) & 1u);
+        for (int g = 0; g < 2; ++g)
+          if (tiles[g] > 0) land(a_full(g), (tiles[g] - 1) & 1u);
       }
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ products: the whole warp waits, one lane issues
-    constexpr uint32_t kSlotUnits = kSlotBytes >> 4;
-    const uint64_t a_desc0 = smem_desc_sw128(base + kScoreA), b_desc0 = smem_desc_sw128(base + kScoreB);
     constexpr uint32_t idesc = instr_desc_bf16(kTileRows);
+    const uint64_t b_desc0 = smem_desc_sw128(base + kScoreB);
     bool ok = true;
-    uint32_t it = 0, pairs = 0, done[2] = {0, 0};          // B tiles, pairs, products of each A tile
+    uint32_t it = 0, done = 0, tiles[2] = {0, 0};          // B tiles, products, A tiles
     auto wait = [&](uint32_t bar, uint32_t parity) { ok = mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns) && ok; };
-    for (int k = 0; ok && unit_at(k) < a.units; ++k) {
-      const ScoreUnit<COLS> u(a, (int)unit_at(k));
-      if (u.steps == 0) continue;
-      const uint32_t s = pairs & 1u;
-      wait(a_full(s), (pairs >> 1) & 1u);
-      ++pairs;
-      for (int x = 0; x < u.steps; ++x, ++it) {
+    for (; ok && deal.more(a); deal.next(a, u)) {
+      for (int x = 0; ok && x < u.steps; ++x, ++it) {
         const uint32_t slot = it % kScoreRing;
         wait(b_full(slot), (it / kScoreRing) & 1u);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
-          if (g >= u.count) continue;
-          const uint32_t buf = done[g] & 1u;
-          wait(s_empty(g, buf), ((done[g] >> 1) & 1u) ^ 1u);
-          ++done[g];
-          if (!(ok = __all_sync(0xffffffffu, ok))) break;
+          if (g >= u.count || !ok) continue;
+          if (x == 0) {
+            wait(a_ready(g), tiles[g] & 1u);
+            ++tiles[g];
+          }
+          const uint32_t buf = done % kScoreBufs;
+          wait(s_empty(buf), ((done / kScoreBufs) & 1u) ^ 1u);
+          ++done;
+          if (!(ok = __all_sync(0xffffffffu, ok))) continue;
           tc_fence_after();
-          const uint64_t ad = a_desc0 + (2 * s + g) * kSlotUnits, bd = b_desc0 + slot * kSlotUnits;
+          const uint64_t bd = b_desc0 + slot * (kSlotBytes >> 4);
           if (elect_one()) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const uint32_t off = (uint32_t)(e >> 2) * (kHalfBytes >> 4) + (uint32_t)(e & 3) * 2u;
-              tc_mma_bf16(tmem_base + 128u * (2 * g + buf), ad + off, bd + off, idesc, e > 0);
+              tc_mma_bf16_ts(tmem_base + 128u * buf, tmem_base + kScoreTmemA + 64u * g + 8u * e, bd + off, idesc, e > 0);
             }
-            tc_commit(s_full(g, buf));
+            tc_commit(s_full(buf));
           }
           __syncwarp();
         }
-        if (!ok) break;
-        if (elect_one()) tc_commit(b_empty(slot));
+        if (ok && elect_one()) tc_commit(b_empty(slot));
         __syncwarp();
       }
-      if (!ok) break;
-      if (elect_one()) tc_commit(a_empty(s));
-      __syncwarp();
     }
     if (!ok) {
       if (elect_one()) tc_commit(drain_bar);
@@ -246,106 +260,136 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       while (!mbar_try_wait(drain_bar, 0) && global_ns() - t0 < a.wait_ns) {}
     }
   } else {
-    // ------------------------------------------------------------ epilogue: thread r of A tile g
-    const int g = (warp - 2) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+    // ------------------------------------------------------------ epilogue: row r of A tile g, columns 64 half onwards
+    const int g = (warp - 2) >> 3, half = ((warp - 2) >> 2) & 1, quarter = warp & 3, r = quarter * 32 + lane;
     const uint32_t lane_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
     const float sc = a.scale_log2;
     const uint64_t sc2 = pack2(sc, sc);
+    const int P = a.batch * a.heads;
     bool ok = true;
-    uint32_t it = 0, done = 0;
-    for (int k = 0; ok && unit_at(k) < a.units; ++k) {
-      const ScoreUnit<COLS> u(a, (int)unit_at(k));
+    uint32_t it = 0, done = 0, tiles = 0;                  // B tiles, products before this step, this group's A tiles
+    // Brings A tile g of the unit `v` into TMEM (this thread: 64 channels of row r).  The products with the one before have
+    // all retired.
+    auto stage = [&](const ScoreUnit<COLS>& v) {
+      if (g >= v.count) return;
+      ok = mbar_wait(a_full(g), tiles & 1u, abort_flag, a.status, a.wait_ns) && ok;
+      if (!(ok = __all_sync(0xffffffffu, ok))) return;
+      ++tiles;
+      float w[32];
+      const unsigned char* src = base_ptr + kScoreA + g * kSlotBytes + half * kHalfBytes + r * 128;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) *reinterpret_cast<float4*>(w + 4 * c) = *reinterpret_cast<const float4*>(src + ((c ^ (r & 7)) * 16));
+      tmem_st32(lane_addr + kScoreTmemA + 64u * g + 32u * half, w);
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (elect_one()) {
+        mbar_arrive(a_ready(g));
+        mbar_arrive(a_empty(g));
+      }
+      __syncwarp();
+    };
+    if (deal.more(a)) stage(u);
+    while (ok && deal.more(a)) {
       const ScoreSeq seq(a, u.b);
       const bool mine = g < u.count;
-      const int P = a.batch * a.heads;
-      if (COLS) {
-        const int key = (u.a0 + g) * kTileRows + r;
-        uint64_t part[2] = {0ull, 0ull};
-        for (int x = 0; x < u.steps; ++x, ++it) {
-          const uint32_t slot = it % kScoreRing;
-          // (L of the row tile lands with it; a group without a tile keeps pace, its arrivals count)
-          ok = mbar_wait(b_full(slot), (it / kScoreRing) & 1u, abort_flag, a.status, a.wait_ns);
-          if (!(ok = __all_sync(0xffffffffu, ok))) break;
-          if (mine) {
-            const uint32_t buf = done & 1u;
-            ok = mbar_wait(s_full(g, buf), (done >> 1) & 1u, abort_flag, a.status, a.wait_ns);
-            if (!(ok = __all_sync(0xffffffffu, ok))) break;
-            ++done;
-            tc_fence_after();
-            const uint32_t s_addr = lane_addr + 128u * (2 * g + buf);
-            const float4* L = reinterpret_cast<const float4*>(base_ptr + kScoreLog + slot * 512);
-            const int tile = u.first + x, tok0 = tile * a.tokens;
-            // columns [c_lo, c_hi) count: tokens at or behind this key, and those that exist
-            const int c_hi = min(seq.q - tok0, a.tokens) * a.group;
-            const int ahead = key - (seq.pos0 + tok0), c_lo = ahead > 0 ? min(ahead, a.tokens) * a.group : 0;
-            const bool whole = __all_sync(0xffffffffu, c_lo == 0) && c_hi >= rows_used;
+      ScoreUnit<COLS> then = u;
+      deal.next(a, then);
+      float top = -INFINITY, sum = 0.f, lost = 0.f;
+      const int key = (u.a0 + g) * kTileRows + r;          // columns
+      const int tok = (u.a0 + g) * a.tokens + r / a.group; // rows
+      const int pos = !COLS && r < rows_used && tok < seq.q ? seq.pos0 + tok : -1;           // keys up to here
+      for (int x = 0; x < u.steps; ++x, ++it) {
+        // A group without a tile waits for the other's product, so that it stays less than a round of the accumulators behind
+        // or ahead (a barrier tells only two rounds apart), and its arrivals below mean what they say.
+        const uint32_t product = done + (mine ? g : 0), slot = it % kScoreRing, buf = product % kScoreBufs;
+        done += u.count;
+        if (COLS) ok = mbar_wait(b_full(slot), (it / kScoreRing) & 1u, abort_flag, a.status, a.wait_ns);
+        ok = ok && mbar_wait(s_full(buf), (product / kScoreBufs) & 1u, abort_flag, a.status, a.wait_ns);
+        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+        tc_fence_after();
+        if (x == u.steps - 1 && deal.more(a)) {            // this group's A tile is done with
+          stage(then);
+          if (!ok) break;
+        }
+        const uint32_t s_addr = lane_addr + 128u * buf + 64u * half;
+        if (COLS && mine) {
+          const float4* L = reinterpret_cast<const float4*>(base_ptr + kScoreLog + slot * 512 + 256 * half);
+          const int tok0 = (u.first + x) * a.tokens;
+          // columns [c_lo, c_hi) count: tokens at or behind this key, and those that exist
+          const int c_hi = min(seq.q - tok0, a.tokens) * a.group - 64 * half;
+          const int ahead = key - (seq.pos0 + tok0), c_lo = (ahead > 0 ? min(ahead, a.tokens) * a.group : 0) - 64 * half;
+          uint64_t part[4] = {0ull, 0ull, 0ull, 0ull};
+          if (__all_sync(0xffffffffu, c_lo <= 0) && c_hi >= rows_used - 64 * half) {
+            float v[2][32];
+            tmem_ld32(s_addr, v[0]);
 #pragma unroll
-            for (int c0 = 0; c0 < 128; c0 += 32) {
+            for (int c = 0; c < 2; ++c) {
+              tmem_ld_wait();
+              if (c < 1) tmem_ld32(s_addr + 32, v[1]);
+              const float(&w)[32] = v[c];
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) {
+                const float4 l4 = L[8 * c + (e >> 2)];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                  const int j = (e >> 1) + i;
+                  const uint64_t x2 = fma2(pack2(w[2 * j], w[2 * j + 1]), sc2, i == 0 ? pack2(l4.x, l4.y) : pack2(l4.z, l4.w));
+                  part[j & 3] = add2(part[j & 3], j % 8 < kScorePoly ? exp2_pair_fma(x2) : exp2_pair(x2));
+                }
+              }
+            }
+          } else {
+#pragma unroll 1
+            for (int c0 = 0; c0 < 64; c0 += 32) {
               float v[32];
               tmem_ld32(s_addr + c0, v);
               tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                const float4 l4 = L[(c0 + e) >> 2];
-                float x0, x1, x2, x3;
-                unpack2(fma2(pack2(v[e], v[e + 1]), sc2, pack2(-l4.x, -l4.y)), x0, x1);
-                unpack2(fma2(pack2(v[e + 2], v[e + 3]), sc2, pack2(-l4.z, -l4.w)), x2, x3);
-                if (!whole) {
-                  const int c = c0 + e;
-                  if (c < c_lo || c >= c_hi) x0 = -INFINITY;
-                  if (c + 1 < c_lo || c + 1 >= c_hi) x1 = -INFINITY;
-                  if (c + 2 < c_lo || c + 2 >= c_hi) x2 = -INFINITY;
-                  if (c + 3 < c_lo || c + 3 >= c_hi) x3 = -INFINITY;
-                }
-                part[0] = add2(part[0], pack2(fast_exp2(x0), fast_exp2(x1)));
-                part[1] = add2(part[1], pack2(fast_exp2(x2), fast_exp2(x3)));
+              for (int e = 0; e < 32; e += 2) {
+                const float2 l2 = reinterpret_cast<const float2*>(L)[(c0 + e) >> 1];
+                const int c = c0 + e;
+                const float x0 = c < c_lo || c >= c_hi ? -INFINITY : fmaf(v[e], sc, l2.x);
+                const float x1 = c + 1 < c_lo || c + 1 >= c_hi ? -INFINITY : fmaf(v[e + 1], sc, l2.y);
+                part[(e >> 1) & 3] = add2(part[(e >> 1) & 3], pack2(fast_exp2(x0), fast_exp2(x1)));
               }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (elect_one()) mbar_arrive(s_empty(g, buf));
           }
+          tc_fence_before();
+          __syncwarp();
+          if (elect_one()) mbar_arrive(s_empty(buf));
+          float p0, p1;
+          unpack2(add2(add2(part[0], part[1]), add2(part[2], part[3])), p0, p1);
+          // the tiles' sums are added with what their additions lose (thousands of rows may follow one another)
+          const float y = (p0 + p1) - lost, now = sum + y;
+          lost = (now - sum) - y;
+          sum = now;
+        }
+        if (COLS) {
           __syncwarp();
           if (elect_one()) mbar_arrive(b_empty(slot));
         }
-        if (ok && mine && key < a.n_max) {
-          float p0, p1;
-          unpack2(add2(part[0], part[1]), p0, p1);
-          float w = p0 + p1;
-          if (a.normalise) w *= 1.f / (float)max(min(seq.q, seq.n) * a.group, 1);
-          a.out[((int64_t)u.seg * P + u.p) * a.n_max + key] = key < seq.n ? w : 0.f;
-        }
-      } else if (mine) {
-        const int tile = u.a0 + g, tok = tile * a.tokens + r / a.group;
-        const int pos = r < rows_used && tok < seq.q ? seq.pos0 + tok : -1;        // keys up to here
-        float top = -INFINITY, sum = 0.f;
-        for (int x = 0; x < u.steps; ++x) {
-          const uint32_t buf = done & 1u;
-          ok = mbar_wait(s_full(g, buf), (done >> 1) & 1u, abort_flag, a.status, a.wait_ns);
-          if (!(ok = __all_sync(0xffffffffu, ok))) break;
-          ++done;
-          tc_fence_after();
-          const uint32_t s_addr = lane_addr + 128u * (2 * g + buf);
-          float v[128];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, *reinterpret_cast<float(*)[32]>(v + 32 * c));
+        if (!COLS && mine) {
+          float v[64];
+          tmem_ld32(s_addr, *reinterpret_cast<float(*)[32]>(v));
+          tmem_ld32(s_addr + 32, *reinterpret_cast<float(*)[32]>(v + 32));
           tmem_ld_wait();
           tc_fence_before();
           __syncwarp();
-          if (elect_one()) mbar_arrive(s_empty(g, buf));   // S is in registers
-          const int see = pos + 1 - (u.first + x) * kTileRows;                     // columns below this
-          if (__any_sync(0xffffffffu, see < kTileRows)) {
+          if (elect_one()) mbar_arrive(s_empty(buf));      // S is in registers
+          const int see = pos + 1 - (u.first + x) * kTileRows - 64 * half;         // columns below this
+          if (__any_sync(0xffffffffu, see < 64)) {
 #pragma unroll
-            for (int e = 0; e < 128; ++e)
+            for (int e = 0; e < 64; ++e)
               if (e >= see) v[e] = -INFINITY;
           }
           float ext[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-          for (int e = 4; e < 124; e += 8)
+          for (int e = 4; e < 60; e += 8)
 #pragma unroll
             for (int j = 0; j < 4; ++j) ext[j] = max3(ext[j], v[e + 2 * j], v[e + 2 * j + 1]);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) ext[j] = fmaxf(ext[j], v[124 + j]);
+          for (int j = 0; j < 4; ++j) ext[j] = fmaxf(ext[j], v[60 + j]);
           const float tile_top = fmaxf(fmaxf(ext[0], ext[1]), fmaxf(ext[2], ext[3])) * sc;
           if (tile_top > top + kScoreSlack || top == -INFINITY) {
             const float now = fmaxf(top, tile_top);
@@ -354,20 +398,27 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
           }
           const float ref = top == -INFINITY ? 0.f : top;
           const uint64_t nref2 = pack2(-ref, -ref);
-          uint64_t part[2] = {0ull, 0ull};
+          uint64_t part[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
-          for (int e = 0; e < 128; e += 2) {
-            float x0, x1;
-            unpack2(fma2(pack2(v[e], v[e + 1]), sc2, nref2), x0, x1);
-            part[(e >> 1) & 1] = add2(part[(e >> 1) & 1], pack2(fast_exp2(x0), fast_exp2(x1)));
+          for (int e = 0; e < 64; e += 2) {
+            const uint64_t x2 = fma2(pack2(v[e], v[e + 1]), sc2, nref2);
+            part[(e >> 1) & 3] = add2(part[(e >> 1) & 3], (e >> 1) % 8 < kScorePoly ? exp2_pair_fma(x2) : exp2_pair(x2));
           }
           float p0, p1;
-          unpack2(add2(part[0], part[1]), p0, p1);
+          unpack2(add2(add2(part[0], part[1]), add2(part[2], part[3])), p0, p1);
           sum += p0 + p1;
         }
-        if (ok && u.steps > 0)
-          a.stats[(((int64_t)u.seg * P + u.p) * a.row_tiles + tile) * kTileRows + r] = make_float2(top, sum);
       }
+      if (!ok) break;
+      if (COLS && mine && key < seq.n) {
+        if (a.segs == 1)                                   // two halves are added to 0: either order gives the same
+          atomicAdd(a.out + (int64_t)u.p * a.n_max + key, a.normalise ? sum * (1.f / (float)max(min(seq.q, seq.n) * a.group, 1)) : sum);
+        else
+          a.out[((int64_t)(2 * u.seg + half) * P + u.p) * a.n_max + key] = sum;
+      }
+      if (!COLS && mine)
+        a.stats[(((int64_t)(2 * u.seg + half) * P + u.p) * a.row_tiles + (u.a0 + g)) * kTileRows + r] = make_float2(top, sum);
+      u = then;
     }
   }
 
@@ -381,10 +432,12 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
   }
 }
 
-// L of every query row, from the parts of the rows pass or from log sums that the caller has; +inf where a row does not count.
-// grid = batch * heads * row tiles, block = 128.
-__global__ void __launch_bounds__(128) score_logsum_kernel(const ScoreArgs a, const float* given, float* logsum, float* lse_out) {
+// -L of every query row, from the parts of the rows pass or from log sums that the caller has; -inf where a row does not count.
+// Clears `clear` floats of `scores` beside it.  grid = batch * heads * row tiles, block = 128.
+__global__ void __launch_bounds__(128) score_logsum_kernel(const ScoreArgs a, const float* given, float* logsum, float* lse_out,
+                                                           float* scores, int64_t clear) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  for (int64_t x = (int64_t)blockIdx.x * 128 + threadIdx.x; x < clear; x += (int64_t)gridDim.x * 128) scores[x] = 0.f;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tile = blockIdx.x % a.row_tiles, p = blockIdx.x / a.row_tiles, b = p / a.heads, h = p % a.heads, r = threadIdx.x;
   const ScoreSeq s(a, b);
@@ -394,12 +447,12 @@ __global__ void __launch_bounds__(128) score_logsum_kernel(const ScoreArgs a, co
   float L = INFINITY;
   if (live && s.pos0 + tok >= 0) {
     if (given != nullptr) {
-      L = given[at] * 1.4426950408889634f;
+      L = given[at] * a.log2_of_ln;
       if (L == -INFINITY) L = INFINITY;                    // (a row that saw nothing)
     } else {
       // the pair of tiles this one belongs to walked these key tiles
       const int end_tok = min((tile / 2 * 2 + min(2, a.row_tiles - tile / 2 * 2)) * a.tokens, s.q);
-      const int used = (((s.pos0 + end_tok) + kTileRows - 1) / kTileRows + a.seg - 1) / a.seg;
+      const int used = 2 * ((((s.pos0 + end_tok) + kTileRows - 1) / kTileRows + a.seg - 1) / a.seg);
       float top = -INFINITY, sum = 0.f;
       for (int g = 0; g < used; ++g)
         top = fmaxf(top, a.stats[(((int64_t)g * a.batch * a.heads + p) * a.row_tiles + tile) * kTileRows + r].x);
@@ -410,8 +463,8 @@ __global__ void __launch_bounds__(128) score_logsum_kernel(const ScoreArgs a, co
       L = sum == 0.f ? INFINITY : top + log2f(sum);
     }
   }
-  logsum[((int64_t)p * a.row_tiles + tile) * kTileRows + r] = L;
-  if (live && lse_out != nullptr) lse_out[at] = L == INFINITY ? -INFINITY : L * 0.6931471805599453f;
+  logsum[((int64_t)p * a.row_tiles + tile) * kTileRows + r] = -L;
+  if (live && lse_out != nullptr) lse_out[at] = L == INFINITY ? -INFINITY : L * a.ln_of_log2;
 }
 
 // Sums the units' parts of each key in order.  grid = batch * heads * ceil(n_max / 256), block = 256.
@@ -422,7 +475,10 @@ __global__ void __launch_bounds__(256) score_sum_kernel(const ScoreArgs a, const
   const ScoreSeq s(a, p / a.heads);
   float w = 0.f;
   if (key < s.n) {
-    for (int g = 0; g < a.segs; ++g) w += parts[((int64_t)g * a.batch * a.heads + p) * a.n_max + key];
+    // what the key's pair of tiles sees, and so the units that had something to do
+    const int first = max(0, key / (2 * kTileRows) * (2 * kTileRows) - s.pos0) / a.tokens, end = (s.q + a.tokens - 1) / a.tokens;
+    const int used = end > first ? 2 * ((end - first + a.seg - 1) / a.seg) : 0;
+    for (int g = 0; g < used; ++g) w += parts[((int64_t)g * a.batch * a.heads + p) * a.n_max + key];
     if (normalise) w *= 1.f / (float)max(min(s.q, s.n) * a.group, 1);
   }
   scores[(int64_t)p * a.n_max + key] = w;

@@ -17,11 +17,11 @@ struct ScoresPlan {
   size_t stats_at, logsum_at, parts_at, bytes;
 };
 
-// B tiles a unit takes: four units a CTA, so that the last round costs little, but eight tiles each (a unit costs about one
+// B tiles a unit takes: eight units a CTA, so that the last round costs little, but eight tiles each (a unit costs about one
 // beside them) while that leaves every SM one.
 int unit_length(int64_t steps) {
   const int64_t n = sms();
-  int64_t seg = (steps + 4 * n - 1) / (4 * n), each = (steps + n - 1) / n;
+  int64_t seg = (steps + 8 * n - 1) / (8 * n), each = (steps + n - 1) / n;
   const int64_t least = each < 8 ? each : 8;
   if (seg < least) seg = least;
   return (int)(seg < 1 ? 1 : seg);
@@ -47,9 +47,9 @@ bool plan_scores(const curdkv_desc* d, int32_t q_rows, ScoresPlan* pl) {
   pl->key_segs = (pl->row_tiles + pl->key_seg - 1) / pl->key_seg;
   const size_t rows = (size_t)P * pl->row_tiles * kTileRows;
   pl->stats_at = 256;
-  pl->logsum_at = pl->stats_at + round256(rows * pl->row_segs * sizeof(float2));
+  pl->logsum_at = pl->stats_at + round256(rows * pl->row_segs * 2 * sizeof(float2));
   pl->parts_at = pl->logsum_at + round256(rows * sizeof(float));
-  pl->bytes = pl->parts_at + (pl->key_segs > 1 ? round256((size_t)P * pl->key_segs * d->n_max * sizeof(float)) : 0);
+  pl->bytes = pl->parts_at + (pl->key_segs > 1 ? round256((size_t)P * pl->key_segs * 2 * d->n_max * sizeof(float)) : 0);
   return P * row_pairs * pl->row_segs <= 0x7fffffff && P * key_pairs * pl->key_segs <= 0x7fffffff && P * pl->row_tiles <= 0x7fffffff &&
          P * ((d->n_max + 255) / 256) <= 0x7fffffff;
 }
@@ -120,7 +120,13 @@ curdkv_status curdkv_attention_scores(const void* Q, int32_t q_rows, int64_t q_s
   a.row_tiles = pl.row_tiles;
   a.key_tiles = pl.key_tiles;
   // (products are masked before they are scaled, and -inf times 0 would be NaN)
-  a.scale_log2 = scale * 1.4426950408889634f > FLT_MIN ? scale * 1.4426950408889634f : FLT_MIN;
+  const float scale_log2 = (float)((double)scale * 1.4426950408889634);
+  a.scale_log2 = scale_log2 > FLT_MIN ? scale_log2 : FLT_MIN;
+  // Log sums carry the factor that the logits really get: with L = scale_log2 / scale times the natural one, what rounding
+  // did to scale_log2 cancels where a key weighs something (6e-7 of a weight for logits of 10 otherwise).
+  const double ratio = scale_log2 > FLT_MIN ? (double)scale_log2 / scale : 1.4426950408889634;
+  a.log2_of_ln = (float)ratio;
+  a.ln_of_log2 = (float)(1.0 / ratio);
   a.stats = reinterpret_cast<float2*>(ws + pl.stats_at);
   a.status = reinterpret_cast<uint32_t*>(ws);
   float* logsum = reinterpret_cast<float*>(ws + pl.logsum_at);
@@ -130,7 +136,8 @@ curdkv_status curdkv_attention_scores(const void* Q, int32_t q_rows, int64_t q_s
   a.units = (int)(P * ((pl.row_tiles + 1) / 2) * pl.row_segs);
   if (d.n_max == 0) {                                      // no scores; a query that sees nothing has a log sum all the same
     if (lse == nullptr || lse_given) return CURDKV_OK;
-    return launch(umma::score_logsum_kernel, P * pl.row_tiles, kTileRows, 0, false, stream, a, (const float*)nullptr, logsum, lse)
+    return launch(umma::score_logsum_kernel, P * pl.row_tiles, kTileRows, 0, false, stream, a, (const float*)nullptr, logsum, lse,
+                  scores, (int64_t)0)
                ? CURDKV_OK : CURDKV_ERR_CUDA;
   }
   if (!bf16_map(&mq, Q, 5, sizes, strides, box) ||
@@ -146,7 +153,8 @@ curdkv_status curdkv_attention_scores(const void* Q, int32_t q_rows, int64_t q_s
               stream, mq, mk, a))
     return CURDKV_ERR_CUDA;
   if (!launch(umma::score_logsum_kernel, P * pl.row_tiles, kTileRows, 0, !lse_given, stream, a,
-              (const float*)(lse_given ? lse : nullptr), logsum, lse_given ? (float*)nullptr : lse))
+              (const float*)(lse_given ? lse : nullptr), logsum, lse_given ? (float*)nullptr : lse, scores,
+              pl.key_segs > 1 ? (int64_t)0 : P * d.n_max))
     return CURDKV_ERR_CUDA;
   a.segs = pl.key_segs;
   a.seg = pl.key_seg;
