@@ -1,8 +1,10 @@
 // Generation over a cache whose rows collect the attention weights they receive, and the attention of a
 // batch that shares a prefix.  Argument checks and kernel launches.
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 
+#include "attn_prefix.cuh"
 #include "attn_rows.cuh"
 #include "host.cuh"
 
@@ -113,20 +115,51 @@ bool plan_cache(const curdkv_cache* c, const curdkv_desc* d, int32_t q_rows, Cac
 // ---- attention behind a shared prefix ----------------------------------------------------------
 struct PrefixPlan {
   RowsPlan pre, own;
+  bool tiles;                        // the prefix in 128-row tiles on the tensor cores
+  int seqs, tokens, token_tiles, row_tiles, chunk, chunks;
   size_t pre_at, own_at, bytes;
 };
+
+// The tile form of the prefix: CTAs (one an SM) per tile of query rows so that their rounds, each as long as its run of key
+// tiles and some eight tiles more (start, first and last tile, output), end soonest.
+void plan_tiles(int64_t problems, int share, int t, int group, int64_t keys, PrefixPlan* pl) {
+  const int most = kTileRows / group;                      // (sequence, token) pairs of a tile
+  pl->tokens = t < most ? t : most;
+  pl->seqs = most / pl->tokens < share ? most / pl->tokens : share;
+  pl->token_tiles = (t + pl->tokens - 1) / pl->tokens;
+  pl->row_tiles = (share + pl->seqs - 1) / pl->seqs * pl->token_tiles;
+  const int64_t key_tiles = (keys + kTileRows - 1) / kTileRows, items = problems * pl->row_tiles, places = sms();
+  int64_t best = -1;
+  for (int64_t c = 1; c <= key_tiles && c <= 512; ++c) {
+    const int64_t each = (key_tiles + c - 1) / c, cost = (items * c + places - 1) / places * (each + 8);
+    if (best < 0 || cost < best) {
+      best = cost;
+      pl->chunk = (int)each * kTileRows;
+      pl->chunks = (int)((key_tiles + each - 1) / each);
+    }
+    if (items * c > 8 * places) break;                     // (many rounds are even enough)
+  }
+}
 
 bool plan_prefix(const curdkv_desc* dp, const curdkv_desc* d, int32_t q_rows, PrefixPlan* pl) {
   if (!heads_ok(dp) || !heads_ok(d) || q_rows < 1 || dp->n_max < 0 || d->n_max < 0 || dp->n_max > (1 << 30) || d->n_max > (1 << 30))
     return false;
   if (dp->kv_heads != d->kv_heads || (d->batch > 0 && (dp->batch < 1 || d->batch % dp->batch != 0))) return false;
   const int64_t P = (int64_t)d->batch * d->kv_heads, P0 = (int64_t)dp->batch * dp->kv_heads;
-  const int64_t rows = (int64_t)(d->q_heads / d->kv_heads) * q_rows, share = d->batch > 0 ? d->batch / dp->batch : 1;
+  const int group = d->q_heads / d->kv_heads;
+  const int64_t rows = (int64_t)group * q_rows, share = d->batch > 0 ? d->batch / dp->batch : 1;
   if (P > (1 << 24) || rows > (1 << 24) || rows * share > (1 << 28)) return false;
   pl->pre = plan_rows(P0, rows * share, dp->n_max);
   pl->own = plan_rows(P, rows, d->n_max);
+  pl->tiles = rows * share > 16 && group <= kTileRows && dp->n_max > 0;
+  size_t entries = pl->pre.entries;
+  if (pl->tiles) {
+    plan_tiles(P0, (int)share, q_rows, group, dp->n_max, pl);
+    const size_t tiles = (size_t)P0 * pl->row_tiles * pl->chunks * kTileRows;
+    if (tiles > entries) entries = tiles;                  // (rows that the maps cannot hold take the other form)
+  }
   pl->pre_at = 256;
-  pl->own_at = pl->pre_at + parts_bytes(pl->pre.entries);
+  pl->own_at = pl->pre_at + parts_bytes(entries);
   pl->bytes = pl->own_at + parts_bytes(pl->own.entries);
   return true;
 }
@@ -236,7 +269,7 @@ curdkv_status curdkv_attention_prefix(const void* Q, int32_t q_rows, int64_t q_s
   const int64_t P = (int64_t)desc->batch * desc->kv_heads, P0 = (int64_t)desc_prefix->batch * desc->kv_heads;
   if (P == 0) return CURDKV_OK;
   const int64_t pre_ctas = P0 * pl.pre.blocks * pl.pre.chunks, own_ctas = P * pl.own.blocks * pl.own.chunks;
-  if (pre_ctas > 0x7fffffffLL || own_ctas > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+  if (own_ctas > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   const int group = desc->q_heads / desc->kv_heads, share = desc->batch / desc_prefix->batch;
@@ -255,7 +288,60 @@ curdkv_status curdkv_attention_prefix(const void* Q, int32_t q_rows, int64_t q_s
     a.part_o = const_cast<float*>(parts.o);
     return r.nt == 1 ? launch_parts<1, false>(a, ctas, stream) : launch_parts<2, false>(a, ctas, stream);
   };
-  if (desc_prefix->n_max > 0) {
+  const bool tiles = pl.tiles &&
+      map_strides_ok(desc_prefix->batch, desc->kv_heads, desc_prefix->k_stride_b, desc_prefix->k_stride_h, desc_prefix->k_stride_n) &&
+      map_strides_ok(desc_prefix->batch, desc->kv_heads, desc_prefix->v_stride_b, desc_prefix->v_stride_h, desc_prefix->v_stride_n) &&
+      map_strides_ok(desc->batch, desc->q_heads, q_stride_b, q_stride_h, q_stride_n) &&
+      map_strides_ok(1, desc->kv_heads, 0, (int64_t)group * q_stride_h, 128) && P0 * pl.row_tiles * pl.chunks <= 0x7fffffffLL;
+  if (tiles) {
+    j.prefix = rows::Parts{};
+    const size_t entries = (size_t)P0 * pl.row_tiles * pl.chunks * kTileRows;
+    j.prefix.ml = reinterpret_cast<const float2*>(ws + pl.pre_at);
+    j.prefix.o = reinterpret_cast<const float*>(ws + pl.pre_at + round256(entries * sizeof(float2)));
+    j.prefix.lens = desc_prefix->seqlens;
+    j.prefix.n_max = desc_prefix->n_max;
+    j.prefix.chunk = pl.chunk;
+    j.prefix.chunks = pl.chunks;
+    j.prefix.tile_rows = kTileRows;
+    j.prefix.tiles = pl.row_tiles;
+    j.prefix.seqs = pl.seqs;
+    j.prefix.tokens = pl.tokens;
+    j.prefix.token_tiles = pl.token_tiles;
+    umma::PrefixArgs x = {};
+    x.lens = desc_prefix->seqlens;
+    x.n_max = desc_prefix->n_max;
+    x.heads = desc->kv_heads;
+    x.group = group;
+    x.t = q_rows;
+    x.share = share;
+    x.seqs = pl.seqs;
+    x.tokens = pl.tokens;
+    x.token_tiles = pl.token_tiles;
+    x.tiles = pl.row_tiles;
+    x.chunk = pl.chunk;
+    x.chunks = pl.chunks;
+    // (products are masked before they are scaled, and -inf times 0 would be NaN)
+    x.scale_log2 = a.scale_log2 > FLT_MIN ? a.scale_log2 : FLT_MIN;
+    x.part_ml = const_cast<float2*>(j.prefix.ml);
+    x.part_o = const_cast<float*>(j.prefix.o);
+    x.status = a.status;
+    CUtensorMap mq, mk, mv;
+    const uint64_t sizes[5] = {128, (uint64_t)group, (uint64_t)q_rows, (uint64_t)desc->kv_heads, (uint64_t)desc->batch};
+    const int64_t strides[5] = {1, q_stride_h, q_stride_n, (int64_t)group * q_stride_h, q_stride_b};
+    const uint32_t box[5] = {64, (uint32_t)group, (uint32_t)pl.tokens, 1, (uint32_t)pl.seqs};
+    if (!bf16_map(&mq, Q, 5, sizes, strides, box) ||
+        !rows_map(&mk, K_prefix, desc_prefix->batch, desc->kv_heads, desc_prefix->n_max, desc_prefix->k_stride_b,
+                  desc_prefix->k_stride_h, desc_prefix->k_stride_n) ||
+        !rows_map(&mv, V_prefix, desc_prefix->batch, desc->kv_heads, desc_prefix->n_max, desc_prefix->v_stride_b,
+                  desc_prefix->v_stride_h, desc_prefix->v_stride_n))
+      return CURDKV_ERR_CUDA;
+    static std::atomic<uint64_t> done{0};
+    if (!allow_smem(umma::prefix_attention_kernel, umma::kPrefixDynamic, done)) return CURDKV_ERR_CUDA;
+    umma::prefix_attention_kernel<<<(unsigned)(P0 * pl.row_tiles * pl.chunks), umma::kPrefixThreads, umma::kPrefixDynamic, stream>>>(
+        mq, mk, mv, x);
+    if (!launched()) return CURDKV_ERR_CUDA;
+  } else if (desc_prefix->n_max > 0) {
+    if (pre_ctas > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
     a.q = rows::Queries{static_cast<const __nv_bfloat16*>(Q), q_stride_b, q_stride_h, q_stride_n, desc->kv_heads, group, q_rows,
                         share, share * q_rows * group};
     a.K = KvView{static_cast<const __nv_bfloat16*>(K_prefix), desc_prefix->k_stride_b, desc_prefix->k_stride_h, desc_prefix->k_stride_n};
