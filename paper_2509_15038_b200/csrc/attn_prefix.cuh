@@ -28,16 +28,19 @@ struct PrefixArgs {
   unsigned long long wait_ns = kWaitLimitNs;
 };
 
-constexpr int kPrefixThreads = 320;                        // TMA, MMA, 2 x 4 softmax warps
+constexpr int kPrefixThreads = 320;                        // TMA, products, two sets of four softmax warps
 constexpr int kPrefixRing = 5;
-constexpr int kPrefixQ = 0;
-constexpr int kPrefixSlot0 = kSlotBytes;
+constexpr int kPrefixQ = 0;                                // one or two tiles
+constexpr int kPrefixSlot0 = 2 * kSlotBytes;
 constexpr int kPrefixBar = kPrefixSlot0 + kPrefixRing * kSlotBytes;
 constexpr int kPrefixDynamic = kPrefixBar + 256 + 1024;
 constexpr int kPrefixTmemCols = 512;                       // S of group g at 128 g (its weights over it), O of group g at 256 + 128 g
 constexpr float kPrefixSlack = 8.f;
 
-// grid = sets * heads * chunks * tiles, tiles innermost: CTAs that read the same keys run side by side.
+// PAIR: two tiles of query rows, a group of softmax warps each, which share every tile of keys and values; else one tile, whose
+// groups take every other tile of keys each and meet at the end.
+// grid = sets * heads * chunks * (tiles or pairs of tiles), these innermost: CTAs that read the same keys run side by side.
+template <bool PAIR>
 __global__ void __launch_bounds__(kPrefixThreads, 1)
 prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                         const __grid_constant__ CUtensorMap map_v, const PrefixArgs a) {
@@ -45,39 +48,39 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
   unsigned char* base_ptr = smem_dyn + (base - smem_u32(smem_dyn));
   const uint32_t bar0 = base + kPrefixBar;
-  auto full_bar = [&](int s) { return bar0 + 8u * s; };
-  auto empty_bar = [&](int s) { return bar0 + 8u * (kPrefixRing + s); };
-  auto s_full_bar = [&](int s) { return bar0 + 8u * (2 * kPrefixRing + s); };
-  auto p_ready_bar = [&](int s) { return bar0 + 8u * (2 * kPrefixRing + 2 + s); };
-  const uint32_t q_full_bar = bar0 + 8u * (2 * kPrefixRing + 4);
-  const uint32_t o_full_bar = bar0 + 8u * (2 * kPrefixRing + 5);
-  const uint32_t drain_bar = bar0 + 8u * (2 * kPrefixRing + 6);
-  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(base_ptr + kPrefixBar + 8 * (2 * kPrefixRing + 7));
+  auto full_bar = [&](uint32_t s) { return bar0 + 8u * s; };
+  auto empty_bar = [&](uint32_t s) { return bar0 + 8u * (kPrefixRing + s); };
+  const uint32_t gbar = bar0 + 16u * kPrefixRing;
+  auto s_full_bar = [&](uint32_t g) { return gbar + 8u * g; };
+  auto p_ready_bar = [&](uint32_t g, uint32_t half) { return gbar + 16u + 16u * g + 8u * half; };
+  auto o_full_bar = [&](uint32_t g) { return gbar + 48u + 8u * g; };
+  const uint32_t q_full_bar = gbar + 64u, drain_bar = gbar + 72u;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(base_ptr + kPrefixBar + 16 * kPrefixRing + 80);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
-  __shared__ float2 xchg[2][kTileRows];                    // each group's reference and sum
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  const int tile = blockIdx.x % a.tiles, chunk = blockIdx.x / a.tiles % a.chunks, p = blockIdx.x / a.tiles / a.chunks;
-  const int set = p / a.heads, h = p % a.heads;
+  const int sets_of_tiles = PAIR ? (a.tiles + 1) / 2 : a.tiles;
+  const int tile0 = blockIdx.x % sets_of_tiles * (PAIR ? 2 : 1), chunk = blockIdx.x / sets_of_tiles % a.chunks;
+  const int p = blockIdx.x / sets_of_tiles / a.chunks, set = p / a.heads, h = p % a.heads;
+  const int count = PAIR ? min(2, a.tiles - tile0) : 1;    // tiles of query rows
   int n = a.n_max;
   if (a.lens != nullptr) {
     n = seq_len_of(a.lens, set, a.n_max);
-    if (n != a.lens[set] && tid == 0 && chunk == 0 && tile == 0) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
+    if (n != a.lens[set] && tid == 0 && chunk == 0 && tile0 == 0) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
   }
   const int k0 = chunk * a.chunk, keys = min(n - k0, a.chunk);
   if (keys <= 0) return;
   const int T = (keys + kTileRows - 1) / kTileRows;
-  const int seq0 = tile / a.token_tiles * a.seqs, tok0 = tile % a.token_tiles * a.tokens;
 
   if (tid == 0) {
     for (int s = 0; s < kPrefixRing; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int s = 0; s < 2; ++s) {
-      mbar_init(s_full_bar(s), 1);
-      mbar_init(p_ready_bar(s), 128);
+    for (int g = 0; g < 2; ++g) {
+      mbar_init(s_full_bar(g), 1);
+      mbar_init(o_full_bar(g), 1);
+      for (int half = 0; half < 2; ++half) mbar_init(p_ready_bar(g, half), 128);
     }
     mbar_init(q_full_bar, 1);
-    mbar_init(o_full_bar, 1);
     mbar_init(drain_bar, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -93,31 +96,36 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   tc_fence_after();
   constexpr uint32_t tmem_base = 0u;                       // all 512 columns are this CTA's: they begin at 0
 
-  // Tiles go through the ring in the order the products consume them: K_0, K_1, then for every t: V_t, K_{t+2} (if any).
+  // Ring order, that of the products: a pair K_0, V_0, K_1, V_1, ...; else K_0, K_1, V_0, K_2, V_1, ...  Every entry is waited
+  // for in order by one warp (a barrier tells only two rounds apart).
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
     if (lane == 0) {
       uint64_t pol;
       asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(pol));
-      mbar_arrive_expect_tx(q_full_bar, (uint32_t)(a.seqs * a.tokens * a.group) * 256u);
-      tma_load_5d(base + kPrefixQ, &map_q, q_full_bar, 0, 0, tok0, h, set * a.share + seq0);
-      tma_load_5d(base + kPrefixQ + kHalfBytes, &map_q, q_full_bar, 64, 0, tok0, h, set * a.share + seq0);
+      mbar_arrive_expect_tx(q_full_bar, (uint32_t)(count * a.seqs * a.tokens * a.group) * 256u);
+      for (int g = 0; g < count; ++g) {
+        const int tok0 = (tile0 + g) % a.token_tiles * a.tokens, seq = set * a.share + (tile0 + g) / a.token_tiles * a.seqs;
+        const uint32_t dst = base + kPrefixQ + g * kSlotBytes;
+        tma_load_5d(dst, &map_q, q_full_bar, 0, 0, tok0, h, seq);
+        tma_load_5d(dst + kHalfBytes, &map_q, q_full_bar, 64, 0, tok0, h, seq);
+      }
       uint32_t it = 0;
       bool ok = true;
       auto load = [&](const CUtensorMap* map, int t) {
-        const int slot = it % kPrefixRing;
-        if (!(ok = mbar_wait(empty_bar(slot), ((it / kPrefixRing) & 1u) ^ 1u, abort_flag, a.status, a.wait_ns))) return;
+        const uint32_t slot = it % kPrefixRing;
+        if (!(ok = ok && mbar_wait(empty_bar(slot), ((it / kPrefixRing) & 1u) ^ 1u, abort_flag, a.status, a.wait_ns))) return;
         mbar_arrive_expect_tx(full_bar(slot), kSlotBytes);
         const uint32_t dst = base + kPrefixSlot0 + slot * kSlotBytes;
         tma_load_4d(dst, map, full_bar(slot), 0, k0 + t * kTileRows, h, set, pol);
         tma_load_4d(dst + kHalfBytes, map, full_bar(slot), 64, k0 + t * kTileRows, h, set, pol);
         ++it;
       };
-      load(&map_k, 0);
-      if (ok && T > 1) load(&map_k, 1);
+      constexpr int kAhead = PAIR ? 1 : 2;
+      for (int t = 0; t < kAhead && t < T; ++t) load(&map_k, t);
       for (int t = 0; ok && t < T; ++t) {
         load(&map_v, t);
-        if (ok && t + 2 < T) load(&map_k, t + 2);
+        if (t + kAhead < T) load(&map_k, t + kAhead);
       }
       if (!ok) {                                           // let what was issued land before the CTA ends
         auto land = [&](uint32_t bar, uint32_t parity) {
@@ -133,63 +141,104 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     constexpr uint32_t idesc_s = instr_desc_bf16(128), idesc_pv = instr_desc_pv();
     const uint64_t q_desc = smem_desc_sw128(base + kPrefixQ);
     const uint64_t k_desc0 = smem_desc_sw128(base + kPrefixSlot0), v_desc0 = smem_desc_mn_sw128(base + kPrefixSlot0);
-    uint32_t it = 0;
+    uint32_t it = 0;                                       // entries of the ring that have landed
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) {
       ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns) && ok);
       tc_fence_after();
     };
-    wait(q_full_bar, 0);
-    auto issue_s = [&](uint32_t buf) {                     // S[buf] = Q K^T for the next K tile of the ring
+    auto next_slot = [&]() {
       const uint32_t slot = it % kPrefixRing;
       wait(full_bar(slot), (it / kPrefixRing) & 1u);
       ++it;
-      if (!ok) return;
-      const uint64_t kd = k_desc0 + slot * (kSlotBytes >> 4);
-      if (elect_one()) {
+      return slot;
+    };
+    auto release = [&](uint32_t slot) {
+      if (ok && elect_one()) tc_commit(empty_bar(slot));
+      __syncwarp();
+    };
+    auto issue_s = [&](uint32_t g, uint32_t slot) {        // S_g = Q K^T
+      if (ok && elect_one()) {
+        const uint64_t qd = q_desc + (PAIR ? g * (kSlotBytes >> 4) : 0u), kd = k_desc0 + slot * (kSlotBytes >> 4);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const uint32_t off = (uint32_t)(k >> 2) * (kHalfBytes >> 4) + (uint32_t)(k & 3) * 2u;
-          tc_mma_bf16(tmem_base + buf * 128u, q_desc + off, kd + off, idesc_s, k > 0);
+          tc_mma_bf16(tmem_base + 128u * g, qd + off, kd + off, idesc_s, k > 0);
         }
-        tc_commit(empty_bar(slot));
-        tc_commit(s_full_bar(buf));
+        tc_commit(s_full_bar(g));
       }
       __syncwarp();
     };
-    // A group's S is taken over by its weights; S_{t+2} goes into it right behind P_t V_t (the tensor pipe runs one thread's
-    // products in order, so the product has read P by then).
-    if (ok) issue_s(0);
-    if (ok && T > 1) issue_s(1);
-    for (int t = 0; ok && t < T; ++t) {
-      const uint32_t slot = it % kPrefixRing, buf = (uint32_t)t & 1u;
-      wait(full_bar(slot), (it / kPrefixRing) & 1u);
-      ++it;
-      if (!ok) break;
-      const int rows = min(kTileRows, keys - t * kTileRows), groups = (rows + 15) >> 4;
-      if (rows < groups * 16) {                            // value rows that do not exist: a weight of 0 would not stop a NaN
-        for (int x = lane; x < (groups * 16 - rows) * 16; x += 32)
-          *reinterpret_cast<uint4*>(base_ptr + kPrefixSlot0 + slot * kSlotBytes + (x >> 3 & 1) * kHalfBytes + (rows + (x >> 4)) * 128 +
-                                    (x & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    // O_g += P_g V: 16 keys per product, 8 columns of P, 2048 bytes (128 units) of the V tile; the weights come in halves
+    auto issue_pv = [&](uint32_t g, uint32_t slot, int groups, uint32_t parity, bool first) {
+      const uint64_t vd = v_desc0 + slot * (kSlotBytes >> 4);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        if (ok) wait(p_ready_bar(g, half), parity);
+        if (ok && elect_one()) {
+#pragma unroll
+          for (int k = 4 * half; k < 4 * half + 4; ++k)
+            if (k < groups)
+              tc_mma_bf16_ts(tmem_base + 256u + 128u * g, tmem_base + 128u * g + 8u * k, vd + 128u * k, idesc_pv, (!first || k > 0) ? 1u : 0u);
+        }
         __syncwarp();
       }
-      wait(p_ready_bar(buf), (uint32_t)(t >> 1) & 1u);
-      if (!ok) break;
-      const uint64_t vd = v_desc0 + slot * (kSlotBytes >> 4);
-      const uint32_t o_tmem = tmem_base + 256u + buf * 128u, p_tmem = tmem_base + buf * 128u;
-      if (elect_one()) {
-        // 16 keys per product: 8 columns of P, 2048 bytes (128 units) of the V tile
-#pragma unroll
-        for (int g = 0; g < 8; ++g)
-          if (g < groups) tc_mma_bf16_ts(o_tmem, p_tmem + 8u * g, vd + 128u * g, idesc_pv, (t > 1 || g > 0) ? 1u : 0u);
-        tc_commit(empty_bar(slot));
-      }
+    };
+    auto finish = [&](uint32_t g) {
+      if (ok && elect_one()) tc_commit(o_full_bar(g));
       __syncwarp();
-      if (t + 2 < T) issue_s(buf);
+    };
+    auto clear_behind = [&](uint32_t slot, int rows) {     // value rows that do not exist: a weight of 0 would not stop a NaN
+      const int upto = (rows + 15) / 16 * 16;
+      if (rows >= upto) return;
+      for (int x = lane; x < (upto - rows) * 16; x += 32)
+        *reinterpret_cast<uint4*>(base_ptr + kPrefixSlot0 + slot * kSlotBytes + (x >> 3 & 1) * kHalfBytes + (rows + (x >> 4)) * 128 +
+                                  (x & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+    };
+    wait(q_full_bar, 0);
+    // A group's S is taken over by its weights; its next S goes into it right behind P V (the tensor pipe runs one thread's
+    // products in order, so the product has read P by then).
+    if (PAIR) {
+      uint32_t slot = ok ? next_slot() : 0u;
+      for (int g = 0; g < count; ++g) issue_s((uint32_t)g, slot);
+      release(slot);
+      for (int t = 0; ok && t < T; ++t) {
+        const int rows = min(kTileRows, keys - t * kTileRows);
+        const uint32_t v_slot = next_slot();
+        if (!ok) break;
+        clear_behind(v_slot, rows);
+        const bool more = t + 1 < T;
+        const uint32_t k_slot = more ? next_slot() : 0u;
+        for (int g = 0; ok && g < count; ++g) {
+          issue_pv((uint32_t)g, v_slot, (rows + 15) >> 4, (uint32_t)t & 1u, t == 0);
+          if (more) issue_s((uint32_t)g, k_slot); else finish((uint32_t)g);
+        }
+        release(v_slot);
+        if (more) release(k_slot);
+      }
+    } else {
+      for (uint32_t g = 0; g < 2u && (int)g < T && ok; ++g) {
+        const uint32_t slot = next_slot();
+        issue_s(g, slot);
+        release(slot);
+      }
+      for (int t = 0; ok && t < T; ++t) {
+        const uint32_t g = (uint32_t)t & 1u, v_slot = next_slot();
+        if (!ok) break;
+        const int rows = min(kTileRows, keys - t * kTileRows);
+        clear_behind(v_slot, rows);
+        issue_pv(g, v_slot, (rows + 15) >> 4, (uint32_t)(t >> 1) & 1u, t < 2);
+        release(v_slot);
+        if (ok && t + 2 < T) {
+          const uint32_t slot = next_slot();
+          issue_s(g, slot);
+          release(slot);
+        }
+      }
+      for (uint32_t g = 0; g < 2u; ++g) finish(g);
     }
-    if (ok && elect_one()) tc_commit(o_full_bar);
-    __syncwarp();
     if (!ok) {
       if (elect_one()) tc_commit(drain_bar);
       __syncwarp();
@@ -197,7 +246,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       while (!mbar_try_wait(drain_bar, 0) && global_ns() - t0 < a.wait_ns) {}
     }
   } else {
-    // ------------------------------------------------------------ softmax: thread r of the tile, every other tile of keys
+    // ------------------------------------------------------------ softmax: thread r of a tile of query rows
     const int group = (warp - 2) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
     const uint32_t lane_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
     const uint32_t s_addr = lane_addr + group * 128u, o_addr = lane_addr + 256u + group * 128u;
@@ -205,8 +254,9 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     const uint64_t sc2 = pack2(sc, sc);
     float top = -INFINITY, sum = 0.f;
     bool has_o = false, ok = true;
-    for (int t = group; ok && t < T; t += 2) {
-      ok = mbar_wait(s_full_bar(group), (uint32_t)(t >> 1) & 1u, abort_flag, a.status, a.wait_ns);
+    const int step = PAIR ? 1 : 2, end = PAIR && group >= count ? 0 : T;
+    for (int t = PAIR ? 0 : group; ok && t < end; t += step) {
+      ok = mbar_wait(s_full_bar(group), (uint32_t)(PAIR ? t : t >> 1) & 1u, abort_flag, a.status, a.wait_ns);
       if (!(ok = __all_sync(0xffffffffu, ok))) break;
       tc_fence_after();
       const int valid = keys - t * kTileRows;              // keys of this tile that exist
@@ -262,44 +312,59 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
           w[e] = *reinterpret_cast<const uint32_t*>(&b);
         }
         tmem_st16(s_addr + 16 * c, w);
+        if (c & 1) {                                       // 64 keys' weights are in place
+          tmem_st_wait();
+          tc_fence_before();
+          mbar_arrive(p_ready_bar(group, c >> 1));
+        }
       }
       float p0, p1;
       unpack2(add2(add2(part[0], part[1]), add2(part[2], part[3])), p0, p1);
       sum += p0 + p1;
-      tmem_st_wait();
-      tc_fence_before();
-      mbar_arrive(p_ready_bar(group));
       has_o = true;
     }
-    // ------------------------------------------------------------ the groups' halves meet; each writes 64 channels
-    xchg[group][r] = make_float2(has_o ? top : -INFINITY, has_o ? sum : 0.f);
-    asm volatile("bar.sync 1, 256;" ::: "memory");         // reached by all eight warps, aborted or not
-    if (ok) ok = mbar_wait(o_full_bar, 0, abort_flag, a.status, a.wait_ns);
+    // ------------------------------------------------------------ output
+    // Rows go through shared memory, so that a warp writes 128 contiguous bytes of four rows at a time; a row's eight places
+    // are permuted against bank conflicts.  The space: a row tile's own Q (for a single tile the one behind it), which no
+    // product reads any more once all of the group are done.
+    if (end > 0) ok = ok && mbar_wait(o_full_bar(group), 0, abort_flag, a.status, a.wait_ns);
+    if (!PAIR) ok = ok && mbar_wait(o_full_bar(1 - group), 0, abort_flag, a.status, a.wait_ns);
     ok = __all_sync(0xffffffffu, ok);
-    if (ok) {
+    unsigned char* stage = base_ptr + kPrefixQ + (PAIR ? group * kSlotBytes : kSlotBytes) + (PAIR ? warp - 2 - 4 * group : warp - 2) * 4096;
+    float f0 = 1.f, f1 = 0.f, m = top, l = sum;
+    if (!PAIR) {                                           // the groups' halves meet (group 0 always has a tile of keys)
+      float2* xchg = reinterpret_cast<float2*>(base_ptr + kPrefixQ);
+      xchg[group * kTileRows + r] = make_float2(has_o ? top : -INFINITY, has_o ? sum : 0.f);
+      asm volatile("bar.sync 1, 256;" ::: "memory");       // reached by all eight warps, aborted or not
+      const float2 e0 = xchg[r], e1 = xchg[kTileRows + r];
+      m = fmaxf(e0.x, e1.x);
+      f0 = m == -INFINITY ? 1.f : fast_exp2(e0.x - m);
+      f1 = T > 1 ? (m == -INFINITY ? 1.f : fast_exp2(e1.x - m)) : 0.f;
+      l = f0 * e0.y + f1 * e1.y;
+    }
+    if (ok && end > 0) {
       tc_fence_after();
-      const float2 e0 = xchg[0][r], e1 = xchg[1][r];       // (group 0 always has a tile)
-      const float m = fmaxf(e0.x, e1.x);
-      const float f0 = m == -INFINITY ? 1.f : fast_exp2(e0.x - m), f1 = T > 1 ? (m == -INFINITY ? 1.f : fast_exp2(e1.x - m)) : 0.f;
-      const size_t part = (((size_t)p * a.tiles + tile) * a.chunks + chunk) * kTileRows;
+      const size_t part = (((size_t)p * a.tiles + tile0 + (PAIR ? group : 0)) * a.chunks + chunk) * kTileRows;
       const int used = a.seqs * a.tokens * a.group;
-      if (group == 0 && r < used) a.part_ml[part + r] = make_float2(m, f0 * e0.y + f1 * e1.y);
-      // Rows go through shared memory (all tiles of the ring are done with), so that a warp writes 128 contiguous bytes of
-      // four rows at a time; a row's eight places are permuted against bank conflicts.
-      unsigned char* stage = base_ptr + kPrefixSlot0 + (warp - 2) * 4096;
+      if ((PAIR || group == 0) && r < used) a.part_ml[part + r] = make_float2(m, l);
+      const bool both = !PAIR && T > 1;
+      const int c_from = PAIR ? 0 : 64 * group, c_to = PAIR ? 128 : c_from + 64;
 #pragma unroll 1
-      for (int c0 = 64 * group; c0 < 64 * group + 64; c0 += 32) {
+      for (int c0 = c_from; c0 < c_to; c0 += 32) {
         float v[32], w[32];
-        tmem_ld32(lane_addr + 256u + c0, v);
-        if (T > 1) tmem_ld32(lane_addr + 384u + c0, w);
+        tmem_ld32((PAIR ? o_addr : lane_addr + 256u) + c0, v);
+        if (both) tmem_ld32(lane_addr + 384u + c0, w);
         tmem_ld_wait();
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
-          float4 o;
-          o.x = v[4 * c] * f0 + (T > 1 ? w[4 * c] * f1 : 0.f);
-          o.y = v[4 * c + 1] * f0 + (T > 1 ? w[4 * c + 1] * f1 : 0.f);
-          o.z = v[4 * c + 2] * f0 + (T > 1 ? w[4 * c + 2] * f1 : 0.f);
-          o.w = v[4 * c + 3] * f0 + (T > 1 ? w[4 * c + 3] * f1 : 0.f);
+          float4 o = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+          if (!PAIR) { o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0; }
+          if (both) {
+            o.x = fmaf(w[4 * c], f1, o.x);
+            o.y = fmaf(w[4 * c + 1], f1, o.y);
+            o.z = fmaf(w[4 * c + 2], f1, o.z);
+            o.w = fmaf(w[4 * c + 3], f1, o.w);
+          }
           *reinterpret_cast<float4*>(stage + lane * 128 + ((c ^ (lane & 7)) * 16)) = o;
         }
         __syncwarp();

@@ -128,7 +128,7 @@ void plan_tiles(int64_t problems, int share, int t, int group, int64_t keys, Pre
   pl->seqs = most / pl->tokens < share ? most / pl->tokens : share;
   pl->token_tiles = (t + pl->tokens - 1) / pl->tokens;
   pl->row_tiles = (share + pl->seqs - 1) / pl->seqs * pl->token_tiles;
-  const int64_t key_tiles = (keys + kTileRows - 1) / kTileRows, items = problems * pl->row_tiles, places = sms();
+  const int64_t key_tiles = (keys + kTileRows - 1) / kTileRows, items = problems * ((pl->row_tiles + 1) / 2), places = sms();
   int64_t best = -1;
   for (int64_t c = 1; c <= key_tiles && c <= 512; ++c) {
     const int64_t each = (key_tiles + c - 1) / c, cost = (items * c + places - 1) / places * (each + 8);
@@ -335,10 +335,15 @@ curdkv_status curdkv_attention_prefix(const void* Q, int32_t q_rows, int64_t q_s
         !rows_map(&mv, V_prefix, desc_prefix->batch, desc->kv_heads, desc_prefix->n_max, desc_prefix->v_stride_b,
                   desc_prefix->v_stride_h, desc_prefix->v_stride_n))
       return CURDKV_ERR_CUDA;
-    static std::atomic<uint64_t> done{0};
-    if (!allow_smem(umma::prefix_attention_kernel, umma::kPrefixDynamic, done)) return CURDKV_ERR_CUDA;
-    umma::prefix_attention_kernel<<<(unsigned)(P0 * pl.row_tiles * pl.chunks), umma::kPrefixThreads, umma::kPrefixDynamic, stream>>>(
-        mq, mk, mv, x);
+    static std::atomic<uint64_t> pair_done{0}, one_done{0};
+    const unsigned grid = (unsigned)(P0 * ((pl.row_tiles + 1) / 2) * pl.chunks);
+    if (pl.row_tiles > 1) {
+      if (!allow_smem(umma::prefix_attention_kernel<true>, umma::kPrefixDynamic, pair_done)) return CURDKV_ERR_CUDA;
+      umma::prefix_attention_kernel<true><<<grid, umma::kPrefixThreads, umma::kPrefixDynamic, stream>>>(mq, mk, mv, x);
+    } else {
+      if (!allow_smem(umma::prefix_attention_kernel<false>, umma::kPrefixDynamic, one_done)) return CURDKV_ERR_CUDA;
+      umma::prefix_attention_kernel<false><<<grid, umma::kPrefixThreads, umma::kPrefixDynamic, stream>>>(mq, mk, mv, x);
+    }
     if (!launched()) return CURDKV_ERR_CUDA;
   } else if (desc_prefix->n_max > 0) {
     if (pre_ctas > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
