@@ -49,7 +49,7 @@ struct Args {
   float2* part_ml;                   // [items][chunks][8 NT]: m, l
   float* part_o;                     // [items][chunks][8 NT][128]
   float* logits;                     // [sets * heads][blocks][n_max][pitch], or nullptr
-  int pitch;                         // even
+  int pitch;                         // 2 or a multiple of 4, at least the rows of a block
   uint32_t* status;
 };
 
@@ -362,85 +362,165 @@ struct JoinArgs {
 constexpr int kJoinWarps = 4;
 constexpr int kMostRows = 1024;                            // query rows of a problem whose weights are kept
 
-// A warp per query row joins its parts, in their order; with LOGITS the problem's CTAs then add the weights of their share
-// of the keys, summed over the query rows in order.  grid = sequences * heads * slices.
+// The CTAs of a problem take its query rows in turn.  A row's parts are dealt to the four warps, which ask for four each
+// before they know what these count (that, and not their bytes, is what takes time here), and their sums are added in order.
+// With LOGITS the problem's CTAs then add the weights of their share of the keys, summed over the query rows in order.
+// grid = sequences * heads * slices.
 template <bool PREFIX, bool LOGITS>
 __global__ void __launch_bounds__(kJoinWarps * 32) join_parts_kernel(const JoinArgs a) {
-  __shared__ float2 s_norm[LOGITS ? kMostRows : 1];        // reference, 1 / sum
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  __shared__ float2 s_norm[LOGITS ? kMostRows + 16 : 1];   // reference, 1 / sum
+  __shared__ float4 s_part[2][kJoinWarps][32];
   const int p = blockIdx.x / a.slices, slice = blockIdx.x % a.slices, b = p / a.heads, h = p % a.heads;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rows = a.t * a.group, live = a.q_lens != nullptr ? min(max(a.q_lens[b], 0), a.t) : a.t;
-  const int own = a.own.used(b), set = PREFIX ? b / a.share : 0, all_parts = own + (PREFIX ? a.prefix.used(set) : 0);
-  for (int r = LOGITS ? warp : warp + slice * kJoinWarps; r < rows; r += LOGITS ? kJoinWarps : kJoinWarps * a.slices) {
+  const int rows = a.t * a.group, set = PREFIX ? b / a.share : 0;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int live = a.q_lens != nullptr ? min(max(a.q_lens[b], 0), a.t) : a.t;
+  const int own = a.own.used(b), all_parts = own + (PREFIX ? a.prefix.used(set) : 0);
+  struct Row {
+    size_t own_at, pre_at;
+  };
+  auto row_of = [&](int r) {
     const int i = r / a.group, g = r % a.group;
-    if (i >= live) {
-      if (LOGITS && lane == 0) s_norm[r] = make_float2(0.f, 0.f);
-      continue;
+    return Row{a.own.entry(p, 0, i, g, a.t, a.group), PREFIX ? a.prefix.entry(set * a.heads + h, b % a.share, i, g, a.t, a.group) : 0};
+  };
+  auto ml = [&](const Row& x, int c) {
+    return PREFIX && c >= own ? a.prefix.ml[x.pre_at + (size_t)(c - own) * a.prefix.tile_rows] : a.own.ml[x.own_at + (size_t)c * a.own.tile_rows];
+  };
+  auto values = [&](const Row& x, int c) {
+    const float* o = PREFIX && c >= own ? a.prefix.o + (x.pre_at + (size_t)(c - own) * a.prefix.tile_rows) * 128
+                                        : a.own.o + (x.own_at + (size_t)c * a.own.tile_rows) * 128;
+    return *reinterpret_cast<const float4*>(o + lane * 4);
+  };
+  auto most = [](float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+  };
+  auto total = [](float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  };
+  auto share = [](float m, float top) { return top == -INFINITY ? 1.f : token::exp2_approx(m - top); };   // (top -inf: zeros, or NaN)
+  // reference and sum of a row, a lane per part
+  auto stats = [&](const Row& x, float& top, float& sum) {
+    const float2 first = lane < all_parts ? ml(x, lane) : make_float2(-INFINITY, 0.f);
+    top = first.x;
+    for (int c = 32 + lane; c < all_parts; c += 32) top = fmaxf(top, ml(x, c).x);
+    top = most(top);
+    sum = lane < all_parts ? share(first.x, top) * first.y : 0.f;
+    for (int c = 32 + lane; c < all_parts; c += 32) {
+      const float2 e = ml(x, c);
+      sum += share(e.x, top) * e.y;
     }
-    const size_t own_at = a.own.entry(p, 0, i, g, a.t, a.group);
-    const size_t pre_at = PREFIX ? a.prefix.entry(set * a.heads + h, b % a.share, i, g, a.t, a.group) : 0;
-    auto entry = [&](int c) {
-      return PREFIX && c >= own ? pre_at + (size_t)(c - own) * a.prefix.tile_rows : own_at + (size_t)c * a.own.tile_rows;
-    };
-    auto ml = [&](int c) { return (PREFIX && c >= own ? a.prefix.ml : a.own.ml)[entry(c)]; };
-    float top = -INFINITY;
-    for (int c = lane; c < all_parts; c += 32) top = fmaxf(top, ml(c).x);
+    sum = total(sum);
+  };
+  auto inverse = [](float sum) { return sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum); };              // a NaN sum stays one
+
+  int turn = 0;
+  for (int r = slice; r < rows; r += a.slices) {
+    const int i = r / a.group, g = r % a.group;
+    if (i >= live) continue;
+    const Row x = row_of(r);
+    float4 v[4];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    auto share = [&](float m) { return top == -INFINITY ? 1.f : token::exp2_approx(m - top); };    // (top -inf: zeros, or NaN)
-    const bool mine = !LOGITS || (r / kJoinWarps) % a.slices == slice;
-    float sum = 0.f;
+    for (int k = 0; k < 4; ++k)
+      if (warp + 4 * k < all_parts) v[k] = values(x, warp + 4 * k);
+    float top, sum;
+    stats(x, top, sum);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int c0 = 0; c0 < all_parts; c0 += 32) {
-      const float2 e = c0 + lane < all_parts ? ml(c0 + lane) : make_float2(-INFINITY, 0.f);
-      const float f = c0 + lane < all_parts ? share(e.x) : 0.f;
-      float l = f * e.y;
-      if (c0 + lane >= all_parts) l = 0.f;
+    for (int c0 = warp; c0 < all_parts; c0 += 16) {
+      float4 now[4];
 #pragma unroll
-      for (int d = 16; d > 0; d >>= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-      sum += l;
-      if (!mine) continue;
-      const int n = min(32, all_parts - c0);
-#pragma unroll 4
-      for (int k = 0; k < n; ++k) {
-        const int c = c0 + k;
-        const float4 x = *reinterpret_cast<const float4*>((PREFIX && c >= own ? a.prefix.o : a.own.o) + entry(c) * 128 + lane * 4);
-        const float fk = __shfl_sync(0xffffffffu, f, k);
-        o.x = fmaf(fk, x.x, o.x); o.y = fmaf(fk, x.y, o.y); o.z = fmaf(fk, x.z, o.z); o.w = fmaf(fk, x.w, o.w);
+      for (int k = 0; k < 4; ++k) {
+        now[k] = v[k];
+        if (c0 + 16 + 4 * k < all_parts) v[k] = values(x, c0 + 16 + 4 * k);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (c0 + 4 * k >= all_parts) continue;
+        const float f = share(ml(x, c0 + 4 * k).x, top);
+        o.x = fmaf(f, now[k].x, o.x); o.y = fmaf(f, now[k].y, o.y); o.z = fmaf(f, now[k].z, o.z); o.w = fmaf(f, now[k].w, o.w);
       }
     }
-    const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);        // a NaN sum stays one
-    if (mine) {
+    s_part[turn][warp][lane] = o;
+    __syncthreads();                                       // (the other buffer is free again behind the next one)
+    if (warp == 0) {
+#pragma unroll
+      for (int w = 1; w < kJoinWarps; ++w) {
+        const float4 y = s_part[turn][w][lane];
+        o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
+      }
+      const float inv = inverse(sum);
       const int hq = h * a.group + g;
       *reinterpret_cast<uint2*>(a.O + b * a.o_sb + hq * a.o_sh + i * a.o_sn + lane * 4) =
           make_uint2(token::pack_bf16(o.x * inv, o.y * inv), token::pack_bf16(o.z * inv, o.w * inv));
       if (lane == 0 && a.lse != nullptr)
         a.lse[((int64_t)b * a.heads * a.group + hq) * a.t + i] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     }
-    if (LOGITS && lane == 0) s_norm[r] = make_float2(top == -INFINITY ? 0.f : top, inv);
+    turn ^= 1;
   }
   if (!LOGITS) return;
+  const int blocks = (rows + a.block_rows - 1) / a.block_rows, padded = (blocks - 1) * a.block_rows + a.pitch;
+  for (int r = warp; r < padded; r += kJoinWarps) {
+    float top = 0.f, inv = 0.f;                            // (a row that does not exist weighs nothing)
+    if (r < rows && r / a.group < live) {
+      float sum;
+      stats(row_of(r), top, sum);
+      inv = inverse(sum);
+      if (top == -INFINITY) top = 0.f;
+    }
+    if (lane == 0) {
+      s_norm[r].x = top;
+      s_norm[r].y = inv;
+    }
+  }
   __syncthreads();
   const int held = seq_len_of(a.own.lens, b, a.n_max);
   const int j0 = (int)((int64_t)held * slice / a.slices), j1 = (int)((int64_t)held * (slice + 1) / a.slices);
-  const int blocks = (rows + a.block_rows - 1) / a.block_rows;
-  for (int j = j0 + threadIdx.x; j < j1; j += kJoinWarps * 32) {
-    float w = 0.f;
+  const float* logits = a.logits + (int64_t)p * blocks * a.n_max * a.pitch;
+  float* weights = a.weights + (int64_t)p * a.n_max;
+  constexpr int kAtOnce = 4;                               // keys of a thread in flight
+  for (int j = j0 + threadIdx.x; j < j1; j += kAtOnce * kJoinWarps * 32) {
+    float w[kAtOnce], was[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int jk = j + k * kJoinWarps * 32;
+      w[k] = 0.f;
+      if (jk < j1) was[k] = weights[jk];
+    }
     for (int blk = 0; blk < blocks; ++blk) {
-      const float* x = a.logits + (((int64_t)p * blocks + blk) * a.n_max + j) * a.pitch;
-      const int n = min(a.block_rows, rows - blk * a.block_rows);
-      for (int r = 0; r < n; r += 2) {
-        const float2 v = *reinterpret_cast<const float2*>(x + r);
-        const float2 s0 = s_norm[blk * a.block_rows + r];
-        w = fmaf(token::exp2_approx(v.x - s0.x), s0.y, w);
-        if (r + 1 < n) {
-          const float2 s1 = s_norm[blk * a.block_rows + r + 1];
-          w = fmaf(token::exp2_approx(v.y - s1.x), s1.y, w);
+      const float* x = logits + ((int64_t)blk * a.n_max + j) * a.pitch;
+      const float2* norm = s_norm + blk * a.block_rows;
+      if (a.pitch == 2) {
+        float2 v[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+          if (j + k * kJoinWarps * 32 < j1) v[k] = *reinterpret_cast<const float2*>(x + k * kJoinWarps * 64);
+        const float2 n0 = norm[0], n1 = norm[1];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+          w[k] = fmaf(token::exp2_approx(v[k].y - n1.x), n1.y, fmaf(token::exp2_approx(v[k].x - n0.x), n0.y, w[k]));
+        continue;
+      }
+      for (int r = 0; r < a.pitch; r += 4) {
+        float4 v[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+          if (j + k * kJoinWarps * 32 < j1) v[k] = *reinterpret_cast<const float4*>(x + (int64_t)k * kJoinWarps * 32 * a.pitch + r);
+        const float2 n0 = norm[r], n1 = norm[r + 1], n2 = norm[r + 2], n3 = norm[r + 3];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          w[k] = fmaf(token::exp2_approx(v[k].x - n0.x), n0.y, w[k]);
+          w[k] = fmaf(token::exp2_approx(v[k].y - n1.x), n1.y, w[k]);
+          w[k] = fmaf(token::exp2_approx(v[k].z - n2.x), n2.y, w[k]);
+          w[k] = fmaf(token::exp2_approx(v[k].w - n3.x), n3.y, w[k]);
         }
       }
     }
-    a.weights[(int64_t)p * a.n_max + j] += w;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (j + k * kJoinWarps * 32 < j1) weights[j + k * kJoinWarps * 32] = was[k] + w[k];
   }
 }
 

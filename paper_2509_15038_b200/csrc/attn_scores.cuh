@@ -433,33 +433,53 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
 }
 
 // -L of every query row, from the parts of the rows pass or from log sums that the caller has; -inf where a row does not count.
-// Clears `clear` floats of `scores` beside it.  grid = batch * heads * row tiles, block = 128.
-__global__ void __launch_bounds__(128) score_logsum_kernel(const ScoreArgs a, const float* given, float* logsum, float* lse_out,
-                                                           float* scores, int64_t clear) {
+// Clears `clear` floats of `scores` beside it.  grid = batch * heads * row tiles; four threads a row take its parts in turn.
+constexpr int kLogsumThreads = 4 * kTileRows;
+__global__ void __launch_bounds__(kLogsumThreads) score_logsum_kernel(const ScoreArgs a, const float* given, float* logsum,
+                                                                      float* lse_out, float* scores, int64_t clear) {
+  __shared__ float2 s_part[3][kTileRows];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  for (int64_t x = (int64_t)blockIdx.x * 128 + threadIdx.x; x < clear; x += (int64_t)gridDim.x * 128) scores[x] = 0.f;
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int tile = blockIdx.x % a.row_tiles, p = blockIdx.x / a.row_tiles, b = p / a.heads, h = p % a.heads, r = threadIdx.x;
+  for (int64_t x = (int64_t)blockIdx.x * kLogsumThreads + threadIdx.x; x < clear; x += (int64_t)gridDim.x * kLogsumThreads) scores[x] = 0.f;
+  const int tile = blockIdx.x % a.row_tiles, p = blockIdx.x / a.row_tiles, b = p / a.heads, h = p % a.heads;
+  const int r = threadIdx.x % kTileRows, sub = threadIdx.x / kTileRows;
   const ScoreSeq s(a, b);
   const int tok = tile * a.tokens + r / a.group;
-  const bool live = r < a.tokens * a.group && tok < s.q;
+  const bool live = r < a.tokens * a.group && tok < s.q, sees = live && s.pos0 + tok >= 0;
+  float top = -INFINITY, sum = 0.f;
+  auto join = [&](float2 e) {
+    const float now = fmaxf(top, e.x);
+    sum = sum * (now == -INFINITY ? 1.f : fast_exp2(top - now)) + e.y * (now == -INFINITY ? 1.f : fast_exp2(e.x - now));
+    top = now;
+  };
+  if (given == nullptr) {
+    if (sees) {
+      // the pair of tiles this one belongs to walked these key tiles
+      const int end_tok = min((tile / 2 * 2 + min(2, a.row_tiles - tile / 2 * 2)) * a.tokens, s.q);
+      const int used = 2 * ((((s.pos0 + end_tok) + kTileRows - 1) / kTileRows + a.seg - 1) / a.seg);
+      const float2* stats = a.stats + ((int64_t)p * a.row_tiles + tile) * kTileRows + r;
+      const int64_t next = (int64_t)a.batch * a.heads * a.row_tiles * kTileRows;
+      for (int g = sub; g < used; g += 16) {
+        float2 e[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) e[k] = g + 4 * k < used ? stats[(g + 4 * k) * next] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) join(e[k]);
+      }
+    }
+    if (sub > 0) s_part[sub - 1][r] = make_float2(top, sum);
+    __syncthreads();
+  }
+  if (sub > 0) return;
   const int64_t at = ((int64_t)b * a.heads * a.group + h * a.group + r % a.group) * a.q_rows + tok;
   float L = INFINITY;
-  if (live && s.pos0 + tok >= 0) {
+  if (sees) {
     if (given != nullptr) {
       L = given[at] * a.log2_of_ln;
       if (L == -INFINITY) L = INFINITY;                    // (a row that saw nothing)
     } else {
-      // the pair of tiles this one belongs to walked these key tiles
-      const int end_tok = min((tile / 2 * 2 + min(2, a.row_tiles - tile / 2 * 2)) * a.tokens, s.q);
-      const int used = 2 * ((((s.pos0 + end_tok) + kTileRows - 1) / kTileRows + a.seg - 1) / a.seg);
-      float top = -INFINITY, sum = 0.f;
-      for (int g = 0; g < used; ++g)
-        top = fmaxf(top, a.stats[(((int64_t)g * a.batch * a.heads + p) * a.row_tiles + tile) * kTileRows + r].x);
-      for (int g = 0; g < used; ++g) {
-        const float2 e = a.stats[(((int64_t)g * a.batch * a.heads + p) * a.row_tiles + tile) * kTileRows + r];
-        sum += e.y * (top == -INFINITY ? 1.f : fast_exp2(e.x - top));
-      }
+#pragma unroll
+      for (int k = 0; k < 3; ++k) join(s_part[k][r]);
       L = sum == 0.f ? INFINITY : top + log2f(sum);
     }
   }

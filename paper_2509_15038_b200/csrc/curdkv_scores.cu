@@ -136,7 +136,7 @@ curdkv_status curdkv_attention_scores(const void* Q, int32_t q_rows, int64_t q_s
   a.units = (int)(P * ((pl.row_tiles + 1) / 2) * pl.row_segs);
   if (d.n_max == 0) {                                      // no scores; a query that sees nothing has a log sum all the same
     if (lse == nullptr || lse_given) return CURDKV_OK;
-    return launch(umma::score_logsum_kernel, P * pl.row_tiles, kTileRows, 0, false, stream, a, (const float*)nullptr, logsum, lse,
+    return launch(umma::score_logsum_kernel, P * pl.row_tiles, umma::kLogsumThreads, 0, false, stream, a, (const float*)nullptr, logsum, lse,
                   scores, (int64_t)0)
                ? CURDKV_OK : CURDKV_ERR_CUDA;
   }
@@ -152,7 +152,7 @@ curdkv_status curdkv_attention_scores(const void* Q, int32_t q_rows, int64_t q_s
       !launch(umma::score_attention_kernel<false>, a.units < places ? a.units : places, umma::kScoreThreads, umma::kScoreDynamic, false,
               stream, mq, mk, a))
     return CURDKV_ERR_CUDA;
-  if (!launch(umma::score_logsum_kernel, P * pl.row_tiles, kTileRows, 0, !lse_given, stream, a,
+  if (!launch(umma::score_logsum_kernel, P * pl.row_tiles, umma::kLogsumThreads, 0, !lse_given, stream, a,
               (const float*)(lse_given ? lse : nullptr), logsum, lse_given ? (float*)nullptr : lse, scores,
               pl.key_segs > 1 ? (int64_t)0 : P * d.n_max))
     return CURDKV_ERR_CUDA;

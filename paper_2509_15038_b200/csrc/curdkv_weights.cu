@@ -79,6 +79,12 @@ rows::Parts parts_of(const RowsPlan& pl, unsigned char* at, const int32_t* lens,
   return x;
 }
 
+// CTAs that join a problem's parts: one for each query row, as long as a grid holds them.
+int join_slices(int64_t problems, int64_t query_rows) {
+  const int64_t most = 0x7fffffffLL / (problems > 0 ? problems : 1);
+  return (int)(query_rows < most ? query_rows : most);
+}
+
 bool cache_ok(const curdkv_cache* c) {
   return c != nullptr && c->K != nullptr && c->V != nullptr && c->raw != nullptr && c->pos != nullptr &&
          c->count != nullptr && c->total != nullptr && c->capacity >= 1;
@@ -100,10 +106,10 @@ bool plan_cache(const curdkv_cache* c, const curdkv_desc* d, int32_t q_rows, Cac
   const int64_t P = (int64_t)d->batch * d->kv_heads, rows = (int64_t)(d->q_heads / d->kv_heads) * q_rows;
   if (rows > rows::kMostRows || P > (1 << 24)) return false;
   pl->rows = plan_rows(P, rows, c->capacity);
-  pl->pitch = (int)(rows < 8 * pl->rows.nt ? (rows + 1) / 2 * 2 : 8 * pl->rows.nt);
-  // joining: about four CTAs an SM, but 512 keys each at least
-  int64_t slices = (4 * (int64_t)sms() + (P > 0 ? P : 1) - 1) / (P > 0 ? P : 1);
-  const int64_t most = (c->capacity + 511) / 512;
+  pl->pitch = (int)(rows <= 2 ? 2 : (rows < 8 * pl->rows.nt ? (rows + 3) / 4 * 4 : 8 * pl->rows.nt));
+  // joining: about eight CTAs an SM, but 128 keys each at least
+  int64_t slices = (8 * (int64_t)sms() + (P > 0 ? P : 1) - 1) / (P > 0 ? P : 1);
+  const int64_t most = (c->capacity + 127) / 128;
   if (slices > most) slices = most;
   pl->slices = (int)slices;
   pl->parts_at = 256;
@@ -225,10 +231,10 @@ curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_st
   j.O = static_cast<__nv_bfloat16*>(O);
   j.o_sb = o_stride_b; j.o_sh = o_stride_h; j.o_sn = o_stride_n;
   j.lse = lse;
-  j.slices = 1;
+  j.slices = join_slices(P, a.q.rows);
   if (weights == nullptr) {
     if (!(pl.rows.nt == 1 ? launch_parts<1, false>(a, ctas, stream) : launch_parts<2, false>(a, ctas, stream))) return CURDKV_ERR_CUDA;
-    return launch_join<false, false>(j, P, stream) ? CURDKV_OK : CURDKV_ERR_CUDA;
+    return launch_join<false, false>(j, P * j.slices, stream) ? CURDKV_OK : CURDKV_ERR_CUDA;
   }
   a.logits = reinterpret_cast<float*>(ws + pl.logits_at);
   a.pitch = pl.pitch;
@@ -373,8 +379,7 @@ curdkv_status curdkv_attention_prefix(const void* Q, int32_t q_rows, int64_t q_s
   j.O = static_cast<__nv_bfloat16*>(O);
   j.o_sb = o_stride_b; j.o_sh = o_stride_h; j.o_sn = o_stride_n;
   j.lse = lse;
-  j.slices = (group * q_rows + 4 * rows::kJoinWarps - 1) / (4 * rows::kJoinWarps);
-  if (P * j.slices > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
+  j.slices = join_slices(P, (int64_t)group * q_rows);
   return launch_join<true, false>(j, P * j.slices, stream) ? CURDKV_OK : CURDKV_ERR_CUDA;
 }
 
