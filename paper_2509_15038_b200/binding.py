@@ -439,6 +439,7 @@ class DeviceCache:
         self.c = Cache(K.data_ptr(), V.data_ptr(), raw.data_ptr(), pos.data_ptr(), count.data_ptr(), total.data_ptr(),
                        self.capacity)
         self._ref = ctypes.byref(self.c)
+        self._descs = {}
 
 
 def cache_workspace(batch: int, kv_heads: int, t_max: int, capacity: int, budget: int,
@@ -542,6 +543,7 @@ def _on_device(what: str, first: torch.Tensor, *rest: Optional[torch.Tensor]) ->
 
 # batch, kv_heads, q_heads, n_max, d, r and the strides of K and V
 _DESC_ROWS = struct.Struct("=6i6q").unpack_from
+_DESC = struct.Struct("=6i6qQ4id").pack                    # a whole descriptor, lengths' address and flags behind those
 
 
 def _described(what: str, K: torch.Tensor, V: torch.Tensor, desc: Desc, dev: int) -> None:
@@ -862,13 +864,19 @@ def curdkv_cache_push(cache: DeviceCache, K_new, V_new, budget: int, workspace: 
     what = "curdkv_cache_push"
     dev = _on_device(what, cache.K, K_new, V_new, scores_new, t_new, workspace)
     _status_buffer(what, workspace)
-    desc = make_desc(K_new, V_new, 1, seqlens=t_new)
-    shape = K_new.shape
-    if shape[0] != cache.batch or shape[1] != cache.kv_heads or shape[3] != cache.d:
+    if K_new.dtype is not torch.bfloat16 or V_new.dtype is not torch.bfloat16:
+        raise TypeError(f"{what}: K_new and V_new must be bf16")
+    shape, k, v = K_new.shape, K_new.stride(), V_new.stride()
+    if len(shape) != 4 or shape != V_new.shape or k[3] != 1 or v[3] != 1:
+        raise ValueError(f"{what}: K_new and V_new must be [B, Hkv, t, d] with a contiguous last axis")
+    B, H, t, d = shape
+    if B != cache.batch or H != cache.kv_heads or d != cache.d:
         raise ValueError(f"{what}: new rows are {tuple(shape)}, the cache {(cache.batch, cache.kv_heads, cache.capacity, cache.d)}")
+    _int32("t_new", t_new, B)
     if scores_new is not None and (scores_new.dtype is not torch.float32 or scores_new.shape != shape[:3]
                                    or not scores_new.is_contiguous()):
         raise ValueError(f"{what}: scores_new must be contiguous fp32 {tuple(shape[:3])}")
+    desc = Desc.from_buffer_copy(_DESC(B, H, H, t, d, 1, *k[:3], *v[:3], 0 if t_new is None else t_new.data_ptr(), 0, 1, 0, 0, 0.0))
     code = load().curdkv_cache_push(cache._ref, _base(K_new, cache.K), _base(V_new, cache.K), _addr(scores_new),
                                     ctypes.byref(desc), index(budget), _count(num_sink), _count(window), workspace.data_ptr(),
                                     workspace.numel() * workspace.element_size(), _raw_stream(dev))
@@ -876,13 +884,16 @@ def curdkv_cache_push(cache: DeviceCache, K_new, V_new, budget: int, workspace: 
         _check(code, what)
 
 
-def _cache_desc(cache: DeviceCache, q_heads: int) -> Desc:
-    return Desc(cache.batch, cache.kv_heads, q_heads, cache.capacity, cache.d, 1)
+def _cache_desc(cache: DeviceCache, q_heads: int):
+    """Reference to a descriptor of the cache's shape for this number of query heads (shapes only: kept on the cache)."""
+    ref = cache._descs.get(q_heads)
+    if ref is None:
+        ref = cache._descs[q_heads] = ctypes.byref(Desc(cache.batch, cache.kv_heads, q_heads, cache.capacity, cache.d, 1))
+    return ref
 
 
 def cache_attention_workspace(cache: DeviceCache, q_heads: int, q_rows: int) -> torch.Tensor:
-    desc = _cache_desc(cache, int(q_heads))
-    nbytes = int(load().curdkv_cache_attention_workspace_bytes(cache._ref, ctypes.byref(desc), int(q_rows)))
+    nbytes = int(load().curdkv_cache_attention_workspace_bytes(cache._ref, _cache_desc(cache, int(q_heads)), int(q_rows)))
     if nbytes == 0:
         raise ValueError("invalid shape for curdkv_cache_attention")
     return torch.zeros((nbytes,), dtype=torch.uint8, device=cache.K.device)
@@ -909,8 +920,7 @@ def curdkv_cache_attention(Q, cache: DeviceCache, *, scale: float, weights: Opti
     dev = _on_device(what, cache.K, Q, O, lse, q_lens, weights, workspace)
     if B == 0:
         return O, workspace
-    desc = _cache_desc(cache, H)
-    code = load().curdkv_cache_attention(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), cache._ref, ctypes.byref(desc), scale,
+    code = load().curdkv_cache_attention(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), cache._ref, _cache_desc(cache, H), scale,
                                          O.data_ptr(), o[0], o[1], o[2], _addr(lse), _addr(weights), workspace.data_ptr(),
                                          workspace.numel() * workspace.element_size(), _raw_stream(dev))
     if code:

@@ -62,26 +62,47 @@ __device__ __forceinline__ int rows_held(const int32_t* lens, int set, int n_max
 }
 
 template <int NT>
-constexpr int smem_bytes() {
+__host__ __device__ constexpr int smem_bytes() {
   constexpr int ring = kWarps * kStages * kStageBytes, meet = kWarps * 8 * NT * 132 * 4;
   return ring > meet ? ring : meet;
 }
 
-template <int NT, bool LOGITS>
-__global__ void __launch_bounds__(kThreads, 2) part_kernel(const Args a) {
+// Where results go.
+struct Outputs {
+  __nv_bfloat16* O;                  // [batch][heads * group][t][128], strides in elements
+  int64_t o_sb, o_sh, o_sn;
+  float* lse;                        // [batch][heads * group][t] or nullptr
+  float* weights;                    // [batch][heads][n_max] or nullptr
+};
+
+__device__ __forceinline__ float inverse(float sum) { return sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum); }   // a NaN sum stays one
+__device__ __forceinline__ float share(float m, float top) { return top == -INFINITY ? 1.f : token::exp2_approx(m - top); }   // (top -inf: zeros, or NaN)
+
+// FUSED: the parts of an item are the CTAs of a cluster, which join them through distributed shared memory; logits (where
+// weights are asked for) stay in shared memory until reference and sum are known, and the call is one launch.
+constexpr int kMostSplit = 3;                              // log2 of the CTAs of a cluster
+constexpr int kLogitBytes = 14 * 1024;                     // what two CTAs an SM leave room for beside their rings
+constexpr int kMostKeys = 1024;                            // of a CTA with logits
+
+template <int NT, bool LOGITS, bool FUSED>
+__global__ void __launch_bounds__(kThreads, 2) part_kernel(const Args a, const Outputs out) {
   using namespace token;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ float2 s_ml[kWarps][8 * NT];
+  __shared__ float2 s_cta[8 * NT];                         // FUSED: this CTA's references and sums
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // the joining kernel waits for this one's end
 
-  const int item = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
+  const int item = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;       // (FUSED: chunk = rank in the cluster)
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int p = item / a.blocks, blk = item % a.blocks, set = p / a.q.heads, h = p % a.q.heads;
   bool held_ok = true;
   const int held = rows_held(a.lens, set, a.n_max, held_ok);
   if (!held_ok && chunk == 0 && tid == 0) flag_status(a.status, CURDKV_DEV_BAD_INDEX);
-  const int k0 = chunk * a.chunk, k1 = min(held, k0 + a.chunk);          // (chunks * chunk stays below 2^31)
-  if (k0 >= k1) return;
+  // (chunks * chunk stays below 2^31; the CTAs of a cluster share what is there evenly)
+  const int each = FUSED ? ((held + a.chunks - 1) / a.chunks + kKeys - 1) / kKeys * kKeys : a.chunk;
+  const int k0 = chunk * each, k1 = min(held, k0 + each);
+  if (!FUSED && k0 >= k1) return;
   const int r0 = blk * 8 * NT, r1 = min(a.q.rows, r0 + 8 * NT);
 
   // ------------------------------------------------------------ the ring of this warp
@@ -153,7 +174,11 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const Args a) {
     sees_to = __reduce_min_sync(0xffffffffu, sees_to);
   }
   const int32_t* pos = a.pos != nullptr ? a.pos + (int64_t)p * a.n_max : nullptr;
-  float* logits = LOGITS ? a.logits + ((int64_t)p * a.blocks + blk) * a.n_max * a.pitch : nullptr;
+  float* logits = nullptr;                                 // of key k0 onwards
+  if (LOGITS) {
+    if (FUSED) logits = reinterpret_cast<float*>(smem + smem_bytes<NT>());
+    else logits = a.logits + (((int64_t)p * a.blocks + blk) * a.n_max + k0) * a.pitch;
+  }
 
   float acc[NT][8][4], m[NT][2], l[NT][2];
 #pragma unroll
@@ -214,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const Args a) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           if (8 * nt + 2 * t < a.pitch && u0 + 8 * i + g < k1)
-            *reinterpret_cast<float2*>(logits + (int64_t)(u0 + 8 * i + g) * a.pitch + 8 * nt + 2 * t) =
+            *reinterpret_cast<float2*>(logits + (int64_t)(u0 - k0 + 8 * i + g) * a.pitch + 8 * nt + 2 * t) =
                 make_float2(s[nt][2 * i], s[nt][2 * i + 1]);
     }
     bool move = false;
@@ -304,15 +329,105 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const Args a) {
       const float4 x = *reinterpret_cast<const float4*>(meet + ((size_t)w * 8 * NT + qi) * 132 + c4);
       o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
     }
-    *reinterpret_cast<float4*>(a.part_o + (part + qi) * 128 + c4) = o;
+    float2 ml = make_float2(-INFINITY, 0.f);
     if (c4 == 0) {
-      float all = -INFINITY, sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) all = fmaxf(all, s_ml[w][qi].x);
+      for (int w = 0; w < kWarps; ++w) ml.x = fmaxf(ml.x, s_ml[w][qi].x);
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) sum += s_ml[w][qi].y * (all == -INFINITY ? 1.f : exp2_approx(s_ml[w][qi].x - all));
-      a.part_ml[part + qi] = make_float2(all, sum);
+      for (int w = 0; w < kWarps; ++w) ml.y += s_ml[w][qi].y * share(s_ml[w][qi].x, ml.x);
     }
+    if (FUSED) {                                           // (only this thread reads these four places)
+      *reinterpret_cast<float4*>(meet + (size_t)qi * 132 + c4) = o;
+      if (c4 == 0) s_cta[qi] = ml;
+    } else {
+      *reinterpret_cast<float4*>(a.part_o + (part + qi) * 128 + c4) = o;
+      if (c4 == 0) a.part_ml[part + qi] = ml;
+    }
+  }
+  if constexpr (FUSED) {
+    // ---------------------------------------------------------- the cluster joins its parts, in the order of their ranks
+    __shared__ float2 s_norm[8 * NT];                      // reference, 1 / sum
+    __shared__ float2 s_all[1 << kMostSplit][8 * NT];
+    // (the old weights are asked for before the wait for the others)
+    float* weights = LOGITS ? out.weights + (int64_t)p * a.n_max + k0 : nullptr;
+    float was[kMostKeys / kThreads];
+    if (LOGITS) {
+#pragma unroll
+      for (int k = 0; k < kMostKeys / kThreads; ++k)
+        if (tid + k * kThreads < k1 - k0) was[k] = weights[tid + k * kThreads];
+    }
+    if (a.chunks > 1) cluster_sync(); else __syncthreads();
+    for (int e = tid; e < a.chunks * 8 * NT; e += kThreads) {
+      const int c = e / (8 * NT), qi = e % (8 * NT);
+      if (a.chunks == 1) {
+        s_all[c][qi] = s_cta[qi];
+      } else {
+        float2 v;
+        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(peer_addr(smem_addr(&s_cta[qi]), c)) : "memory");
+        s_all[c][qi] = v;
+      }
+    }
+    __syncthreads();
+    if (LOGITS && tid < 8 * NT) {
+      float top = -INFINITY, sum = 0.f;
+      int i = 0;
+      const bool there = tid < r1 - r0;
+      const int bb = place(there ? r0 + tid : 0, i);
+      const bool live = there && i < (a.q_lens != nullptr ? min(max(a.q_lens[bb], 0), a.q.t) : a.q.t);
+      for (int c = 0; c < a.chunks; ++c) top = fmaxf(top, s_all[c][tid].x);
+      for (int c = 0; c < a.chunks; ++c) sum = fmaf(share(s_all[c][tid].x, top), s_all[c][tid].y, sum);
+      // (a row that does not exist weighs nothing)
+      s_norm[tid] = live ? make_float2(top == -INFINITY ? 0.f : top, inverse(sum)) : make_float2(0.f, 0.f);
+    }
+    const int rows = r1 - r0;
+    for (int e = chunk * kThreads + tid; e < rows * 32; e += a.chunks * kThreads) {
+      const int qi = e >> 5, c4 = (e & 31) * 4;
+      float2 ml[1 << kMostSplit];
+      float4 x[1 << kMostSplit];
+      float top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int c = 0; c < (1 << kMostSplit); ++c) {
+        if (c >= a.chunks) break;
+        ml[c] = s_all[c][qi];
+        const float* at_c4 = meet + (size_t)qi * 132 + c4;
+        x[c] = a.chunks == 1 ? *reinterpret_cast<const float4*>(at_c4) : peer_float4(peer_addr(smem_addr(at_c4), c));
+        top = fmaxf(top, ml[c].x);
+      }
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int c = 0; c < (1 << kMostSplit); ++c) {
+        if (c >= a.chunks) break;
+        const float f = share(ml[c].x, top);
+        sum = fmaf(f, ml[c].y, sum);
+        o.x = fmaf(f, x[c].x, o.x); o.y = fmaf(f, x[c].y, o.y); o.z = fmaf(f, x[c].z, o.z); o.w = fmaf(f, x[c].w, o.w);
+      }
+      int i;
+      const int r = r0 + qi, bb = place(r, i), hq = h * a.q.group + r % a.q.group;
+      const int live = a.q_lens != nullptr ? min(max(a.q_lens[bb], 0), a.q.t) : a.q.t;
+      if (i >= live) continue;                             // rows behind the last query stay as they are
+      const float inv = inverse(sum);
+      *reinterpret_cast<uint2*>(out.O + bb * out.o_sb + hq * out.o_sh + i * out.o_sn + c4) =
+          make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+      if (c4 == 0 && out.lse != nullptr)
+        out.lse[((int64_t)bb * a.q.heads * a.q.group + hq) * a.q.t + i] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    }
+    if (LOGITS) {
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kMostKeys / kThreads; ++k) {
+        const int j = tid + k * kThreads;
+        if (j >= k1 - k0) break;
+        const float* x = logits + (size_t)j * a.pitch;
+        float w = 0.f;
+        for (int r = 0; r < a.pitch; r += 2) {
+          const float2 v = *reinterpret_cast<const float2*>(x + r), n0 = s_norm[r], n1 = s_norm[r + 1];
+          w = fmaf(exp2_approx(v.x - n0.x), n0.y, w);
+          w = fmaf(exp2_approx(v.y - n1.x), n1.y, w);
+        }
+        weights[j] = was[k] + w;
+      }
+    }
+    if (a.chunks > 1) cluster_sync();                      // nobody leaves while its parts are read
   }
 }
 
@@ -350,13 +465,10 @@ struct JoinArgs {
   Parts own, prefix;                 // prefix: only with PREFIX
   int heads, group, t, share;        // (set of the prefix: sequence / share)
   const int32_t* q_lens;
-  __nv_bfloat16* O;                  // [batch][heads * group][t][128], strides in elements
-  int64_t o_sb, o_sh, o_sn;
-  float* lse;
+  Outputs out;
   int slices;                        // CTAs per problem
   const float* logits;               // as in Args, with LOGITS
   int n_max, pitch, block_rows;
-  float* weights;                    // [batch][heads][n_max]
 };
 
 constexpr int kJoinWarps = 4;
@@ -401,7 +513,6 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_parts_kernel(const JoinA
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
   };
-  auto share = [](float m, float top) { return top == -INFINITY ? 1.f : token::exp2_approx(m - top); };   // (top -inf: zeros, or NaN)
   // reference and sum of a row, a lane per part
   auto stats = [&](const Row& x, float& top, float& sum) {
     const float2 first = lane < all_parts ? ml(x, lane) : make_float2(-INFINITY, 0.f);
@@ -415,7 +526,6 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_parts_kernel(const JoinA
     }
     sum = total(sum);
   };
-  auto inverse = [](float sum) { return sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum); };              // a NaN sum stays one
 
   int turn = 0;
   for (int r = slice; r < rows; r += a.slices) {
@@ -453,10 +563,10 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_parts_kernel(const JoinA
       }
       const float inv = inverse(sum);
       const int hq = h * a.group + g;
-      *reinterpret_cast<uint2*>(a.O + b * a.o_sb + hq * a.o_sh + i * a.o_sn + lane * 4) =
+      *reinterpret_cast<uint2*>(a.out.O + b * a.out.o_sb + hq * a.out.o_sh + i * a.out.o_sn + lane * 4) =
           make_uint2(token::pack_bf16(o.x * inv, o.y * inv), token::pack_bf16(o.z * inv, o.w * inv));
-      if (lane == 0 && a.lse != nullptr)
-        a.lse[((int64_t)b * a.heads * a.group + hq) * a.t + i] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+      if (lane == 0 && a.out.lse != nullptr)
+        a.out.lse[((int64_t)b * a.heads * a.group + hq) * a.t + i] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     }
     turn ^= 1;
   }
@@ -479,7 +589,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_parts_kernel(const JoinA
   const int held = seq_len_of(a.own.lens, b, a.n_max);
   const int j0 = (int)((int64_t)held * slice / a.slices), j1 = (int)((int64_t)held * (slice + 1) / a.slices);
   const float* logits = a.logits + (int64_t)p * blocks * a.n_max * a.pitch;
-  float* weights = a.weights + (int64_t)p * a.n_max;
+  float* weights = a.out.weights + (int64_t)p * a.n_max;
   constexpr int kAtOnce = 4;                               // keys of a thread in flight
   for (int j = j0 + threadIdx.x; j < j1; j += kAtOnce * kJoinWarps * 32) {
     float w[kAtOnce], was[kAtOnce];

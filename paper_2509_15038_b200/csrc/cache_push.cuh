@@ -26,6 +26,8 @@ __global__ void __launch_bounds__(1024) cache_push_kernel(const PushArgs s) {
   __shared__ int s_leave[kPushMost];
   const AppendArgs& a = s.append;
   const int p = blockIdx.x, b = p / a.heads, h = p % a.heads, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");       // launched behind the kernel before it without waiting for its end
   const int cap = a.cache.capacity;
   int tb = a.t_new != nullptr ? a.t_new[b] : a.t;
   tb = tb < 0 ? 0 : (tb > a.t ? a.t : tb);
@@ -49,9 +51,25 @@ __global__ void __launch_bounds__(1024) cache_push_kernel(const PushArgs s) {
     return ((unsigned long long)key << 32) | (uint32_t)~j;
   };
   constexpr unsigned long long kNone = ~0ull;
+  // Held slots come four at a time where rows of weights and positions are 16-byte aligned, two such loads of each in flight.
+  const bool wide = (cap & 3) == 0 && ((reinterpret_cast<uintptr_t>(a.cache.raw) | reinterpret_cast<uintptr_t>(a.cache.pos)) & 15u) == 0;
+  const int quads = wide ? held >> 2 : 0;
   auto least_above = [&](unsigned long long last, bool any) {                // of this thread's slots
     unsigned long long best = kNone;
-    for (int j = tid; j < n; j += blockDim.x) {
+    auto take = [&](int j, int at, float w) {
+      const uint32_t key = at < s.num_sink || at >= recent ? kForcedKey : score_key(w);
+      const unsigned long long x = ((unsigned long long)key << 32) | (uint32_t)~j;
+      if ((!any || x > last) && x < best) best = x;
+    };
+    for (int q = tid; q < quads; q += 2 * blockDim.x) {
+      const int q1 = q + blockDim.x;
+      const bool two = q1 < quads;
+      const int4 p0 = reinterpret_cast<const int4*>(pos)[q], p1 = reinterpret_cast<const int4*>(pos)[two ? q1 : q];
+      const float4 w0 = reinterpret_cast<const float4*>(raw)[q], w1 = reinterpret_cast<const float4*>(raw)[two ? q1 : q];
+      take(4 * q, p0.x, w0.x); take(4 * q + 1, p0.y, w0.y); take(4 * q + 2, p0.z, w0.z); take(4 * q + 3, p0.w, w0.w);
+      if (two) { take(4 * q1, p1.x, w1.x); take(4 * q1 + 1, p1.y, w1.y); take(4 * q1 + 2, p1.z, w1.z); take(4 * q1 + 3, p1.w, w1.w); }
+    }
+    for (int j = 4 * quads + tid; j < n; j += blockDim.x) {
       const unsigned long long x = rank(j);
       if ((!any || x > last) && x < best) best = x;
     }

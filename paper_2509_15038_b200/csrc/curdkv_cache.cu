@@ -331,13 +331,16 @@ curdkv_status curdkv_cache_push(const curdkv_cache* cache, const void* K_new, co
   cfg.gridDim = dim3((unsigned)P);
   cfg.blockDim = dim3(cache->capacity <= 4096 ? 256 : 1024);
   cfg.stream = stream;
-  cudaLaunchAttribute attr = {};
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
   if (a.heads <= 8) {                                      // a cluster per sequence
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)a.heads;
-    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)a.heads;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.numAttrs = 2;
   } else {
     s.tickets = reinterpret_cast<int32_t*>(static_cast<unsigned char*>(workspace) + L.tickets);
     if (cudaMemsetAsync(s.tickets, 0, (size_t)desc_new->batch * sizeof(int32_t), stream) != cudaSuccess) return CURDKV_ERR_CUDA;

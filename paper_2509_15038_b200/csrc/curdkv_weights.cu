@@ -41,29 +41,38 @@ RowsPlan plan_rows(int64_t problems, int64_t query_rows, int64_t keys) {
 
 size_t parts_bytes(size_t entries) { return round256(entries * sizeof(float2)) + round256(entries * 128 * sizeof(float)); }
 
-template <int NT, bool LOGITS>
-bool launch_parts(const rows::Args& a, int64_t ctas, cudaStream_t stream) {
-  constexpr int smem = rows::smem_bytes<NT>();
-  static std::atomic<uint64_t> done{0};
-  if (!allow_smem(rows::part_kernel<NT, LOGITS>, smem, done)) return false;
-  rows::part_kernel<NT, LOGITS><<<(unsigned)ctas, rows::kThreads, smem, stream>>>(a);
+// Launched behind the kernel before it on the stream without waiting for its end: the kernels themselves wait.  `cluster` CTAs
+// each, where above 1.
+template <typename Kernel, typename... Args>
+bool launch_behind(Kernel kernel, int64_t ctas, int threads, int smem, int cluster, cudaStream_t stream, const Args&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  if (cudaLaunchKernelEx(&cfg, kernel, args...) != cudaSuccess) return false;
   return launched();
+}
+
+template <int NT, bool LOGITS, bool FUSED>
+bool launch_parts(const rows::Args& a, const rows::Outputs& out, int64_t ctas, cudaStream_t stream) {
+  constexpr int most = rows::smem_bytes<NT>() + (FUSED && LOGITS ? rows::kLogitBytes : 0);
+  static std::atomic<uint64_t> done{0};
+  if (!allow_smem(rows::part_kernel<NT, LOGITS, FUSED>, most, done)) return false;
+  return launch_behind(rows::part_kernel<NT, LOGITS, FUSED>, ctas, rows::kThreads, most, FUSED ? a.chunks : 1, stream, a, out);
 }
 
 template <bool PREFIX, bool LOGITS>
 bool launch_join(const rows::JoinArgs& a, int64_t ctas, cudaStream_t stream) {
-  // launched behind the kernel before it without waiting for its end: the kernel itself waits
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)ctas);
-  cfg.blockDim = dim3(rows::kJoinWarps * 32);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr = {};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, rows::join_parts_kernel<PREFIX, LOGITS>, a) != cudaSuccess) return false;
-  return launched();
+  return launch_behind(rows::join_parts_kernel<PREFIX, LOGITS>, ctas, rows::kJoinWarps * 32, 0, 1, stream, a);
 }
 
 rows::Parts parts_of(const RowsPlan& pl, unsigned char* at, const int32_t* lens, int n_max) {
@@ -93,6 +102,7 @@ bool cache_ok(const curdkv_cache* c) {
 // ---- attention over a generation-phase cache ---------------------------------------------------
 struct CachePlan {
   RowsPlan rows;
+  int cluster;                       // CTAs of a KV head's cluster; 0: parts and a second kernel
   int pitch, slices;
   size_t parts_at, logits_at, bytes;
 };
@@ -107,6 +117,26 @@ bool plan_cache(const curdkv_cache* c, const curdkv_desc* d, int32_t q_rows, Cac
   if (rows > rows::kMostRows || P > (1 << 24)) return false;
   pl->rows = plan_rows(P, rows, c->capacity);
   pl->pitch = (int)(rows <= 2 ? 2 : (rows < 8 * pl->rows.nt ? (rows + 3) / 4 * 4 : 8 * pl->rows.nt));
+  // One launch where a KV head's query rows are one block and its logits fit into the shared memory of a cluster, with more
+  // CTAs while all find room on the device and each keeps two steps of its warps.  Not where that takes more than two rounds
+  // of clusters (their ends, when nothing is loaded, add up) nor where clusters of eight leave half the places empty to long
+  // caches.  With weights, 4 query rows, us, clusters | parts and a second kernel:
+  //   8 heads of 200 rows 6.0 | 8.9, of 1702 8.0 | 8.2, of 7000 15.0 | 12.5        32 of 1702 9.0 | 10.8        64 of 7000 46.9 | 48.3
+  //   128 heads of 2048 31.0 | 33.7, of 4096 60.3 | 54.9       320 of 2048 74 | 69         1024 of 500 55 | 65, of 2048 211 | 188
+  pl->cluster = 0;
+  if (pl->rows.blocks == 1) {
+    const int64_t keys = c->capacity, slots = 2 * (int64_t)sms();
+    int split = 0;
+    auto fits = [&](int k) {
+      const int64_t each = ((keys + (1 << k) - 1) >> k) + rows::kKeys;
+      return each <= rows::kMostKeys && each * pl->pitch * 4 <= rows::kLogitBytes;
+    };
+    while (split < rows::kMostSplit && !fits(split)) ++split;
+    const bool fit = fits(split);
+    while (split < rows::kMostSplit && (P << (split + 1)) <= slots && keys > (2 * rows::kWarps * rows::kKeys) << split) ++split;
+    const bool waves = split > 0 && (P << split) > 2 * slots, idle = 2 * (P << split) <= slots && (keys >> split) > 512;
+    if (fit && !waves && !idle) pl->cluster = 1 << split;
+  }
   // joining: about eight CTAs an SM, but 128 keys each at least
   int64_t slices = (8 * (int64_t)sms() + (P > 0 ? P : 1) - 1) / (P > 0 ? P : 1);
   const int64_t most = (c->capacity + 127) / 128;
@@ -195,7 +225,7 @@ curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_st
   if (workspace_bytes < pl.bytes) return CURDKV_ERR_WORKSPACE;
   const int64_t P = (int64_t)desc->batch * desc->kv_heads;
   if (P == 0) return CURDKV_OK;
-  const int64_t ctas = P * pl.rows.blocks * pl.rows.chunks;
+  const int64_t ctas = pl.cluster > 0 ? P * pl.cluster : P * pl.rows.blocks * pl.rows.chunks;
   if (ctas > 0x7fffffffLL || P * pl.slices > 0x7fffffffLL) return CURDKV_ERR_UNSUPPORTED;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
@@ -221,6 +251,15 @@ curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_st
   a.part_ml = const_cast<float2*>(own.ml);
   a.part_o = const_cast<float*>(own.o);
   a.status = reinterpret_cast<uint32_t*>(ws);
+  a.pitch = pl.pitch;
+  const rows::Outputs out = {static_cast<__nv_bfloat16*>(O), o_stride_b, o_stride_h, o_stride_n, lse, weights};
+  const bool one = pl.rows.nt == 1;
+  if (pl.cluster > 0) {
+    a.chunks = pl.cluster;
+    const bool done = weights != nullptr ? (one ? launch_parts<1, true, true>(a, out, ctas, stream) : launch_parts<2, true, true>(a, out, ctas, stream))
+                                         : (one ? launch_parts<1, false, true>(a, out, ctas, stream) : launch_parts<2, false, true>(a, out, ctas, stream));
+    return done ? CURDKV_OK : CURDKV_ERR_CUDA;
+  }
   rows::JoinArgs j = {};
   j.own = own;
   j.heads = desc->kv_heads;
@@ -228,23 +267,19 @@ curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_st
   j.t = q_rows;
   j.share = 1;
   j.q_lens = q_lens;
-  j.O = static_cast<__nv_bfloat16*>(O);
-  j.o_sb = o_stride_b; j.o_sh = o_stride_h; j.o_sn = o_stride_n;
-  j.lse = lse;
-  j.slices = join_slices(P, a.q.rows);
+  j.out = out;
   if (weights == nullptr) {
-    if (!(pl.rows.nt == 1 ? launch_parts<1, false>(a, ctas, stream) : launch_parts<2, false>(a, ctas, stream))) return CURDKV_ERR_CUDA;
+    j.slices = join_slices(P, a.q.rows);
+    if (!(one ? launch_parts<1, false, false>(a, out, ctas, stream) : launch_parts<2, false, false>(a, out, ctas, stream))) return CURDKV_ERR_CUDA;
     return launch_join<false, false>(j, P * j.slices, stream) ? CURDKV_OK : CURDKV_ERR_CUDA;
   }
   a.logits = reinterpret_cast<float*>(ws + pl.logits_at);
-  a.pitch = pl.pitch;
   j.slices = pl.slices;
   j.logits = a.logits;
   j.n_max = cache->capacity;
   j.pitch = pl.pitch;
   j.block_rows = 8 * pl.rows.nt;
-  j.weights = weights;
-  if (!(pl.rows.nt == 1 ? launch_parts<1, true>(a, ctas, stream) : launch_parts<2, true>(a, ctas, stream))) return CURDKV_ERR_CUDA;
+  if (!(one ? launch_parts<1, true, false>(a, out, ctas, stream) : launch_parts<2, true, false>(a, out, ctas, stream))) return CURDKV_ERR_CUDA;
   return launch_join<false, true>(j, P * pl.slices, stream) ? CURDKV_OK : CURDKV_ERR_CUDA;
 }
 
@@ -292,7 +327,7 @@ curdkv_status curdkv_attention_prefix(const void* Q, int32_t q_rows, int64_t q_s
     a.chunks = r.chunks;
     a.part_ml = const_cast<float2*>(parts.ml);
     a.part_o = const_cast<float*>(parts.o);
-    return r.nt == 1 ? launch_parts<1, false>(a, ctas, stream) : launch_parts<2, false>(a, ctas, stream);
+    return r.nt == 1 ? launch_parts<1, false, false>(a, rows::Outputs{}, ctas, stream) : launch_parts<2, false, false>(a, rows::Outputs{}, ctas, stream);
   };
   const bool tiles = pl.tiles &&
       map_strides_ok(desc_prefix->batch, desc->kv_heads, desc_prefix->k_stride_b, desc_prefix->k_stride_h, desc_prefix->k_stride_n) &&
@@ -376,9 +411,7 @@ curdkv_status curdkv_attention_prefix(const void* Q, int32_t q_rows, int64_t q_s
   j.t = q_rows;
   j.share = share;
   j.q_lens = q_lens;
-  j.O = static_cast<__nv_bfloat16*>(O);
-  j.o_sb = o_stride_b; j.o_sh = o_stride_h; j.o_sn = o_stride_n;
-  j.lse = lse;
+  j.out = rows::Outputs{static_cast<__nv_bfloat16*>(O), o_stride_b, o_stride_h, o_stride_n, lse, nullptr};
   j.slices = join_slices(P, (int64_t)group * q_rows);
   return launch_join<true, false>(j, P * j.slices, stream) ? CURDKV_OK : CURDKV_ERR_CUDA;
 }
