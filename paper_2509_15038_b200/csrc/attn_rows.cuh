@@ -109,6 +109,10 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const Args a, const O
   const uint32_t ring = smem_addr(smem) + warp * kStages * kStageBytes;
   const __nv_bfloat16* kb = a.K.base + set * a.K.stride_b + h * a.K.stride_h + (lane & 15) * 8;
   const __nv_bfloat16* vb = a.V.base + set * a.V.stride_b + h * a.V.stride_h + (lane & 15) * 8;
+  // rows that one block of queries reads once leave the L2 to the logits and parts (128 heads of 2048 rows 189 -> 182 us)
+  uint64_t pol;
+  if (a.blocks > 1) asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
+  else asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol));
   auto fetch = [&](int u0, int stage) {
     const uint32_t dst = ring + stage * kStageBytes;
 #pragma unroll
@@ -117,8 +121,8 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const Args a, const O
       const bool live = u0 + key < k1;
       const int64_t j = live ? u0 + key : k0;
       const uint32_t at = (uint32_t)(key * 256 + (((lane & 15) ^ (key & 7)) * 16));
-      copy16(dst + at, kb + j * a.K.stride_n, live);
-      copy16(dst + kKeys * 256 + at, vb + j * a.V.stride_n, live);
+      copy16(dst + at, kb + j * a.K.stride_n, live, pol);
+      copy16(dst + kKeys * 256 + at, vb + j * a.V.stride_n, live, pol);
     }
   };
   constexpr int kStep = kWarps * kKeys;
