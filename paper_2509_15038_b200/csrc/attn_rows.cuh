@@ -49,6 +49,7 @@ struct Args {
   float2* part_ml;                   // [items][chunks][8 NT]: m, l
   float* part_o;                     // [items][chunks][8 NT][128]
   float* logits;                     // [sets * heads][blocks][n_max][pitch], or nullptr
+  int late;                          // 1: runs beside the kernel before it
   int pitch;                         // 2 or a multiple of 4, at least the rows of a block
   uint32_t* status;
 };
@@ -85,7 +86,8 @@ constexpr int kLogitBytes = 14 * 1024;                     // what two CTAs an S
 constexpr int kMostKeys = 1024;                            // of a CTA with logits
 
 template <int NT, bool LOGITS, bool FUSED>
-__global__ void __launch_bounds__(kThreads, 2) part_kernel(const Args a, const Outputs out) {
+__global__ void __launch_bounds__(kThreads, 2) part_kernel(const __grid_constant__ Args before, const __grid_constant__ Args behind,
+                                                           const int first_ctas, const Outputs out) {
   using namespace token;
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ float2 s_ml[kWarps][8 * NT];
@@ -93,8 +95,12 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const Args a, const O
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");       // the joining kernel waits for this one's end
 
-  const int item = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;       // (FUSED: chunk = rank in the cluster)
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  // two sets of parts may share a launch (the prefix's and the own rows'): the first CTAs take the first
+  const bool second = (int)blockIdx.x >= first_ctas;
+  const Args& a = second ? behind : before;
+  const int cta = (int)blockIdx.x - (second ? first_ctas : 0);
+  const int item = cta / a.chunks, chunk = cta % a.chunks;             // (FUSED: chunk = rank in the cluster)
+  if (!a.late) asm volatile("griddepcontrol.wait;" ::: "memory");
   const int p = item / a.blocks, blk = item % a.blocks, set = p / a.q.heads, h = p % a.q.heads;
   bool held_ok = true;
   const int held = rows_held(a.lens, set, a.n_max, held_ok);
@@ -102,7 +108,15 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const Args a, const O
   // (chunks * chunk stays below 2^31; the CTAs of a cluster share what is there evenly)
   const int each = FUSED ? ((held + a.chunks - 1) / a.chunks + kKeys - 1) / kKeys * kKeys : a.chunk;
   const int k0 = chunk * each, k1 = min(held, k0 + each);
-  if (!FUSED && k0 >= k1) return;
+  // With `late` the kernel before this one has begun and nothing of it is needed here, but the joining kernel, which waits for
+  // the end of this one only, needs both: the first CTA stays until that one has ended, the others make room.
+  auto wait_late = [&]() {
+    if (a.late && blockIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+  };
+  if (!FUSED && k0 >= k1) {
+    wait_late();
+    return;
+  }
   const int r0 = blk * 8 * NT, r1 = min(a.q.rows, r0 + 8 * NT);
 
   // ------------------------------------------------------------ the ring of this warp
@@ -324,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const Args a, const O
       }
     }
   __syncthreads();
-  const size_t part = (size_t)blockIdx.x * 8 * NT;
+  const size_t part = (size_t)cta * 8 * NT;
   for (int e = tid; e < (r1 - r0) * 32; e += kThreads) {
     const int qi = e >> 5, c4 = (e & 31) * 4;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -433,6 +447,7 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const Args a, const O
     }
     if (a.chunks > 1) cluster_sync();                      // nobody leaves while its parts are read
   }
+  wait_late();
 }
 
 // ---- joining -----------------------------------------------------------------------------------

@@ -23,9 +23,9 @@ struct RowsPlan {
 // rounds of them while each has 2048 keys (64 heads of 65540 rows, 8 query rows: 421 us instead of 440); several
 // rounds of parts when heads are many, so that the last round costs little and ragged heads even out.  A part has at least
 // two steps of its four warps (128 keys).
-RowsPlan plan_rows(int64_t problems, int64_t query_rows, int64_t keys) {
+RowsPlan plan_rows(int64_t problems, int64_t query_rows, int64_t keys, int nt = 0) {
   RowsPlan pl;
-  pl.nt = query_rows <= 8 ? 1 : 2;
+  pl.nt = nt > 0 ? nt : (query_rows <= 8 ? 1 : 2);
   pl.blocks = (int)((query_rows + 8 * pl.nt - 1) / (8 * pl.nt));
   const int64_t items = problems * pl.blocks > 0 ? problems * pl.blocks : 1, slots = 2 * (int64_t)sms();
   int64_t chunks = items <= slots ? slots / items : (6 * slots + items - 1) / items;
@@ -65,11 +65,13 @@ bool launch_behind(Kernel kernel, int64_t ctas, int threads, int smem, int clust
 }
 
 template <int NT, bool LOGITS, bool FUSED>
-bool launch_parts(const rows::Args& a, const rows::Outputs& out, int64_t ctas, cudaStream_t stream) {
+bool launch_parts(const rows::Args& a, const rows::Outputs& out, int64_t ctas, cudaStream_t stream, const rows::Args* first = nullptr,
+                  int64_t first_ctas = 0) {
   constexpr int most = rows::smem_bytes<NT>() + (FUSED && LOGITS ? rows::kLogitBytes : 0);
   static std::atomic<uint64_t> done{0};
   if (!allow_smem(rows::part_kernel<NT, LOGITS, FUSED>, most, done)) return false;
-  return launch_behind(rows::part_kernel<NT, LOGITS, FUSED>, ctas, rows::kThreads, most, FUSED ? a.chunks : 1, stream, a, out);
+  return launch_behind(rows::part_kernel<NT, LOGITS, FUSED>, first_ctas + ctas, rows::kThreads, most, FUSED ? a.chunks : 1, stream,
+                       first_ctas > 0 ? *first : a, a, (int)first_ctas, out);
 }
 
 template <bool PREFIX, bool LOGITS>
@@ -158,24 +160,31 @@ struct PrefixPlan {
   size_t pre_at, own_at, bytes;
 };
 
-// The tile form of the prefix: CTAs (one an SM) per tile of query rows so that their rounds, each as long as its run of key
-// tiles and some eight tiles more (start, first and last tile, output), end soonest.
-void plan_tiles(int64_t problems, int share, int t, int group, int64_t keys, PrefixPlan* pl) {
+// The tile form of the prefix: CTAs (one an SM) per tile of query rows, or pair of them, so that the call ends soonest.  A
+// round takes its run of key tiles, 1.75 us each for a pair and 1.15 us for a single tile, and 8 us for start, first and last
+// tile and output.  SMs that it leaves free read the own rows meanwhile, up to 90 GB/s each; what is left of these then
+// takes the whole device, 6 TB/s.  (64 sequences of up to 512 own rows behind 32768: 112 CTAs of
+// 19 steps 58 us, 144 of 15 steps 64.)
+void plan_tiles(int64_t problems, int share, int t, int group, int64_t keys, double own_bytes, PrefixPlan* pl) {
   const int most = kTileRows / group;                      // (sequence, token) pairs of a tile
   pl->tokens = t < most ? t : most;
   pl->seqs = most / pl->tokens < share ? most / pl->tokens : share;
   pl->token_tiles = (t + pl->tokens - 1) / pl->tokens;
   pl->row_tiles = (share + pl->seqs - 1) / pl->seqs * pl->token_tiles;
   const int64_t key_tiles = (keys + kTileRows - 1) / kTileRows, items = problems * ((pl->row_tiles + 1) / 2), places = sms();
-  int64_t best = -1;
-  for (int64_t c = 1; c <= key_tiles && c <= 512; ++c) {
-    const int64_t each = (key_tiles + c - 1) / c, cost = (items * c + places - 1) / places * (each + 8);
-    if (best < 0 || cost < best) {
+  const double step = pl->row_tiles > 1 ? 1.75 : 1.15;
+  double best = -1.;
+  const int64_t upto = 2 * places / items + 2;             // (two rounds)
+  for (int64_t c = 1; c <= key_tiles && c <= upto; ++c) {
+    const int64_t each = (key_tiles + c - 1) / c, ctas = items * ((key_tiles + each - 1) / each);
+    const double walk = (double)((ctas + places - 1) / places) * ((double)each * step + 8.);
+    const double beside = ctas < places ? (double)(places - ctas) * 90e3 * walk : 0.;
+    const double cost = walk + (own_bytes > beside ? (own_bytes - beside) / 6e6 : 0.);
+    if (best < 0. || cost < best) {
       best = cost;
       pl->chunk = (int)each * kTileRows;
       pl->chunks = (int)((key_tiles + each - 1) / each);
     }
-    if (items * c > 8 * places) break;                     // (many rounds are even enough)
   }
 }
 
@@ -188,12 +197,17 @@ bool plan_prefix(const curdkv_desc* dp, const curdkv_desc* d, int32_t q_rows, Pr
   const int64_t rows = (int64_t)group * q_rows, share = d->batch > 0 ? d->batch / dp->batch : 1;
   if (P > (1 << 24) || rows > (1 << 24) || rows * share > (1 << 28)) return false;
   pl->pre = plan_rows(P0, rows * share, dp->n_max);
-  pl->own = plan_rows(P, rows, d->n_max);
+  pl->own = plan_rows(P, rows, d->n_max, pl->pre.nt);      // (both may be one launch)
+  if (rows * share > 16) pl->own = plan_rows(P, rows, d->n_max);
   pl->tiles = rows * share > 16 && group <= kTileRows && dp->n_max > 0;
   size_t entries = pl->pre.entries;
   if (pl->tiles) {
-    plan_tiles(P0, (int)share, q_rows, group, dp->n_max, pl);
-    const size_t tiles = (size_t)P0 * pl->row_tiles * pl->chunks * kTileRows;
+    plan_tiles(P0, (int)share, q_rows, group, dp->n_max, 512. * (double)P * d->n_max * ((rows + 15) / 16), pl);
+    // as many parts as any own rows could lead to: a workspace for long ones serves short ones too
+    const int64_t items = P0 * ((pl->row_tiles + 1) / 2), key_tiles = ((int64_t)dp->n_max + kTileRows - 1) / kTileRows;
+    int64_t most = items > 0 ? 2 * (int64_t)sms() / items + 2 : 1;
+    if (most > key_tiles) most = key_tiles;
+    const size_t tiles = (size_t)P0 * pl->row_tiles * most * kTileRows;
     if (tiles > entries) entries = tiles;                  // (rows that the maps cannot hold take the other form)
   }
   pl->pre_at = 256;
@@ -323,14 +337,15 @@ curdkv_status curdkv_attention_prefix(const void* Q, int32_t q_rows, int64_t q_s
   a.scale_log2 = scale * 1.4426950408889634f;
   a.q_lens = q_lens;
   a.status = reinterpret_cast<uint32_t*>(ws);
-  auto run = [&](const RowsPlan& r, const rows::Parts& parts, int64_t ctas) {
+  auto cut = [&](const RowsPlan& r, const rows::Parts& parts) {
     a.blocks = r.blocks;
     a.chunk = r.chunk;
     a.chunks = r.chunks;
     a.part_ml = const_cast<float2*>(parts.ml);
     a.part_o = const_cast<float*>(parts.o);
-    return r.nt == 1 ? launch_parts<1, false, false>(a, rows::Outputs{}, ctas, stream) : launch_parts<2, false, false>(a, rows::Outputs{}, ctas, stream);
   };
+  rows::Args both = {};                                    // the prefix's parts, where the own rows' launch takes them along
+  int64_t both_ctas = 0;
   const bool tiles = pl.tiles &&
       map_strides_ok(desc_prefix->batch, desc->kv_heads, desc_prefix->k_stride_b, desc_prefix->k_stride_h, desc_prefix->k_stride_n) &&
       map_strides_ok(desc_prefix->batch, desc->kv_heads, desc_prefix->v_stride_b, desc_prefix->v_stride_h, desc_prefix->v_stride_n) &&
@@ -396,7 +411,9 @@ curdkv_status curdkv_attention_prefix(const void* Q, int32_t q_rows, int64_t q_s
     a.V = KvView{static_cast<const __nv_bfloat16*>(V_prefix), desc_prefix->v_stride_b, desc_prefix->v_stride_h, desc_prefix->v_stride_n};
     a.lens = desc_prefix->seqlens;
     a.n_max = desc_prefix->n_max;
-    if (!run(pl.pre, j.prefix, pre_ctas)) return CURDKV_ERR_CUDA;
+    cut(pl.pre, j.prefix);
+    both = a;
+    both_ctas = pre_ctas;
   }
   if (desc->n_max > 0) {
     a.q = rows::Queries{static_cast<const __nv_bfloat16*>(Q), q_stride_b, q_stride_h, q_stride_n, desc->kv_heads, group, q_rows,
@@ -406,7 +423,20 @@ curdkv_status curdkv_attention_prefix(const void* Q, int32_t q_rows, int64_t q_s
     a.lens = desc->seqlens;
     a.n_max = desc->n_max;
     a.causal = 1;
-    if (!run(pl.own, j.own, own_ctas)) return CURDKV_ERR_CUDA;
+    a.late = tiles ? 1 : 0;                                // (that kernel is launched behind everything before it)
+    cut(pl.own, j.own);
+  }
+  const int64_t ctas = desc->n_max > 0 ? own_ctas : 0;
+  if (both_ctas > 0 && (pl.pre.nt != pl.own.nt || ctas + both_ctas > 0x7fffffffLL)) {
+    if (!(pl.pre.nt == 1 ? launch_parts<1, false, false>(both, rows::Outputs{}, both_ctas, stream)
+                         : launch_parts<2, false, false>(both, rows::Outputs{}, both_ctas, stream)))
+      return CURDKV_ERR_CUDA;
+    both_ctas = 0;
+  }
+  if (ctas + both_ctas > 0) {
+    if (!(pl.own.nt == 1 ? launch_parts<1, false, false>(a, rows::Outputs{}, ctas, stream, &both, both_ctas)
+                         : launch_parts<2, false, false>(a, rows::Outputs{}, ctas, stream, &both, both_ctas)))
+      return CURDKV_ERR_CUDA;
   }
   j.heads = desc->kv_heads;
   j.group = group;
