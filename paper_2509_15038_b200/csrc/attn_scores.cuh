@@ -7,14 +7,9 @@
 //
 // Transposing the second product puts each sum into one thread: no exchange between lanes, no atomics, a fixed order.
 // Both are one kernel: "fixed" operand tiles A (M side: a thread a row of them) against a stream of tiles B.  A CTA works on
-// a pair of A tiles, eight epilogue warps each (two threads a row, 64 columns each), so that every B tile is used twice; three accumulators
-// (128 x 128 fp32) go round.  What a pair sees -- the key tiles up to its last position, the row tiles from
-// its first one on -- is cut into units of at most `seg` B tiles, dealt to the persistent CTAs longest first, in
-// alternating direction.
-//
-// A's operand comes from TMEM: a product of 128 x 128 x 16 reads 4 KB of shared memory then instead of 8, and takes 67 cycles
-// instead of 130.  The epilogue warps bring the next unit's A tiles there, each its row, as soon as the last product with the
-// one before has retired, and only then turn to that product's sums: the tensor pipe does not wait for the change.
+// a pair of A tiles, eight epilogue warps each (two threads a row, 64 columns each), so that every B tile is used twice; and the accumulators
+// (128 x 128 fp32) are double-buffered per A tile and fill TMEM.  What a pair sees -- the key tiles up to its last position, the row tiles from
+// its first one on -- is cut into units of at most `seg` B tiles, which persistent CTAs take one by one, longest first.
 //
 // Query rows of a KV head are tiled as tokens x heads of the group (a 5-D map), so a tile of 128 rows is 128 / group tokens:
 // few tokens of many heads fill a tile, and little of a tile lies beyond the diagonal.
@@ -32,6 +27,7 @@ struct ScoreArgs {
   int row_tiles, key_tiles;          // per (sequence, KV head)
   int segs, seg;                     // units per pair, B tiles of a unit at most
   int units;                         // pairs * batch * heads * segs
+  uint32_t* next_unit;               // counter, 0 before, from which the CTAs take their units behind the first
   float scale_log2;                  // scale log2(e)
   float log2_of_ln, ln_of_log2;      // from natural log sums to L and back: log2(e) times what rounding made of scale_log2
   float2* stats;                     // rows: [segs][2][batch * heads][row_tiles][128] maximum (log2 units), sum
@@ -43,16 +39,16 @@ struct ScoreArgs {
 };
 
 constexpr int kScoreThreads = 576;                         // TMA, MMA, 2 x 8 epilogue warps
-constexpr int kScoreRing = 4;
-constexpr int kScoreA = 0;                                 // a pair of A tiles on its way to TMEM
-constexpr int kScoreB = 2 * kSlotBytes;
+constexpr int kScoreRing = 3;
+constexpr int kScoreA = 0;                                 // two pairs of A tiles
+constexpr int kScoreB = 4 * kSlotBytes;
 constexpr int kScoreLog = kScoreB + kScoreRing * kSlotBytes;          // -L of the row tile in each B slot
 constexpr int kScoreBar = kScoreLog + kScoreRing * 512;
 constexpr int kScoreDynamic = kScoreBar + 256 + 1024;
-constexpr int kScoreTmemCols = 512;                        // three accumulators of 128 columns, then A tile g at 384 + 64 g
-constexpr uint32_t kScoreTmemA = 384, kScoreBufs = 3;
+constexpr int kScoreTmemCols = 512;                        // S of A tile g, buffer u at 128 (2 g + u)
+constexpr int kScoreUnits = 3;                             // units told ahead
 constexpr float kScoreSlack = 8.f;
-constexpr int kScorePoly = 2;                              // of 8 pairs of exponentials, how many the FMA pipe takes
+constexpr int kScorePoly = 1;                              // of 8 pairs of exponentials, how many the FMA pipe takes
 
 // The live query tokens of a sequence and where they stand.
 struct ScoreSeq {
@@ -93,24 +89,6 @@ struct ScoreUnit {
   }
 };
 
-// The units of a CTA in turn, those without steps passed over: the deal changes direction every round.
-template <bool COLS>
-struct ScoreDeal {
-  int64_t at;                                              // unit, or beyond the last
-  int k;
-  __device__ __forceinline__ void next(const ScoreArgs& a, ScoreUnit<COLS>& u) {
-    for (;; ++k) {
-      const int G = (int)gridDim.x, c = (int)blockIdx.x;
-      at = (int64_t)k * G + ((k & 1) ? G - 1 - c : c);
-      if (at >= a.units) return;
-      u = ScoreUnit<COLS>(a, (int)at);
-      if (u.steps > 0) break;
-    }
-    ++k;
-  }
-  __device__ __forceinline__ bool more(const ScoreArgs& a) const { return at < a.units; }
-};
-
 // map_q: 5-D (channel, head of the group, token, KV head, sequence), boxes of 64 x group x tokens; map_k: tiles of 128 rows.
 template <bool COLS>
 __global__ void __launch_bounds__(kScoreThreads, 1)
@@ -119,34 +97,37 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
   const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
   unsigned char* base_ptr = smem_dyn + (base - smem_u32(smem_dyn));
   const uint32_t bar0 = base + kScoreBar;
-  auto a_full = [&](uint32_t g) { return bar0 + 8u * g; };             // in shared memory
-  auto a_empty = [&](uint32_t g) { return bar0 + 16u + 8u * g; };
-  auto a_ready = [&](uint32_t g) { return bar0 + 32u + 8u * g; };      // in TMEM
-  auto s_full = [&](uint32_t u) { return bar0 + 48u + 8u * u; };
-  auto s_empty = [&](uint32_t u) { return bar0 + 48u + 8u * (kScoreBufs + u); };
-  const uint32_t bbar = bar0 + 48u + 16u * kScoreBufs;
-  auto b_full = [&](uint32_t s) { return bbar + 8u * s; };
-  auto b_empty = [&](uint32_t s) { return bbar + 8u * (kScoreRing + s); };
-  constexpr int kBars = 48 + 16 * (int)kScoreBufs + 16 * kScoreRing;
+  auto a_full = [&](uint32_t s) { return bar0 + 8u * s; };
+  auto a_empty = [&](uint32_t s) { return bar0 + 16u + 8u * s; };
+  auto s_full = [&](uint32_t g, uint32_t u) { return bar0 + 32u + 16u * g + 8u * u; };
+  auto s_empty = [&](uint32_t g, uint32_t u) { return bar0 + 64u + 16u * g + 8u * u; };
+  auto b_full = [&](uint32_t s) { return bar0 + 96u + 8u * s; };
+  auto b_empty = [&](uint32_t s) { return bar0 + 96u + 8u * (kScoreRing + s); };
+  constexpr int kBars = 96 + 16 * kScoreRing;
   const uint32_t drain_bar = bar0 + kBars;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(base_ptr + kScoreBar + kBars + 8);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
-  static_assert(kBars + 16 <= 256, "barriers fit");
+  auto i_full = [&](uint32_t e) { return bar0 + kBars + 16u + 8u * e; };
+  auto i_empty = [&](uint32_t e) { return bar0 + kBars + 16u + 8u * (kScoreUnits + e); };
+  volatile int* unit_ring = reinterpret_cast<volatile int*>(base_ptr + kScoreBar + kBars + 16 + 16 * kScoreUnits);
+  static_assert(kBars + 16 + 20 * kScoreUnits <= 256, "barriers fit");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rows_used = a.tokens * a.group;                // of a row tile
 
   if (tid == 0) {
-    for (int g = 0; g < 2; ++g) { mbar_init(a_full(g), 1); mbar_init(a_empty(g), 8); mbar_init(a_ready(g), 8); }
+    for (int k = 0; k < 2; ++k) { mbar_init(a_full(k), 1); mbar_init(a_empty(k), 1); }
     // (columns: the sixteen epilogue warps read the row tile's L beside the product)
     for (int s = 0; s < kScoreRing; ++s) { mbar_init(b_full(s), 1); mbar_init(b_empty(s), COLS ? 17 : 1); }
-    for (uint32_t u = 0; u < kScoreBufs; ++u) { mbar_init(s_full(u), 1); mbar_init(s_empty(u), 8); }
+    for (int g = 0; g < 2; ++g)
+      for (int k = 0; k < 2; ++k) { mbar_init(s_full(g, k), 1); mbar_init(s_empty(g, k), 8); }
+    for (int e = 0; e < kScoreUnits; ++e) { mbar_init(i_full(e), 1); mbar_init(i_empty(e), 17); }
     mbar_init(drain_bar, 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   // rows of a query tile that no copy ever fills: zeros
   if (rows_used < kTileRows) {
-    const int slots = COLS ? kScoreRing : 2, from = COLS ? kScoreB : kScoreA, dead = (kTileRows - rows_used) * 8;
+    const int slots = COLS ? kScoreRing : 4, from = COLS ? kScoreB : kScoreA, dead = (kTileRows - rows_used) * 8;
     for (int x = tid; x < slots * 2 * dead; x += kScoreThreads) {
       const int half = x / dead, y = x % dead;             // half tiles lie kHalfBytes apart
       *reinterpret_cast<uint4*>(base_ptr + from + half * kHalfBytes + rows_used * 128 + y * 16) = make_uint4(0u, 0u, 0u, 0u);
@@ -166,9 +147,19 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");       // L comes from the kernel before
 
+  // The producer takes units from the counter, longest first, and tells the others one ahead; -1: no more.  (Which CTA takes
+  // which changes no result.)  A fixed deal in alternating direction left SMs idle a tenth of the time.
   ScoreUnit<COLS> u(a, 0);
-  ScoreDeal<COLS> deal{0, 0};
-  deal.next(a, u);
+  uint32_t told = 0;                                       // units heard of
+  auto next_unit = [&](bool& ok) {                         // for the warps that listen
+    const uint32_t e = told % kScoreUnits;
+    ok = __all_sync(0xffffffffu, mbar_wait(i_full(e), (told / kScoreUnits) & 1u, abort_flag, a.status, a.wait_ns) && ok);
+    const int unit = ok ? unit_ring[e] : -1;
+    __syncwarp();
+    if (elect_one()) mbar_arrive(i_empty(e));
+    ++told;
+    return unit;
+  };
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
     if (lane == 0) {
@@ -176,7 +167,7 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(keep));
       const uint32_t q_bytes = (uint32_t)rows_used * 256u;
       bool ok = true;
-      uint32_t it = 0, tiles[2] = {0, 0};
+      uint32_t it = 0, pairs = 0;
       auto wait = [&](uint32_t bar, uint32_t parity) { return ok = ok && mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns); };
       auto load = [&](bool queries, uint32_t dst, uint32_t bar, int tile) {
         if (queries) {
@@ -187,13 +178,30 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
           tma_load_4d(dst + kHalfBytes, &map_k, bar, 64, tile * kTileRows, u.h, u.b, keep);
         }
       };
-      for (; ok && deal.more(a); deal.next(a, u)) {
-        for (int g = 0; g < u.count; ++g) {
-          if (!wait(a_empty(g), (tiles[g] & 1u) ^ 1u)) break;
-          ++tiles[g];
-          mbar_arrive_expect_tx(a_full(g), COLS ? (uint32_t)kSlotBytes : q_bytes);
-          load(!COLS, base + kScoreA + g * kSlotBytes, a_full(g), u.a0 + g);
+      int taken = 0;
+      auto take = [&]() {                                  // the next unit that has steps, told to the others
+        int unit;
+        do {
+          const int64_t at = taken++ == 0 ? (int64_t)blockIdx.x
+                                          : a.units > (int)gridDim.x ? (int64_t)gridDim.x + atomicAdd(a.next_unit, 1u) : (int64_t)a.units;
+          unit = at < a.units ? (int)at : -1;
+        } while (unit >= 0 && ScoreUnit<COLS>(a, unit).steps == 0);
+        const uint32_t e = told % kScoreUnits;
+        if (wait(i_empty(e), ((told / kScoreUnits) & 1u) ^ 1u)) {
+          unit_ring[e] = unit;
+          mbar_arrive(i_full(e));
         }
+        ++told;
+        return unit;
+      };
+      int unit = take(), then = unit >= 0 ? take() : -1;
+      for (; ok && unit >= 0; unit = then, then = then >= 0 ? take() : -1) {
+        u = ScoreUnit<COLS>(a, unit);
+        const uint32_t pair = pairs & 1u;
+        if (!wait(a_empty(pair), ((pairs >> 1) & 1u) ^ 1u)) break;
+        ++pairs;
+        mbar_arrive_expect_tx(a_full(pair), (uint32_t)u.count * (COLS ? (uint32_t)kSlotBytes : q_bytes));
+        for (int g = 0; g < u.count; ++g) load(!COLS, base + kScoreA + (2 * pair + g) * kSlotBytes, a_full(pair), u.a0 + g);
         for (int x = 0; ok && x < u.steps; ++x) {
           const uint32_t slot = it % kScoreRing;
           if (!wait(b_empty(slot), ((it / kScoreRing) & 1u) ^ 1u)) break;
@@ -211,47 +219,48 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
           while (!mbar_try_wait(bar, parity) && global_ns() - t0 < a.wait_ns) {}
         };
         for (uint32_t x = it - min(it, (uint32_t)kScoreRing); x < it; ++x) land(b_full(x % kScoreRing), (x / kScoreRing) & 1u);
-        for (int g = 0; g < 2; ++g)
-          if (tiles[g] > 0) land(a_full(g), (tiles[g] - 1) & 1u);
+        for (uint32_t x = pairs - min(pairs, 2u); x < pairs; ++x) land(a_full(x & 1u), (x >> 1) & 1u);
       }
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ products: the whole warp waits, one lane issues
     constexpr uint32_t idesc = instr_desc_bf16(kTileRows);
-    const uint64_t b_desc0 = smem_desc_sw128(base + kScoreB);
+    const uint64_t a_desc0 = smem_desc_sw128(base + kScoreA), b_desc0 = smem_desc_sw128(base + kScoreB);
     bool ok = true;
-    uint32_t it = 0, done = 0, tiles[2] = {0, 0};          // B tiles, products, A tiles
+    uint32_t it = 0, pairs = 0, done[2] = {0, 0};          // B tiles, pairs of A tiles, products of each group
     auto wait = [&](uint32_t bar, uint32_t parity) { ok = mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns) && ok; };
-    for (; ok && deal.more(a); deal.next(a, u)) {
+    for (int unit = next_unit(ok); ok && unit >= 0; unit = next_unit(ok)) {
+      u = ScoreUnit<COLS>(a, unit);
+      const uint32_t pair = pairs & 1u;
+      wait(a_full(pair), (pairs >> 1) & 1u);
+      ++pairs;
       for (int x = 0; ok && x < u.steps; ++x, ++it) {
         const uint32_t slot = it % kScoreRing;
         wait(b_full(slot), (it / kScoreRing) & 1u);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           if (g >= u.count || !ok) continue;
-          if (x == 0) {
-            wait(a_ready(g), tiles[g] & 1u);
-            ++tiles[g];
-          }
-          const uint32_t buf = done % kScoreBufs;
-          wait(s_empty(buf), ((done / kScoreBufs) & 1u) ^ 1u);
-          ++done;
+          const uint32_t buf = done[g] & 1u;
+          wait(s_empty(g, buf), ((done[g] >> 1) & 1u) ^ 1u);
+          ++done[g];
           if (!(ok = __all_sync(0xffffffffu, ok))) continue;
           tc_fence_after();
-          const uint64_t bd = b_desc0 + slot * (kSlotBytes >> 4);
+          const uint64_t ad = a_desc0 + (2 * pair + g) * (kSlotBytes >> 4), bd = b_desc0 + slot * (kSlotBytes >> 4);
           if (elect_one()) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const uint32_t off = (uint32_t)(e >> 2) * (kHalfBytes >> 4) + (uint32_t)(e & 3) * 2u;
-              tc_mma_bf16_ts(tmem_base + 128u * buf, tmem_base + kScoreTmemA + 64u * g + 8u * e, bd + off, idesc, e > 0);
+              tc_mma_bf16(tmem_base + 128u * (2 * g + buf), ad + off, bd + off, idesc, e > 0);
             }
-            tc_commit(s_full(buf));
+            tc_commit(s_full(g, buf));
           }
           __syncwarp();
         }
         if (ok && elect_one()) tc_commit(b_empty(slot));
         __syncwarp();
       }
+      if (ok && elect_one()) tc_commit(a_empty(pair));
+      __syncwarp();
     }
     if (!ok) {
       if (elect_one()) tc_commit(drain_bar);
@@ -267,52 +276,27 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     const uint64_t sc2 = pack2(sc, sc);
     const int P = a.batch * a.heads;
     bool ok = true;
-    uint32_t it = 0, done = 0, tiles = 0;                  // B tiles, products before this step, this group's A tiles
-    // Brings A tile g of the unit `v` into TMEM (this thread: 64 channels of row r).  The products with the one before have
-    // all retired.
-    auto stage = [&](const ScoreUnit<COLS>& v) {
-      if (g >= v.count) return;
-      ok = mbar_wait(a_full(g), tiles & 1u, abort_flag, a.status, a.wait_ns) && ok;
-      if (!(ok = __all_sync(0xffffffffu, ok))) return;
-      ++tiles;
-      float w[32];
-      const unsigned char* src = base_ptr + kScoreA + g * kSlotBytes + half * kHalfBytes + r * 128;
-#pragma unroll
-      for (int c = 0; c < 8; ++c) *reinterpret_cast<float4*>(w + 4 * c) = *reinterpret_cast<const float4*>(src + ((c ^ (r & 7)) * 16));
-      tmem_st32(lane_addr + kScoreTmemA + 64u * g + 32u * half, w);
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (elect_one()) {
-        mbar_arrive(a_ready(g));
-        mbar_arrive(a_empty(g));
-      }
-      __syncwarp();
-    };
-    if (deal.more(a)) stage(u);
-    while (ok && deal.more(a)) {
+    uint32_t it = 0, done = 0;                             // B tiles, this group's products
+    for (int unit = next_unit(ok); ok && unit >= 0; unit = next_unit(ok)) {
+      u = ScoreUnit<COLS>(a, unit);
       const ScoreSeq seq(a, u.b);
       const bool mine = g < u.count;
-      ScoreUnit<COLS> then = u;
-      deal.next(a, then);
       float top = -INFINITY, sum = 0.f, lost = 0.f;
       const int key = (u.a0 + g) * kTileRows + r;          // columns
       const int tok = (u.a0 + g) * a.tokens + r / a.group; // rows
       const int pos = !COLS && r < rows_used && tok < seq.q ? seq.pos0 + tok : -1;           // keys up to here
       for (int x = 0; x < u.steps; ++x, ++it) {
-        // A group without a tile waits for the other's product, so that it stays less than a round of the accumulators behind
-        // or ahead (a barrier tells only two rounds apart), and its arrivals below mean what they say.
-        const uint32_t product = done + (mine ? g : 0), slot = it % kScoreRing, buf = product % kScoreBufs;
-        done += u.count;
+        if (!COLS && !mine) break;
+        // (columns: L lands with the tile, and a group without an A tile keeps pace, its arrivals count)
+        const uint32_t slot = it % kScoreRing, buf = done & 1u;
         if (COLS) ok = mbar_wait(b_full(slot), (it / kScoreRing) & 1u, abort_flag, a.status, a.wait_ns);
-        ok = ok && mbar_wait(s_full(buf), (product / kScoreBufs) & 1u, abort_flag, a.status, a.wait_ns);
+        if (mine) {
+          ok = ok && mbar_wait(s_full(g, buf), (done >> 1) & 1u, abort_flag, a.status, a.wait_ns);
+          ++done;
+        }
         if (!(ok = __all_sync(0xffffffffu, ok))) break;
         tc_fence_after();
-        if (x == u.steps - 1 && deal.more(a)) {            // this group's A tile is done with
-          stage(then);
-          if (!ok) break;
-        }
-        const uint32_t s_addr = lane_addr + 128u * buf + 64u * half;
+        const uint32_t s_addr = lane_addr + 128u * (2 * g + buf) + 64u * half;
         if (COLS && mine) {
           const float4* L = reinterpret_cast<const float4*>(base_ptr + kScoreLog + slot * 512 + 256 * half);
           const int tok0 = (u.first + x) * a.tokens;
@@ -357,7 +341,7 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
           }
           tc_fence_before();
           __syncwarp();
-          if (elect_one()) mbar_arrive(s_empty(buf));
+          if (elect_one()) mbar_arrive(s_empty(g, buf));
           float p0, p1;
           unpack2(add2(add2(part[0], part[1]), add2(part[2], part[3])), p0, p1);
           // the tiles' sums are added with what their additions lose (thousands of rows may follow one another)
@@ -376,7 +360,7 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
           tmem_ld_wait();
           tc_fence_before();
           __syncwarp();
-          if (elect_one()) mbar_arrive(s_empty(buf));      // S is in registers
+          if (elect_one()) mbar_arrive(s_empty(g, buf));   // S is in registers
           const int see = pos + 1 - (u.first + x) * kTileRows - 64 * half;         // columns below this
           if (__any_sync(0xffffffffu, see < 64)) {
 #pragma unroll
@@ -418,7 +402,6 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       }
       if (!COLS && mine)
         a.stats[(((int64_t)(2 * u.seg + half) * P + u.p) * a.row_tiles + (u.a0 + g)) * kTileRows + r] = make_float2(top, sum);
-      u = then;
     }
   }
 
@@ -433,16 +416,19 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
 }
 
 // -L of every query row, from the parts of the rows pass or from log sums that the caller has; -inf where a row does not count.
-// Clears `clear` floats of `scores` beside it.  grid = batch * heads * row tiles; four threads a row take its parts in turn.
+// Clears `clear` floats of `scores` and the columns pass's counter beside it.  grid = batch * heads * row tiles, block = 128, or
+// 512 for many parts: four threads a row take them in turn.
 constexpr int kLogsumThreads = 4 * kTileRows;
 __global__ void __launch_bounds__(kLogsumThreads) score_logsum_kernel(const ScoreArgs a, const float* given, float* logsum,
-                                                                      float* lse_out, float* scores, int64_t clear) {
+                                                                      float* lse_out, float* scores, int64_t clear,
+                                                                      uint32_t* next_unit) {
   __shared__ float2 s_part[3][kTileRows];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  for (int64_t x = (int64_t)blockIdx.x * kLogsumThreads + threadIdx.x; x < clear; x += (int64_t)gridDim.x * kLogsumThreads) scores[x] = 0.f;
+  for (int64_t x = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; x < clear; x += (int64_t)gridDim.x * blockDim.x) scores[x] = 0.f;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *next_unit = 0u;
   const int tile = blockIdx.x % a.row_tiles, p = blockIdx.x / a.row_tiles, b = p / a.heads, h = p % a.heads;
-  const int r = threadIdx.x % kTileRows, sub = threadIdx.x / kTileRows;
+  const int r = threadIdx.x % kTileRows, sub = threadIdx.x / kTileRows, subs = blockDim.x / kTileRows;
   const ScoreSeq s(a, b);
   const int tok = tile * a.tokens + r / a.group;
   const bool live = r < a.tokens * a.group && tok < s.q, sees = live && s.pos0 + tok >= 0;
@@ -459,10 +445,10 @@ __global__ void __launch_bounds__(kLogsumThreads) score_logsum_kernel(const Scor
       const int used = 2 * ((((s.pos0 + end_tok) + kTileRows - 1) / kTileRows + a.seg - 1) / a.seg);
       const float2* stats = a.stats + ((int64_t)p * a.row_tiles + tile) * kTileRows + r;
       const int64_t next = (int64_t)a.batch * a.heads * a.row_tiles * kTileRows;
-      for (int g = sub; g < used; g += 16) {
+      for (int g = sub; g < used; g += 4 * subs) {
         float2 e[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) e[k] = g + 4 * k < used ? stats[(g + 4 * k) * next] : make_float2(-INFINITY, 0.f);
+        for (int k = 0; k < 4; ++k) e[k] = g + subs * k < used ? stats[(g + subs * k) * next] : make_float2(-INFINITY, 0.f);
 #pragma unroll
         for (int k = 0; k < 4; ++k) join(e[k]);
       }
@@ -478,8 +464,7 @@ __global__ void __launch_bounds__(kLogsumThreads) score_logsum_kernel(const Scor
       L = given[at] * a.log2_of_ln;
       if (L == -INFINITY) L = INFINITY;                    // (a row that saw nothing)
     } else {
-#pragma unroll
-      for (int k = 0; k < 3; ++k) join(s_part[k][r]);
+      for (int k = 0; k < subs - 1; ++k) join(s_part[k][r]);
       L = sum == 0.f ? INFINITY : top + log2f(sum);
     }
   }

@@ -17,12 +17,12 @@ struct ScoresPlan {
   size_t stats_at, logsum_at, parts_at, bytes;
 };
 
-// B tiles a unit takes: eight units a CTA, so that the last round costs little, but eight tiles each (a unit costs about one
-// beside them) while that leaves every SM one.
+// B tiles a unit takes: eight units a CTA, so that they end together, but sixteen tiles each (a unit costs about one beside
+// them) while that leaves every SM one.
 int unit_length(int64_t steps) {
   const int64_t n = sms();
   int64_t seg = (steps + 8 * n - 1) / (8 * n), each = (steps + n - 1) / n;
-  const int64_t least = each < 8 ? each : 8;
+  const int64_t least = each < 16 ? each : 16;
   if (seg < least) seg = least;
   return (int)(seg < 1 ? 1 : seg);
 }
@@ -46,7 +46,7 @@ bool plan_scores(const curdkv_desc* d, int32_t q_rows, ScoresPlan* pl) {
   pl->key_seg = unit_length(P * (whole * pl->row_tiles + (key_pairs - whole) * (pl->row_tiles + 1) / 2));
   pl->key_segs = (pl->row_tiles + pl->key_seg - 1) / pl->key_seg;
   const size_t rows = (size_t)P * pl->row_tiles * kTileRows;
-  pl->stats_at = 256;
+  pl->stats_at = 512;                                      // (status word, and at 256 the two passes' counters)
   pl->logsum_at = pl->stats_at + round256(rows * pl->row_segs * 2 * sizeof(float2));
   pl->parts_at = pl->logsum_at + round256(rows * sizeof(float));
   pl->bytes = pl->parts_at + (pl->key_segs > 1 ? round256((size_t)P * pl->key_segs * 2 * d->n_max * sizeof(float)) : 0);
@@ -131,13 +131,15 @@ curdkv_status curdkv_attention_scores(const void* Q, int32_t q_rows, int64_t q_s
   a.status = reinterpret_cast<uint32_t*>(ws);
   float* logsum = reinterpret_cast<float*>(ws + pl.logsum_at);
   a.logsum = logsum;
+  a.next_unit = reinterpret_cast<uint32_t*>(ws + 256);
   a.segs = pl.row_segs;
   a.seg = pl.row_seg;
   a.units = (int)(P * ((pl.row_tiles + 1) / 2) * pl.row_segs);
+  const int logsum_threads = !lse_given && pl.row_segs > 4 ? umma::kLogsumThreads : kTileRows;
   if (d.n_max == 0) {                                      // no scores; a query that sees nothing has a log sum all the same
     if (lse == nullptr || lse_given) return CURDKV_OK;
-    return launch(umma::score_logsum_kernel, P * pl.row_tiles, umma::kLogsumThreads, 0, false, stream, a, (const float*)nullptr, logsum, lse,
-                  scores, (int64_t)0)
+    return launch(umma::score_logsum_kernel, P * pl.row_tiles, logsum_threads, 0, false, stream, a, (const float*)nullptr, logsum, lse,
+                  scores, (int64_t)0, reinterpret_cast<uint32_t*>(ws + 256) + 1)
                ? CURDKV_OK : CURDKV_ERR_CUDA;
   }
   if (!bf16_map(&mq, Q, 5, sizes, strides, box) ||
@@ -148,14 +150,16 @@ curdkv_status curdkv_attention_scores(const void* Q, int32_t q_rows, int64_t q_s
       !allow_smem(umma::score_attention_kernel<true>, umma::kScoreDynamic, cols_done))
     return CURDKV_ERR_CUDA;
   const int64_t places = sms();
+  if (!lse_given && a.units > places && cudaMemsetAsync(a.next_unit, 0, sizeof(uint32_t), stream) != cudaSuccess) return CURDKV_ERR_CUDA;
   if (!lse_given &&
       !launch(umma::score_attention_kernel<false>, a.units < places ? a.units : places, umma::kScoreThreads, umma::kScoreDynamic, false,
               stream, mq, mk, a))
     return CURDKV_ERR_CUDA;
-  if (!launch(umma::score_logsum_kernel, P * pl.row_tiles, umma::kLogsumThreads, 0, !lse_given, stream, a,
+  if (!launch(umma::score_logsum_kernel, P * pl.row_tiles, logsum_threads, 0, !lse_given, stream, a,
               (const float*)(lse_given ? lse : nullptr), logsum, lse_given ? (float*)nullptr : lse, scores,
-              pl.key_segs > 1 ? (int64_t)0 : P * d.n_max))
+              pl.key_segs > 1 ? (int64_t)0 : P * d.n_max, a.next_unit + 1))
     return CURDKV_ERR_CUDA;
+  a.next_unit += 1;
   a.segs = pl.key_segs;
   a.seg = pl.key_seg;
   a.units = (int)(P * ((pl.key_tiles + 1) / 2) * pl.key_segs);
