@@ -495,7 +495,8 @@ curdkv_status curdkv_attention_scores(const void* Q, int32_t q_rows, int64_t q_s
  * kept rows, order of slots and status flags), with the new rows' scores given instead of formed with G.
  *   scores_new  fp32 [batch][kv_heads][n_max], or NULL: 0 each (rows to be kept on arrival belong in the window)
  *   desc_new    as in curdkv_cache_append; r, score_mode, raw_scores and whiten are not used
- *   workspace   curdkv_cache_workspace_bytes(batch, kv_heads, n_max, capacity, budget)
+ *   workspace   curdkv_cache_workspace_bytes(batch, kv_heads, n_max, capacity, budget), 256-byte aligned; its status word
+ *               collects (it is not cleared)
  * Requires budget >= 1 and num_sink + window <= budget.  A cache of at most 8 rows above its budget, as generation needs,
  * takes one launch (two with more than 8 heads), whose CTAs look for the rows that leave instead of sorting, and
  * leaves slots at or beyond the new count as they were; others (capacity <= 204800) run as the calls it stands for, whose
@@ -515,9 +516,9 @@ curdkv_status curdkv_cache_push(const curdkv_cache* cache, const void* K_new, co
  *   lse       NULL, or fp32 [batch][q_heads][q_rows]: log of each row's sum of exponentials
  *   weights   NULL, or fp32 [batch][kv_heads][capacity], cache->raw for instance; only held slots are changed
  *   scale     finite, >= 0
- * q_rows * (q_heads / kv_heads) <= 1024.  A query that sees nothing gives O = 0, lse = -inf and no weight.  Held rows must be
- * finite.  Softmax and sums in fp32, weights added in a fixed order; a weight is rounded to bf16 before it multiplies the
- * values, O is rounded once.  Two launches.  Workspace (256-byte aligned): its status word collects (it is not cleared)
+ * q_rows * (q_heads / kv_heads) <= 1024.  A query that sees nothing gives O = 0, lse = -inf and no weight.  Held rows and live
+ * queries must be finite.  Softmax and sums in fp32, weights added in a fixed order; a weight is rounded to bf16 before it multiplies the
+ * values, O is rounded once.  One launch, or two.  Workspace (256-byte aligned): its status word collects (it is not cleared)
  * CURDKV_DEV_BAD_INDEX, a count out of range; two calls that may overlap need a workspace each. */
 size_t curdkv_cache_attention_workspace_bytes(const curdkv_cache* cache, const curdkv_desc* desc, int32_t q_rows);
 curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_n,

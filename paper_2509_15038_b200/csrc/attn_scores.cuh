@@ -39,12 +39,17 @@ struct ScoreArgs {
 };
 
 constexpr int kScoreThreads = 576;                         // TMA, MMA, 2 x 8 epilogue warps
-constexpr int kScoreRing = 3;
-constexpr int kScoreA = 0;                                 // two pairs of A tiles
-constexpr int kScoreB = 4 * kSlotBytes;
-constexpr int kScoreLog = kScoreB + kScoreRing * kSlotBytes;          // -L of the row tile in each B slot
-constexpr int kScoreBar = kScoreLog + kScoreRing * 512;
-constexpr int kScoreDynamic = kScoreBar + 256 + 1024;
+// Seven tiles of shared memory: where the stream B is the keys, out of device memory, it gets five (a pair of A tiles is there
+// for many of them then), where B is the queries, two pairs of A tiles (keys, two steps a pair when only a prompt's last
+// tokens ask).
+template <bool COLS>
+struct ScoreSmem {
+  static constexpr int kPairs = COLS ? 2 : 1, kRing = 7 - 2 * kPairs;
+  static constexpr int kA = 0, kB = 2 * kPairs * kSlotBytes;
+};
+constexpr int kScoreLog = 7 * kSlotBytes;                  // columns: -L of the row tile in each B slot
+constexpr int kScoreBar = kScoreLog + 3 * 512;
+constexpr int kScoreDynamic = kScoreBar + 512 + 1024;
 constexpr int kScoreTmemCols = 512;                        // S of A tile g, buffer u at 128 (2 g + u)
 constexpr int kScoreUnits = 3;                             // units told ahead
 constexpr float kScoreSlack = 8.f;
@@ -53,6 +58,7 @@ constexpr int kScorePoly = 1;                              // of 8 pairs of expo
 // The live query tokens of a sequence and where they stand.
 struct ScoreSeq {
   int n, q, pos0;                                          // rows, tokens, position of token 0
+  __device__ __forceinline__ ScoreSeq() {}
   __device__ __forceinline__ ScoreSeq(const ScoreArgs& a, int b) {
     n = seq_len_of(a.seqlens, b, a.n_max);
     q = a.q_lens != nullptr ? min(max(a.q_lens[b], 0), a.q_rows) : a.q_rows;
@@ -64,6 +70,7 @@ struct ScoreSeq {
 template <bool COLS>
 struct ScoreUnit {
   int p, b, h, seg, a0, count, first, steps;               // A tiles a0 .. a0 + count - 1; B tiles first .. first + steps - 1
+  __device__ __forceinline__ ScoreUnit() {}
   __device__ __forceinline__ ScoreUnit(const ScoreArgs& a, int unit) {
     const int tiles = COLS ? a.key_tiles : a.row_tiles, P = a.batch * a.heads, pairs = (tiles + 1) / 2;
     seg = unit % a.segs;
@@ -96,28 +103,29 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
   extern __shared__ unsigned char smem_dyn[];
   const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
   unsigned char* base_ptr = smem_dyn + (base - smem_u32(smem_dyn));
+  constexpr int kRing = ScoreSmem<COLS>::kRing, kPairs = ScoreSmem<COLS>::kPairs;
   const uint32_t bar0 = base + kScoreBar;
   auto a_full = [&](uint32_t s) { return bar0 + 8u * s; };
   auto a_empty = [&](uint32_t s) { return bar0 + 16u + 8u * s; };
   auto s_full = [&](uint32_t g, uint32_t u) { return bar0 + 32u + 16u * g + 8u * u; };
   auto s_empty = [&](uint32_t g, uint32_t u) { return bar0 + 64u + 16u * g + 8u * u; };
   auto b_full = [&](uint32_t s) { return bar0 + 96u + 8u * s; };
-  auto b_empty = [&](uint32_t s) { return bar0 + 96u + 8u * (kScoreRing + s); };
-  constexpr int kBars = 96 + 16 * kScoreRing;
+  auto b_empty = [&](uint32_t s) { return bar0 + 96u + 8u * (kRing + s); };
+  constexpr int kBars = 96 + 16 * kRing;
   const uint32_t drain_bar = bar0 + kBars;
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(base_ptr + kScoreBar + kBars + 8);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
   auto i_full = [&](uint32_t e) { return bar0 + kBars + 16u + 8u * e; };
   auto i_empty = [&](uint32_t e) { return bar0 + kBars + 16u + 8u * (kScoreUnits + e); };
-  volatile int* unit_ring = reinterpret_cast<volatile int*>(base_ptr + kScoreBar + kBars + 16 + 16 * kScoreUnits);
-  static_assert(kBars + 16 + 20 * kScoreUnits <= 256, "barriers fit");
+  int4* unit_ring = reinterpret_cast<int4*>(base_ptr + kScoreBar + 256);         // [kScoreUnits][3]
+  static_assert(kBars + 16 + 16 * kScoreUnits <= 256 && 48 * kScoreUnits <= 256, "barriers and units fit");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rows_used = a.tokens * a.group;                // of a row tile
 
   if (tid == 0) {
-    for (int k = 0; k < 2; ++k) { mbar_init(a_full(k), 1); mbar_init(a_empty(k), 1); }
+    for (int k = 0; k < kPairs; ++k) { mbar_init(a_full(k), 1); mbar_init(a_empty(k), 1); }
     // (columns: the sixteen epilogue warps read the row tile's L beside the product)
-    for (int s = 0; s < kScoreRing; ++s) { mbar_init(b_full(s), 1); mbar_init(b_empty(s), COLS ? 17 : 1); }
+    for (int s = 0; s < kRing; ++s) { mbar_init(b_full(s), 1); mbar_init(b_empty(s), COLS ? 17 : 1); }
     for (int g = 0; g < 2; ++g)
       for (int k = 0; k < 2; ++k) { mbar_init(s_full(g, k), 1); mbar_init(s_empty(g, k), 8); }
     for (int e = 0; e < kScoreUnits; ++e) { mbar_init(i_full(e), 1); mbar_init(i_empty(e), 17); }
@@ -127,7 +135,7 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
   }
   // rows of a query tile that no copy ever fills: zeros
   if (rows_used < kTileRows) {
-    const int slots = COLS ? kScoreRing : 4, from = COLS ? kScoreB : kScoreA, dead = (kTileRows - rows_used) * 8;
+    const int slots = COLS ? kRing : 2 * kPairs, from = COLS ? ScoreSmem<COLS>::kB : ScoreSmem<COLS>::kA, dead = (kTileRows - rows_used) * 8;
     for (int x = tid; x < slots * 2 * dead; x += kScoreThreads) {
       const int half = x / dead, y = x % dead;             // half tiles lie kHalfBytes apart
       *reinterpret_cast<uint4*>(base_ptr + from + half * kHalfBytes + rows_used * 128 + y * 16) = make_uint4(0u, 0u, 0u, 0u);
@@ -147,18 +155,21 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");       // L comes from the kernel before
 
-  // The producer takes units from the counter, longest first, and tells the others one ahead; -1: no more.  (Which CTA takes
+  // The producer takes units from the counter, longest first, and tells the others one ahead; one without steps: no more.  (Which CTA takes
   // which changes no result.)  A fixed deal in alternating direction left SMs idle a tenth of the time.
-  ScoreUnit<COLS> u(a, 0);
   uint32_t told = 0;                                       // units heard of
-  auto next_unit = [&](bool& ok) {                         // for the warps that listen
+  auto next_unit = [&](ScoreUnit<COLS>& u, ScoreSeq& seq, bool& ok) {        // for the warps that listen
     const uint32_t e = told % kScoreUnits;
     ok = __all_sync(0xffffffffu, mbar_wait(i_full(e), (told / kScoreUnits) & 1u, abort_flag, a.status, a.wait_ns) && ok);
-    const int unit = ok ? unit_ring[e] : -1;
+    if (!ok) return false;
+    const int4 x = unit_ring[3 * e], y = unit_ring[3 * e + 1], z = unit_ring[3 * e + 2];
     __syncwarp();
     if (elect_one()) mbar_arrive(i_empty(e));
     ++told;
-    return unit;
+    u.p = x.x; u.b = x.y; u.h = x.z; u.seg = x.w;
+    u.a0 = y.x; u.count = y.y; u.first = y.z; u.steps = y.w;
+    seq.n = z.x; seq.q = z.y; seq.pos0 = z.z;
+    return u.steps > 0;
   };
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer
@@ -169,7 +180,7 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       bool ok = true;
       uint32_t it = 0, pairs = 0;
       auto wait = [&](uint32_t bar, uint32_t parity) { return ok = ok && mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns); };
-      auto load = [&](bool queries, uint32_t dst, uint32_t bar, int tile) {
+      auto load = [&](const ScoreUnit<COLS>& u, bool queries, uint32_t dst, uint32_t bar, int tile) {
         if (queries) {
           tma_load_5d(dst, &map_q, bar, 0, 0, tile * a.tokens, u.h, u.b);
           tma_load_5d(dst + kHalfBytes, &map_q, bar, 64, 0, tile * a.tokens, u.h, u.b);
@@ -178,65 +189,78 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
           tma_load_4d(dst + kHalfBytes, &map_k, bar, 64, tile * kTileRows, u.h, u.b, keep);
         }
       };
-      int taken = 0;
-      auto take = [&]() {                                  // the next unit that has steps, told to the others
-        int unit;
+      // (of very many units, of which short sequences leave many without steps, several are taken at a time)
+      const int64_t batch = min(max(a.units / (32 * (int)gridDim.x), 1), 16);
+      int64_t at = blockIdx.x, last = at + 1;              // units taken
+      auto take = [&](ScoreUnit<COLS>& u) {                // the next unit that has steps, told to the others
         do {
-          const int64_t at = taken++ == 0 ? (int64_t)blockIdx.x
-                                          : a.units > (int)gridDim.x ? (int64_t)gridDim.x + atomicAdd(a.next_unit, 1u) : (int64_t)a.units;
-          unit = at < a.units ? (int)at : -1;
-        } while (unit >= 0 && ScoreUnit<COLS>(a, unit).steps == 0);
+          if (at == last) {
+            at = a.units > (int)gridDim.x ? (int64_t)gridDim.x + batch * atomicAdd(a.next_unit, 1u) : (int64_t)a.units;
+            last = at + batch;
+          }
+          if (at >= a.units) {
+            u.steps = 0;
+            break;
+          }
+          u = ScoreUnit<COLS>(a, (int)at++);
+        } while (u.steps == 0);
         const uint32_t e = told % kScoreUnits;
         if (wait(i_empty(e), ((told / kScoreUnits) & 1u) ^ 1u)) {
-          unit_ring[e] = unit;
+          const ScoreSeq seq(a, u.b);
+          unit_ring[3 * e] = make_int4(u.p, u.b, u.h, u.seg);
+          unit_ring[3 * e + 1] = make_int4(u.a0, u.count, u.first, u.steps);
+          unit_ring[3 * e + 2] = make_int4(seq.n, seq.q, seq.pos0, 0);
           mbar_arrive(i_full(e));
         }
         ++told;
-        return unit;
       };
-      int unit = take(), then = unit >= 0 ? take() : -1;
-      for (; ok && unit >= 0; unit = then, then = then >= 0 ? take() : -1) {
-        u = ScoreUnit<COLS>(a, unit);
-        const uint32_t pair = pairs & 1u;
-        if (!wait(a_empty(pair), ((pairs >> 1) & 1u) ^ 1u)) break;
+      ScoreUnit<COLS> u(a, 0), then(a, 0);
+      take(u);
+      if (u.steps > 0) take(then);
+      while (ok && u.steps > 0) {
+        const uint32_t pair = pairs % kPairs;
+        if (!wait(a_empty(pair), ((pairs / kPairs) & 1u) ^ 1u)) break;
         ++pairs;
         mbar_arrive_expect_tx(a_full(pair), (uint32_t)u.count * (COLS ? (uint32_t)kSlotBytes : q_bytes));
-        for (int g = 0; g < u.count; ++g) load(!COLS, base + kScoreA + (2 * pair + g) * kSlotBytes, a_full(pair), u.a0 + g);
+        for (int g = 0; g < u.count; ++g) load(u, !COLS, base + ScoreSmem<COLS>::kA + (2 * pair + g) * kSlotBytes, a_full(pair), u.a0 + g);
         for (int x = 0; ok && x < u.steps; ++x) {
-          const uint32_t slot = it % kScoreRing;
-          if (!wait(b_empty(slot), ((it / kScoreRing) & 1u) ^ 1u)) break;
+          const uint32_t slot = it % kRing;
+          if (!wait(b_empty(slot), ((it / kRing) & 1u) ^ 1u)) break;
           ++it;
           const int tile = u.first + x;
           mbar_arrive_expect_tx(b_full(slot), COLS ? q_bytes + 512u : (uint32_t)kSlotBytes);
-          load(COLS, base + kScoreB + slot * kSlotBytes, b_full(slot), tile);
+          load(u, COLS, base + ScoreSmem<COLS>::kB + slot * kSlotBytes, b_full(slot), tile);
           if (COLS)
             bulk_load(base + kScoreLog + slot * 512, a.logsum + ((int64_t)u.p * a.row_tiles + tile) * kTileRows, 512u, b_full(slot));
         }
+        u = then;
+        if (u.steps > 0) take(then);                       // (behind the last unit `then` stays as it is)
       }
       if (!ok) {                                           // let what was issued land before the CTA ends
         auto land = [&](uint32_t bar, uint32_t parity) {
           const unsigned long long t0 = global_ns();
           while (!mbar_try_wait(bar, parity) && global_ns() - t0 < a.wait_ns) {}
         };
-        for (uint32_t x = it - min(it, (uint32_t)kScoreRing); x < it; ++x) land(b_full(x % kScoreRing), (x / kScoreRing) & 1u);
-        for (uint32_t x = pairs - min(pairs, 2u); x < pairs; ++x) land(a_full(x & 1u), (x >> 1) & 1u);
+        for (uint32_t x = it - min(it, (uint32_t)kRing); x < it; ++x) land(b_full(x % kRing), (x / kRing) & 1u);
+        for (uint32_t x = pairs - min(pairs, (uint32_t)kPairs); x < pairs; ++x) land(a_full(x % kPairs), (x / kPairs) & 1u);
       }
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------ products: the whole warp waits, one lane issues
     constexpr uint32_t idesc = instr_desc_bf16(kTileRows);
-    const uint64_t a_desc0 = smem_desc_sw128(base + kScoreA), b_desc0 = smem_desc_sw128(base + kScoreB);
+    const uint64_t a_desc0 = smem_desc_sw128(base + ScoreSmem<COLS>::kA), b_desc0 = smem_desc_sw128(base + ScoreSmem<COLS>::kB);
     bool ok = true;
     uint32_t it = 0, pairs = 0, done[2] = {0, 0};          // B tiles, pairs of A tiles, products of each group
     auto wait = [&](uint32_t bar, uint32_t parity) { ok = mbar_wait(bar, parity, abort_flag, a.status, a.wait_ns) && ok; };
-    for (int unit = next_unit(ok); ok && unit >= 0; unit = next_unit(ok)) {
-      u = ScoreUnit<COLS>(a, unit);
-      const uint32_t pair = pairs & 1u;
-      wait(a_full(pair), (pairs >> 1) & 1u);
+    ScoreUnit<COLS> u;
+    ScoreSeq seq;
+    while (next_unit(u, seq, ok)) {
+      const uint32_t pair = pairs % kPairs;
+      wait(a_full(pair), (pairs / kPairs) & 1u);
       ++pairs;
       for (int x = 0; ok && x < u.steps; ++x, ++it) {
-        const uint32_t slot = it % kScoreRing;
-        wait(b_full(slot), (it / kScoreRing) & 1u);
+        const uint32_t slot = it % kRing;
+        wait(b_full(slot), (it / kRing) & 1u);
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
           if (g >= u.count || !ok) continue;
@@ -277,9 +301,9 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     const int P = a.batch * a.heads;
     bool ok = true;
     uint32_t it = 0, done = 0;                             // B tiles, this group's products
-    for (int unit = next_unit(ok); ok && unit >= 0; unit = next_unit(ok)) {
-      u = ScoreUnit<COLS>(a, unit);
-      const ScoreSeq seq(a, u.b);
+    ScoreUnit<COLS> u;
+    ScoreSeq seq;
+    while (next_unit(u, seq, ok)) {
       const bool mine = g < u.count;
       float top = -INFINITY, sum = 0.f, lost = 0.f;
       const int key = (u.a0 + g) * kTileRows + r;          // columns
@@ -288,8 +312,8 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       for (int x = 0; x < u.steps; ++x, ++it) {
         if (!COLS && !mine) break;
         // (columns: L lands with the tile, and a group without an A tile keeps pace, its arrivals count)
-        const uint32_t slot = it % kScoreRing, buf = done & 1u;
-        if (COLS) ok = mbar_wait(b_full(slot), (it / kScoreRing) & 1u, abort_flag, a.status, a.wait_ns);
+        const uint32_t slot = it % kRing, buf = done & 1u;
+        if (COLS) ok = mbar_wait(b_full(slot), (it / kRing) & 1u, abort_flag, a.status, a.wait_ns);
         if (mine) {
           ok = ok && mbar_wait(s_full(g, buf), (done >> 1) & 1u, abort_flag, a.status, a.wait_ns);
           ++done;
@@ -323,7 +347,7 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 }
               }
             }
-          } else {
+          } else if (__any_sync(0xffffffffu, c_lo < 64) && c_hi > 0) {
 #pragma unroll 1
             for (int c0 = 0; c0 < 64; c0 += 32) {
               float v[32];
@@ -362,6 +386,7 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
           __syncwarp();
           if (elect_one()) mbar_arrive(s_empty(g, buf));   // S is in registers
           const int see = pos + 1 - (u.first + x) * kTileRows - 64 * half;         // columns below this
+          if (!__any_sync(0xffffffffu, see > 0)) continue;
           if (__any_sync(0xffffffffu, see < 64)) {
 #pragma unroll
             for (int e = 0; e < 64; ++e)
