@@ -17,12 +17,12 @@ struct ScoresPlan {
   size_t stats_at, logsum_at, parts_at, bytes;
 };
 
-// B tiles a unit takes: eight units a CTA, so that they end together, but sixteen tiles each (a unit costs about one beside
+// B tiles a unit takes: twelve units a CTA, so that they end together, but twelve tiles each (a unit costs about one beside
 // them) while that leaves every SM one.
 int unit_length(int64_t steps) {
   const int64_t n = sms();
-  int64_t seg = (steps + 8 * n - 1) / (8 * n), each = (steps + n - 1) / n;
-  const int64_t least = each < 16 ? each : 16;
+  int64_t seg = (steps + 12 * n - 1) / (12 * n), each = (steps + n - 1) / n;
+  const int64_t least = each < 12 ? each : 12;
   if (seg < least) seg = least;
   return (int)(seg < 1 ? 1 : seg);
 }
