@@ -49,6 +49,7 @@ struct Args {
   float2* part_ml;                   // [items][chunks][8 NT]: m, l
   float* part_o;                     // [items][chunks][8 NT][128]
   float* logits;                     // [sets * heads][blocks][n_max][pitch], or nullptr
+  int stages;                        // of a warp's ring: kStages, or 1 with chunk <= 64
   int late;                          // 1: runs beside the kernel before it
   int pitch;                         // 2 or a multiple of 4, at least the rows of a block
   uint32_t* status;
@@ -62,9 +63,11 @@ __device__ __forceinline__ int rows_held(const int32_t* lens, int set, int n_max
   return cut;
 }
 
+// Shared memory of a CTA with rings of `stages`: three, or one where a part is a single step of its warps (three CTAs an SM
+// then, for many short sequences).
 template <int NT>
-__host__ __device__ constexpr int smem_bytes() {
-  constexpr int ring = kWarps * kStages * kStageBytes, meet = kWarps * 8 * NT * 132 * 4;
+__host__ __device__ constexpr int smem_bytes(int stages = kStages) {
+  const int ring = kWarps * stages * kStageBytes, meet = kWarps * 8 * NT * 132 * 4;
   return ring > meet ? ring : meet;
 }
 
@@ -120,7 +123,8 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const __grid_constant
   const int r0 = blk * 8 * NT, r1 = min(a.q.rows, r0 + 8 * NT);
 
   // ------------------------------------------------------------ the ring of this warp
-  const uint32_t ring = smem_addr(smem) + warp * kStages * kStageBytes;
+  const int stages = FUSED ? kStages : a.stages;
+  const uint32_t ring = smem_addr(smem) + warp * stages * kStageBytes;
   const __nv_bfloat16* kb = a.K.base + set * a.K.stride_b + h * a.K.stride_h + (lane & 15) * 8;
   const __nv_bfloat16* vb = a.V.base + set * a.V.stride_b + h * a.V.stride_h + (lane & 15) * 8;
   // rows that one block of queries reads once leave the L2 to the logits and parts (128 heads of 2048 rows 189 -> 182 us)
@@ -143,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const __grid_constant
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) {
     const int u = k0 + warp * kKeys + s * kStep;
-    if (u < k1) fetch(u, s);
+    if (s < stages && u < k1) fetch(u, s);                 // (a ring of one: the only step)
     copy_commit();
   }
 
@@ -214,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const __grid_constant
   for (int u0 = k0 + warp * kKeys; u0 < k1; u0 += kStep) {
     {
       const int ahead = u0 + (kStages - 1) * kStep;        // (k1 + 3 kStep stays below 2^31)
-      if (ahead < k1) fetch(ahead, stage == 0 ? kStages - 1 : stage - 1);
+      if (ahead < k1) fetch(ahead, stage == 0 ? kStages - 1 : stage - 1);            // (never with a ring of one)
       copy_commit();
     }
     int key_at[2];                                         // positions of keys g, g + 8
@@ -486,6 +490,7 @@ struct JoinArgs {
   const int32_t* q_lens;
   Outputs out;
   int slices;                        // CTAs per problem
+  int by_warp;                       // 1: a warp per query row (few parts, many rows)
   const float* logits;               // as in Args, with LOGITS
   int n_max, pitch, block_rows;
 };
@@ -546,6 +551,39 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_parts_kernel(const JoinA
     sum = total(sum);
   };
 
+  auto finish = [&](int i, int g, const float4& o, float top, float sum) {
+    const float inv = inverse(sum);
+    const int hq = h * a.group + g;
+    *reinterpret_cast<uint2*>(a.out.O + b * a.out.o_sb + hq * a.out.o_sh + i * a.out.o_sn + lane * 4) =
+        make_uint2(token::pack_bf16(o.x * inv, o.y * inv), token::pack_bf16(o.z * inv, o.w * inv));
+    if (lane == 0 && a.out.lse != nullptr)
+      a.out.lse[((int64_t)b * a.heads * a.group + hq) * a.t + i] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+  };
+  if (!LOGITS && a.by_warp) {
+    for (int r = slice * kJoinWarps + warp; r < rows; r += a.slices * kJoinWarps) {
+      const int i = r / a.group, g = r % a.group;
+      if (i >= live) continue;
+      const Row x = row_of(r);
+      float4 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (k < all_parts) v[k] = values(x, k);
+      float top, sum;
+      stats(x, top, sum);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int c0 = 0; c0 < all_parts; c0 += 4) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (c0 + k >= all_parts) continue;
+          const float4 y = c0 == 0 ? v[k] : values(x, c0 + k);
+          const float f = share(ml(x, c0 + k).x, top);
+          o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
+        }
+      }
+      finish(i, g, o, top, sum);
+    }
+    return;
+  }
   int turn = 0;
   for (int r = slice; r < rows; r += a.slices) {
     const int i = r / a.group, g = r % a.group;
@@ -580,12 +618,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32) join_parts_kernel(const JoinA
         const float4 y = s_part[turn][w][lane];
         o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
       }
-      const float inv = inverse(sum);
-      const int hq = h * a.group + g;
-      *reinterpret_cast<uint2*>(a.out.O + b * a.out.o_sb + hq * a.out.o_sh + i * a.out.o_sn + lane * 4) =
-          make_uint2(token::pack_bf16(o.x * inv, o.y * inv), token::pack_bf16(o.z * inv, o.w * inv));
-      if (lane == 0 && a.out.lse != nullptr)
-        a.out.lse[((int64_t)b * a.heads * a.group + hq) * a.t + i] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+      finish(i, g, o, top, sum);
     }
     turn ^= 1;
   }

@@ -33,6 +33,7 @@ RowsPlan plan_rows(int64_t problems, int64_t query_rows, int64_t keys, int nt = 
   int64_t chunk = chunks > 0 ? (keys + chunks - 1) / chunks : keys;
   const int64_t least = items <= slots ? 128 : 512;
   if (chunk < least) chunk = least;
+  if (chunk > keys) chunk = keys > 0 ? keys : 1;
   chunk = (chunk + 63) / 64 * 64;
   chunks = keys > 0 ? (keys + chunk - 1) / chunk : 1;
   pl.chunk = (int)chunk;
@@ -70,8 +71,12 @@ bool launch_parts(const rows::Args& a, const rows::Outputs& out, int64_t ctas, c
   constexpr int most = rows::smem_bytes<NT>() + (FUSED && LOGITS ? rows::kLogitBytes : 0);
   static std::atomic<uint64_t> done{0};
   if (!allow_smem(rows::part_kernel<NT, LOGITS, FUSED>, most, done)) return false;
-  return launch_behind(rows::part_kernel<NT, LOGITS, FUSED>, first_ctas + ctas, rows::kThreads, most, FUSED ? a.chunks : 1, stream,
-                       first_ctas > 0 ? *first : a, a, (int)first_ctas, out);
+  rows::Args x = a, y = first_ctas > 0 ? *first : a;
+  const int64_t longest = ctas == 0 || (first_ctas > 0 && first->chunk > a.chunk) ? y.chunk : x.chunk;
+  x.stages = y.stages = longest <= rows::kWarps * rows::kKeys ? 1 : rows::kStages;
+  const int smem = FUSED ? most : rows::smem_bytes<NT>(x.stages);
+  return launch_behind(rows::part_kernel<NT, LOGITS, FUSED>, first_ctas + ctas, rows::kThreads, smem, FUSED ? a.chunks : 1, stream,
+                       y, x, (int)first_ctas, out);
 }
 
 template <bool PREFIX, bool LOGITS>
@@ -444,7 +449,8 @@ curdkv_status curdkv_attention_prefix(const void* Q, int32_t q_rows, int64_t q_s
   j.share = share;
   j.q_lens = q_lens;
   j.out = rows::Outputs{static_cast<__nv_bfloat16*>(O), o_stride_b, o_stride_h, o_stride_n, lse, nullptr};
-  j.slices = join_slices(P, (int64_t)group * q_rows);
+  j.by_warp = (desc_prefix->n_max > 0 ? j.prefix.chunks : 0) + pl.own.chunks <= 8;
+  j.slices = join_slices(P, j.by_warp ? ((int64_t)group * q_rows + rows::kJoinWarps - 1) / rows::kJoinWarps : (int64_t)group * q_rows);
   return launch_join<true, false>(j, P * j.slices, stream) ? CURDKV_OK : CURDKV_ERR_CUDA;
 }
 
