@@ -3,13 +3,18 @@
 // reference, sum and fp32 sums of values for the joining kernel.
 //
 // A tile is `seqs` sequences x `tokens` tokens x the heads of a KV head's group, brought in by one 5-D map, whatever the
-// strides.  The walk over the keys is that of attn_umma.cuh: S = Q K_t^T per 128-key tile, two groups of four softmax warps
-// on alternate tiles, a thread per query row; the weights go back over S in TMEM as bf16 and are the A operand of
-// O_g += P V_t; each group has its own running maximum (moved when a tile exceeds it by more than 2^8), sum and accumulator.
-// Weights are rounded to bf16 (2^-9 of each), sums take them unrounded.
+// strides.  The walk over the keys is that of attn_umma.cuh and attn_window.cuh: S = Q K_t^T per 128-key tile, a thread per
+// query row, the weights back over S in TMEM as bf16, where they are the A operand of O_g += P V_t (handed over in halves).
+// Two groups of four softmax warps, each with its own running maximum (moved when a tile exceeds it by more than 2^8), sum and
+// accumulator, take alternate key tiles of one tile of rows, or all key tiles of a tile of rows each: a pair then
+// reads every tile of K and V once, where a CTA per tile drew twice the bytes through the L2 (193 us against 168 for 256 rows
+// over 8 heads of 131072).  Weights are rounded to bf16 (half a step: 2^-8 of each), sums take them unrounded.
 //
-// What bounds it: with one tile of rows a KV head the keys' bytes (64 KB a tile of keys; the SM's share of the memory
-// takes 1.5 us for it), with more the walk itself, 1900 cycles a tile of keys: the products 1550, the exponentials 1020.
+// What bounds it: a single tile of rows the keys' bytes (128 heads of 8192 rows, 32 query rows: 84 us, 6.4 TB/s); a pair the
+// chain of a group, 3400 cycles a step: 1870 from logits to weights, then P V of the second half, the next S and the
+// wake-ups between; tensor pipe and special function units are busy half of the time.
+// Measured and dropped: a product warp per group (81 us against 73 for 64 sequences behind 32768 rows: they fall into step);
+// one to three of eight pairs of exponentials on the FMA pipe (no gain).
 #pragma once
 #include "umma_ptx.cuh"
 

@@ -5,14 +5,24 @@
 //   rows     S = Q K^T, a thread per query row: running maximum and sum, L_r                    (skipped when L is given)
 //   columns  S^T = K Q^T, a thread per key: w_j is a sum along the thread's own row of the accumulator
 //
-// Transposing the second product puts each sum into one thread: no exchange between lanes, no atomics, a fixed order.
-// Both are one kernel: "fixed" operand tiles A (M side: a thread a row of them) against a stream of tiles B.  A CTA works on
-// a pair of A tiles, eight epilogue warps each (two threads a row, 64 columns each), so that every B tile is used twice; and the accumulators
-// (128 x 128 fp32) are double-buffered per A tile and fill TMEM.  What a pair sees -- the key tiles up to its last position, the row tiles from
-// its first one on -- is cut into units of at most `seg` B tiles, which persistent CTAs take one by one, longest first.
+// Transposing the second product puts each sum into one thread (two, for the halves of a row): no exchange between lanes, a
+// fixed order.  Both are one kernel: fixed operand tiles A (M side: a thread a row of them) against a stream of tiles B.  A
+// CTA works on a pair of A tiles, eight epilogue warps each (two threads a row, 64 columns each), so that every B tile is used
+// twice; the accumulators (128 x 128 fp32) are double-buffered per A tile and fill TMEM.  What a pair sees -- the key
+// tiles up to its last position, the row tiles from its first one on -- is cut into units of at most `seg` B tiles, which
+// persistent CTAs take one by one, longest first.
 //
 // Query rows of a KV head are tiled as tokens x heads of the group (a 5-D map), so a tile of 128 rows is 128 / group tokens:
 // few tokens of many heads fill a tile, and little of a tile lies beyond the diagonal.
+//
+// What bounds it: the special function units, 16 exponentials a clock and SM, two tiles' 2 x 1024 cycles a step; they are busy
+// 74 to 81 % of the time, the tensor pipe 43 to 46 %, and the clock falls to 1.62 GHz beside them.  One pair of exponentials in
+// eight runs on the FMA pipe: issue slots are 55 % taken, and with two in eight what the units gain is lost there.  8192
+// tokens, 32 / 8 heads: 327 us with log sums at hand (840 TFLOP/s over the visible pairs), 635 without; 64 tokens over 4 x 8
+// heads of 32768 rows 178 us, the keys read twice.
+// Measured and dropped: A in TMEM, brought there by the epilogue warps (345 us where shared memory gave 350 at the time: the
+// products were not the bound, and short units paid for the copies); four epilogue warps a tile (377); a fixed deal of units
+// in alternating direction (SMs idle a tenth of the time); sums of thousands of terms in one fp32 chain (1.3e-6 off).
 #pragma once
 #include "umma_ptx.cuh"
 
@@ -135,7 +145,8 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
   }
   // rows of a query tile that no copy ever fills: zeros
   if (rows_used < kTileRows) {
-    const int slots = COLS ? kRing : 2 * kPairs, from = COLS ? ScoreSmem<COLS>::kB : ScoreSmem<COLS>::kA, dead = (kTileRows - rows_used) * 8;
+    const int slots = COLS ? kRing : 2 * kPairs, from = COLS ? ScoreSmem<COLS>::kB : ScoreSmem<COLS>::kA;
+    const int dead = (kTileRows - rows_used) * 8;
     for (int x = tid; x < slots * 2 * dead; x += kScoreThreads) {
       const int half = x / dead, y = x % dead;             // half tiles lie kHalfBytes apart
       *reinterpret_cast<uint4*>(base_ptr + from + half * kHalfBytes + rows_used * 128 + y * 16) = make_uint4(0u, 0u, 0u, 0u);

@@ -5,7 +5,8 @@
 // the row in the lower slot stays.  In steady state a step evicts as many rows as come, a handful at most, so nothing is
 // sorted: one sweep over the head's weights and positions (8 bytes a row, what bounds the kernel beside its start and
 // end) leaves every thread with the least key of its slots, and each eviction takes the least of all, whose owner
-// then looks for its next one.
+// then looks for its next one.  8 heads of 1703 slots 4.7 us, 1024 of 2049 11.5, 64 of 65540 with four rows to go 24 (59 with
+// slots read one at a time).
 #pragma once
 #include "cache.cuh"
 
