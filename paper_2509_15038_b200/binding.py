@@ -849,7 +849,7 @@ def curdkv_attention_scores(Q, K, desc: Desc, *, scale: float, q_lens: Optional[
         return scores, workspace
     code = load().curdkv_attention_scores(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), _base(K, Q), ctypes.byref(desc), scale,
                                           _addr(lse), int(bool(lse_given)), _base(scores, Q), workspace.data_ptr(),
-                                          workspace.numel() * workspace.element_size(), _raw_stream(dev))
+                                          workspace.nbytes, _raw_stream(dev))
     if code:
         _check(code, what)
     return scores, workspace
@@ -863,7 +863,8 @@ def curdkv_cache_push(cache: DeviceCache, K_new, V_new, budget: int, workspace: 
     The workspace is :func:`cache_workspace`'s."""
     what = "curdkv_cache_push"
     dev = _on_device(what, cache.K, K_new, V_new, scores_new, t_new, workspace)
-    _status_buffer(what, workspace)
+    if not workspace.is_contiguous():
+        raise ValueError(f"{what}: workspace must be contiguous")
     if K_new.dtype is not torch.bfloat16 or V_new.dtype is not torch.bfloat16:
         raise TypeError(f"{what}: K_new and V_new must be bf16")
     shape, k, v = K_new.shape, K_new.stride(), V_new.stride()
@@ -872,14 +873,15 @@ def curdkv_cache_push(cache: DeviceCache, K_new, V_new, budget: int, workspace: 
     B, H, t, d = shape
     if B != cache.batch or H != cache.kv_heads or d != cache.d:
         raise ValueError(f"{what}: new rows are {tuple(shape)}, the cache {(cache.batch, cache.kv_heads, cache.capacity, cache.d)}")
-    _int32("t_new", t_new, B)
+    if t_new is not None:
+        _int32("t_new", t_new, B)
     if scores_new is not None and (scores_new.dtype is not torch.float32 or scores_new.shape != shape[:3]
                                    or not scores_new.is_contiguous()):
         raise ValueError(f"{what}: scores_new must be contiguous fp32 {tuple(shape[:3])}")
-    desc = Desc.from_buffer_copy(_DESC(B, H, H, t, d, 1, *k[:3], *v[:3], 0 if t_new is None else t_new.data_ptr(), 0, 1, 0, 0, 0.0))
-    code = load().curdkv_cache_push(cache._ref, _base(K_new, cache.K), _base(V_new, cache.K), _addr(scores_new),
+    desc = Desc.from_buffer_copy(_DESC(B, H, H, t, d, 1, k[0], k[1], k[2], v[0], v[1], v[2], 0 if t_new is None else t_new.data_ptr(), 0, 1, 0, 0, 0.0))
+    code = load().curdkv_cache_push(cache._ref, K_new.data_ptr() or cache.K.data_ptr(), V_new.data_ptr() or cache.K.data_ptr(), _addr(scores_new),
                                     ctypes.byref(desc), index(budget), _count(num_sink), _count(window), workspace.data_ptr(),
-                                    workspace.numel() * workspace.element_size(), _raw_stream(dev))
+                                    workspace.nbytes, _raw_stream(dev))
     if code:
         _check(code, what)
 
@@ -922,7 +924,7 @@ def curdkv_cache_attention(Q, cache: DeviceCache, *, scale: float, weights: Opti
         return O, workspace
     code = load().curdkv_cache_attention(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), cache._ref, _cache_desc(cache, H), scale,
                                          O.data_ptr(), o[0], o[1], o[2], _addr(lse), _addr(weights), workspace.data_ptr(),
-                                         workspace.numel() * workspace.element_size(), _raw_stream(dev))
+                                         workspace.nbytes, _raw_stream(dev))
     if code:
         _check(code, what)
     return O, workspace
@@ -960,7 +962,7 @@ def curdkv_attention_prefix(Q, K_prefix, V_prefix, desc_prefix: Desc, K, V, desc
     code = load().curdkv_attention_prefix(Q.data_ptr(), t, q[0], q[1], q[2], _addr(q_lens), _base(K_prefix, Q), _base(V_prefix, Q),
                                           ctypes.byref(desc_prefix), _base(K, Q), _base(V, Q), ctypes.byref(desc), scale,
                                           O.data_ptr(), o[0], o[1], o[2], _addr(lse), workspace.data_ptr(),
-                                          workspace.numel() * workspace.element_size(), _raw_stream(dev))
+                                          workspace.nbytes, _raw_stream(dev))
     if code:
         _check(code, what)
     return O, workspace
