@@ -14,12 +14,12 @@
 // 2^slack.  Weights are rounded to bf16 before they multiply the values (half a step: 2^-8 of each), the sums take them
 // unrounded.
 //
-// What bounds it: bytes.  1024 heads of 2048 rows (1.07 GB) 162 us without weights, 6.6 TB/s, and 182 with (the logits'
-// 33 MB written and read, 16 MB of weights); 64 heads of 65540 rows, 8 query rows, 330 and 421 us (134 MB of logits).  8
+// What bounds it: bytes.  1024 heads of 2048 rows (1.07 GB) 156 us without weights, 6.9 TB/s, and 177 with (the logits'
+// 33 MB written and read, 16 MB of weights); 64 heads of 65540 rows, 8 query rows, 311 and 416 us (134 MB of logits).  8
 // heads of 1702 rows 7.9 us: a launch, one dependent chain of loads in a cluster of eight, the join.
-// Measured and dropped: streaming hints on the logits' stores (no change); the cluster form for more heads than fill the
-// device twice (211 against 188 us for 1024 heads); a warp per row for the join of many parts (53 us where four warps a row
-// with their loads ahead take 14, cold).
+// Measured and dropped: streaming hints on the logits' stores (no change); rings of three with 14 KB of logits a CTA, so
+// clusters of two for 1024 heads (211 us); a warp per row for the join of many parts (53 us where four warps a row with
+// their loads ahead take 14, cold).
 #pragma once
 #include "warp_ptx.cuh"
 
@@ -27,7 +27,7 @@ namespace curdkv {
 namespace rows {
 
 constexpr int kKeys = 16;                                  // of a warp's step
-constexpr int kStages = 3;
+constexpr int kStages = 2;                                 // (three leave room for two CTAs an SM: 128 heads of 2048 rows 29.0 us, so 23.3)
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kStageBytes = 2 * kKeys * 256;
 constexpr float kSlack = 6.f;
@@ -71,8 +71,7 @@ __device__ __forceinline__ int rows_held(const int32_t* lens, int set, int n_max
   return cut;
 }
 
-// Shared memory of a CTA with rings of `stages`: three, or one where a part is a single step of its warps (three CTAs an SM
-// then, for many short sequences).
+// Shared memory of a CTA with rings of `stages`: two, or one where a part is a single step of its warps.
 template <int NT>
 __host__ __device__ constexpr int smem_bytes(int stages = kStages) {
   const int ring = kWarps * stages * kStageBytes, meet = kWarps * 8 * NT * 132 * 4;
@@ -93,8 +92,7 @@ __device__ __forceinline__ float share(float m, float top) { return top == -INFI
 // FUSED: the parts of an item are the CTAs of a cluster, which join them through distributed shared memory; logits (where
 // weights are asked for) stay in shared memory until reference and sum are known, and the call is one launch.
 constexpr int kMostSplit = 3;                              // log2 of the CTAs of a cluster
-constexpr int kLogitBytes = 14 * 1024;                     // what two CTAs an SM leave room for beside their rings
-constexpr int kMostKeys = 1024;                            // of a CTA with logits
+constexpr int kLogitBytes = 35 * 1024;                     // of a CTA; two an SM fit beside their rings
 
 template <int NT, bool LOGITS, bool FUSED>
 __global__ void __launch_bounds__(kThreads, 2) part_kernel(const __grid_constant__ Args before, const __grid_constant__ Args behind,
@@ -135,7 +133,7 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const __grid_constant
   const uint32_t ring = smem_addr(smem) + warp * stages * kStageBytes;
   const __nv_bfloat16* kb = a.K.base + set * a.K.stride_b + h * a.K.stride_h + (lane & 15) * 8;
   const __nv_bfloat16* vb = a.V.base + set * a.V.stride_b + h * a.V.stride_h + (lane & 15) * 8;
-  // rows that one block of queries reads once leave the L2 to the logits and parts (128 heads of 2048 rows 189 -> 182 us)
+  // rows that one block of queries reads once leave the L2 to the logits and parts (1024 heads of 2048 rows 189 -> 182 us)
   uint64_t pol;
   if (a.blocks > 1) asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
   else asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol));
@@ -380,12 +378,14 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const __grid_constant
     __shared__ float2 s_all[1 << kMostSplit][8 * NT];
     // (the old weights are asked for before the wait for the others)
     float* weights = LOGITS ? out.weights + (int64_t)p * a.n_max + k0 : nullptr;
-    float was[kMostKeys / kThreads];
-    if (LOGITS) {
+    constexpr int kAhead = 5;                              // (18: 1024 heads of 500 rows 56.5 -> 58.9 us, for the code's length)
+    float was[kAhead];
+    auto ask = [&](int from, float (&x)[kAhead]) {
 #pragma unroll
-      for (int k = 0; k < kMostKeys / kThreads; ++k)
-        if (tid + k * kThreads < k1 - k0) was[k] = weights[tid + k * kThreads];
-    }
+      for (int k = 0; k < kAhead; ++k)
+        if (from + tid + k * kThreads < k1 - k0) x[k] = weights[from + tid + k * kThreads];
+    };
+    if (LOGITS) ask(0, was);
     if (a.chunks > 1) cluster_sync(); else __syncthreads();
     for (int e = tid; e < a.chunks * 8 * NT; e += kThreads) {
       const int c = e / (8 * NT), qi = e % (8 * NT);
@@ -443,10 +443,7 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const __grid_constant
     }
     if (LOGITS) {
       __syncthreads();
-#pragma unroll
-      for (int k = 0; k < kMostKeys / kThreads; ++k) {
-        const int j = tid + k * kThreads;
-        if (j >= k1 - k0) break;
+      auto weight = [&](int j) {
         const float* x = logits + (size_t)j * a.pitch;
         float w = 0.f;
         for (int r = 0; r < a.pitch; r += 2) {
@@ -454,7 +451,18 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const __grid_constant
           w = fmaf(exp2_approx(v.x - n0.x), n0.y, w);
           w = fmaf(exp2_approx(v.y - n1.x), n1.y, w);
         }
-        weights[j] = was[k] + w;
+        return w;
+      };
+      for (int from = 0; from < k1 - k0; from += kAhead * kThreads) {
+        float next[kAhead];
+        ask(from + kAhead * kThreads, next);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int j = from + tid + k * kThreads;
+          if (j < k1 - k0) weights[j] = was[k] + weight(j);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) was[k] = next[k];
       }
     }
     if (a.chunks > 1) cluster_sync();                      // nobody leaves while its parts are read

@@ -127,24 +127,24 @@ bool plan_cache(const curdkv_cache* c, const curdkv_desc* d, int32_t q_rows, Cac
   pl->rows = plan_rows(P, rows, c->capacity);
   pl->pitch = (int)(rows <= 2 ? 2 : (rows < 8 * pl->rows.nt ? (rows + 3) / 4 * 4 : 8 * pl->rows.nt));
   // One launch where a KV head's query rows are one block and its logits fit into the shared memory of a cluster, with more
-  // CTAs while all find room on the device and each keeps two steps of its warps.  Not where that takes more than two rounds
-  // of clusters (their ends, when nothing is loaded, add up) nor where clusters of eight leave half the places empty to long
-  // caches.  With weights, 4 query rows, us, clusters | parts and a second kernel:
-  //   8 heads of 200 rows 6.0 | 8.9, of 1702 8.0 | 8.2, of 7000 15.0 | 12.5        32 of 1702 9.0 | 10.8        64 of 7000 46.9 | 48.3
-  //   128 heads of 2048 31.0 | 33.7, of 4096 60.3 | 54.9       320 of 2048 74 | 69         1024 of 500 55 | 65, of 2048 211 | 188
+  // CTAs while all find room on the device and each keeps two steps of its warps.  Not where clusters fill their last round
+  // badly, nor where clusters of eight leave half the places empty to long caches.  The rule does not ask for weights, so that
+  // outputs are the same with them and without (480 heads without: 90 | 81).
+  // 4 query rows, with weights, us, clusters | parts and a second kernel:
+  //   8 heads of 200 rows 6.1 | 8.9, of 1702 7.9 | 8.2, of 7000 15.0 | 12.4        32 of 1702 9.0 | 10.8        64 of 7000 39.0 | 43.5
+  //   128 heads of 2048 23.2 | 28.5, of 4096 45.2 | 49.7       320 of 2048 78 | 67       480 of 2048 84 | 88       1024 of 500 55 | 65, of 2048 177 | 181
   pl->cluster = 0;
   if (pl->rows.blocks == 1) {
     const int64_t keys = c->capacity, slots = 2 * (int64_t)sms();
     int split = 0;
-    auto fits = [&](int k) {
-      const int64_t each = ((keys + (1 << k) - 1) >> k) + rows::kKeys;
-      return each <= rows::kMostKeys && each * pl->pitch * 4 <= rows::kLogitBytes;
-    };
+    auto fits = [&](int k) { return (((keys + (1 << k) - 1) >> k) + rows::kKeys) * pl->pitch * 4 <= rows::kLogitBytes; };
     while (split < rows::kMostSplit && !fits(split)) ++split;
     const bool fit = fits(split);
     while (split < rows::kMostSplit && (P << (split + 1)) <= slots && keys > (2 * rows::kWarps * rows::kKeys) << split) ++split;
-    const bool waves = split > 0 && (P << split) > 2 * slots, idle = 2 * (P << split) <= slots && (keys >> split) > 512;
-    if (fit && !waves && !idle) pl->cluster = 1 << split;
+    const int64_t ctas = P << split, rounds = (ctas + slots - 1) / slots;
+    const bool full = ctas <= slots || 10 * rounds * slots <= 13 * ctas;
+    const bool idle = 2 * ctas <= slots && (keys >> split) > 512;
+    if (fit && full && !idle) pl->cluster = 1 << split;
   }
   // joining: about eight CTAs an SM, but 128 keys each at least
   int64_t slices = (8 * (int64_t)sms() + (P > 0 ? P : 1) - 1) / (P > 0 ? P : 1);
