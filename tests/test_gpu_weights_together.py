@@ -1,0 +1,102 @@
+"""Attention-weight calls beside one another, on the GPU: forms that only many heads reach, one workspace in several captured
+graphs, calls of different sizes in turn over one workspace.  Needs a B200."""
+import pytest
+import torch
+
+from paper_2509_15038_b200 import binding as cur
+from tests import test_gpu_scores as scores
+from tests import test_gpu_weights as weights
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+SCALE = weights.SCALE
+
+
+@pytest.mark.parametrize("B,H,cap,t", [(37, 16, 500, 1), (25, 16, 500, 1), (37, 8, 2600, 1), (9, 8, 4400, 2), (75, 16, 130, 4)])
+def test_rounds_of_clusters(B, H, cap, t):
+    """More heads than the device holds at a time: whole rounds, a part of one, clusters of several CTAs."""
+    held = [max(0, cap - (b * 37) % (cap + 5)) for b in range(B)]
+    weights._attend(B, H, 4, t, cap, held, seed=1000 + cap)
+
+
+@pytest.mark.parametrize("lens_step,n", [(1, 130), (7, 260)])
+def test_scores_of_very_many_short_prompts(lens_step, n):
+    """More units of work than are taken one at a time, many of them empty."""
+    B = 1250
+    lens = [(b * lens_step) % (n + 1) for b in range(B)]
+    scores._run(B, 8, 1, n, 2, lens=lens, q_lens=[b % 3 for b in range(B)], seed=1100, heads=[0, 7])
+
+
+def _graph(f):
+    f()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        f()
+    return g
+
+
+def test_graphs_share_a_workspace():
+    """Graphs of different sizes captured over one workspace, replayed in turn: every time the results of a call alone."""
+    ws = torch.zeros(64 << 20, dtype=torch.uint8, device=DEV)
+    calls = []
+    for i, (B, H, group, n, t) in enumerate([(2, 2, 4, 900, 32), (300, 1, 1, 200, 1), (1, 8, 4, 1500, 700)]):
+        K, Q = weights._rand((B, H, n, 128), 1200 + i), weights._rand((B, H * group, t, 128), 1210 + i)
+        desc, out = cur.make_desc(K, K, 1, q_heads=H * group), torch.zeros((B, H, n), device=DEV)
+        calls.append((out, lambda Q=Q, K=K, desc=desc, out=out, w=None: cur.curdkv_attention_scores(Q, K, desc, scale=SCALE, scores=out, workspace=w)))
+    for i, (B, H, group, n, t) in enumerate([(1, 8, 4, 1700, 1), (1, 2, 4, 40000, 1), (60, 8, 4, 600, 1), (2, 2, 4, 700, 9)]):
+        c, Q = weights._cache(B, H, n, [n] * B, 1220 + i), weights._rand((B, H * group, t, 128), 1230 + i)
+        O = torch.zeros_like(Q)
+        calls.append((O, lambda Q=Q, c=c, O=O, w=None: cur.curdkv_cache_attention(Q, c, scale=SCALE, O=O, weights=torch.zeros_like(c.raw), workspace=w)))
+    for i, (Bp, share, n0, n) in enumerate([(1, 2, 500, 30), (2, 40, 700, 90)]):
+        K0, K = weights._rand((Bp, 2, n0, 128), 1240 + i), weights._rand((Bp * share, 2, n, 128), 1250 + i)
+        Q = weights._rand((Bp * share, 8, 1, 128), 1260 + i)
+        d0, d, O = cur.make_desc(K0, K0, 1, q_heads=8), cur.make_desc(K, K, 1, q_heads=8), torch.zeros_like(Q)
+        calls.append((O, lambda Q=Q, K0=K0, K=K, d0=d0, d=d, O=O, w=None: cur.curdkv_attention_prefix(Q, K0, K0, d0, K, K, d, scale=SCALE, O=O, workspace=w)))
+    want = []
+    for out, f in calls:
+        f()
+        want.append(out.clone())
+    graphs = [_graph(lambda f=f: f(w=ws)) for _, f in calls]
+    for order in (range(len(calls)), reversed(range(len(calls))), [0, 0, 3, 1, 5, 1, 4, 2, 8, 3, 7, 6, 2]):
+        for out, _ in calls:
+            out.fill_(9.0)
+        used = set()
+        for i in order:
+            graphs[i].replay()
+            used.add(i)
+        torch.cuda.synchronize()
+        for i in used:
+            assert torch.equal(calls[i][0], want[i]), i
+    assert cur.curdkv_device_status(ws) == 0
+
+
+def test_streams_side_by_side():
+    """The three attentions at once on three streams, a workspace each, again and again: the results of each alone."""
+    c = weights._cache(3, 8, 1700, [1700, 900, 3], 1300)
+    Q = weights._rand((3, 32, 1, 128), 1301)
+    K, Qs = weights._rand((3, 8, 1000, 128), 1302), weights._rand((3, 32, 64, 128), 1303)
+    desc = cur.make_desc(K, K, 1, q_heads=32)
+    K0, Kp, Qp = weights._rand((1, 8, 3000, 128), 1304), weights._rand((24, 8, 100, 128), 1305), weights._rand((24, 32, 1, 128), 1306)
+    d0, d = cur.make_desc(K0, K0, 1, q_heads=32), cur.make_desc(Kp, Kp, 1, q_heads=32)
+
+    def calls(ws):
+        w = torch.zeros_like(c.raw)
+        return [lambda: (cur.curdkv_cache_attention(Q, c, scale=SCALE, weights=w.zero_(), workspace=ws[0]), w)[0][0],
+                lambda: cur.curdkv_attention_scores(Qs, K, desc, scale=SCALE, workspace=ws[1])[0],
+                lambda: cur.curdkv_attention_prefix(Qp, K0, K0, d0, Kp, Kp, d, scale=SCALE, workspace=ws[2])[0]]
+
+    want = [f() for f in calls([None] * 3)]
+    ws = [torch.zeros(16 << 20, dtype=torch.uint8, device=DEV) for _ in range(3)]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    fs = calls(ws)
+    torch.cuda.synchronize()
+    got = [[] for _ in fs]
+    for _ in range(20):
+        for s, f, g in zip(streams, fs, got):
+            with torch.cuda.stream(s):
+                g.append(f())
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert all(torch.equal(x, w) for x in g)
+    assert all(cur.curdkv_device_status(x) == 0 for x in ws)
