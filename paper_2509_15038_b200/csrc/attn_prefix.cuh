@@ -14,7 +14,9 @@
 // chain of a group, 3400 cycles a step: 1870 from logits to weights, then P V of the second half, the next S and the
 // wake-ups between; tensor pipe and special function units are busy half of the time.
 // Measured and dropped: a product warp per group (81 us against 73 for 64 sequences behind 32768 rows: they fall into step);
-// one to three of eight pairs of exponentials on the FMA pipe (no gain).
+// one to three of eight pairs of exponentials on the FMA pipe (no gain); a pair's steps in halves of 64 keys, so that one half
+// of S is formed while the group is at the other (156 us against 143 for 512 rows over 8 heads of 131072: products of 64
+// columns); the weights handed over in 32 + 96 or 96 + 32 keys (143 to 145).
 #pragma once
 #include "umma_ptx.cuh"
 
