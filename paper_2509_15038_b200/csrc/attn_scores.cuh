@@ -44,6 +44,9 @@ struct ScoreArgs {
   const float* logsum;               // columns: [batch * heads][row_tiles][128] -L, -inf for rows that do not count
   float* out;                        // columns: [segs][2][batch * heads][n_max]; [batch * heads][n_max], 0 before, where segs = 1
   int normalise;                     // columns: divide by the rows that count (segs = 1)
+  int join_segs, join_seg;           // columns that join the rows pass's parts themselves: its `segs` and `seg`
+  float* clear;                      // rows: cleared for the columns pass, clear_count of them
+  int64_t clear_count;
   uint32_t* status;
   unsigned long long wait_ns = kWaitLimitNs;
 };
@@ -76,6 +79,32 @@ struct ScoreSeq {
   }
 };
 
+// Maximum and sum of a query row, from the parts that the rows pass left.
+struct RowSum {
+  float top = -INFINITY, sum = 0.f;
+  __device__ __forceinline__ void join(float2 e) {
+    const float now = fmaxf(top, e.x);
+    sum = sum * (now == -INFINITY ? 1.f : fast_exp2(top - now)) + e.y * (now == -INFINITY ? 1.f : fast_exp2(e.x - now));
+    top = now;
+  }
+  // Parts `sub`, `sub` + `subs`, ...; the pair of tiles that `tile` belongs to walked units of `seg` key tiles.
+  __device__ __forceinline__ void join_parts(const ScoreArgs& a, const ScoreSeq& s, int p, int tile, int r, int sub, int subs, int seg) {
+    const int end_tok = min((tile / 2 * 2 + min(2, a.row_tiles - tile / 2 * 2)) * a.tokens, s.q);
+    const int used = 2 * ((((s.pos0 + end_tok) + kTileRows - 1) / kTileRows + seg - 1) / seg);
+    const float2* stats = a.stats + ((int64_t)p * a.row_tiles + tile) * kTileRows + r;
+    const int64_t next = (int64_t)a.batch * a.heads * a.row_tiles * kTileRows;
+    for (int g = sub; g < used; g += 4 * subs) {
+      float2 e[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) e[k] = g + subs * k < used ? stats[(g + subs * k) * next] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) join(e[k]);
+    }
+  }
+  __device__ __forceinline__ float log() const { return sum == 0.f ? INFINITY : top + log2f(sum); }      // (of no weights: every 2^-L is 0)
+};
+__host__ __device__ constexpr int row_threads(int segs) { return segs > 4 ? 4 : 1; }           // that join a row's parts in turn
+
 // A unit: a pair of A tiles of one (sequence, KV head) and a run of B tiles.
 template <bool COLS>
 struct ScoreUnit {
@@ -107,7 +136,8 @@ struct ScoreUnit {
 };
 
 // map_q: 5-D (channel, head of the group, token, KV head, sequence), boxes of 64 x group x tokens; map_k: tiles of 128 rows.
-template <bool COLS>
+// JOIN: a columns pass whose CTAs have one unit each, of no more steps than B slots, and join the rows pass's parts themselves.
+template <bool COLS, bool JOIN>
 __global__ void __launch_bounds__(kScoreThreads, 1)
 score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const ScoreArgs a) {
   extern __shared__ unsigned char smem_dyn[];
@@ -164,7 +194,13 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
   tc_fence_after();
   constexpr uint32_t tmem_base = 0u;                       // all 512 columns are this CTA's: they begin at 0
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");       // L comes from the kernel before
+  // The columns pass is launched behind the kernel that leaves L (or its parts), which began when everything before it had
+  // ended: queries and keys are loaded at once, what comes from that kernel is waited for where it is needed.
+  auto wait_before = [&]() { asm volatile("griddepcontrol.wait;" ::: "memory"); };
+  if (!COLS) {
+    wait_before();
+    for (int64_t x = (int64_t)blockIdx.x * kScoreThreads + tid; x < a.clear_count; x += (int64_t)gridDim.x * kScoreThreads) a.clear[x] = 0.f;
+  }
 
   // The producer takes units from the counter, longest first, and tells the others one ahead; one without steps: no more.  (Which CTA takes
   // which changes no result.)  A fixed deal in alternating direction left SMs idle a tenth of the time.
@@ -203,9 +239,15 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       // (of very many units, of which short sequences leave many without steps, several are taken at a time)
       const int64_t batch = min(max(a.units / (32 * (int)gridDim.x), 1), 16);
       int64_t at = blockIdx.x, last = at + 1;              // units taken
+      bool waited = !COLS;
+      auto behind = [&]() {
+        if (!waited) wait_before();
+        waited = true;
+      };
       auto take = [&](ScoreUnit<COLS>& u) {                // the next unit that has steps, told to the others
         do {
           if (at == last) {
+            if (a.units > (int)gridDim.x) behind();
             at = a.units > (int)gridDim.x ? (int64_t)gridDim.x + batch * atomicAdd(a.next_unit, 1u) : (int64_t)a.units;
             last = at + batch;
           }
@@ -239,10 +281,12 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
           if (!wait(b_empty(slot), ((it / kRing) & 1u) ^ 1u)) break;
           ++it;
           const int tile = u.first + x;
-          mbar_arrive_expect_tx(b_full(slot), COLS ? q_bytes + 512u : (uint32_t)kSlotBytes);
+          mbar_arrive_expect_tx(b_full(slot), COLS ? q_bytes + (JOIN ? 0u : 512u) : (uint32_t)kSlotBytes);
           load(u, COLS, base + ScoreSmem<COLS>::kB + slot * kSlotBytes, b_full(slot), tile);
-          if (COLS)
+          if (COLS && !JOIN) {
+            behind();
             bulk_load(base + kScoreLog + slot * 512, a.logsum + ((int64_t)u.p * a.row_tiles + tile) * kTileRows, 512u, b_full(slot));
+          }
         }
         u = then;
         if (u.steps > 0) take(then);                       // (behind the last unit `then` stays as it is)
@@ -259,6 +303,7 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
   } else if (warp == 1) {
     // ------------------------------------------------------------ products: the whole warp waits, one lane issues
     constexpr uint32_t idesc = instr_desc_bf16(kTileRows);
+    if (COLS && !JOIN) wait_before();                      // (it would spin on L; joined calls are short)
     const uint64_t a_desc0 = smem_desc_sw128(base + ScoreSmem<COLS>::kA), b_desc0 = smem_desc_sw128(base + ScoreSmem<COLS>::kB);
     bool ok = true;
     uint32_t it = 0, pairs = 0, done[2] = {0, 0};          // B tiles, pairs of A tiles, products of each group
@@ -310,6 +355,28 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     const float sc = a.scale_log2;
     const uint64_t sc2 = pack2(sc, sc);
     const int P = a.batch * a.heads;
+    if (COLS) wait_before();
+    if constexpr (JOIN) {
+      // This CTA's only unit has a slot for each of its row tiles: -L goes to where a copy would bring it.  (The second pair of
+      // A tiles is never used then.)
+      const ScoreUnit<COLS> own(a, (int)blockIdx.x);
+      const ScoreSeq s(a, own.b);
+      float2* others = reinterpret_cast<float2*>(base_ptr + ScoreSmem<COLS>::kA + 2 * kSlotBytes);
+      const int e = tid - 64, row = e % kTileRows, sub = e / kTileRows, subs = row_threads(a.join_segs);
+      for (int x = 0; x < own.steps; ++x) {
+        const int tok = (own.first + x) * a.tokens + row / a.group;
+        const bool sees = row < rows_used && tok < s.q && s.pos0 + tok >= 0;
+        RowSum all;
+        if (sees && sub < subs) all.join_parts(a, s, own.p, own.first + x, row, sub, subs, a.join_seg);
+        if (sub > 0) others[(sub - 1) * kTileRows + row] = make_float2(all.top, all.sum);
+        asm volatile("bar.sync 1, 512;" ::: "memory");
+        if (sub == 0) {
+          for (int k = 0; k < subs - 1; ++k) all.join(others[k * kTileRows + row]);
+          reinterpret_cast<float*>(base_ptr + kScoreLog + x * 512)[row] = sees ? -all.log() : -INFINITY;
+        }
+        asm volatile("bar.sync 1, 512;" ::: "memory");
+      }
+    }
     bool ok = true;
     uint32_t it = 0, done = 0;                             // B tiles, this group's products
     ScoreUnit<COLS> u;
@@ -468,28 +535,10 @@ __global__ void __launch_bounds__(kLogsumThreads) score_logsum_kernel(const Scor
   const ScoreSeq s(a, b);
   const int tok = tile * a.tokens + r / a.group;
   const bool live = r < a.tokens * a.group && tok < s.q, sees = live && s.pos0 + tok >= 0;
-  float top = -INFINITY, sum = 0.f;
-  auto join = [&](float2 e) {
-    const float now = fmaxf(top, e.x);
-    sum = sum * (now == -INFINITY ? 1.f : fast_exp2(top - now)) + e.y * (now == -INFINITY ? 1.f : fast_exp2(e.x - now));
-    top = now;
-  };
+  RowSum all;
   if (given == nullptr) {
-    if (sees) {
-      // the pair of tiles this one belongs to walked these key tiles
-      const int end_tok = min((tile / 2 * 2 + min(2, a.row_tiles - tile / 2 * 2)) * a.tokens, s.q);
-      const int used = 2 * ((((s.pos0 + end_tok) + kTileRows - 1) / kTileRows + a.seg - 1) / a.seg);
-      const float2* stats = a.stats + ((int64_t)p * a.row_tiles + tile) * kTileRows + r;
-      const int64_t next = (int64_t)a.batch * a.heads * a.row_tiles * kTileRows;
-      for (int g = sub; g < used; g += 4 * subs) {
-        float2 e[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) e[k] = g + subs * k < used ? stats[(g + subs * k) * next] : make_float2(-INFINITY, 0.f);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) join(e[k]);
-      }
-    }
-    if (sub > 0) s_part[sub - 1][r] = make_float2(top, sum);
+    if (sees) all.join_parts(a, s, p, tile, r, sub, subs, a.seg);
+    if (sub > 0) s_part[sub - 1][r] = make_float2(all.top, all.sum);
     __syncthreads();
   }
   if (sub > 0) return;
@@ -500,8 +549,8 @@ __global__ void __launch_bounds__(kLogsumThreads) score_logsum_kernel(const Scor
       L = given[at] * a.log2_of_ln;
       if (L == -INFINITY) L = INFINITY;                    // (a row that saw nothing)
     } else {
-      for (int k = 0; k < subs - 1; ++k) join(s_part[k][r]);
-      L = sum == 0.f ? INFINITY : top + log2f(sum);
+      for (int k = 0; k < subs - 1; ++k) all.join(s_part[k][r]);
+      L = all.log();
     }
   }
   logsum[((int64_t)p * a.row_tiles + tile) * kTileRows + r] = -L;

@@ -135,7 +135,7 @@ curdkv_status curdkv_attention_scores(const void* Q, int32_t q_rows, int64_t q_s
   a.segs = pl.row_segs;
   a.seg = pl.row_seg;
   a.units = (int)(P * ((pl.row_tiles + 1) / 2) * pl.row_segs);
-  const int logsum_threads = !lse_given && pl.row_segs > 4 ? umma::kLogsumThreads : kTileRows;
+  const int logsum_threads = kTileRows * (lse_given ? 1 : umma::row_threads(pl.row_segs));
   if (d.n_max == 0) {                                      // no scores; a query that sees nothing has a log sum all the same
     if (lse == nullptr || lse_given) return CURDKV_OK;
     return launch(umma::score_logsum_kernel, P * pl.row_tiles, logsum_threads, 0, false, stream, a, (const float*)nullptr, logsum, lse,
@@ -145,29 +145,42 @@ curdkv_status curdkv_attention_scores(const void* Q, int32_t q_rows, int64_t q_s
   if (!bf16_map(&mq, Q, 5, sizes, strides, box) ||
       !rows_map(&mk, K, d.batch, d.kv_heads, d.n_max, d.k_stride_b, d.k_stride_h, d.k_stride_n))
     return CURDKV_ERR_CUDA;
-  static std::atomic<uint64_t> rows_done{0}, cols_done{0};
-  if (!allow_smem(umma::score_attention_kernel<false>, umma::kScoreDynamic, rows_done) ||
-      !allow_smem(umma::score_attention_kernel<true>, umma::kScoreDynamic, cols_done))
-    return CURDKV_ERR_CUDA;
+  static std::atomic<uint64_t> rows_done{0}, cols_done{0}, join_done{0};
+  const auto rows_pass = umma::score_attention_kernel<false, false>;
   const int64_t places = sms();
+  // Short calls whose log sums nobody asks for go without the kernel between the passes: the columns' CTAs, a unit each, join the
+  // parts that they need, as often as there are pairs of key tiles (us, so | with the kernel
+  // between: 32 tokens over 8 heads of 1024 rows 11.1 | 14.9, of 4096 13.7 | 16.2; 64 over one head of 4000 15.4 | 16.8.)
+  const int64_t key_units = P * ((pl.key_tiles + 1) / 2) * pl.key_segs;
+  const bool direct = !lse_given && lse == nullptr && key_units <= places && pl.key_seg <= umma::ScoreSmem<true>::kRing && pl.row_segs <= 16;
+  const auto cols_pass = direct ? umma::score_attention_kernel<true, true> : umma::score_attention_kernel<true, false>;
+  if (!allow_smem(rows_pass, umma::kScoreDynamic, rows_done) || !allow_smem(cols_pass, umma::kScoreDynamic, direct ? join_done : cols_done))
+    return CURDKV_ERR_CUDA;
+  if (direct && pl.key_segs == 1) {
+    a.clear = scores;
+    a.clear_count = P * d.n_max;
+  }
   if (!lse_given && a.units > places && cudaMemsetAsync(a.next_unit, 0, sizeof(uint32_t), stream) != cudaSuccess) return CURDKV_ERR_CUDA;
   if (!lse_given &&
-      !launch(umma::score_attention_kernel<false>, a.units < places ? a.units : places, umma::kScoreThreads, umma::kScoreDynamic, false,
+      !launch(rows_pass, a.units < places ? a.units : places, umma::kScoreThreads, umma::kScoreDynamic, false,
               stream, mq, mk, a))
     return CURDKV_ERR_CUDA;
-  if (!launch(umma::score_logsum_kernel, P * pl.row_tiles, logsum_threads, 0, !lse_given, stream, a,
+  if (!direct &&
+      !launch(umma::score_logsum_kernel, P * pl.row_tiles, logsum_threads, 0, !lse_given, stream, a,
               (const float*)(lse_given ? lse : nullptr), logsum, lse_given ? (float*)nullptr : lse, scores,
               pl.key_segs > 1 ? (int64_t)0 : P * d.n_max, a.next_unit + 1))
     return CURDKV_ERR_CUDA;
   a.next_unit += 1;
+  a.join_segs = direct ? pl.row_segs : 0;
+  a.join_seg = pl.row_seg;
   a.segs = pl.key_segs;
   a.seg = pl.key_seg;
-  a.units = (int)(P * ((pl.key_tiles + 1) / 2) * pl.key_segs);
+  a.units = (int)key_units;
   float* parts = reinterpret_cast<float*>(ws + pl.parts_at);
   const int normalise = d.raw_scores ? 0 : 1;
   a.out = pl.key_segs > 1 ? parts : scores;
   a.normalise = pl.key_segs > 1 ? 0 : normalise;
-  if (!launch(umma::score_attention_kernel<true>, a.units < places ? a.units : places, umma::kScoreThreads, umma::kScoreDynamic, true,
+  if (!launch(cols_pass, a.units < places ? a.units : places, umma::kScoreThreads, umma::kScoreDynamic, true,
               stream, mq, mk, a))
     return CURDKV_ERR_CUDA;
   if (pl.key_segs > 1 && !launch(umma::score_sum_kernel, P * ((d.n_max + 255) / 256), 256, 0, true, stream, a, (const float*)parts, scores, normalise))
