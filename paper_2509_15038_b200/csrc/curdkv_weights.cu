@@ -204,13 +204,13 @@ bool plan_prefix(const curdkv_desc* dp, const curdkv_desc* d, int32_t q_rows, Pr
   pl->pre = plan_rows(P0, rows * share, dp->n_max);
   pl->own = plan_rows(P, rows, d->n_max, pl->pre.nt);      // (both may be one launch)
   if (rows * share > 16) pl->own = plan_rows(P, rows, d->n_max);
-  pl->tiles = rows * share > 16 && group <= kTileRows && dp->n_max > 0;
+  pl->tiles = P0 > 0 && rows * share > 16 && group <= kTileRows && dp->n_max > 0;
   size_t entries = pl->pre.entries;
   if (pl->tiles) {
     plan_tiles(P0, (int)share, q_rows, group, dp->n_max, 512. * (double)P * d->n_max * ((rows + 15) / 16), pl);
     // as many parts as any own rows could lead to: a workspace for long ones serves short ones too
     const int64_t items = P0 * ((pl->row_tiles + 1) / 2), key_tiles = ((int64_t)dp->n_max + kTileRows - 1) / kTileRows;
-    int64_t most = items > 0 ? 2 * (int64_t)sms() / items + 2 : 1;
+    int64_t most = 2 * (int64_t)sms() / items + 2;
     if (most > key_tiles) most = key_tiles;
     const size_t tiles = (size_t)P0 * pl->row_tiles * most * kTileRows;
     if (tiles > entries) entries = tiles;                  // (rows that the maps cannot hold take the other form)

@@ -113,6 +113,23 @@ def test_calls_on_nothing():
     assert _scores(d=_desc(batch=0)) == 0
 
 
+@pytest.mark.parametrize("rows,q_heads", [(1, 8), (5, 8), (8, 8), (2, 64), (1, 34), (300, 8)])
+def test_calls_on_nothing_with_many_query_rows(rows, q_heads):
+    """The same with more than 16 query rows a KV head, where a prefix would be read in tiles: no sequences, and no prefixes or
+    some, have a workspace and an answer."""
+    lib, none = cur.load(), _desc(batch=0, q_heads=q_heads)
+    strides = (q_heads * rows * 128, rows * 128, 128)
+    for prefixes in (0, 1):
+        prefix = _desc(batch=prefixes)
+        assert lib.curdkv_attention_prefix_workspace_bytes(ctypes.byref(prefix), ctypes.byref(none), rows) >= 256
+        assert _prefix(d=none, d0=prefix, rows=rows, qs=strides, os=strides) == 0
+    assert lib.curdkv_attention_scores_workspace_bytes(ctypes.byref(none), rows) >= 256
+    assert _scores(d=none, rows=rows, qs=strides) == 0
+    if rows * q_heads // 2 <= 1024:
+        assert lib.curdkv_cache_attention_workspace_bytes(ctypes.byref(_cache()), ctypes.byref(none), rows) >= 256
+        assert _attend(d=none, rows=rows, qs=strides, os=strides) == 0
+
+
 def test_binding_checks_without_a_device():
     K = torch.zeros((1, 2, 8, 128), dtype=torch.bfloat16)
     raw, pos = torch.zeros((1, 2, 8)), torch.zeros((1, 2, 8), dtype=torch.int32)
