@@ -24,7 +24,7 @@ int unit_length(int64_t steps) {
   int64_t seg = (steps + 12 * n - 1) / (12 * n), each = (steps + n - 1) / n;
   const int64_t least = each < 12 ? each : 12;
   if (seg < least) seg = least;
-  return (int)(seg < 1 ? 1 : seg);
+  return (int)(seg < 1 ? 1 : (seg < (1 << 30) ? seg : 1 << 30));             // (no tensor has that many tiles)
 }
 
 bool plan_scores(const curdkv_desc* d, int32_t q_rows, ScoresPlan* pl) {
@@ -37,6 +37,7 @@ bool plan_scores(const curdkv_desc* d, int32_t q_rows, ScoresPlan* pl) {
   pl->tokens = kTileRows / group;
   pl->row_tiles = (q_rows + pl->tokens - 1) / pl->tokens;
   pl->key_tiles = d->n_max > 0 ? (d->n_max + kTileRows - 1) / kTileRows : 1;
+  if (P * pl->row_tiles > 0x7fffffff) return false;        // (so that the counts below stay within 64 bits)
   // B tiles of all pairs, from what the first and the last pair see
   const int64_t row_pairs = (pl->row_tiles + 1) / 2, key_pairs = (pl->key_tiles + 1) / 2;
   const int64_t before = d->n_max > q_rows ? d->n_max - q_rows : 0;          // keys that every token sees
@@ -50,8 +51,7 @@ bool plan_scores(const curdkv_desc* d, int32_t q_rows, ScoresPlan* pl) {
   pl->logsum_at = pl->stats_at + round256(rows * pl->row_segs * 2 * sizeof(float2));
   pl->parts_at = pl->logsum_at + round256(rows * sizeof(float));
   pl->bytes = pl->parts_at + (pl->key_segs > 1 ? round256((size_t)P * pl->key_segs * 2 * d->n_max * sizeof(float)) : 0);
-  return P * row_pairs * pl->row_segs <= 0x7fffffff && P * key_pairs * pl->key_segs <= 0x7fffffff && P * pl->row_tiles <= 0x7fffffff &&
-         P * ((d->n_max + 255) / 256) <= 0x7fffffff;
+  return P * row_pairs * pl->row_segs <= 0x7fffffff && P * key_pairs * pl->key_segs <= 0x7fffffff && P * ((d->n_max + 255) / 256) <= 0x7fffffff;
 }
 
 // Launched behind the kernel before it without waiting for its end (`chained`): the kernel itself waits.

@@ -130,6 +130,15 @@ def test_calls_on_nothing_with_many_query_rows(rows, q_heads):
         assert _attend(d=none, rows=rows, qs=strides, os=strides) == 0
 
 
+def test_scores_of_absurd_sizes_are_refused():
+    """Sizes that no memory holds: units of more tiles than an int counts, and counts beyond 64 bits."""
+    for batch, kv_heads, n, rows in ((4736, 8, 1 << 24, 1 << 29), (16, 8, 1 << 24, 1 << 29), (1 << 20, 16, 1 << 29, 1 << 29)):
+        d = _desc(batch=batch, kv_heads=kv_heads, q_heads=kv_heads * 128, n_max=n)
+        assert cur.load().curdkv_attention_scores_workspace_bytes(ctypes.byref(d), rows) == 0
+    d = _desc(batch=1, kv_heads=1, q_heads=128, n_max=1 << 29)
+    assert cur.load().curdkv_attention_scores_workspace_bytes(ctypes.byref(d), 1 << 29) > 1 << 40
+
+
 def test_binding_checks_without_a_device():
     K = torch.zeros((1, 2, 8, 128), dtype=torch.bfloat16)
     raw, pos = torch.zeros((1, 2, 8)), torch.zeros((1, 2, 8), dtype=torch.int32)
