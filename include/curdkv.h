@@ -483,8 +483,9 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
  *   scale      finite, >= 0
  * Rows of K at or beyond n_b and query rows at or beyond t_b may hold anything, the others must be finite.  Products are
  * those of bf16 numbers summed in fp32, exponentials and sums fp32, added in a fixed order.  q_heads / kv_heads <= 128;
- * strides below 2^39 bytes.  Up to four launches.  Workspace (256-byte aligned): its status word collects (it is not
- * cleared) CURDKV_DEV_TIMEOUT; two calls that may overlap need a workspace each. */
+ * strides below 2^39 bytes.  Up to four launches.  Workspace (256-byte aligned; the size for some batch, n_max and q_rows serves
+ * calls of no larger ones): its status word collects (it is not cleared) CURDKV_DEV_TIMEOUT; two calls that may overlap
+ * need a workspace each. */
 size_t curdkv_attention_scores_workspace_bytes(const curdkv_desc* desc, int32_t q_rows);
 curdkv_status curdkv_attention_scores(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_n,
                                       const int32_t* q_lens, const void* K, const curdkv_desc* desc, float scale, float* lse,
@@ -518,8 +519,9 @@ curdkv_status curdkv_cache_push(const curdkv_cache* cache, const void* K_new, co
  *   scale     finite, >= 0
  * q_rows * (q_heads / kv_heads) <= 1024.  A query that sees nothing gives O = 0, lse = -inf and no weight.  Held rows and live
  * queries must be finite.  Softmax and sums in fp32, weights added in a fixed order; a weight is rounded to bf16 before it multiplies the
- * values, O is rounded once.  One launch, or two.  Workspace (256-byte aligned): its status word collects (it is not cleared)
- * CURDKV_DEV_BAD_INDEX, a count out of range; two calls that may overlap need a workspace each. */
+ * values, O is rounded once.  One launch, or two.  Workspace (256-byte aligned; the size for some batch, capacity and q_rows serves
+ * calls of no larger ones): its status word collects (it is not cleared) CURDKV_DEV_BAD_INDEX, a count out of range; two calls
+ * that may overlap need a workspace each. */
 size_t curdkv_cache_attention_workspace_bytes(const curdkv_cache* cache, const curdkv_desc* desc, int32_t q_rows);
 curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_n,
                                      const int32_t* q_lens, const curdkv_cache* cache, const curdkv_desc* desc, float scale,
@@ -542,9 +544,9 @@ curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_st
  * Meant for generation, few tokens a sequence: own rows are read once for every 16 of its query rows.  A query that sees
  * nothing gives O = 0 and lse = -inf.  Rows at or beyond a length may hold anything, the others must be finite.  Softmax and
  * sums in fp32, weights rounded to bf16 before they multiply the values, O rounded once; parts are joined in a fixed
- * order.  Up to three launches.  Workspace (256-byte aligned): its status word collects (it is not cleared)
- * CURDKV_DEV_BAD_INDEX, a length out of range (it is cut), and CURDKV_DEV_TIMEOUT; two calls that may overlap need a
- * workspace each. */
+ * order.  Up to three launches.  Workspace (256-byte aligned; the size for some prefixes, sequences a prefix, rows of either and
+ * q_rows serves calls of no larger ones): its status word collects (it is not cleared) CURDKV_DEV_BAD_INDEX, a length out
+ * of range (it is cut), and CURDKV_DEV_TIMEOUT; two calls that may overlap need a workspace each. */
 size_t curdkv_attention_prefix_workspace_bytes(const curdkv_desc* desc_prefix, const curdkv_desc* desc, int32_t q_rows);
 curdkv_status curdkv_attention_prefix(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_n,
                                       const int32_t* q_lens, const void* K_prefix, const void* V_prefix,

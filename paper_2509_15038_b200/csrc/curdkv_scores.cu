@@ -46,11 +46,24 @@ bool plan_scores(const curdkv_desc* d, int32_t q_rows, ScoresPlan* pl) {
   const int64_t whole = before / (2 * kTileRows);                             // pairs of key tiles that every token sees
   pl->key_seg = unit_length(P * (whole * pl->row_tiles + (key_pairs - whole) * (pl->row_tiles + 1) / 2));
   pl->key_segs = (pl->row_tiles + pl->key_seg - 1) / pl->key_seg;
-  const size_t rows = (size_t)P * pl->row_tiles * kTileRows;
+  // Room for the most that any call of no larger sizes leaves: shorter ones may be cut into more units (the last 32 of 2305 rows
+  // into 19, of 2369 into 10).  With U = 12 n units aimed at on n SMs and S steps in all, a unit has at least S / U of them (S / n
+  // below twelve), and the tiles of all pairs, row_tiles x key_tiles each, are at most 4 S: the rows pass leaves 4 U parts and one
+  // for each row tile at most, 2 U and one of a single row tile.
+  const int64_t n = sms(), row_all = P * pl->row_tiles, units = (pl->row_tiles > 1 ? 48 : 24) * n + row_all;
+  const int64_t row_parts = row_all * pl->key_tiles < units ? row_all * pl->key_tiles : units;
   pl->stats_at = 512;                                      // (status word, and at 256 the two passes' counters)
-  pl->logsum_at = pl->stats_at + round256(rows * pl->row_segs * 2 * sizeof(float2));
-  pl->parts_at = pl->logsum_at + round256(rows * sizeof(float));
-  pl->bytes = pl->parts_at + (pl->key_segs > 1 ? round256((size_t)P * pl->key_segs * 2 * d->n_max * sizeof(float)) : 0);
+  pl->logsum_at = pl->stats_at + round256((size_t)row_parts * kTileRows * 2 * sizeof(float2));
+  pl->parts_at = pl->logsum_at + round256((size_t)row_all * kTileRows * sizeof(float));
+  // The columns pass has pairs x row_tiles <= 2 S: at most 2 U parts and one a pair.  Twelve row tiles or fewer are one unit, and
+  // so no part, but where S / n is below twelve: 4 n at most.
+  int64_t key_parts = 0;
+  if (pl->row_tiles > 1) {
+    key_parts = P * key_pairs * pl->row_tiles;
+    const int64_t most = pl->row_tiles <= 12 ? 4 * n : 24 * n + P * key_pairs;
+    if (key_parts > most) key_parts = most;
+  }
+  pl->bytes = pl->parts_at + (size_t)key_parts * 2 * 2 * kTileRows * sizeof(float);
   return P * row_pairs * pl->row_segs <= 0x7fffffff && P * key_pairs * pl->key_segs <= 0x7fffffff && P * ((d->n_max + 255) / 256) <= 0x7fffffff;
 }
 

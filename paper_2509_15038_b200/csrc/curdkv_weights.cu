@@ -16,8 +16,25 @@ using namespace curdkv::host;
 // How the keys of `problems` KV heads with `query_rows` query rows each are cut into parts.
 struct RowsPlan {
   int nt, blocks, chunk, chunks;
-  size_t entries;                    // query rows of all parts
+  size_t entries, most;              // query rows of all parts; and at most, of any call of no larger sizes
 };
+
+// Parts at most of up to `items` items of up to `keys` keys.  What plan_rows makes of shorter or fewer ones can be more parts
+// (one key fewer, a step less a part: 37 of 128 keys for 4736, 25 of 192 for 4737), so a size that is to serve them too has to come
+// from bounds: `slots` parts, or four rounds of them for long caches, of at least 128 keys each; six rounds and a part an
+// item, of at least 512 keys, for more items.  Each grows with items and keys.
+int64_t most_parts(int64_t items, int64_t keys) {
+  const int64_t slots = 2 * (int64_t)sms();
+  if (items < 1) items = 1;
+  auto of = [](int64_t n, int64_t each) { return n > 0 ? (n + each - 1) / each : 1; };
+  auto few = [&](int64_t n) {
+    const int64_t rounds = keys / (4 * slots / n) >= 2048 ? 4 * slots : slots, all = n * of(keys, 128);
+    return all < rounds ? all : rounds;
+  };
+  if (items <= slots) return few(items);
+  const int64_t rounds = 6 * slots + items, all = items * of(keys, 512), many = all < rounds ? all : rounds, less = few(slots);
+  return many > less ? many : less;
+}
 
 // As many parts as fill the device (two CTAs an SM) when heads are few, so that a head's keys are read by many SMs, and four
 // rounds of them while each has 2048 keys (64 heads of 65540 rows, 8 query rows: 421 us instead of 440); several
@@ -39,6 +56,7 @@ RowsPlan plan_rows(int64_t problems, int64_t query_rows, int64_t keys, int nt = 
   pl.chunk = (int)chunk;
   pl.chunks = (int)chunks;
   pl.entries = (size_t)items * chunks * 8 * pl.nt;
+  pl.most = (size_t)most_parts(items, keys) * 8 * pl.nt;
   return pl;
 }
 
@@ -152,7 +170,7 @@ bool plan_cache(const curdkv_cache* c, const curdkv_desc* d, int32_t q_rows, Cac
   if (slices > most) slices = most;
   pl->slices = (int)slices;
   pl->parts_at = 256;
-  pl->logits_at = pl->parts_at + parts_bytes(pl->rows.entries);
+  pl->logits_at = pl->parts_at + parts_bytes(pl->rows.most);
   pl->bytes = pl->logits_at + round256((size_t)P * pl->rows.blocks * c->capacity * pl->pitch * sizeof(float));
   return true;
 }
@@ -205,19 +223,20 @@ bool plan_prefix(const curdkv_desc* dp, const curdkv_desc* d, int32_t q_rows, Pr
   pl->own = plan_rows(P, rows, d->n_max, pl->pre.nt);      // (both may be one launch)
   if (rows * share > 16) pl->own = plan_rows(P, rows, d->n_max);
   pl->tiles = P0 > 0 && rows * share > 16 && group <= kTileRows && dp->n_max > 0;
-  size_t entries = pl->pre.entries;
+  size_t entries = pl->pre.most;
   if (pl->tiles) {
     plan_tiles(P0, (int)share, q_rows, group, dp->n_max, 512. * (double)P * d->n_max * ((rows + 15) / 16), pl);
-    // as many parts as any own rows could lead to: a workspace for long ones serves short ones too
-    const int64_t items = P0 * ((pl->row_tiles + 1) / 2), key_tiles = ((int64_t)dp->n_max + kTileRows - 1) / kTileRows;
-    int64_t most = 2 * (int64_t)sms() / items + 2;
-    if (most > key_tiles) most = key_tiles;
-    const size_t tiles = (size_t)P0 * pl->row_tiles * most * kTileRows;
+    // as many parts as any own rows, and any fewer and shorter prefixes, could lead to (plan_tiles' runs of CTAs, a pair of
+    // tiles or a single one each)
+    const int64_t row_tiles = P0 * pl->row_tiles, key_tiles = ((int64_t)dp->n_max + kTileRows - 1) / kTileRows;
+    const int64_t runs = (pl->row_tiles > 1 ? 4 : 2) * (int64_t)sms() + 2 * row_tiles, all = row_tiles * key_tiles;
+    const size_t tiles = (size_t)(all < runs ? all : runs) * kTileRows;
     if (tiles > entries) entries = tiles;                  // (rows that the maps cannot hold take the other form)
   }
   pl->pre_at = 256;
   pl->own_at = pl->pre_at + parts_bytes(entries);
-  pl->bytes = pl->own_at + parts_bytes(pl->own.entries);
+  // (blocks of 8 query rows turn into such of 16 and back as sequences join)
+  pl->bytes = pl->own_at + parts_bytes((size_t)most_parts(P * ((rows + 15) / 16), d->n_max) * 16);
   return true;
 }
 

@@ -100,3 +100,38 @@ def test_streams_side_by_side():
     for g, w in zip(got, want):
         assert all(torch.equal(x, w) for x in g)
     assert all(cur.curdkv_device_status(x) == 0 for x in ws)
+
+
+def test_one_workspace_for_all_shorter_calls():
+    """A workspace of the size for the longest rows, in calls of shorter ones that are cut into more parts: the results of calls with
+    one of their own."""
+    rows = [1, 127, 129, 2305, 2368, 4736, 4737, 9000]
+    K, Q = weights._rand((1, 2, 9000, 128), 1400), weights._rand((1, 8, 32, 128), 1401)
+    full = cur.make_desc(K, K, 1, q_heads=8)
+    ws_s = cur.attention_scores_workspace(full, 32)
+    d0, ws_p = cur.make_desc(K[:, :, :300], K[:, :, :300], 1), None
+    for n in reversed(rows):
+        x = K[:, :, :n]
+        d = cur.make_desc(x, x, 1, q_heads=8)
+        want = cur.curdkv_attention_scores(Q, x, d, scale=SCALE)[0]
+        assert torch.equal(cur.curdkv_attention_scores(Q, x, d, scale=SCALE, workspace=ws_s)[0], want)
+        for t in (1, 3):
+            q = Q[:, :, :t]
+            if ws_p is None:
+                ws_p = cur.attention_prefix_workspace(d0, d, 3)
+                ws_0 = cur.attention_prefix_workspace(cur.make_desc(x, x, 1), cur.make_desc(x, x, 1, q_heads=8), 3)
+            want = cur.curdkv_attention_prefix(q, K[:, :, :300], K[:, :, :300], d0, x, x, d, scale=SCALE)[0]
+            assert torch.equal(cur.curdkv_attention_prefix(q, K[:, :, :300], K[:, :, :300], d0, x, x, d, scale=SCALE, workspace=ws_p)[0], want)
+            want = cur.curdkv_attention_prefix(q, x, x, cur.make_desc(x, x, 1), x, x, d, scale=SCALE)[0]
+            assert torch.equal(cur.curdkv_attention_prefix(q, x, x, cur.make_desc(x, x, 1), x, x, d, scale=SCALE, workspace=ws_0)[0], want)
+    c = weights._cache(1, 2, 9000, [9000], 1402)
+    ws_c = cur.cache_attention_workspace(c, 8, 3)
+    for n in rows:
+        short = cur.DeviceCache.of(*(x[:, :, :n].contiguous() for x in (c.K, c.V, c.raw, c.pos)), torch.full_like(c.count, n), c.total)
+        for t in (1, 3):
+            w, v = torch.zeros_like(short.raw), torch.zeros_like(short.raw)
+            want = cur.curdkv_cache_attention(Q[:, :, :t], short, scale=SCALE, weights=w)[0]
+            assert torch.equal(cur.curdkv_cache_attention(Q[:, :, :t], short, scale=SCALE, weights=v, workspace=ws_c)[0], want)
+            assert torch.equal(v, w)
+    for ws in (ws_s, ws_p, ws_0, ws_c):
+        assert cur.curdkv_device_status(ws) == 0

@@ -105,6 +105,59 @@ def test_a_prefix_workspace_for_long_own_rows_serves_short_ones(share, group, t)
         assert all(a <= sizes[-1] for a in sizes), sizes
 
 
+def _lengths(most):
+    return [*range(min(most, 300)), *range(300, most, 61), *(x for e in range(5, 18) for x in (2 ** e - 1, 2 ** e, 2 ** e + 1) if x < most), most]
+
+
+@pytest.mark.parametrize("heads,group,share", [(8, 4, 1), (1, 1, 1), (8, 4, 8), (2, 8, 64), (16, 1, 16), (1, 128, 3), (4, 200, 2)])
+def test_a_workspace_for_the_largest_sizes_serves_all_smaller_ones(heads, group, share):
+    """Along every axis, densely, from several places: no call asks for more than one that is no smaller in anything."""
+    lib, r = cur.load(), ctypes.byref
+
+    def desc(batch, n):
+        return _desc(batch=batch, kv_heads=heads, q_heads=heads * group, n_max=n)
+
+    def prefix(prefixes=1, seqs=share, n0=1000, n=100, t=1):
+        return lib.curdkv_attention_prefix_workspace_bytes(r(desc(prefixes, n0)), r(desc(prefixes * seqs, n)), t)
+
+    def cache(batch=1, capacity=2049, t=1):
+        return lib.curdkv_cache_attention_workspace_bytes(r(_cache(capacity=capacity)), r(desc(batch, 0)), t)
+
+    def scores(batch=1, n=2000, t=32):
+        return lib.curdkv_attention_scores_workspace_bytes(r(desc(batch, n)), t)
+
+    def grows(size, axis, values, **at):
+        values = sorted(set(values))
+        sizes = [size(**{axis: x}, **at) for x in values]
+        assert min(sizes) >= 256
+        for a, b, x in zip(sizes, sizes[1:], values[1:]):
+            assert a <= b, (axis, x, at, a, b)
+
+    long, counts = _lengths(40000), range(1, 300)
+    for t in (1, 5):
+        grows(prefix, "n", long, t=t)
+        grows(prefix, "n", long, t=t, n0=0)
+        grows(prefix, "n0", long, t=t)
+        grows(prefix, "n0", long, t=t, n=5000)
+    grows(prefix, "t", counts, n0=20000)
+    grows(prefix, "t", counts, n0=100, n=3000)
+    grows(prefix, "seqs", counts)
+    grows(prefix, "seqs", counts, n0=30000, n=700)
+    grows(prefix, "prefixes", counts, n0=3000)
+    grows(cache, "capacity", long[1:])
+    grows(cache, "capacity", long[1:], t=3)
+    grows(cache, "batch", counts)
+    grows(cache, "t", range(1, 1024 // group + 1))
+    if group <= 128:
+        grows(scores, "n", long)
+        grows(scores, "n", long, t=2000)
+        grows(scores, "t", long[1:])
+        grows(scores, "t", long[1:], n=30000)
+        grows(scores, "batch", counts)
+        if (heads, group) == (8, 4):
+            grows(lambda n: scores(n=n, t=max(n, 1)), "n", long)
+
+
 def test_calls_on_nothing():
     """A batch of none is an answer, not an error."""
     assert _push(d=_desc(batch=0)) == 0
