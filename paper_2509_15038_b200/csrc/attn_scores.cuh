@@ -16,8 +16,8 @@
 // few tokens of many heads fill a tile, and little of a tile lies beyond the diagonal.
 //
 // What bounds it: the special function units, 16 exponentials a clock and SM, two tiles' 2 x 1024 cycles a step; they are busy
-// 74 to 81 % of the time, the tensor pipe 43 to 46 %, and the clock falls to 1.62 GHz beside them.  One pair of exponentials in
-// eight runs on the FMA pipe: issue slots are 55 % taken, and with two in eight what the units gain is lost there.  8192
+// 74 to 81 % of the time, the tensor pipe 43 to 46 %, and the clock falls to 1.62 GHz beside them.  In the rows pass one pair of
+// exponentials in eight runs on the FMA pipe: issue slots are 55 % taken, and with two in eight what the units gain is lost there.  8192
 // tokens, 32 / 8 heads: 327 us with log sums at hand (840 TFLOP/s over the visible pairs), 635 without; 64 tokens over 4 x 8
 // heads of 32768 rows 178 us, the keys read twice.
 // Measured and dropped: A in TMEM, brought there by the epilogue warps (345 us where shared memory gave 350 at the time: the
@@ -66,7 +66,9 @@ constexpr int kScoreDynamic = kScoreBar + 512 + 1024;
 constexpr int kScoreTmemCols = 512;                        // S of A tile g, buffer u at 128 (2 g + u)
 constexpr int kScoreUnits = 3;                             // units told ahead
 constexpr float kScoreSlack = 8.f;
-constexpr int kScorePoly = 1;                              // of 8 pairs of exponentials, how many the FMA pipe takes
+// Of 8 pairs of exponentials in the rows pass, how many the FMA pipe takes.  None in the columns pass, where they gained nothing
+// (8192 tokens 365 us without, 367 with one) and where a caller's log sums may leave x beyond what that form takes.
+constexpr int kScorePoly = 1;
 
 // The live query tokens of a sequence and where they stand.
 struct ScoreSeq {
@@ -421,7 +423,7 @@ score_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 for (int i = 0; i < 2; ++i) {
                   const int j = (e >> 1) + i;
                   const uint64_t x2 = fma2(pack2(w[2 * j], w[2 * j + 1]), sc2, i == 0 ? pack2(l4.x, l4.y) : pack2(l4.z, l4.w));
-                  part[j & 3] = add2(part[j & 3], j % 8 < kScorePoly ? exp2_pair_fma(x2) : exp2_pair(x2));
+                  part[j & 3] = add2(part[j & 3], exp2_pair(x2));
                 }
               }
             }

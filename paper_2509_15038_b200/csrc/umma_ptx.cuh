@@ -233,6 +233,11 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
 __device__ __forceinline__ uint64_t sub2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
@@ -245,12 +250,17 @@ __device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
 }
 // The same on the FMA and integer pipes, for kernels that the special function units hold back: x = n + f with n whole and
 // |f| <= 1/2 (adding 1.5 * 2^23 rounds to whole numbers and leaves n in the low bits), 2^f as a polynomial (least
-// greatest relative error with constant term 1, found by reweighted least squares: 1.7e-7 in fp32), n added to the exponent.
-// x below -127 gives 0; x at most 126.
+// greatest relative error with constant term 1, found by reweighted least squares: 1.7e-7 in fp32), times a float of exponent
+// n.  x below -126.5 gives 0, and a NaN stays one, as on the special function units; x at most 127.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float c;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(c) : "f"(a), "f"(b));
+  return c;
+}
 __device__ __forceinline__ uint64_t exp2_pair_fma(uint64_t x) {
   float a, b;
   unpack2(x, a, b);
-  x = pack2(fmaxf(a, -127.f), fmaxf(b, -127.f));
+  x = pack2(max_nan(a, -127.f), max_nan(b, -127.f));
   const uint64_t magic = pack2(12582912.f, 12582912.f);
   const uint64_t t = add2(x, magic), f = sub2(x, sub2(t, magic));
   uint64_t p = pack2(0x1.5bba14p-10f, 0x1.5bba14p-10f);
@@ -259,11 +269,10 @@ __device__ __forceinline__ uint64_t exp2_pair_fma(uint64_t x) {
   p = fma2(p, f, pack2(0x1.ebf9bcp-3f, 0x1.ebf9bcp-3f));
   p = fma2(p, f, pack2(0x1.62e42ap-1f, 0x1.62e42ap-1f));
   p = fma2(p, f, pack2(1.f, 1.f));
-  float p0, p1, t0, t1;
-  unpack2(p, p0, p1);
+  float t0, t1;
   unpack2(t, t0, t1);
-  return pack2(__int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23)),
-               __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23)));
+  const int one = 127 << 23;                               // (n = -127: a factor of 0)
+  return mul2(p, pack2(__int_as_float((__float_as_int(t0) << 23) + one), __int_as_float((__float_as_int(t1) << 23) + one)));
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;

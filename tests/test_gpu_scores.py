@@ -221,3 +221,54 @@ def test_prompt_to_generation():
                 grown = cache.raw[b, h, :budget].cpu().numpy() - mid[b, h, :budget].cpu().numpy().astype(np.float64)
                 assert np.all(np.abs(grown - w.sum((0, 1))) <= 1e-4 * w.sum((0, 1)) + 2.0 ** -22 * (1 + mid[b, h, :budget].cpu().numpy()))
     assert cur.curdkv_device_status(wsp) == 0 and cur.curdkv_device_status(wsa) == 0 and cur.curdkv_device_status(ws) == 0
+
+
+@pytest.mark.parametrize("t,lse", [(300, False), (300, True), (40, False), (40, True)])
+def test_a_nan_reaches_every_row_that_it_should(t, lse):
+    """Wherever it stands in a tile: one in a query makes the scores of all rows that it sees NaN and leaves the others as they are,
+    one in a key the log sums of the tokens that see it, and the scores of the rows that these see."""
+    n = 300
+    K, Q = _rand((1, 1, n, 128), 300), _rand((1, 4, t, 128), 301)
+
+    def call(Q, K):
+        out = torch.zeros((1, 4, t), device=DEV) if lse else None
+        return cur.curdkv_attention_scores(Q, K, cur.make_desc(K, K, 1, q_heads=4, raw_scores=1), scale=SCALE, lse=out)[0], out
+
+    clean, clean_lse = call(Q, K)
+    assert clean.isfinite().all()
+    for i in [*range(9), 16, 31, t - 1]:                     # rows 4 i + head of a tile: each of 16 columns, and further tiles
+        for head in range(4):
+            q = Q.clone()
+            q[0, head, i, 5] = float("nan")
+            got, sums = call(q, K)
+            sees = n - t + i + 1
+            assert got[0, 0, :sees].isnan().all() and torch.equal(got[0, 0, sees:], clean[0, 0, sees:]), (i, head)
+            if lse:
+                assert sums[0, head, i].isnan()
+                sums[0, head, i] = clean_lse[0, head, i]
+                assert torch.equal(sums, clean_lse)
+    for j in [*range(18), 64, 65, 66, 255, n - 1]:
+        k = K.clone()
+        k[0, 0, j, 77] = float("nan")
+        got, sums = call(Q, k)
+        assert got.isnan().all(), j                          # (the last token sees every row)
+        if lse:
+            first = max(0, j - (n - t))
+            assert sums[0, :, first:].isnan().all() and torch.equal(sums[0, :, :first], clean_lse[0, :, :first]), j
+
+
+@pytest.mark.parametrize("n,t", [(300, 300), (300, 40)])
+def test_a_log_sum_far_too_low_gives_nothing_finite(n, t):
+    """Weights of some 2^144 in one query row, wherever it stands in a tile: infinite scores (or NaN) of all rows that it sees, no
+    numbers of either sign; the other rows' scores as they are."""
+    K, Q = _rand((1, 1, n, 128), 310), _rand((1, 4, t, 128), 311)
+    desc, lse = cur.make_desc(K, K, 1, q_heads=4), torch.zeros((1, 4, t), device=DEV)
+    cur.curdkv_attention_scores(Q, K, desc, scale=SCALE, lse=lse)
+    clean = cur.curdkv_attention_scores(Q, K, desc, scale=SCALE, lse=lse, lse_given=True)[0]
+    for i in (0, 1, 2, 3, 4, 17, t - 1):
+        for head in range(4):
+            low = lse.clone()
+            low[0, head, i] = -100.0
+            got = cur.curdkv_attention_scores(Q, K, desc, scale=SCALE, lse=low, lse_given=True)[0]
+            sees = n - t + i + 1
+            assert not got[0, 0, :sees].isfinite().any() and torch.equal(got[0, 0, sees:], clean[0, 0, sees:]), (i, head)
