@@ -519,10 +519,15 @@ curdkv_status curdkv_cache_push(const curdkv_cache* cache, const void* K_new, co
  *   scale     finite, >= 0
  * q_rows * (q_heads / kv_heads) <= 1024.  A query that sees nothing gives O = 0, lse = -inf and no weight.  Held rows and live
  * queries must be finite.  Softmax and sums in fp32, weights added in a fixed order; a weight is rounded to bf16 before it multiplies the
- * values, O is rounded once.  One launch, or two.  Workspace (256-byte aligned; the size for some batch, capacity and q_rows serves
- * calls of no larger ones): its status word collects (it is not cleared) CURDKV_DEV_BAD_INDEX, a count out of range; two calls
- * that may overlap need a workspace each. */
+ * values, O is rounded once.  One launch, or two.  Workspace (256-byte aligned): its status word collects (it is not cleared)
+ * CURDKV_DEV_BAD_INDEX, a count out of range; two calls that may overlap need a workspace each.
+ *   _workspace_bytes       serves every call of no larger batch, capacity and q_rows.  Most of it is room for logits, 4 bytes a
+ *                          row and query row: at 64 query rows a KV head half of the cache's size, at 1024 eight times it
+ *   _call_workspace_bytes  what one call with these sizes, with weights or without, uses of it: no logits without weights, 256
+ *                          bytes where it is one launch (a smaller call may use more) */
 size_t curdkv_cache_attention_workspace_bytes(const curdkv_cache* cache, const curdkv_desc* desc, int32_t q_rows);
+size_t curdkv_cache_attention_call_workspace_bytes(const curdkv_cache* cache, const curdkv_desc* desc, int32_t q_rows,
+                                                   int32_t with_weights);
 curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_n,
                                      const int32_t* q_lens, const curdkv_cache* cache, const curdkv_desc* desc, float scale,
                                      void* O, int64_t o_stride_b, int64_t o_stride_h, int64_t o_stride_n, float* lse,

@@ -35,7 +35,8 @@ EXPORTS = (
     "curdkv_qcache_store", "curdkv_qcache_append", "curdkv_qcache_read",
     "curdkv_qcache_attention_workspace_bytes", "curdkv_qcache_attention",
     "curdkv_attention_window_workspace_bytes", "curdkv_attention_window",
-    "curdkv_cache_push", "curdkv_cache_attention_workspace_bytes", "curdkv_cache_attention",
+    "curdkv_cache_push", "curdkv_cache_attention_workspace_bytes", "curdkv_cache_attention_call_workspace_bytes",
+    "curdkv_cache_attention",
     "curdkv_attention_prefix_workspace_bytes", "curdkv_attention_prefix",
     "curdkv_attention_scores_workspace_bytes", "curdkv_attention_scores",
 )
@@ -162,6 +163,8 @@ def load():
     lib.curdkv_cache_push.argtypes = [cp, vp, vp, vp, dp, i32, i32, i32, vp, ctypes.c_size_t, vp]
     lib.curdkv_cache_attention_workspace_bytes.restype = ctypes.c_size_t
     lib.curdkv_cache_attention_workspace_bytes.argtypes = [cp, dp, i32]
+    lib.curdkv_cache_attention_call_workspace_bytes.restype = ctypes.c_size_t
+    lib.curdkv_cache_attention_call_workspace_bytes.argtypes = [cp, dp, i32, i32]
     lib.curdkv_cache_attention.restype = ctypes.c_int
     lib.curdkv_cache_attention.argtypes = [vp, i32, i64, i64, i64, vp, cp, dp, f32, vp, i64, i64, i64, vp, vp, vp,
                                            ctypes.c_size_t, vp]
@@ -894,11 +897,20 @@ def _cache_desc(cache: DeviceCache, q_heads: int):
     return ref
 
 
-def cache_attention_workspace(cache: DeviceCache, q_heads: int, q_rows: int) -> torch.Tensor:
-    nbytes = int(load().curdkv_cache_attention_workspace_bytes(cache._ref, _cache_desc(cache, int(q_heads)), int(q_rows)))
+def cache_attention_workspace(cache: DeviceCache, q_heads: int, q_rows: int, *,
+                              weights: Optional[bool] = None) -> torch.Tensor:
+    """For every call of no more tokens on caches that are no larger; with ``weights`` True or False only for calls of
+    exactly these sizes that ask for weights or do not (much less where logits need no room)."""
+    args = cache._ref, _cache_desc(cache, int(q_heads)), int(q_rows)
+    if weights is None:
+        nbytes = int(load().curdkv_cache_attention_workspace_bytes(*args))
+    else:
+        nbytes = int(load().curdkv_cache_attention_call_workspace_bytes(*args, int(bool(weights))))
     if nbytes == 0:
         raise ValueError("invalid shape for curdkv_cache_attention")
-    return torch.zeros((nbytes,), dtype=torch.uint8, device=cache.K.device)
+    ws = torch.empty((nbytes,), dtype=torch.uint8, device=cache.K.device)
+    ws[:256].zero_()                                         # (the rest is written before it is read)
+    return ws
 
 
 def curdkv_cache_attention(Q, cache: DeviceCache, *, scale: float, weights: Optional[torch.Tensor] = None,

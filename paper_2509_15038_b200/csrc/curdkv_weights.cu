@@ -175,6 +175,10 @@ bool plan_cache(const curdkv_cache* c, const curdkv_desc* d, int32_t q_rows, Cac
   return true;
 }
 
+// Of a workspace, what one call uses: logits only where weights are asked for, and where a cluster keeps everything nothing but the
+// status word.
+size_t call_bytes(const CachePlan& pl, bool weights) { return pl.cluster > 0 ? 256 : (weights ? pl.bytes : pl.logits_at); }
+
 // ---- attention behind a shared prefix ----------------------------------------------------------
 struct PrefixPlan {
   RowsPlan pre, own;
@@ -249,6 +253,12 @@ size_t curdkv_cache_attention_workspace_bytes(const curdkv_cache* cache, const c
   return plan_cache(cache, desc, q_rows, &pl) ? pl.bytes : 0;
 }
 
+size_t curdkv_cache_attention_call_workspace_bytes(const curdkv_cache* cache, const curdkv_desc* desc, int32_t q_rows,
+                                                   int32_t with_weights) {
+  CachePlan pl;
+  return plan_cache(cache, desc, q_rows, &pl) ? call_bytes(pl, with_weights != 0) : 0;
+}
+
 curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_stride_b, int64_t q_stride_h, int64_t q_stride_n,
                                      const int32_t* q_lens, const curdkv_cache* cache, const curdkv_desc* desc, float scale,
                                      void* O, int64_t o_stride_b, int64_t o_stride_h, int64_t o_stride_n, float* lse,
@@ -262,7 +272,7 @@ curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_st
   if (workspace == nullptr || !status_ok(workspace)) return CURDKV_ERR_INVALID_ARG;
   CachePlan pl;
   if (!plan_cache(cache, desc, q_rows, &pl)) return CURDKV_ERR_UNSUPPORTED;
-  if (workspace_bytes < pl.bytes) return CURDKV_ERR_WORKSPACE;
+  if (workspace_bytes < call_bytes(pl, weights != nullptr)) return CURDKV_ERR_WORKSPACE;
   const int64_t P = (int64_t)desc->batch * desc->kv_heads;
   if (P == 0) return CURDKV_OK;
   const int64_t ctas = pl.cluster > 0 ? P * pl.cluster : P * pl.rows.blocks * pl.rows.chunks;

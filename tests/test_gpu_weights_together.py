@@ -135,3 +135,20 @@ def test_one_workspace_for_all_shorter_calls():
             assert torch.equal(v, w)
     for ws in (ws_s, ws_p, ws_0, ws_c):
         assert cur.curdkv_device_status(ws) == 0
+
+
+@pytest.mark.parametrize("B,H,group,cap,t", [(1, 2, 4, 300, 1), (1, 8, 4, 1703, 1), (40, 8, 4, 2049, 1), (1, 2, 4, 40001, 1), (2, 2, 8, 700, 5)])
+def test_a_workspace_of_what_one_call_uses(B, H, group, cap, t):
+    """With weights and without: the same results, and not a byte behind it touched."""
+    c, Q = weights._cache(B, H, cap, [cap - b % 3 for b in range(B)], 1500), weights._rand((B, H * group, t, 128), 1501)
+    for ask in (True, False):
+        w = torch.zeros_like(c.raw) if ask else None
+        want = cur.curdkv_cache_attention(Q, c, scale=SCALE, weights=w)[0]
+        size = cur.cache_attention_workspace(c, H * group, t, weights=ask).numel()
+        assert size <= cur.cache_attention_workspace(c, H * group, t).numel()
+        buf = torch.full((size + 4096,), 7, dtype=torch.uint8, device=DEV)
+        buf[:256] = 0
+        v = torch.zeros_like(c.raw) if ask else None
+        got = cur.curdkv_cache_attention(Q, c, scale=SCALE, weights=v, workspace=buf[:size])[0]
+        assert torch.equal(got, want) and torch.all(buf[size:] == 7) and cur.curdkv_device_status(buf) == 0
+        assert not ask or torch.equal(v, w)

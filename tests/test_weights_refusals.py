@@ -158,6 +158,24 @@ def test_a_workspace_for_the_largest_sizes_serves_all_smaller_ones(heads, group,
             grows(lambda n: scores(n=n, t=max(n, 1)), "n", long)
 
 
+@pytest.mark.parametrize("batch,group,capacity,t", [(1, 4, 64, 1), (64, 4, 2049, 1), (20, 4, 2049, 1), (4, 2, 65540, 4), (1, 64, 3000, 1), (1, 4, 900, 256)])
+def test_a_cache_attention_asks_for_what_it_uses(batch, group, capacity, t):
+    """Logits have room only where weights are asked for and memory has to hold them, the status word is all that one launch
+    needs, and a call takes just that."""
+    lib, r = cur.load(), ctypes.byref
+    c, d = _cache(capacity=capacity), _desc(batch=batch, q_heads=2 * group)
+    whole = lib.curdkv_cache_attention_workspace_bytes(r(c), r(d), t)
+    with_weights, without = (lib.curdkv_cache_attention_call_workspace_bytes(r(c), r(d), t, w) for w in (1, 0))
+    logits = 4 * 2 * batch * capacity * max(2, -(-group * t // 4) * 4)
+    assert 256 <= without <= with_weights <= whole and whole >= logits
+    assert with_weights == whole if without > 256 else with_weights == 256
+    assert without <= whole - logits
+    strides = (group * 2 * t * 128, t * 128, 128)
+    for weights, need in ((ANY, with_weights), (None, without)):
+        assert _attend(c=c, d=d, rows=t, qs=strides, os=strides, weights=weights, nbytes=need - 1) == 3
+    assert lib.curdkv_cache_attention_call_workspace_bytes(r(c), r(_desc(q_heads=7)), t, 1) == 0
+
+
 def test_calls_on_nothing():
     """A batch of none is an answer, not an error."""
     assert _push(d=_desc(batch=0)) == 0
