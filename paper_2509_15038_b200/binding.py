@@ -881,6 +881,8 @@ def curdkv_cache_push(cache: DeviceCache, K_new, V_new, budget: int, workspace: 
     if scores_new is not None and (scores_new.dtype is not torch.float32 or scores_new.shape != shape[:3]
                                    or not scores_new.is_contiguous()):
         raise ValueError(f"{what}: scores_new must be contiguous fp32 {tuple(shape[:3])}")
+    if B == 0:
+        return
     desc = Desc.from_buffer_copy(_DESC(B, H, H, t, d, 1, k[0], k[1], k[2], v[0], v[1], v[2], 0 if t_new is None else t_new.data_ptr(), 0, 1, 0, 0, 0.0))
     code = load().curdkv_cache_push(cache._ref, K_new.data_ptr() or cache.K.data_ptr(), V_new.data_ptr() or cache.K.data_ptr(), _addr(scores_new),
                                     ctypes.byref(desc), index(budget), _count(num_sink), _count(window), workspace.data_ptr(),

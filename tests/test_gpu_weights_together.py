@@ -152,3 +152,17 @@ def test_a_workspace_of_what_one_call_uses(B, H, group, cap, t):
         got = cur.curdkv_cache_attention(Q, c, scale=SCALE, weights=v, workspace=buf[:size])[0]
         assert torch.equal(got, want) and torch.all(buf[size:] == 7) and cur.curdkv_device_status(buf) == 0
         assert not ask or torch.equal(v, w)
+
+
+def test_batches_of_none():
+    """No sequences: every call answers, with outputs of none."""
+    none = cur.DeviceCache(0, 2, 65, 128)
+    for t in (1, 8):
+        new, Q = torch.zeros((0, 2, t, 128), dtype=torch.bfloat16, device=DEV), torch.zeros((0, 8, t, 128), dtype=torch.bfloat16, device=DEV)
+        cur.curdkv_cache_push(none, new, new, 64, cur.cache_workspace(0, 2, t, 65, 64), num_sink=4, window=8)
+        assert cur.curdkv_cache_attention(Q, none, scale=SCALE, weights=none.raw)[0].shape == Q.shape
+        K = torch.zeros((0, 2, 50, 128), dtype=torch.bfloat16, device=DEV)
+        desc = cur.make_desc(K, K, 1, q_heads=8)
+        assert cur.curdkv_attention_scores(Q, K, desc, scale=SCALE)[0].shape == (0, 2, 50)
+        for K0 in (K, weights._rand((1, 2, 50, 128), 1600)):
+            assert cur.curdkv_attention_prefix(Q, K0, K0, cur.make_desc(K0, K0, 1), K, K, desc, scale=SCALE)[0].shape == Q.shape
