@@ -518,8 +518,8 @@ curdkv_status curdkv_cache_push(const curdkv_cache* cache, const void* K_new, co
  *   weights   NULL, or fp32 [batch][kv_heads][capacity], cache->raw for instance; only held slots are changed
  *   scale     finite, >= 0
  * q_rows * (q_heads / kv_heads) <= 1024.  A query that sees nothing gives O = 0, lse = -inf and no weight.  Held rows and live
- * queries must be finite.  Softmax and sums in fp32, weights added in a fixed order; a weight is rounded to bf16 before it multiplies the
- * values, O is rounded once.  One launch, or two.  Workspace (256-byte aligned): its status word collects (it is not cleared)
+ * queries must be finite.  Softmax and sums in fp32, weights added in a fixed order; two bf16 parts of a weight multiply the values
+ * (2^-16 of it is lost), O is rounded once.  One launch, or two.  Workspace (256-byte aligned): its status word collects (it is not cleared)
  * CURDKV_DEV_BAD_INDEX, a count out of range; two calls that may overlap need a workspace each.
  *   _workspace_bytes       serves every call of no larger batch, capacity and q_rows.  Most of it is room for logits, 4 bytes a
  *                          row and query row: at 64 query rows a KV head half of the cache's size, at 1024 eight times it
@@ -548,7 +548,8 @@ curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_st
  *   scale     finite, >= 0
  * Meant for generation, few tokens a sequence: own rows are read once for every 16 of its query rows.  A query that sees
  * nothing gives O = 0 and lse = -inf.  Rows at or beyond a length may hold anything, the others must be finite.  Softmax and
- * sums in fp32, weights rounded to bf16 before they multiply the values, O rounded once; parts are joined in a fixed
+ * sums in fp32, O rounded once; two bf16 parts of a weight multiply own values and a prefix's behind at most 16 query rows a KV
+ * head (2^-16 of the weight is lost), one part (2^-8) those of a prefix behind more; parts are joined in a fixed
  * order.  Up to three launches.  Workspace (256-byte aligned; the size for some prefixes, sequences a prefix, rows of either and
  * q_rows serves calls of no larger ones): its status word collects (it is not cleared) CURDKV_DEV_BAD_INDEX, a length out
  * of range (it is cut), and CURDKV_DEV_TIMEOUT; two calls that may overlap need a workspace each. */

@@ -11,8 +11,9 @@
 //
 // As in attn_token.cuh a warp takes 16 keys at a time from a ring that asynchronous copies fill, forms S^T = K Q^T and
 // O^T += V^T P^T with keys as the M side of m16n8k16, and moves its reference only when a logit exceeds it by more than
-// 2^slack.  Weights are rounded to bf16 before they multiply the values (half a step: 2^-8 of each), the sums take them
-// unrounded.
+// 2^slack.  Weights multiply the values as two bf16 parts each (2^-16 of each is lost), so that O's own rounding is all that is
+// left of its error; rounded to one they added a fifth to it, and the second product costs 0 to 5 % (8 heads of 1702 rows 7.9 ->
+// 8.2 us, 1024 of 2048 177.9 -> 179.1, 64 of 65540 with 8 query rows 464 -> 470 for a step).
 //
 // What bounds it: bytes.  1024 heads of 2048 rows (1.07 GB) 156 us without weights, 6.9 TB/s, and 177 with (the logits'
 // 33 MB written and read, 16 MB of weights); 64 heads of 65540 rows, 8 query rows, 311 and 416 us (134 MB of logits).  8
@@ -297,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const __grid_constant
           }
         }
     }
-    uint32_t pt[NT][2];                                    // P^T as B operand
+    uint32_t hi[NT][2], lo[NT][2];                         // P^T as B operand, in two parts
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -305,7 +306,12 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const __grid_constant
       l[nt][0] += s[nt][0] + s[nt][2];
       l[nt][1] += s[nt][1] + s[nt][3];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) pt[nt][i] = transpose8x8(pack_bf16(s[nt][2 * i], s[nt][2 * i + 1]));
+      for (int i = 0; i < 2; ++i) {
+        uint32_t a0, a1;
+        split_bf16(s[nt][2 * i], s[nt][2 * i + 1], a0, a1);
+        hi[nt][i] = transpose8x8(a0);
+        lo[nt][i] = transpose8x8(a1);
+      }
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -313,7 +319,10 @@ __global__ void __launch_bounds__(kThreads, 2) part_kernel(const __grid_constant
       const int key = (lane & 7) + ((lane >> 4) & 1) * 8, c = 2 * i + ((lane >> 3) & 1);
       ldmatrix4_trans(x, st + kKeys * 256 + key * 256 + ((c ^ (key & 7)) * 16));
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) mma_bf16(acc[nt][i], x[0], x[1], x[2], x[3], pt[nt][0], pt[nt][1]);
+      for (int nt = 0; nt < NT; ++nt) {
+        mma_bf16(acc[nt][i], x[0], x[1], x[2], x[3], hi[nt][0], hi[nt][1]);
+        mma_bf16(acc[nt][i], x[0], x[1], x[2], x[3], lo[nt][0], lo[nt][1]);
+      }
     }
     __syncwarp();                                          // the stage may be filled again
     stage = stage == kStages - 1 ? 0 : stage + 1;

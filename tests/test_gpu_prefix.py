@@ -200,3 +200,23 @@ def test_same_results_every_time_and_in_a_graph(share):
         graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(outs[0], want)
+
+
+@pytest.mark.parametrize("share,t,n0,n", [(1, 1, 40, 30), (4, 1, 700, 65), (2, 2, 300, 200), (3, 1, 0, 500), (40, 1, 0, 300), (1, 1, 9000, 0)])
+def test_weights_keep_their_bits_before_the_values(share, t, n0, n):
+    """Own rows, and prefixes behind few query rows (those that are read in tiles round weights to bf16).  Error budget: two bf16
+    parts of a weight leave 2^-16 of it; logits (in numerator and denominator), exponentials and sums as above; O rounded once."""
+    H, group = 2, 4
+    K0, V0, K, V = (_rand((1 if i < 2 else share, H, n0 if i < 2 else n, 128), 150 + i) for i in range(4))
+    Q = _rand((share, H * group, t, 128), 155)
+    d0, d = cur.make_desc(K0, V0, 1), cur.make_desc(K, V, 1, q_heads=H * group)
+    O = _f64(cur.curdkv_attention_prefix(Q, K0, V0, d0, K, V, d, scale=SCALE)[0])
+    for b in {0, share - 1}:
+        for hq in range(H * group):
+            h, q = hq // group, _f64(Q[b, hq])
+            k0, v0, k, v = _f64(K0[0, h]), _f64(V0[0, h]), _f64(K[b, h]), _f64(V[b, h])
+            want, _, w = orc.prefix_attention(q, k0, v0, k, v, SCALE)
+            e = 2.0 ** -20 * SCALE * (np.abs(q) @ np.abs(np.concatenate([k0, k])).T).max(-1)
+            tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -16 + 2 * e + 2.0 ** -18)[:, None] * (w @ np.abs(np.concatenate([v0, v]))) * (1 + 2.0 ** -7)
+            err = np.abs(O[b, hq] - want)
+            assert np.all(err <= tol), f"{(err / tol).max():.3g} of the tolerance"

@@ -335,3 +335,20 @@ def test_same_results_every_time_and_in_a_graph():
     for _ in range(3):
         graph.replay()
     same()
+
+
+@pytest.mark.parametrize("B,H,group,t,cap", [(1, 2, 4, 1, 40), (1, 8, 4, 1, 1702), (1, 2, 4, 1, 40000), (40, 8, 4, 1, 2049), (2, 2, 4, 4, 900), (1, 1, 8, 5, 700)])
+def test_weights_keep_their_bits_before_the_values(B, H, group, t, cap):
+    """Every form of the call.  Error budget of O: two bf16 parts of a weight leave 2^-16 of it; logits (in numerator and
+    denominator), exponentials and sums as above; O rounded once."""
+    c, Q = _cache(B, H, cap, [cap] * B, 900 + cap), _rand((B, H * group, t, 128), 901 + cap)
+    for weights in (None, torch.zeros_like(c.raw)):
+        O = _f64(cur.curdkv_cache_attention(Q, c, scale=SCALE, weights=weights)[0])
+        for b, h in {(0, 0), (B - 1, H - 1)}:
+            q, k, v = _f64(Q[b, h * group: (h + 1) * group]), _f64(c.K[b, h]), _f64(c.V[b, h])
+            pos = c.pos[b, h].cpu().numpy() if t > 1 else np.zeros(cap, np.int64)
+            want, _, w = orc.cache_attention(q, k, v, pos, int(c.total[b]) if t > 1 else 1, SCALE)
+            d = (2.0 ** -20 + 2.0 ** -23) * SCALE * (np.abs(q) @ np.abs(k).T).max(-1)
+            tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -16 + 2 * d + 2.0 ** -18)[..., None] * (w @ np.abs(v)) * (1 + 2.0 ** -7)
+            err = np.abs(O[b, h * group: (h + 1) * group] - want)
+            assert np.all(err <= tol), f"{(err / tol).max():.3g} of the tolerance"
