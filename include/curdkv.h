@@ -481,8 +481,10 @@ curdkv_status curdkv_attention_window(const void* Q, int32_t q_rows, int64_t q_s
  *              live tokens (-inf for one that sees nothing)
  *   scores     fp32 [batch][kv_heads][n_max]; entries j >= n_b are set to 0
  *   scale      finite, >= 0
- * Rows of K at or beyond n_b and query rows at or beyond t_b may hold anything, the others must be finite.  Products are
- * those of bf16 numbers summed in fp32, exponentials and sums fp32, added in a fixed order.  q_heads / kv_heads <= 128;
+ * Rows of K at or beyond n_b and query rows at or beyond t_b may hold anything, the others must be finite (a NaN reaches every
+ * score that depends on it).  Products are those of bf16 numbers summed in fp32, exponentials and sums fp32, added in a
+ * fixed order.  The tensor cores cut sums of products towards zero by some 1.4e-7 of them, which the scale gives back on
+ * average: with log sums from elsewhere 3 to 5e-7 of a score are left (2-norm, 8192 tokens).  q_heads / kv_heads <= 128;
  * strides below 2^39 bytes.  Up to four launches.  Workspace (256-byte aligned; the size for some batch, n_max and q_rows serves
  * calls of no larger ones): its status word collects (it is not cleared) CURDKV_DEV_TIMEOUT; two calls that may overlap
  * need a workspace each. */

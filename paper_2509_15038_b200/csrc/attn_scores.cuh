@@ -39,7 +39,7 @@ struct ScoreArgs {
   int units;                         // pairs * batch * heads * segs
   uint32_t* next_unit;               // counter, 0 before, from which the CTAs take their units behind the first
   float scale_log2;                  // scale log2(e)
-  float log2_of_ln, ln_of_log2;      // from natural log sums to L and back: log2(e) times what rounding made of scale_log2
+  float2 log2_of_ln, ln_of_log2;     // from natural log sums to L and back, in two parts each
   float2* stats;                     // rows: [segs][2][batch * heads][row_tiles][128] maximum (log2 units), sum
   const float* logsum;               // columns: [batch * heads][row_tiles][128] -L, -inf for rows that do not count
   float* out;                        // columns: [segs][2][batch * heads][n_max]; [batch * heads][n_max], 0 before, where segs = 1
@@ -548,15 +548,15 @@ __global__ void __launch_bounds__(kLogsumThreads) score_logsum_kernel(const Scor
   float L = INFINITY;
   if (sees) {
     if (given != nullptr) {
-      L = given[at] * a.log2_of_ln;
-      if (L == -INFINITY) L = INFINITY;                    // (a row that saw nothing)
+      const float g = given[at];
+      L = g == -INFINITY ? INFINITY : fmaf(g, a.log2_of_ln.x, g * a.log2_of_ln.y);           // (-inf: a row that saw nothing)
     } else {
       for (int k = 0; k < subs - 1; ++k) all.join(s_part[k][r]);
       L = all.log();
     }
   }
   logsum[((int64_t)p * a.row_tiles + tile) * kTileRows + r] = -L;
-  if (live && lse_out != nullptr) lse_out[at] = L == INFINITY ? -INFINITY : L * a.ln_of_log2;
+  if (live && lse_out != nullptr) lse_out[at] = L == INFINITY ? -INFINITY : fmaf(L, a.ln_of_log2.x, L * a.ln_of_log2.y);
 }
 
 // Sums the units' parts of each key in order.  grid = batch * heads * ceil(n_max / 256), block = 256.

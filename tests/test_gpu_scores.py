@@ -272,3 +272,24 @@ def test_a_log_sum_far_too_low_gives_nothing_finite(n, t):
             got = cur.curdkv_attention_scores(Q, K, desc, scale=SCALE, lse=low, lse_given=True)[0]
             sees = n - t + i + 1
             assert not got[0, 0, :sees].isfinite().any() and torch.equal(got[0, 0, sees:], clean[0, 0, sees:]), (i, head)
+
+
+@pytest.mark.parametrize("seed", [320, 330, 340])
+@pytest.mark.parametrize("scale", [SCALE, 0.1, 0.0625])
+def test_log_sums_in_full_precision(seed, scale):
+    """Logits up to some 12 with log sums from elsewhere, exact but for their fp32.  Error budget of the 2-norm of the scores: the
+    tensor cores cut a sum by 0.8e-7 to 1.5e-7 of it on average, of which all but 0.3e-7 is given back at the logits that carry
+    weight (12 of it: 3.6e-7), and what is random (the rest of it, and half a step of a log sum, 2^-21) averages over a hundred rows
+    and more to a tenth (0.4e-7); exponentials and sums 1e-7."""
+    n, group = 1024, 4
+    K = _rand((1, 2, n, 128), seed).float()
+    strong = torch.rand((1, 2, 1, 128), generator=torch.Generator(device=DEV).manual_seed(seed + 1), device=DEV).argsort(-1) < 4
+    K = torch.where(strong, 10.0 * K, K).to(torch.bfloat16)
+    Q = _rand((1, 2 * group, n, 128), seed + 2)
+    x = (Q.double() @ K.double().repeat_interleave(group, 1).transpose(2, 3)) * float(np.float32(scale))
+    x = x.masked_fill(torch.ones((n, n), dtype=torch.bool, device=DEV).triu(1), float("-inf"))
+    lse = torch.logsumexp(x, -1).float()
+    want = torch.exp(x - lse.double()[..., None]).sum(2).unflatten(1, (2, group)).sum(2)
+    got = cur.curdkv_attention_scores(Q, K, cur.make_desc(K, K, 1, q_heads=2 * group, raw_scores=1), scale=scale, lse=lse, lse_given=True)[0]
+    off = float((got.double() - want).norm() / want.norm())
+    assert off <= 5e-7, off
