@@ -503,7 +503,7 @@ curdkv_status curdkv_attention_scores(const void* Q, int32_t q_rows, int64_t q_s
  * Requires budget >= 1 and num_sink + window <= budget.  A cache of at most 8 rows above its budget, as generation needs,
  * takes one launch (two with more than 8 heads), whose CTAs look for the rows that leave instead of sorting, and
  * leaves slots at or beyond the new count as they were; others (capacity <= 204800) run as the calls it stands for, whose
- * evicted rows may stay behind in those slots. */
+ * evicted rows may stay behind in those slots (five launches; 16 rows to go: 1024 heads of 2064 rows 47 us, 64 of 65552 150). */
 curdkv_status curdkv_cache_push(const curdkv_cache* cache, const void* K_new, const void* V_new, const float* scores_new,
                                 const curdkv_desc* desc_new, int32_t budget, int32_t num_sink, int32_t window,
                                 void* workspace, size_t workspace_bytes, void* cuda_stream);
@@ -520,7 +520,8 @@ curdkv_status curdkv_cache_push(const curdkv_cache* cache, const void* K_new, co
  *   weights   NULL, or fp32 [batch][kv_heads][capacity], cache->raw for instance; only held slots are changed
  *   scale     finite, >= 0
  * q_rows * (q_heads / kv_heads) <= 1024.  A query that sees nothing gives O = 0, lse = -inf and no weight.  Held rows and live
- * queries must be finite.  Softmax and sums in fp32, weights added in a fixed order; two bf16 parts of a weight multiply the values
+ * queries must be finite.  Softmax and sums in fp32 (weights up to 2^6 before they are divided by their sum: values times 2^6
+ * times the rows seen have to stay within fp32), added in a fixed order; two bf16 parts of a weight multiply the values
  * (2^-16 of it is lost), O is rounded once.  One launch, or two.  Workspace (256-byte aligned): its status word collects (it is not cleared)
  * CURDKV_DEV_BAD_INDEX, a count out of range; two calls that may overlap need a workspace each.
  *   _workspace_bytes       serves every call of no larger batch, capacity and q_rows.  Most of it is room for logits, 4 bytes a
@@ -550,7 +551,8 @@ curdkv_status curdkv_cache_attention(const void* Q, int32_t q_rows, int64_t q_st
  *   scale     finite, >= 0
  * Meant for generation, few tokens a sequence: own rows are read once for every 16 of its query rows.  A query that sees
  * nothing gives O = 0 and lse = -inf.  Rows at or beyond a length may hold anything, the others must be finite.  Softmax and
- * sums in fp32, O rounded once; two bf16 parts of a weight multiply own values and a prefix's behind at most 16 query rows a KV
+ * sums in fp32 (weights up to 2^8 before they are divided by their sum: values times 2^8 times the rows seen have to stay
+ * within fp32), O rounded once; two bf16 parts of a weight multiply own values and a prefix's behind at most 16 query rows a KV
  * head (2^-16 of the weight is lost), one part (2^-8) those of a prefix behind more; parts are joined in a fixed
  * order.  Up to three launches.  Workspace (256-byte aligned; the size for some prefixes, sequences a prefix, rows of either and
  * q_rows serves calls of no larger ones): its status word collects (it is not cleared) CURDKV_DEV_BAD_INDEX, a length out

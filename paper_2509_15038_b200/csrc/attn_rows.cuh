@@ -15,10 +15,12 @@
 // left of its error; rounded to one they added a fifth to it, and the second product costs 0 to 5 % (8 heads of 1702 rows 7.9 ->
 // 8.2 us, 1024 of 2048 177.9 -> 179.1, 64 of 65540 with 8 query rows 464 -> 470 for a step).
 //
-// What bounds it: bytes.  1024 heads of 2048 rows (1.07 GB) 156 us without weights, 6.9 TB/s, and 177 with (the logits'
-// 33 MB written and read, 16 MB of weights); 64 heads of 65540 rows, 8 query rows, 311 and 416 us (134 MB of logits).  8
-// heads of 1702 rows 7.9 us: a launch, one dependent chain of loads in a cluster of eight, the join.
-// Measured and dropped: streaming hints on the logits' stores (no change); rings of three with 14 KB of logits a CTA, so
+// What bounds it: bytes.  1024 heads of 2048 rows (1.07 GB) 158 us without weights, 6.8 TB/s, and 177 with (the logits'
+// 33 MB written and read, 16 MB of weights); 64 heads of 65540 rows, 8 query rows, 315 and 424 us (134 MB of logits).  8
+// heads of 1702 rows 8.2 us: a launch, one dependent chain of loads in a cluster of eight, the join.  Beyond 16 query rows
+// keys and values are read once for every 16 of them, and logits outgrow them: 64 heads of 65540 rows with 32 rows 610 and
+// 853 us, with 256 4250 and 5830.
+// Measured and dropped (with one product a weight): streaming hints on the logits' stores (no change); rings of three with 14 KB of logits a CTA, so
 // clusters of two for 1024 heads (211 us); a warp per row for the join of many parts (53 us where four warps a row with
 // their loads ahead take 14, cold).
 #pragma once

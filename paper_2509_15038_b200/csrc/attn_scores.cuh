@@ -16,10 +16,10 @@
 // few tokens of many heads fill a tile, and little of a tile lies beyond the diagonal.
 //
 // What bounds it: the special function units, 16 exponentials a clock and SM, two tiles' 2 x 1024 cycles a step; they are busy
-// 74 to 81 % of the time, the tensor pipe 43 to 46 %, and the clock falls to 1.62 GHz beside them.  In the rows pass one pair of
-// exponentials in eight runs on the FMA pipe: issue slots are 55 % taken, and with two in eight what the units gain is lost there.  8192
-// tokens, 32 / 8 heads: 327 us with log sums at hand (840 TFLOP/s over the visible pairs), 635 without; 64 tokens over 4 x 8
-// heads of 32768 rows 178 us, the keys read twice.
+// 80 to 82 % of the time, the tensor pipe 42 to 46 %, and the clock falls to 1.65 GHz beside them.  In the rows pass one pair of
+// exponentials in eight runs on the FMA pipe: issue slots are 53 % taken, and with two in eight what the units gain is lost
+// there.  8192 tokens, 32 / 8 heads: 333 us with log sums at hand (825 TFLOP/s over the visible pairs), 635 without; 64
+// tokens over 4 x 8 heads of 32768 rows 178 us, the keys read twice.
 // Measured and dropped: A in TMEM, brought there by the epilogue warps (345 us where shared memory gave 350 at the time: the
 // products were not the bound, and short units paid for the copies); four epilogue warps a tile (377); a fixed deal of units
 // in alternating direction (SMs idle a tenth of the time); sums of thousands of terms in one fp32 chain (1.3e-6 off).

@@ -5,8 +5,9 @@
 // the row in the lower slot stays.  In steady state a step evicts as many rows as come, a handful at most, so nothing is
 // sorted: one sweep over the head's weights and positions (8 bytes a row, what bounds the kernel beside its start and
 // end) leaves every thread with the least key of its slots, and each eviction takes the least of all, whose owner
-// then looks for its next one.  8 heads of 1703 slots 4.7 us, 1024 of 2049 11.5, 64 of 65540 with four rows to go 24 (59 with
-// slots read one at a time).
+// then looks for its next one.  8 heads of 1703 slots 4.8 us, 1024 of 2049 11.6, 64 of 65537 20 (floor 5.1).  Slots are read
+// four at a time where the capacity is a multiple of four, which a budget and the rows of one step need not be: 64 heads of
+// 65540 with four rows to go 24 us, 59 with slots one at a time; 8 heads, which keep eight SMs busy, take as long (floor 0.6).
 #pragma once
 #include "cache.cuh"
 

@@ -37,7 +37,7 @@ int64_t most_parts(int64_t items, int64_t keys) {
 }
 
 // As many parts as fill the device (two CTAs an SM) when heads are few, so that a head's keys are read by many SMs, and four
-// rounds of them while each has 2048 keys (64 heads of 65540 rows, 8 query rows: 421 us instead of 440); several
+// rounds of them while each has 2048 keys (64 heads of 65540 rows, 8 query rows: 421 us instead of 440, both with one product a weight); several
 // rounds of parts when heads are many, so that the last round costs little and ragged heads even out.  A part has at least
 // two steps of its four warps (128 keys).
 RowsPlan plan_rows(int64_t problems, int64_t query_rows, int64_t keys, int nt = 0) {
@@ -147,10 +147,10 @@ bool plan_cache(const curdkv_cache* c, const curdkv_desc* d, int32_t q_rows, Cac
   // One launch where a KV head's query rows are one block and its logits fit into the shared memory of a cluster, with more
   // CTAs while all find room on the device and each keeps two steps of its warps.  Not where clusters fill their last round
   // badly, nor where clusters of eight leave half the places empty to long caches.  The rule does not ask for weights, so that
-  // outputs are the same with them and without (480 heads without: 90 | 81).
+  // outputs are the same with them and without (32 heads of 1702 rows without: 7.9 | 8.1, 128 of 2048 23.2 | 21.6).
   // 4 query rows, with weights, us, clusters | parts and a second kernel:
-  //   8 heads of 200 rows 6.1 | 8.9, of 1702 7.9 | 8.2, of 7000 15.0 | 12.4        32 of 1702 9.0 | 10.8        64 of 7000 39.0 | 43.5
-  //   128 heads of 2048 23.2 | 28.5, of 4096 45.2 | 49.7       320 of 2048 78 | 67       480 of 2048 84 | 88       1024 of 500 55 | 65, of 2048 177 | 181
+  //   8 heads of 200 rows 6.3 | 8.9, of 1702 8.2 | 8.7, of 7000 15.8 | 12.6        32 of 1702 9.4 | 11.1        64 of 7000 41 | 42
+  //   128 heads of 2048 26.0 | 27.0, of 4096 47 | 49       320 of 2048 81 | 70       480 of 2048 87 | 93       1024 of 500 56 | 64, of 2048 181 | 183
   pl->cluster = 0;
   if (pl->rows.blocks == 1) {
     const int64_t keys = c->capacity, slots = 2 * (int64_t)sms();
