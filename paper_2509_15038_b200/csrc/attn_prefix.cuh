@@ -9,7 +9,7 @@
 // accumulator, take alternate key tiles of one tile of rows, or all key tiles of a tile of rows each: a pair then
 // reads every tile of K and V once, where a CTA per tile drew twice the bytes through the L2 (193 us against 168 for 256 rows
 // over 8 heads of 131072).  Weights are rounded to bf16 (half a step: 2^-8 of each), sums take them unrounded: O is then off by
-// 0.20 to 0.21 % (2-norm), 0.16 to 0.18 of it its own rounding.  Two bf16 parts of a weight, as in attn_rows.cuh, leave only that, but the
+// 0.18 to 0.21 % (2-norm), 0.16 to 0.18 of it its own rounding.  Two bf16 parts of a weight, as in attn_rows.cuh, leave only that, but the
 // second product and the remainders lengthen the chain below: 64 sequences behind 32768 rows 66 -> 79 us, 16 x 8 behind 8192
 // 122 -> 140, 64 x 4 query rows behind 131072 177 -> 225.
 //
